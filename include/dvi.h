@@ -330,6 +330,97 @@ dvi_status dvi_linear(dvi_ctx* ctx, const void* d_w, int n_out, int k_in,
 dvi_status dvi_linear_noalloc(int dtype, const void* d_w, int n_out, int k_in, const float* d_x,
                               int m_rows, float* d_y, dvi_stream stream);
 
+/* ---------------------------------------------------------------- paged 8-bit KV cache
+ * Keys and values in pages of 8-bit codes with an f32 scale for each page
+ * and KV head (value = code * scale), for programs that serve many sequences
+ * of changing length.  The calls need no context: the caller owns the page
+ * pool, the page tables and the lengths, all on the device, and every call
+ * only enqueues work on `stream` (a graph may capture them).  A call's rows
+ * of sequence b take the positions lens[b], lens[b] + 1, ..., so one pass is
+ * dvi_paged_append, then dvi_paged_attend with the same batch; the caller
+ * then advances lens by the rows it keeps.  Lowering a length rolls rows back.
+ *
+ * Pointers and row strides (in bytes) are multiples of 16.  Errors found on
+ * the device set DVI_DEV_* bits of `status` (a device int32 the caller zeroes
+ * and reads, or null). */
+typedef enum { DVI_KV_INT8 = 0, DVI_KV_E4M3 = 1 } dvi_kv_format;
+
+typedef struct {
+  int n_pages;
+  int n_kv_heads;       /* H_kv */
+  int page_tokens;      /* P: 16, 32, 64 or 128 */
+  int head_dim;         /* 64 or 128 */
+  int format;           /* dvi_kv_format */
+  void* k;              /* codes [n_pages][H_kv][P][head_dim]: int8, or e4m3 bytes */
+  void* v;
+  float* k_scale;       /* [n_pages][H_kv], positive where the page is in use */
+  float* v_scale;
+} dvi_paged_cache;
+
+typedef struct {
+  int n_seqs;                 /* 1..1024 */
+  int max_pages;              /* columns of the page table */
+  int n_rows;                 /* rows of the call, all sequences together */
+  int max_rows;               /* no sequence has more (more are dropped: DVI_DEV_KV_FULL) */
+  const int32_t* table;       /* [n_seqs][max_pages] pages of each sequence, in order; a negative entry is a
+                                 page that is not held: its positions are not attended to (an entry past
+                                 n_pages counts as one, DVI_DEV_KV_FULL) */
+  const int32_t* lens;        /* [n_seqs] positions before the call's rows */
+  const int32_t* row_start;   /* [n_seqs + 1] first row of each sequence, or null: n_rows / n_seqs each */
+  int32_t* status;
+} dvi_paged_batch;
+
+/* Append n_rows rows of keys and values: k, v [n_rows][H_kv][head_dim] with
+ * ld_k, ld_v elements from row to row (a slice of a projection's output).
+ * rotary: [n_pos][rot_dim / 2] pairs (cos, sin) by which dims d and
+ * d + rot_dim / 2 of the keys (d < rot_dim / 2; rot_dim a multiple of 16) are
+ * rotated at their position, or null.  q (or null): the call's queries
+ * [n_rows][n_heads][head_dim], rotated alike into q_out (which may be q).
+ * dtype (dvi_dtype) is that of k, v, q and q_out; the arithmetic is f32.
+ *
+ * A page's scale is the largest magnitude it has held since its first row was
+ * written, over 127 (int8) or 448 (e4m3), at least 2^-80; when it grows, the
+ * page's earlier codes are rounded again to the new scale.  NaN is stored as
+ * 0 and an infinity as the largest code (DVI_DEV_NONFINITE), rows whose page
+ * is not held are dropped (DVI_DEV_KV_FULL), positions past the rotary table
+ * are not rotated (DVI_DEV_KV_FULL).  No two sequences of a call may append
+ * to the same page. */
+dvi_status dvi_paged_append(const dvi_paged_cache* cache, const dvi_paged_batch* batch, int dtype, const void* d_k,
+                            int64_t ld_k, const void* d_v, int64_t ld_v, const float* d_rotary, int rot_dim,
+                            int n_pos, const void* d_q, int64_t ld_q, void* d_q_out, int64_t ld_q_out, int n_heads,
+                            dvi_stream stream);
+
+/* Options of dvi_paged_attend: score = scale (q . k), then softcap * tanh(score
+ * / softcap) where softcap > 0, then + slopes[head] * (p_key - p_row) where
+ * slopes (device f32 [n_heads]) is given.  A row at position p sees the held
+ * positions up to p, and with window > 0 only those past p - window. */
+typedef struct {
+  int n_heads;          /* a multiple of H_kv: heads h G .. h G + G - 1 read KV head h */
+  float scale;
+  float softcap;
+  int window;
+  const float* slopes;
+} dvi_paged_options;
+
+/* Attention of the call's rows, already appended: q, o [n_rows][n_heads]
+ * [head_dim] with ld_q, ld_o elements from row to row, in dtype.  Scores,
+ * softmax and sums are f32.  A row that sees nothing gets zeros.  workspace:
+ * dvi_paged_workspace_bytes, 256-byte aligned, zeroed once before its first
+ * use; calls that may overlap need one each. */
+dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_paged_batch* batch,
+                            const dvi_paged_options* options, int dtype, const void* d_q, int64_t ld_q, void* d_o,
+                            int64_t ld_o, void* workspace, size_t workspace_bytes, dvi_stream stream);
+
+/* Bytes of workspace that dvi_paged_attend needs on the current device for
+ * any batch of this head_dim; 0 for one that it does not take. */
+size_t dvi_paged_workspace_bytes(int head_dim);
+
+/* Cached rows as values, in dtype: positions lens[b] .. of each sequence (the
+ * batch's rows) to k_out, v_out [n_rows][H_kv][head_dim].  Rows of a page that
+ * is not held are zeros. */
+dvi_status dvi_paged_read(const dvi_paged_cache* cache, const dvi_paged_batch* batch, int dtype, void* d_k_out,
+                          void* d_v_out, dvi_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -5,3 +5,4 @@ ctypes binding and `build` compiles it in-tree with nvcc.
 """
 from .dvi import (DVIEngine, DeviceWeights, DVIError, lib, update_config, LIB_PATH, EXPORTS,  # noqa: F401
                   DVI_F32, DVI_BF16)
+from .paged import PagedCache, rotary_table  # noqa: F401

@@ -1,0 +1,196 @@
+// The 8-bit paged KV cache: what its kernels share.
+//
+// Codes lie in pages [n_pages][H_kv][P][D] (int8, or e4m3 bytes), one f32
+// scale for each page and KV head: value = code * scale.  Sequence b's
+// position p is row p % P of page table[b][p / P]; a negative entry is a page
+// that is not held.  A call's rows of sequence b take the positions lens[b],
+// lens[b] + 1, ...
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace dvi {
+
+constexpr int kPagedMaxSeqs = 1024;
+constexpr float kPagedMinScale = 8.271806125530277e-25f;   // 2^-80
+
+struct PagedArgs {
+  uint8_t* k; uint8_t* v;
+  float* k_scale; float* v_scale;
+  const int* table; const int* lens; const int* row_start;
+  int* status;
+  int n_pages, H, P, log_p, D;
+  int n_seqs, max_pages, n_rows, max_rows;
+};
+
+struct PagedAppendArgs {
+  PagedArgs c;
+  const void* kin; const void* vin; const void* q; void* q_out;
+  long long ld_k, ld_v, ld_q, ld_qo;     // elements from row to row
+  const float2* rotary;                   // [n_pos][rot / 2] (cos, sin); null: no rotation
+  int rot, n_pos, n_heads, dtype;
+};
+
+struct PagedReadArgs {
+  PagedArgs c;
+  void* k_out; void* v_out;
+  int dtype;
+};
+
+struct PagedAttendArgs {
+  PagedArgs c;
+  const void* q; void* o;
+  long long ld_q, ld_o;
+  const float* slopes;                    // [n_heads] or null
+  int n_heads, G, dtype;
+  float scale, softcap;
+  int window;                             // 0: none
+  int min_vectors, max_vectors;           // sequences with rows * G in this range are this launch's
+  float* part;                            // partial results, then the counters
+  int* counters;
+};
+
+cudaError_t launch_paged_append(const PagedAppendArgs& a, bool e4m3, cudaStream_t s);
+cudaError_t launch_paged_read(const PagedReadArgs& a, bool e4m3, cudaStream_t s);
+template <bool E4M3> cudaError_t launch_paged_attend(const PagedAttendArgs& a, int n_sms, cudaStream_t s);
+
+// Workspace of the attention: a counter for each team of warps, zero between
+// calls, then two partial results of at most 32 vectors for each team.
+constexpr int kPagedTeams = 4;   // most teams per SM
+inline size_t paged_attend_counter_bytes(int n_sms) {
+  return (static_cast<size_t>(n_sms) * kPagedTeams * sizeof(int) + 255) / 256 * 256;
+}
+inline size_t paged_attend_part_bytes(int head_dim, int n_sms) {
+  return static_cast<size_t>(n_sms) * kPagedTeams * 2 * 32 * (head_dim + 2) * sizeof(float);
+}
+
+// ---------------------------------------------------------------- rows of a sequence
+struct PagedSeq {
+  int len;      // positions before the call's rows
+  int row0;     // first row
+  int n;        // rows
+};
+// Out-of-range row_start entries are cut to the call's rows, and a negative
+// length counts as 0, so that no index leaves its buffer; both are flagged.
+__device__ __forceinline__ PagedSeq paged_seq(const PagedArgs& c, int b) {
+  PagedSeq s;
+  s.len = c.lens[b];
+  int r1;
+  if (c.row_start) {
+    s.row0 = c.row_start[b];
+    r1 = c.row_start[b + 1];
+  } else {
+    const int per = c.n_rows / c.n_seqs;
+    s.row0 = b * per;
+    r1 = s.row0 + per;
+  }
+  s.n = r1 - s.row0;
+  const long long cap = static_cast<long long>(c.max_pages) << c.log_p;
+  if (s.len < 0 || s.row0 < 0 || s.n < 0 || r1 > c.n_rows || s.n > c.max_rows ||
+      static_cast<long long>(s.len) + s.n > cap) {
+    flag_status(c.status, DVI_DEV_KV_FULL);
+    s.len = max(s.len, 0);
+    s.row0 = min(max(s.row0, 0), c.n_rows);
+    s.n = min(min(max(s.n, 0), c.max_rows), c.n_rows - s.row0);
+    // positions stay below 2^31 (the host refuses capacities above 2^30)
+    s.len = static_cast<int>(min(static_cast<long long>(s.len), cap));
+  }
+  return s;
+}
+// The page of a table slot, or -1 where none is held.
+__device__ __forceinline__ int paged_page(const PagedArgs& c, int b, int slot) {
+  if (slot >= c.max_pages) return -1;
+  const int p = __ldg(c.table + static_cast<size_t>(b) * c.max_pages + slot);
+  if (p >= c.n_pages) {
+    flag_status(c.status, DVI_DEV_KV_FULL);
+    return -1;
+  }
+  return p;
+}
+
+// Work items of ragged sequences on a flat grid: sequence b owns the items
+// from row_start[b] / unit + extra * b on, and has at most
+// (n_b - 1) / unit + 1 + (extra - 1) of them, so no two sequences overlap.
+// Every thread of the block calls it with the same item; -1: nobody's.
+__device__ __forceinline__ int paged_seq_of_item(const PagedArgs& c, int item, int unit, int extra, int* first) {
+  int n = 0;
+  for (int b0 = 0; b0 < c.n_seqs; b0 += blockDim.x) {
+    const int b = b0 + static_cast<int>(threadIdx.x);
+    int begin = 0x7fffffff;
+    if (b < c.n_seqs) {
+      const int r0 = c.row_start ? c.row_start[b] : b * (c.n_rows / c.n_seqs);
+      begin = min(max(r0, 0), c.n_rows) / unit + extra * b;
+    }
+    n += __syncthreads_count(begin <= item);
+  }
+  const int b = n - 1;
+  if (b >= 0) {
+    const int r0 = c.row_start ? c.row_start[b] : b * (c.n_rows / c.n_seqs);
+    *first = min(max(r0, 0), c.n_rows) / unit + extra * b;
+  }
+  return b;
+}
+
+// ---------------------------------------------------------------- codes
+template <bool E4M3> struct Code;
+template <> struct Code<false> {
+  static constexpr float kTop = 127.f;
+  static __device__ __forceinline__ uint32_t enc(float x) {   // finite or infinite, not NaN
+    return static_cast<uint32_t>(__float2int_rn(fminf(fmaxf(x, -127.f), 127.f))) & 0xffu;
+  }
+  static __device__ __forceinline__ uint32_t enc4(float a, float b, float c, float d) {
+    return enc(a) | (enc(b) << 8) | (enc(c) << 16) | (enc(d) << 24);
+  }
+  static __device__ __forceinline__ void dec4(uint32_t w, float (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = static_cast<float>(static_cast<int8_t>(w >> (8 * i)));
+  }
+};
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 h;\n\tcvt.u16.u32 h, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(two));
+  return r;
+}
+template <> struct Code<true> {
+  static constexpr float kTop = 448.f;
+  static __device__ __forceinline__ uint32_t enc2(float lo, float hi) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 h;\n\tcvt.rn.satfinite.e4m3x2.f32 h, %2, %1;\n\tcvt.u32.u16 %0, h;\n\t}"
+        : "=r"(r)
+        : "f"(lo), "f"(hi));
+    return r;
+  }
+  static __device__ __forceinline__ uint32_t enc4(float a, float b, float c, float d) {
+    return enc2(a, b) | (enc2(c, d) << 16);
+  }
+  static __device__ __forceinline__ void dec4(uint32_t w, float (&x)[4]) {
+    const uint32_t lo = e4m3x2_to_f16x2(w), hi = e4m3x2_to_f16x2(w >> 16);
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo));
+    const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+    x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;
+  }
+};
+
+// Eight consecutive elements as f32.
+__device__ __forceinline__ void ld8(const float* p, float (&x)[8]) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+}
+__device__ __forceinline__ void ld8(const __nv_bfloat16* p, float (&x)[8]) {
+  const uint4 a = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[2 * i] = bf16_lo(w[i]), x[2 * i + 1] = bf16_hi(w[i]);
+}
+__device__ __forceinline__ void st8(float* p, const float (&x)[8]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ void st8(__nv_bfloat16* p, const float (&x)[8]) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
+                                            pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+}
+
+}  // namespace dvi

@@ -1,0 +1,166 @@
+// C entry points of the 8-bit paged KV cache: argument checks and launches.
+#include <mutex>
+
+#include "paged.cuh"
+
+namespace {
+
+using namespace dvi;
+
+// Multiprocessors of the current device, looked up once per device.
+int current_sms() {
+  constexpr int kMaxDevices = 64;
+  static std::atomic<int> sms[kMaxDevices];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return 0;
+  int n = dev < kMaxDevices ? sms[dev].load(std::memory_order_relaxed) : 0;
+  if (n == 0) {
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    if (dev < kMaxDevices) sms[dev].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool ld_ok(int64_t ld, int64_t least, int esz) { return ld >= least && (ld * esz) % 16 == 0; }
+
+// DVI_OK, or what is wrong with the cache and the batch.
+dvi_status check(const dvi_paged_cache* c, const dvi_paged_batch* b, int dtype, PagedArgs* out) {
+  if (!c || !b || (dtype != DVI_F32 && dtype != DVI_BF16)) return DVI_ERR_INVALID_ARG;
+  const int P = c->page_tokens;
+  if (c->n_pages < 1 || c->n_kv_heads < 1 || c->n_kv_heads > 1024 || (P != 16 && P != 32 && P != 64 && P != 128) ||
+      (c->head_dim != 64 && c->head_dim != 128) || (c->format != DVI_KV_INT8 && c->format != DVI_KV_E4M3))
+    return DVI_ERR_INVALID_ARG;
+  if (!c->k || !c->v || !c->k_scale || !c->v_scale || !on16(c->k) || !on16(c->v) || !on16(c->k_scale) ||
+      !on16(c->v_scale))
+    return DVI_ERR_INVALID_ARG;
+  if (b->n_seqs < 1 || b->max_pages < 1 || b->n_rows < 0 || b->max_rows < 0 || !b->table || !b->lens)
+    return DVI_ERR_INVALID_ARG;
+  if (!b->row_start && b->n_rows % b->n_seqs) return DVI_ERR_INVALID_ARG;
+  if (!b->row_start && b->max_rows < b->n_rows / b->n_seqs) return DVI_ERR_INVALID_ARG;
+  // positions and row counts are 32-bit numbers on the device
+  if (b->n_seqs > kPagedMaxSeqs || static_cast<int64_t>(b->max_pages) * P > (1ll << 30) || b->n_rows > (1 << 30))
+    return DVI_ERR_CAPACITY;
+  PagedArgs a{};
+  a.k = static_cast<uint8_t*>(c->k);
+  a.v = static_cast<uint8_t*>(c->v);
+  a.k_scale = c->k_scale;
+  a.v_scale = c->v_scale;
+  a.table = b->table;
+  a.lens = b->lens;
+  a.row_start = b->row_start;
+  a.status = b->status;
+  a.n_pages = c->n_pages;
+  a.H = c->n_kv_heads;
+  a.P = P;
+  a.log_p = P == 16 ? 4 : P == 32 ? 5 : P == 64 ? 6 : 7;
+  a.D = c->head_dim;
+  a.n_seqs = b->n_seqs;
+  a.max_pages = b->max_pages;
+  a.n_rows = b->n_rows;
+  a.max_rows = b->max_rows < b->n_rows ? b->max_rows : b->n_rows;
+  *out = a;
+  return DVI_OK;
+}
+
+dvi_status launched(cudaError_t e) { return e == cudaSuccess ? DVI_OK : DVI_ERR_CUDA; }
+
+}  // namespace
+
+extern "C" dvi_status dvi_paged_append(const dvi_paged_cache* cache, const dvi_paged_batch* batch, int dtype,
+                                       const void* d_k, int64_t ld_k, const void* d_v, int64_t ld_v,
+                                       const float* d_rotary, int rot_dim, int n_pos, const void* d_q, int64_t ld_q,
+                                       void* d_q_out, int64_t ld_q_out, int n_heads, dvi_stream stream) {
+  PagedAppendArgs a{};
+  const dvi_status rc = check(cache, batch, dtype, &a.c);
+  if (rc != DVI_OK) return rc;
+  if (a.c.n_rows == 0 || a.c.max_rows == 0) return DVI_OK;
+  const int esz = dtype == DVI_F32 ? 4 : 2;
+  const int64_t kv = static_cast<int64_t>(a.c.H) * a.c.D;
+  if (!d_k || !d_v || !on16(d_k) || !on16(d_v) || !ld_ok(ld_k, kv, esz) || !ld_ok(ld_v, kv, esz))
+    return DVI_ERR_INVALID_ARG;
+  if (d_rotary && (rot_dim < 16 || rot_dim > a.c.D || rot_dim % 16 || n_pos < 1 || !on16(d_rotary)))
+    return DVI_ERR_INVALID_ARG;
+  if (d_q) {
+    const int64_t least = static_cast<int64_t>(n_heads) * a.c.D;
+    if (n_heads < 1 || n_heads > (1 << 16) || !d_q_out || !on16(d_q) || !on16(d_q_out) || !ld_ok(ld_q, least, esz) ||
+        !ld_ok(ld_q_out, least, esz))
+      return DVI_ERR_INVALID_ARG;
+  }
+  a.kin = d_k;
+  a.vin = d_v;
+  a.ld_k = ld_k;
+  a.ld_v = ld_v;
+  a.rotary = reinterpret_cast<const float2*>(d_rotary);
+  a.rot = d_rotary ? rot_dim : 0;
+  a.n_pos = n_pos;
+  a.q = d_q;
+  a.q_out = d_q_out;
+  a.ld_q = ld_q;
+  a.ld_qo = ld_q_out;
+  a.n_heads = n_heads;
+  a.dtype = dtype;
+  cudaGetLastError();   // an error left pending by the caller is not this call's
+  return launched(launch_paged_append(a, cache->format == DVI_KV_E4M3, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+extern "C" dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_paged_batch* batch,
+                                       const dvi_paged_options* options, int dtype, const void* d_q, int64_t ld_q,
+                                       void* d_o, int64_t ld_o, void* workspace, size_t workspace_bytes,
+                                       dvi_stream stream) {
+  PagedAttendArgs a{};
+  const dvi_status rc = check(cache, batch, dtype, &a.c);
+  if (rc != DVI_OK) return rc;
+  const int esz = dtype == DVI_F32 ? 4 : 2;
+  if (!options || options->n_heads < 1 || options->n_heads > (1 << 16) || options->n_heads % a.c.H ||
+      !(options->scale > 0.f) || !(options->scale < 1e30f) || !(options->softcap >= 0.f) ||
+      !(options->softcap < 1e30f) || options->window < 0)
+    return DVI_ERR_INVALID_ARG;
+  if (a.c.n_rows == 0 || a.c.max_rows == 0) return DVI_OK;
+  const int64_t least = static_cast<int64_t>(options->n_heads) * a.c.D;
+  if (!d_q || !d_o || !on16(d_q) || !on16(d_o) || !ld_ok(ld_q, least, esz) || !ld_ok(ld_o, least, esz))
+    return DVI_ERR_INVALID_ARG;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return DVI_ERR_INVALID_ARG;
+  const int sms = current_sms();
+  if (sms <= 0) return DVI_ERR_CUDA;
+  if (workspace_bytes < dvi_paged_workspace_bytes(a.c.D)) return DVI_ERR_CAPACITY;
+  a.q = d_q;
+  a.o = d_o;
+  a.ld_q = ld_q;
+  a.ld_o = ld_o;
+  a.slopes = options->slopes;
+  a.n_heads = options->n_heads;
+  a.G = options->n_heads / a.c.H;
+  a.dtype = dtype;
+  a.scale = options->scale;
+  a.softcap = options->softcap;
+  a.window = options->window;
+  a.min_vectors = 1;
+  a.max_vectors = 0x7fffffff;
+  a.counters = static_cast<int*>(workspace);
+  a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + paged_attend_counter_bytes(sms));
+  cudaGetLastError();
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  return launched(cache->format == DVI_KV_E4M3 ? launch_paged_attend<true>(a, sms, st)
+                                               : launch_paged_attend<false>(a, sms, st));
+}
+
+extern "C" size_t dvi_paged_workspace_bytes(int head_dim) {
+  const int sms = current_sms();
+  if ((head_dim != 64 && head_dim != 128) || sms <= 0) return 0;
+  return paged_attend_counter_bytes(sms) + paged_attend_part_bytes(head_dim, sms);
+}
+
+extern "C" dvi_status dvi_paged_read(const dvi_paged_cache* cache, const dvi_paged_batch* batch, int dtype,
+                                     void* d_k_out, void* d_v_out, dvi_stream stream) {
+  PagedReadArgs a{};
+  const dvi_status rc = check(cache, batch, dtype, &a.c);
+  if (rc != DVI_OK) return rc;
+  if (a.c.n_rows == 0 || a.c.max_rows == 0) return DVI_OK;
+  if (!d_k_out || !d_v_out || !on16(d_k_out) || !on16(d_v_out)) return DVI_ERR_INVALID_ARG;
+  a.k_out = d_k_out;
+  a.v_out = d_v_out;
+  a.dtype = dtype;
+  cudaGetLastError();
+  return launched(launch_paged_read(a, cache->format == DVI_KV_E4M3, reinterpret_cast<cudaStream_t>(stream)));
+}

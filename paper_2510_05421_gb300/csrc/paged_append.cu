@@ -1,0 +1,331 @@
+// Rows into the 8-bit paged cache, and rows of it back as values.
+//
+// Append: k' = rot(k, p) in f32 (products and sums rounded one by one), then
+// for each (page, KV head) that the call's rows touch
+//   s = max(max |x| * (1 / Q), 2^-80)      Q = 127 (int8) or 448 (e4m3)
+//   s = max(s, s_old)                      where earlier rows lie in the page
+//   code = sat(rne(x * (1 / s)))
+// and where s > s_old the earlier rows become rne(code * (s_old / s)).  A
+// rolled-back row leaves its share in s, never in a value.  NaN is stored as
+// 0 and an infinity as the largest code (both flagged), so that no cached
+// value can reach another row through a probability of 0.
+//
+// A team of 32 to 256 threads owns one page of one head of K or of V: its
+// rows are loaded and rotated once, 16 elements a thread (8 and their 8
+// rotation partners), and wait in registers for the page's maximum.  Bound:
+// bytes (the rows in, half or a quarter of them out); single tokens: latency.
+#include <algorithm>
+
+#include "paged.cuh"
+
+namespace dvi {
+
+namespace {
+
+constexpr int kApThreads = 256;
+constexpr int kApItems = 4;            // 16-element items a thread holds
+constexpr int kApQSteps = 2;           // 32-item steps of a query warp
+
+template <typename T>
+__device__ __forceinline__ void rotate8(float (&a)[8], float (&b)[8], const float2* cs) {
+  float4 w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = __ldg(reinterpret_cast<const float4*>(cs) + i);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float co = i & 1 ? w[i >> 1].z : w[i >> 1].x, si = i & 1 ? w[i >> 1].w : w[i >> 1].y;
+    const float x = __fsub_rn(__fmul_rn(a[i], co), __fmul_rn(b[i], si));
+    const float y = __fadd_rn(__fmul_rn(b[i], co), __fmul_rn(a[i], si));
+    a[i] = x;
+    b[i] = y;
+  }
+}
+
+// Element offsets of item j of a row: 8 elements and their 8 partners (the
+// rotated dims first, then the others in the same halves).
+__device__ __forceinline__ void item_dims(int j, int rot, int D, int& a, int& b) {
+  if (8 * j < rot / 2) {
+    a = 8 * j;
+    b = a + rot / 2;
+  } else {
+    a = rot + 8 * j - rot / 2;
+    b = a + (D - rot) / 2;
+  }
+}
+
+template <int TEAM>
+__device__ __forceinline__ float team_max(float v, float* red, int team, int t) {
+  v = warp_max(v);
+  if (TEAM == 32) return v;
+  const int w = t >> 5;
+  if ((t & 31) == 0) red[team * (TEAM / 32) + w] = v;
+  named_bar(1 + team, TEAM);
+#pragma unroll
+  for (int i = 0; i < TEAM / 32; ++i) v = fmaxf(v, red[team * (TEAM / 32) + i]);
+  return v;
+}
+
+template <bool E4M3, int D, typename T, int TEAM>
+__device__ void append_page(const PagedAppendArgs& a, int item, int group) {
+  __shared__ float red[kApThreads / 32];
+  const PagedArgs& c = a.c;
+  int first = 0;
+  const int b = paged_seq_of_item(c, item, c.P, 2, &first);
+  if (b < 0) return;
+  const PagedSeq sq = paged_seq(c, b);
+  const int slot = (sq.len >> c.log_p) + item - first;
+  const int page0 = slot << c.log_p;                              // position of the page's row 0
+  const int p0 = max(sq.len, page0), p1 = min(sq.len + sq.n, page0 + c.P);
+  const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM;
+  const int task = group * (kApThreads / TEAM) + team;
+  if (p0 >= p1 || task >= 2 * c.H) return;                        // uniform over a team
+  const int page = paged_page(c, b, slot);
+  if (page < 0) {
+    if (t == 0) flag_status(c.status, DVI_DEV_KV_FULL);
+    return;
+  }
+  const bool is_v = task >= c.H;
+  const int h = is_v ? task - c.H : task;
+  const size_t ph = static_cast<size_t>(page) * c.H + h;
+  float* sp = (is_v ? c.v_scale : c.k_scale) + ph;
+  uint8_t* codes = (is_v ? c.v : c.k) + (ph << c.log_p) * D;
+  const int held = p0 - page0;
+  const float old = held > 0 ? *sp : 0.f;
+  const T* in = static_cast<const T*>(is_v ? a.vin : a.kin) + h * D;
+  const long long ld = is_v ? a.ld_v : a.ld_k;
+  const int rot = is_v ? 0 : a.rot;
+  constexpr int kPer = D / 16;                                    // items of a row
+  const int n_items = (p1 - p0) * kPer;
+  float x[kApItems][16];
+  float most = 0.f;
+  bool odd = false;
+#pragma unroll
+  for (int u = 0; u < kApItems; ++u) {
+    const int it = u * TEAM + t;
+    if (it >= n_items) continue;
+    const int r = it / kPer, j = it % kPer;
+    int da, db;
+    item_dims(j, rot, D, da, db);
+    const T* row = in + static_cast<long long>(sq.row0 + p0 - sq.len + r) * ld;
+    float lo[8], hi[8];
+    ld8(row + da, lo);
+    ld8(row + db, hi);
+    if (8 * j < rot / 2) {
+      const int pos = p0 + r;
+      if (pos < a.n_pos) rotate8<T>(lo, hi, a.rotary + static_cast<size_t>(pos) * (rot / 2) + 8 * j);
+      else if (j == 0) flag_status(c.status, DVI_DEV_KV_FULL);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      float v = i < 8 ? lo[i & 7] : hi[i & 7];
+      if (v != v) v = 0.f, odd = true;
+      const float m = fabsf(v);
+      if (m <= 3.402823466e38f) most = fmaxf(most, m);
+      else odd = true;
+      x[u][i] = v;
+    }
+  }
+  if (odd) flag_status(c.status, DVI_DEV_NONFINITE);
+  most = team_max<TEAM>(most, red, team, t);
+  float s = fmaxf(__fmul_rn(most, 1.f / Code<E4M3>::kTop), kPagedMinScale);
+  if (held > 0) s = fmaxf(s, old);
+  __syncwarp();   // the team has read the old scale (a larger team: by its barrier)
+  if (t == 0) *sp = s;
+  const float inv = __fdiv_rn(1.f, s);
+#pragma unroll
+  for (int u = 0; u < kApItems; ++u) {
+    const int it = u * TEAM + t;
+    if (it >= n_items) continue;
+    const int r = it / kPer, j = it % kPer;
+    int da, db;
+    item_dims(j, rot, D, da, db);
+    uint8_t* row = codes + static_cast<size_t>(held + r) * D;
+    float y[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = __fmul_rn(x[u][i], inv);
+    using C = Code<E4M3>;
+    *reinterpret_cast<uint2*>(row + da) = make_uint2(C::enc4(y[0], y[1], y[2], y[3]), C::enc4(y[4], y[5], y[6], y[7]));
+    *reinterpret_cast<uint2*>(row + db) =
+        make_uint2(C::enc4(y[8], y[9], y[10], y[11]), C::enc4(y[12], y[13], y[14], y[15]));
+  }
+  if (held > 0 && s > old) {
+    const float f = __fdiv_rn(old, s);
+    uint4* w = reinterpret_cast<uint4*>(codes);
+    for (int i = t; i < held * kPer; i += TEAM) {
+      const uint4 q = w[i];
+      const uint32_t in4[4] = {q.x, q.y, q.z, q.w};
+      uint32_t out4[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float v[4];
+        Code<E4M3>::dec4(in4[e], v);
+        out4[e] = Code<E4M3>::enc4(__fmul_rn(v[0], f), __fmul_rn(v[1], f), __fmul_rn(v[2], f), __fmul_rn(v[3], f));
+      }
+      w[i] = make_uint4(out4[0], out4[1], out4[2], out4[3]);
+    }
+  }
+}
+
+// Queries: a warp takes one row and kApQSteps * 32 items of its heads.
+template <int D, typename T>
+__device__ void rotate_queries(const PagedAppendArgs& a, int warp_task, int parts) {
+  const PagedArgs& c = a.c;
+  const int lane = threadIdx.x & 31;
+  const int r = warp_task / parts, part = warp_task % parts;
+  if (r >= c.n_rows) return;
+  int b;
+  if (c.row_start) {
+    int n = 0;
+    for (int b0 = 0; b0 < c.n_seqs; b0 += 32) {
+      const int e = b0 + lane;
+      n += __popc(__ballot_sync(0xffffffffu, e < c.n_seqs && c.row_start[e] <= r));
+    }
+    b = n - 1;
+  } else {
+    b = r / (c.n_rows / c.n_seqs);
+  }
+  if (b < 0) return;
+  const PagedSeq sq = paged_seq(c, b);
+  const int i = r - sq.row0;
+  if (i < 0 || i >= sq.n) return;
+  const int pos = sq.len + i;
+  constexpr int kPer = D / 16;
+  const int total = a.n_heads * kPer;
+#pragma unroll
+  for (int u = 0; u < kApQSteps; ++u) {
+    const int it = (part * kApQSteps + u) * 32 + lane;
+    if (it >= total) continue;
+    const int h = it / kPer, j = it % kPer;
+    int da, db;
+    item_dims(j, a.rot, D, da, db);
+    const T* row = static_cast<const T*>(a.q) + static_cast<long long>(r) * a.ld_q + h * D;
+    T* out = static_cast<T*>(a.q_out) + static_cast<long long>(r) * a.ld_qo + h * D;
+    float lo[8], hi[8];
+    ld8(row + da, lo);
+    ld8(row + db, hi);
+    if (8 * j < a.rot / 2 && pos < a.n_pos)
+      rotate8<T>(lo, hi, a.rotary + static_cast<size_t>(pos) * (a.rot / 2) + 8 * j);
+    st8(out + da, lo);
+    st8(out + db, hi);
+  }
+}
+
+template <bool E4M3, int D, typename T, int TEAM>
+__global__ void __launch_bounds__(kApThreads) paged_append_kernel(const __grid_constant__ PagedAppendArgs a,
+                                                                  int n_items, int groups, int parts) {
+  griddep_wait();
+  griddep_launch();
+  const int bid = static_cast<int>(blockIdx.x);
+  const int pages = n_items * groups;
+  if (bid < pages) append_page<E4M3, D, T, TEAM>(a, bid / groups, bid % groups);
+  else rotate_queries<D, T>(a, (bid - pages) * (kApThreads / 32) + static_cast<int>(threadIdx.x >> 5), parts);
+}
+
+template <bool E4M3, int D, typename T, int TEAM>
+cudaError_t launch_append(const PagedAppendArgs& a, cudaStream_t s) {
+  const PagedArgs& c = a.c;
+  const long long n_items = static_cast<long long>(c.n_rows >> c.log_p) + 2ll * c.n_seqs;
+  const int teams = kApThreads / TEAM, groups = (2 * c.H + teams - 1) / teams;
+  const int parts = a.q ? (a.n_heads * (D / 16) + 32 * kApQSteps - 1) / (32 * kApQSteps) : 0;
+  const long long q_blocks = (static_cast<long long>(c.n_rows) * parts + kApThreads / 32 - 1) / (kApThreads / 32);
+  const long long blocks = n_items * groups + q_blocks;
+  if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+  return launch_pdl(paged_append_kernel<E4M3, D, T, TEAM>, dim3(static_cast<unsigned>(blocks)), dim3(kApThreads), 0, s,
+                    a, static_cast<int>(n_items), groups, parts);
+}
+// A team holds kApItems items a thread: the rows of one page, as far as one
+// sequence's rows go.
+template <bool E4M3, int D, typename T>
+cudaError_t append_teams(const PagedAppendArgs& a, cudaStream_t s) {
+  const int items = std::min(a.c.P, a.c.max_rows) * (D / 16);
+  if (items <= 32 * kApItems) return launch_append<E4M3, D, T, 32>(a, s);
+  if (items <= 128 * kApItems) return launch_append<E4M3, D, T, 128>(a, s);
+  return launch_append<E4M3, D, T, 256>(a, s);
+}
+template <bool E4M3>
+cudaError_t append_types(const PagedAppendArgs& a, cudaStream_t s) {
+  if (a.dtype == DVI_BF16)
+    return a.c.D == 128 ? append_teams<E4M3, 128, __nv_bfloat16>(a, s) : append_teams<E4M3, 64, __nv_bfloat16>(a, s);
+  return a.c.D == 128 ? append_teams<E4M3, 128, float>(a, s) : append_teams<E4M3, 64, float>(a, s);
+}
+
+// ---------------------------------------------------------------- read
+// A block takes one page slot of one sequence and kRdWarps (head, K or V)
+// pairs: a warp copies the slot's rows, 16 codes a lane and step.
+constexpr int kRdWarps = 8;
+
+template <bool E4M3, int D, typename T>
+__global__ void __launch_bounds__(kRdWarps * 32) paged_read_kernel(const __grid_constant__ PagedReadArgs a, int groups) {
+  griddep_wait();
+  griddep_launch();
+  const PagedArgs& c = a.c;
+  const int item = static_cast<int>(blockIdx.x) / groups, group = static_cast<int>(blockIdx.x) % groups;
+  int first = 0;
+  const int b = paged_seq_of_item(c, item, c.P, 2, &first);
+  if (b < 0) return;
+  const PagedSeq sq = paged_seq(c, b);
+  const int slot = (sq.len >> c.log_p) + item - first;
+  const int page0 = slot << c.log_p;
+  const int p0 = max(sq.len, page0), p1 = min(sq.len + sq.n, page0 + c.P);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int task = group * kRdWarps + warp;
+  if (p0 >= p1 || task >= 2 * c.H) return;
+  const bool is_v = task >= c.H;
+  const int h = is_v ? task - c.H : task;
+  const int page = paged_page(c, b, slot);
+  const size_t ph = static_cast<size_t>(max(page, 0)) * c.H + h;
+  const float s = page < 0 ? 0.f : (is_v ? c.v_scale : c.k_scale)[ph];
+  constexpr int kPer = D / 16;
+  const uint4* codes =
+      reinterpret_cast<const uint4*>((is_v ? c.v : c.k) + ((ph << c.log_p) + static_cast<size_t>(p0 - page0)) * D);
+  T* out = static_cast<T*>(is_v ? a.v_out : a.k_out);
+  const size_t row0 = static_cast<size_t>(sq.row0 + p0 - sq.len);
+  const int n = (p1 - p0) * kPer;
+#pragma unroll 4
+  for (int i = lane; i < n; i += 32) {
+    const uint4 q = page < 0 ? make_uint4(0u, 0u, 0u, 0u) : __ldg(codes + i);
+    const int r = i / kPer, j = i % kPer;
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    float x[16];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float v[4];
+      Code<E4M3>::dec4(w[e], v);
+#pragma unroll
+      for (int f = 0; f < 4; ++f) x[4 * e + f] = __fmul_rn(v[f], s);
+    }
+    T* dst = out + ((row0 + r) * c.H + h) * D + 16 * j;
+    float lo[8], hi[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) lo[e] = x[e], hi[e] = x[8 + e];
+    st8(dst, lo);
+    st8(dst + 8, hi);
+  }
+}
+
+template <bool E4M3, int D, typename T>
+cudaError_t launch_read(const PagedReadArgs& a, cudaStream_t s) {
+  const PagedArgs& c = a.c;
+  const int groups = (2 * c.H + kRdWarps - 1) / kRdWarps;
+  const long long blocks = (static_cast<long long>(c.n_rows >> c.log_p) + 2ll * c.n_seqs) * groups;
+  if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+  return launch_pdl(paged_read_kernel<E4M3, D, T>, dim3(static_cast<unsigned>(blocks)), dim3(kRdWarps * 32), 0, s, a,
+                    groups);
+}
+template <bool E4M3>
+cudaError_t read_types(const PagedReadArgs& a, cudaStream_t s) {
+  if (a.dtype == DVI_BF16)
+    return a.c.D == 128 ? launch_read<E4M3, 128, __nv_bfloat16>(a, s) : launch_read<E4M3, 64, __nv_bfloat16>(a, s);
+  return a.c.D == 128 ? launch_read<E4M3, 128, float>(a, s) : launch_read<E4M3, 64, float>(a, s);
+}
+
+}  // namespace
+
+cudaError_t launch_paged_append(const PagedAppendArgs& a, bool e4m3, cudaStream_t s) {
+  return e4m3 ? append_types<true>(a, s) : append_types<false>(a, s);
+}
+cudaError_t launch_paged_read(const PagedReadArgs& a, bool e4m3, cudaStream_t s) {
+  return e4m3 ? read_types<true>(a, s) : read_types<false>(a, s);
+}
+
+}  // namespace dvi

@@ -1,0 +1,662 @@
+// Attention of few rows over the 8-bit paged cache: decode rows and verify
+// blocks (any number of rows is right; prompt chunks have a kernel of their
+// own).
+//
+//   s_ij = (q_i . c_j) scale ks      s = cap tanh(s / cap)      s += slope (p_j - p_i)
+//   o_i  = sum_j w_ij c_j / sum_j (w_ij / vs)       w_ij = 2^(s_ij log2 e + log2 vs - m_i)
+// over the held positions p_i - window < p_j <= p_i.  Folding vs into the
+// exponent keeps w in f16's range whatever the scales are, and the codes
+// enter both products as they are (int8 and e4m3 values are exact in f16).
+//
+// The query vectors of one KV head (rows x its G query heads, 8 NT to a tile)
+// are the columns of both products (warp MMAs, K and V as the row operand):
+// the 16 x 16 K fragment takes 4 consecutive codes of a key per thread and
+// step, any order of the dims being one, and the V fragment 16 consecutive
+// codes of a key; the codes are loaded 16 bytes at a time and go to f16 in
+// registers (1.25 to 1.5 instructions a code).
+//
+// Work: blocks of 16 positions.  The blocks of all (sequence, KV head, tile)
+// groups lie in one row and every team of 4 to 16 warps takes an equal share of
+// it, so ragged batches fill the GPU evenly; a group cut by shares is joined
+// by whichever of its teams ends last, in the order of the shares (the result
+// does not depend on which that is).  Inside a team the warps take blocks in
+// turn, each with its own running maximum and a private ring of cp.async
+// stages, and are joined in shared memory at the end of the group.
+//
+// f32 queries (PAIR) enter as an f16 pair hi + lo, as do their probabilities.
+// A query vector is scaled by a power of two so that f16's range does not
+// matter.
+#pragma once
+
+#include <algorithm>
+
+#include "paged.cuh"
+
+namespace dvi {
+
+namespace {
+
+constexpr int kPaKeys = 16;               // positions per block: never more than a page
+constexpr int kPaTeam = 4;                // warps of the smallest team
+constexpr float kPaLazy = 8.f;            // growth of a maximum (base 2) that rescales the accumulator
+constexpr float kPaUp = 5.f;              // weights are at most 2^(kPaLazy + kPaUp): f16 keeps small ones exact
+constexpr float kPaLog2e = 1.4426950408889634f;
+
+template <int HD, int NT, bool PAIR>
+struct PaShape {
+  // sixteen warps where their registers allow it (128 a thread)
+  static constexpr int kWarps = NT * (PAIR ? 2 : 1) <= 2 ? 16 : 8;
+  static constexpr int kThreads = kWarps * 32;
+  static constexpr int kTeams = kWarps / kPaTeam;            // most teams of a CTA
+  static constexpr int kHalf = kPaKeys * HD;                 // K (or V) codes of a block
+  static constexpr int kStage = 2 * kHalf;
+  static constexpr int kStages = (HD == 128 ? 3 : 6) * (16 / kWarps) - (kWarps == 8 ? 1 : 0);
+  static constexpr int kScales = (kStages * 8 + 15) / 16 * 16;
+  static constexpr int kRing = kWarps * kStages * kStage;
+  static constexpr int kQ = NT * HD * 16 * (PAIR ? 2 : 1);   // query fragments of a team
+  static constexpr int kVec = NT * 8 * 16;                   // per vector: factor, slope, position, -
+  static constexpr int kQAt = kRing;
+  static constexpr int kVecAt = kQAt + kTeams * kQ;
+  static constexpr int kScaleAt = kVecAt + kTeams * kVec;
+  static constexpr int kUnitsAt = kScaleAt + kWarps * kScales;
+  // a warp's partial result (8 NT rows of HD sums, a maximum and a sum each) lies in its ring
+  static_assert(NT * 8 * (HD + 2) * 4 <= kStages * kStage, "partial results");
+  static_assert(kTeams <= kPagedTeams, "the workspace");
+  static_assert(kUnitsAt + 4 * (kPagedMaxSeqs + 1) + 512 <= 232448, "shared memory");
+};
+
+__device__ __forceinline__ float pa_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float pa_lg2(float x) {
+  float y;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t n) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, uint32_t n) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ uint4 lds16(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds8(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                              uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void split_f16x2(float a, float b, uint32_t& hi, uint32_t& lo) {
+  const __half2 h = __floats2half2_rn(a, b);
+  const float2 f = __half22float2(h);
+  hi = *reinterpret_cast<const uint32_t*>(&h);
+  lo = pack_f16x2(a - f.x, b - f.y);
+}
+__device__ __forceinline__ uint32_t hsub2_1152(uint32_t x) {
+  const uint32_t c = 0x64806480u;   // 1152, 1152
+  const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&c));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// Codes 0, 1 and 2, 3 of a word as two f16 pairs.  int8: the byte with its sign
+// bit turned is code + 128, and 0x6400 | byte is the f16 number 1024 + byte.
+template <bool E4M3>
+__device__ __forceinline__ void codes_f16(uint32_t w, uint32_t& a, uint32_t& b) {
+  if (E4M3) {
+    a = e4m3x2_to_f16x2(w & 0xffffu);
+    b = e4m3x2_to_f16x2(w >> 16);
+  } else {
+    const uint32_t u = w ^ 0x80808080u;
+    a = hsub2_1152(__byte_perm(u, 0x64646464u, 0x4140));
+    b = hsub2_1152(__byte_perm(u, 0x64646464u, 0x4342));
+  }
+}
+
+// Byte offset of 16-byte chunk `ch` of row `r` (0..31) in a block's K or V
+// codes.  Chunks are permuted so that the fragment loads of both products
+// (8 lanes: two rows by four chunks, or four rows two apart by two chunks)
+// and the row-wise copies meet no bank twice.
+template <int HD>
+__device__ __forceinline__ uint32_t pa_chunk(int r, int ch) {
+  if (HD == 128) return r * 128u + ((ch ^ ((((r ^ (r >> 2)) & 1) << 2) | (r & 2))) << 4);
+  return (r >> 1) * 128u + (((r ^ (r >> 1)) & 1) << 6) + ((ch ^ (((r >> 2) & 1) << 1)) << 4);
+}
+
+}  // namespace
+
+template <bool E4M3, int HD, int NT, bool PAIR>
+__global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
+    paged_attend_kernel(const __grid_constant__ PagedAttendArgs a) {
+  using SH = PaShape<HD, NT, PAIR>;
+  constexpr int NV = 8 * NT;                 // vectors per tile
+  constexpr int kSteps = HD / 16;            // k-steps of the scores, and 16-dim tiles of the output
+  constexpr int kParts = PAIR ? 2 : 1;
+  constexpr int W = SH::kWarps, ST = SH::kStages;
+  extern __shared__ __align__(128) uint8_t sm[];
+  const PagedArgs& c = a.c;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  uint8_t* ring = sm + warp * ST * SH::kStage;
+  const uint32_t ring_s = smem_u32(ring);
+  float* scl = reinterpret_cast<float*>(sm + SH::kScaleAt + warp * SH::kScales);
+  const uint32_t scl_s = smem_u32(scl);
+  int* units = reinterpret_cast<int*>(sm + SH::kUnitsAt);               // [n_seqs + 1] blocks before a sequence
+  __shared__ int scan_s[2][W];
+  __shared__ int last_s[SH::kTeams];
+
+  griddep_wait();
+  griddep_launch();
+
+  // ---------------- the row of blocks
+  // Blocks [first, first + n) of sequence b that any of its rows sees, its tiles.
+  auto extent = [&](const PagedSeq& s, int& first, int& tiles) {
+    const long long vecs = static_cast<long long>(s.n) * a.G;
+    if (s.n <= 0 || vecs < a.min_vectors || vecs > a.max_vectors) {
+      first = tiles = 0;
+      return 0;
+    }
+    const int end = min(s.len + s.n, c.max_pages << c.log_p);
+    first = (a.window > 0 ? max(0, s.len - a.window + 1) : 0) / kPaKeys;
+    tiles = static_cast<int>((vecs + NV - 1) / NV);
+    return max(1, (end + kPaKeys - 1) / kPaKeys - first);   // at least one, so that empty rows are written
+  };
+  int total = 0, groups = 0;
+  for (int b0 = 0; b0 < c.n_seqs; b0 += SH::kThreads) {
+    const int b = b0 + tid;
+    int n = 0, ng = 0;
+    if (b < c.n_seqs) {
+      int first, tiles;
+      const int blocks = extent(paged_seq(c, b), first, tiles);
+      ng = tiles * c.H;
+      n = blocks * ng;
+    }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, n, o), y = __shfl_up_sync(0xffffffffu, ng, o);
+      if (lane >= o) n += x, ng += y;
+    }
+    if (b0 > 0) __syncthreads();
+    if (lane == 31) scan_s[0][warp] = n, scan_s[1][warp] = ng;
+    __syncthreads();
+    int before = total;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      if (w < warp) before += scan_s[0][w];
+      total += scan_s[0][w];
+      groups += scan_s[1][w];
+    }
+    if (b < c.n_seqs) units[b + 1] = before + n;
+  }
+  if (tid == 0) units[0] = 0;
+  __syncthreads();
+  if (total == 0) return;
+
+  // ---------------- teams and shares
+  const int per_group = total / max(1, groups);
+  const int S = per_group >= 8 * W ? W : per_group >= 4 * W ? W / 2 : kPaTeam;
+  const int tw = warp % S, in_cta = warp / S;
+  // (a share is at least a block for each warp; few shares spread over the CTAs)
+  const int n_teams = min(static_cast<int>(gridDim.x) * (W / S), (total + S - 1) / S);
+  const int team = in_cta * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x);
+  if (team >= n_teams) return;
+  auto share = [&](int k) { return static_cast<int>(static_cast<long long>(total) * k / n_teams); };
+  auto team_of = [&](int unit) { return static_cast<int>((static_cast<long long>(unit + 1) * n_teams - 1) / total); };
+  const int u_begin = share(team), u_end = share(team + 1);
+  auto team_bar = [&] { named_bar(1 + in_cta, 32 * S); };
+  const int G = a.G;
+  uint8_t* qf = sm + SH::kQAt + in_cta * SH::kQ;
+  const uint32_t q_s = smem_u32(qf);
+  float4* vec = reinterpret_cast<float4*>(sm + SH::kVecAt + in_cta * SH::kVec);
+
+  int u = u_begin;
+  int b = 0;
+  while (u < u_end) {
+    // ---------------- the group of block u
+    {
+      int lo = b, hi = c.n_seqs - 1;
+      while (lo < hi) {                       // the last b with units[b] <= u
+        const int mid = (lo + hi + 1) >> 1;
+        if (units[mid] <= u) lo = mid;
+        else hi = mid - 1;
+      }
+      b = lo;
+    }
+    const PagedSeq sq = paged_seq(c, b);
+    int first, tiles;
+    const int n_blocks = extent(sq, first, tiles);
+    const int grp = (u - units[b]) / n_blocks;
+    const int g_begin = units[b] + grp * n_blocks, g_end = g_begin + n_blocks;
+    const int blk0 = u - g_begin, blk1 = min(u_end, g_end) - g_begin;
+    const int h = grp / tiles, tile = grp - h * tiles;
+    const int n0 = tile * NV;                                      // first vector
+    const int n_vec = min(NV, sq.n * G - n0);
+    const int row_lo = n0 / G, row_hi = (n0 + n_vec - 1) / G;      // rows of the tile
+    // positions that some row of the tile sees
+    const int cap = c.max_pages << c.log_p;
+    const int see_end = min(sq.len + row_hi + 1, cap);
+    const int see_begin = a.window > 0 ? max(0, sq.len + row_lo - a.window + 1) : 0;
+    const int held_end = min(sq.len + sq.n, cap);                  // rows of the cache past it are nobody's
+    const int s0 = max(first + blk0, see_begin / kPaKeys), s1 = min(first + blk1, (see_end + kPaKeys - 1) / kPaKeys);
+
+    // ---------------- queries: a warp loads whole vectors, HD / 32 dims a lane
+    constexpr int kDims = HD / 32;
+    constexpr int kMine = NV / kPaTeam;                            // most vectors of a warp
+    float qx[kMine][kDims];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+#pragma unroll
+      for (int e = 0; e < kDims; ++e) qx[i][e] = 0.f;
+      const int n = tw + i * S;
+      if (n < n_vec) {
+        const int row = (n0 + n) / G, hq = h * G + (n0 + n) - row * G;
+        const long long off = static_cast<long long>(sq.row0 + row) * a.ld_q + hq * HD + lane * kDims;
+        if (a.dtype == DVI_BF16) {
+          const uint32_t* p = reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(a.q) + off);
+#pragma unroll
+          for (int e = 0; e < kDims / 2; ++e) qx[i][2 * e] = bf16_lo(p[e]), qx[i][2 * e + 1] = bf16_hi(p[e]);
+        } else {
+          const float2* p = reinterpret_cast<const float2*>(static_cast<const float*>(a.q) + off);
+#pragma unroll
+          for (int e = 0; e < kDims / 2; ++e) qx[i][2 * e] = p[e].x, qx[i][2 * e + 1] = p[e].y;
+        }
+      }
+    }
+
+    // ---------------- copies of a block; its page is looked up one step ahead
+    const uint8_t* kh = c.k + ((static_cast<size_t>(h) << c.log_p) * HD);
+    const uint8_t* vh = c.v + ((static_cast<size_t>(h) << c.log_p) * HD);
+    const size_t page_bytes = (static_cast<size_t>(c.H) << c.log_p) * HD;
+    constexpr int kRow = HD / 16;                                  // 16-byte chunks of a row
+    constexpr int kRows = 32 / kRow;                               // rows a warp copies at once
+    const int ch = lane % kRow, r0 = lane / kRow;
+    auto entry = [&](int blk) { return blk < s1 ? paged_page(c, b, (blk * kPaKeys) >> c.log_p) : -1; };
+    auto issue = [&](int blk, int stage, int pg) {
+      if (blk < s1) {
+        const uint32_t dst = ring_s + stage * SH::kStage;
+        const int p = blk * kPaKeys;
+        const size_t off = static_cast<size_t>(max(pg, 0)) * page_bytes +
+                           static_cast<size_t>(((p & (c.P - 1)) + r0) * HD + ch * 16);
+        const int live = pg >= 0 ? held_end - p - r0 : 0;          // rows r0 + r, r < live, are somebody's
+#pragma unroll
+        for (int r = 0; r < kPaKeys; r += kRows) {
+          const uint32_t n = r < live ? 16u : 0u;
+          const uint32_t at = pa_chunk<HD>(r + r0, ch);
+          cp_async16(dst + at, kh + off + r * HD, n);
+          cp_async16(dst + SH::kHalf + at, vh + off + r * HD, n);
+        }
+        if (lane < 2) {
+          const float* sp = (lane & 1 ? c.v_scale : c.k_scale) + static_cast<size_t>(max(pg, 0)) * c.H + h;
+          cp_async4(scl_s + stage * 8 + lane * 4, sp, pg >= 0 ? 4u : 0u);
+        }
+      }
+      cp_commit();
+    };
+    int nxt;
+    {
+      int pg[ST - 1];
+#pragma unroll
+      for (int i = 0; i < ST - 1; ++i) pg[i] = entry(s0 + tw + i * S);
+      nxt = entry(s0 + tw + (ST - 1) * S);
+#pragma unroll
+      for (int i = 0; i < ST - 1; ++i) issue(s0 + tw + i * S, i, pg[i]);
+    }
+
+    // ---------------- query fragments: thread (g, t) of vector 8 nt + g holds, for
+    // step j, dims 16 t + 4 j .. + 3 (hd 128: from step 4 on 64 + 16 t + 4 (j - 4))
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int n = tw + i * S;
+      if (n >= NV) continue;
+      float top = 0.f;
+#pragma unroll
+      for (int e = 0; e < kDims; ++e) top = fmaxf(top, fabsf(qx[i][e]));
+      top = warp_max(top);
+      // a power of two brings the largest element to [2^14, 2^15)
+      const int ex = max(static_cast<int>(__float_as_uint(top) >> 23), 15);
+      const float up = __uint_as_float(static_cast<uint32_t>(268 - ex) << 23);
+      const float down = __uint_as_float(static_cast<uint32_t>(ex - 14) << 23);
+      const int d = lane * kDims;
+      uint8_t* at = qf + (((n >> 3) * kSteps + (d / 64) * 4 + (d % 16) / 4) * 32 + (n & 7) * 4 + (d % 64) / 16) * 8 +
+                    (d % 4) * 2;
+#pragma unroll
+      for (int e = 0; e < kDims; e += 2) {
+        uint32_t hi, lo;
+        split_f16x2(qx[i][e] * up, qx[i][e + 1] * up, hi, lo);
+        *reinterpret_cast<uint32_t*>(at + e * 2) = hi;
+        if (PAIR) *reinterpret_cast<uint32_t*>(at + NT * kSteps * 256 + e * 2) = lo;
+      }
+      if (lane == 0) {
+        const int row = (n0 + n) / G, hq = h * G + (n0 + n) - row * G;
+        const bool live = n < n_vec;
+        const float f = a.softcap > 0.f ? down * (a.scale / a.softcap) : down * (a.scale * kPaLog2e);
+        vec[n] = make_float4(f, live && a.slopes ? __ldg(a.slopes + hq) * kPaLog2e : 0.f,
+                             __int_as_float(live ? sq.len + row : -1), 0.f);
+      }
+    }
+    team_bar();
+
+    float o[kSteps][NT][4];
+    float m[NT][2], l[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[i][nt][e] = 0.f;
+      m[nt][0] = m[nt][1] = -INFINITY;
+      l[nt][0] = l[nt][1] = 0.f;
+    }
+
+    int stage = 0;
+#pragma unroll 1
+    for (int blk = s0 + tw; blk < s1; blk += S) {
+      {
+        // the stage that the last step read is free: its next block's copies
+        const int pg = nxt;
+        nxt = entry(blk + ST * S);
+        __syncwarp();
+        issue(blk + (ST - 1) * S, stage == 0 ? ST - 1 : stage - 1, pg);
+      }
+      cp_wait<ST - 1>();
+      __syncwarp();
+      const uint32_t ks_s = ring_s + stage * SH::kStage, vs_s = ks_s + SH::kHalf;
+      const float ks = scl[stage * 2], vs = scl[stage * 2 + 1];
+      // ---------------- scores
+      float s[NT][4];
+      {
+        uint32_t w0[kSteps], w1[kSteps];   // codes of keys g and g + 8
+#pragma unroll
+        for (int i = 0; i < HD / 64; ++i) {
+          const uint4 x = lds16(ks_s + pa_chunk<HD>(g, 4 * i + t));
+          const uint4 y = lds16(ks_s + pa_chunk<HD>(g + 8, 4 * i + t));
+          w0[4 * i] = x.x, w0[4 * i + 1] = x.y, w0[4 * i + 2] = x.z, w0[4 * i + 3] = x.w;
+          w1[4 * i] = y.x, w1[4 * i + 1] = y.y, w1[4 * i + 2] = y.z, w1[4 * i + 3] = y.w;
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[nt][e] = 0.f;
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) {
+          uint32_t a0, a1, a2, a3;
+          codes_f16<E4M3>(w0[j], a0, a2);
+          codes_f16<E4M3>(w1[j], a1, a3);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int part = 0; part < kParts; ++part) {
+              const uint2 q = lds8(q_s + ((part * NT + nt) * kSteps + j) * 256 + lane * 8);
+              mma_f16_16816(s[nt], a0, a1, a2, a3, q.x, q.y);
+            }
+        }
+      }
+      // ---------------- softmax: element e of s[nt]: key g + 8 (e / 2), vector 8 nt + 2 t + e % 2
+      const int p_blk = blk * kPaKeys;
+      const bool plain = p_blk + kPaKeys - 1 <= sq.len + row_lo && vs > 0.f &&
+                         (a.window == 0 || p_blk > sq.len + row_hi - a.window);
+      const float vx = fmaxf(vs, kPagedMinScale), lv = pa_lg2(vx), iv = __frcp_rn(vx);
+      uint32_t pb[NT][2], pl[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const float4 va = vec[nt * 8 + 2 * t], vb = vec[nt * 8 + 2 * t + 1];
+        const float fa = va.x * ks, fb = vb.x * ks;
+        if (a.softcap > 0.f) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float x = s[nt][e] * (e & 1 ? fb : fa);
+            if (PAIR) x = tanhf(x);
+            else x = 1.f - __fdividef(2.f, 1.f + pa_ex2(x * (2.f * kPaLog2e)));
+            s[nt][e] = fmaf(a.softcap * kPaLog2e, x, lv);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[nt][e] = fmaf(s[nt][e], e & 1 ? fb : fa, lv);
+        }
+        if (a.slopes) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float4& v = e & 1 ? vb : va;
+            s[nt][e] = fmaf(v.y, static_cast<float>(p_blk + g + 8 * (e >> 1) - __float_as_int(v.z)), s[nt][e]);
+          }
+        }
+        if (!plain) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int d = p_blk + g + 8 * (e >> 1) - __float_as_int(e & 1 ? vb.z : va.z);
+            if (d > 0 || !(vs > 0.f) || (a.window > 0 && d <= -a.window)) s[nt][e] = -INFINITY;
+          }
+        }
+        const float top0 = fmaxf(s[nt][0], s[nt][2]), top1 = fmaxf(s[nt][1], s[nt][3]);
+        const bool grow = top0 > m[nt][0] + (kPaLazy + kPaUp) || top1 > m[nt][1] + (kPaLazy + kPaUp);
+        if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            float x = q ? top1 : top0;
+#pragma unroll
+            for (int off = 4; off < 32; off <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
+            x -= kPaUp;                                           // the reference sits below the maximum
+            const float f = x > m[nt][q] ? (m[nt][q] == -INFINITY ? 0.f : pa_ex2(m[nt][q] - x)) : 1.f;
+            m[nt][q] = fmaxf(m[nt][q], x);
+            l[nt][q] *= f;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) o[i][nt][q] *= f, o[i][nt][q + 2] *= f;
+          }
+        }
+        const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = pa_ex2(s[nt][e] - (e & 1 ? m1 : m0));
+        l[nt][0] = fmaf(p[0] + p[2], iv, l[nt][0]);
+        l[nt][1] = fmaf(p[1] + p[3], iv, l[nt][1]);
+        if (PAIR) {
+          uint32_t h0, h1, l0, l1;
+          split_f16x2(p[0], p[1], h0, l0);
+          split_f16x2(p[2], p[3], h1, l1);
+          pb[nt][0] = movmatrix_trans(h0), pb[nt][1] = movmatrix_trans(h1);
+          pl[nt][0] = movmatrix_trans(l0), pl[nt][1] = movmatrix_trans(l1);
+        } else {
+          pb[nt][0] = movmatrix_trans(pack_f16x2(p[0], p[1]));
+          pb[nt][1] = movmatrix_trans(pack_f16x2(p[2], p[3]));
+        }
+      }
+      // ---------------- values: keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9, HD / 8 dims from g HD / 8 on
+      {
+        constexpr int kW = HD / 32;                                // words of a thread's dims
+        uint32_t w[4][kW];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int r = 2 * t + (k & 1) + 8 * (k >> 1);
+          if (HD == 128) {
+            const uint4 x = lds16(vs_s + pa_chunk<HD>(r, g));
+            w[k][0] = x.x, w[k][1] = x.y, w[k][kW - 2] = x.z, w[k][kW - 1] = x.w;
+          } else {
+            const uint2 x = lds8(vs_s + pa_chunk<HD>(r, g >> 1) + (g & 1) * 8);
+            w[k][0] = x.x, w[k][1] = x.y;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+          const uint32_t sel = i & 1 ? 0x7362u : 0x5140u;          // dims 2 i and 2 i + 1 of two keys
+          uint32_t a0, a1, a2, a3;
+          codes_f16<E4M3>(__byte_perm(w[0][i >> 1], w[1][i >> 1], sel), a0, a1);
+          codes_f16<E4M3>(__byte_perm(w[2][i >> 1], w[3][i >> 1], sel), a2, a3);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            if (PAIR) {
+              // a fresh accumulator each step: the sum over thousands of steps rounds to nearest
+              float d[4] = {0.f, 0.f, 0.f, 0.f};
+              mma_f16_16816(d, a0, a1, a2, a3, pl[nt][0], pl[nt][1]);
+              mma_f16_16816(d, a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[i][nt][e] += d[e];
+            } else {
+              mma_f16_16816(o[i][nt], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+            }
+          }
+        }
+      }
+      stage = stage + 1 == ST ? 0 : stage + 1;
+    }
+    cp_wait<0>();
+    __syncwarp();
+
+    // ---------------- join: o[i][nt][e] is dim g HD/8 + 2 i + e / 2 of vector 8 nt + 2 t + e % 2
+    float* mine = reinterpret_cast<float*>(ring);                  // [NV][HD], maxima [NV], sums [NV]
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        float x = l[nt][q];
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
+        const int n = nt * 8 + 2 * t + q;
+        if (g == 0) {
+          mine[NV * HD + n] = m[nt][q];
+          mine[NV * HD + NV + n] = x;
+        }
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+          *reinterpret_cast<float2*>(mine + n * HD + g * (HD / 8) + 2 * i) = make_float2(o[i][nt][q], o[i][nt][q + 2]);
+      }
+    team_bar();
+    const bool whole = blk0 == 0 && blk1 == n_blocks;
+    constexpr int kSlot = NV * (HD + 2);
+    float* slot = a.part + static_cast<size_t>(2 * team + (u == u_begin ? 0 : 1)) * kSlot;
+    // Dims d .. d + 3 of vector v: the result, or this share's part of it.
+    auto emit = [&](int v, int d, float4 acc, float M, float L, bool final) {
+      if (final) {
+        if (v >= n_vec) return;
+        const float inv = L > 0.f ? 1.f / L : (L == L ? 0.f : L);
+        const int row = (n0 + v) / G, hq = h * G + (n0 + v) - row * G;
+        const long long off = static_cast<long long>(sq.row0 + row) * a.ld_o + hq * HD + d;
+        if (a.dtype == DVI_BF16)
+          *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + off) =
+              make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+        else
+          *reinterpret_cast<float4*>(static_cast<float*>(a.o) + off) =
+              make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+      } else {
+        __stcg(reinterpret_cast<float4*>(slot + v * HD + d), acc);
+        if (d == 0) {
+          __stcg(slot + NV * HD + v, M);
+          __stcg(slot + NV * HD + NV + v, L);
+        }
+      }
+    };
+    constexpr int kWarpFloats = ST * SH::kStage / 4;
+    const float* parts = reinterpret_cast<const float*>(sm) + in_cta * S * kWarpFloats;
+    for (int i = tw * 32 + lane; i < NV * HD / 4; i += S * 32) {
+      const int v = i / (HD / 4), d = (i % (HD / 4)) * 4;
+      float M = -INFINITY;
+      for (int w = 0; w < S; ++w) M = fmaxf(M, parts[w * kWarpFloats + NV * HD + v]);
+      const float mu = M == -INFINITY ? 0.f : M;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      float L = 0.f;
+#pragma unroll 4
+      for (int w = 0; w < S; ++w) {
+        const float* p = parts + w * kWarpFloats;
+        const float f = pa_ex2(p[NV * HD + v] - mu);
+        const float4 x = *reinterpret_cast<const float4*>(p + v * HD + d);
+        acc.x = fmaf(x.x, f, acc.x), acc.y = fmaf(x.y, f, acc.y);
+        acc.z = fmaf(x.z, f, acc.z), acc.w = fmaf(x.w, f, acc.w);
+        L = fmaf(p[NV * HD + NV + v], f, L);
+      }
+      emit(v, d, acc, M, L, whole);
+    }
+    if (!whole) {
+      // teams of the group: t0 .. t1; whoever of them counts last joins their parts in order
+      const int t0 = team_of(g_begin), t1 = team_of(g_end - 1);
+      __threadfence();
+      team_bar();
+      if (tw == 0 && lane == 0) {
+        const int n = atomicAdd(a.counters + t0, 1);
+        last_s[in_cta] = n == t1 - t0;
+        if (n == t1 - t0) a.counters[t0] = 0;
+        __threadfence();
+      }
+      team_bar();
+      if (last_s[in_cta]) {
+        const float* p0 = a.part + static_cast<size_t>(2 * t0 + (share(t0) == g_begin ? 0 : 1)) * kSlot;
+        const float* p1 = a.part + static_cast<size_t>(2 * t0 + 2) * kSlot;
+        const int n = t1 - t0 + 1;
+        for (int i = tw * 32 + lane; i < NV * HD / 4; i += S * 32) {
+          const int v = i / (HD / 4), d = (i % (HD / 4)) * 4;
+          float M = -INFINITY, L = 0.f;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+          for (int k = 0; k < n; ++k) {
+            const float* p = k == 0 ? p0 : p1 + static_cast<size_t>(2 * (k - 1)) * kSlot;
+            const float pm = __ldcg(p + NV * HD + v), ps = __ldcg(p + NV * HD + NV + v);
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(p + v * HD + d));
+            const float top = fmaxf(M, pm), mu = top == -INFINITY ? 0.f : top;
+            const float fa = pa_ex2(M - mu), fb = pa_ex2(pm - mu);
+            M = top;
+            acc.x = fmaf(x.x, fb, acc.x * fa), acc.y = fmaf(x.y, fb, acc.y * fa);
+            acc.z = fmaf(x.z, fb, acc.z * fa), acc.w = fmaf(x.w, fb, acc.w * fa);
+            L = fmaf(ps, fb, L * fa);
+          }
+          emit(v, d, acc, M, L, true);
+        }
+      }
+    }
+    team_bar();   // the rings and the queries are read before the next group's
+    u = g_begin + blk1;
+  }
+}
+
+namespace {
+template <bool E4M3, int HD, int NT, bool PAIR>
+cudaError_t launch_pa(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
+  using SH = PaShape<HD, NT, PAIR>;
+  // the blocks of all groups are counted in 32 bits
+  const long long tiles = static_cast<long long>(a.c.n_rows) * a.G / (8 * NT) + a.c.n_seqs;
+  const long long blocks = ((static_cast<long long>(a.c.max_pages) << a.c.log_p) / kPaKeys + 1) * a.c.H;
+  if (tiles * blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+  static PerDevice attr;
+  attr.once([] {
+    cudaFuncSetAttribute(paged_attend_kernel<E4M3, HD, NT, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                         SH::kUnitsAt + 4 * (kPagedMaxSeqs + 1));
+  });
+  return launch_pdl(paged_attend_kernel<E4M3, HD, NT, PAIR>, dim3(n_sms), dim3(SH::kThreads),
+                    SH::kUnitsAt + 4 * (a.c.n_seqs + 1), s, a);
+}
+template <bool E4M3, int HD>
+cudaError_t pa_tiles(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
+  const long long vecs = std::min<long long>(static_cast<long long>(a.c.max_rows) * a.G, a.max_vectors);
+  if (a.dtype == DVI_F32)
+    return vecs <= 8 ? launch_pa<E4M3, HD, 1, true>(a, n_sms, s) : launch_pa<E4M3, HD, 2, true>(a, n_sms, s);
+  if (vecs <= 8) return launch_pa<E4M3, HD, 1, false>(a, n_sms, s);
+  if (vecs <= 16) return launch_pa<E4M3, HD, 2, false>(a, n_sms, s);
+  return launch_pa<E4M3, HD, 4, false>(a, n_sms, s);
+}
+}  // namespace
+
+template <bool E4M3>
+cudaError_t launch_paged_attend(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
+  return a.c.D == 128 ? pa_tiles<E4M3, 128>(a, n_sms, s) : pa_tiles<E4M3, 64>(a, n_sms, s);
+}
+
+}  // namespace dvi

@@ -25,7 +25,8 @@ BUF = dict(LENS=0, PENDING=1, DRAFT_IDS=2, LOG_U=3, LOG_LOGITS=4, LOG_META=5, GR
            X_DRAFT=8, X_VERIFY=9, K_CACHE=10, V_CACHE=11, STATUS=12, GRAD_W=13, Z=14)
 EXPORTS = ["dvi_workspace_bytes", "dvi_create", "dvi_prefill", "dvi_draft_verify_commit", "dvi_log",
            "dvi_update_drafter", "dvi_ar_step", "dvi_get_stats", "dvi_last_error", "dvi_destroy",
-           "dvi_debug_buffer", "dvi_linear", "dvi_timing", "dvi_get_timing", "dvi_linear_noalloc"]
+           "dvi_debug_buffer", "dvi_linear", "dvi_timing", "dvi_get_timing", "dvi_linear_noalloc",
+           "dvi_paged_append", "dvi_paged_attend", "dvi_paged_read", "dvi_paged_workspace_bytes"]
 
 
 class ModelConfig(ctypes.Structure):
@@ -115,6 +116,15 @@ def lib() -> ctypes.CDLL:
         L.dvi_get_timing.argtypes = [vp, P(ctypes.c_double), P(i)]
         L.dvi_linear_noalloc.restype = i
         L.dvi_linear_noalloc.argtypes = [i, vp, i, i, vp, i, vp, vp]
+        ll, sz = ctypes.c_int64, ctypes.c_size_t
+        L.dvi_paged_append.restype = i
+        L.dvi_paged_append.argtypes = [vp, vp, i, vp, ll, vp, ll, vp, i, i, vp, ll, vp, ll, i, vp]
+        L.dvi_paged_attend.restype = i
+        L.dvi_paged_attend.argtypes = [vp, vp, vp, i, vp, ll, vp, ll, vp, sz, vp]
+        L.dvi_paged_read.restype = i
+        L.dvi_paged_read.argtypes = [vp, vp, i, vp, vp, vp]
+        L.dvi_paged_workspace_bytes.restype = sz
+        L.dvi_paged_workspace_bytes.argtypes = [i]
         _lib = L
     return _lib
 
