@@ -45,6 +45,7 @@ struct PagedAttendArgs {
   long long ld_q, ld_o;
   const float* slopes;                    // [n_heads] or null
   int n_heads, G, dtype;
+  uint32_t inv_g;                         // ceil(2^32 / G): n / G = n inv_g >> 32 for small n (G = 1: 0, not used)
   float scale, softcap;
   int window;                             // 0: none
   int min_vectors, max_vectors;           // sequences with rows * G in this range are this launch's
@@ -99,15 +100,19 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedArgs& c, int b) {
   }
   return s;
 }
-// The page of a table slot, or -1 where none is held.
+// A table entry as it lies there (a slot past the table: not held), and the
+// page it names, or -1 where none is held.  Apart, so that entries can be in
+// flight before the first of them is looked at.
+__device__ __forceinline__ int paged_entry(const PagedArgs& c, int b, int slot) {
+  return slot < c.max_pages ? __ldg(c.table + static_cast<size_t>(b) * c.max_pages + slot) : -1;
+}
+__device__ __forceinline__ int paged_valid(const PagedArgs& c, int entry) {
+  if (entry < c.n_pages) return max(entry, -1);
+  flag_status(c.status, DVI_DEV_KV_FULL);
+  return -1;
+}
 __device__ __forceinline__ int paged_page(const PagedArgs& c, int b, int slot) {
-  if (slot >= c.max_pages) return -1;
-  const int p = __ldg(c.table + static_cast<size_t>(b) * c.max_pages + slot);
-  if (p >= c.n_pages) {
-    flag_status(c.status, DVI_DEV_KV_FULL);
-    return -1;
-  }
-  return p;
+  return paged_valid(c, paged_entry(c, b, slot));
 }
 
 // Work items of ragged sequences on a flat grid: sequence b owns the items

@@ -131,6 +131,7 @@ extern "C" dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_p
   a.slopes = options->slopes;
   a.n_heads = options->n_heads;
   a.G = options->n_heads / a.c.H;
+  a.inv_g = a.G == 1 ? 0u : static_cast<uint32_t>(((1ull << 32) + a.G - 1) / a.G);
   a.dtype = dtype;
   a.scale = options->scale;
   a.softcap = options->softcap;

@@ -62,7 +62,7 @@ struct PaShape {
   // a warp's partial result (8 NT rows of HD sums, a maximum and a sum each) lies in its ring
   static_assert(NT * 8 * (HD + 2) * 4 <= kStages * kStage, "partial results");
   static_assert(kTeams <= kPagedTeams, "the workspace");
-  static_assert(kUnitsAt + 4 * (kPagedMaxSeqs + 1) + 512 <= 232448, "shared memory");
+  static_assert(kUnitsAt + 16 * (kPagedMaxSeqs + 1) + 512 <= 232448, "shared memory");
 };
 
 __device__ __forceinline__ float pa_ex2(float x) {
@@ -163,33 +163,40 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
   const uint32_t ring_s = smem_u32(ring);
   float* scl = reinterpret_cast<float*>(sm + SH::kScaleAt + warp * SH::kScales);
   const uint32_t scl_s = smem_u32(scl);
-  int* units = reinterpret_cast<int*>(sm + SH::kUnitsAt);               // [n_seqs + 1] blocks before a sequence
+  // per sequence b: [b] length, first row, units before it; [b + 1].w its rows
+  int4* seqs = reinterpret_cast<int4*>(sm + SH::kUnitsAt);
   __shared__ int scan_s[2][W];
   __shared__ int last_s[SH::kTeams];
 
   griddep_wait();
   griddep_launch();
 
-  // ---------------- the row of blocks
-  // Blocks [first, first + n) of sequence b that any of its rows sees, its tiles.
-  auto extent = [&](const PagedSeq& s, int& first, int& tiles) {
-    const long long vecs = static_cast<long long>(s.n) * a.G;
-    if (s.n <= 0 || vecs < a.min_vectors || vecs > a.max_vectors) {
-      first = tiles = 0;
-      return 0;
-    }
-    const int end = min(s.len + s.n, c.max_pages << c.log_p);
-    first = (a.window > 0 ? max(0, s.len - a.window + 1) : 0) / kPaKeys;
+  // ---------------- sequences
+  // Blocks [first, first + n) of a sequence that any of its rows sees, its tiles.
+  const int G = a.G;
+  auto extent = [&](int len, int rows, int& first, int& tiles) {
+    const long long vecs = static_cast<long long>(rows) * G;
+    first = tiles = 0;
+    if (rows <= 0 || vecs < a.min_vectors || vecs > a.max_vectors) return 0;
+    const int end = min(len + rows, c.max_pages << c.log_p);
+    if (a.window > 0) first = max(0, len - a.window + 1) / kPaKeys;
     tiles = static_cast<int>((vecs + NV - 1) / NV);
     return max(1, (end + kPaKeys - 1) / kPaKeys - first);   // at least one, so that empty rows are written
   };
-  int total = 0, groups = 0;
-  for (int b0 = 0; b0 < c.n_seqs; b0 += SH::kThreads) {
+  constexpr int kPasses = (kPagedMaxSeqs + SH::kThreads - 1) / SH::kThreads;
+  int blocks_all = 0, groups = 0;
+  int upto[kPasses];                          // groups up to and with this thread's sequences
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
+    const int b0 = i * SH::kThreads;
+    if (b0 >= c.n_seqs) break;
     const int b = b0 + tid;
     int n = 0, ng = 0;
+    PagedSeq sq{};
     if (b < c.n_seqs) {
       int first, tiles;
-      const int blocks = extent(paged_seq(c, b), first, tiles);
+      sq = paged_seq(c, b);
+      const int blocks = extent(sq.len, sq.n, first, tiles);
       ng = tiles * c.H;
       n = blocks * ng;
     }
@@ -201,59 +208,102 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     if (b0 > 0) __syncthreads();
     if (lane == 31) scan_s[0][warp] = n, scan_s[1][warp] = ng;
     __syncthreads();
-    int before = total;
+    int before = blocks_all, g_before = groups;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      if (w < warp) before += scan_s[0][w];
-      total += scan_s[0][w];
+      if (w < warp) before += scan_s[0][w], g_before += scan_s[1][w];
+      blocks_all += scan_s[0][w];
       groups += scan_s[1][w];
     }
-    if (b < c.n_seqs) units[b + 1] = before + n;
+    upto[i] = g_before + ng;
+    if (b < c.n_seqs) {
+      reinterpret_cast<int2*>(seqs + b)[0] = make_int2(sq.len, sq.row0);
+      reinterpret_cast<int2*>(seqs + b + 1)[1] = make_int2(before + n, sq.n);
+    }
   }
-  if (tid == 0) units[0] = 0;
-  __syncthreads();
-  if (total == 0) return;
+  if (groups == 0) return;
 
-  // ---------------- teams and shares
-  const int per_group = total / max(1, groups);
-  const int S = per_group >= 8 * W ? W : per_group >= 4 * W ? W / 2 : kPaTeam;
+  // ---------------- teams: a team's share is an equal part of a row of units, a
+  // group's being as many as its blocks and kOver = S more for what a group costs
+  // beside them (a step of each warp).  Groups of equal size are not cut across a
+  // share where each share holds one part.  16 warps on a group while that leaves
+  // each of them two steps and the shares fill the GPU about as well as smaller
+  // teams' would.
+  int S = kPaTeam, n_teams = 0;
+  {
+    const int per_group = blocks_all / groups;
+    int best = -1;
+#pragma unroll
+    for (int s = W; s >= kPaTeam; s >>= 1) {
+      if (s > kPaTeam && per_group < 2 * s) continue;
+      const int most = static_cast<int>(gridDim.x) * (W / s);
+      const int few = max(1, (blocks_all + groups * s) / (2 * s));     // a share is two steps at least
+      int n = min(most, few);
+      if (n >= groups) n = n / groups * groups;
+      const int fill = n >= groups ? (n == min(most, few) ? 100 : 100 * n / most) : 90;
+      if (best < 0 || fill > best + 6) best = fill, S = s, n_teams = n;
+    }
+  }
+  const int over = S;
+  const int total = blocks_all + groups * over;
   const int tw = warp % S, in_cta = warp / S;
-  // (a share is at least a block for each warp; few shares spread over the CTAs)
-  const int n_teams = min(static_cast<int>(gridDim.x) * (W / S), (total + S - 1) / S);
   const int team = in_cta * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x);
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
+    const int b = i * SH::kThreads + tid;
+    if (b < c.n_seqs) seqs[b + 1].z += upto[i] * over;
+  }
+  if (tid == 0) seqs[0].z = 0;
+  __syncthreads();
   if (team >= n_teams) return;
-  auto share = [&](int k) { return static_cast<int>(static_cast<long long>(total) * k / n_teams); };
-  auto team_of = [&](int unit) { return static_cast<int>((static_cast<long long>(unit + 1) * n_teams - 1) / total); };
+  const int share_q = total / n_teams, share_r = total - share_q * n_teams;
+  auto share = [&](int k) { return share_q * k + share_r * k / n_teams; };
+  auto team_of = [&](int unit) {
+    int k = min(n_teams - 1, static_cast<int>(static_cast<float>(unit) * (static_cast<float>(n_teams) / static_cast<float>(total))));
+    while (k > 0 && share(k) > unit) --k;
+    while (share(k + 1) <= unit) ++k;
+    return k;
+  };
   const int u_begin = share(team), u_end = share(team + 1);
   auto team_bar = [&] { named_bar(1 + in_cta, 32 * S); };
-  const int G = a.G;
   uint8_t* qf = sm + SH::kQAt + in_cta * SH::kQ;
   const uint32_t q_s = smem_u32(qf);
   float4* vec = reinterpret_cast<float4*>(sm + SH::kVecAt + in_cta * SH::kVec);
 
   int u = u_begin;
   int b = 0;
-  while (u < u_end) {
-    // ---------------- the group of block u
-    {
-      int lo = b, hi = c.n_seqs - 1;
-      while (lo < hi) {                       // the last b with units[b] <= u
-        const int mid = (lo + hi + 1) >> 1;
-        if (units[mid] <= u) lo = mid;
-        else hi = mid - 1;
-      }
-      b = lo;
+  {
+    int hi = c.n_seqs - 1;
+    while (b < hi) {                          // the last b whose units begin at or before u
+      const int mid = (b + hi + 1) >> 1;
+      if (seqs[mid].z <= u) b = mid;
+      else hi = mid - 1;
     }
-    const PagedSeq sq = paged_seq(c, b);
+  }
+  while (u < u_end) {
+    // ---------------- the group of unit u, and the share's part of it
+    while (b + 1 < c.n_seqs && seqs[b + 1].z <= u) ++b;
+    const int4 sq4 = seqs[b];
+    PagedSeq sq;
+    sq.len = sq4.x, sq.row0 = sq4.y;
+    sq.n = seqs[b + 1].w;
     int first, tiles;
-    const int n_blocks = extent(sq, first, tiles);
-    const int grp = (u - units[b]) / n_blocks;
-    const int g_begin = units[b] + grp * n_blocks, g_end = g_begin + n_blocks;
-    const int blk0 = u - g_begin, blk1 = min(u_end, g_end) - g_begin;
+    const int n_blocks = extent(sq.len, sq.n, first, tiles);
+    const int grp = (u - sq4.z) / (n_blocks + over);
+    const int g_begin = sq4.z + grp * (n_blocks + over) + over, g_end = g_begin + n_blocks;   // its blocks' units
+    const int blk0 = max(u - g_begin, 0), blk1 = min(u_end, g_end) - g_begin;
+    if (blk1 <= 0) break;                     // the share ends before the group's first block
+    u = g_end;
     const int h = grp / tiles, tile = grp - h * tiles;
     const int n0 = tile * NV;                                      // first vector
     const int n_vec = min(NV, sq.n * G - n0);
-    const int row_lo = n0 / G, row_hi = (n0 + n_vec - 1) / G;      // rows of the tile
+    const int row_lo = n0 / G, rest = n0 - row_lo * G;            // rows of the tile, and where the first begins
+    const int row_hi = row_lo + (rest + n_vec - 1) / G;
+    auto row_of = [&](int n, int& hq) {                            // vector n of the tile: its row, its head
+      const int r = G == 1 ? n : static_cast<int>(__umulhi(static_cast<uint32_t>(rest + n), a.inv_g));
+      hq = h * G + rest + n - r * G;
+      return row_lo + r;
+    };
     // positions that some row of the tile sees
     const int cap = c.max_pages << c.log_p;
     const int see_end = min(sq.len + row_hi + 1, cap);
@@ -271,7 +321,8 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
       for (int e = 0; e < kDims; ++e) qx[i][e] = 0.f;
       const int n = tw + i * S;
       if (n < n_vec) {
-        const int row = (n0 + n) / G, hq = h * G + (n0 + n) - row * G;
+        int hq;
+        const int row = row_of(n, hq);
         const long long off = static_cast<long long>(sq.row0 + row) * a.ld_q + hq * HD + lane * kDims;
         if (a.dtype == DVI_BF16) {
           const uint32_t* p = reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(a.q) + off);
@@ -292,9 +343,10 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     constexpr int kRow = HD / 16;                                  // 16-byte chunks of a row
     constexpr int kRows = 32 / kRow;                               // rows a warp copies at once
     const int ch = lane % kRow, r0 = lane / kRow;
-    auto entry = [&](int blk) { return blk < s1 ? paged_page(c, b, (blk * kPaKeys) >> c.log_p) : -1; };
-    auto issue = [&](int blk, int stage, int pg) {
+    auto entry = [&](int blk) { return blk < s1 ? paged_entry(c, b, (blk * kPaKeys) >> c.log_p) : -1; };
+    auto issue = [&](int blk, int stage, int raw) {
       if (blk < s1) {
+        const int pg = paged_valid(c, raw);
         const uint32_t dst = ring_s + stage * SH::kStage;
         const int p = blk * kPaKeys;
         const size_t off = static_cast<size_t>(max(pg, 0)) * page_bytes +
@@ -349,7 +401,8 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
         if (PAIR) *reinterpret_cast<uint32_t*>(at + NT * kSteps * 256 + e * 2) = lo;
       }
       if (lane == 0) {
-        const int row = (n0 + n) / G, hq = h * G + (n0 + n) - row * G;
+        int hq;
+        const int row = row_of(n, hq);
         const bool live = n < n_vec;
         const float f = a.softcap > 0.f ? down * (a.scale / a.softcap) : down * (a.scale * kPaLog2e);
         vec[n] = make_float4(f, live && a.slopes ? __ldg(a.slopes + hq) * kPaLog2e : 0.f,
@@ -375,10 +428,10 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     for (int blk = s0 + tw; blk < s1; blk += S) {
       {
         // the stage that the last step read is free: its next block's copies
-        const int pg = nxt;
+        const int raw = nxt;
         nxt = entry(blk + ST * S);
         __syncwarp();
-        issue(blk + (ST - 1) * S, stage == 0 ? ST - 1 : stage - 1, pg);
+        issue(blk + (ST - 1) * S, stage == 0 ? ST - 1 : stage - 1, raw);
       }
       cp_wait<ST - 1>();
       __syncwarp();
@@ -417,7 +470,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
       const int p_blk = blk * kPaKeys;
       const bool plain = p_blk + kPaKeys - 1 <= sq.len + row_lo && vs > 0.f &&
                          (a.window == 0 || p_blk > sq.len + row_hi - a.window);
-      const float vx = fmaxf(vs, kPagedMinScale), lv = pa_lg2(vx), iv = __frcp_rn(vx);
+      const float vx = fmaxf(vs, kPagedMinScale), lv = pa_lg2(vx), iv = __fdividef(1.f, vx);
       uint32_t pb[NT][2], pl[NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -544,13 +597,15 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     team_bar();
     const bool whole = blk0 == 0 && blk1 == n_blocks;
     constexpr int kSlot = NV * (HD + 2);
-    float* slot = a.part + static_cast<size_t>(2 * team + (u == u_begin ? 0 : 1)) * kSlot;
+    // a share cuts at most two groups: the one it begins in, and the one it ends in
+    float* slot = a.part + static_cast<size_t>(2 * team + (blk0 > 0 ? 0 : 1)) * kSlot;
     // Dims d .. d + 3 of vector v: the result, or this share's part of it.
     auto emit = [&](int v, int d, float4 acc, float M, float L, bool final) {
       if (final) {
         if (v >= n_vec) return;
         const float inv = L > 0.f ? 1.f / L : (L == L ? 0.f : L);
-        const int row = (n0 + v) / G, hq = h * G + (n0 + v) - row * G;
+        int hq;
+        const int row = row_of(v, hq);
         const long long off = static_cast<long long>(sq.row0 + row) * a.ld_o + hq * HD + d;
         if (a.dtype == DVI_BF16)
           *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + off) =
@@ -599,7 +654,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
       }
       team_bar();
       if (last_s[in_cta]) {
-        const float* p0 = a.part + static_cast<size_t>(2 * t0 + (share(t0) == g_begin ? 0 : 1)) * kSlot;
+        const float* p0 = a.part + static_cast<size_t>(2 * t0 + 1) * kSlot;
         const float* p1 = a.part + static_cast<size_t>(2 * t0 + 2) * kSlot;
         const int n = t1 - t0 + 1;
         for (int i = tw * 32 + lane; i < NV * HD / 4; i += S * 32) {
@@ -623,7 +678,6 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
       }
     }
     team_bar();   // the rings and the queries are read before the next group's
-    u = g_begin + blk1;
   }
 }
 
@@ -631,17 +685,17 @@ namespace {
 template <bool E4M3, int HD, int NT, bool PAIR>
 cudaError_t launch_pa(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
   using SH = PaShape<HD, NT, PAIR>;
-  // the blocks of all groups are counted in 32 bits
+  // the units of all groups are counted in 32 bits
   const long long tiles = static_cast<long long>(a.c.n_rows) * a.G / (8 * NT) + a.c.n_seqs;
-  const long long blocks = ((static_cast<long long>(a.c.max_pages) << a.c.log_p) / kPaKeys + 1) * a.c.H;
+  const long long blocks = ((static_cast<long long>(a.c.max_pages) << a.c.log_p) / kPaKeys + 17) * a.c.H;
   if (tiles * blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
   static PerDevice attr;
   attr.once([] {
     cudaFuncSetAttribute(paged_attend_kernel<E4M3, HD, NT, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                         SH::kUnitsAt + 4 * (kPagedMaxSeqs + 1));
+                         SH::kUnitsAt + 16 * (kPagedMaxSeqs + 1));
   });
   return launch_pdl(paged_attend_kernel<E4M3, HD, NT, PAIR>, dim3(n_sms), dim3(SH::kThreads),
-                    SH::kUnitsAt + 4 * (a.c.n_seqs + 1), s, a);
+                    SH::kUnitsAt + 16 * (a.c.n_seqs + 1), s, a);
 }
 template <bool E4M3, int HD>
 cudaError_t pa_tiles(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
