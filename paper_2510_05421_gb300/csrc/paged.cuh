@@ -153,10 +153,12 @@ template <> struct Code<false> {
     for (int i = 0; i < 4; ++i) x[i] = static_cast<float>(static_cast<int8_t>(w >> (8 * i)));
   }
 };
-__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {
-  uint32_t r;
-  asm("{\n\t.reg .b16 h;\n\tcvt.u16.u32 h, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(two));
-  return r;
+// Four e4m3 codes as two f16 pairs (exact).
+__device__ __forceinline__ void e4m3x4_to_f16(uint32_t w, uint32_t& a, uint32_t& b) {
+  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %1, hi;\n\t}"
+      : "=r"(a), "=r"(b)
+      : "r"(w));
 }
 template <> struct Code<true> {
   static constexpr float kTop = 448.f;
@@ -171,7 +173,8 @@ template <> struct Code<true> {
     return enc2(a, b) | (enc2(c, d) << 16);
   }
   static __device__ __forceinline__ void dec4(uint32_t w, float (&x)[4]) {
-    const uint32_t lo = e4m3x2_to_f16x2(w), hi = e4m3x2_to_f16x2(w >> 16);
+    uint32_t lo, hi;
+    e4m3x4_to_f16(w, lo, hi);
     const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&lo));
     const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&hi));
     x[0] = a.x, x[1] = a.y, x[2] = b.x, x[3] = b.y;

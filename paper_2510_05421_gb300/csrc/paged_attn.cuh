@@ -40,7 +40,20 @@ constexpr int kPaKeys = 16;               // positions per block: never more tha
 constexpr int kPaTeam = 4;                // warps of the smallest team
 constexpr float kPaLazy = 8.f;            // growth of a maximum (base 2) that rescales the accumulator
 constexpr float kPaUp = 5.f;              // weights are at most 2^(kPaLazy + kPaUp): f16 keeps small ones exact
+constexpr float kPaMost = 8192.f;         // 2^(kPaLazy + kPaUp)
+constexpr float kPaUnset = -1e30f;        // the reference of a vector that has seen no key
 constexpr float kPaLog2e = 1.4426950408889634f;
+
+// A share's part of one group.
+struct __align__(16) PaPiece {
+  int len, row0, h, n_vec;          // the sequence's length and first row; KV head; vectors of the tile
+  int row_lo, rest, row_hi, held_end;   // the tile's rows (and where in the first it begins); positions that are somebody's
+  int s0, s1, cut, whole;           // its blocks; it begins inside the group; it is all of the group's blocks
+  int g_begin, g_end, b, valid;     // units of the group's blocks (the share goes on at g_end); sequence
+};
+struct PaPlan {
+  int S, n_teams, total, share_q, share_r, over;
+};
 
 template <int HD, int NT, bool PAIR>
 struct PaShape {
@@ -51,18 +64,16 @@ struct PaShape {
   static constexpr int kHalf = kPaKeys * HD;                 // K (or V) codes of a block
   static constexpr int kStage = 2 * kHalf;
   static constexpr int kStages = (HD == 128 ? 3 : 6) * (16 / kWarps) - (kWarps == 8 ? 1 : 0);
-  static constexpr int kScales = (kStages * 8 + 15) / 16 * 16;
   static constexpr int kRing = kWarps * kStages * kStage;
   static constexpr int kQ = NT * HD * 16 * (PAIR ? 2 : 1);   // query fragments of a team
-  static constexpr int kVec = NT * 8 * 16;                   // per vector: factor, slope, position, -
+  static constexpr int kVec = NT * 8 * 12;                   // per vector: factor, then slope and position
   static constexpr int kQAt = kRing;
   static constexpr int kVecAt = kQAt + kTeams * kQ;
-  static constexpr int kScaleAt = kVecAt + kTeams * kVec;
-  static constexpr int kUnitsAt = kScaleAt + kWarps * kScales;
+  static constexpr int kUnitsAt = kVecAt + kTeams * kVec;
   // a warp's partial result (8 NT rows of HD sums, a maximum and a sum each) lies in its ring
   static_assert(NT * 8 * (HD + 2) * 4 <= kStages * kStage, "partial results");
   static_assert(kTeams <= kPagedTeams, "the workspace");
-  static_assert(kUnitsAt + 16 * (kPagedMaxSeqs + 1) + 512 <= 232448, "shared memory");
+  static_assert(kUnitsAt + 8 * (kPagedMaxSeqs + 1) + 1536 <= 232448, "shared memory");
 };
 
 __device__ __forceinline__ float pa_ex2(float x) {
@@ -78,8 +89,8 @@ __device__ __forceinline__ float pa_lg2(float x) {
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t n) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, uint32_t n) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() {
@@ -127,8 +138,7 @@ __device__ __forceinline__ uint32_t hsub2_1152(uint32_t x) {
 template <bool E4M3>
 __device__ __forceinline__ void codes_f16(uint32_t w, uint32_t& a, uint32_t& b) {
   if (E4M3) {
-    a = e4m3x2_to_f16x2(w & 0xffffu);
-    b = e4m3x2_to_f16x2(w >> 16);
+    e4m3x4_to_f16(w, a, b);
   } else {
     const uint32_t u = w ^ 0x80808080u;
     a = hsub2_1152(__byte_perm(u, 0x64646464u, 0x4140));
@@ -161,155 +171,189 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   uint8_t* ring = sm + warp * ST * SH::kStage;
   const uint32_t ring_s = smem_u32(ring);
-  float* scl = reinterpret_cast<float*>(sm + SH::kScaleAt + warp * SH::kScales);
-  const uint32_t scl_s = smem_u32(scl);
-  // per sequence b: [b] length, first row, units before it; [b + 1].w its rows
-  int4* seqs = reinterpret_cast<int4*>(sm + SH::kUnitsAt);
-  __shared__ int scan_s[2][W];
+  int2* before = reinterpret_cast<int2*>(sm + SH::kUnitsAt);      // [n_seqs + 1] blocks, groups before a sequence
+  constexpr int kFew = 32;                                        // sequences whose numbers one warp holds
+  __shared__ PagedSeq few_s[kFew];
+  __shared__ PaPiece piece_s[SH::kTeams][2];
+  __shared__ PaPlan plan_s;
+  __shared__ int2 scan_s[W];
   __shared__ int last_s[SH::kTeams];
+  const int G = a.G;
 
   griddep_wait();
   griddep_launch();
 
   // ---------------- sequences
   // Blocks [first, first + n) of a sequence that any of its rows sees, its tiles.
-  const int G = a.G;
   auto extent = [&](int len, int rows, int& first, int& tiles) {
     const long long vecs = static_cast<long long>(rows) * G;
     first = tiles = 0;
     if (rows <= 0 || vecs < a.min_vectors || vecs > a.max_vectors) return 0;
     const int end = min(len + rows, c.max_pages << c.log_p);
     if (a.window > 0) first = max(0, len - a.window + 1) / kPaKeys;
-    tiles = static_cast<int>((vecs + NV - 1) / NV);
+    tiles = static_cast<int>((static_cast<unsigned>(vecs) + NV - 1) / NV);
     return max(1, (end + kPaKeys - 1) / kPaKeys - first);   // at least one, so that empty rows are written
   };
-  constexpr int kPasses = (kPagedMaxSeqs + SH::kThreads - 1) / SH::kThreads;
-  int blocks_all = 0, groups = 0;
-  int upto[kPasses];                          // groups up to and with this thread's sequences
-#pragma unroll
-  for (int i = 0; i < kPasses; ++i) {
-    const int b0 = i * SH::kThreads;
-    if (b0 >= c.n_seqs) break;
+  auto find = [&](int u, int u_end) {
+    PaPiece r;
+    r.valid = 0;
+    if (u >= u_end) return r;
+    const int over = plan_s.over;
+    int b = 0;
+    for (int hi = c.n_seqs - 1; b < hi;) {                  // the last b whose units begin at or before u
+      const int mid = (b + hi + 1) >> 1;
+      if (before[mid].x + before[mid].y * over <= u) b = mid;
+      else hi = mid - 1;
+    }
+    const PagedSeq sq = c.n_seqs <= kFew ? few_s[b] : paged_seq(c, b);
+    int first, tiles;
+    const int n_blocks = extent(sq.len, sq.n, first, tiles), unit0 = before[b].x + before[b].y * over;
+    const int grp = (u - unit0) / (n_blocks + over);
+    r.g_begin = unit0 + grp * (n_blocks + over) + over;
+    r.g_end = r.g_begin + n_blocks;
+    const int blk0 = max(u - r.g_begin, 0), blk1 = min(u_end, r.g_end) - r.g_begin;
+    if (blk1 <= 0) return r;                                // the share ends before the group's first block
+    const int tile = tiles == 1 ? 0 : grp % tiles;
+    r.h = tiles == 1 ? grp : grp / tiles;
+    const int n0 = tile * NV;                               // first vector
+    r.n_vec = min(NV, sq.n * G - n0);
+    r.row_lo = tile == 0 ? 0 : n0 / G;
+    r.rest = n0 - r.row_lo * G;
+    r.row_hi = r.row_lo + (r.rest + r.n_vec - 1) / G;
+    // positions that some row of the tile sees
+    const int cap = c.max_pages << c.log_p;
+    const int see_end = min(sq.len + r.row_hi + 1, cap);
+    const int see_begin = a.window > 0 ? max(0, sq.len + r.row_lo - a.window + 1) : 0;
+    r.held_end = min(sq.len + sq.n, cap);                   // rows of the cache past it are nobody's
+    r.s0 = max(first + blk0, see_begin / kPaKeys);
+    r.s1 = min(first + blk1, (see_end + kPaKeys - 1) / kPaKeys);
+    r.len = sq.len;
+    r.row0 = sq.row0;
+    r.cut = blk0 > 0;
+    r.whole = blk0 == 0 && blk1 == n_blocks;
+    r.b = b;
+    r.valid = 1;
+    return r;
+  };
+  // floor(total k / n_teams); the fraction's numerator is below 2^20, so f32 decides it
+  auto share = [&](int k) {
+    return plan_s.share_q * k +
+           static_cast<int>((static_cast<float>(plan_s.share_r * k) + 0.5f) / static_cast<float>(plan_s.n_teams));
+  };
+  int2 all = make_int2(0, 0);                                    // blocks and groups of all sequences
+  for (int b0 = 0; b0 < c.n_seqs; b0 += SH::kThreads) {
+    if (c.n_seqs <= kFew && warp > 0) break;
     const int b = b0 + tid;
     int n = 0, ng = 0;
-    PagedSeq sq{};
     if (b < c.n_seqs) {
       int first, tiles;
-      sq = paged_seq(c, b);
+      const PagedSeq sq = paged_seq(c, b);
       const int blocks = extent(sq.len, sq.n, first, tiles);
       ng = tiles * c.H;
       n = blocks * ng;
+      if (c.n_seqs <= kFew) few_s[b] = sq;
     }
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int x = __shfl_up_sync(0xffffffffu, n, o), y = __shfl_up_sync(0xffffffffu, ng, o);
       if (lane >= o) n += x, ng += y;
     }
-    if (b0 > 0) __syncthreads();
-    if (lane == 31) scan_s[0][warp] = n, scan_s[1][warp] = ng;
-    __syncthreads();
-    int before = blocks_all, g_before = groups;
-#pragma unroll
-    for (int w = 0; w < W; ++w) {
-      if (w < warp) before += scan_s[0][w], g_before += scan_s[1][w];
-      blocks_all += scan_s[0][w];
-      groups += scan_s[1][w];
-    }
-    upto[i] = g_before + ng;
-    if (b < c.n_seqs) {
-      reinterpret_cast<int2*>(seqs + b)[0] = make_int2(sq.len, sq.row0);
-      reinterpret_cast<int2*>(seqs + b + 1)[1] = make_int2(before + n, sq.n);
+    if (c.n_seqs <= kFew) {
+      if (b < c.n_seqs) before[b + 1] = make_int2(n, ng);
+      all = make_int2(__shfl_sync(0xffffffffu, n, 31), __shfl_sync(0xffffffffu, ng, 31));
+    } else {
+      if (b0 > 0) __syncthreads();
+      if (lane == 31) scan_s[warp] = make_int2(n, ng);
+      __syncthreads();
+      int2 at = all;
+#pragma unroll 4
+      for (int w = 0; w < W; ++w) {
+        const int2 x = scan_s[w];
+        if (w < warp) at.x += x.x, at.y += x.y;
+        all.x += x.x, all.y += x.y;
+      }
+      if (b < c.n_seqs) before[b + 1] = make_int2(at.x + n, at.y + ng);
     }
   }
-  if (groups == 0) return;
+  if (tid == 0) before[0] = make_int2(0, 0);
+  if (c.n_seqs > kFew) __syncthreads();
 
-  // ---------------- teams: a team's share is an equal part of a row of units, a
-  // group's being as many as its blocks and kOver = S more for what a group costs
-  // beside them (a step of each warp).  Groups of equal size are not cut across a
-  // share where each share holds one part.  16 warps on a group while that leaves
-  // each of them two steps and the shares fill the GPU about as well as smaller
-  // teams' would.
-  int S = kPaTeam, n_teams = 0;
-  {
-    const int per_group = blocks_all / groups;
-    int best = -1;
+  // ---------------- plan (one warp): teams of S warps take equal shares of a row of
+  // units, a group's being as many as its blocks and `over` = S more for what a
+  // group costs beside them (a step of each warp).  Groups of equal size are not
+  // cut across a share where each share holds one part.  16 warps on a group while
+  // that leaves each of them two steps and the shares fill the GPU nearly as well
+  // as smaller teams' would.
+  if (warp == 0) {
+    const int groups = all.y;
+    int S = kPaTeam, n_teams = 0;
+    const float per = 1.f / static_cast<float>(max(groups, 1));
+    float best = -1.f;
 #pragma unroll
     for (int s = W; s >= kPaTeam; s >>= 1) {
-      if (s > kPaTeam && per_group < 2 * s) continue;
+      if (s > kPaTeam && all.x < 2 * s * groups) continue;
       const int most = static_cast<int>(gridDim.x) * (W / s);
-      const int few = max(1, (blocks_all + groups * s) / (2 * s));     // a share is two steps at least
+      const int few = max(1, (all.x + groups * s) / (2 * s));          // a share is two steps at least
       int n = min(most, few);
-      if (n >= groups) n = n / groups * groups;
-      const int fill = n >= groups ? (n == min(most, few) ? 100 : 100 * n / most) : 90;
-      if (best < 0 || fill > best + 6) best = fill, S = s, n_teams = n;
+      float fill = 0.9f;
+      if (n >= groups) {
+        int k = static_cast<int>(static_cast<float>(n) * per);         // n / groups, to within one
+        k += (k + 1) * groups <= n ? 1 : 0;
+        k -= k * groups > n ? 1 : 0;
+        n = k * groups;
+        fill = static_cast<float>(n) * (1.f / static_cast<float>(most));
+      }
+      if (fill > best + 0.2f) best = fill, S = s, n_teams = n;
+    }
+    const int total = all.x + groups * S;
+    if (lane == 0) {
+      plan_s.S = S, plan_s.over = S;
+      plan_s.n_teams = n_teams, plan_s.total = total;
+      plan_s.share_q = n_teams > 0 ? total / n_teams : 0;
+      plan_s.share_r = total - plan_s.share_q * n_teams;
+    }
+    __syncwarp();
+    if (lane < W / S) {
+      const int team = lane * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x);
+      if (team < n_teams) piece_s[lane][0] = find(share(team), share(team + 1));
+      else piece_s[lane][0].valid = 0;
     }
   }
-  const int over = S;
-  const int total = blocks_all + groups * over;
-  const int tw = warp % S, in_cta = warp / S;
-  const int team = in_cta * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x);
-#pragma unroll
-  for (int i = 0; i < kPasses; ++i) {
-    const int b = i * SH::kThreads + tid;
-    if (b < c.n_seqs) seqs[b + 1].z += upto[i] * over;
-  }
-  if (tid == 0) seqs[0].z = 0;
   __syncthreads();
-  if (team >= n_teams) return;
-  const int share_q = total / n_teams, share_r = total - share_q * n_teams;
-  auto share = [&](int k) { return share_q * k + share_r * k / n_teams; };
+  const int S = plan_s.S, log_s = 31 - __clz(S);
+  const int tw = warp & (S - 1), in_cta = warp >> log_s;
+  const int team = in_cta * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x);
   auto team_of = [&](int unit) {
-    int k = min(n_teams - 1, static_cast<int>(static_cast<float>(unit) * (static_cast<float>(n_teams) / static_cast<float>(total))));
+    const int n_teams = plan_s.n_teams;
+    int k = min(n_teams - 1, static_cast<int>(static_cast<float>(unit) *
+                                              (static_cast<float>(n_teams) / static_cast<float>(plan_s.total))));
     while (k > 0 && share(k) > unit) --k;
     while (share(k + 1) <= unit) ++k;
     return k;
   };
-  const int u_begin = share(team), u_end = share(team + 1);
   auto team_bar = [&] { named_bar(1 + in_cta, 32 * S); };
   uint8_t* qf = sm + SH::kQAt + in_cta * SH::kQ;
   const uint32_t q_s = smem_u32(qf);
-  float4* vec = reinterpret_cast<float4*>(sm + SH::kVecAt + in_cta * SH::kVec);
+  float* fac = reinterpret_cast<float*>(sm + SH::kVecAt + in_cta * SH::kVec);
+  float2* vec = reinterpret_cast<float2*>(fac + NV);
 
-  int u = u_begin;
-  int b = 0;
-  {
-    int hi = c.n_seqs - 1;
-    while (b < hi) {                          // the last b whose units begin at or before u
-      const int mid = (b + hi + 1) >> 1;
-      if (seqs[mid].z <= u) b = mid;
-      else hi = mid - 1;
-    }
-  }
-  while (u < u_end) {
-    // ---------------- the group of unit u, and the share's part of it
-    while (b + 1 < c.n_seqs && seqs[b + 1].z <= u) ++b;
-    const int4 sq4 = seqs[b];
-    PagedSeq sq;
-    sq.len = sq4.x, sq.row0 = sq4.y;
-    sq.n = seqs[b + 1].w;
-    int first, tiles;
-    const int n_blocks = extent(sq.len, sq.n, first, tiles);
-    const int grp = (u - sq4.z) / (n_blocks + over);
-    const int g_begin = sq4.z + grp * (n_blocks + over) + over, g_end = g_begin + n_blocks;   // its blocks' units
-    const int blk0 = max(u - g_begin, 0), blk1 = min(u_end, g_end) - g_begin;
-    if (blk1 <= 0) break;                     // the share ends before the group's first block
-    u = g_end;
-    const int h = grp / tiles, tile = grp - h * tiles;
-    const int n0 = tile * NV;                                      // first vector
-    const int n_vec = min(NV, sq.n * G - n0);
-    const int row_lo = n0 / G, rest = n0 - row_lo * G;            // rows of the tile, and where the first begins
-    const int row_hi = row_lo + (rest + n_vec - 1) / G;
+  for (int turn = 0;; turn ^= 1) {
+    const PaPiece pc = piece_s[in_cta][turn];
+    if (!pc.valid) break;
+    const int len = pc.len, h = pc.h, n_vec = pc.n_vec, s0 = pc.s0, s1 = pc.s1, held_end = pc.held_end;
     auto row_of = [&](int n, int& hq) {                            // vector n of the tile: its row, its head
-      const int r = G == 1 ? n : static_cast<int>(__umulhi(static_cast<uint32_t>(rest + n), a.inv_g));
-      hq = h * G + rest + n - r * G;
-      return row_lo + r;
+      const int r = G == 1 ? n : static_cast<int>(__umulhi(static_cast<uint32_t>(pc.rest + n), a.inv_g));
+      hq = h * G + pc.rest + n - r * G;
+      return pc.row_lo + r;
     };
-    // positions that some row of the tile sees
-    const int cap = c.max_pages << c.log_p;
-    const int see_end = min(sq.len + row_hi + 1, cap);
-    const int see_begin = a.window > 0 ? max(0, sq.len + row_lo - a.window + 1) : 0;
-    const int held_end = min(sq.len + sq.n, cap);                  // rows of the cache past it are nobody's
-    const int s0 = max(first + blk0, see_begin / kPaKeys), s1 = min(first + blk1, (see_end + kPaKeys - 1) / kPaKeys);
+
+    // ---------------- the warp's blocks s0 + tw + i S.  Lane i % 32 holds the table
+    // entry of block i, and its page's scales: entries are read 32 blocks ahead
+    const int n_mine = s1 - s0 - tw > 0 ? (s1 - s0 - tw + S - 1) >> log_s : 0;
+    auto entry = [&](int i) {
+      return i < n_mine ? paged_entry(c, pc.b, ((s0 + tw + (i << log_s)) * kPaKeys) >> c.log_p) : -1;
+    };
+    int ent = entry(lane), ent_next = -1;
 
     // ---------------- queries: a warp loads whole vectors, HD / 32 dims a lane
     constexpr int kDims = HD / 32;
@@ -323,7 +367,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
       if (n < n_vec) {
         int hq;
         const int row = row_of(n, hq);
-        const long long off = static_cast<long long>(sq.row0 + row) * a.ld_q + hq * HD + lane * kDims;
+        const long long off = static_cast<long long>(pc.row0 + row) * a.ld_q + hq * HD + lane * kDims;
         if (a.dtype == DVI_BF16) {
           const uint32_t* p = reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(a.q) + off);
 #pragma unroll
@@ -336,45 +380,55 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
       }
     }
 
-    // ---------------- copies of a block; its page is looked up one step ahead
-    const uint8_t* kh = c.k + ((static_cast<size_t>(h) << c.log_p) * HD);
-    const uint8_t* vh = c.v + ((static_cast<size_t>(h) << c.log_p) * HD);
-    const size_t page_bytes = (static_cast<size_t>(c.H) << c.log_p) * HD;
+    // ---------------- copies
+    const float* ks_h = c.k_scale + h;
+    const float* vs_h = c.v_scale + h;
     constexpr int kRow = HD / 16;                                  // 16-byte chunks of a row
     constexpr int kRows = 32 / kRow;                               // rows a warp copies at once
-    const int ch = lane % kRow, r0 = lane / kRow;
-    auto entry = [&](int blk) { return blk < s1 ? paged_entry(c, b, (blk * kPaKeys) >> c.log_p) : -1; };
-    auto issue = [&](int blk, int stage, int raw) {
-      if (blk < s1) {
-        const int pg = paged_valid(c, raw);
-        const uint32_t dst = ring_s + stage * SH::kStage;
-        const int p = blk * kPaKeys;
-        const size_t off = static_cast<size_t>(max(pg, 0)) * page_bytes +
-                           static_cast<size_t>(((p & (c.P - 1)) + r0) * HD + ch * 16);
-        const int live = pg >= 0 ? held_end - p - r0 : 0;          // rows r0 + r, r < live, are somebody's
+    const int r0 = lane / kRow, ch = lane % kRow;
+    const size_t page_bytes = (static_cast<size_t>(c.H) << c.log_p) * HD;
+    const uint8_t* k_lane = c.k + ((static_cast<size_t>(h) << c.log_p) + r0) * HD + ch * 16;
+    const long long v_from_k = c.v - c.k;
+    // the permutation has a period of 8 rows: at most two lane offsets
+    const uint32_t at0 = ring_s + pa_chunk<HD>(r0, ch), at1 = ring_s + pa_chunk<HD>(r0 + kRows, ch);
+    auto copy = [&](int i, int stage) {
+      const int pg = __shfl_sync(0xffffffffu, ent, i & 31);
+      const int p = (s0 + tw + (i << log_s)) * kPaKeys;
+      const uint8_t* src = k_lane + static_cast<size_t>(max(pg, 0)) * page_bytes + (p & (c.P - 1)) * HD;
+      const uint32_t d0 = at0 + stage * SH::kStage, d1 = at1 + stage * SH::kStage;
+      if (pg >= 0 && p + kPaKeys <= held_end) {
 #pragma unroll
-        for (int r = 0; r < kPaKeys; r += kRows) {
-          const uint32_t n = r < live ? 16u : 0u;
-          const uint32_t at = pa_chunk<HD>(r + r0, ch);
-          cp_async16(dst + at, kh + off + r * HD, n);
-          cp_async16(dst + SH::kHalf + at, vh + off + r * HD, n);
+        for (int r = 0; r < kPaKeys / kRows; ++r) {
+          const uint32_t dst = (r & 1 ? d1 : d0) + (r >> 1) * 2 * kRows * HD;
+          cp_async16(dst, src + r * kRows * HD);
+          cp_async16(dst + SH::kHalf, src + v_from_k + r * kRows * HD);
         }
-        if (lane < 2) {
-          const float* sp = (lane & 1 ? c.v_scale : c.k_scale) + static_cast<size_t>(max(pg, 0)) * c.H + h;
-          cp_async4(scl_s + stage * 8 + lane * 4, sp, pg >= 0 ? 4u : 0u);
+      } else {
+        const int live = pg >= 0 ? held_end - p - r0 : 0;          // rows past it, and pages not held: zeros
+#pragma unroll 1
+        for (int r = 0; r < kPaKeys / kRows; ++r) {
+          const uint32_t n = r * kRows < live ? 16u : 0u;
+          const uint32_t dst = (r & 1 ? d1 : d0) + (r >> 1) * 2 * kRows * HD;
+          cp_async16(dst, src + r * kRows * HD, n);
+          cp_async16(dst + SH::kHalf, src + v_from_k + r * kRows * HD, n);
         }
       }
-      cp_commit();
     };
-    int nxt;
-    {
-      int pg[ST - 1];
-#pragma unroll
-      for (int i = 0; i < ST - 1; ++i) pg[i] = entry(s0 + tw + i * S);
-      nxt = entry(s0 + tw + (ST - 1) * S);
-#pragma unroll
-      for (int i = 0; i < ST - 1; ++i) issue(s0 + tw + i * S, i, pg[i]);
+
+    float ks_in, vs_in;                          // scales of the blocks being copied
+    auto batch = [&](int j) {                    // block j is the first of 32
+      ent = paged_valid(c, ent);
+      ent_next = entry(j + 32 + lane);
+      ks_in = ent >= 0 ? __ldg(ks_h + static_cast<size_t>(ent) * c.H) : 0.f;
+      vs_in = ent >= 0 ? __ldg(vs_h + static_cast<size_t>(ent) * c.H) : 0.f;
+    };
+    batch(0);
+#pragma unroll 1
+    for (int j = 0; j < ST - 1; ++j) {
+      if (j < n_mine) copy(j, j);
+      cp_commit();
     }
+    if (tw == 0 && lane == 0) piece_s[in_cta][turn ^ 1] = find(pc.g_end, share(team + 1));
 
     // ---------------- query fragments: thread (g, t) of vector 8 nt + g holds, for
     // step j, dims 16 t + 4 j .. + 3 (hd 128: from step 4 on 64 + 16 t + 4 (j - 4))
@@ -405,8 +459,9 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
         const int row = row_of(n, hq);
         const bool live = n < n_vec;
         const float f = a.softcap > 0.f ? down * (a.scale / a.softcap) : down * (a.scale * kPaLog2e);
-        vec[n] = make_float4(f, live && a.slopes ? __ldg(a.slopes + hq) * kPaLog2e : 0.f,
-                             __int_as_float(live ? sq.len + row : -1), 0.f);
+        fac[n] = f;
+        vec[n] = make_float2(live && a.slopes ? __ldg(a.slopes + hq) * kPaLog2e : 0.f,
+                             __int_as_float(live ? len + row : -1));
       }
     }
     team_bar();
@@ -419,24 +474,40 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
       for (int i = 0; i < kSteps; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[i][nt][e] = 0.f;
-      m[nt][0] = m[nt][1] = -INFINITY;
+      m[nt][0] = m[nt][1] = kPaUnset;
       l[nt][0] = l[nt][1] = 0.f;
     }
 
+    // blocks that every row of the tile sees whole: full_begin .. full_end - 1
+    const int full_end = min((len + pc.row_lo + 1) / kPaKeys, held_end / kPaKeys);
+    const int full_begin = a.window > 0 ? max(0, len + pc.row_hi - a.window + kPaKeys) / kPaKeys : 0;
+    const bool curved = a.softcap > 0.f || a.slopes != nullptr;
+    float ks_l = 0.f, lv_l = 0.f, iv_l = 0.f;    // ks, log2 vs and 1 / vs (0: no page) of the blocks at work
     int stage = 0;
 #pragma unroll 1
-    for (int blk = s0 + tw; blk < s1; blk += S) {
+    for (int i = 0; i < n_mine; ++i) {
+      if ((i & 31) == 0) {
+        const float x = fmaxf(vs_in, kPagedMinScale);
+        ks_l = ks_in, lv_l = pa_lg2(x), iv_l = vs_in > 0.f ? __fdividef(1.f, x) : 0.f;
+      }
       {
-        // the stage that the last step read is free: its next block's copies
-        const int raw = nxt;
-        nxt = entry(blk + ST * S);
-        __syncwarp();
-        issue(blk + (ST - 1) * S, stage == 0 ? ST - 1 : stage - 1, raw);
+        const int j = i + ST - 1;                // its copies go where the last step read
+        if (j < n_mine) {
+          if ((j & 31) == 0) {
+            ent = ent_next;
+            batch(j);
+          }
+          __syncwarp();
+          copy(j, stage == 0 ? ST - 1 : stage - 1);
+        }
+        cp_commit();
       }
       cp_wait<ST - 1>();
       __syncwarp();
+      const int blk = s0 + tw + (i << log_s);
+      const float ks = __shfl_sync(0xffffffffu, ks_l, i & 31), iv = __shfl_sync(0xffffffffu, iv_l, i & 31);
+      float lv = __shfl_sync(0xffffffffu, lv_l, i & 31);
       const uint32_t ks_s = ring_s + stage * SH::kStage, vs_s = ks_s + SH::kHalf;
-      const float ks = scl[stage * 2], vs = scl[stage * 2 + 1];
       // ---------------- scores
       float s[NT][4];
       {
@@ -467,72 +538,81 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
         }
       }
       // ---------------- softmax: element e of s[nt]: key g + 8 (e / 2), vector 8 nt + 2 t + e % 2
-      const int p_blk = blk * kPaKeys;
-      const bool plain = p_blk + kPaKeys - 1 <= sq.len + row_lo && vs > 0.f &&
-                         (a.window == 0 || p_blk > sq.len + row_hi - a.window);
-      const float vx = fmaxf(vs, kPagedMinScale), lv = pa_lg2(vx), iv = __fdividef(1.f, vx);
+      const bool plain = blk >= full_begin && blk < full_end && iv > 0.f;
+      float f[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const float2 x = *reinterpret_cast<const float2*>(fac + nt * 8 + 2 * t);
+        f[nt][0] = x.x * ks, f[nt][1] = x.y * ks;
+      }
+      if (!plain || curved) {
+        // the finished scores in place of the products
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const float4 v = *reinterpret_cast<const float4*>(vec + nt * 8 + 2 * t);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float x = s[nt][e] * f[nt][e & 1];
+            if (a.softcap > 0.f) {
+              if (PAIR) x = tanhf(x);
+              else x = 1.f - __fdividef(2.f, 1.f + pa_ex2(x * (2.f * kPaLog2e)));
+              x *= a.softcap * kPaLog2e;
+            }
+            const int d = blk * kPaKeys + g + 8 * (e >> 1) - __float_as_int(e & 1 ? v.w : v.y);
+            x = fmaf(e & 1 ? v.z : v.x, static_cast<float>(d), x + lv);
+            if (!plain && (d > 0 || !(iv > 0.f) || (a.window > 0 && d <= -a.window))) x = -INFINITY;
+            s[nt][e] = x;
+          }
+          f[nt][0] = f[nt][1] = 1.f;
+        }
+        lv = 0.f;
+      }
+      float p[NT][4], most = 0.f;
+      auto weights = [&] {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const float c0 = lv - m[nt][0], c1 = lv - m[nt][1];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[nt][e] = pa_ex2(fmaf(s[nt][e], f[nt][e & 1], e & 1 ? c1 : c0));
+        }
+      };
+      weights();
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) most = fmaxf(most, p[nt][e]);
+      if (__any_sync(0xffffffffu, most > kPaMost)) {
+        // some maximum has outgrown its reference (or is the first)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            float x = fmaxf(fmaf(s[nt][q], f[nt][q], lv), fmaf(s[nt][q + 2], f[nt][q], lv));
+#pragma unroll
+            for (int off = 4; off < 32; off <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
+            x = fmaxf(x - kPaUp, m[nt][q]);                       // the reference sits below the maximum
+            const float shrink = pa_ex2(m[nt][q] - x);
+            m[nt][q] = x;
+            l[nt][q] *= shrink;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) o[i][nt][q] *= shrink, o[i][nt][q + 2] *= shrink;
+          }
+        weights();
+      }
       uint32_t pb[NT][2], pl[NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const float4 va = vec[nt * 8 + 2 * t], vb = vec[nt * 8 + 2 * t + 1];
-        const float fa = va.x * ks, fb = vb.x * ks;
-        if (a.softcap > 0.f) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float x = s[nt][e] * (e & 1 ? fb : fa);
-            if (PAIR) x = tanhf(x);
-            else x = 1.f - __fdividef(2.f, 1.f + pa_ex2(x * (2.f * kPaLog2e)));
-            s[nt][e] = fmaf(a.softcap * kPaLog2e, x, lv);
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[nt][e] = fmaf(s[nt][e], e & 1 ? fb : fa, lv);
-        }
-        if (a.slopes) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float4& v = e & 1 ? vb : va;
-            s[nt][e] = fmaf(v.y, static_cast<float>(p_blk + g + 8 * (e >> 1) - __float_as_int(v.z)), s[nt][e]);
-          }
-        }
-        if (!plain) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int d = p_blk + g + 8 * (e >> 1) - __float_as_int(e & 1 ? vb.z : va.z);
-            if (d > 0 || !(vs > 0.f) || (a.window > 0 && d <= -a.window)) s[nt][e] = -INFINITY;
-          }
-        }
-        const float top0 = fmaxf(s[nt][0], s[nt][2]), top1 = fmaxf(s[nt][1], s[nt][3]);
-        const bool grow = top0 > m[nt][0] + (kPaLazy + kPaUp) || top1 > m[nt][1] + (kPaLazy + kPaUp);
-        if (__any_sync(0xffffffffu, grow)) {
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            float x = q ? top1 : top0;
-#pragma unroll
-            for (int off = 4; off < 32; off <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, off));
-            x -= kPaUp;                                           // the reference sits below the maximum
-            const float f = x > m[nt][q] ? (m[nt][q] == -INFINITY ? 0.f : pa_ex2(m[nt][q] - x)) : 1.f;
-            m[nt][q] = fmaxf(m[nt][q], x);
-            l[nt][q] *= f;
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i) o[i][nt][q] *= f, o[i][nt][q + 2] *= f;
-          }
-        }
-        const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
-        float p[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] = pa_ex2(s[nt][e] - (e & 1 ? m1 : m0));
-        l[nt][0] = fmaf(p[0] + p[2], iv, l[nt][0]);
-        l[nt][1] = fmaf(p[1] + p[3], iv, l[nt][1]);
+        l[nt][0] = fmaf(p[nt][0] + p[nt][2], iv, l[nt][0]);
+        l[nt][1] = fmaf(p[nt][1] + p[nt][3], iv, l[nt][1]);
         if (PAIR) {
           uint32_t h0, h1, l0, l1;
-          split_f16x2(p[0], p[1], h0, l0);
-          split_f16x2(p[2], p[3], h1, l1);
+          split_f16x2(p[nt][0], p[nt][1], h0, l0);
+          split_f16x2(p[nt][2], p[nt][3], h1, l1);
           pb[nt][0] = movmatrix_trans(h0), pb[nt][1] = movmatrix_trans(h1);
           pl[nt][0] = movmatrix_trans(l0), pl[nt][1] = movmatrix_trans(l1);
         } else {
-          pb[nt][0] = movmatrix_trans(pack_f16x2(p[0], p[1]));
-          pb[nt][1] = movmatrix_trans(pack_f16x2(p[2], p[3]));
+          pb[nt][0] = movmatrix_trans(pack_f16x2(p[nt][0], p[nt][1]));
+          pb[nt][1] = movmatrix_trans(pack_f16x2(p[nt][2], p[nt][3]));
         }
       }
       // ---------------- values: keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9, HD / 8 dims from g HD / 8 on
@@ -595,10 +675,10 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
           *reinterpret_cast<float2*>(mine + n * HD + g * (HD / 8) + 2 * i) = make_float2(o[i][nt][q], o[i][nt][q + 2]);
       }
     team_bar();
-    const bool whole = blk0 == 0 && blk1 == n_blocks;
+    const bool whole = pc.whole;
     constexpr int kSlot = NV * (HD + 2);
     // a share cuts at most two groups: the one it begins in, and the one it ends in
-    float* slot = a.part + static_cast<size_t>(2 * team + (blk0 > 0 ? 0 : 1)) * kSlot;
+    float* slot = a.part + static_cast<size_t>(2 * team + (pc.cut ? 0 : 1)) * kSlot;
     // Dims d .. d + 3 of vector v: the result, or this share's part of it.
     auto emit = [&](int v, int d, float4 acc, float M, float L, bool final) {
       if (final) {
@@ -606,7 +686,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
         const float inv = L > 0.f ? 1.f / L : (L == L ? 0.f : L);
         int hq;
         const int row = row_of(v, hq);
-        const long long off = static_cast<long long>(sq.row0 + row) * a.ld_o + hq * HD + d;
+        const long long off = static_cast<long long>(pc.row0 + row) * a.ld_o + hq * HD + d;
         if (a.dtype == DVI_BF16)
           *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + off) =
               make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
@@ -625,15 +705,14 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     const float* parts = reinterpret_cast<const float*>(sm) + in_cta * S * kWarpFloats;
     for (int i = tw * 32 + lane; i < NV * HD / 4; i += S * 32) {
       const int v = i / (HD / 4), d = (i % (HD / 4)) * 4;
-      float M = -INFINITY;
+      float M = kPaUnset;
       for (int w = 0; w < S; ++w) M = fmaxf(M, parts[w * kWarpFloats + NV * HD + v]);
-      const float mu = M == -INFINITY ? 0.f : M;
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
       float L = 0.f;
 #pragma unroll 4
       for (int w = 0; w < S; ++w) {
         const float* p = parts + w * kWarpFloats;
-        const float f = pa_ex2(p[NV * HD + v] - mu);
+        const float f = pa_ex2(p[NV * HD + v] - M);
         const float4 x = *reinterpret_cast<const float4*>(p + v * HD + d);
         acc.x = fmaf(x.x, f, acc.x), acc.y = fmaf(x.y, f, acc.y);
         acc.z = fmaf(x.z, f, acc.z), acc.w = fmaf(x.w, f, acc.w);
@@ -643,7 +722,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     }
     if (!whole) {
       // teams of the group: t0 .. t1; whoever of them counts last joins their parts in order
-      const int t0 = team_of(g_begin), t1 = team_of(g_end - 1);
+      const int t0 = team_of(pc.g_begin), t1 = team_of(pc.g_end - 1);
       __threadfence();
       team_bar();
       if (tw == 0 && lane == 0) {
@@ -659,15 +738,15 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
         const int n = t1 - t0 + 1;
         for (int i = tw * 32 + lane; i < NV * HD / 4; i += S * 32) {
           const int v = i / (HD / 4), d = (i % (HD / 4)) * 4;
-          float M = -INFINITY, L = 0.f;
+          float M = kPaUnset, L = 0.f;
           float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
           for (int k = 0; k < n; ++k) {
             const float* p = k == 0 ? p0 : p1 + static_cast<size_t>(2 * (k - 1)) * kSlot;
             const float pm = __ldcg(p + NV * HD + v), ps = __ldcg(p + NV * HD + NV + v);
             const float4 x = __ldcg(reinterpret_cast<const float4*>(p + v * HD + d));
-            const float top = fmaxf(M, pm), mu = top == -INFINITY ? 0.f : top;
-            const float fa = pa_ex2(M - mu), fb = pa_ex2(pm - mu);
+            const float top = fmaxf(M, pm);
+            const float fa = pa_ex2(M - top), fb = pa_ex2(pm - top);
             M = top;
             acc.x = fmaf(x.x, fb, acc.x * fa), acc.y = fmaf(x.y, fb, acc.y * fa);
             acc.z = fmaf(x.z, fb, acc.z * fa), acc.w = fmaf(x.w, fb, acc.w * fa);
@@ -692,10 +771,10 @@ cudaError_t launch_pa(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
   static PerDevice attr;
   attr.once([] {
     cudaFuncSetAttribute(paged_attend_kernel<E4M3, HD, NT, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                         SH::kUnitsAt + 16 * (kPagedMaxSeqs + 1));
+                         SH::kUnitsAt + 8 * (kPagedMaxSeqs + 1));
   });
   return launch_pdl(paged_attend_kernel<E4M3, HD, NT, PAIR>, dim3(n_sms), dim3(SH::kThreads),
-                    SH::kUnitsAt + 16 * (a.c.n_seqs + 1), s, a);
+                    SH::kUnitsAt + 8 * (a.c.n_seqs + 1), s, a);
 }
 template <bool E4M3, int HD>
 cudaError_t pa_tiles(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
