@@ -88,15 +88,12 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedArgs& c, int b) {
     r1 = s.row0 + per;
   }
   s.n = r1 - s.row0;
-  const long long cap = static_cast<long long>(c.max_pages) << c.log_p;
-  if (s.len < 0 || s.row0 < 0 || s.n < 0 || r1 > c.n_rows || s.n > c.max_rows ||
-      static_cast<long long>(s.len) + s.n > cap) {
+  const int cap = c.max_pages << c.log_p;                         // the host refuses more than 2^30
+  if (s.len < 0 || s.row0 < 0 || s.n < 0 || r1 > c.n_rows || s.n > c.max_rows || s.n > cap - s.len) {
     flag_status(c.status, DVI_DEV_KV_FULL);
-    s.len = max(s.len, 0);
+    s.len = min(max(s.len, 0), cap);
     s.row0 = min(max(s.row0, 0), c.n_rows);
     s.n = min(min(max(s.n, 0), c.max_rows), c.n_rows - s.row0);
-    // positions stay below 2^31 (the host refuses capacities above 2^30)
-    s.len = static_cast<int>(min(static_cast<long long>(s.len), cap));
   }
   return s;
 }

@@ -70,8 +70,8 @@ struct PaShape {
   static constexpr int kQAt = kRing;
   static constexpr int kVecAt = kQAt + kTeams * kQ;
   static constexpr int kUnitsAt = kVecAt + kTeams * kVec;
-  // a warp's partial result (8 NT rows of HD sums, a maximum and a sum each) lies in its ring
-  static_assert(NT * 8 * (HD + 2) * 4 <= kStages * kStage, "partial results");
+  // a warp's partial result (8 NT rows of HD + 8 floats, a maximum and a sum each) lies in its ring
+  static_assert(NT * 8 * (HD + 10) * 4 <= kStages * kStage, "partial results");
   static_assert(kTeams <= kPagedTeams, "the workspace");
   static_assert(kUnitsAt + 8 * (kPagedMaxSeqs + 1) + 1536 <= 232448, "shared memory");
 };
@@ -89,9 +89,11 @@ __device__ __forceinline__ float pa_lg2(float x) {
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t n) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy)
+               : "memory");
 }
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
@@ -182,11 +184,20 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
 
   griddep_wait();
   griddep_launch();
+  {
+    // what the pieces will ask for first, on its way to L2 while one warp plans: a
+    // line of the page table and one of the queries for each thread of the grid
+    const size_t i = static_cast<size_t>(blockIdx.x) * SH::kThreads + tid;
+    const size_t table_bytes = static_cast<size_t>(c.n_seqs) * c.max_pages * 4;
+    const size_t q_bytes = (static_cast<size_t>(c.n_rows - 1) * a.ld_q + a.n_heads * HD) * (a.dtype == DVI_BF16 ? 2 : 4);
+    if (warp > 0 && i * 128 < table_bytes) prefetch_l2(reinterpret_cast<const uint8_t*>(c.table) + i * 128);
+    if (warp > 0 && i * 128 < q_bytes) prefetch_l2(static_cast<const uint8_t*>(a.q) + i * 128);
+  }
 
   // ---------------- sequences
   // Blocks [first, first + n) of a sequence that any of its rows sees, its tiles.
   auto extent = [&](int len, int rows, int& first, int& tiles) {
-    const long long vecs = static_cast<long long>(rows) * G;
+    const int vecs = rows * G;                              // the host refuses more than 2^31
     first = tiles = 0;
     if (rows <= 0 || vecs < a.min_vectors || vecs > a.max_vectors) return 0;
     const int end = min(len + rows, c.max_pages << c.log_p);
@@ -238,7 +249,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
   // floor(total k / n_teams); the fraction's numerator is below 2^20, so f32 decides it
   auto share = [&](int k) {
     return plan_s.share_q * k +
-           static_cast<int>((static_cast<float>(plan_s.share_r * k) + 0.5f) / static_cast<float>(plan_s.n_teams));
+           static_cast<int>(__fdividef(static_cast<float>(plan_s.share_r * k) + 0.5f, static_cast<float>(plan_s.n_teams)));
   };
   int2 all = make_int2(0, 0);                                    // blocks and groups of all sequences
   for (int b0 = 0; b0 < c.n_seqs; b0 += SH::kThreads) {
@@ -287,13 +298,13 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
   if (warp == 0) {
     const int groups = all.y;
     int S = kPaTeam, n_teams = 0;
-    const float per = 1.f / static_cast<float>(max(groups, 1));
+    const float per = __fdividef(1.f, static_cast<float>(max(groups, 1)));
     float best = -1.f;
-#pragma unroll
+#pragma unroll 1
     for (int s = W; s >= kPaTeam; s >>= 1) {
       if (s > kPaTeam && all.x < 2 * s * groups) continue;
-      const int most = static_cast<int>(gridDim.x) * (W / s);
-      const int few = max(1, (all.x + groups * s) / (2 * s));          // a share is two steps at least
+      const int log = 31 - __clz(s), most = static_cast<int>(gridDim.x) * (W >> log);
+      const int few = max(1, (all.x + groups * s) >> (log + 1));       // a share is two steps at least
       int n = min(most, few);
       float fill = 0.9f;
       if (n >= groups) {
@@ -301,7 +312,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
         k += (k + 1) * groups <= n ? 1 : 0;
         k -= k * groups > n ? 1 : 0;
         n = k * groups;
-        fill = static_cast<float>(n) * (1.f / static_cast<float>(most));
+        fill = __fdividef(static_cast<float>(n), static_cast<float>(most));
       }
       if (fill > best + 0.2f) best = fill, S = s, n_teams = n;
     }
@@ -332,6 +343,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     return k;
   };
   auto team_bar = [&] { named_bar(1 + in_cta, 32 * S); };
+  const uint64_t once = l2_evict_first_policy();   // codes are read once; tables, queries and parts are to stay
   uint8_t* qf = sm + SH::kQAt + in_cta * SH::kQ;
   const uint32_t q_s = smem_u32(qf);
   float* fac = reinterpret_cast<float*>(sm + SH::kVecAt + in_cta * SH::kVec);
@@ -355,28 +367,22 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     };
     int ent = entry(lane), ent_next = -1;
 
-    // ---------------- queries: a warp loads whole vectors, HD / 32 dims a lane
+    // ---------------- queries: a warp loads whole vectors, HD / 32 dims a lane, as they lie there
     constexpr int kDims = HD / 32;
     constexpr int kMine = NV / kPaTeam;                            // most vectors of a warp
-    float qx[kMine][kDims];
+    uint32_t qx[kMine][PAIR ? kDims : kDims / 2];
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
-#pragma unroll
-      for (int e = 0; e < kDims; ++e) qx[i][e] = 0.f;
       const int n = tw + i * S;
+#pragma unroll
+      for (int e = 0; e < (PAIR ? kDims : kDims / 2); ++e) qx[i][e] = 0u;
       if (n < n_vec) {
         int hq;
         const int row = row_of(n, hq);
-        const long long off = static_cast<long long>(pc.row0 + row) * a.ld_q + hq * HD + lane * kDims;
-        if (a.dtype == DVI_BF16) {
-          const uint32_t* p = reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(a.q) + off);
+        const uint32_t* p = static_cast<const uint32_t*>(a.q) +
+                            (static_cast<long long>(pc.row0 + row) * a.ld_q + hq * HD + lane * kDims) / (PAIR ? 1 : 2);
 #pragma unroll
-          for (int e = 0; e < kDims / 2; ++e) qx[i][2 * e] = bf16_lo(p[e]), qx[i][2 * e + 1] = bf16_hi(p[e]);
-        } else {
-          const float2* p = reinterpret_cast<const float2*>(static_cast<const float*>(a.q) + off);
-#pragma unroll
-          for (int e = 0; e < kDims / 2; ++e) qx[i][2 * e] = p[e].x, qx[i][2 * e + 1] = p[e].y;
-        }
+        for (int e = 0; e < (PAIR ? kDims : kDims / 2); ++e) qx[i][e] = p[e];
       }
     }
 
@@ -400,8 +406,8 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
 #pragma unroll
         for (int r = 0; r < kPaKeys / kRows; ++r) {
           const uint32_t dst = (r & 1 ? d1 : d0) + (r >> 1) * 2 * kRows * HD;
-          cp_async16(dst, src + r * kRows * HD);
-          cp_async16(dst + SH::kHalf, src + v_from_k + r * kRows * HD);
+          cp_async16(dst, src + r * kRows * HD, once);
+          cp_async16(dst + SH::kHalf, src + v_from_k + r * kRows * HD, once);
         }
       } else {
         const int live = pg >= 0 ? held_end - p - r0 : 0;          // rows past it, and pages not held: zeros
@@ -436,9 +442,13 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     for (int i = 0; i < kMine; ++i) {
       const int n = tw + i * S;
       if (n >= NV) continue;
+      float x[kDims];
+#pragma unroll
+      for (int e = 0; e < kDims; ++e)
+        x[e] = PAIR ? __uint_as_float(qx[i][PAIR ? e : 0]) : e & 1 ? bf16_hi(qx[i][e >> 1]) : bf16_lo(qx[i][e >> 1]);
       float top = 0.f;
 #pragma unroll
-      for (int e = 0; e < kDims; ++e) top = fmaxf(top, fabsf(qx[i][e]));
+      for (int e = 0; e < kDims; ++e) top = fmaxf(top, fabsf(x[e]));
       top = warp_max(top);
       // a power of two brings the largest element to [2^14, 2^15)
       const int ex = max(static_cast<int>(__float_as_uint(top) >> 23), 15);
@@ -450,7 +460,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
 #pragma unroll
       for (int e = 0; e < kDims; e += 2) {
         uint32_t hi, lo;
-        split_f16x2(qx[i][e] * up, qx[i][e + 1] * up, hi, lo);
+        split_f16x2(x[e] * up, x[e + 1] * up, hi, lo);
         *reinterpret_cast<uint32_t*>(at + e * 2) = hi;
         if (PAIR) *reinterpret_cast<uint32_t*>(at + NT * kSteps * 256 + e * 2) = lo;
       }
@@ -656,8 +666,10 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     cp_wait<0>();
     __syncwarp();
 
-    // ---------------- join: o[i][nt][e] is dim g HD/8 + 2 i + e / 2 of vector 8 nt + 2 t + e % 2
-    float* mine = reinterpret_cast<float*>(ring);                  // [NV][HD], maxima [NV], sums [NV]
+    // ---------------- join.  o[i][nt][e] is dim g HD/8 + 2 i + e / 2 of vector 8 nt + 2 t + e % 2; a warp's
+    // part lies in its ring as rows of [i][g] pairs, 8 floats apart from HD so that no bank meets twice
+    constexpr int kPart = HD + 8;
+    float* mine = reinterpret_cast<float*>(ring);                  // [NV][kPart], maxima [NV], sums [NV]
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -667,65 +679,69 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
         for (int off = 4; off < 32; off <<= 1) x += __shfl_xor_sync(0xffffffffu, x, off);
         const int n = nt * 8 + 2 * t + q;
         if (g == 0) {
-          mine[NV * HD + n] = m[nt][q];
-          mine[NV * HD + NV + n] = x;
+          mine[NV * kPart + n] = m[nt][q];
+          mine[NV * kPart + NV + n] = x;
         }
 #pragma unroll
         for (int i = 0; i < kSteps; ++i)
-          *reinterpret_cast<float2*>(mine + n * HD + g * (HD / 8) + 2 * i) = make_float2(o[i][nt][q], o[i][nt][q + 2]);
+          *reinterpret_cast<float2*>(mine + n * kPart + i * 16 + g * 2) = make_float2(o[i][nt][q], o[i][nt][q + 2]);
       }
     team_bar();
     const bool whole = pc.whole;
+    // a part in the workspace: [NV][HD / 32][8] quads of dims, maxima [NV], sums [NV]
     constexpr int kSlot = NV * (HD + 2);
-    // a share cuts at most two groups: the one it begins in, and the one it ends in
+    constexpr int kQuads = NV * HD / 4;
     float* slot = a.part + static_cast<size_t>(2 * team + (pc.cut ? 0 : 1)) * kSlot;
-    // Dims d .. d + 3 of vector v: the result, or this share's part of it.
-    auto emit = [&](int v, int d, float4 acc, float M, float L, bool final) {
-      if (final) {
-        if (v >= n_vec) return;
-        const float inv = L > 0.f ? 1.f / L : (L == L ? 0.f : L);
-        int hq;
-        const int row = row_of(v, hq);
-        const long long off = static_cast<long long>(pc.row0 + row) * a.ld_o + hq * HD + d;
-        if (a.dtype == DVI_BF16)
-          *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + off) =
-              make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
-        else
-          *reinterpret_cast<float4*>(static_cast<float*>(a.o) + off) =
-              make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    auto emit = [&](int i, float4 acc, float L) {                  // quad i: dims d .. d + 3 of vector v
+      const int v = i / (HD / 4), d = (i % 8) * (HD / 8) + i % (HD / 4) / 8 * 4;
+      if (v >= n_vec) return;
+      const float inv = L > 0.f ? __fdividef(1.f, L) : (L == L ? 0.f : L);
+      int hq;
+      const int row = row_of(v, hq);
+      const long long off = static_cast<long long>(pc.row0 + row) * a.ld_o + hq * HD + d;
+      if (PAIR)
+        *reinterpret_cast<float4*>(static_cast<float*>(a.o) + off) =
+            make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+      else
+        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + off) =
+            make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+    };
+    constexpr int kWarpFloats = ST * SH::kStage / 4;
+    const float* parts = reinterpret_cast<const float*>(sm) + in_cta * S * kWarpFloats;
+#pragma unroll 1
+    for (int i = tw * 32 + lane; i < kQuads; i += S * 32) {
+      const int v = i / (HD / 4);
+      const float* head = parts + NV * kPart + v;
+      const float* quad = parts + v * kPart + i % (HD / 4) / 8 * 32 + (i % 8) * 2;
+      float M = kPaUnset, L = 0.f;
+#pragma unroll 4
+      for (int w = 0; w < S; ++w) M = fmaxf(M, head[w * kWarpFloats]);
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+      for (int w = 0; w < S; ++w) {
+        const float f = pa_ex2(head[w * kWarpFloats] - M);
+        const float2 x = *reinterpret_cast<const float2*>(quad + w * kWarpFloats);
+        const float2 y = *reinterpret_cast<const float2*>(quad + w * kWarpFloats + 16);
+        acc.x = fmaf(x.x, f, acc.x), acc.y = fmaf(x.y, f, acc.y);
+        acc.z = fmaf(y.x, f, acc.z), acc.w = fmaf(y.y, f, acc.w);
+        L = fmaf(head[w * kWarpFloats + NV], f, L);
+      }
+      if (whole) {
+        emit(i, acc, L);
       } else {
-        __stcg(reinterpret_cast<float4*>(slot + v * HD + d), acc);
-        if (d == 0) {
+        __stcg(reinterpret_cast<float4*>(slot) + i, acc);
+        if (i % (HD / 4) == 0) {
           __stcg(slot + NV * HD + v, M);
           __stcg(slot + NV * HD + NV + v, L);
         }
       }
-    };
-    constexpr int kWarpFloats = ST * SH::kStage / 4;
-    const float* parts = reinterpret_cast<const float*>(sm) + in_cta * S * kWarpFloats;
-    for (int i = tw * 32 + lane; i < NV * HD / 4; i += S * 32) {
-      const int v = i / (HD / 4), d = (i % (HD / 4)) * 4;
-      float M = kPaUnset;
-      for (int w = 0; w < S; ++w) M = fmaxf(M, parts[w * kWarpFloats + NV * HD + v]);
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      float L = 0.f;
-#pragma unroll 4
-      for (int w = 0; w < S; ++w) {
-        const float* p = parts + w * kWarpFloats;
-        const float f = pa_ex2(p[NV * HD + v] - M);
-        const float4 x = *reinterpret_cast<const float4*>(p + v * HD + d);
-        acc.x = fmaf(x.x, f, acc.x), acc.y = fmaf(x.y, f, acc.y);
-        acc.z = fmaf(x.z, f, acc.z), acc.w = fmaf(x.w, f, acc.w);
-        L = fmaf(p[NV * HD + NV + v], f, L);
-      }
-      emit(v, d, acc, M, L, whole);
     }
     if (!whole) {
       // teams of the group: t0 .. t1; whoever of them counts last joins their parts in order
       const int t0 = team_of(pc.g_begin), t1 = team_of(pc.g_end - 1);
-      __threadfence();
       team_bar();
       if (tw == 0 && lane == 0) {
+        __threadfence();
         const int n = atomicAdd(a.counters + t0, 1);
         last_s[in_cta] = n == t1 - t0;
         if (n == t1 - t0) a.counters[t0] = 0;
@@ -734,25 +750,44 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
       team_bar();
       if (last_s[in_cta]) {
         const float* p0 = a.part + static_cast<size_t>(2 * t0 + 1) * kSlot;
-        const float* p1 = a.part + static_cast<size_t>(2 * t0 + 2) * kSlot;
+        const float* p1 = a.part + static_cast<size_t>(2 * t0) * kSlot;
         const int n = t1 - t0 + 1;
-        for (int i = tw * 32 + lane; i < NV * HD / 4; i += S * 32) {
-          const int v = i / (HD / 4), d = (i % (HD / 4)) * 4;
+#pragma unroll 1
+        for (int i = tw * 32 + lane; i < kQuads; i += S * 32) {
+          const int v = i / (HD / 4);
           float M = kPaUnset, L = 0.f;
           float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-          for (int k = 0; k < n; ++k) {
-            const float* p = k == 0 ? p0 : p1 + static_cast<size_t>(2 * (k - 1)) * kSlot;
-            const float pm = __ldcg(p + NV * HD + v), ps = __ldcg(p + NV * HD + NV + v);
-            const float4 x = __ldcg(reinterpret_cast<const float4*>(p + v * HD + d));
-            const float top = fmaxf(M, pm);
-            const float fa = pa_ex2(M - top), fb = pa_ex2(pm - top);
+          constexpr int kAtOnce = 6;
+#pragma unroll 1
+          for (int k0 = 0; k0 < n; k0 += kAtOnce) {
+            float pm[kAtOnce], ps[kAtOnce];
+            float4 x[kAtOnce];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+              const float* p = k0 + k == 0 ? p0 : p1 + static_cast<size_t>(2 * min(k0 + k, n - 1)) * kSlot;
+              pm[k] = __ldcg(p + NV * HD + v), ps[k] = __ldcg(p + NV * HD + NV + v);
+              x[k] = __ldcg(reinterpret_cast<const float4*>(p) + i);
+            }
+            float top = M;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+              if (k0 + k >= n) pm[k] = -INFINITY;
+              top = fmaxf(top, pm[k]);
+            }
+            const float shrink = pa_ex2(M - top);
             M = top;
-            acc.x = fmaf(x.x, fb, acc.x * fa), acc.y = fmaf(x.y, fb, acc.y * fa);
-            acc.z = fmaf(x.z, fb, acc.z * fa), acc.w = fmaf(x.w, fb, acc.w * fa);
-            L = fmaf(ps, fb, L * fa);
+            acc.x *= shrink, acc.y *= shrink, acc.z *= shrink, acc.w *= shrink, L *= shrink;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+              const float f = pa_ex2(pm[k] - top);
+              if (k0 + k < n) {
+                acc.x = fmaf(x[k].x, f, acc.x), acc.y = fmaf(x[k].y, f, acc.y);
+                acc.z = fmaf(x[k].z, f, acc.z), acc.w = fmaf(x[k].w, f, acc.w);
+                L = fmaf(ps[k], f, L);
+              }
+            }
           }
-          emit(v, d, acc, M, L, true);
+          emit(i, acc, L);
         }
       }
     }
@@ -765,9 +800,9 @@ template <bool E4M3, int HD, int NT, bool PAIR>
 cudaError_t launch_pa(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
   using SH = PaShape<HD, NT, PAIR>;
   // the units of all groups are counted in 32 bits
-  const long long tiles = static_cast<long long>(a.c.n_rows) * a.G / (8 * NT) + a.c.n_seqs;
+  const long long vecs = static_cast<long long>(a.c.n_rows) * a.G, tiles = vecs / (8 * NT) + a.c.n_seqs;
   const long long blocks = ((static_cast<long long>(a.c.max_pages) << a.c.log_p) / kPaKeys + 17) * a.c.H;
-  if (tiles * blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+  if (vecs > 0x7fffffffll || tiles * blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
   static PerDevice attr;
   attr.once([] {
     cudaFuncSetAttribute(paged_attend_kernel<E4M3, HD, NT, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
