@@ -38,6 +38,7 @@ namespace {
 
 constexpr int kPaKeys = 16;               // positions per block: never more than a page
 constexpr int kPaTeam = 4;                // warps of the smallest team
+constexpr int kPaOver = 4;                // steps of a warp that a group costs beside its blocks
 constexpr float kPaLazy = 8.f;            // growth of a maximum (base 2) that rescales the accumulator
 constexpr float kPaUp = 5.f;              // weights are at most 2^(kPaLazy + kPaUp): f16 keeps small ones exact
 constexpr float kPaMost = 8192.f;         // 2^(kPaLazy + kPaUp)
@@ -316,9 +317,9 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
       }
       if (fill > best + 0.2f) best = fill, S = s, n_teams = n;
     }
-    const int total = all.x + groups * S;
+    const int total = all.x + groups * S * kPaOver;
     if (lane == 0) {
-      plan_s.S = S, plan_s.over = S;
+      plan_s.S = S, plan_s.over = S * kPaOver;
       plan_s.n_teams = n_teams, plan_s.total = total;
       plan_s.share_q = n_teams > 0 ? total / n_teams : 0;
       plan_s.share_r = total - plan_s.share_q * n_teams;
@@ -801,7 +802,7 @@ cudaError_t launch_pa(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
   using SH = PaShape<HD, NT, PAIR>;
   // the units of all groups are counted in 32 bits
   const long long vecs = static_cast<long long>(a.c.n_rows) * a.G, tiles = vecs / (8 * NT) + a.c.n_seqs;
-  const long long blocks = ((static_cast<long long>(a.c.max_pages) << a.c.log_p) / kPaKeys + 17) * a.c.H;
+  const long long blocks = ((static_cast<long long>(a.c.max_pages) << a.c.log_p) / kPaKeys + 16 * kPaOver + 1) * a.c.H;
   if (vecs > 0x7fffffffll || tiles * blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
   static PerDevice attr;
   attr.once([] {
