@@ -116,38 +116,48 @@ __device__ __forceinline__ int paged_page(const PagedArgs& c, int b, int slot) {
 // from row_start[b] / unit + extra * b on, and has at most
 // (n_b - 1) / unit + 1 + (extra - 1) of them, so no two sequences overlap.
 // Every thread of the block calls it with the same item; -1: nobody's.
-__device__ __forceinline__ int paged_seq_of_item(const PagedArgs& c, int item, int unit, int extra, int* first) {
+__device__ __forceinline__ int paged_seq_of_item(const PagedArgs& c, int item, int log_unit, int extra, int* first) {
+  if (!c.row_start) {
+    const int per = c.n_rows / c.n_seqs;
+    auto begin = [&](int b) { return ((b * per) >> log_unit) + extra * b; };
+    int b = static_cast<int>(__fdividef(static_cast<float>(item) * static_cast<float>(1 << log_unit),
+                                        static_cast<float>(per) + static_cast<float>(extra << log_unit)));
+    b = min(b, c.n_seqs - 1);
+    while (b > 0 && begin(b) > item) --b;
+    while (b + 1 < c.n_seqs && begin(b + 1) <= item) ++b;
+    *first = begin(b);
+    return b;
+  }
   int n = 0;
   for (int b0 = 0; b0 < c.n_seqs; b0 += blockDim.x) {
     const int b = b0 + static_cast<int>(threadIdx.x);
     int begin = 0x7fffffff;
-    if (b < c.n_seqs) {
-      const int r0 = c.row_start ? c.row_start[b] : b * (c.n_rows / c.n_seqs);
-      begin = min(max(r0, 0), c.n_rows) / unit + extra * b;
-    }
+    if (b < c.n_seqs) begin = (min(max(c.row_start[b], 0), c.n_rows) >> log_unit) + extra * b;
     n += __syncthreads_count(begin <= item);
   }
   const int b = n - 1;
-  if (b >= 0) {
-    const int r0 = c.row_start ? c.row_start[b] : b * (c.n_rows / c.n_seqs);
-    *first = min(max(r0, 0), c.n_rows) / unit + extra * b;
-  }
+  if (b >= 0) *first = (min(max(c.row_start[b], 0), c.n_rows) >> log_unit) + extra * b;
   return b;
 }
 
 // ---------------------------------------------------------------- codes
 template <bool E4M3> struct Code;
+// int8: adding 1.5 * 2^23 rounds |x| < 2^22 to the nearest integer (ties to
+// even) and leaves it in the low bits; the byte with its sign bit turned is
+// code + 128, and 0x4b000000 | byte is the f32 number 2^23 + byte.
 template <> struct Code<false> {
   static constexpr float kTop = 127.f;
-  static __device__ __forceinline__ uint32_t enc(float x) {   // finite or infinite, not NaN
-    return static_cast<uint32_t>(__float2int_rn(fminf(fmaxf(x, -127.f), 127.f))) & 0xffu;
-  }
-  static __device__ __forceinline__ uint32_t enc4(float a, float b, float c, float d) {
-    return enc(a) | (enc(b) << 8) | (enc(c) << 16) | (enc(d) << 24);
+  static __device__ __forceinline__ uint32_t enc4(float a, float b, float c, float d) {   // |x| < 128
+    const float r = 12582912.f;
+    const uint32_t ab = __byte_perm(__float_as_uint(__fadd_rn(a, r)), __float_as_uint(__fadd_rn(b, r)), 0x0040);
+    const uint32_t cd = __byte_perm(__float_as_uint(__fadd_rn(c, r)), __float_as_uint(__fadd_rn(d, r)), 0x0040);
+    return __byte_perm(ab, cd, 0x5410);
   }
   static __device__ __forceinline__ void dec4(uint32_t w, float (&x)[4]) {
+    const uint32_t u = w ^ 0x80808080u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = static_cast<float>(static_cast<int8_t>(w >> (8 * i)));
+    for (int i = 0; i < 4; ++i)
+      x[i] = __fsub_rn(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440 | i)), 8388736.f);
   }
 };
 // Four e4m3 codes as two f16 pairs (exact).

@@ -24,16 +24,19 @@ namespace {
 
 constexpr int kApThreads = 256;
 constexpr int kApItems = 4;            // 16-element items a thread holds
-constexpr int kApQSteps = 2;           // 32-item steps of a query warp
 
-template <typename T>
-__device__ __forceinline__ void rotate8(float (&a)[8], float (&b)[8], const float2* cs) {
+// The (cos, sin) pairs of 8 dims.
+struct Turn {
   float4 w[4];
+  __device__ __forceinline__ void load(const float2* cs) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = __ldg(reinterpret_cast<const float4*>(cs) + i);
+    for (int i = 0; i < 4; ++i) w[i] = __ldg(reinterpret_cast<const float4*>(cs) + i);
+  }
+};
+__device__ __forceinline__ void rotate8(float (&a)[8], float (&b)[8], const Turn& t) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float co = i & 1 ? w[i >> 1].z : w[i >> 1].x, si = i & 1 ? w[i >> 1].w : w[i >> 1].y;
+    const float co = i & 1 ? t.w[i >> 1].z : t.w[i >> 1].x, si = i & 1 ? t.w[i >> 1].w : t.w[i >> 1].y;
     const float x = __fsub_rn(__fmul_rn(a[i], co), __fmul_rn(b[i], si));
     const float y = __fadd_rn(__fmul_rn(b[i], co), __fmul_rn(a[i], si));
     a[i] = x;
@@ -70,7 +73,7 @@ __device__ void append_page(const PagedAppendArgs& a, int item, int group) {
   __shared__ float red[kApThreads / 32];
   const PagedArgs& c = a.c;
   int first = 0;
-  const int b = paged_seq_of_item(c, item, c.P, 2, &first);
+  const int b = paged_seq_of_item(c, item, c.log_p, 2, &first);
   if (b < 0) return;
   const PagedSeq sq = paged_seq(c, b);
   const int slot = (sq.len >> c.log_p) + item - first;
@@ -97,8 +100,7 @@ __device__ void append_page(const PagedAppendArgs& a, int item, int group) {
   constexpr int kPer = D / 16;                                    // items of a row
   const int n_items = (p1 - p0) * kPer;
   float x[kApItems][16];
-  float most = 0.f;
-  bool odd = false;
+  float most = 0.f, odd = 0.f;                                    // odd: NaN where some value is not finite
 #pragma unroll
   for (int u = 0; u < kApItems; ++u) {
     const int it = u * TEAM + t;
@@ -112,20 +114,36 @@ __device__ void append_page(const PagedAppendArgs& a, int item, int group) {
     ld8(row + db, hi);
     if (8 * j < rot / 2) {
       const int pos = p0 + r;
-      if (pos < a.n_pos) rotate8<T>(lo, hi, a.rotary + static_cast<size_t>(pos) * (rot / 2) + 8 * j);
-      else if (j == 0) flag_status(c.status, DVI_DEV_KV_FULL);
+      if (pos < a.n_pos) {
+        Turn turn;
+        turn.load(a.rotary + static_cast<size_t>(pos) * (rot / 2) + 8 * j);
+        rotate8(lo, hi, turn);
+      } else if (j == 0) {
+        flag_status(c.status, DVI_DEV_KV_FULL);
+      }
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      float v = i < 8 ? lo[i & 7] : hi[i & 7];
-      if (v != v) v = 0.f, odd = true;
-      const float m = fabsf(v);
-      if (m <= 3.402823466e38f) most = fmaxf(most, m);
-      else odd = true;
+      const float v = i < 8 ? lo[i & 7] : hi[i & 7];
+      most = fmaxf(most, fabsf(v));
+      odd = fmaf(v, 0.f, odd);
       x[u][i] = v;
     }
   }
-  if (odd) flag_status(c.status, DVI_DEV_NONFINITE);
+  if (odd != odd) {
+    // NaN becomes 0, an infinity the largest code; neither counts for the scale
+    flag_status(c.status, DVI_DEV_NONFINITE);
+    most = 0.f;
+#pragma unroll
+    for (int u = 0; u < kApItems; ++u) {
+      if (u * TEAM + t >= n_items) continue;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        if (x[u][i] != x[u][i]) x[u][i] = 0.f;
+        else if (fabsf(x[u][i]) <= 3.402823466e38f) most = fmaxf(most, fabsf(x[u][i]));
+      }
+    }
+  }
   most = team_max<TEAM>(most, red, team, t);
   float s = fmaxf(__fmul_rn(most, 1.f / Code<E4M3>::kTop), kPagedMinScale);
   if (held > 0) s = fmaxf(s, old);
@@ -143,6 +161,10 @@ __device__ void append_page(const PagedAppendArgs& a, int item, int group) {
     float y[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) y[i] = __fmul_rn(x[u][i], inv);
+    if (odd != odd) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) y[i] = fminf(fmaxf(y[i], -Code<E4M3>::kTop), Code<E4M3>::kTop);
+    }
     using C = Code<E4M3>;
     *reinterpret_cast<uint2*>(row + da) = make_uint2(C::enc4(y[0], y[1], y[2], y[3]), C::enc4(y[4], y[5], y[6], y[7]));
     *reinterpret_cast<uint2*>(row + db) =
@@ -166,9 +188,10 @@ __device__ void append_page(const PagedAppendArgs& a, int item, int group) {
   }
 }
 
-// Queries: a warp takes one row and kApQSteps * 32 items of its heads.
+// Queries: a warp takes one row and `steps` * 32 items of its heads; a lane's
+// dims are the same in every head, so it reads its (cos, sin) once.
 template <int D, typename T>
-__device__ void rotate_queries(const PagedAppendArgs& a, int warp_task, int parts) {
+__device__ void rotate_queries(const PagedAppendArgs& a, int warp_task, int parts, int steps) {
   const PagedArgs& c = a.c;
   const int lane = threadIdx.x & 31;
   const int r = warp_task / parts, part = warp_task % parts;
@@ -190,35 +213,38 @@ __device__ void rotate_queries(const PagedAppendArgs& a, int warp_task, int part
   if (i < 0 || i >= sq.n) return;
   const int pos = sq.len + i;
   constexpr int kPer = D / 16;
-  const int total = a.n_heads * kPer;
-#pragma unroll
-  for (int u = 0; u < kApQSteps; ++u) {
-    const int it = (part * kApQSteps + u) * 32 + lane;
-    if (it >= total) continue;
-    const int h = it / kPer, j = it % kPer;
-    int da, db;
-    item_dims(j, a.rot, D, da, db);
-    const T* row = static_cast<const T*>(a.q) + static_cast<long long>(r) * a.ld_q + h * D;
-    T* out = static_cast<T*>(a.q_out) + static_cast<long long>(r) * a.ld_qo + h * D;
+  const int j = lane % kPer, total = a.n_heads * kPer;
+  int da, db;
+  item_dims(j, a.rot, D, da, db);
+  const bool turns = 8 * j < a.rot / 2 && pos < a.n_pos;
+  if (pos >= a.n_pos && a.rot > 0 && lane == 0) flag_status(c.status, DVI_DEV_KV_FULL);
+  Turn turn;
+  if (turns) turn.load(a.rotary + static_cast<size_t>(pos) * (a.rot / 2) + 8 * j);
+  const T* row = static_cast<const T*>(a.q) + static_cast<long long>(r) * a.ld_q;
+  T* out = static_cast<T*>(a.q_out) + static_cast<long long>(r) * a.ld_qo;
+#pragma unroll 4
+  for (int u = part * steps; u < (part + 1) * steps; ++u) {
+    const int it = u * 32 + lane;
+    if (it >= total) break;
+    const int h = it / kPer * D;
     float lo[8], hi[8];
-    ld8(row + da, lo);
-    ld8(row + db, hi);
-    if (8 * j < a.rot / 2 && pos < a.n_pos)
-      rotate8<T>(lo, hi, a.rotary + static_cast<size_t>(pos) * (a.rot / 2) + 8 * j);
-    st8(out + da, lo);
-    st8(out + db, hi);
+    ld8(row + h + da, lo);
+    ld8(row + h + db, hi);
+    if (turns) rotate8(lo, hi, turn);
+    st8(out + h + da, lo);
+    st8(out + h + db, hi);
   }
 }
 
 template <bool E4M3, int D, typename T, int TEAM>
 __global__ void __launch_bounds__(kApThreads) paged_append_kernel(const __grid_constant__ PagedAppendArgs a,
-                                                                  int n_items, int groups, int parts) {
+                                                                  int n_items, int groups, int parts, int steps) {
   griddep_wait();
   griddep_launch();
   const int bid = static_cast<int>(blockIdx.x);
   const int pages = n_items * groups;
   if (bid < pages) append_page<E4M3, D, T, TEAM>(a, bid / groups, bid % groups);
-  else rotate_queries<D, T>(a, (bid - pages) * (kApThreads / 32) + static_cast<int>(threadIdx.x >> 5), parts);
+  else rotate_queries<D, T>(a, (bid - pages) * (kApThreads / 32) + static_cast<int>(threadIdx.x >> 5), parts, steps);
 }
 
 template <bool E4M3, int D, typename T, int TEAM>
@@ -226,12 +252,15 @@ cudaError_t launch_append(const PagedAppendArgs& a, cudaStream_t s) {
   const PagedArgs& c = a.c;
   const long long n_items = static_cast<long long>(c.n_rows >> c.log_p) + 2ll * c.n_seqs;
   const int teams = kApThreads / TEAM, groups = (2 * c.H + teams - 1) / teams;
-  const int parts = a.q ? (a.n_heads * (D / 16) + 32 * kApQSteps - 1) / (32 * kApQSteps) : 0;
+  // a warp for all heads of a row where the rows alone fill the GPU, else for 64 items
+  const int all_steps = (a.n_heads * (D / 16) + 31) / 32;
+  const int steps = c.n_rows >= 4096 ? std::min(all_steps, 16) : std::min(all_steps, 2);
+  const int parts = a.q ? (all_steps + steps - 1) / steps : 0;
   const long long q_blocks = (static_cast<long long>(c.n_rows) * parts + kApThreads / 32 - 1) / (kApThreads / 32);
   const long long blocks = n_items * groups + q_blocks;
   if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
   return launch_pdl(paged_append_kernel<E4M3, D, T, TEAM>, dim3(static_cast<unsigned>(blocks)), dim3(kApThreads), 0, s,
-                    a, static_cast<int>(n_items), groups, parts);
+                    a, static_cast<int>(n_items), groups, parts, steps);
 }
 // A team holds kApItems items a thread: the rows of one page, as far as one
 // sequence's rows go.
@@ -250,9 +279,10 @@ cudaError_t append_types(const PagedAppendArgs& a, cudaStream_t s) {
 }
 
 // ---------------------------------------------------------------- read
-// A block takes one page slot of one sequence and kRdWarps (head, K or V)
-// pairs: a warp copies the slot's rows, 16 codes a lane and step.
-constexpr int kRdWarps = 8;
+// A warp copies 16 positions (never more than a page) of one KV head of K or
+// V, all its codes in flight at once; a block takes kRdWarps such tasks of the
+// same positions.
+constexpr int kRdWarps = 8, kRdLog = 4;
 
 template <bool E4M3, int D, typename T>
 __global__ void __launch_bounds__(kRdWarps * 32) paged_read_kernel(const __grid_constant__ PagedReadArgs a, int groups) {
@@ -261,45 +291,47 @@ __global__ void __launch_bounds__(kRdWarps * 32) paged_read_kernel(const __grid_
   const PagedArgs& c = a.c;
   const int item = static_cast<int>(blockIdx.x) / groups, group = static_cast<int>(blockIdx.x) % groups;
   int first = 0;
-  const int b = paged_seq_of_item(c, item, c.P, 2, &first);
+  const int b = paged_seq_of_item(c, item, kRdLog, 2, &first);
   if (b < 0) return;
   const PagedSeq sq = paged_seq(c, b);
-  const int slot = (sq.len >> c.log_p) + item - first;
-  const int page0 = slot << c.log_p;
-  const int p0 = max(sq.len, page0), p1 = min(sq.len + sq.n, page0 + c.P);
+  const int slot = (sq.len >> kRdLog) + item - first;
+  const int begin = slot << kRdLog;
+  const int p0 = max(sq.len, begin), p1 = min(sq.len + sq.n, begin + (1 << kRdLog));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int task = group * kRdWarps + warp;
   if (p0 >= p1 || task >= 2 * c.H) return;
   const bool is_v = task >= c.H;
   const int h = is_v ? task - c.H : task;
-  const int page = paged_page(c, b, slot);
+  const int page = paged_page(c, b, p0 >> c.log_p);
   const size_t ph = static_cast<size_t>(max(page, 0)) * c.H + h;
-  const float s = page < 0 ? 0.f : (is_v ? c.v_scale : c.k_scale)[ph];
-  constexpr int kPer = D / 16;
-  const uint4* codes =
-      reinterpret_cast<const uint4*>((is_v ? c.v : c.k) + ((ph << c.log_p) + static_cast<size_t>(p0 - page0)) * D);
-  T* out = static_cast<T*>(is_v ? a.v_out : a.k_out);
-  const size_t row0 = static_cast<size_t>(sq.row0 + p0 - sq.len);
+  constexpr int kPer = D / 16, kSteps = (16 << kRdLog) * kPer / 16 / 32;
+  const uint4* codes = reinterpret_cast<const uint4*>((is_v ? c.v : c.k) +
+                                                      ((ph << c.log_p) + static_cast<size_t>(p0 & (c.P - 1))) * D);
   const int n = (p1 - p0) * kPer;
-#pragma unroll 4
-  for (int i = lane; i < n; i += 32) {
-    const uint4 q = page < 0 ? make_uint4(0u, 0u, 0u, 0u) : __ldg(codes + i);
-    const int r = i / kPer, j = i % kPer;
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-    float x[16];
+  uint4 q[kSteps];
+#pragma unroll
+  for (int u = 0; u < kSteps; ++u) {
+    const int i = u * 32 + lane;
+    q[u] = page >= 0 && i < n ? __ldg(codes + i) : make_uint4(0u, 0u, 0u, 0u);
+  }
+  const float s = page < 0 ? 0.f : (is_v ? c.v_scale : c.k_scale)[ph];
+  T* out = static_cast<T*>(is_v ? a.v_out : a.k_out) + (static_cast<size_t>(sq.row0 + p0 - sq.len) * c.H + h) * D;
+#pragma unroll
+  for (int u = 0; u < kSteps; ++u) {
+    const int i = u * 32 + lane;
+    if (i >= n) break;
+    const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+    float x[2][8];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       float v[4];
       Code<E4M3>::dec4(w[e], v);
 #pragma unroll
-      for (int f = 0; f < 4; ++f) x[4 * e + f] = __fmul_rn(v[f], s);
+      for (int f = 0; f < 4; ++f) x[e >> 1][(e & 1) * 4 + f] = __fmul_rn(v[f], s);
     }
-    T* dst = out + ((row0 + r) * c.H + h) * D + 16 * j;
-    float lo[8], hi[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) lo[e] = x[e], hi[e] = x[8 + e];
-    st8(dst, lo);
-    st8(dst + 8, hi);
+    T* dst = out + static_cast<size_t>(i / kPer) * c.H * D + 16 * (i % kPer);
+    st8(dst, x[0]);
+    st8(dst + 8, x[1]);
   }
 }
 
@@ -307,7 +339,7 @@ template <bool E4M3, int D, typename T>
 cudaError_t launch_read(const PagedReadArgs& a, cudaStream_t s) {
   const PagedArgs& c = a.c;
   const int groups = (2 * c.H + kRdWarps - 1) / kRdWarps;
-  const long long blocks = (static_cast<long long>(c.n_rows >> c.log_p) + 2ll * c.n_seqs) * groups;
+  const long long blocks = (static_cast<long long>(c.n_rows >> kRdLog) + 2ll * c.n_seqs) * groups;
   if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
   return launch_pdl(paged_read_kernel<E4M3, D, T>, dim3(static_cast<unsigned>(blocks)), dim3(kRdWarps * 32), 0, s, a,
                     groups);

@@ -4,6 +4,7 @@ on the caller's current stream (or the one it names)."""
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import Optional, Tuple
 
 import torch
@@ -30,6 +31,13 @@ class PagedBatchC(ctypes.Structure):
 class PagedOptionsC(ctypes.Structure):
     _fields_ = [("n_heads", ctypes.c_int), ("scale", ctypes.c_float), ("softcap", ctypes.c_float),
                 ("window", ctypes.c_int), ("slopes", ctypes.c_void_p)]
+
+
+# PagedBatchC and PagedOptionsC as bytes: a pack is a fraction of a ctypes structure's cost, and a decode step's
+# calls are short enough to notice
+_BATCH = struct.Struct("@4i4Q")
+_OPTIONS = struct.Struct("@iffiQ")
+assert _BATCH.size == ctypes.sizeof(PagedBatchC) and _OPTIONS.size == ctypes.sizeof(PagedOptionsC)
 
 
 def rotary_table(n_pos: int, rot_dim: int, theta: float = 10000.0, device="cuda") -> torch.Tensor:
@@ -76,10 +84,12 @@ class PagedCache:
         self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = n_pages, H, P, D
         self.device = k.device
         self._index = k.device.index
+        self._one_device = torch.cuda.device_count() == 1
         self.status_word = torch.zeros(1, dtype=torch.int32, device=k.device)
         self._c = PagedCacheC(n_pages, H, P, D, KV_FORMATS[fmt], k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
                               v_scale.data_ptr())
         self._cref = ctypes.byref(self._c)
+        self._status_ptr = self.status_word.data_ptr()
         self._lib = lib()
         self._workspaces = {}
 
@@ -96,54 +106,55 @@ class PagedCache:
 
     # -- marshalling ------------------------------------------------------
     def _batch(self, what, table, lens, n_rows, row_start, max_rows):
-        if table.dtype != torch.int32 or lens.dtype != torch.int32 or table.dim() != 2:
+        """dvi_paged_batch of a call, as bytes."""
+        i32, dev = torch.int32, self._index
+        if table.dtype is not i32 or lens.dtype is not i32 or table.dim() != 2:
             raise ValueError(f"{what}: table must be int32 [B, max_pages] and lens int32 [B]")
         B, width = table.shape
         if lens.shape != (B,) or not (table.is_contiguous() and lens.is_contiguous()):
             raise ValueError(f"{what}: table and lens must be contiguous, with one row and one length a sequence")
-        if table.device != self.device or lens.device != self.device:
+        if table.get_device() != dev or lens.get_device() != dev:
             raise ValueError(f"{what}: table and lens must be on {self.device}")
-        start = None
+        if not 1 <= B <= 1024 or not 1 <= width <= (1 << 30) // self.page_tokens:
+            raise ValueError(f"{what}: 1 to 1024 sequences of 1 to {(1 << 30) // self.page_tokens} pages")
+        start = 0
         if row_start is None:
-            if B < 1 or n_rows % B:
+            if n_rows % B:
                 raise ValueError(f"{what}: {n_rows} rows do not divide into {B} sequences (give row_start)")
             max_rows = n_rows // B
         else:
-            if row_start.dtype != torch.int32 or row_start.shape != (B + 1,) or not row_start.is_contiguous() or \
-                    row_start.device != self.device:
+            if row_start.dtype is not i32 or row_start.shape != (B + 1,) or not row_start.is_contiguous() or \
+                    row_start.get_device() != dev:
                 raise ValueError(f"{what}: row_start must be contiguous int32 [B + 1] on {self.device}")
             start = row_start.data_ptr()
-            max_rows = n_rows if max_rows is None else max_rows
+            max_rows = n_rows if max_rows is None else min(max_rows, n_rows)
             if max_rows < 0:
                 raise ValueError(f"{what}: max_rows must not be negative")
-        if not 1 <= B <= 1024 or width < 1 or width * self.page_tokens > 1 << 30:
-            raise ValueError(f"{what}: 1 to 1024 sequences of 1 to {(1 << 30) // self.page_tokens} pages")
-        return PagedBatchC(B, width, n_rows, max_rows, table.data_ptr(), lens.data_ptr(), start,
-                           self.status_word.data_ptr())
+        return _BATCH.pack(B, width, n_rows, max_rows, table.data_ptr(), lens.data_ptr(), start, self._status_ptr)
 
-    def _rows(self, what, t, heads, dtype, n_rows):
-        """Elements from row to row of t [n_rows, heads, head_dim], whose rows may lie apart."""
-        if t.dtype != dtype or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != self.head_dim or \
-                t.shape[0] != n_rows:
-            raise ValueError(f"{what} must be {dtype} [{n_rows}, {heads}, {self.head_dim}], got {t.dtype} "
-                             f"{tuple(t.shape)}")
+    def _rows(self, what, t, heads, dtype, esz, n_rows):
+        """Elements from row to row of t [n_rows, heads, head_dim], whose rows may lie apart, and its address."""
+        D = self.head_dim
+        if t.dtype is not dtype or t.shape != (n_rows, heads, D):
+            raise ValueError(f"{what} must be {dtype} [{n_rows}, {heads}, {D}], got {t.dtype} {tuple(t.shape)}")
         ld, sh, sd = t.stride()
         if n_rows <= 1:
-            ld = heads * self.head_dim
-        if sd != 1 or (sh != self.head_dim and heads > 1) or ld < heads * self.head_dim:
+            ld = heads * D
+        if sd != 1 or (sh != D and heads > 1) or ld < heads * D:
             raise ValueError(f"{what}: each row's heads must be contiguous")
-        if t.device != self.device:
+        if t.get_device() != self._index:
             raise ValueError(f"{what} must be on {self.device}")
-        if t.data_ptr() % 16 or ld * t.element_size() % 16:
+        p = t.data_ptr()
+        if p % 16 or ld * esz % 16:
             raise ValueError(f"{what}: rows must start on 16-byte boundaries")
-        return ld
+        return ld, p
 
-    def _call(self, what, fn, stream, *args):
-        if self._index != torch.cuda.current_device():
-            with torch.cuda.device(self._index):
-                rc = fn(*args, stream)
+    def _call(self, what, fn, *args):
+        if self._one_device or self._index == torch.cuda.current_device():
+            rc = fn(*args)
         else:
-            rc = fn(*args, stream)
+            with torch.cuda.device(self._index):
+                rc = fn(*args)
         if rc != 0:
             raise DVIError(f"{what}: {STATUS.get(rc, rc)}")
 
@@ -158,16 +169,18 @@ class PagedCache:
         """Write rows k, v [n, H_kv, head_dim] (bf16 or f32) behind lens, the keys rotated by `rotary`
         ([n_pos, rot_dim / 2, 2], see rotary_table) at their positions.  Returns q [n, H_q, head_dim]
         rotated alike (into q_out, which may be q), or None without q."""
-        if k.dtype not in _TYPES:
-            raise ValueError("append: k must be bfloat16 or float32")
-        n = k.shape[0]
+        td = k.dtype
+        if td not in _TYPES or k.dim() != 3:
+            raise ValueError("append: k must be bfloat16 or float32 [n, H_kv, head_dim]")
+        code, esz = _TYPES[td]
+        n, H = k.shape[0], self.n_kv_heads
         bt = self._batch("append", table, lens, n, row_start, max_rows)
-        ld_k = self._rows("append: k", k, self.n_kv_heads, k.dtype, n)
-        ld_v = self._rows("append: v", v, self.n_kv_heads, k.dtype, n)
+        ld_k, k_p = self._rows("append: k", k, H, td, esz, n)
+        ld_v, v_p = self._rows("append: v", v, H, td, esz, n)
         rot_p, rot_dim, n_pos = None, 0, 0
         if rotary is not None:
-            if rotary.dtype != torch.float32 or rotary.dim() != 3 or rotary.shape[2] != 2 or \
-                    not rotary.is_contiguous() or rotary.device != self.device or rotary.data_ptr() % 16:
+            if rotary.dtype is not torch.float32 or rotary.dim() != 3 or rotary.shape[2] != 2 or \
+                    not rotary.is_contiguous() or rotary.get_device() != self._index or rotary.data_ptr() % 16:
                 raise ValueError(f"append: rotary must be contiguous float32 [n_pos, rot_dim / 2, 2] on {self.device}")
             n_pos, rot_dim = rotary.shape[0], 2 * rotary.shape[1]
             if rot_dim % 16 or not 16 <= rot_dim <= self.head_dim or n_pos < 1:
@@ -179,16 +192,14 @@ class PagedCache:
             if q.dim() != 3 or q.shape[1] < 1:
                 raise ValueError("append: q must be [n, H_q, head_dim]")
             heads = q.shape[1]
-            ld_q = self._rows("append: q", q, heads, k.dtype, n)
+            ld_q, q_p = self._rows("append: q", q, heads, td, esz, n)
             if q_out is None:
-                q_out = torch.empty((n, heads, self.head_dim), dtype=k.dtype, device=self.device)
-            ld_o = self._rows("append: q_out", q_out, heads, k.dtype, n)
-            q_p, o_p = q.data_ptr(), q_out.data_ptr()
+                q_out = torch.empty((n, heads, self.head_dim), dtype=td, device=self.device)
+            ld_o, o_p = self._rows("append: q_out", q_out, heads, td, esz, n)
         elif q_out is not None:
             raise ValueError("append: q_out without q")
-        self._call("append", self._lib.dvi_paged_append, self._stream(stream), self._cref, ctypes.byref(bt),
-                   _TYPES[k.dtype][0], k.data_ptr(), ld_k, v.data_ptr(), ld_v, rot_p, rot_dim, n_pos, q_p, ld_q, o_p,
-                   ld_o, heads)
+        self._call("append", self._lib.dvi_paged_append, self._cref, bt, code, k_p, ld_k, v_p, ld_v, rot_p, rot_dim,
+                   n_pos, q_p, ld_q, o_p, ld_o, heads, self._stream(stream))
         return q_out
 
     def attend(self, table: torch.Tensor, lens: torch.Tensor, q: torch.Tensor, scale: Optional[float] = None,
@@ -198,27 +209,31 @@ class PagedCache:
         """Attention of rows q [n, H_q, head_dim] (bf16 or f32), appended before at the same lens: the row at
         position p sees the held positions up to p (the last `window` of them).  scale: head_dim^-0.5 unless
         given; softcap c > 0: scores become c tanh(score / c); slopes f32 [H_q]: + slope (p_key - p)."""
-        if q.dtype not in _TYPES or q.dim() != 3:
+        td = q.dtype
+        if td not in _TYPES or q.dim() != 3:
             raise ValueError("attend: q must be bfloat16 or float32 [n, H_q, head_dim]")
+        code, esz = _TYPES[td]
         n, heads = q.shape[0], q.shape[1]
         if heads < 1 or heads % self.n_kv_heads:
             raise ValueError(f"attend: {heads} heads do not divide over {self.n_kv_heads} KV heads")
         bt = self._batch("attend", table, lens, n, row_start, max_rows)
-        ld_q = self._rows("attend: q", q, heads, q.dtype, n)
+        ld_q, q_p = self._rows("attend: q", q, heads, td, esz, n)
         if out is None:
-            out = torch.empty((n, heads, self.head_dim), dtype=q.dtype, device=self.device)
-        ld_o = self._rows("attend: out", out, heads, q.dtype, n)
-        if slopes is not None and (slopes.dtype != torch.float32 or slopes.shape != (heads,) or
-                                   not slopes.is_contiguous() or slopes.device != self.device):
-            raise ValueError(f"attend: slopes must be contiguous float32 [{heads}] on {self.device}")
+            out = torch.empty((n, heads, self.head_dim), dtype=td, device=self.device)
+        ld_o, o_p = self._rows("attend: out", out, heads, td, esz, n)
+        slopes_p = 0
+        if slopes is not None:
+            if slopes.dtype is not torch.float32 or slopes.shape != (heads,) or not slopes.is_contiguous() or \
+                    slopes.get_device() != self._index:
+                raise ValueError(f"attend: slopes must be contiguous float32 [{heads}] on {self.device}")
+            slopes_p = slopes.data_ptr()
         scale = self.head_dim ** -0.5 if scale is None else scale
         if not 0.0 < scale < 1e30 or not 0.0 <= softcap < 1e30 or not 0 <= window < 1 << 31:
             raise ValueError("attend: needs scale > 0, softcap >= 0 and window >= 0")
-        opt = PagedOptionsC(heads, scale, softcap, window, None if slopes is None else slopes.data_ptr())
         s = self._stream(stream)
-        ws = self._workspace(s)
-        self._call("attend", self._lib.dvi_paged_attend, s, self._cref, ctypes.byref(bt), ctypes.byref(opt),
-                   _TYPES[q.dtype][0], q.data_ptr(), ld_q, out.data_ptr(), ld_o, ws.data_ptr(), ws.numel())
+        ws, ws_p, ws_n = self._workspaces.get(s) or self._workspace(s)
+        self._call("attend", self._lib.dvi_paged_attend, self._cref, bt,
+                   _OPTIONS.pack(heads, scale, softcap, window, slopes_p), code, q_p, ld_q, o_p, ld_o, ws_p, ws_n, s)
         return out
 
     def read(self, table: torch.Tensor, lens: torch.Tensor, n_rows: int, row_start: Optional[torch.Tensor] = None,
@@ -228,11 +243,13 @@ class PagedCache:
         (k, v) [n_rows, H_kv, head_dim] in dtype; zeros where no page is held."""
         if dtype not in _TYPES:
             raise ValueError("read: dtype must be bfloat16 or float32")
+        code, esz = _TYPES[dtype]
+        H, D = self.n_kv_heads, self.head_dim
         bt = self._batch("read", table, lens, n_rows, row_start, max_rows)
-        out = torch.empty((2, n_rows, self.n_kv_heads, self.head_dim), dtype=dtype, device=self.device)
-        k, v = out[0], out[1]
-        self._call("read", self._lib.dvi_paged_read, self._stream(stream), self._cref, ctypes.byref(bt),
-                   _TYPES[dtype][0], k.data_ptr(), v.data_ptr())
+        k = torch.empty((n_rows, H, D), dtype=dtype, device=self.device)
+        v = torch.empty((n_rows, H, D), dtype=dtype, device=self.device)
+        self._call("read", self._lib.dvi_paged_read, self._cref, bt, code, k.data_ptr(), v.data_ptr(),
+                   self._stream(stream))
         return k, v
 
     def status(self) -> list:
@@ -242,15 +259,15 @@ class PagedCache:
             self.status_word.zero_()
         return [name for bit, name in DEV_BITS.items() if word & bit]
 
-    def _workspace(self, stream: int) -> torch.Tensor:
-        """attend's workspace, one for each stream (calls on different streams may overlap)."""
-        ws = self._workspaces.get(stream)
-        if ws is None:
-            with torch.cuda.device(self._index):
-                n = self._lib.dvi_paged_workspace_bytes(self.head_dim)
-                ws = torch.zeros(n, dtype=torch.uint8, device=self.device)
-                # memory made inside a capture is the graph's: it serves this call only
-                if not torch.cuda.is_current_stream_capturing():
-                    torch.cuda.current_stream(self._index).synchronize()   # zeroed for whichever stream asks
-                    self._workspaces[stream] = ws
-        return ws
+    def _workspace(self, stream: int):
+        """attend's workspace, one for each stream (calls on different streams may overlap): the tensor, its
+        address and its size."""
+        with torch.cuda.device(self._index):
+            n = self._lib.dvi_paged_workspace_bytes(self.head_dim)
+            ws = torch.zeros(n, dtype=torch.uint8, device=self.device)
+            got = (ws, ws.data_ptr(), n)
+            # memory made inside a capture is the graph's: it serves this call only
+            if not torch.cuda.is_current_stream_capturing():
+                torch.cuda.current_stream(self._index).synchronize()   # zeroed for whichever stream asks
+                self._workspaces[stream] = got
+        return got
