@@ -82,38 +82,48 @@ __device__ void append_page(const PagedAppendArgs& a, int item, int group) {
   const int team = threadIdx.x / TEAM, t = threadIdx.x % TEAM;
   const int task = group * (kApThreads / TEAM) + team;
   if (p0 >= p1 || task >= 2 * c.H) return;                        // uniform over a team
-  const int page = paged_page(c, b, slot);
+  const bool is_v = task >= c.H;
+  const int h = is_v ? task - c.H : task;
+  const T* in = static_cast<const T*>(is_v ? a.vin : a.kin) + h * D;
+  const long long ld = is_v ? a.ld_v : a.ld_k;
+  const int rot = is_v ? 0 : a.rot;
+  constexpr int kPer = D / 16;                                    // items of a row
+  static_assert(TEAM % kPer == 0, "a thread's dims are the same in all its rows");
+  const int n_items = (p1 - p0) * kPer, j = t % kPer;
+  int da, db;
+  item_dims(j, rot, D, da, db);
+  // the rows do not wait for the page: both are in flight together
+  const int entry = paged_entry(c, b, slot);
+  Raw8<T> raw[kApItems][2];
+#pragma unroll
+  for (int u = 0; u < kApItems; ++u) {
+    const int it = u * TEAM + t;
+    if (it >= n_items) continue;
+    const T* row = in + static_cast<long long>(sq.row0 + p0 - sq.len + it / kPer) * ld;
+    raw[u][0].load(row + da);
+    raw[u][1].load(row + db);
+  }
+  const int page = paged_valid(c, entry);
   if (page < 0) {
     if (t == 0) flag_status(c.status, DVI_DEV_KV_FULL);
     return;
   }
-  const bool is_v = task >= c.H;
-  const int h = is_v ? task - c.H : task;
   const size_t ph = static_cast<size_t>(page) * c.H + h;
   float* sp = (is_v ? c.v_scale : c.k_scale) + ph;
   uint8_t* codes = (is_v ? c.v : c.k) + (ph << c.log_p) * D;
   const int held = p0 - page0;
   const float old = held > 0 ? *sp : 0.f;
-  const T* in = static_cast<const T*>(is_v ? a.vin : a.kin) + h * D;
-  const long long ld = is_v ? a.ld_v : a.ld_k;
-  const int rot = is_v ? 0 : a.rot;
-  constexpr int kPer = D / 16;                                    // items of a row
-  const int n_items = (p1 - p0) * kPer;
   float x[kApItems][16];
   float most = 0.f, odd = 0.f;                                    // odd: NaN where some value is not finite
 #pragma unroll
   for (int u = 0; u < kApItems; ++u) {
     const int it = u * TEAM + t;
     if (it >= n_items) continue;
-    const int r = it / kPer, j = it % kPer;
-    int da, db;
-    item_dims(j, rot, D, da, db);
-    const T* row = in + static_cast<long long>(sq.row0 + p0 - sq.len + r) * ld;
     float lo[8], hi[8];
-    ld8(row + da, lo);
-    ld8(row + db, hi);
+    raw[u][0].get(lo);
+    raw[u][1].get(hi);
     if (8 * j < rot / 2) {
-      const int pos = p0 + r;
+      const int pos = p0 + it / kPer;
       if (pos < a.n_pos) {
         Turn turn;
         turn.load(a.rotary + static_cast<size_t>(pos) * (rot / 2) + 8 * j);
@@ -154,10 +164,7 @@ __device__ void append_page(const PagedAppendArgs& a, int item, int group) {
   for (int u = 0; u < kApItems; ++u) {
     const int it = u * TEAM + t;
     if (it >= n_items) continue;
-    const int r = it / kPer, j = it % kPer;
-    int da, db;
-    item_dims(j, rot, D, da, db);
-    uint8_t* row = codes + static_cast<size_t>(held + r) * D;
+    uint8_t* row = codes + static_cast<size_t>(held + it / kPer) * D;
     float y[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) y[i] = __fmul_rn(x[u][i], inv);
