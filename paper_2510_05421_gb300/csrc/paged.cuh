@@ -51,20 +51,27 @@ struct PagedAttendArgs {
   int min_vectors, max_vectors;           // sequences with rows * G in this range are this launch's
   float* part;                            // partial results, then the counters
   int* counters;
+  float* pf_part;                         // the same of the prompt kernel
+  int* pf_counters;
 };
 
 cudaError_t launch_paged_append(const PagedAppendArgs& a, bool e4m3, cudaStream_t s);
 cudaError_t launch_paged_read(const PagedReadArgs& a, bool e4m3, cudaStream_t s);
 template <bool E4M3> cudaError_t launch_paged_attend(const PagedAttendArgs& a, int n_sms, cudaStream_t s);
+cudaError_t launch_paged_pf(const PagedAttendArgs& a, bool e4m3, int n_sms, cudaStream_t s);
 
-// Workspace of the attention: a counter for each team of warps, zero between
-// calls, then two partial results of at most 32 vectors for each team.
+// Workspace of the attention: a counter for each team of warps (few rows) and
+// for each pair of tiles (prompts), zero between calls, then two partial
+// results of at most 32 vectors for each team, and one of 256 for each SM.
 constexpr int kPagedTeams = 4;   // most teams per SM
-inline size_t paged_attend_counter_bytes(int n_sms) {
-  return (static_cast<size_t>(n_sms) * kPagedTeams * sizeof(int) + 255) / 256 * 256;
+inline size_t paged_counter_bytes(int n_sms) {
+  return (static_cast<size_t>(n_sms) * (kPagedTeams + 1) * sizeof(int) + 255) / 256 * 256;
 }
-inline size_t paged_attend_part_bytes(int head_dim, int n_sms) {
-  return static_cast<size_t>(n_sms) * kPagedTeams * 2 * 32 * (head_dim + 2) * sizeof(float);
+inline size_t paged_part_floats(int head_dim, int n_sms) {
+  return static_cast<size_t>(n_sms) * kPagedTeams * 2 * 32 * (head_dim + 2);
+}
+inline size_t paged_pf_part_floats(int head_dim, int n_sms) {
+  return static_cast<size_t>(n_sms) * 256 * (head_dim + 2);
 }
 
 // ---------------------------------------------------------------- rows of a sequence

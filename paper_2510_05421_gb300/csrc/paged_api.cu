@@ -21,6 +21,10 @@ int current_sms() {
   return n;
 }
 
+// Query vectors (rows x query heads of a KV head) up to which a sequence's rows
+// are few.
+constexpr int kFewVectors = 64;
+
 bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool ld_ok(int64_t ld, int64_t least, int esz) { return ld >= least && (ld * esz) % 16 == 0; }
 
@@ -136,20 +140,38 @@ extern "C" dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_p
   a.scale = options->scale;
   a.softcap = options->softcap;
   a.window = options->window;
-  a.min_vectors = 1;
-  a.max_vectors = 0x7fffffff;
   a.counters = static_cast<int*>(workspace);
-  a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + paged_attend_counter_bytes(sms));
+  a.pf_counters = a.counters + static_cast<size_t>(sms) * kPagedTeams;
+  a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + paged_counter_bytes(sms));
+  a.pf_part = a.part + paged_part_floats(a.c.D, sms);
   cudaGetLastError();
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  return launched(cache->format == DVI_KV_E4M3 ? launch_paged_attend<true>(a, sms, st)
-                                               : launch_paged_attend<false>(a, sms, st));
+  const bool e4m3 = cache->format == DVI_KV_E4M3;
+  // bf16 sequences of more than kFewVectors query vectors per KV head go to the
+  // prompt kernel; a ragged batch may hold both kinds, and each launch skips
+  // the other's
+  const int64_t most = static_cast<int64_t>(a.c.max_rows) * a.G;
+  const bool prompts = dtype == DVI_BF16 && a.G <= 128 && most > kFewVectors;
+  const bool few = !prompts || (a.c.row_start && a.c.n_seqs > 1);
+  if (prompts) {
+    a.min_vectors = kFewVectors + 1;
+    a.max_vectors = 0x7fffffff;
+    if (launch_paged_pf(a, e4m3, sms, st) != cudaSuccess) return DVI_ERR_CUDA;
+  }
+  if (few) {
+    a.min_vectors = 1;
+    a.max_vectors = prompts ? kFewVectors : 0x7fffffff;
+    const cudaError_t e = e4m3 ? launch_paged_attend<true>(a, sms, st) : launch_paged_attend<false>(a, sms, st);
+    if (e != cudaSuccess) return DVI_ERR_CUDA;
+  }
+  return DVI_OK;
 }
 
 extern "C" size_t dvi_paged_workspace_bytes(int head_dim) {
   const int sms = current_sms();
   if ((head_dim != 64 && head_dim != 128) || sms <= 0) return 0;
-  return paged_attend_counter_bytes(sms) + paged_attend_part_bytes(head_dim, sms);
+  return paged_counter_bytes(sms) +
+         (paged_part_floats(head_dim, sms) + paged_pf_part_floats(head_dim, sms)) * sizeof(float);
 }
 
 extern "C" dvi_status dvi_paged_read(const dvi_paged_cache* cache, const dvi_paged_batch* batch, int dtype,

@@ -1,0 +1,607 @@
+// Attention of many rows (prompt chunks, bf16) over the 8-bit paged cache on
+// tcgen05 / TMEM; the formulas are those of paged_attn.cuh.
+//
+// A CTA owns one KV head and two tiles of 128 query vectors (tile row v: row
+// v / G of the tile, query head v % G) and walks the 128-position chunks of
+// the cache that its rows see.  Both tiles share every chunk, so the codes
+// cross L2 and are widened to f16 once per 256 query vectors.  Per chunk and
+// tile:
+//   S = Q C_k^T    M = 128 vectors, N = 128 positions, K = hd (codes are exact
+//                  in f16, and so are bf16 queries scaled by a power of two);
+//   weights        one thread per vector: w = 2^(S f ks + log2 vs - m) as f16
+//                  back into the TMEM columns of S, sum of w / vs;
+//   O += W C_v     A = W from TMEM, B = the widened codes as they lie (rows are
+//                  the K index: MN-major).
+// The accumulator is rescaled only when a vector's maximum outgrows its
+// reference by 2^13.  The scores are read from TMEM twice, for the maximum and
+// for the weights: that keeps a thread within 128 registers.
+//
+// Roles (512 threads): warps 0-3 and 4-7 hold the vectors of tile 0 and 1,
+// warps 8-11 widen codes (global -> registers -> SW128 tiles in shared memory,
+// the next tile's codes in flight meanwhile), warp 12 issues the MMAs.
+//
+// Where the tiles are fewer than the SMs, `splits` CTAs share a pair of tiles
+// along the positions; the last of them to end joins their parts in order.
+//
+// Every wait is bounded (flag, then wind down).
+#include <algorithm>
+
+#include "paged.cuh"
+
+namespace dvi {
+
+namespace {
+
+constexpr int kPfThreads = 512;
+constexpr int kPfQ = 128;                // vectors per tile
+constexpr int kPfPos = 128;              // positions per chunk
+constexpr int kPfSegs = kPfPos / 16;     // a page covers whole segments
+constexpr int kPfStages = 4;
+constexpr float kPfLazy = 13.f;          // growth of a maximum that rescales the accumulator
+constexpr float kPfUp = 5.f;             // a new reference sits so far below the maximum
+constexpr float kPfUnset = -1e30f;
+constexpr float kPfLog2e = 1.4426950408889634f;
+
+template <int HD>
+struct PfSmem {
+  static constexpr int kBoxes = HD / 64;               // 64-dim boxes per row
+  static constexpr int kBox = kPfPos * 128;            // 128 rows x 64 f16
+  static constexpr int kStage = kBoxes * kBox;         // one chunk's K or V
+  static constexpr int kQ = kBoxes * kBox;             // one tile's queries
+  static constexpr int kRing = 2 * kQ;
+  static constexpr int kFac = kRing + kPfStages * kStage;
+  static constexpr int kBars = kFac + 2 * kPfQ * 4;
+  static constexpr int kTotal = kBars + 256 + 1024 /*align*/;
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float lg2(float x) {
+  float y;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// Instruction descriptor of tcgen05.mma kind::f16 with f16 operands, M = 128.
+__host__ __device__ constexpr uint32_t idesc_f16_m128(uint32_t n) {
+  return (1u << 4) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+}
+// Waits for this thread's TMEM loads, v's among them: the compiler cannot use v before.
+__device__ __forceinline__ void tmem_ld_wait32(float (&v)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
+                 "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]),
+                 "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]),
+                 "+f"(v[22]), "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]),
+                 "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
+               :
+               : "memory");
+}
+// 16 codes as 16 f16.
+template <bool E4M3>
+__device__ __forceinline__ void widen(const uint4& q, uint4& lo, uint4& hi) {
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+  uint32_t h[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (E4M3) {
+      e4m3x4_to_f16(w[i], h[2 * i], h[2 * i + 1]);
+    } else {
+      const uint32_t u = w[i] ^ 0x80808080u, c = 0x64806480u;     // 1152, 1152
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t x = __byte_perm(u, 0x64646464u, k ? 0x4342 : 0x4140);
+        const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&c));
+        h[2 * i + k] = *reinterpret_cast<const uint32_t*>(&r);
+      }
+    }
+  }
+  lo = make_uint4(h[0], h[1], h[2], h[3]);
+  hi = make_uint4(h[4], h[5], h[6], h[7]);
+}
+
+}  // namespace
+
+template <bool E4M3, int HD>
+__global__ void __launch_bounds__(kPfThreads, 1)
+    paged_pf_kernel(const __grid_constant__ PagedAttendArgs a, int n_items, int rows_per_tile, int splits) {
+  using SM = PfSmem<HD>;
+  extern __shared__ uint8_t dsm_raw[];
+  const uint32_t raw = smem_u32(dsm_raw);
+  uint8_t* sm = dsm_raw + (((raw + 1023u) & ~1023u) - raw);
+  float* fac = reinterpret_cast<float*>(sm + SM::kFac);
+  uint64_t* full = reinterpret_cast<uint64_t*>(sm + SM::kBars);
+  uint64_t* empty = full + kPfStages;
+  uint64_t* q_ready = empty + kPfStages;   // the queries are in shared memory
+  uint64_t* s_full = q_ready + 1;          // [2] the tile's scores are in TMEM
+  uint64_t* p_ready = s_full + 2;          // [2] its weights are
+  uint64_t* pv_done = p_ready + 2;         // [2] its accumulator holds the chunk
+  uint64_t* fin = pv_done + 2;             // every MMA issued is done
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(fin + 1);
+  int* last_s = reinterpret_cast<int*>(tmem_holder + 1);
+
+  const PagedArgs& c = a.c;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int G = a.G, RT = rows_per_tile;
+
+  griddep_wait();
+  griddep_launch();
+  // ---------------- this CTA's item: a pair of tiles of one sequence (the last
+  // pairs see most and go first), a KV head, a range of positions
+  const int split = static_cast<int>(blockIdx.y);
+  const int h = static_cast<int>(blockIdx.x) % c.H;
+  const int item = n_items - 1 - static_cast<int>(blockIdx.x) / c.H;
+  int first = 0;
+  const int pair = 2 * RT;
+  int b = 0;
+  {
+    auto begin = [&](int s) {
+      const int r0 = c.row_start ? min(max(c.row_start[s], 0), c.n_rows) : s * (c.n_rows / c.n_seqs);
+      return r0 / pair + s;
+    };
+    int n = 0;
+    for (int s0 = 0; s0 < c.n_seqs; s0 += kPfThreads) {
+      const int s = s0 + tid;
+      n += __syncthreads_count(s < c.n_seqs && begin(s) <= item);
+    }
+    b = n - 1;
+    if (b < 0) return;
+    first = begin(b);
+  }
+  const PagedSeq sq = paged_seq(c, b);
+  const int i0 = (item - first) * pair;                 // first row of tile 0
+  const int vecs = sq.n * G;
+  if (i0 >= sq.n || vecs < a.min_vectors || vecs > a.max_vectors) return;
+  const int cap = c.max_pages << c.log_p;
+  const int held_end = min(sq.len + sq.n, cap);         // rows of the cache past it are nobody's
+  // chunks that some row of tile t sees (0: the tile has no row), and those of this CTA
+  auto seen = [&](int t) {
+    const int nr = min(RT, sq.n - i0 - t * RT);
+    return nr <= 0 ? 0 : (min(sq.len + i0 + t * RT + nr, cap) + kPfPos - 1) / kPfPos;
+  };
+  const int all0 = seen(0), all1 = seen(1), all = max(all0, all1);
+  const int begin_all = min(a.window > 0 ? max(0, sq.len + i0 - a.window + 1) / kPfPos : 0, max(all - 1, 0));
+  const int c0 = begin_all + (all - begin_all) * split / splits;
+  const int c1 = begin_all + (all - begin_all) * (split + 1) / splits;
+  const int nch0 = max(0, min(all0, c1) - c0), nch1 = max(0, min(all1, c1) - c0), nch = max(nch0, nch1);
+
+  if (tid == 0) {
+    for (int s = 0; s < kPfStages; ++s) {
+      mbar_init(&full[s], 4);
+      mbar_init(&empty[s], 1);
+    }
+    mbar_init(q_ready, 8);
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&s_full[t], 1);
+      mbar_init(&p_ready[t], 4);
+      mbar_init(&pv_done[t], 1);
+    }
+    mbar_init(fin, 1);
+    mbar_fence_init();
+  }
+  if (warp == 12) tmem_alloc(tmem_holder, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_holder;
+  // S / W of tile t: columns 128 t ..; O: 256 + 128 t ..
+
+  if (warp >= 12) {
+    if (warp == 12 && lane == 0) {
+      // ---------------- MMA issuer
+      const uint32_t id_s = idesc_f16_m128(kPfPos);
+      const uint32_t id_o = idesc_f16_m128(HD) | kIdescBMn;
+      auto scores = [&](int t, int s) {
+        const uint32_t q = smem_u32(sm + t * SM::kQ), k = smem_u32(sm + SM::kRing + s * SM::kStage);
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk) {
+          const uint32_t off = (kk / 4) * SM::kBox + (kk % 4) * 32;
+          tc_mma_bf16(tmem + 128u * t, smem_desc_sw128(q + off), smem_desc_sw128(k + off), id_s, kk != 0);
+        }
+        tc_commit(&s_full[t]);
+      };
+      auto values = [&](int t, int s, bool fresh) {
+        const uint32_t v = smem_u32(sm + SM::kRing + s * SM::kStage);
+#pragma unroll
+        for (int kk = 0; kk < kPfPos / 16; ++kk)
+          tc_mma_bf16_ta(tmem + 256u + 128u * t, tmem + 128u * t + 8u * kk, smem_desc_sw128_mn(v + kk * 2048, SM::kBox),
+                         id_o, !fresh || kk != 0);
+        tc_commit(&pv_done[t]);
+      };
+      auto full_wait = [&](int it) { return mbar_wait(&full[it % kPfStages], (it / kPfStages) & 1, c.status); };
+      bool ok = nch > 0 && mbar_wait(q_ready, 0, c.status) && full_wait(0);
+      if (ok) {
+        tc_fence_after();
+        if (nch0 > 0) scores(0, 0);
+        if (nch1 > 0) scores(1, 0);
+        tc_commit(&empty[0]);
+      }
+      for (int i = 0; i < nch && ok; ++i) {
+        const int iv = 2 * i + 1, sv = iv % kPfStages, ik = iv + 1, sk = ik % kPfStages;
+        ok = full_wait(iv) && (i + 1 >= nch || full_wait(ik));
+        // one tile's W C_v and next scores while the other's weights are made
+        for (int t = 0; t < 2 && ok; ++t) {
+          const int mine = t ? nch1 : nch0;
+          if (i >= mine) continue;
+          ok = mbar_wait(&p_ready[t], i & 1, c.status);
+          if (!ok) break;
+          tc_fence_after();
+          values(t, sv, i == 0);
+          if (i + 1 >= mine) continue;
+          // the next scores overwrite the columns that W C_v reads
+          ok = mbar_wait(&pv_done[t], i & 1, c.status);
+          if (!ok) break;
+          tc_fence_after();
+          scores(t, sk);
+        }
+        if (!ok) break;
+        tc_commit(&empty[sv]);
+        if (i + 1 < nch) tc_commit(&empty[sk]);
+      }
+      // every MMA issued is done before the TMEM is freed
+      tc_commit(fin);
+      mbar_wait(fin, 0, c.status);
+    }
+    __syncwarp();
+  } else if (warp >= 8) {
+    // ---------------- widening: tiles K c0, V c0, K c0 + 1, ...; a warp's 32 rows are two 16-row segments
+    const int w = warp - 8;
+    constexpr int kRow = HD / 16;                       // 16-byte chunks of a row
+    constexpr int kRows = 32 / kRow;                    // rows at once
+    constexpr int kLoads = 32 / kRows;
+    const int r0 = lane / kRow, ch = lane % kRow;
+    const size_t page_bytes = (static_cast<size_t>(c.H) << c.log_p) * HD;
+    const size_t lane_off = ((static_cast<size_t>(h) << c.log_p) + r0) * HD + ch * 16;
+    auto entry = [&](int i, int half) {
+      const int p = (c0 + i) * kPfPos + 32 * w + 16 * half;
+      return i < nch && p < held_end ? paged_entry(c, b, p >> c.log_p) : -1;
+    };
+    int e0 = entry(0, 0), e1 = entry(0, 1);
+    uint4 next[kLoads];
+    auto load = [&](int it) {                           // codes of tile `it` (its chunk's entries in e0, e1)
+      const uint8_t* pool = it & 1 ? c.v : c.k;
+      const int p = (c0 + (it >> 1)) * kPfPos + 32 * w;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int pg = paged_valid(c, half ? e1 : e0), ph = p + 16 * half;
+        const uint8_t* src = pool + static_cast<size_t>(max(pg, 0)) * page_bytes + (ph & (c.P - 1)) * HD + lane_off;
+        const int live = pg >= 0 ? held_end - ph - r0 : 0;         // rows past it, and pages not held: zeros
+#pragma unroll
+        for (int u = 0; u < kLoads / 2; ++u)
+          next[half * (kLoads / 2) + u] = u * kRows < live ? __ldg(reinterpret_cast<const uint4*>(src + u * kRows * HD))
+                                                           : make_uint4(0u, 0u, 0u, 0u);
+      }
+    };
+    if (nch > 0) load(0);
+    // lanes of the two 64-dim boxes write their two chunks in opposite order: no bank meets twice
+    const int box = ch / 4, flip = box;
+    for (int it = 0; it < 2 * nch; ++it) {
+      const int s = it % kPfStages;
+      uint4 now[kLoads];
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) now[u] = next[u];
+      if (it & 1) {
+        // the next chunk's pages, looked up while this tile is widened
+        e0 = entry((it >> 1) + 1, 0);
+        e1 = entry((it >> 1) + 1, 1);
+      } else {
+        load(it + 1);
+      }
+      if (!mbar_wait(&empty[s], ((it / kPfStages) & 1) ^ 1, c.status)) break;
+      uint8_t* dst = sm + SM::kRing + s * SM::kStage + box * SM::kBox;
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
+        const int row = 32 * w + u * kRows + r0;
+        uint4 x[2];
+        widen<E4M3>(now[u], x[0], x[1]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int half = k ^ flip;
+          *reinterpret_cast<uint4*>(dst + sw128_offset(row, (2 * (ch % 4) + half) * 8)) = half ? x[1] : x[0];
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&full[s]);
+      if ((it & 1) && it + 1 < 2 * nch) load(it + 1);
+    }
+  } else {
+    // ---------------- a tile's vectors
+    const int t = warp >> 2, wq = warp & 3;
+    const int r0 = i0 + t * RT;
+    const int nrows = max(0, min(RT, sq.n - r0));
+    const int my = t ? nch1 : nch0;
+    // queries: a warp per vector, HD / 32 dims a lane, scaled by a power of two to [2^14, 2^15)
+    {
+      constexpr int kDims = HD / 32;
+      uint8_t* qs = sm + t * SM::kQ;
+      const int d = lane * kDims;
+#pragma unroll 1
+      for (int u0 = 0; u0 < 32; u0 += 8) {
+        uint32_t x[8][kDims / 2];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int v = wq * 32 + u0 + u, ii = v / G;
+#pragma unroll
+          for (int e = 0; e < kDims / 2; ++e) x[u][e] = 0u;
+          if (ii < nrows) {
+            const uint32_t* p = reinterpret_cast<const uint32_t*>(
+                static_cast<const __nv_bfloat16*>(a.q) + static_cast<long long>(sq.row0 + r0 + ii) * a.ld_q +
+                (h * G + v - ii * G) * HD + d);
+#pragma unroll
+            for (int e = 0; e < kDims / 2; ++e) x[u][e] = __ldg(p + e);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int v = wq * 32 + u0 + u;
+          float top = 0.f;
+#pragma unroll
+          for (int e = 0; e < kDims / 2; ++e) top = fmaxf(top, fmaxf(fabsf(bf16_lo(x[u][e])), fabsf(bf16_hi(x[u][e]))));
+          top = warp_max(top);
+          const int ex = max(static_cast<int>(__float_as_uint(top) >> 23), 15);
+          const float up = __uint_as_float(static_cast<uint32_t>(268 - ex) << 23);
+          if (lane == 0) {
+            const float down = __uint_as_float(static_cast<uint32_t>(ex - 14) << 23);
+            fac[t * kPfQ + v] = a.softcap > 0.f ? down * (a.scale / a.softcap) : down * (a.scale * kPfLog2e);
+          }
+#pragma unroll
+          for (int e = 0; e < kDims / 2; ++e)
+            *reinterpret_cast<uint32_t*>(qs + (d / 64) * SM::kBox + sw128_offset(v, d % 64 + 2 * e)) =
+                pack_h2(bf16_lo(x[u][e]) * up, bf16_hi(x[u][e]) * up);
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_ready);
+    }
+    // thread = TMEM lane = vector
+    const int v = wq * 32 + lane, vi = v / G, hq = h * G + v - vi * G;
+    const bool live = vi < nrows;
+    const int pos = live ? sq.len + r0 + vi : -1;
+    const float f = fac[t * kPfQ + v];
+    const float slope = a.slopes && live ? __ldg(a.slopes + hq) * kPfLog2e : 0.f;
+    const bool curved = a.softcap > 0.f || a.slopes != nullptr;
+    const uint32_t lanes = static_cast<uint32_t>(wq * 32) << 16;
+    const uint32_t ts = tmem + 128u * t + lanes, to = tmem + 256u + 128u * t + lanes;
+    // scales: lane e < 8 holds those of segment e; entries are read two chunks ahead, scales one
+    auto entry = [&](int i) {
+      const int p = (c0 + i) * kPfPos + 16 * lane;
+      return lane < kPfSegs && i < my && p < held_end ? paged_entry(c, b, p >> c.log_p) : -1;
+    };
+    int e_next = entry(0);
+    float ks_next = 0.f, vs_next = 0.f;
+    auto scales = [&] {
+      const int pg = paged_valid(c, e_next);
+      ks_next = pg >= 0 ? __ldg(c.k_scale + static_cast<size_t>(pg) * c.H + h) : 0.f;
+      vs_next = pg >= 0 ? __ldg(c.v_scale + static_cast<size_t>(pg) * c.H + h) : 0.f;
+    };
+    scales();
+    e_next = entry(1);
+    float m = kPfUnset, l = 0.f;
+    bool ok = true;
+#pragma unroll 1
+    for (int i = 0; i < my; ++i) {
+      const float vx = fmaxf(vs_next, kPagedMinScale);
+      const float ks_l = ks_next, lv_l = vs_next > 0.f ? lg2(vx) : -INFINITY, iv_l = __fdividef(1.f, vx);
+      scales();
+      e_next = entry(i + 2);
+      if (!mbar_wait(&s_full[t], i & 1, c.status)) {
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      const int at = (c0 + i) * kPfPos;
+      const int see = pos - at;                        // positions 0 .. see of the chunk are visible,
+      const int from = a.window > 0 ? see - a.window + 1 : 0;       // and only those from here on
+      const bool edge = see < kPfPos - 1 || from > 0;
+      // the finished scores of 32 columns
+      auto finish = [&](float (&s)[32], int c32) {
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const float fk = f * __shfl_sync(0xffffffffu, ks_l, c32 / 16 + g);
+          const float lv = __shfl_sync(0xffffffffu, lv_l, c32 / 16 + g);
+          if (curved) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              float x = s[16 * g + e] * fk;
+              if (a.softcap > 0.f) x = (1.f - __fdividef(2.f, 1.f + ex2(x * (2.f * kPfLog2e)))) * (a.softcap * kPfLog2e);
+              s[16 * g + e] = fmaf(slope, static_cast<float>(c32 + 16 * g + e - see), x + lv);
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[16 * g + e] = fmaf(s[16 * g + e], fk, lv);
+          }
+        }
+        if (edge) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) s[e] = c32 + e <= see && c32 + e >= from ? s[e] : -INFINITY;
+        }
+      };
+      float buf[2][32];
+      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      tmem_ld32_async(ts, buf[0]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        tmem_ld_wait32(buf[q & 1]);
+        if (q < 3) tmem_ld32_async(ts + 32 * (q + 1), buf[(q + 1) & 1]);
+        finish(buf[q & 1], 32 * q);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], buf[q & 1][e]);
+      }
+      const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+      const bool move = top > m + kPfLazy;
+      if (__any_sync(0xffffffffu, move)) {
+        const float ref = move ? top - kPfUp : m, shrink = ex2(m - ref);
+        m = ref;
+        l *= shrink;
+        if (i > 0) {
+          if (!mbar_wait(&pv_done[t], (i - 1) & 1, c.status)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+#pragma unroll 1
+          for (int d = 0; d < HD; d += 16) {
+            float o[16];
+            tmem_ld16(to + d, o);
+            uint32_t r[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) r[e] = __float_as_uint(o[e] * shrink);
+            tmem_st16(to + d, r);
+          }
+          tmem_st_wait();
+        }
+      }
+      tmem_ld32_async(ts, buf[0]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        tmem_ld_wait32(buf[q & 1]);
+        if (q < 3) tmem_ld32_async(ts + 32 * (q + 1), buf[(q + 1) & 1]);
+        float (&s)[32] = buf[q & 1];
+        finish(s, 32 * q);
+        uint32_t w[16];
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const float p0 = ex2(s[16 * g + 2 * e] - m), p1 = ex2(s[16 * g + 2 * e + 1] - m);
+            sum0 += p0;
+            sum1 += p1;
+            w[8 * g + e] = pack_h2(p0, p1);
+          }
+          l = fmaf(sum0 + sum1, __shfl_sync(0xffffffffu, iv_l, 2 * q + g), l);
+        }
+        // columns up to 16 q + 15 hold scores that are read by now
+        tmem_st16(ts + 16 * q, w);
+      }
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&p_ready[t]);
+    }
+    // ---------------- O / l, or this split's part
+    constexpr int kPart = 2 * kPfQ * (HD + 2);
+    const int unit = item * c.H + h;
+    float* part = a.pf_part + static_cast<size_t>(unit * splits + split) * kPart;
+    const bool done = ok && my > 0 && mbar_wait(&pv_done[t], (my - 1) & 1, c.status);
+    if (done) tc_fence_after();
+    const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.o) + static_cast<long long>(sq.row0 + r0 + vi) * a.ld_o + hq * HD;
+    auto store16 = [&](int d, const float (&o)[16], float k) {
+      uint32_t w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = pack_bf16x2(o[2 * e] * k, o[2 * e + 1] * k);
+      reinterpret_cast<uint4*>(out + d)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+      reinterpret_cast<uint4*>(out + d)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    };
+    // (a vector whose weights were all 0 has an accumulator of zeros; a tile without chunks none at all)
+    const int vp = t * kPfQ + v;
+#pragma unroll 1
+    for (int d = 0; d < HD; d += 16) {
+      float o[16];
+      if (done) tmem_ld16(to + d, o);
+      else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[e] = 0.f;
+      }
+      if (!live) continue;
+      if (splits == 1) {
+        store16(d, o, inv);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+          __stcg(reinterpret_cast<float4*>(part + static_cast<size_t>((d + e) / 4) * (2 * kPfQ * 4) + vp * 4),
+                 make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]));
+      }
+    }
+    if (splits > 1) {
+      __stcg(part + 2 * kPfQ * HD + vp, m);
+      __stcg(part + 2 * kPfQ * HD + 2 * kPfQ + vp, l);
+      named_bar(1, 256);
+      if (tid == 0) {
+        __threadfence();
+        const int n = atomicAdd(a.pf_counters + unit, 1);
+        *last_s = n == splits - 1;
+        if (n == splits - 1) a.pf_counters[unit] = 0;
+        __threadfence();
+      }
+      named_bar(1, 256);
+      if (*last_s && live) {
+        const float* p0 = a.pf_part + static_cast<size_t>(unit * splits) * kPart;
+        float M = kPfUnset, L = 0.f;
+        for (int s = 0; s < splits; ++s) M = fmaxf(M, __ldcg(p0 + static_cast<size_t>(s) * kPart + 2 * kPfQ * HD + vp));
+        for (int s = 0; s < splits; ++s) {
+          const float* p = p0 + static_cast<size_t>(s) * kPart + 2 * kPfQ * HD + vp;
+          L = fmaf(__ldcg(p + 2 * kPfQ), ex2(__ldcg(p) - M), L);
+        }
+        const float k = L > 0.f ? 1.f / L : (L == L ? 0.f : L);
+#pragma unroll 1
+        for (int d = 0; d < HD; d += 16) {
+          float o[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[e] = 0.f;
+#pragma unroll 2
+          for (int s = 0; s < splits; ++s) {
+            const float* p = p0 + static_cast<size_t>(s) * kPart;
+            const float w = ex2(__ldcg(p + 2 * kPfQ * HD + vp) - M);
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+              const float4 x = __ldcg(reinterpret_cast<const float4*>(
+                  p + static_cast<size_t>((d + e) / 4) * (2 * kPfQ * 4) + vp * 4));
+              o[e] = fmaf(x.x, w, o[e]), o[e + 1] = fmaf(x.y, w, o[e + 1]);
+              o[e + 2] = fmaf(x.z, w, o[e + 2]), o[e + 3] = fmaf(x.w, w, o[e + 3]);
+            }
+          }
+          store16(d, o, k);
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 12) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+namespace {
+
+template <bool E4M3, int HD>
+cudaError_t launch_pf(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
+  static PerDevice attr;
+  attr.once([] {
+    cudaFuncSetAttribute(paged_pf_kernel<E4M3, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, PfSmem<HD>::kTotal);
+  });
+  const PagedArgs& c = a.c;
+  const int rt = kPfQ / a.G;
+  const int per = c.row_start ? 0 : c.n_rows / c.n_seqs;
+  // pairs of tiles: sequence b's begin at row_start[b] / (2 rt) + b
+  const long long items = c.row_start ? c.n_rows / (2 * rt) + c.n_seqs
+                                      : (static_cast<long long>(c.n_seqs - 1) * per) / (2 * rt) + c.n_seqs - 1 +
+                                            (per + 2 * rt - 1) / (2 * rt);
+  const long long units = items * c.H;
+  if (units > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+  // splits only fill SMs that the tiles leave idle, four chunks each at the least
+  const int chunks = static_cast<int>(((static_cast<long long>(c.max_pages) << c.log_p) + kPfPos - 1) / kPfPos);
+  const int splits = static_cast<int>(std::max(1ll, std::min<long long>({n_sms / units, chunks / 4, 16})));
+  return launch_pdl(paged_pf_kernel<E4M3, HD>, dim3(static_cast<unsigned>(units), splits), dim3(kPfThreads),
+                    PfSmem<HD>::kTotal, s, a, static_cast<int>(items), rt, splits);
+}
+
+}  // namespace
+
+cudaError_t launch_paged_pf(const PagedAttendArgs& a, bool e4m3, int n_sms, cudaStream_t s) {
+  if (a.c.D == 128) return e4m3 ? launch_pf<true, 128>(a, n_sms, s) : launch_pf<false, 128>(a, n_sms, s);
+  return e4m3 ? launch_pf<true, 64>(a, n_sms, s) : launch_pf<false, 64>(a, n_sms, s);
+}
+
+}  // namespace dvi
