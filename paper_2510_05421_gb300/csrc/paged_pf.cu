@@ -64,6 +64,32 @@ __device__ __forceinline__ float lg2(float x) {
   asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Two f32 operations in one instruction.
+__device__ __forceinline__ uint64_t pack2(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 __device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -108,7 +134,7 @@ __device__ __forceinline__ void widen(const uint4& q, uint4& lo, uint4& hi) {
 
 }  // namespace
 
-template <bool E4M3, int HD>
+template <bool E4M3, int HD, bool CURVED>
 __global__ void __launch_bounds__(kPfThreads, 1)
     paged_pf_kernel(const __grid_constant__ PagedAttendArgs a, int n_items, int rows_per_tile, int splits) {
   using SM = PfSmem<HD>;
@@ -193,26 +219,42 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   // S / W of tile t: columns 128 t ..; O: 256 + 128 t ..
 
   if (warp >= 12) {
-    if (warp == 12 && lane == 0) {
-      // ---------------- MMA issuer
+    if (warp == 12) {
+      // ---------------- MMA issuer: the whole warp walks the chunks, so that the
+      // descriptors are uniform values, and its lane 0 issues
       const uint32_t id_s = idesc_f16_m128(kPfPos);
       const uint32_t id_o = idesc_f16_m128(HD) | kIdescBMn;
+      const uint64_t q_desc = smem_desc_sw128(smem_u32(sm));
+      const uint64_t k_desc = smem_desc_sw128(smem_u32(sm + SM::kRing));
+      const uint64_t v_desc = smem_desc_sw128_mn(smem_u32(sm + SM::kRing), SM::kBox);
       auto scores = [&](int t, int s) {
-        const uint32_t q = smem_u32(sm + t * SM::kQ), k = smem_u32(sm + SM::kRing + s * SM::kStage);
+        const uint64_t q = q_desc + static_cast<uint64_t>(t * (SM::kQ >> 4));
+        const uint64_t k = k_desc + static_cast<uint64_t>(s * (SM::kStage >> 4));
+        if (lane == 0) {
 #pragma unroll
-        for (int kk = 0; kk < HD / 16; ++kk) {
-          const uint32_t off = (kk / 4) * SM::kBox + (kk % 4) * 32;
-          tc_mma_bf16(tmem + 128u * t, smem_desc_sw128(q + off), smem_desc_sw128(k + off), id_s, kk != 0);
+          for (int kk = 0; kk < HD / 16; ++kk) {
+            constexpr int kBox16 = SM::kBox >> 4;
+            const uint64_t off = (kk / 4) * kBox16 + (kk % 4) * 2;
+            tc_mma_bf16(tmem + 128u * t, q + off, k + off, id_s, kk != 0);
+          }
+          tc_commit(&s_full[t]);
         }
-        tc_commit(&s_full[t]);
+        __syncwarp();
       };
       auto values = [&](int t, int s, bool fresh) {
-        const uint32_t v = smem_u32(sm + SM::kRing + s * SM::kStage);
+        const uint64_t v = v_desc + static_cast<uint64_t>(s * (SM::kStage >> 4));
+        if (lane == 0) {
 #pragma unroll
-        for (int kk = 0; kk < kPfPos / 16; ++kk)
-          tc_mma_bf16_ta(tmem + 256u + 128u * t, tmem + 128u * t + 8u * kk, smem_desc_sw128_mn(v + kk * 2048, SM::kBox),
-                         id_o, !fresh || kk != 0);
-        tc_commit(&pv_done[t]);
+          for (int kk = 0; kk < kPfPos / 16; ++kk)
+            tc_mma_bf16_ta(tmem + 256u + 128u * t, tmem + 128u * t + 8u * kk, v + kk * (2048 >> 4), id_o,
+                           kk != 0 || !fresh);
+          tc_commit(&pv_done[t]);
+        }
+        __syncwarp();
+      };
+      auto release = [&](int s) {
+        if (lane == 0) tc_commit(&empty[s]);
+        __syncwarp();
       };
       auto full_wait = [&](int it) { return mbar_wait(&full[it % kPfStages], (it / kPfStages) & 1, c.status); };
       bool ok = nch > 0 && mbar_wait(q_ready, 0, c.status) && full_wait(0);
@@ -220,7 +262,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         tc_fence_after();
         if (nch0 > 0) scores(0, 0);
         if (nch1 > 0) scores(1, 0);
-        tc_commit(&empty[0]);
+        release(0);
       }
       for (int i = 0; i < nch && ok; ++i) {
         const int iv = 2 * i + 1, sv = iv % kPfStages, ik = iv + 1, sk = ik % kPfStages;
@@ -241,11 +283,11 @@ __global__ void __launch_bounds__(kPfThreads, 1)
           scores(t, sk);
         }
         if (!ok) break;
-        tc_commit(&empty[sv]);
-        if (i + 1 < nch) tc_commit(&empty[sk]);
+        release(sv);
+        if (i + 1 < nch) release(sk);
       }
       // every MMA issued is done before the TMEM is freed
-      tc_commit(fin);
+      if (lane == 0) tc_commit(fin);
       mbar_wait(fin, 0, c.status);
     }
     __syncwarp();
@@ -263,53 +305,56 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       return i < nch && p < held_end ? paged_entry(c, b, p >> c.log_p) : -1;
     };
     int e0 = entry(0, 0), e1 = entry(0, 1);
-    uint4 next[kLoads];
-    auto load = [&](int it) {                           // codes of tile `it` (its chunk's entries in e0, e1)
-      const uint8_t* pool = it & 1 ? c.v : c.k;
-      const int p = (c0 + (it >> 1)) * kPfPos + 32 * w;
+    uint4 code[2][kLoads];                              // the next K tile's codes, and the next V tile's
+    auto load = [&](int i, int kv, int g0, int g1) {    // chunk i, its pages' entries
+      const uint8_t* pool = kv ? c.v : c.k;
+      const int p = (c0 + i) * kPfPos + 32 * w;
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        const int pg = paged_valid(c, half ? e1 : e0), ph = p + 16 * half;
+        const int pg = paged_valid(c, half ? g1 : g0), ph = p + 16 * half;
         const uint8_t* src = pool + static_cast<size_t>(max(pg, 0)) * page_bytes + (ph & (c.P - 1)) * HD + lane_off;
         const int live = pg >= 0 ? held_end - ph - r0 : 0;         // rows past it, and pages not held: zeros
 #pragma unroll
         for (int u = 0; u < kLoads / 2; ++u)
-          next[half * (kLoads / 2) + u] = u * kRows < live ? __ldg(reinterpret_cast<const uint4*>(src + u * kRows * HD))
-                                                           : make_uint4(0u, 0u, 0u, 0u);
+          code[kv][half * (kLoads / 2) + u] =
+              u * kRows < live ? __ldg(reinterpret_cast<const uint4*>(src + u * kRows * HD)) : make_uint4(0u, 0u, 0u, 0u);
       }
     };
-    if (nch > 0) load(0);
+    if (nch > 0) {
+      load(0, 0, e0, e1);
+      load(0, 1, e0, e1);
+      e0 = entry(1, 0);
+      e1 = entry(1, 1);
+    }
     // lanes of the two 64-dim boxes write their two chunks in opposite order: no bank meets twice
-    const int box = ch / 4, flip = box;
-    for (int it = 0; it < 2 * nch; ++it) {
-      const int s = it % kPfStages;
-      uint4 now[kLoads];
+    const int box = ch / 4;
+    bool ok = true;
+    for (int i = 0; i < nch && ok; ++i) {
+      const int n0 = e0, n1 = e1;                       // the next chunk's
+      e0 = entry(i + 2, 0);
+      e1 = entry(i + 2, 1);
 #pragma unroll
-      for (int u = 0; u < kLoads; ++u) now[u] = next[u];
-      if (it & 1) {
-        // the next chunk's pages, looked up while this tile is widened
-        e0 = entry((it >> 1) + 1, 0);
-        e1 = entry((it >> 1) + 1, 1);
-      } else {
-        load(it + 1);
-      }
-      if (!mbar_wait(&empty[s], ((it / kPfStages) & 1) ^ 1, c.status)) break;
-      uint8_t* dst = sm + SM::kRing + s * SM::kStage + box * SM::kBox;
+      for (int kv = 0; kv < 2; ++kv) {
+        const int it = 2 * i + kv, s = it % kPfStages;
+        ok = ok && mbar_wait(&empty[s], ((it / kPfStages) & 1) ^ 1, c.status);
+        if (!ok) break;
+        uint8_t* dst = sm + SM::kRing + s * SM::kStage + box * SM::kBox;
 #pragma unroll
-      for (int u = 0; u < kLoads; ++u) {
-        const int row = 32 * w + u * kRows + r0;
-        uint4 x[2];
-        widen<E4M3>(now[u], x[0], x[1]);
+        for (int u = 0; u < kLoads; ++u) {
+          const int row = 32 * w + u * kRows + r0;
+          uint4 x[2];
+          widen<E4M3>(code[kv][u], x[0], x[1]);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int half = k ^ flip;
-          *reinterpret_cast<uint4*>(dst + sw128_offset(row, (2 * (ch % 4) + half) * 8)) = half ? x[1] : x[0];
+          for (int k = 0; k < 2; ++k) {
+            const int half = k ^ box;
+            *reinterpret_cast<uint4*>(dst + sw128_offset(row, (2 * (ch % 4) + half) * 8)) = half ? x[1] : x[0];
+          }
         }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&full[s]);
+        if (i + 1 < nch) load(i + 1, kv, n0, n1);
       }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&full[s]);
-      if ((it & 1) && it + 1 < 2 * nch) load(it + 1);
     }
   } else {
     // ---------------- a tile's vectors
@@ -364,10 +409,9 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     // thread = TMEM lane = vector
     const int v = wq * 32 + lane, vi = v / G, hq = h * G + v - vi * G;
     const bool live = vi < nrows;
-    const int pos = live ? sq.len + r0 + vi : -1;
-    const float f = fac[t * kPfQ + v];
+    const int pos = sq.len + r0 + vi;
+    const float f = fmaxf(fac[t * kPfQ + v], 1.2e-38f);
     const float slope = a.slopes && live ? __ldg(a.slopes + hq) * kPfLog2e : 0.f;
-    const bool curved = a.softcap > 0.f || a.slopes != nullptr;
     const uint32_t lanes = static_cast<uint32_t>(wq * 32) << 16;
     const uint32_t ts = tmem + 128u * t + lanes, to = tmem + 256u + 128u * t + lanes;
     // scales: lane e < 8 holds those of segment e; entries are read two chunks ahead, scales one
@@ -389,7 +433,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
 #pragma unroll 1
     for (int i = 0; i < my; ++i) {
       const float vx = fmaxf(vs_next, kPagedMinScale);
-      const float ks_l = ks_next, lv_l = vs_next > 0.f ? lg2(vx) : -INFINITY, iv_l = __fdividef(1.f, vx);
+      const float ks_l = vs_next > 0.f ? ks_next : 1.f, lv_l = vs_next > 0.f ? lg2(vx) : -INFINITY;
+      const float iv_l = __fdividef(1.f, vx);
       scales();
       e_next = entry(i + 2);
       if (!mbar_wait(&s_full[t], i & 1, c.status)) {
@@ -400,23 +445,20 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       const int at = (c0 + i) * kPfPos;
       const int see = pos - at;                        // positions 0 .. see of the chunk are visible,
       const int from = a.window > 0 ? see - a.window + 1 : 0;       // and only those from here on
-      const bool edge = see < kPfPos - 1 || from > 0;
-      // the finished scores of 32 columns
+      const bool edge = __any_sync(0xffffffffu, live && (see < kPfPos - 1 || from > 0));
+      // what the vector does not see of 32 columns; with CURVED the finished scores, else still the products
       auto finish = [&](float (&s)[32], int c32) {
+        if (CURVED) {
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const float fk = f * __shfl_sync(0xffffffffu, ks_l, c32 / 16 + g);
-          const float lv = __shfl_sync(0xffffffffu, lv_l, c32 / 16 + g);
-          if (curved) {
+          for (int g = 0; g < 2; ++g) {
+            const float fk = f * __shfl_sync(0xffffffffu, ks_l, c32 / 16 + g);
+            const float lv = __shfl_sync(0xffffffffu, lv_l, c32 / 16 + g);
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
               float x = s[16 * g + e] * fk;
               if (a.softcap > 0.f) x = (1.f - __fdividef(2.f, 1.f + ex2(x * (2.f * kPfLog2e)))) * (a.softcap * kPfLog2e);
               s[16 * g + e] = fmaf(slope, static_cast<float>(c32 + 16 * g + e - see), x + lv);
             }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[16 * g + e] = fmaf(s[16 * g + e], fk, lv);
           }
         }
         if (edge) {
@@ -425,17 +467,31 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         }
       };
       float buf[2][32];
-      float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      float top = -INFINITY;
       tmem_ld32_async(ts, buf[0]);
+      // (two groups of columns to an iteration: the loops' code stays in the instruction cache)
+#pragma unroll 1
+      for (int q0 = 0; q0 < 4; q0 += 2) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        tmem_ld_wait32(buf[q & 1]);
-        if (q < 3) tmem_ld32_async(ts + 32 * (q + 1), buf[(q + 1) & 1]);
-        finish(buf[q & 1], 32 * q);
+        for (int k = 0; k < 2; ++k) {
+          const int q = q0 + k;
+          tmem_ld_wait32(buf[k]);
+          if (q < 3) tmem_ld32_async(ts + 32 * (q + 1), buf[k ^ 1]);
+          float (&s)[32] = buf[k];
+          finish(s, 32 * q);
 #pragma unroll
-        for (int e = 0; e < 32; ++e) mx[e & 3] = fmaxf(mx[e & 3], buf[q & 1][e]);
+          for (int g = 0; g < 2; ++g) {
+            float x = fmaxf(s[16 * g], s[16 * g + 1]), y = fmaxf(s[16 * g + 2], s[16 * g + 3]);
+#pragma unroll
+            for (int e = 4; e < 16; e += 4) x = max3(x, s[16 * g + e], s[16 * g + e + 1]), y = max3(y, s[16 * g + e + 2], s[16 * g + e + 3]);
+            x = fmaxf(x, y);
+            // a segment's factor is positive: its largest product is its largest score
+            if (!CURVED)
+              x = fmaf(x, f * __shfl_sync(0xffffffffu, ks_l, 2 * q + g), __shfl_sync(0xffffffffu, lv_l, 2 * q + g));
+            top = fmaxf(top, x);
+          }
+        }
       }
-      const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
       const bool move = top > m + kPfLazy;
       if (__any_sync(0xffffffffu, move)) {
         const float ref = move ? top - kPfUp : m, shrink = ex2(m - ref);
@@ -460,27 +516,35 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         }
       }
       tmem_ld32_async(ts, buf[0]);
+#pragma unroll 1
+      for (int q0 = 0; q0 < 4; q0 += 2) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        tmem_ld_wait32(buf[q & 1]);
-        if (q < 3) tmem_ld32_async(ts + 32 * (q + 1), buf[(q + 1) & 1]);
-        float (&s)[32] = buf[q & 1];
-        finish(s, 32 * q);
-        uint32_t w[16];
+        for (int k = 0; k < 2; ++k) {
+          const int q = q0 + k;
+          tmem_ld_wait32(buf[k]);
+          if (q < 3) tmem_ld32_async(ts + 32 * (q + 1), buf[k ^ 1]);
+          float (&s)[32] = buf[k];
+          finish(s, 32 * q);
+          uint32_t w[16];
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          float sum0 = 0.f, sum1 = 0.f;
+          for (int g = 0; g < 2; ++g) {
+            const float fk = CURVED ? 1.f : f * __shfl_sync(0xffffffffu, ks_l, 2 * q + g);
+            const float lv = (CURVED ? 0.f : __shfl_sync(0xffffffffu, lv_l, 2 * q + g)) - m;
+            const uint64_t fk2 = pack2(fk, fk), lv2 = pack2(lv, lv);
+            uint64_t sum = 0ull;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float p0 = ex2(s[16 * g + 2 * e] - m), p1 = ex2(s[16 * g + 2 * e + 1] - m);
-            sum0 += p0;
-            sum1 += p1;
-            w[8 * g + e] = pack_h2(p0, p1);
+            for (int e = 0; e < 8; ++e) {
+              const float2 x = unpack2(fma2(pack2(s[16 * g + 2 * e], s[16 * g + 2 * e + 1]), fk2, lv2));
+              const float p0 = ex2(x.x), p1 = ex2(x.y);
+              sum = add2(sum, pack2(p0, p1));
+              w[8 * g + e] = pack_h2(p0, p1);
+            }
+            const float2 both = unpack2(sum);
+            l = fmaf(both.x + both.y, __shfl_sync(0xffffffffu, iv_l, 2 * q + g), l);
           }
-          l = fmaf(sum0 + sum1, __shfl_sync(0xffffffffu, iv_l, 2 * q + g), l);
+          // columns up to 16 q + 15 hold scores that are read by now
+          tmem_st16(ts + 16 * q, w);
         }
-        // columns up to 16 q + 15 hold scores that are read by now
-        tmem_st16(ts + 16 * q, w);
       }
       tmem_st_wait();
       tc_fence_before();
@@ -575,11 +639,11 @@ __global__ void __launch_bounds__(kPfThreads, 1)
 
 namespace {
 
-template <bool E4M3, int HD>
+template <bool E4M3, int HD, bool CURVED>
 cudaError_t launch_pf(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
   static PerDevice attr;
   attr.once([] {
-    cudaFuncSetAttribute(paged_pf_kernel<E4M3, HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, PfSmem<HD>::kTotal);
+    cudaFuncSetAttribute(paged_pf_kernel<E4M3, HD, CURVED>, cudaFuncAttributeMaxDynamicSharedMemorySize, PfSmem<HD>::kTotal);
   });
   const PagedArgs& c = a.c;
   const int rt = kPfQ / a.G;
@@ -593,15 +657,20 @@ cudaError_t launch_pf(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
   // splits only fill SMs that the tiles leave idle, four chunks each at the least
   const int chunks = static_cast<int>(((static_cast<long long>(c.max_pages) << c.log_p) + kPfPos - 1) / kPfPos);
   const int splits = static_cast<int>(std::max(1ll, std::min<long long>({n_sms / units, chunks / 4, 16})));
-  return launch_pdl(paged_pf_kernel<E4M3, HD>, dim3(static_cast<unsigned>(units), splits), dim3(kPfThreads),
+  return launch_pdl(paged_pf_kernel<E4M3, HD, CURVED>, dim3(static_cast<unsigned>(units), splits), dim3(kPfThreads),
                     PfSmem<HD>::kTotal, s, a, static_cast<int>(items), rt, splits);
+}
+
+template <bool E4M3, int HD>
+cudaError_t pf_scores(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
+  return a.softcap > 0.f || a.slopes ? launch_pf<E4M3, HD, true>(a, n_sms, s) : launch_pf<E4M3, HD, false>(a, n_sms, s);
 }
 
 }  // namespace
 
 cudaError_t launch_paged_pf(const PagedAttendArgs& a, bool e4m3, int n_sms, cudaStream_t s) {
-  if (a.c.D == 128) return e4m3 ? launch_pf<true, 128>(a, n_sms, s) : launch_pf<false, 128>(a, n_sms, s);
-  return e4m3 ? launch_pf<true, 64>(a, n_sms, s) : launch_pf<false, 64>(a, n_sms, s);
+  if (a.c.D == 128) return e4m3 ? pf_scores<true, 128>(a, n_sms, s) : pf_scores<false, 128>(a, n_sms, s);
+  return e4m3 ? pf_scores<true, 64>(a, n_sms, s) : pf_scores<false, 64>(a, n_sms, s);
 }
 
 }  // namespace dvi
