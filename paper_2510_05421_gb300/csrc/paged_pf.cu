@@ -109,6 +109,12 @@ __device__ __forceinline__ void tmem_ld_wait32(float (&v)[32]) {
                :
                : "memory");
 }
+// One lane of a converged warp, always the same.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
 // 16 codes as 16 f16.
 template <bool E4M3>
 __device__ __forceinline__ void widen(const uint4& q, uint4& lo, uint4& hi) {
@@ -221,7 +227,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   if (warp >= 12) {
     if (warp == 12) {
       // ---------------- MMA issuer: the whole warp walks the chunks, so that the
-      // descriptors are uniform values, and its lane 0 issues
+      // descriptors are uniform values, and one lane issues
       const uint32_t id_s = idesc_f16_m128(kPfPos);
       const uint32_t id_o = idesc_f16_m128(HD) | kIdescBMn;
       const uint64_t q_desc = smem_desc_sw128(smem_u32(sm));
@@ -230,7 +236,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       auto scores = [&](int t, int s) {
         const uint64_t q = q_desc + static_cast<uint64_t>(t * (SM::kQ >> 4));
         const uint64_t k = k_desc + static_cast<uint64_t>(s * (SM::kStage >> 4));
-        if (lane == 0) {
+        if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < HD / 16; ++kk) {
             constexpr int kBox16 = SM::kBox >> 4;
@@ -243,7 +249,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       };
       auto values = [&](int t, int s, bool fresh) {
         const uint64_t v = v_desc + static_cast<uint64_t>(s * (SM::kStage >> 4));
-        if (lane == 0) {
+        if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < kPfPos / 16; ++kk)
             tc_mma_bf16_ta(tmem + 256u + 128u * t, tmem + 128u * t + 8u * kk, v + kk * (2048 >> 4), id_o,
@@ -253,7 +259,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         __syncwarp();
       };
       auto release = [&](int s) {
-        if (lane == 0) tc_commit(&empty[s]);
+        if (elect_one()) tc_commit(&empty[s]);
         __syncwarp();
       };
       auto full_wait = [&](int it) { return mbar_wait(&full[it % kPfStages], (it / kPfStages) & 1, c.status); };
@@ -287,7 +293,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         if (i + 1 < nch) release(sk);
       }
       // every MMA issued is done before the TMEM is freed
-      if (lane == 0) tc_commit(fin);
+      if (elect_one()) tc_commit(fin);
       mbar_wait(fin, 0, c.status);
     }
     __syncwarp();
