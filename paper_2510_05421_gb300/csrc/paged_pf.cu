@@ -303,7 +303,9 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     constexpr int kRow = HD / 16;                       // 16-byte chunks of a row
     constexpr int kRows = 32 / kRow;                    // rows at once
     constexpr int kLoads = 32 / kRows;
-    const int r0 = lane / kRow, ch = lane % kRow;
+    // eight lanes write two rows of one 64-dim box: no bank meets twice
+    const int ch = HD == 128 ? (lane & 3) | ((lane >> 1) & 4) : lane & 3;
+    const int r0 = HD == 128 ? ((lane >> 2) & 1) | ((lane >> 3) & 2) : lane >> 2;
     const size_t page_bytes = (static_cast<size_t>(c.H) << c.log_p) * HD;
     const size_t lane_off = ((static_cast<size_t>(h) << c.log_p) + r0) * HD + ch * 16;
     auto entry = [&](int i, int half) {
@@ -332,8 +334,6 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       e0 = entry(1, 0);
       e1 = entry(1, 1);
     }
-    // lanes of the two 64-dim boxes write their two chunks in opposite order: no bank meets twice
-    const int box = ch / 4;
     bool ok = true;
     for (int i = 0; i < nch && ok; ++i) {
       const int n0 = e0, n1 = e1;                       // the next chunk's
@@ -344,17 +344,15 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         const int it = 2 * i + kv, s = it % kPfStages;
         ok = ok && mbar_wait(&empty[s], ((it / kPfStages) & 1) ^ 1, c.status);
         if (!ok) break;
-        uint8_t* dst = sm + SM::kRing + s * SM::kStage + box * SM::kBox;
+        uint8_t* dst = sm + SM::kRing + s * SM::kStage + (ch / 4) * SM::kBox;
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
           const int row = 32 * w + u * kRows + r0;
           uint4 x[2];
           widen<E4M3>(code[kv][u], x[0], x[1]);
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const int half = k ^ box;
-            *reinterpret_cast<uint4*>(dst + sw128_offset(row, (2 * (ch % 4) + half) * 8)) = half ? x[1] : x[0];
-          }
+          for (int k = 0; k < 2; ++k)
+            *reinterpret_cast<uint4*>(dst + sw128_offset(row, (2 * (ch % 4) + k) * 8)) = x[k];
         }
         fence_proxy_async_smem();
         __syncwarp();
