@@ -49,6 +49,7 @@ struct PagedAttendArgs {
   float scale, softcap;
   int window;                             // 0: none
   int min_vectors, max_vectors;           // sequences with rows * G in this range are this launch's
+  int beside;                             // 1: the launch before is the same call's, on other rows: run beside it
   float* part;                            // partial results, then the counters
   int* counters;
   float* pf_part;                         // the same of the prompt kernel

@@ -161,6 +161,7 @@ extern "C" dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_p
   if (few) {
     a.min_vectors = 1;
     a.max_vectors = prompts ? kFewVectors : 0x7fffffff;
+    a.beside = prompts;
     const cudaError_t e = e4m3 ? launch_paged_attend<true>(a, sms, st) : launch_paged_attend<false>(a, sms, st);
     if (e != cudaSuccess) return DVI_ERR_CUDA;
   }

@@ -183,7 +183,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
   __shared__ int last_s[SH::kTeams];
   const int G = a.G;
 
-  griddep_wait();
+  if (!a.beside) griddep_wait();
   griddep_launch();
   {
     // what the pieces will ask for first, on its way to L2 while one warp plans: a
@@ -794,6 +794,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     }
     team_bar();   // the rings and the queries are read before the next group's
   }
+  if (a.beside) griddep_wait();   // whoever waits for this grid waits for the one before it too
 }
 
 namespace {

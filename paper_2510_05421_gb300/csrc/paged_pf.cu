@@ -49,8 +49,7 @@ struct PfSmem {
   static constexpr int kStage = kBoxes * kBox;         // one chunk's K or V
   static constexpr int kQ = kBoxes * kBox;             // one tile's queries
   static constexpr int kRing = 2 * kQ;
-  static constexpr int kFac = kRing + kPfStages * kStage;
-  static constexpr int kBars = kFac + 2 * kPfQ * 4;
+  static constexpr int kBars = kRing + kPfStages * kStage;
   static constexpr int kTotal = kBars + 256 + 1024 /*align*/;
 };
 
@@ -147,7 +146,6 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   extern __shared__ uint8_t dsm_raw[];
   const uint32_t raw = smem_u32(dsm_raw);
   uint8_t* sm = dsm_raw + (((raw + 1023u) & ~1023u) - raw);
-  float* fac = reinterpret_cast<float*>(sm + SM::kFac);
   uint64_t* full = reinterpret_cast<uint64_t*>(sm + SM::kBars);
   uint64_t* empty = full + kPfStages;
   uint64_t* q_ready = empty + kPfStages;   // the queries are in shared memory
@@ -366,55 +364,44 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     const int r0 = i0 + t * RT;
     const int nrows = max(0, min(RT, sq.n - r0));
     const int my = t ? nch1 : nch0;
-    // queries: a warp per vector, HD / 32 dims a lane, scaled by a power of two to [2^14, 2^15)
+    // thread = TMEM lane = vector.  Its query, scaled by a power of two to [2^14, 2^15):
+    // a whole row each, which the swizzle spreads over all banks
+    const int v = wq * 32 + lane, vi = v / G, hq = h * G + v - vi * G;
+    const bool live = vi < nrows;
+    float f;
     {
-      constexpr int kDims = HD / 32;
-      uint8_t* qs = sm + t * SM::kQ;
-      const int d = lane * kDims;
-#pragma unroll 1
-      for (int u0 = 0; u0 < 32; u0 += 8) {
-        uint32_t x[8][kDims / 2];
+      uint4 x[HD / 8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const int v = wq * 32 + u0 + u, ii = v / G;
+      for (int i = 0; i < HD / 8; ++i) x[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (live) {
+        const uint4* p = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) +
+                                                        static_cast<long long>(sq.row0 + r0 + vi) * a.ld_q + hq * HD);
 #pragma unroll
-          for (int e = 0; e < kDims / 2; ++e) x[u][e] = 0u;
-          if (ii < nrows) {
-            const uint32_t* p = reinterpret_cast<const uint32_t*>(
-                static_cast<const __nv_bfloat16*>(a.q) + static_cast<long long>(sq.row0 + r0 + ii) * a.ld_q +
-                (h * G + v - ii * G) * HD + d);
-#pragma unroll
-            for (int e = 0; e < kDims / 2; ++e) x[u][e] = __ldg(p + e);
-          }
-        }
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const int v = wq * 32 + u0 + u;
-          float top = 0.f;
-#pragma unroll
-          for (int e = 0; e < kDims / 2; ++e) top = fmaxf(top, fmaxf(fabsf(bf16_lo(x[u][e])), fabsf(bf16_hi(x[u][e]))));
-          top = warp_max(top);
-          const int ex = max(static_cast<int>(__float_as_uint(top) >> 23), 15);
-          const float up = __uint_as_float(static_cast<uint32_t>(268 - ex) << 23);
-          if (lane == 0) {
-            const float down = __uint_as_float(static_cast<uint32_t>(ex - 14) << 23);
-            fac[t * kPfQ + v] = a.softcap > 0.f ? down * (a.scale / a.softcap) : down * (a.scale * kPfLog2e);
-          }
-#pragma unroll
-          for (int e = 0; e < kDims / 2; ++e)
-            *reinterpret_cast<uint32_t*>(qs + (d / 64) * SM::kBox + sw128_offset(v, d % 64 + 2 * e)) =
-                pack_h2(bf16_lo(x[u][e]) * up, bf16_hi(x[u][e]) * up);
-        }
+        for (int i = 0; i < HD / 8; ++i) x[i] = __ldg(p + i);
       }
+      float top = 0.f;
+#pragma unroll
+      for (int i = 0; i < HD / 8; ++i) {
+        top = max3(top, fabsf(bf16_lo(x[i].x)), fabsf(bf16_hi(x[i].x)));
+        top = max3(top, fabsf(bf16_lo(x[i].y)), fabsf(bf16_hi(x[i].y)));
+        top = max3(top, fabsf(bf16_lo(x[i].z)), fabsf(bf16_hi(x[i].z)));
+        top = max3(top, fabsf(bf16_lo(x[i].w)), fabsf(bf16_hi(x[i].w)));
+      }
+      const int ex = max(static_cast<int>(__float_as_uint(top) >> 23), 15);
+      const float up = __uint_as_float(static_cast<uint32_t>(268 - ex) << 23);
+      const float down = __uint_as_float(static_cast<uint32_t>(ex - 14) << 23);
+      f = fmaxf(a.softcap > 0.f ? down * (a.scale / a.softcap) : down * (a.scale * kPfLog2e), 1.2e-38f);
+      uint8_t* qs = sm + t * SM::kQ;
+#pragma unroll
+      for (int i = 0; i < HD / 8; ++i)
+        *reinterpret_cast<uint4*>(qs + (i / 8) * SM::kBox + sw128_offset(v, (i % 8) * 8)) =
+            make_uint4(pack_h2(bf16_lo(x[i].x) * up, bf16_hi(x[i].x) * up), pack_h2(bf16_lo(x[i].y) * up, bf16_hi(x[i].y) * up),
+                       pack_h2(bf16_lo(x[i].z) * up, bf16_hi(x[i].z) * up), pack_h2(bf16_lo(x[i].w) * up, bf16_hi(x[i].w) * up));
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(q_ready);
     }
-    // thread = TMEM lane = vector
-    const int v = wq * 32 + lane, vi = v / G, hq = h * G + v - vi * G;
-    const bool live = vi < nrows;
     const int pos = sq.len + r0 + vi;
-    const float f = fmaxf(fac[t * kPfQ + v], 1.2e-38f);
     const float slope = a.slopes && live ? __ldg(a.slopes + hq) * kPfLog2e : 0.f;
     const uint32_t lanes = static_cast<uint32_t>(wq * 32) << 16;
     const uint32_t ts = tmem + 128u * t + lanes, to = tmem + 256u + 128u * t + lanes;
