@@ -294,8 +294,9 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
   // units, a group's being as many as its blocks and `over` = S more for what a
   // group costs beside them (a step of each warp).  Groups of equal size are not
   // cut across a share where each share holds one part.  16 warps on a group while
-  // that leaves each of them two steps and the shares fill the GPU nearly as well
-  // as smaller teams' would.
+  // that leaves each of them two steps (32 where a share holds several groups: the
+  // small teams of an SM work through one group's start and end beside another's
+  // blocks) and the shares fill the GPU nearly as well as smaller teams' would.
   if (warp == 0) {
     const int groups = all.y;
     int S = kPaTeam, n_teams = 0;
@@ -303,8 +304,8 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     float best = -1.f;
 #pragma unroll 1
     for (int s = W; s >= kPaTeam; s >>= 1) {
-      if (s > kPaTeam && all.x < 2 * s * groups) continue;
       const int log = 31 - __clz(s), most = static_cast<int>(gridDim.x) * (W >> log);
+      if (s > kPaTeam && all.x < (groups > most ? 32 : 2) * s * groups) continue;
       const int few = max(1, (all.x + groups * s) >> (log + 1));       // a share is two steps at least
       int n = min(most, few);
       float fill = 0.9f;

@@ -150,6 +150,7 @@ class PagedCache:
         return ld, p
 
     def _call(self, what, fn, *args):
+        """fn(*args) with the cache's device current (the library launches on the current one)."""
         if self._one_device or self._index == torch.cuda.current_device():
             rc = fn(*args)
         else:
@@ -195,7 +196,9 @@ class PagedCache:
             ld_q, q_p = self._rows("append: q", q, heads, td, esz, n)
             if q_out is None:
                 q_out = torch.empty((n, heads, self.head_dim), dtype=td, device=self.device)
-            ld_o, o_p = self._rows("append: q_out", q_out, heads, td, esz, n)
+                ld_o, o_p = heads * self.head_dim, q_out.data_ptr()
+            else:
+                ld_o, o_p = self._rows("append: q_out", q_out, heads, td, esz, n)
         elif q_out is not None:
             raise ValueError("append: q_out without q")
         self._call("append", self._lib.dvi_paged_append, self._cref, bt, code, k_p, ld_k, v_p, ld_v, rot_p, rot_dim,
@@ -220,7 +223,9 @@ class PagedCache:
         ld_q, q_p = self._rows("attend: q", q, heads, td, esz, n)
         if out is None:
             out = torch.empty((n, heads, self.head_dim), dtype=td, device=self.device)
-        ld_o, o_p = self._rows("attend: out", out, heads, td, esz, n)
+            ld_o, o_p = heads * self.head_dim, out.data_ptr()
+        else:
+            ld_o, o_p = self._rows("attend: out", out, heads, td, esz, n)
         slopes_p = 0
         if slopes is not None:
             if slopes.dtype is not torch.float32 or slopes.shape != (heads,) or not slopes.is_contiguous() or \
