@@ -2,19 +2,19 @@
 // tcgen05 / TMEM; the formulas are those of paged_attn.cuh.
 //
 // A CTA owns one KV head and two tiles of 128 query vectors (tile row v: row
-// v / G of the tile, query head v % G) and walks the 128-position chunks of
+// v / G of the tile, query head v % G) and walks the 64-position chunks of
 // the cache that its rows see.  Both tiles share every chunk, so the codes
 // cross L2 and are widened to f16 once per 256 query vectors.  Per chunk and
 // tile:
-//   S = Q C_k^T    M = 128 vectors, N = 128 positions, K = hd (codes are exact
+//   S = Q C_k^T    M = 128 vectors, N = 64 positions, K = hd (codes are exact
 //                  in f16, and so are bf16 queries scaled by a power of two);
 //   weights        one thread per vector: w = 2^(S f ks + log2 vs - m) as f16
 //                  back into the TMEM columns of S, sum of w / vs;
 //   O += W C_v     A = W from TMEM, B = the widened codes as they lie (rows are
 //                  the K index: MN-major).
 // The accumulator is rescaled only when a vector's maximum outgrows its
-// reference by 2^13.  The scores are read from TMEM twice, for the maximum and
-// for the weights: that keeps a thread within 128 registers.
+// reference by 2^13.  A tile's scores are double-buffered in TMEM, two chunks
+// ahead of the product of its weights, so its threads never wait for them.
 //
 // Roles (512 threads): warps 0-3 and 4-7 hold the vectors of tile 0 and 1,
 // warps 8-11 widen codes (global -> registers -> SW128 tiles in shared memory,
@@ -34,9 +34,9 @@ namespace {
 
 constexpr int kPfThreads = 512;
 constexpr int kPfQ = 128;                // vectors per tile
-constexpr int kPfPos = 128;              // positions per chunk
+constexpr int kPfPos = 64;               // positions per chunk
 constexpr int kPfSegs = kPfPos / 16;     // a page covers whole segments
-constexpr int kPfStages = 4;
+constexpr int kPfStages = 4;             // of K, and of V
 constexpr float kPfLazy = 13.f;          // growth of a maximum that rescales the accumulator
 constexpr float kPfUp = 5.f;             // a new reference sits so far below the maximum
 constexpr float kPfUnset = -1e30f;
@@ -45,11 +45,12 @@ constexpr float kPfLog2e = 1.4426950408889634f;
 template <int HD>
 struct PfSmem {
   static constexpr int kBoxes = HD / 64;               // 64-dim boxes per row
-  static constexpr int kBox = kPfPos * 128;            // 128 rows x 64 f16
+  static constexpr int kBox = kPfPos * 128;            // 64 rows x 64 f16
   static constexpr int kStage = kBoxes * kBox;         // one chunk's K or V
-  static constexpr int kQ = kBoxes * kBox;             // one tile's queries
+  static constexpr int kQBox = kPfQ * 128;
+  static constexpr int kQ = kBoxes * kQBox;            // one tile's queries
   static constexpr int kRing = 2 * kQ;
-  static constexpr int kBars = kRing + kPfStages * kStage;
+  static constexpr int kBars = kRing + 2 * kPfStages * kStage;
   static constexpr int kTotal = kBars + 256 + 1024 /*align*/;
 };
 
@@ -98,15 +99,12 @@ __host__ __device__ constexpr uint32_t idesc_f16_m128(uint32_t n) {
   return (1u << 4) | ((n >> 3) << 17) | ((128u >> 4) << 24);
 }
 // Waits for this thread's TMEM loads, v's among them: the compiler cannot use v before.
-__device__ __forceinline__ void tmem_ld_wait32(float (&v)[32]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+f"(v[0]), "+f"(v[1]), "+f"(v[2]), "+f"(v[3]), "+f"(v[4]), "+f"(v[5]), "+f"(v[6]), "+f"(v[7]),
-                 "+f"(v[8]), "+f"(v[9]), "+f"(v[10]), "+f"(v[11]), "+f"(v[12]), "+f"(v[13]), "+f"(v[14]),
-                 "+f"(v[15]), "+f"(v[16]), "+f"(v[17]), "+f"(v[18]), "+f"(v[19]), "+f"(v[20]), "+f"(v[21]),
-                 "+f"(v[22]), "+f"(v[23]), "+f"(v[24]), "+f"(v[25]), "+f"(v[26]), "+f"(v[27]), "+f"(v[28]),
-                 "+f"(v[29]), "+f"(v[30]), "+f"(v[31])
-               :
-               : "memory");
+__device__ __forceinline__ void tmem_ld_wait64(float (&v)[64]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 64; i += 8)
+    asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]),
+                 "+f"(v[i + 6]), "+f"(v[i + 7]));
 }
 // One lane of a converged warp, always the same.
 __device__ __forceinline__ bool elect_one() {
@@ -146,12 +144,12 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   extern __shared__ uint8_t dsm_raw[];
   const uint32_t raw = smem_u32(dsm_raw);
   uint8_t* sm = dsm_raw + (((raw + 1023u) & ~1023u) - raw);
-  uint64_t* full = reinterpret_cast<uint64_t*>(sm + SM::kBars);
-  uint64_t* empty = full + kPfStages;
-  uint64_t* q_ready = empty + kPfStages;   // the queries are in shared memory
-  uint64_t* s_full = q_ready + 1;          // [2] the tile's scores are in TMEM
-  uint64_t* p_ready = s_full + 2;          // [2] its weights are
-  uint64_t* pv_done = p_ready + 2;         // [2] its accumulator holds the chunk
+  uint64_t* full = reinterpret_cast<uint64_t*>(sm + SM::kBars);   // [K stages, V stages]
+  uint64_t* empty = full + 2 * kPfStages;
+  uint64_t* q_ready = empty + 2 * kPfStages;   // the queries are in shared memory
+  uint64_t* s_full = q_ready + 1;          // [tile][2] the chunk's scores are in TMEM
+  uint64_t* p_ready = s_full + 4;          // [tile][2] its weights are (made up to a chunk before they are used)
+  uint64_t* pv_done = p_ready + 4;         // [2] its accumulator holds the chunk
   uint64_t* fin = pv_done + 2;             // every MMA issued is done
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(fin + 1);
   int* last_s = reinterpret_cast<int*>(tmem_holder + 1);
@@ -202,14 +200,16 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   const int nch0 = max(0, min(all0, c1) - c0), nch1 = max(0, min(all1, c1) - c0), nch = max(nch0, nch1);
 
   if (tid == 0) {
-    for (int s = 0; s < kPfStages; ++s) {
+    for (int s = 0; s < 2 * kPfStages; ++s) {
       mbar_init(&full[s], 4);
       mbar_init(&empty[s], 1);
     }
     mbar_init(q_ready, 8);
     for (int t = 0; t < 2; ++t) {
-      mbar_init(&s_full[t], 1);
-      mbar_init(&p_ready[t], 4);
+      mbar_init(&s_full[2 * t], 1);
+      mbar_init(&s_full[2 * t + 1], 1);
+      mbar_init(&p_ready[2 * t], 4);
+      mbar_init(&p_ready[2 * t + 1], 4);
       mbar_init(&pv_done[t], 1);
     }
     mbar_init(fin, 1);
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_holder;
-  // S / W of tile t: columns 128 t ..; O: 256 + 128 t ..
+  // S of tile t and chunk i: columns 128 t + 64 (i % 2) .., W over its first half; O: 256 + 128 t ..
 
   if (warp >= 12) {
     if (warp == 12) {
@@ -230,65 +230,69 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       const uint32_t id_o = idesc_f16_m128(HD) | kIdescBMn;
       const uint64_t q_desc = smem_desc_sw128(smem_u32(sm));
       const uint64_t k_desc = smem_desc_sw128(smem_u32(sm + SM::kRing));
-      const uint64_t v_desc = smem_desc_sw128_mn(smem_u32(sm + SM::kRing), SM::kBox);
-      auto scores = [&](int t, int s) {
+      const uint64_t v_desc = smem_desc_sw128_mn(smem_u32(sm + SM::kRing + kPfStages * SM::kStage), SM::kBox);
+      auto scores = [&](int t, int i) {
         const uint64_t q = q_desc + static_cast<uint64_t>(t * (SM::kQ >> 4));
-        const uint64_t k = k_desc + static_cast<uint64_t>(s * (SM::kStage >> 4));
+        const uint64_t k = k_desc + static_cast<uint64_t>(i % kPfStages * (SM::kStage >> 4));
+        const uint32_t to = tmem + 128u * t + 64u * (i & 1);
         if (elect_one()) {
 #pragma unroll
-          for (int kk = 0; kk < HD / 16; ++kk) {
-            constexpr int kBox16 = SM::kBox >> 4;
-            const uint64_t off = (kk / 4) * kBox16 + (kk % 4) * 2;
-            tc_mma_bf16(tmem + 128u * t, q + off, k + off, id_s, kk != 0);
-          }
-          tc_commit(&s_full[t]);
+          for (int kk = 0; kk < HD / 16; ++kk)
+            tc_mma_bf16(to, q + ((kk / 4) * (SM::kQBox >> 4) + (kk % 4) * 2), k + ((kk / 4) * (SM::kBox >> 4) + (kk % 4) * 2),
+                        id_s, kk != 0);
+          tc_commit(&s_full[2 * t + (i & 1)]);
         }
         __syncwarp();
       };
-      auto values = [&](int t, int s, bool fresh) {
-        const uint64_t v = v_desc + static_cast<uint64_t>(s * (SM::kStage >> 4));
+      auto values = [&](int t, int i) {
+        const uint64_t v = v_desc + static_cast<uint64_t>(i % kPfStages * (SM::kStage >> 4));
+        const uint32_t from = tmem + 128u * t + 64u * (i & 1);
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < kPfPos / 16; ++kk)
-            tc_mma_bf16_ta(tmem + 256u + 128u * t, tmem + 128u * t + 8u * kk, v + kk * (2048 >> 4), id_o,
-                           kk != 0 || !fresh);
+            tc_mma_bf16_ta(tmem + 256u + 128u * t, from + 8u * kk, v + kk * (2048 >> 4), id_o, kk != 0 || i > 0);
           tc_commit(&pv_done[t]);
         }
         __syncwarp();
       };
-      auto release = [&](int s) {
-        if (elect_one()) tc_commit(&empty[s]);
+      auto release = [&](int kv, int i) {
+        if (elect_one()) tc_commit(&empty[kv * kPfStages + i % kPfStages]);
         __syncwarp();
       };
-      auto full_wait = [&](int it) { return mbar_wait(&full[it % kPfStages], (it / kPfStages) & 1, c.status); };
-      bool ok = nch > 0 && mbar_wait(q_ready, 0, c.status) && full_wait(0);
-      if (ok) {
+      auto full_wait = [&](int kv, int i) {
+        const bool r = mbar_wait(&full[kv * kPfStages + i % kPfStages], (i / kPfStages) & 1, c.status);
         tc_fence_after();
-        if (nch0 > 0) scores(0, 0);
-        if (nch1 > 0) scores(1, 0);
-        release(0);
+        return r;
+      };
+      bool ok = nch > 0 && mbar_wait(q_ready, 0, c.status);
+      for (int i = 0; i < min(nch, 2) && ok; ++i) {
+        ok = full_wait(0, i);
+        if (!ok) break;
+        if (i < nch0) scores(0, i);
+        if (i < nch1) scores(1, i);
+        release(0, i);
       }
+      // the scores are two chunks ahead of the weights' product, so the weights never wait for them
       for (int i = 0; i < nch && ok; ++i) {
-        const int iv = 2 * i + 1, sv = iv % kPfStages, ik = iv + 1, sk = ik % kPfStages;
-        ok = full_wait(iv) && (i + 1 >= nch || full_wait(ik));
-        // one tile's W C_v and next scores while the other's weights are made
+        const bool more = i + 2 < nch;
+        ok = full_wait(1, i) && (!more || full_wait(0, i + 2));
         for (int t = 0; t < 2 && ok; ++t) {
           const int mine = t ? nch1 : nch0;
           if (i >= mine) continue;
-          ok = mbar_wait(&p_ready[t], i & 1, c.status);
+          ok = mbar_wait(&p_ready[2 * t + (i & 1)], (i >> 1) & 1, c.status);
           if (!ok) break;
           tc_fence_after();
-          values(t, sv, i == 0);
-          if (i + 1 >= mine) continue;
-          // the next scores overwrite the columns that W C_v reads
+          values(t, i);
+          if (i + 2 >= mine) continue;
+          // the scores of chunk i + 2 overwrite the columns that this product reads
           ok = mbar_wait(&pv_done[t], i & 1, c.status);
           if (!ok) break;
           tc_fence_after();
-          scores(t, sk);
+          scores(t, i + 2);
         }
         if (!ok) break;
-        release(sv);
-        if (i + 1 < nch) release(sk);
+        release(1, i);
+        if (more) release(0, i + 2);
       }
       // every MMA issued is done before the TMEM is freed
       if (elect_one()) tc_commit(fin);
@@ -296,66 +300,63 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     }
     __syncwarp();
   } else if (warp >= 8) {
-    // ---------------- widening: tiles K c0, V c0, K c0 + 1, ...; a warp's 32 rows are two 16-row segments
+    // ---------------- widening: tiles K c0, V c0, K c0 + 1, ...; a warp has the 16 rows of one segment
     const int w = warp - 8;
     constexpr int kRow = HD / 16;                       // 16-byte chunks of a row
     constexpr int kRows = 32 / kRow;                    // rows at once
-    constexpr int kLoads = 32 / kRows;
+    constexpr int kLoads = 16 / kRows;
     // eight lanes write two rows of one 64-dim box: no bank meets twice
     const int ch = HD == 128 ? (lane & 3) | ((lane >> 1) & 4) : lane & 3;
     const int r0 = HD == 128 ? ((lane >> 2) & 1) | ((lane >> 3) & 2) : lane >> 2;
     const size_t page_bytes = (static_cast<size_t>(c.H) << c.log_p) * HD;
     const size_t lane_off = ((static_cast<size_t>(h) << c.log_p) + r0) * HD + ch * 16;
-    auto entry = [&](int i, int half) {
-      const int p = (c0 + i) * kPfPos + 32 * w + 16 * half;
+    auto entry = [&](int i) {
+      const int p = (c0 + i) * kPfPos + 16 * w;
       return i < nch && p < held_end ? paged_entry(c, b, p >> c.log_p) : -1;
     };
-    int e0 = entry(0, 0), e1 = entry(0, 1);
-    uint4 code[2][kLoads];                              // the next K tile's codes, and the next V tile's
-    auto load = [&](int i, int kv, int g0, int g1) {    // chunk i, its pages' entries
-      const uint8_t* pool = kv ? c.v : c.k;
-      const int p = (c0 + i) * kPfPos + 32 * w;
+    // codes of two chunks are in flight: chunk i's in code[i % 2]
+    uint4 code[2][2][kLoads];
+    auto load = [&](int i, uint4 (&to)[2][kLoads], int raw_entry) {
+      const int pg = paged_valid(c, raw_entry), p = (c0 + i) * kPfPos + 16 * w;
+      const size_t at = static_cast<size_t>(max(pg, 0)) * page_bytes + (p & (c.P - 1)) * HD + lane_off;
+      const int live = pg >= 0 ? held_end - p - r0 : 0;            // rows past it, and pages not held: zeros
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int pg = paged_valid(c, half ? g1 : g0), ph = p + 16 * half;
-        const uint8_t* src = pool + static_cast<size_t>(max(pg, 0)) * page_bytes + (ph & (c.P - 1)) * HD + lane_off;
-        const int live = pg >= 0 ? held_end - ph - r0 : 0;         // rows past it, and pages not held: zeros
+      for (int kv = 0; kv < 2; ++kv)
 #pragma unroll
-        for (int u = 0; u < kLoads / 2; ++u)
-          code[kv][half * (kLoads / 2) + u] =
-              u * kRows < live ? __ldg(reinterpret_cast<const uint4*>(src + u * kRows * HD)) : make_uint4(0u, 0u, 0u, 0u);
-      }
+        for (int u = 0; u < kLoads; ++u)
+          to[kv][u] = u * kRows < live ? __ldg(reinterpret_cast<const uint4*>((kv ? c.v : c.k) + at + u * kRows * HD))
+                                       : make_uint4(0u, 0u, 0u, 0u);
     };
-    if (nch > 0) {
-      load(0, 0, e0, e1);
-      load(0, 1, e0, e1);
-      e0 = entry(1, 0);
-      e1 = entry(1, 1);
-    }
+    const int first_entry = entry(0), second_entry = entry(1);
+    int ent = entry(2);
+    if (nch > 0) load(0, code[0], first_entry);
+    if (nch > 1) load(1, code[1], second_entry);
     bool ok = true;
-    for (int i = 0; i < nch && ok; ++i) {
-      const int n0 = e0, n1 = e1;                       // the next chunk's
-      e0 = entry(i + 2, 0);
-      e1 = entry(i + 2, 1);
+    for (int i0w = 0; i0w < nch && ok; i0w += 2) {
 #pragma unroll
-      for (int kv = 0; kv < 2; ++kv) {
-        const int it = 2 * i + kv, s = it % kPfStages;
-        ok = ok && mbar_wait(&empty[s], ((it / kPfStages) & 1) ^ 1, c.status);
-        if (!ok) break;
-        uint8_t* dst = sm + SM::kRing + s * SM::kStage + (ch / 4) * SM::kBox;
+      for (int k = 0; k < 2; ++k) {
+        const int i = i0w + k;
+        if (i >= nch || !ok) break;
+        const int s = i % kPfStages;
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) {
-          const int row = 32 * w + u * kRows + r0;
-          uint4 x[2];
-          widen<E4M3>(code[kv][u], x[0], x[1]);
+        for (int kv = 0; kv < 2; ++kv) {
+          ok = ok && mbar_wait(&empty[kv * kPfStages + s], ((i / kPfStages) & 1) ^ 1, c.status);
+          if (!ok) break;
+          uint8_t* dst = sm + SM::kRing + (kv * kPfStages + s) * SM::kStage + (ch / 4) * SM::kBox;
 #pragma unroll
-          for (int k = 0; k < 2; ++k)
-            *reinterpret_cast<uint4*>(dst + sw128_offset(row, (2 * (ch % 4) + k) * 8)) = x[k];
+          for (int u = 0; u < kLoads; ++u) {
+            uint4 x[2];
+            widen<E4M3>(code[k][kv][u], x[0], x[1]);
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              *reinterpret_cast<uint4*>(dst + sw128_offset(16 * w + u * kRows + r0, (2 * (ch % 4) + e) * 8)) = x[e];
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&full[kv * kPfStages + s]);
         }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&full[s]);
-        if (i + 1 < nch) load(i + 1, kv, n0, n1);
+        if (ok && i + 2 < nch) load(i + 2, code[k], ent);
+        ent = entry(i + 3);
       }
     }
   } else {
@@ -394,7 +395,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       uint8_t* qs = sm + t * SM::kQ;
 #pragma unroll
       for (int i = 0; i < HD / 8; ++i)
-        *reinterpret_cast<uint4*>(qs + (i / 8) * SM::kBox + sw128_offset(v, (i % 8) * 8)) =
+        *reinterpret_cast<uint4*>(qs + (i / 8) * SM::kQBox + sw128_offset(v, (i % 8) * 8)) =
             make_uint4(pack_h2(bf16_lo(x[i].x) * up, bf16_hi(x[i].x) * up), pack_h2(bf16_lo(x[i].y) * up, bf16_hi(x[i].y) * up),
                        pack_h2(bf16_lo(x[i].z) * up, bf16_hi(x[i].z) * up), pack_h2(bf16_lo(x[i].w) * up, bf16_hi(x[i].w) * up));
       fence_proxy_async_smem();
@@ -405,7 +406,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     const float slope = a.slopes && live ? __ldg(a.slopes + hq) * kPfLog2e : 0.f;
     const uint32_t lanes = static_cast<uint32_t>(wq * 32) << 16;
     const uint32_t ts = tmem + 128u * t + lanes, to = tmem + 256u + 128u * t + lanes;
-    // scales: lane e < 8 holds those of segment e; entries are read two chunks ahead, scales one
+    // scales: lane e < 4 holds those of segment e; entries are read two chunks ahead, scales one
     auto entry = [&](int i) {
       const int p = (c0 + i) * kPfPos + 16 * lane;
       return lane < kPfSegs && i < my && p < held_end ? paged_entry(c, b, p >> c.log_p) : -1;
@@ -428,60 +429,48 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       const float iv_l = __fdividef(1.f, vx);
       scales();
       e_next = entry(i + 2);
-      if (!mbar_wait(&s_full[t], i & 1, c.status)) {
+      if (!mbar_wait(&s_full[2 * t + (i & 1)], (i >> 1) & 1, c.status)) {
         ok = false;
         break;
       }
       tc_fence_after();
+      const uint32_t tsi = ts + 64u * (i & 1);
       const int at = (c0 + i) * kPfPos;
       const int see = pos - at;                        // positions 0 .. see of the chunk are visible,
       const int from = a.window > 0 ? see - a.window + 1 : 0;       // and only those from here on
       const bool edge = __any_sync(0xffffffffu, live && (see < kPfPos - 1 || from > 0));
-      // what the vector does not see of 32 columns; with CURVED the finished scores, else still the products
-      auto finish = [&](float (&s)[32], int c32) {
-        if (CURVED) {
+      float s[kPfPos], fk[kPfSegs], lv[kPfSegs];
+      tmem_ld32_async(tsi, s);
+      tmem_ld32_async(tsi + 32, s + 32);
 #pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const float fk = f * __shfl_sync(0xffffffffu, ks_l, c32 / 16 + g);
-            const float lv = __shfl_sync(0xffffffffu, lv_l, c32 / 16 + g);
+      for (int g = 0; g < kPfSegs; ++g) {
+        fk[g] = f * __shfl_sync(0xffffffffu, ks_l, g);
+        lv[g] = __shfl_sync(0xffffffffu, lv_l, g);
+      }
+      tmem_ld_wait64(s);
+      if (CURVED) {
+        // the finished scores in place of the products
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              float x = s[16 * g + e] * fk;
-              if (a.softcap > 0.f) x = (1.f - __fdividef(2.f, 1.f + ex2(x * (2.f * kPfLog2e)))) * (a.softcap * kPfLog2e);
-              s[16 * g + e] = fmaf(slope, static_cast<float>(c32 + 16 * g + e - see), x + lv);
-            }
-          }
+        for (int e = 0; e < kPfPos; ++e) {
+          float x = s[e] * fk[e / 16];
+          if (a.softcap > 0.f) x = (1.f - __fdividef(2.f, 1.f + ex2(x * (2.f * kPfLog2e)))) * (a.softcap * kPfLog2e);
+          s[e] = fmaf(slope, static_cast<float>(e - see), x + lv[e / 16]);
         }
-        if (edge) {
+      }
+      if (edge) {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) s[e] = c32 + e <= see && c32 + e >= from ? s[e] : -INFINITY;
-        }
-      };
-      float buf[2][32];
+        for (int e = 0; e < kPfPos; ++e) s[e] = e <= see && e >= from ? s[e] : -INFINITY;
+      }
       float top = -INFINITY;
-      tmem_ld32_async(ts, buf[0]);
-      // (two groups of columns to an iteration: the loops' code stays in the instruction cache)
-#pragma unroll 1
-      for (int q0 = 0; q0 < 4; q0 += 2) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int q = q0 + k;
-          tmem_ld_wait32(buf[k]);
-          if (q < 3) tmem_ld32_async(ts + 32 * (q + 1), buf[k ^ 1]);
-          float (&s)[32] = buf[k];
-          finish(s, 32 * q);
+      for (int g = 0; g < kPfSegs; ++g) {
+        const float* z = s + 16 * g;
+        float x = fmaxf(z[0], z[1]), y = fmaxf(z[2], z[3]);
 #pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            float x = fmaxf(s[16 * g], s[16 * g + 1]), y = fmaxf(s[16 * g + 2], s[16 * g + 3]);
-#pragma unroll
-            for (int e = 4; e < 16; e += 4) x = max3(x, s[16 * g + e], s[16 * g + e + 1]), y = max3(y, s[16 * g + e + 2], s[16 * g + e + 3]);
-            x = fmaxf(x, y);
-            // a segment's factor is positive: its largest product is its largest score
-            if (!CURVED)
-              x = fmaf(x, f * __shfl_sync(0xffffffffu, ks_l, 2 * q + g), __shfl_sync(0xffffffffu, lv_l, 2 * q + g));
-            top = fmaxf(top, x);
-          }
-        }
+        for (int e = 4; e < 16; e += 4) x = max3(x, z[e], z[e + 1]), y = max3(y, z[e + 2], z[e + 3]);
+        x = fmaxf(x, y);
+        // a segment's factor is positive: its largest product is its largest score
+        top = fmaxf(top, CURVED ? x : fmaf(x, fk[g], lv[g]));
       }
       const bool move = top > m + kPfLazy;
       if (__any_sync(0xffffffffu, move)) {
@@ -506,41 +495,38 @@ __global__ void __launch_bounds__(kPfThreads, 1)
           tmem_st_wait();
         }
       }
-      tmem_ld32_async(ts, buf[0]);
-#pragma unroll 1
-      for (int q0 = 0; q0 < 4; q0 += 2) {
+#pragma unroll
+      for (int q = 0; q < kPfPos / 32; ++q) {
+        uint32_t w[16];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const int q = q0 + k;
-          tmem_ld_wait32(buf[k]);
-          if (q < 3) tmem_ld32_async(ts + 32 * (q + 1), buf[k ^ 1]);
-          float (&s)[32] = buf[k];
-          finish(s, 32 * q);
-          uint32_t w[16];
+          const int g = 2 * q + k;
+          const float fg = CURVED ? 1.f : fk[g], lg = (CURVED ? 0.f : lv[g]) - m;
+          const uint64_t f2 = pack2(fg, fg), l2 = pack2(lg, lg);
+          uint64_t sum = 0ull;
 #pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const float fk = CURVED ? 1.f : f * __shfl_sync(0xffffffffu, ks_l, 2 * q + g);
-            const float lv = (CURVED ? 0.f : __shfl_sync(0xffffffffu, lv_l, 2 * q + g)) - m;
-            const uint64_t fk2 = pack2(fk, fk), lv2 = pack2(lv, lv);
-            uint64_t sum = 0ull;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float2 x = unpack2(fma2(pack2(s[16 * g + 2 * e], s[16 * g + 2 * e + 1]), fk2, lv2));
-              const float p0 = ex2(x.x), p1 = ex2(x.y);
-              sum = add2(sum, pack2(p0, p1));
-              w[8 * g + e] = pack_h2(p0, p1);
-            }
-            const float2 both = unpack2(sum);
-            l = fmaf(both.x + both.y, __shfl_sync(0xffffffffu, iv_l, 2 * q + g), l);
+          for (int e = 0; e < 8; ++e) {
+            const float2 x = unpack2(fma2(pack2(s[16 * g + 2 * e], s[16 * g + 2 * e + 1]), f2, l2));
+            const float p0 = ex2(x.x), p1 = ex2(x.y);
+            sum = add2(sum, pack2(p0, p1));
+            w[8 * k + e] = pack_h2(p0, p1);
           }
-          // columns up to 16 q + 15 hold scores that are read by now
-          tmem_st16(ts + 16 * q, w);
+          const float2 both = unpack2(sum);
+          l = fmaf(both.x + both.y, __shfl_sync(0xffffffffu, iv_l, g), l);
         }
+        tmem_st16(tsi + 16 * q, w);
       }
       tmem_st_wait();
+      // A parity tells neighbouring phases apart only.  Chunk i's scores say that product
+      // i - 2 is done; the wait for the last product, below, needs the one before it
+      // done, and the last not begun, while this warp still holds its weights back.
+      if (i + 1 == my && i > 0 && !mbar_wait(&pv_done[t], (i - 1) & 1, c.status)) {
+        ok = false;
+        break;
+      }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&p_ready[t]);
+      if (lane == 0) mbar_arrive(&p_ready[2 * t + (i & 1)]);
     }
     // ---------------- O / l, or this split's part
     constexpr int kPart = 2 * kPfQ * (HD + 2);
@@ -645,9 +631,9 @@ cudaError_t launch_pf(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
                                             (per + 2 * rt - 1) / (2 * rt);
   const long long units = items * c.H;
   if (units > 0x7fffffffll) return cudaErrorInvalidConfiguration;
-  // splits only fill SMs that the tiles leave idle, four chunks each at the least
+  // splits only fill SMs that the tiles leave idle, eight chunks each at the least
   const int chunks = static_cast<int>(((static_cast<long long>(c.max_pages) << c.log_p) + kPfPos - 1) / kPfPos);
-  const int splits = static_cast<int>(std::max(1ll, std::min<long long>({n_sms / units, chunks / 4, 16})));
+  const int splits = static_cast<int>(std::max(1ll, std::min<long long>({n_sms / units, chunks / 8, 16})));
   return launch_pdl(paged_pf_kernel<E4M3, HD, CURVED>, dim3(static_cast<unsigned>(units), splits), dim3(kPfThreads),
                     PfSmem<HD>::kTotal, s, a, static_cast<int>(items), rt, splits);
 }
