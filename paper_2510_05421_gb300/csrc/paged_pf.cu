@@ -283,8 +283,10 @@ __global__ void __launch_bounds__(kPfThreads, 1)
           if (!ok) break;
           tc_fence_after();
           values(t, i);
-          if (i + 2 >= mine) continue;
-          // the scores of chunk i + 2 overwrite the columns that this product reads
+        }
+        for (int t = 0; t < 2 && ok; ++t) {
+          if (i + 2 >= (t ? nch1 : nch0)) continue;
+          // the scores of chunk i + 2 overwrite the columns that product i reads
           ok = mbar_wait(&pv_done[t], i & 1, c.status);
           if (!ok) break;
           tc_fence_after();
