@@ -36,7 +36,7 @@ constexpr int kPfThreads = 512;
 constexpr int kPfQ = 128;                // vectors per tile
 constexpr int kPfPos = 64;               // positions per chunk
 constexpr int kPfSegs = kPfPos / 16;     // a page covers whole segments
-constexpr int kPfStages = 4;             // of K, and of V
+constexpr int kPfStages = 4;             // of K, and of V (even: a chunk's stage tells its score buffer)
 constexpr float kPfLazy = 13.f;          // growth of a maximum that rescales the accumulator
 constexpr float kPfUp = 5.f;             // a new reference sits so far below the maximum
 constexpr float kPfUnset = -1e30f;
@@ -224,39 +224,42 @@ __global__ void __launch_bounds__(kPfThreads, 1)
 
   if (warp >= 12) {
     if (warp == 12) {
-      // ---------------- MMA issuer: the whole warp walks the chunks, so that the
-      // descriptors are uniform values, and one lane issues
+      // ---------------- MMA issuer: the whole warp walks the chunks and one lane issues.
+      // The loop is unrolled over the stages, so that every descriptor is a uniform base
+      // and a constant: with stages computed at run time an MMA took 107 cycles to issue
+      // (54 on the pipe).
       const uint32_t id_s = idesc_f16_m128(kPfPos);
       const uint32_t id_o = idesc_f16_m128(HD) | kIdescBMn;
       const uint64_t q_desc = smem_desc_sw128(smem_u32(sm));
       const uint64_t k_desc = smem_desc_sw128(smem_u32(sm + SM::kRing));
       const uint64_t v_desc = smem_desc_sw128_mn(smem_u32(sm + SM::kRing + kPfStages * SM::kStage), SM::kBox);
-      auto scores = [&](int t, int i) {
+      const uint32_t tm = __reduce_max_sync(0xffffffffu, tmem);
+      // scores of tile t and a chunk whose stage is s (a multiple of 4 before it)
+      auto scores = [&](int t, int s) {
         const uint64_t q = q_desc + static_cast<uint64_t>(t * (SM::kQ >> 4));
-        const uint64_t k = k_desc + static_cast<uint64_t>(i % kPfStages * (SM::kStage >> 4));
-        const uint32_t to = tmem + 128u * t + 64u * (i & 1);
+        const uint64_t k = k_desc + static_cast<uint64_t>(s * (SM::kStage >> 4));
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < HD / 16; ++kk)
-            tc_mma_bf16(to, q + ((kk / 4) * (SM::kQBox >> 4) + (kk % 4) * 2), k + ((kk / 4) * (SM::kBox >> 4) + (kk % 4) * 2),
-                        id_s, kk != 0);
-          tc_commit(&s_full[2 * t + (i & 1)]);
+            tc_mma_bf16(tm + 128u * t + 64u * (s & 1), q + ((kk / 4) * (SM::kQBox >> 4) + (kk % 4) * 2),
+                        k + ((kk / 4) * (SM::kBox >> 4) + (kk % 4) * 2), id_s, kk != 0);
+          tc_commit(&s_full[2 * t + (s & 1)]);
         }
         __syncwarp();
       };
-      auto values = [&](int t, int i) {
-        const uint64_t v = v_desc + static_cast<uint64_t>(i % kPfStages * (SM::kStage >> 4));
-        const uint32_t from = tmem + 128u * t + 64u * (i & 1);
+      auto values = [&](int t, int s, uint32_t add) {
+        const uint64_t v = v_desc + static_cast<uint64_t>(s * (SM::kStage >> 4));
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < kPfPos / 16; ++kk)
-            tc_mma_bf16_ta(tmem + 256u + 128u * t, from + 8u * kk, v + kk * (2048 >> 4), id_o, kk != 0 || i > 0);
+            tc_mma_bf16_ta(tm + 256u + 128u * t, tm + 128u * t + 64u * (s & 1) + 8u * kk, v + kk * (2048 >> 4), id_o,
+                           kk == 0 ? add : 1u);
           tc_commit(&pv_done[t]);
         }
         __syncwarp();
       };
-      auto release = [&](int kv, int i) {
-        if (elect_one()) tc_commit(&empty[kv * kPfStages + i % kPfStages]);
+      auto release = [&](int kv, int s) {
+        if (elect_one()) tc_commit(&empty[kv * kPfStages + s]);
         __syncwarp();
       };
       auto full_wait = [&](int kv, int i) {
@@ -265,7 +268,9 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         return r;
       };
       bool ok = nch > 0 && mbar_wait(q_ready, 0, c.status);
-      for (int i = 0; i < min(nch, 2) && ok; ++i) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (i >= nch || !ok) break;
         ok = full_wait(0, i);
         if (!ok) break;
         if (i < nch0) scores(0, i);
@@ -273,28 +278,34 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         release(0, i);
       }
       // the scores are two chunks ahead of the weights' product, so the weights never wait for them
-      for (int i = 0; i < nch && ok; ++i) {
-        const bool more = i + 2 < nch;
-        ok = full_wait(1, i) && (!more || full_wait(0, i + 2));
-        for (int t = 0; t < 2 && ok; ++t) {
-          const int mine = t ? nch1 : nch0;
-          if (i >= mine) continue;
-          ok = mbar_wait(&p_ready[2 * t + (i & 1)], (i >> 1) & 1, c.status);
+      for (int i4 = 0; i4 < nch && ok; i4 += kPfStages) {
+#pragma unroll
+        for (int s = 0; s < kPfStages; ++s) {
+          const int i = i4 + s, s2 = (s + 2) % kPfStages;
+          if (i >= nch || !ok) break;
+          const bool more = i + 2 < nch;
+          ok = full_wait(1, i) && (!more || full_wait(0, i + 2));
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (!ok || i >= (t ? nch1 : nch0)) continue;
+            ok = mbar_wait(&p_ready[2 * t + (s & 1)], (i >> 1) & 1, c.status);
+            if (!ok) continue;
+            tc_fence_after();
+            values(t, s, i > 0);
+          }
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (!ok || i + 2 >= (t ? nch1 : nch0)) continue;
+            // the scores of chunk i + 2 overwrite the columns that product i reads
+            ok = mbar_wait(&pv_done[t], i & 1, c.status);
+            if (!ok) continue;
+            tc_fence_after();
+            scores(t, s2);
+          }
           if (!ok) break;
-          tc_fence_after();
-          values(t, i);
+          release(1, s);
+          if (more) release(0, s2);
         }
-        for (int t = 0; t < 2 && ok; ++t) {
-          if (i + 2 >= (t ? nch1 : nch0)) continue;
-          // the scores of chunk i + 2 overwrite the columns that product i reads
-          ok = mbar_wait(&pv_done[t], i & 1, c.status);
-          if (!ok) break;
-          tc_fence_after();
-          scores(t, i + 2);
-        }
-        if (!ok) break;
-        release(1, i);
-        if (more) release(0, i + 2);
       }
       // every MMA issued is done before the TMEM is freed
       if (elect_one()) tc_commit(fin);
