@@ -25,6 +25,7 @@
 //
 // Every wait is bounded (flag, then wind down).
 #include <algorithm>
+#include <type_traits>
 
 #include "paged.cuh"
 
@@ -220,6 +221,9 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_holder;
+  // a split's part: [HD / 4][256 vectors] quads of dims, then maxima and sums
+  constexpr int kPart = 2 * kPfQ * (HD + 2);
+  const int unit = item * c.H + h;
   // S of tile t and chunk i: columns 128 t + 64 (i % 2) .., W over its first half; O: 256 + 128 t ..
 
   if (warp >= 12) {
@@ -542,8 +546,6 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       if (lane == 0) mbar_arrive(&p_ready[2 * t + (i & 1)]);
     }
     // ---------------- O / l, or this split's part
-    constexpr int kPart = 2 * kPfQ * (HD + 2);
-    const int unit = item * c.H + h;
     float* part = a.pf_part + static_cast<size_t>(unit * splits + split) * kPart;
     const bool done = ok && my > 0 && mbar_wait(&pv_done[t], (my - 1) & 1, c.status);
     if (done) tc_fence_after();
@@ -579,44 +581,6 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     if (splits > 1) {
       __stcg(part + 2 * kPfQ * HD + vp, m);
       __stcg(part + 2 * kPfQ * HD + 2 * kPfQ + vp, l);
-      named_bar(1, 256);
-      if (tid == 0) {
-        __threadfence();
-        const int n = atomicAdd(a.pf_counters + unit, 1);
-        *last_s = n == splits - 1;
-        if (n == splits - 1) a.pf_counters[unit] = 0;
-        __threadfence();
-      }
-      named_bar(1, 256);
-      if (*last_s && live) {
-        const float* p0 = a.pf_part + static_cast<size_t>(unit * splits) * kPart;
-        float M = kPfUnset, L = 0.f;
-        for (int s = 0; s < splits; ++s) M = fmaxf(M, __ldcg(p0 + static_cast<size_t>(s) * kPart + 2 * kPfQ * HD + vp));
-        for (int s = 0; s < splits; ++s) {
-          const float* p = p0 + static_cast<size_t>(s) * kPart + 2 * kPfQ * HD + vp;
-          L = fmaf(__ldcg(p + 2 * kPfQ), ex2(__ldcg(p) - M), L);
-        }
-        const float k = L > 0.f ? 1.f / L : (L == L ? 0.f : L);
-#pragma unroll 1
-        for (int d = 0; d < HD; d += 16) {
-          float o[16];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] = 0.f;
-#pragma unroll 2
-          for (int s = 0; s < splits; ++s) {
-            const float* p = p0 + static_cast<size_t>(s) * kPart;
-            const float w = ex2(__ldcg(p + 2 * kPfQ * HD + vp) - M);
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-              const float4 x = __ldcg(reinterpret_cast<const float4*>(
-                  p + static_cast<size_t>((d + e) / 4) * (2 * kPfQ * 4) + vp * 4));
-              o[e] = fmaf(x.x, w, o[e]), o[e + 1] = fmaf(x.y, w, o[e + 1]);
-              o[e + 2] = fmaf(x.z, w, o[e + 2]), o[e + 3] = fmaf(x.w, w, o[e + 3]);
-            }
-          }
-          store16(d, o, k);
-        }
-      }
     }
   }
   tc_fence_before();
@@ -625,6 +589,84 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
+  if (splits == 1) return;
+  // ---------------- the last split to end joins all parts, in order
+  if (tid == 0) {
+    __threadfence();
+    const int n = atomicAdd(a.pf_counters + unit, 1);
+    *last_s = n == splits - 1;
+    if (n == splits - 1) a.pf_counters[unit] = 0;
+    __threadfence();
+  }
+  __syncthreads();
+  if (!*last_s) return;
+  const float* parts = a.pf_part + static_cast<size_t>(unit * splits) * kPart;
+  const int rows = min(pair, sq.n - i0), vecs0 = min(rows, RT) * G, vecs_all = vecs0 + max(rows - RT, 0) * G;
+  // kItems quads of a thread at a time, kAtOnce parts of each in flight
+  auto join = [&](auto items, auto at_once) {
+    constexpr int kItems = decltype(items)::value, kAtOnce = decltype(at_once)::value;
+    const int total = vecs_all * (HD / 4);
+#pragma unroll 1
+    for (int e0 = tid; e0 < total; e0 += kItems * kPfThreads) {
+      float M[kItems], L[kItems];
+      float4 acc[kItems];
+      const float* at[kItems];
+      int vp[kItems], quad[kItems];
+#pragma unroll
+      for (int u = 0; u < kItems; ++u) {
+        const int e = min(e0 + u * kPfThreads, total - 1);
+        quad[u] = e / vecs_all;
+        const int x = e - quad[u] * vecs_all, t = x < vecs0 ? 0 : 1;
+        vp[u] = t * kPfQ + x - t * vecs0;
+        at[u] = parts + static_cast<size_t>(quad[u] * (2 * kPfQ) + vp[u]) * 4;
+        M[u] = kPfUnset, L[u] = 0.f, acc[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll 1
+      for (int s0 = 0; s0 < splits; s0 += kAtOnce) {
+        float pm[kItems][kAtOnce], ps[kItems][kAtOnce];
+        float4 o[kItems][kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kItems; ++u)
+#pragma unroll
+          for (int k = 0; k < kAtOnce; ++k) {
+            const size_t p = static_cast<size_t>(min(s0 + k, splits - 1)) * kPart;
+            pm[u][k] = __ldcg(parts + p + 2 * kPfQ * HD + vp[u]);
+            ps[u][k] = __ldcg(parts + p + 2 * kPfQ * HD + 2 * kPfQ + vp[u]);
+            o[u][k] = __ldcg(reinterpret_cast<const float4*>(at[u] + p));
+          }
+#pragma unroll
+        for (int u = 0; u < kItems; ++u) {
+          float top = M[u];
+#pragma unroll
+          for (int k = 0; k < kAtOnce; ++k)
+            if (s0 + k < splits) top = fmaxf(top, pm[u][k]);
+          const float shrink = ex2(M[u] - top);
+          M[u] = top;
+          acc[u].x *= shrink, acc[u].y *= shrink, acc[u].z *= shrink, acc[u].w *= shrink, L[u] *= shrink;
+#pragma unroll
+          for (int k = 0; k < kAtOnce; ++k) {
+            if (s0 + k >= splits) continue;
+            const float w = ex2(pm[u][k] - top);
+            acc[u].x = fmaf(o[u][k].x, w, acc[u].x), acc[u].y = fmaf(o[u][k].y, w, acc[u].y);
+            acc[u].z = fmaf(o[u][k].z, w, acc[u].z), acc[u].w = fmaf(o[u][k].w, w, acc[u].w);
+            L[u] = fmaf(ps[u][k], w, L[u]);
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kItems; ++u) {
+        if (e0 + u * kPfThreads >= total) continue;
+        const int t = vp[u] / kPfQ, v = vp[u] % kPfQ, row = i0 + t * RT + v / G, hq = h * G + v % G;
+        const float k = L[u] > 0.f ? 1.f / L[u] : (L[u] == L[u] ? 0.f : L[u]);
+        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + static_cast<long long>(sq.row0 + row) * a.ld_o +
+                                  hq * HD + 4 * quad[u]) =
+            make_uint2(pack_bf16x2(acc[u].x * k, acc[u].y * k), pack_bf16x2(acc[u].z * k, acc[u].w * k));
+      }
+    }
+  };
+  using std::integral_constant;
+  if (splits <= 3) join(integral_constant<int, 4>{}, integral_constant<int, 3>{});
+  else join(integral_constant<int, 1>{}, integral_constant<int, 8>{});
 }
 
 namespace {
