@@ -1,4 +1,5 @@
-"""Build libdvi.so in-tree from csrc/*.cu for sm_103a (nvcc, no torch extension).
+"""Build libdvi.so in-tree from csrc/*.cu for sm_103a (nvcc, no torch extension), and the CPython module _paged.so
+(the paged cache's argument checks) from csrc/paged_py.c.
 
     python -m paper_2510_05421_gb300.build
 """
@@ -8,11 +9,13 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libdvi.so")
+PY_OUT = os.path.join(HERE, "_paged.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
          "-Xcompiler", "-Wno-deprecated-declarations"]
@@ -27,6 +30,18 @@ def nvcc() -> str:
 
 def sources():
     return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cu"))
+
+
+def build_py() -> str:
+    """The CPython side of the paged cache's binding."""
+    tmp = PY_OUT + ".tmp"
+    cmd = [os.environ.get("CC") or "gcc", "-O2", "-fPIC", "-shared", "-std=c11", "-Wall", "-Wextra",
+           "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "paged_py.c"), "-o", tmp]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{cmd[0]} failed on paged_py.c:\n{r.stderr}")
+    os.replace(tmp, PY_OUT)
+    return PY_OUT
 
 
 def build(verbose: bool = False, ptxas_info: bool = False) -> str:
@@ -55,6 +70,7 @@ def build(verbose: bool = False, ptxas_info: bool = False) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stderr}")
     os.replace(tmp, OUT)
+    build_py()
     return OUT
 
 
