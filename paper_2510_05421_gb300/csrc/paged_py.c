@@ -233,8 +233,8 @@ static PyObject* py_append(PyObject* self, PyObject* const* a, Py_ssize_t n_args
     PyObject* qt;
     int64_t qn;
     if (!lead_of("append: q", a[7], &qt, &qn, &heads)) return NULL;
-    if (heads < 1) {
-      refuse("append: q", "no heads");
+    if (heads < 1 || a[11] == Py_None) {
+      refuse("append: q", "no heads, or no q_out");
       return NULL;
     }
     if (!rows_of(&c, "append: q", a[7], dtype, n, heads, &q, &ld_q) ||
