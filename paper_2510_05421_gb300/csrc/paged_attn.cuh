@@ -306,7 +306,8 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     for (int s = W; s >= kPaTeam; s >>= 1) {
       const int log = 31 - __clz(s), most = static_cast<int>(gridDim.x) * (W >> log);
       if (s > kPaTeam && all.x < (groups > most ? 32 : 2) * s * groups) continue;
-      const int few = max(1, (all.x + groups * s) >> (log + 1));       // a share is two steps at least
+      // a share is two steps at least, but no group waits for another while a team is free
+      const int few = max(groups, (all.x + groups * s) >> (log + 1));
       int n = min(most, few);
       float fill = 0.9f;
       if (n >= groups) {

@@ -51,7 +51,8 @@ struct PfSmem {
   static constexpr int kQBox = kPfQ * 128;
   static constexpr int kQ = kBoxes * kQBox;            // one tile's queries
   static constexpr int kRing = 2 * kQ;
-  static constexpr int kBars = kRing + 2 * kPfStages * kStage;
+  static constexpr int kFac = kRing + 2 * kPfStages * kStage;
+  static constexpr int kBars = kFac + 2 * kPfQ * 4;
   static constexpr int kTotal = kBars + 256 + 1024 /*align*/;
 };
 
@@ -145,6 +146,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   extern __shared__ uint8_t dsm_raw[];
   const uint32_t raw = smem_u32(dsm_raw);
   uint8_t* sm = dsm_raw + (((raw + 1023u) & ~1023u) - raw);
+  float* fac = reinterpret_cast<float*>(sm + SM::kFac);
   uint64_t* full = reinterpret_cast<uint64_t*>(sm + SM::kBars);   // [K stages, V stages]
   uint64_t* empty = full + 2 * kPfStages;
   uint64_t* q_ready = empty + 2 * kPfStages;   // the queries are in shared memory
@@ -382,43 +384,48 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     const int r0 = i0 + t * RT;
     const int nrows = max(0, min(RT, sq.n - r0));
     const int my = t ? nch1 : nch0;
-    // thread = TMEM lane = vector.  Its query, scaled by a power of two to [2^14, 2^15):
-    // a whole row each, which the swizzle spreads over all banks
+    // thread = TMEM lane = vector
     const int v = wq * 32 + lane, vi = v / G, hq = h * G + v - vi * G;
     const bool live = vi < nrows;
-    float f;
+    // The warp's queries, each scaled by a power of two to [2^14, 2^15): a row's 16-byte
+    // pieces on neighbouring lanes, all rows in flight at once
+    constexpr int kPieces = HD / 8, kRowsAtOnce = 32 / kPieces, kReads = 32 / kRowsAtOnce;
+    const int piece = lane % kPieces, sub = lane / kPieces;
     {
-      uint4 x[HD / 8];
+      uint4 x[kReads];
 #pragma unroll
-      for (int i = 0; i < HD / 8; ++i) x[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (live) {
-        const uint4* p = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) +
-                                                        static_cast<long long>(sq.row0 + r0 + vi) * a.ld_q + hq * HD);
-#pragma unroll
-        for (int i = 0; i < HD / 8; ++i) x[i] = __ldg(p + i);
+      for (int i = 0; i < kReads; ++i) {
+        const int vv = wq * 32 + i * kRowsAtOnce + sub, ii = vv / G;
+        x[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (ii < nrows)
+          x[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) +
+                                                      static_cast<long long>(sq.row0 + r0 + ii) * a.ld_q +
+                                                      (h * G + vv - ii * G) * HD) + piece);
       }
-      float top = 0.f;
+      uint8_t* qs = sm + t * SM::kQ + (piece / 8) * SM::kQBox;
 #pragma unroll
-      for (int i = 0; i < HD / 8; ++i) {
-        top = max3(top, fabsf(bf16_lo(x[i].x)), fabsf(bf16_hi(x[i].x)));
-        top = max3(top, fabsf(bf16_lo(x[i].y)), fabsf(bf16_hi(x[i].y)));
-        top = max3(top, fabsf(bf16_lo(x[i].z)), fabsf(bf16_hi(x[i].z)));
-        top = max3(top, fabsf(bf16_lo(x[i].w)), fabsf(bf16_hi(x[i].w)));
+      for (int i = 0; i < kReads; ++i) {
+        const int vv = wq * 32 + i * kRowsAtOnce + sub;
+        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+        float top = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = max3(top, fabsf(bf16_lo(w[e])), fabsf(bf16_hi(w[e])));
+#pragma unroll
+        for (int o = kPieces / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const int ex = max(static_cast<int>(__float_as_uint(top) >> 23), 15);
+        const float up = __uint_as_float(static_cast<uint32_t>(268 - ex) << 23);
+        if (piece == 0) fac[t * kPfQ + vv] = __uint_as_float(static_cast<uint32_t>(ex - 14) << 23);
+        uint32_t y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = pack_h2(bf16_lo(w[e]) * up, bf16_hi(w[e]) * up);
+        *reinterpret_cast<uint4*>(qs + sw128_offset(vv, (piece % 8) * 8)) = make_uint4(y[0], y[1], y[2], y[3]);
       }
-      const int ex = max(static_cast<int>(__float_as_uint(top) >> 23), 15);
-      const float up = __uint_as_float(static_cast<uint32_t>(268 - ex) << 23);
-      const float down = __uint_as_float(static_cast<uint32_t>(ex - 14) << 23);
-      f = fmaxf(a.softcap > 0.f ? down * (a.scale / a.softcap) : down * (a.scale * kPfLog2e), 1.2e-38f);
-      uint8_t* qs = sm + t * SM::kQ;
-#pragma unroll
-      for (int i = 0; i < HD / 8; ++i)
-        *reinterpret_cast<uint4*>(qs + (i / 8) * SM::kQBox + sw128_offset(v, (i % 8) * 8)) =
-            make_uint4(pack_h2(bf16_lo(x[i].x) * up, bf16_hi(x[i].x) * up), pack_h2(bf16_lo(x[i].y) * up, bf16_hi(x[i].y) * up),
-                       pack_h2(bf16_lo(x[i].z) * up, bf16_hi(x[i].z) * up), pack_h2(bf16_lo(x[i].w) * up, bf16_hi(x[i].w) * up));
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(q_ready);
     }
+    const float down = fac[t * kPfQ + v];
+    const float f = fmaxf(a.softcap > 0.f ? down * (a.scale / a.softcap) : down * (a.scale * kPfLog2e), 1.2e-38f);
     const int pos = sq.len + r0 + vi;
     const float slope = a.slopes && live ? __ldg(a.slopes + hq) * kPfLog2e : 0.f;
     const uint32_t lanes = static_cast<uint32_t>(wq * 32) << 16;
@@ -550,16 +557,11 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     const bool done = ok && my > 0 && mbar_wait(&pv_done[t], (my - 1) & 1, c.status);
     if (done) tc_fence_after();
     const float inv = l > 0.f ? 1.f / l : (l == l ? 0.f : l);
-    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.o) + static_cast<long long>(sq.row0 + r0 + vi) * a.ld_o + hq * HD;
-    auto store16 = [&](int d, const float (&o)[16], float k) {
-      uint32_t w[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = pack_bf16x2(o[2 * e] * k, o[2 * e + 1] * k);
-      reinterpret_cast<uint4*>(out + d)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-      reinterpret_cast<uint4*>(out + d)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-    };
     // (a vector whose weights were all 0 has an accumulator of zeros; a tile without chunks none at all)
     const int vp = t * kPfQ + v;
+    // whole: the rows go through the tile's queries' place (every score is computed), so that
+    // a row's pieces leave on neighbouring lanes
+    uint8_t* os = sm + t * SM::kQ;
 #pragma unroll 1
     for (int d = 0; d < HD; d += 16) {
       float o[16];
@@ -568,14 +570,29 @@ __global__ void __launch_bounds__(kPfThreads, 1)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[e] = 0.f;
       }
-      if (!live) continue;
       if (splits == 1) {
-        store16(d, o, inv);
-      } else {
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = pack_bf16x2(o[2 * e] * inv, o[2 * e + 1] * inv);
+        uint8_t* at = os + (d / 64) * SM::kQBox;
+        *reinterpret_cast<uint4*>(at + sw128_offset(v, d % 64)) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4*>(at + sw128_offset(v, d % 64 + 8)) = make_uint4(w[4], w[5], w[6], w[7]);
+      } else if (live) {
 #pragma unroll
         for (int e = 0; e < 16; e += 4)
           __stcg(reinterpret_cast<float4*>(part + static_cast<size_t>((d + e) / 4) * (2 * kPfQ * 4) + vp * 4),
                  make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]));
+      }
+    }
+    if (splits == 1) {
+      __syncwarp();
+#pragma unroll 4
+      for (int i = 0; i < kReads; ++i) {
+        const int vv = wq * 32 + i * kRowsAtOnce + sub, ii = vv / G;
+        if (ii < nrows)
+          *(reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.o) + static_cast<long long>(sq.row0 + r0 + ii) * a.ld_o +
+                                     (h * G + vv - ii * G) * HD) + piece) =
+              *reinterpret_cast<const uint4*>(os + (piece / 8) * SM::kQBox + sw128_offset(vv, (piece % 8) * 8));
       }
     }
     if (splits > 1) {
