@@ -160,6 +160,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   const PagedArgs& c = a.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int G = a.G, RT = rows_per_tile;
+  auto row_of = [&](int v) { return G == 1 ? v : static_cast<int>(__umulhi(static_cast<uint32_t>(v), a.inv_g)); };   // v / G
 
   griddep_wait();
   griddep_launch();
@@ -385,7 +386,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
     const int nrows = max(0, min(RT, sq.n - r0));
     const int my = t ? nch1 : nch0;
     // thread = TMEM lane = vector
-    const int v = wq * 32 + lane, vi = v / G, hq = h * G + v - vi * G;
+    const int v = wq * 32 + lane, vi = row_of(v), hq = h * G + v - vi * G;
     const bool live = vi < nrows;
     // The warp's queries, each scaled by a power of two to [2^14, 2^15): a row's 16-byte
     // pieces on neighbouring lanes, all rows in flight at once
@@ -395,7 +396,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       uint4 x[kReads];
 #pragma unroll
       for (int i = 0; i < kReads; ++i) {
-        const int vv = wq * 32 + i * kRowsAtOnce + sub, ii = vv / G;
+        const int vv = wq * 32 + i * kRowsAtOnce + sub, ii = row_of(vv);
         x[i] = make_uint4(0u, 0u, 0u, 0u);
         if (ii < nrows)
           x[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) +
@@ -588,7 +589,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       __syncwarp();
 #pragma unroll 4
       for (int i = 0; i < kReads; ++i) {
-        const int vv = wq * 32 + i * kRowsAtOnce + sub, ii = vv / G;
+        const int vv = wq * 32 + i * kRowsAtOnce + sub, ii = row_of(vv);
         if (ii < nrows)
           *(reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.o) + static_cast<long long>(sq.row0 + r0 + ii) * a.ld_o +
                                      (h * G + vv - ii * G) * HD) + piece) =
@@ -673,7 +674,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
 #pragma unroll
       for (int u = 0; u < kItems; ++u) {
         if (e0 + u * kPfThreads >= total) continue;
-        const int t = vp[u] / kPfQ, v = vp[u] % kPfQ, row = i0 + t * RT + v / G, hq = h * G + v % G;
+        const int t = vp[u] / kPfQ, v = vp[u] % kPfQ, r = row_of(v), row = i0 + t * RT + r, hq = h * G + v - r * G;
         const float k = L[u] > 0.f ? 1.f / L[u] : (L[u] == L[u] ? 0.f : L[u]);
         *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + static_cast<long long>(sq.row0 + row) * a.ld_o +
                                   hq * HD + 4 * quad[u]) =
