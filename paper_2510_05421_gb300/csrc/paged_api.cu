@@ -23,7 +23,7 @@ int current_sms() {
 
 // Query vectors (rows x query heads of a KV head) up to which a sequence's rows
 // are few.
-constexpr int kFewVectors = 64;
+constexpr int kFewVectors = 32;
 
 bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool ld_ok(int64_t ld, int64_t least, int esz) { return ld >= least && (ld * esz) % 16 == 0; }

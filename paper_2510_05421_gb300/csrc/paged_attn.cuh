@@ -822,6 +822,7 @@ cudaError_t pa_tiles(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
     return vecs <= 8 ? launch_pa<E4M3, HD, 1, true>(a, n_sms, s) : launch_pa<E4M3, HD, 2, true>(a, n_sms, s);
   if (vecs <= 8) return launch_pa<E4M3, HD, 1, false>(a, n_sms, s);
   if (vecs <= 16) return launch_pa<E4M3, HD, 2, false>(a, n_sms, s);
+  if (vecs <= 24) return launch_pa<E4M3, HD, 3, false>(a, n_sms, s);
   return launch_pa<E4M3, HD, 4, false>(a, n_sms, s);
 }
 }  // namespace
