@@ -220,7 +220,9 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     const PagedSeq sq = c.n_seqs <= kFew ? few_s[b] : paged_seq(c, b);
     int first, tiles;
     const int n_blocks = extent(sq.len, sq.n, first, tiles), unit0 = before[b].x + before[b].y * over;
-    const int grp = (u - unit0) / (n_blocks + over);
+    int grp = static_cast<int>(__fdividef(static_cast<float>(u - unit0), static_cast<float>(n_blocks + over)));
+    grp += (grp + 1) * (n_blocks + over) <= u - unit0 ? 1 : 0;   // (u - unit0) / (n_blocks + over), exactly
+    grp -= grp * (n_blocks + over) > u - unit0 ? 1 : 0;
     r.g_begin = unit0 + grp * (n_blocks + over) + over;
     r.g_end = r.g_begin + n_blocks;
     const int blk0 = max(u - r.g_begin, 0), blk1 = min(u_end, r.g_end) - r.g_begin;
@@ -231,7 +233,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     r.n_vec = min(NV, sq.n * G - n0);
     r.row_lo = tile == 0 ? 0 : n0 / G;
     r.rest = n0 - r.row_lo * G;
-    r.row_hi = r.row_lo + (r.rest + r.n_vec - 1) / G;
+    r.row_hi = r.row_lo + (G == 1 ? r.n_vec - 1 : static_cast<int>(__umulhi(static_cast<uint32_t>(r.rest + r.n_vec - 1), a.inv_g)));
     // positions that some row of the tile sees
     const int cap = c.max_pages << c.log_p;
     const int see_end = min(sq.len + r.row_hi + 1, cap);
@@ -299,26 +301,34 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
   // blocks) and the shares fill the GPU nearly as well as smaller teams' would.
   if (warp == 0) {
     const int groups = all.y;
-    int S = kPaTeam, n_teams = 0;
-    const float per = __fdividef(1.f, static_cast<float>(max(groups, 1)));
-    float best = -1.f;
-#pragma unroll 1
-    for (int s = W; s >= kPaTeam; s >>= 1) {
-      const int log = 31 - __clz(s), most = static_cast<int>(gridDim.x) * (W >> log);
-      if (s > kPaTeam && all.x < (groups > most ? 32 : 2) * s * groups) continue;
-      // a share is two steps at least, but no group waits for another while a team is free
-      const int few = max(groups, (all.x + groups * s) >> (log + 1));
-      int n = min(most, few);
-      float fill = 0.9f;
-      if (n >= groups) {
-        int k = static_cast<int>(static_cast<float>(n) * per);         // n / groups, to within one
-        k += (k + 1) * groups <= n ? 1 : 0;
-        k -= k * groups > n ? 1 : 0;
-        n = k * groups;
-        fill = __fdividef(static_cast<float>(n), static_cast<float>(most));
+    // lane e weighs teams of W >> e warps
+    int n_teams = 0;
+    float fill = -1.f;
+    {
+      const int log = 31 - __clz(W) - min(lane, 2), s = 1 << log, most = static_cast<int>(gridDim.x) * (W >> log);
+      if (s == kPaTeam || all.x >= (groups > most ? 32 : 2) * s * groups) {
+        // a share is two steps at least, but no group waits for another while a team is free
+        const int few = max(groups, (all.x + groups * s) >> (log + 1));
+        n_teams = min(most, few);
+        fill = 0.9f;
+        if (n_teams >= groups) {
+          int k = static_cast<int>(__fdividef(static_cast<float>(n_teams), static_cast<float>(max(groups, 1))));
+          k += (k + 1) * groups <= n_teams ? 1 : 0;                      // n_teams / groups, exactly
+          k -= k * groups > n_teams ? 1 : 0;
+          n_teams = k * groups;
+          fill = __fdividef(static_cast<float>(n_teams), static_cast<float>(most));
+        }
       }
-      if (fill > best + 0.2f) best = fill, S = s, n_teams = n;
     }
+    int pick = 0;
+    float best = __shfl_sync(0xffffffffu, fill, 0);
+#pragma unroll
+    for (int e = 1; (W >> e) >= kPaTeam; ++e) {
+      const float f = __shfl_sync(0xffffffffu, fill, e);
+      if (best < 0.f || f > best + 0.2f) best = f, pick = e;
+    }
+    const int S = W >> pick;
+    n_teams = __shfl_sync(0xffffffffu, n_teams, pick);
     const int total = all.x + groups * S * kPaOver;
     if (lane == 0) {
       plan_s.S = S, plan_s.over = S * kPaOver;
