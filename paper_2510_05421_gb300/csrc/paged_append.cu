@@ -11,9 +11,14 @@
 // value can reach another row through a probability of 0.
 //
 // A team of 32 to 256 threads owns one page of one head of K or of V: its
-// rows are loaded and rotated once, 16 elements a thread (8 and their 8
-// rotation partners), and wait in registers for the page's maximum.  Bound:
-// bytes (the rows in, half or a quarter of them out); single tokens: latency.
+// rows are loaded and rotated once, 16 elements a thread and item (8 and their
+// 8 rotation partners), and wait in registers for the page's maximum; its page
+// entry is looked up meanwhile.  Two items a thread keep a thread within 64
+// registers, so four blocks of 256 an SM hide each other's chain of loads
+// (lengths, rows and entry, scale); only pages of 128 rows of hd 128 take four.
+// Bound: bytes (the rows in, half or a quarter of them out).  8192 rows of 32 K,
+// V and query heads each, e4m3 pages of 16: 72.6 us, 4.6 TB/s (83.4 with four
+// items and two blocks); 64 sequences' single tokens 5.6 us, one 2.8 us: latency.
 #include <algorithm>
 
 #include "paged.cuh"
@@ -23,7 +28,6 @@ namespace dvi {
 namespace {
 
 constexpr int kApThreads = 256;
-constexpr int kApItems = 4;            // 16-element items a thread holds
 
 // The (cos, sin) pairs of 8 dims.
 struct Turn {
@@ -68,7 +72,7 @@ __device__ __forceinline__ float team_max(float v, float* red, int team, int t) 
   return v;
 }
 
-template <bool E4M3, int D, typename T, int TEAM>
+template <bool E4M3, int D, typename T, int TEAM, int kApItems>
 __device__ void append_page(const PagedAppendArgs& a, int item, int group) {
   __shared__ float red[kApThreads / 32];
   const PagedArgs& c = a.c;
@@ -243,18 +247,18 @@ __device__ void rotate_queries(const PagedAppendArgs& a, int warp_task, int part
   }
 }
 
-template <bool E4M3, int D, typename T, int TEAM>
-__global__ void __launch_bounds__(kApThreads) paged_append_kernel(const __grid_constant__ PagedAppendArgs a,
+template <bool E4M3, int D, typename T, int TEAM, int kApItems>
+__global__ void __launch_bounds__(kApThreads, kApItems == 2 ? 4 : 2) paged_append_kernel(const __grid_constant__ PagedAppendArgs a,
                                                                   int n_items, int groups, int parts, int steps) {
   griddep_wait();
   griddep_launch();
   const int bid = static_cast<int>(blockIdx.x);
   const int pages = n_items * groups;
-  if (bid < pages) append_page<E4M3, D, T, TEAM>(a, bid / groups, bid % groups);
+  if (bid < pages) append_page<E4M3, D, T, TEAM, kApItems>(a, bid / groups, bid % groups);
   else rotate_queries<D, T>(a, (bid - pages) * (kApThreads / 32) + static_cast<int>(threadIdx.x >> 5), parts, steps);
 }
 
-template <bool E4M3, int D, typename T, int TEAM>
+template <bool E4M3, int D, typename T, int TEAM, int kApItems>
 cudaError_t launch_append(const PagedAppendArgs& a, cudaStream_t s) {
   const PagedArgs& c = a.c;
   const long long n_items = static_cast<long long>(c.n_rows >> c.log_p) + 2ll * c.n_seqs;
@@ -266,17 +270,18 @@ cudaError_t launch_append(const PagedAppendArgs& a, cudaStream_t s) {
   const long long q_blocks = (static_cast<long long>(c.n_rows) * parts + kApThreads / 32 - 1) / (kApThreads / 32);
   const long long blocks = n_items * groups + q_blocks;
   if (blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
-  return launch_pdl(paged_append_kernel<E4M3, D, T, TEAM>, dim3(static_cast<unsigned>(blocks)), dim3(kApThreads), 0, s,
+  return launch_pdl(paged_append_kernel<E4M3, D, T, TEAM, kApItems>, dim3(static_cast<unsigned>(blocks)), dim3(kApThreads), 0, s,
                     a, static_cast<int>(n_items), groups, parts, steps);
 }
-// A team holds kApItems items a thread: the rows of one page, as far as one
-// sequence's rows go.
+// A team's items are the rows of one page, as far as one sequence's rows go.
 template <bool E4M3, int D, typename T>
 cudaError_t append_teams(const PagedAppendArgs& a, cudaStream_t s) {
   const int items = std::min(a.c.P, a.c.max_rows) * (D / 16);
-  if (items <= 32 * kApItems) return launch_append<E4M3, D, T, 32>(a, s);
-  if (items <= 128 * kApItems) return launch_append<E4M3, D, T, 128>(a, s);
-  return launch_append<E4M3, D, T, 256>(a, s);
+  if (items <= 64) return launch_append<E4M3, D, T, 32, 2>(a, s);
+  if (items <= 128) return launch_append<E4M3, D, T, 64, 2>(a, s);
+  if (items <= 256) return launch_append<E4M3, D, T, 128, 2>(a, s);
+  if (items <= 512) return launch_append<E4M3, D, T, 256, 2>(a, s);
+  return launch_append<E4M3, D, T, 256, 4>(a, s);
 }
 template <bool E4M3>
 cudaError_t append_types(const PagedAppendArgs& a, cudaStream_t s) {
