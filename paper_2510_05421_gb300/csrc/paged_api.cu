@@ -21,8 +21,12 @@ int current_sms() {
   return n;
 }
 
-// Query vectors (rows x query heads of a KV head) up to which a sequence's rows
-// are few.
+// Query vectors (rows x query heads of a KV head) up to which a bf16 sequence's
+// rows are few.  us by the few-row kernel / the prompt kernel: 24 vectors over
+// 200 positions 13.7 / 11.4 (8 sequences, 8 KV heads of 128), 32 over 500 16.3 /
+// 28.0 (32 sequences, 8 of 64), 28 over 16000 35.2 / 46.7; above the border 40
+// over 20 10.8 / 8.0, 64 over 500 18.9 / 15.7, 40 over 4000 21.1 / 20.7, 64 over
+// 16000 34.1 / 36.6.
 constexpr int kFewVectors = 32;
 
 bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -67,7 +71,10 @@ dvi_status check(const dvi_paged_cache* c, const dvi_paged_batch* b, int dtype, 
   return DVI_OK;
 }
 
-dvi_status launched(cudaError_t e) { return e == cudaSuccess ? DVI_OK : DVI_ERR_CUDA; }
+// The launchers refuse grids and unit counts past 31 bits.
+dvi_status launched(cudaError_t e) {
+  return e == cudaSuccess ? DVI_OK : e == cudaErrorInvalidConfiguration ? DVI_ERR_CAPACITY : DVI_ERR_CUDA;
+}
 
 }  // namespace
 
@@ -125,6 +132,7 @@ extern "C" dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_p
   if (!d_q || !d_o || !on16(d_q) || !on16(d_o) || !ld_ok(ld_q, least, esz) || !ld_ok(ld_o, least, esz))
     return DVI_ERR_INVALID_ARG;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return DVI_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(a.c.n_rows) * (options->n_heads / a.c.H) > 0x7fffffffll) return DVI_ERR_CAPACITY;
   const int sms = current_sms();
   if (sms <= 0) return DVI_ERR_CUDA;
   if (workspace_bytes < dvi_paged_workspace_bytes(a.c.D)) return DVI_ERR_CAPACITY;
@@ -139,7 +147,7 @@ extern "C" dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_p
   a.dtype = dtype;
   a.scale = options->scale;
   a.softcap = options->softcap;
-  a.window = options->window;
+  a.window = options->window < (1 << 30) ? options->window : 0;   // no position is further back
   a.counters = static_cast<int*>(workspace);
   a.pf_counters = a.counters + static_cast<size_t>(sms) * kPagedTeams;
   a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + paged_counter_bytes(sms));
@@ -147,8 +155,7 @@ extern "C" dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_p
   cudaGetLastError();
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const bool e4m3 = cache->format == DVI_KV_E4M3;
-  // bf16 sequences of more than kFewVectors query vectors per KV head go to the
-  // prompt kernel; a ragged batch may hold both kinds, and each launch skips
+  // a ragged batch may hold both kinds, and each launch skips
   // the other's
   const int64_t most = static_cast<int64_t>(a.c.max_rows) * a.G;
   const bool prompts = dtype == DVI_BF16 && a.G <= 128 && most > kFewVectors;
@@ -156,14 +163,14 @@ extern "C" dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_p
   if (prompts) {
     a.min_vectors = kFewVectors + 1;
     a.max_vectors = 0x7fffffff;
-    if (launch_paged_pf(a, e4m3, sms, st) != cudaSuccess) return DVI_ERR_CUDA;
+    const dvi_status r = launched(launch_paged_pf(a, e4m3, sms, st));
+    if (r != DVI_OK) return r;
   }
   if (few) {
     a.min_vectors = 1;
     a.max_vectors = prompts ? kFewVectors : 0x7fffffff;
     a.beside = prompts;
-    const cudaError_t e = e4m3 ? launch_paged_attend<true>(a, sms, st) : launch_paged_attend<false>(a, sms, st);
-    if (e != cudaSuccess) return DVI_ERR_CUDA;
+    return launched(e4m3 ? launch_paged_attend<true>(a, sms, st) : launch_paged_attend<false>(a, sms, st));
   }
   return DVI_OK;
 }

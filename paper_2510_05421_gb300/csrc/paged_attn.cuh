@@ -42,7 +42,7 @@ constexpr int kPaOver = 4;                // steps of a warp that a group costs 
 constexpr float kPaLazy = 8.f;            // growth of a maximum (base 2) that rescales the accumulator
 constexpr float kPaUp = 5.f;              // weights are at most 2^(kPaLazy + kPaUp): f16 keeps small ones exact
 constexpr float kPaMost = 8192.f;         // 2^(kPaLazy + kPaUp)
-constexpr float kPaUnset = -1e30f;        // the reference of a vector that has seen no key
+constexpr float kPaUnset = -3e38f;        // the reference of a vector that has seen no key
 constexpr float kPaLog2e = 1.4426950408889634f;
 
 // A share's part of one group.
@@ -594,9 +594,10 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
       auto weights = [&] {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          const float c0 = lv - m[nt][0], c1 = lv - m[nt][1];
+          // (the score is rounded as it is for the maximum, before the reference goes off:
+          // one multiply-add for both would leave the rounding of a huge score in the exponent)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) p[nt][e] = pa_ex2(fmaf(s[nt][e], f[nt][e & 1], e & 1 ? c1 : c0));
+          for (int e = 0; e < 4; ++e) p[nt][e] = pa_ex2(fmaf(s[nt][e], f[nt][e & 1], lv) - m[nt][e & 1]);
         }
       };
       weights();

@@ -40,7 +40,7 @@ constexpr int kPfSegs = kPfPos / 16;     // a page covers whole segments
 constexpr int kPfStages = 4;             // of K, and of V (even: a chunk's stage tells its score buffer)
 constexpr float kPfLazy = 13.f;          // growth of a maximum that rescales the accumulator
 constexpr float kPfUp = 5.f;             // a new reference sits so far below the maximum
-constexpr float kPfUnset = -1e30f;
+constexpr float kPfUnset = -3e38f;       // the reference of a vector that has seen no key
 constexpr float kPfLog2e = 1.4426950408889634f;
 
 template <int HD>
@@ -189,7 +189,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   const PagedSeq sq = paged_seq(c, b);
   const int i0 = (item - first) * pair;                 // first row of tile 0
   const int vecs = sq.n * G;
-  if (i0 >= sq.n || vecs < a.min_vectors || vecs > a.max_vectors) return;
+  // (i0 < 0: row starts that do not ascend)
+  if (i0 < 0 || i0 >= sq.n || vecs < a.min_vectors || vecs > a.max_vectors) return;
   const int cap = c.max_pages << c.log_p;
   const int held_end = min(sq.len + sq.n, cap);         // rows of the cache past it are nobody's
   // chunks that some row of tile t sees (0: the tile has no row), and those of this CTA
@@ -526,12 +527,13 @@ __global__ void __launch_bounds__(kPfThreads, 1)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           const int g = 2 * q + k;
-          const float fg = CURVED ? 1.f : fk[g], lg = (CURVED ? 0.f : lv[g]) - m;
-          const uint64_t f2 = pack2(fg, fg), l2 = pack2(lg, lg);
+          // (the score is rounded as it is for the maximum, before the reference goes off)
+          const uint64_t f2 = pack2(fk[g], fk[g]), l2 = pack2(lv[g], lv[g]), m2 = pack2(-m, -m);
           uint64_t sum = 0ull;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const float2 x = unpack2(fma2(pack2(s[16 * g + 2 * e], s[16 * g + 2 * e + 1]), f2, l2));
+            const uint64_t z = pack2(s[16 * g + 2 * e], s[16 * g + 2 * e + 1]);
+            const float2 x = unpack2(add2(CURVED ? z : fma2(z, f2, l2), m2));
             const float p0 = ex2(x.x), p1 = ex2(x.y);
             sum = add2(sum, pack2(p0, p1));
             w[8 * k + e] = pack_h2(p0, p1);

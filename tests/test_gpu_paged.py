@@ -271,6 +271,73 @@ def test_attend_out_of_range_device_values_are_flagged():
         assert out.shape == q.shape
 
 
+@pytest.mark.parametrize("start", [[0, 900, 300, 1000], [700, 100, 900, 1000], [0, -50, 1200, 1000], [1000, 0, 0, 0]])
+def test_row_starts_that_do_not_ascend_stay_inside(start):
+    """Prompt-sized calls whose row starts fall: flagged, and no row outside the call is read or written."""
+    cache = make_cache("int8", 60, 2, 64, 64, 13)
+    table, lens = ints(np.arange(60).reshape(3, 20)), ints([0, 64, 100])
+    room = torch.full((1400, 8, 64), 7.0, device="cuda").bfloat16()
+    q = torch.randn(1400, 8, 64, device="cuda").bfloat16()
+    cache.attend(table, lens, q[200:1200], row_start=ints(start), out=room[200:1200])
+    assert "KV_FULL" in cache.status()
+    assert (room[:200] == 7).all() and (room[1200:] == 7).all()
+    kv = torch.randn(1000, 2, 64, device="cuda")
+    cache.append(table, lens, kv, kv, row_start=ints(start))
+    cache.read(table, lens, 1000, row_start=ints(start))
+    assert "KV_FULL" in cache.status()
+
+
+@pytest.mark.parametrize("rows", [2, 50])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attend_huge_scores(rows, dtype):
+    """Scores around -6e33, where f32 holds no difference between them: the result is still a mean of the
+    values that the row sees (weighted somehow), so within their range."""
+    cache = make_cache("int8", 8, 1, 16, 64, 14)
+    cache.k[:] = 100
+    cache.k_scale[:] = 1e15
+    q = torch.full((rows, 2, 64), -1e17, device="cuda").to(TD[dtype])
+    lens = ints([40])
+    out = cache.attend(ints(np.arange(8)[None]), lens, q, scale=0.01).float()
+    _, v = cache.read(ints(np.arange(8)[None]), ints([0]), 40 + rows, dtype=torch.float32)
+    for r in range(rows):
+        lo, hi = v[:41 + r, 0].amin(0), v[:41 + r, 0].amax(0)
+        # rounded by 2^-8 of itself (bf16), and the means by less than 2^-10 of the largest value
+        slack = (lo.abs() + hi.abs()) * (2.0 ** -8 + 2.0 ** -10)
+        assert torch.isfinite(out[r]).all() and (out[r] >= lo - slack).all() and (out[r] <= hi + slack).all()
+
+
+@pytest.mark.parametrize("rows", [3, 40])
+def test_attend_window_past_every_position(rows):
+    """A window of 2^31 - 1 positions is none."""
+    cache = make_cache("e4m3", 8, 2, 32, 64, 15)
+    q = torch.randn(rows, 4, 64, device="cuda").bfloat16()
+    a = cache.attend(ints(np.arange(8)[None]), ints([100]), q)
+    assert torch.equal(a, cache.attend(ints(np.arange(8)[None]), ints([100]), q, window=2 ** 31 - 1))
+
+
+def test_graph_of_a_mixed_batch():
+    """Prompts, blocks and tokens in one captured call (two launches side by side), replayed between writes to
+    its inputs by the surrounding kernels."""
+    cache = make_cache("int8", 40, 2, 64, 128, 16)
+    lens, n = [77, 0, 130], [150, 3, 1]
+    table, start = ints(make_table(lens, n, 64, 40, 3)), ints(np.concatenate([[0], np.cumsum(n)]))
+    q = torch.zeros(154, 4, 128, device="cuda").bfloat16()
+    fresh = [torch.randn(154, 4, 128, device="cuda").bfloat16() for _ in range(8)]
+    want = [cache.attend(table, ints(lens), x, row_start=start, max_rows=150).clone() for x in fresh]
+    ln = ints(lens)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        cache.attend(table, ln, q, row_start=start, max_rows=150)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out = cache.attend(table, ln, q, row_start=start, max_rows=150) * 1
+    for x, w in zip(fresh, want):
+        q.copy_(x)
+        graph.replay()
+        assert torch.equal(out, w)
+
+
 def test_attend_more_rows_than_max_rows_are_flagged():
     cache = make_cache("int8", 8, 2, 16, 64, 12)
     q = torch.randn(8, 4, 64, device="cuda").bfloat16()
