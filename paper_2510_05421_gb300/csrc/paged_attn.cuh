@@ -221,8 +221,8 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     int first, tiles;
     const int n_blocks = extent(sq.len, sq.n, first, tiles), unit0 = before[b].x + before[b].y * over;
     int grp = static_cast<int>(__fdividef(static_cast<float>(u - unit0), static_cast<float>(n_blocks + over)));
-    grp += (grp + 1) * (n_blocks + over) <= u - unit0 ? 1 : 0;   // (u - unit0) / (n_blocks + over), exactly
-    grp -= grp * (n_blocks + over) > u - unit0 ? 1 : 0;
+    while (grp * (n_blocks + over) > u - unit0) --grp;      // (u - unit0) / (n_blocks + over), exactly
+    while ((grp + 1) * (n_blocks + over) <= u - unit0) ++grp;
     r.g_begin = unit0 + grp * (n_blocks + over) + over;
     r.g_end = r.g_begin + n_blocks;
     const int blk0 = max(u - r.g_begin, 0), blk1 = min(u_end, r.g_end) - r.g_begin;

@@ -470,7 +470,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       tmem_ld32_async(tsi + 32, s + 32);
 #pragma unroll
       for (int g = 0; g < kPfSegs; ++g) {
-        fk[g] = f * __shfl_sync(0xffffffffu, ks_l, g);
+        fk[g] = fmaxf(f * __shfl_sync(0xffffffffu, ks_l, g), 1.2e-38f);   // not 0: a masked score stays -inf
         lv[g] = __shfl_sync(0xffffffffu, lv_l, g);
       }
       tmem_ld_wait64(s);

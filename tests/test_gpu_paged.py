@@ -306,6 +306,18 @@ def test_attend_huge_scores(rows, dtype):
         assert torch.isfinite(out[r]).all() and (out[r] >= lo - slack).all() and (out[r] <= hi + slack).all()
 
 
+@pytest.mark.parametrize("rows", [1, 5, 40, 150])
+@pytest.mark.parametrize("opt", [dict(), dict(window=20), dict(softcap=10.0)])
+def test_attend_zero_queries_and_keys(rows, opt):
+    """Padding: queries of zeros over pages whose keys are zeros (a scale of 2^-80): a score's factor is below
+    what f32 holds, and positions behind a row stay out of it all the same."""
+    cache = make_cache("int8", 16, 2, 16, 64, 18)
+    cache.k[:8] = 0
+    cache.k_scale[:8] = 2.0 ** -80
+    q = torch.zeros(rows, 4, 64, device="cuda").bfloat16()
+    check_attend(cache, np.arange(16)[None], [33], [rows], 4, "bf16", q=q, **opt)
+
+
 @pytest.mark.parametrize("rows", [3, 40])
 def test_attend_window_past_every_position(rows):
     """A window of 2^31 - 1 positions is none."""
