@@ -120,6 +120,21 @@ def test_attend_prompt_chunks(fmt, D, group, rows):
     check_attend(cache, table, lens, n, 2 * group, "bf16", seed=rows)
 
 
+@pytest.mark.parametrize("B,H,ctx,rows,page,opt", [(40, 48, 0, 40, 16, dict()), (3, 40, 500, 300, 64, dict()),
+                                                   (1, 39, 1500, 130, 128, dict()), (5, 32, 40, 270, 32, dict(window=150)),
+                                                   (1, 1, 3000, 200, 64, dict()), (2, 77, 900, 131, 64, dict(softcap=8.0))])
+def test_attend_prompts_are_shared(B, H, ctx, rows, page, opt):
+    """Prompt chunks in more and fewer units than SMs, of even and uneven lengths, cut by shares and by splits;
+    twice, as what the first call leaves in the workspace is the second's to find."""
+    lens = [ctx + 37 * (b % 5) for b in range(B)]
+    n = [max(rows - 29 * (b % 3), 5) for b in range(B)]
+    pages = sum(-(-(a + r) // page) for a, r in zip(lens, n))
+    cache = make_cache("int8", pages, H, page, 64, B)
+    table = make_table(lens, n, page, pages, 5)
+    for seed in (1, 2):
+        check_attend(cache, table, lens, n, H, "bf16", seed=seed, **opt)
+
+
 @pytest.mark.parametrize("rows", [1, 6, 40, 140])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("opt", [dict(softcap=20.0), dict(window=1), dict(window=33), dict(window=100, softcap=5.0),
