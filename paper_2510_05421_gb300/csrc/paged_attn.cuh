@@ -267,14 +267,15 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
       n = blocks * ng;
       if (c.n_seqs <= kFew) few_s[b] = sq;
     }
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
+#pragma unroll 1
+    for (int o = 1; o < min(c.n_seqs, 32); o <<= 1) {
       const int x = __shfl_up_sync(0xffffffffu, n, o), y = __shfl_up_sync(0xffffffffu, ng, o);
       if (lane >= o) n += x, ng += y;
     }
     if (c.n_seqs <= kFew) {
       if (b < c.n_seqs) before[b + 1] = make_int2(n, ng);
-      all = make_int2(__shfl_sync(0xffffffffu, n, 31), __shfl_sync(0xffffffffu, ng, 31));
+      const int last = c.n_seqs - 1;
+      all = make_int2(__shfl_sync(0xffffffffu, n, last), __shfl_sync(0xffffffffu, ng, last));
     } else {
       if (b0 > 0) __syncthreads();
       if (lane == 31) scan_s[warp] = make_int2(n, ng);
@@ -447,7 +448,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
       if (j < n_mine) copy(j, j);
       cp_commit();
     }
-    if (tw == 0 && lane == 0) piece_s[in_cta][turn ^ 1] = find(pc.g_end, share(team + 1));
+    if (tw == S - 1 && lane == 0) piece_s[in_cta][turn ^ 1] = find(pc.g_end, share(team + 1));
 
     // ---------------- query fragments: thread (g, t) of vector 8 nt + g holds, for
     // step j, dims 16 t + 4 j .. + 3 (hd 128: from step 4 on 64 + 16 t + 4 (j - 4))
@@ -702,42 +703,43 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
       }
     team_bar();
     const bool whole = pc.whole;
-    // a part in the workspace: [NV][HD / 32][8] quads of dims, maxima [NV], sums [NV]
+    // a part in the workspace: [NV][HD / 4] quads as they lie here, maxima [NV], sums [NV]
     constexpr int kSlot = NV * (HD + 2);
-    constexpr int kQuads = NV * HD / 4;
+    const int quads = n_vec * (HD / 4);
     float* slot = a.part + static_cast<size_t>(2 * team + (pc.cut ? 0 : 1)) * kSlot;
-    auto emit = [&](int i, float4 acc, float L) {                  // quad i: dims d .. d + 3 of vector v
-      const int v = i / (HD / 4), d = (i % 8) * (HD / 8) + i % (HD / 4) / 8 * 4;
-      if (v >= n_vec) return;
+    auto emit = [&](int i, float4 acc, float L) {                  // quad i: dims d, d + 1 and d + HD / 8, d + HD / 8 + 1
+      const int v = i / (HD / 4), d = (i % 4) * (HD / 4) + i % (HD / 4) / 4 * 2;
       const float inv = L > 0.f ? __fdividef(1.f, L) : (L == L ? 0.f : L);
       int hq;
       const int row = row_of(v, hq);
       const long long off = static_cast<long long>(pc.row0 + row) * a.ld_o + hq * HD + d;
-      if (PAIR)
-        *reinterpret_cast<float4*>(static_cast<float*>(a.o) + off) =
-            make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-      else
-        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.o) + off) =
-            make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+      if (PAIR) {
+        float* at = static_cast<float*>(a.o) + off;
+        *reinterpret_cast<float2*>(at) = make_float2(acc.x * inv, acc.y * inv);
+        *reinterpret_cast<float2*>(at + HD / 8) = make_float2(acc.z * inv, acc.w * inv);
+      } else {
+        __nv_bfloat16* at = static_cast<__nv_bfloat16*>(a.o) + off;
+        *reinterpret_cast<uint32_t*>(at) = pack_bf16x2(acc.x * inv, acc.y * inv);
+        *reinterpret_cast<uint32_t*>(at + HD / 8) = pack_bf16x2(acc.z * inv, acc.w * inv);
+      }
     };
     constexpr int kWarpFloats = ST * SH::kStage / 4;
     const float* parts = reinterpret_cast<const float*>(sm) + in_cta * S * kWarpFloats;
 #pragma unroll 1
-    for (int i = tw * 32 + lane; i < kQuads; i += S * 32) {
+    for (int i = tw * 32 + lane; i < quads; i += S * 32) {
       const int v = i / (HD / 4);
       const float* head = parts + NV * kPart + v;
-      const float* quad = parts + v * kPart + i % (HD / 4) / 8 * 32 + (i % 8) * 2;
+      const float* quad = parts + v * kPart + i % (HD / 4) * 4;
       float M = kPaUnset, L = 0.f;
-#pragma unroll 4
+#pragma unroll 8
       for (int w = 0; w < S; ++w) M = fmaxf(M, head[w * kWarpFloats]);
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+#pragma unroll 8
       for (int w = 0; w < S; ++w) {
         const float f = pa_ex2(head[w * kWarpFloats] - M);
-        const float2 x = *reinterpret_cast<const float2*>(quad + w * kWarpFloats);
-        const float2 y = *reinterpret_cast<const float2*>(quad + w * kWarpFloats + 16);
+        const float4 x = *reinterpret_cast<const float4*>(quad + w * kWarpFloats);
         acc.x = fmaf(x.x, f, acc.x), acc.y = fmaf(x.y, f, acc.y);
-        acc.z = fmaf(y.x, f, acc.z), acc.w = fmaf(y.y, f, acc.w);
+        acc.z = fmaf(x.z, f, acc.z), acc.w = fmaf(x.w, f, acc.w);
         L = fmaf(head[w * kWarpFloats + NV], f, L);
       }
       if (whole) {
@@ -767,7 +769,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
         const float* p1 = a.part + static_cast<size_t>(2 * t0) * kSlot;
         const int n = t1 - t0 + 1;
 #pragma unroll 1
-        for (int i = tw * 32 + lane; i < kQuads; i += S * 32) {
+        for (int i = tw * 32 + lane; i < quads; i += S * 32) {
           const int v = i / (HD / 4);
           float M = kPaUnset, L = 0.f;
           float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
