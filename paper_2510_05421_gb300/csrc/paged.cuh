@@ -75,6 +75,14 @@ inline size_t paged_pf_part_floats(int head_dim, int n_sms) {
   return static_cast<size_t>(n_sms) * 256 * (head_dim + 2);
 }
 
+// Counts one more part of a group in the workspace: how many came before.  What the
+// block wrote before its barrier is released by it, and the others' parts acquired.
+__device__ __forceinline__ int paged_arrive(int* counter) {
+  int n;
+  asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(n) : "l"(counter) : "memory");
+  return n;
+}
+
 // ---------------------------------------------------------------- rows of a sequence
 struct PagedSeq {
   int len;      // positions before the call's rows

@@ -181,6 +181,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
   __shared__ PaPlan plan_s;
   __shared__ int2 scan_s[W];
   __shared__ int last_s[SH::kTeams];
+  __shared__ int2 teams_s[SH::kTeams];
   const int G = a.G;
 
   if (!a.beside) griddep_wait();
@@ -448,7 +449,11 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
       if (j < n_mine) copy(j, j);
       cp_commit();
     }
-    if (tw == S - 1 && lane == 0) piece_s[in_cta][turn ^ 1] = find(pc.g_end, share(team + 1));
+    if (tw == S - 1 && lane == 0) {
+      // (teams of the group, for the join: this warp has time)
+      if (!pc.whole) teams_s[in_cta] = make_int2(team_of(pc.g_begin), team_of(pc.g_end - 1));
+      piece_s[in_cta][turn ^ 1] = find(pc.g_end, share(team + 1));
+    }
 
     // ---------------- query fragments: thread (g, t) of vector 8 nt + g holds, for
     // step j, dims 16 t + 4 j .. + 3 (hd 128: from step 4 on 64 + 16 t + 4 (j - 4))
@@ -754,14 +759,12 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     }
     if (!whole) {
       // teams of the group: t0 .. t1; whoever of them counts last joins their parts in order
-      const int t0 = team_of(pc.g_begin), t1 = team_of(pc.g_end - 1);
+      const int t0 = teams_s[in_cta].x, t1 = teams_s[in_cta].y;
       team_bar();
       if (tw == 0 && lane == 0) {
-        __threadfence();
-        const int n = atomicAdd(a.counters + t0, 1);
+        const int n = paged_arrive(a.counters + t0);
         last_s[in_cta] = n == t1 - t0;
         if (n == t1 - t0) a.counters[t0] = 0;
-        __threadfence();
       }
       team_bar();
       if (last_s[in_cta]) {

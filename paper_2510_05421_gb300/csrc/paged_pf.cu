@@ -612,11 +612,9 @@ __global__ void __launch_bounds__(kPfThreads, 1)
   if (splits == 1) return;
   // ---------------- the last split to end joins all parts, in order
   if (tid == 0) {
-    __threadfence();
-    const int n = atomicAdd(a.pf_counters + unit, 1);
+    const int n = paged_arrive(a.pf_counters + unit);
     *last_s = n == splits - 1;
     if (n == splits - 1) a.pf_counters[unit] = 0;
-    __threadfence();
   }
   __syncthreads();
   if (!*last_s) return;
