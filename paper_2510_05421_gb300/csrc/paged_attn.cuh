@@ -15,6 +15,14 @@
 // codes of a key; the codes are loaded 16 bytes at a time and go to f16 in
 // registers (1.25 to 1.5 instructions a code).
 //
+// Bound: bytes (the codes, read once) where few SMs' worth of ALU work is enough,
+// the ALU at 16 vectors of int8 (widening is 112 of about 200 of its instructions
+// a block).  Measured: 32 sequences of 12000 to 16384 positions, 12 vectors, 8 KV
+// heads of 128, int8 165 us (932 MB, 5.6 TB/s); 9 rows over 16384, 32 heads of 128,
+// int8 38.4 us (134 MB); 8 sequences up to 2560, 32 heads of 128, one row, e4m3
+// 22.2 us (88 MB).  Beside its length a call costs about 7 us: lengths, plan, table
+// entries, codes, joins, each waiting for the one before.
+//
 // Work: blocks of 16 positions.  The blocks of all (sequence, KV head, tile)
 // groups lie in one row and every team of 4 to 16 warps takes an equal share of
 // it, so ragged batches fill the GPU evenly; a group cut by shares is joined
@@ -71,8 +79,8 @@ struct PaShape {
   static constexpr int kQAt = kRing;
   static constexpr int kVecAt = kQAt + kTeams * kQ;
   static constexpr int kUnitsAt = kVecAt + kTeams * kVec;
-  // a warp's partial result (8 NT rows of HD + 8 floats, a maximum and a sum each) lies in its ring
-  static_assert(NT * 8 * (HD + 10) * 4 <= kStages * kStage, "partial results");
+  // a warp's partial result (8 NT rows of HD + 4 floats, a maximum and a sum each) lies in its ring
+  static_assert(NT * 8 * (HD + 6) * 4 <= kStages * kStage, "partial results");
   static_assert(kTeams <= kPagedTeams, "the workspace");
   static_assert(kUnitsAt + 8 * (kPagedMaxSeqs + 1) + 1536 <= 232448, "shared memory");
 };
@@ -687,8 +695,8 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     __syncwarp();
 
     // ---------------- join.  o[i][nt][e] is dim g HD/8 + 2 i + e / 2 of vector 8 nt + 2 t + e % 2; a warp's
-    // part lies in its ring as rows of [i][g] pairs, 8 floats apart from HD so that no bank meets twice
-    constexpr int kPart = HD + 8;
+    // part lies in its ring as rows of [i][g] pairs, 4 floats apart from HD so that no bank meets twice
+    constexpr int kPart = HD + 4;
     float* mine = reinterpret_cast<float*>(ring);                  // [NV][kPart], maxima [NV], sums [NV]
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -836,6 +844,8 @@ cudaError_t pa_tiles(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
   const long long vecs = std::min<long long>(static_cast<long long>(a.c.max_rows) * a.G, a.max_vectors);
   if (a.dtype == DVI_F32)
     return vecs <= 8 ? launch_pa<E4M3, HD, 1, true>(a, n_sms, s) : launch_pa<E4M3, HD, 2, true>(a, n_sms, s);
+  // (24 vectors of 32 sequences, 4000 positions, 8 KV heads of 128: 71.3 us in a tile of
+  // 24, 78.0 in one of 32)
   if (vecs <= 8) return launch_pa<E4M3, HD, 1, false>(a, n_sms, s);
   if (vecs <= 16) return launch_pa<E4M3, HD, 2, false>(a, n_sms, s);
   if (vecs <= 24) return launch_pa<E4M3, HD, 3, false>(a, n_sms, s);

@@ -20,6 +20,11 @@
 // warps 8-11 widen codes (global -> registers -> SW128 tiles in shared memory,
 // the next tile's codes in flight meanwhile), warp 12 issues the MMAs.
 //
+// Bound: 24 MMAs a chunk take 1290 cycles of the tensor pipe (the scores' are fed from
+// shared memory at its rate) of the 2500 that the weights (1770) and the issuer's waits
+// make of it.  Measured: 1000 rows behind 3001 positions, 32 heads of 128, int8 85.4 us
+// (57.4 GFLOP, 0.67 PFLOP/s).
+//
 // Where the tiles are fewer than the SMs, `splits` CTAs share a pair of tiles
 // along the positions; the last of them to end joins their parts in order.
 //
