@@ -67,7 +67,8 @@ dvi_status check(const dvi_paged_cache* c, const dvi_paged_batch* b, int dtype, 
   a.n_seqs = b->n_seqs;
   a.max_pages = b->max_pages;
   a.n_rows = b->n_rows;
-  a.max_rows = b->max_rows < b->n_rows ? b->max_rows : b->n_rows;
+  // (a bound, and what the launches are chosen by: without row starts the count itself is known)
+  a.max_rows = !b->row_start ? b->n_rows / b->n_seqs : b->max_rows < b->n_rows ? b->max_rows : b->n_rows;
   *out = a;
   return DVI_OK;
 }
@@ -156,12 +157,16 @@ extern "C" dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_p
   cudaGetLastError();
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const bool e4m3 = cache->format == DVI_KV_E4M3;
-  // A ragged batch may hold both kinds, and each launch skips the other's
+  // Row starts lie on the device and max_rows only bounds them, so any of their sequences may
+  // hold few rows.  Of several, each launch skips the other's; a single sequence is the
+  // prompt kernel's whatever it holds (both launches / that one, us: 1000 rows behind 20 to
+  // 16000 positions 4 to 13 more of 28 to 333; 1 row in a buffer of 64, 8 KV heads, 14.6 / 11.8
+  // behind 540 and 20.5 / 24.9 behind 16000, 32 KV heads 46.9 / 85.2).
   const int64_t most = static_cast<int64_t>(a.c.max_rows) * a.G;
   const bool prompts = dtype == DVI_BF16 && a.G <= 128 && most > kFewVectors;
   const bool few = !prompts || (a.c.row_start && a.c.n_seqs > 1);
   if (prompts) {
-    a.min_vectors = kFewVectors + 1;
+    a.min_vectors = few ? kFewVectors + 1 : 1;
     a.max_vectors = 0x7fffffff;
     const dvi_status r = launched(launch_paged_pf(a, e4m3, sms, st));
     if (r != DVI_OK) return r;
