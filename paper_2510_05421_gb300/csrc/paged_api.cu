@@ -87,7 +87,7 @@ extern "C" dvi_status dvi_paged_append(const dvi_paged_cache* cache, const dvi_p
   PagedAppendArgs a{};
   const dvi_status rc = check(cache, batch, dtype, &a.c);
   if (rc != DVI_OK) return rc;
-  if (a.c.n_rows == 0 || a.c.max_rows == 0) return DVI_OK;
+  if (a.c.n_rows == 0) return DVI_OK;
   const int esz = dtype == DVI_F32 ? 4 : 2;
   const int64_t kv = static_cast<int64_t>(a.c.H) * a.c.D;
   if (!d_k || !d_v || !on16(d_k) || !on16(d_v) || !ld_ok(ld_k, kv, esz) || !ld_ok(ld_v, kv, esz))
@@ -129,7 +129,7 @@ extern "C" dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_p
       !(options->scale > 0.f) || !(options->scale < 1e30f) || !(options->softcap >= 0.f) ||
       !(options->softcap < 1e30f) || options->window < 0)
     return DVI_ERR_INVALID_ARG;
-  if (a.c.n_rows == 0 || a.c.max_rows == 0) return DVI_OK;
+  if (a.c.n_rows == 0) return DVI_OK;
   const int64_t least = static_cast<int64_t>(options->n_heads) * a.c.D;
   if (!d_q || !d_o || !on16(d_q) || !on16(d_o) || !ld_ok(ld_q, least, esz) || !ld_ok(ld_o, least, esz))
     return DVI_ERR_INVALID_ARG;
@@ -192,7 +192,7 @@ extern "C" dvi_status dvi_paged_read(const dvi_paged_cache* cache, const dvi_pag
   PagedReadArgs a{};
   const dvi_status rc = check(cache, batch, dtype, &a.c);
   if (rc != DVI_OK) return rc;
-  if (a.c.n_rows == 0 || a.c.max_rows == 0) return DVI_OK;
+  if (a.c.n_rows == 0) return DVI_OK;
   if (!d_k_out || !d_v_out || !on16(d_k_out) || !on16(d_v_out)) return DVI_ERR_INVALID_ARG;
   a.k_out = d_k_out;
   a.v_out = d_v_out;
