@@ -39,6 +39,14 @@ struct PagedReadArgs {
   int dtype;
 };
 
+// c tanh(s / c) of scores in powers of two (x = s log2 e), for caps past kPagedPlainCap.
+struct PagedCap {
+  float inv;                              // 1 / (c log2 e)
+  float two_inv;                          // 2 / c
+  float top;                              // c log2 e
+  float near;                             // |x| below it: by the series
+};
+
 struct PagedAttendArgs {
   PagedArgs c;
   const void* q; void* o;
@@ -46,7 +54,9 @@ struct PagedAttendArgs {
   const float* slopes;                    // [n_heads] or null
   int n_heads, G, dtype;
   uint32_t inv_g;                         // ceil(2^32 / G): n / G = n inv_g >> 32 for small n (G = 1: 0, not used)
-  float scale, softcap;
+  float scale;
+  float softcap;                          // c of f32 rows, and of bf16 rows up to kPagedPlainCap; 0: none
+  PagedCap cap;                           // near > 0: that of bf16 rows under a larger one
   int window;                             // 0: none
   int min_vectors, max_vectors;           // sequences with rows * G in this range are this launch's
   int beside;                             // 1: the launch before is the same call's, on other rows: run beside it
@@ -81,6 +91,21 @@ __device__ __forceinline__ int paged_arrive(int* counter) {
   int n;
   asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(n) : "l"(counter) : "memory");
   return n;
+}
+
+// tanh t = 1 - 2 / (1 + e^(2t)) in f32 is off by up to 2^-20 however small t is, a score capped
+// so by that of the cap.  bf16 rows take it for caps up to kPagedPlainCap: the score is off by
+// 2^-12, half of what a weight's rounding to f16 (2^-11 of it) is.  (f32 rows take tanhf.)
+constexpr float kPagedPlainCap = 256.f;
+// Under larger caps scores below a quarter of the cap go by the series of tanh up to t^7 (off by
+// 3.3e-7 of themselves at t = 1/4) and only those beyond by the form above.  1000 rows behind
+// 3001 positions, 32 heads of 128: 224 us so, 162 by the one form alone.
+__device__ __forceinline__ float paged_cap_fine(float x, const PagedCap& c) {
+  const float t = x * c.inv, u = t * t;
+  float e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * c.two_inv));
+  return fabsf(x) < c.near ? fmaf(x * u, fmaf(u, fmaf(u, -17.f / 315.f, 2.f / 15.f), -1.f / 3.f), x)
+                           : fmaf(-c.top, __fdividef(2.f, 1.f + e), c.top);
 }
 
 // ---------------------------------------------------------------- rows of a sequence

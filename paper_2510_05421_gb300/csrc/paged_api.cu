@@ -148,7 +148,12 @@ extern "C" dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_p
   a.inv_g = a.G == 1 ? 0u : static_cast<uint32_t>(((1ull << 32) + a.G - 1) / a.G);
   a.dtype = dtype;
   a.scale = options->scale;
-  a.softcap = options->softcap;
+  if (dtype == DVI_BF16 && options->softcap > kPagedPlainCap) {
+    const float top = options->softcap * 1.4426950408889634f;
+    a.cap = {1.f / top, 2.f / options->softcap, top, 0.25f * top};
+  } else {
+    a.softcap = options->softcap;
+  }
   a.window = options->window < (1 << 30) ? options->window : 0;   // no position is further back
   a.counters = static_cast<int*>(workspace);
   a.pf_counters = a.counters + static_cast<size_t>(sms) * kPagedTeams;

@@ -169,7 +169,7 @@ __device__ __forceinline__ uint32_t pa_chunk(int r, int ch) {
 
 }  // namespace
 
-template <bool E4M3, int HD, int NT, bool PAIR>
+template <bool E4M3, int HD, int NT, bool PAIR, bool FINE>
 __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     paged_attend_kernel(const __grid_constant__ PagedAttendArgs a) {
   using SH = PaShape<HD, NT, PAIR>;
@@ -495,7 +495,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
         int hq;
         const int row = row_of(n, hq);
         const bool live = n < n_vec;
-        const float f = a.softcap > 0.f ? down * (a.scale / a.softcap) : down * (a.scale * kPaLog2e);
+        const float f = !FINE && a.softcap > 0.f ? down * (a.scale / a.softcap) : down * (a.scale * kPaLog2e);
         fac[n] = f;
         vec[n] = make_float2(live && a.slopes ? __ldg(a.slopes + hq) * kPaLog2e : 0.f,
                              __int_as_float(live ? len + row : -1));
@@ -518,7 +518,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
     // blocks that every row of the tile sees whole: full_begin .. full_end - 1
     const int full_end = min((len + pc.row_lo + 1) / kPaKeys, held_end / kPaKeys);
     const int full_begin = a.window > 0 ? max(0, len + pc.row_hi - a.window + kPaKeys) / kPaKeys : 0;
-    const bool curved = a.softcap > 0.f || a.slopes != nullptr;
+    const bool curved = FINE || a.softcap > 0.f || a.slopes != nullptr;
     float ks_l = 0.f, lv_l = 0.f, iv_l = 0.f;    // ks, log2 vs and 1 / vs (0: no page) of the blocks at work
     int stage = 0;
 #pragma unroll 1
@@ -590,7 +590,9 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             float x = s[nt][e] * f[nt][e & 1];
-            if (a.softcap > 0.f) {
+            if (FINE) {
+              x = paged_cap_fine(x, a.cap);
+            } else if (a.softcap > 0.f) {
               if (PAIR) x = tanhf(x);
               else x = 1.f - __fdividef(2.f, 1.f + pa_ex2(x * (2.f * kPaLog2e)));
               x *= a.softcap * kPaLog2e;
@@ -824,7 +826,7 @@ __global__ void __launch_bounds__(PaShape<HD, NT, PAIR>::kThreads, 1)
 }
 
 namespace {
-template <bool E4M3, int HD, int NT, bool PAIR>
+template <bool E4M3, int HD, int NT, bool PAIR, bool FINE = false>
 cudaError_t launch_pa(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
   using SH = PaShape<HD, NT, PAIR>;
   // the units of all groups are counted in 32 bits
@@ -833,10 +835,10 @@ cudaError_t launch_pa(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
   if (vecs > 0x7fffffffll || tiles * blocks > 0x7fffffffll) return cudaErrorInvalidConfiguration;
   static PerDevice attr;
   attr.once([] {
-    cudaFuncSetAttribute(paged_attend_kernel<E4M3, HD, NT, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    cudaFuncSetAttribute(paged_attend_kernel<E4M3, HD, NT, PAIR, FINE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                          SH::kUnitsAt + 8 * (kPagedMaxSeqs + 1));
   });
-  return launch_pdl(paged_attend_kernel<E4M3, HD, NT, PAIR>, dim3(n_sms), dim3(SH::kThreads),
+  return launch_pdl(paged_attend_kernel<E4M3, HD, NT, PAIR, FINE>, dim3(n_sms), dim3(SH::kThreads),
                     SH::kUnitsAt + 8 * (a.c.n_seqs + 1), s, a);
 }
 template <bool E4M3, int HD>
@@ -844,6 +846,10 @@ cudaError_t pa_tiles(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
   const long long vecs = std::min<long long>(static_cast<long long>(a.c.max_rows) * a.G, a.max_vectors);
   if (a.dtype == DVI_F32)
     return vecs <= 8 ? launch_pa<E4M3, HD, 1, true>(a, n_sms, s) : launch_pa<E4M3, HD, 2, true>(a, n_sms, s);
+  // large caps have kernels of their own, as both caps in one take 1 to 4 % of every call with a usual
+  // cap or a bias (6 rows of 32 sequences behind 16384 positions, a bias: 214 to 221 us), and one tile
+  // for all counts (64 single tokens 44 us, 34 under a usual cap in a tile of 8)
+  if (a.cap.near > 0.f) return launch_pa<E4M3, HD, 2, false, true>(a, n_sms, s);
   // (24 vectors of 32 sequences, 4000 positions, 8 KV heads of 128: 71.3 us in a tile of
   // 24, 78.0 in one of 32)
   if (vecs <= 8) return launch_pa<E4M3, HD, 1, false>(a, n_sms, s);

@@ -47,6 +47,10 @@ constexpr float kPfLazy = 13.f;          // growth of a maximum that rescales th
 constexpr float kPfUp = 5.f;             // a new reference sits so far below the maximum
 constexpr float kPfUnset = -3e38f;       // the reference of a vector that has seen no key
 constexpr float kPfLog2e = 1.4426950408889634f;
+// What becomes of a product beside its scale: nothing; a bias or a cap; a large cap (see
+// kPagedPlainCap; a kernel of its own, as the registers of both caps in one take the chunk of
+// 1000 rows with a bias from 126 to 190 us).
+constexpr int kPfStraight = 0, kPfCurved = 1, kPfFineCap = 2;
 
 template <int HD>
 struct PfSmem {
@@ -144,7 +148,7 @@ __device__ __forceinline__ void widen(const uint4& q, uint4& lo, uint4& hi) {
 
 }  // namespace
 
-template <bool E4M3, int HD, bool CURVED>
+template <bool E4M3, int HD, int CURVE>
 __global__ void __launch_bounds__(kPfThreads, 1)
     paged_pf_kernel(const __grid_constant__ PagedAttendArgs a, int n_items, int rows_per_tile, int splits) {
   using SM = PfSmem<HD>;
@@ -432,7 +436,8 @@ __global__ void __launch_bounds__(kPfThreads, 1)
       if (lane == 0) mbar_arrive(q_ready);
     }
     const float down = fac[t * kPfQ + v];
-    const float f = fmaxf(a.softcap > 0.f ? down * (a.scale / a.softcap) : down * (a.scale * kPfLog2e), 1.2e-38f);
+    const float f = fmaxf(CURVE == kPfCurved && a.softcap > 0.f ? down * (a.scale / a.softcap)
+                                                                : down * (a.scale * kPfLog2e), 1.2e-38f);
     const int pos = sq.len + r0 + vi;
     const float slope = a.slopes && live ? __ldg(a.slopes + hq) * kPfLog2e : 0.f;
     const uint32_t lanes = static_cast<uint32_t>(wq * 32) << 16;
@@ -479,12 +484,14 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         lv[g] = __shfl_sync(0xffffffffu, lv_l, g);
       }
       tmem_ld_wait64(s);
-      if (CURVED) {
+      if (CURVE != kPfStraight) {
         // the finished scores in place of the products
 #pragma unroll
         for (int e = 0; e < kPfPos; ++e) {
           float x = s[e] * fk[e / 16];
-          if (a.softcap > 0.f) x = (1.f - __fdividef(2.f, 1.f + ex2(x * (2.f * kPfLog2e)))) * (a.softcap * kPfLog2e);
+          if (CURVE == kPfFineCap) x = paged_cap_fine(x, a.cap);
+          else if (a.softcap > 0.f)
+            x = (1.f - __fdividef(2.f, 1.f + ex2(x * (2.f * kPfLog2e)))) * (a.softcap * kPfLog2e);
           s[e] = fmaf(slope, static_cast<float>(e - see), x + lv[e / 16]);
         }
       }
@@ -501,7 +508,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
         for (int e = 4; e < 16; e += 4) x = max3(x, z[e], z[e + 1]), y = max3(y, z[e + 2], z[e + 3]);
         x = fmaxf(x, y);
         // a segment's factor is positive: its largest product is its largest score
-        top = fmaxf(top, CURVED ? x : fmaf(x, fk[g], lv[g]));
+        top = fmaxf(top, CURVE != kPfStraight ? x : fmaf(x, fk[g], lv[g]));
       }
       const bool move = top > m + kPfLazy;
       if (__any_sync(0xffffffffu, move)) {
@@ -538,7 +545,7 @@ __global__ void __launch_bounds__(kPfThreads, 1)
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             const uint64_t z = pack2(s[16 * g + 2 * e], s[16 * g + 2 * e + 1]);
-            const float2 x = unpack2(add2(CURVED ? z : fma2(z, f2, l2), m2));
+            const float2 x = unpack2(add2(CURVE != kPfStraight ? z : fma2(z, f2, l2), m2));
             const float p0 = ex2(x.x), p1 = ex2(x.y);
             sum = add2(sum, pack2(p0, p1));
             w[8 * k + e] = pack_h2(p0, p1);
@@ -694,11 +701,11 @@ __global__ void __launch_bounds__(kPfThreads, 1)
 
 namespace {
 
-template <bool E4M3, int HD, bool CURVED>
+template <bool E4M3, int HD, int CURVE>
 cudaError_t launch_pf(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
   static PerDevice attr;
   attr.once([] {
-    cudaFuncSetAttribute(paged_pf_kernel<E4M3, HD, CURVED>, cudaFuncAttributeMaxDynamicSharedMemorySize, PfSmem<HD>::kTotal);
+    cudaFuncSetAttribute(paged_pf_kernel<E4M3, HD, CURVE>, cudaFuncAttributeMaxDynamicSharedMemorySize, PfSmem<HD>::kTotal);
   });
   const PagedArgs& c = a.c;
   const int rt = kPfQ / a.G;
@@ -712,13 +719,15 @@ cudaError_t launch_pf(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
   // splits only fill SMs that the tiles leave idle, eight chunks each at the least
   const int chunks = static_cast<int>(((static_cast<long long>(c.max_pages) << c.log_p) + kPfPos - 1) / kPfPos);
   const int splits = static_cast<int>(std::max(1ll, std::min<long long>({n_sms / units, chunks / 8, 16})));
-  return launch_pdl(paged_pf_kernel<E4M3, HD, CURVED>, dim3(static_cast<unsigned>(units), splits), dim3(kPfThreads),
+  return launch_pdl(paged_pf_kernel<E4M3, HD, CURVE>, dim3(static_cast<unsigned>(units), splits), dim3(kPfThreads),
                     PfSmem<HD>::kTotal, s, a, static_cast<int>(items), rt, splits);
 }
 
 template <bool E4M3, int HD>
 cudaError_t pf_scores(const PagedAttendArgs& a, int n_sms, cudaStream_t s) {
-  return a.softcap > 0.f || a.slopes ? launch_pf<E4M3, HD, true>(a, n_sms, s) : launch_pf<E4M3, HD, false>(a, n_sms, s);
+  if (a.cap.near > 0.f) return launch_pf<E4M3, HD, kPfFineCap>(a, n_sms, s);
+  return a.softcap > 0.f || a.slopes ? launch_pf<E4M3, HD, kPfCurved>(a, n_sms, s)
+                                     : launch_pf<E4M3, HD, kPfStraight>(a, n_sms, s);
 }
 
 }  // namespace

@@ -76,11 +76,13 @@ def attend(kv, table, lens, starts, q, scale, softcap=0.0, window=0, slopes=None
     return o, mass, reach
 
 
-def attend_bound(o, mass, reach, keys, head_dim, dtype):
+def attend_bound(o, mass, reach, keys, head_dim, dtype, largest=0.0):
     """How far an attention result may be from `attend`'s, of rows that see up to `keys` positions: a score is off by
     at most reach (head_dim + 8) 2^-23 (f32 products and sums that may truncate), which moves the result by twice that
     times the mass; a weight's f16 rounding is 2^-11 of it (f32 queries: two f16 numbers, 2^-21), the sums of the
-    weights (keys / 16 + 64) 2^-23 of the mass, and a bf16 result is rounded by 2^-8 of itself."""
+    weights (keys / 16 + 64) 2^-23 of the mass, and a bf16 result is rounded by 2^-8 of itself.  Where the weights of a
+    row spread past f16's range, those far below its largest (at least 2^5 in f16) are off by up to 2^-25: with `largest`,
+    the largest |v|, that counts too."""
     tol = mass * (2 * reach[..., None] * (head_dim + 8) * 2.0 ** -23 + (keys / 16 + 64) * 2.0 ** -23 +
-                  (2.0 ** -11 if dtype == "bf16" else 2.0 ** -21)) + 1e-30
+                  (2.0 ** -11 if dtype == "bf16" else 2.0 ** -21)) + keys * 2.0 ** -30 * largest + 1e-30
     return tol + np.abs(o) * 2.0 ** -8 if dtype == "bf16" else tol
