@@ -83,6 +83,10 @@ class PagedCache:
     Rows of a call lie sequence after sequence: with row_start None every
     sequence has the same number, else sequence b has rows row_start[b] ..
     row_start[b + 1] - 1 (int32 [B + 1]) and max_rows bounds the longest.
+
+    A call runs on the current stream.  With `stream` it runs there, behind
+    what the current one has in flight; wait for that stream before its
+    results are used elsewhere.
     """
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
@@ -135,8 +139,31 @@ class PagedCache:
         """Whether the cache's device is current (the library launches on the current one)."""
         return self._one_device or self._index == torch.cuda.current_device()
 
-    def _stream(self, stream):
-        return _raw_stream(self._index) if stream is None else stream.cuda_stream
+    def _elsewhere(self, call, stream, *args):
+        """`call` where the cache's device is not current, or on a stream of the caller's choice: there it waits for
+        what the current stream has in flight (the inputs may be among it), and no tensor's memory is used again
+        before both streams are done with it."""
+        with torch.cuda.device(self._index):
+            if stream is None:
+                return call(*args)
+            if stream.device != self.device:
+                raise ValueError("stream: not on the cache's device")
+            here = torch.cuda.current_stream(self._index)
+            if here.cuda_stream == stream.cuda_stream:
+                return call(*args)
+            alone = not torch.cuda.is_current_stream_capturing()
+            with torch.cuda.stream(stream):
+                # (a capture cannot wait for work outside it)
+                if not (alone and torch.cuda.is_current_stream_capturing()):
+                    stream.wait_stream(here)
+                got = call(*args)
+            for t in (self.k, self.v, self.k_scale, self.v_scale, self.status_word, *args):
+                if isinstance(t, torch.Tensor):
+                    t.record_stream(stream)
+            for t in got if isinstance(got, tuple) else (got,):
+                if t is not None:
+                    t.record_stream(here)
+            return got
 
     def _new(self, shape, dtype):
         """An output (the cache's device is current)."""
@@ -153,13 +180,12 @@ class PagedCache:
         """Write rows k, v [n, H_kv, head_dim] (bf16 or f32) behind lens, the keys rotated by `rotary`
         ([n_pos, rot_dim / 2, 2], see rotary_table) at their positions.  Returns q [n, H_q, head_dim]
         rotated alike (into q_out, which may be q), or None without q."""
-        if not self._on_device():
-            with torch.cuda.device(self._index):
-                return self.append(table, lens, k, v, q, rotary, row_start, max_rows, q_out, stream)
+        if stream is not None or not self._on_device():
+            return self._elsewhere(self.append, stream, table, lens, k, v, q, rotary, row_start, max_rows, q_out)
         if q is not None and q_out is None:
             q_out = self._new(q.shape, q.dtype)
         rc = self._calls.append(*self._at, table, lens, k, v, q, rotary, row_start, max_rows, q_out,
-                                self._stream(stream))
+                                _raw_stream(self._index))
         if rc:
             self._check("append", rc)
         return q_out
@@ -171,12 +197,12 @@ class PagedCache:
         """Attention of rows q [n, H_q, head_dim] (bf16 or f32), appended before at the same lens: the row at
         position p sees the held positions up to p (the last `window` of them).  scale: head_dim^-0.5 unless
         given; softcap c > 0: scores become c tanh(score / c); slopes f32 [H_q]: + slope (p_key - p)."""
-        if not self._on_device():
-            with torch.cuda.device(self._index):
-                return self.attend(table, lens, q, scale, softcap, window, slopes, row_start, max_rows, out, stream)
+        if stream is not None or not self._on_device():
+            return self._elsewhere(self.attend, stream, table, lens, q, scale, softcap, window, slopes, row_start,
+                                   max_rows, out)
         if out is None:
             out = self._new(q.shape, q.dtype)
-        s = self._stream(stream)
+        s = _raw_stream(self._index)
         ws = self._workspaces.get(s) or self._workspace(s)
         rc = self._calls.attend(*self._at, table, lens, q, out, self._scale if scale is None else scale, softcap, window,
                                 slopes, row_start, max_rows, ws[1], ws[2], s)
@@ -189,15 +215,14 @@ class PagedCache:
              stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """Values of n_rows cached rows, positions lens[b], lens[b] + 1, ... of each sequence:
         (k, v) [n_rows, H_kv, head_dim] in dtype; zeros where no page is held."""
-        if not self._on_device():
-            with torch.cuda.device(self._index):
-                return self.read(table, lens, n_rows, row_start, max_rows, dtype, stream)
+        if stream is not None or not self._on_device():
+            return self._elsewhere(self.read, stream, table, lens, n_rows, row_start, max_rows, dtype)
         if dtype not in _TYPES or n_rows < 0:
             raise ValueError("read: dtype must be bfloat16 or float32, and n_rows at least 0")
         shape = (n_rows, self.n_kv_heads, self.head_dim)
         k = self._new(shape, dtype)
         v = self._new(shape, dtype)
-        rc = self._calls.read(*self._at, table, lens, k, v, row_start, max_rows, self._stream(stream))
+        rc = self._calls.read(*self._at, table, lens, k, v, row_start, max_rows, _raw_stream(self._index))
         if rc:
             self._check("read", rc)
         return k, v
