@@ -228,10 +228,14 @@ class PagedCache:
         return k, v
 
     def status(self) -> list:
-        """Names of the DVI_DEV_* flags set since the last look (waits for the device), then cleared."""
+        """Names of the DVI_DEV_* flags set since the last look (waits for the device: calls on any of its streams),
+        then cleared."""
+        torch.cuda.synchronize(self._index)
         word = int(self.status_word.item())
         if word:
-            self.status_word.zero_()
+            # only what is reported, and before any later call's flags
+            self.status_word.bitwise_and_(~word)
+            torch.cuda.synchronize(self._index)
         return [name for bit, name in DEV_BITS.items() if word & bit]
 
     def _workspace(self, stream: int):

@@ -152,3 +152,21 @@ def test_a_stream_of_another_device_is_refused():
     for name, call in calls(cache, table, lens, q, kv, other):
         with pytest.raises(ValueError):
             call()
+
+
+def test_status_waits_for_every_stream():
+    """Flags of a call still in flight on another stream are reported by the look, and only by that one."""
+    cache, table, lens, _, kv = setup()
+    bad = kv.clone()
+    bad[5, 1, 3] = float("nan")
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(LONG)
+            cache.append(table, lens, bad, kv)
+        assert cache.status() == ["NONFINITE"]
+        assert cache.status() == []
+        with torch.cuda.stream(side):
+            cache.append(table, lens, bad, kv)
+        assert cache.status() == ["NONFINITE"]
