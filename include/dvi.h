@@ -406,7 +406,7 @@ typedef struct {
  * [head_dim] with ld_q, ld_o elements from row to row, in dtype.  Scores,
  * softmax and sums are f32.  A row that sees nothing gets zeros.  workspace:
  * dvi_paged_workspace_bytes, 256-byte aligned, zeroed once before its first
- * use; calls that may overlap need one each. */
+ * use; calls that may overlap need one each, the replays of a graph among them. */
 dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_paged_batch* batch,
                             const dvi_paged_options* options, int dtype, const void* d_q, int64_t ld_q, void* d_o,
                             int64_t ld_o, void* workspace, size_t workspace_bytes, dvi_stream stream);
@@ -414,6 +414,11 @@ dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_paged_batch*
 /* Bytes of workspace that dvi_paged_attend needs on the current device for
  * any batch of this head_dim; 0 for one that it does not take. */
 size_t dvi_paged_workspace_bytes(int head_dim);
+
+/* An id of the capture that `stream` is in, 0 if it is in none: the calls of one
+ * capture on one stream follow each other and may share a workspace, which is then
+ * the graph's own. */
+uint64_t dvi_paged_capture(dvi_stream stream);
 
 /* Cached rows as values, in dtype: positions lens[b] .. of each sequence (the
  * batch's rows) to k_out, v_out [n_rows][H_kv][head_dim].  Rows of a page that

@@ -192,6 +192,16 @@ extern "C" size_t dvi_paged_workspace_bytes(int head_dim) {
          (paged_part_floats(head_dim, sms) + paged_pf_part_floats(head_dim, sms)) * sizeof(float);
 }
 
+extern "C" uint64_t dvi_paged_capture(dvi_stream stream) {
+  cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+  unsigned long long id = 0;
+  if (cudaStreamGetCaptureInfo(reinterpret_cast<cudaStream_t>(stream), &status, &id) != cudaSuccess) {
+    cudaGetLastError();   // (the legacy stream while another is captured: a launch there says so)
+    return 0;
+  }
+  return status == cudaStreamCaptureStatusNone ? 0 : id;
+}
+
 extern "C" dvi_status dvi_paged_read(const dvi_paged_cache* cache, const dvi_paged_batch* batch, int dtype,
                                      void* d_k_out, void* d_v_out, dvi_stream stream) {
   PagedReadArgs a{};

@@ -20,9 +20,12 @@ typedef dvi_status (*attend_fn)(const dvi_paged_cache*, const dvi_paged_batch*, 
                                 const void*, int64_t, void*, int64_t, void*, size_t, dvi_stream);
 typedef dvi_status (*read_fn)(const dvi_paged_cache*, const dvi_paged_batch*, int, void*, void*, dvi_stream);
 
+typedef uint64_t (*capture_fn)(dvi_stream);
+
 static append_fn g_append;
 static attend_fn g_attend;
 static read_fn g_read;
+static capture_fn g_capture;
 static PyObject *g_i32, *g_f32, *g_bf16;                                  /* torch dtypes */
 static PyObject *s_dtype, *s_shape, *s_stride, *s_get_device, *s_data_ptr; /* interned names */
 
@@ -318,13 +321,22 @@ static PyObject* py_read(PyObject* self, PyObject* const* a, Py_ssize_t n_args) 
   return PyLong_FromLong(g_read(c.c, &b, dtype == g_f32 ? DVI_F32 : DVI_BF16, (void*)k, (void*)v, stream));
 }
 
-/* init(append, attend, read addresses, int32, float32, bfloat16) */
+/* capture(stream) -> the id of the capture it is in, 0 if it is in none */
+static PyObject* py_capture(PyObject* self, PyObject* stream) {
+  (void)self;
+  dvi_stream s = (dvi_stream)PyLong_AsVoidPtr(stream);
+  if (PyErr_Occurred()) return NULL;
+  return PyLong_FromUnsignedLongLong(g_capture ? g_capture(s) : 0);
+}
+
+/* init(append, attend, read addresses, int32, float32, bfloat16[, capture address]) */
 static PyObject* py_init(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
   (void)self;
-  if (!count(n_args, 6)) return NULL;
+  if (n_args != 7 && !count(n_args, 6)) return NULL;
   g_append = (append_fn)PyLong_AsVoidPtr(a[0]);
   g_attend = (attend_fn)PyLong_AsVoidPtr(a[1]);
   g_read = (read_fn)PyLong_AsVoidPtr(a[2]);
+  g_capture = n_args == 7 ? (capture_fn)PyLong_AsVoidPtr(a[6]) : NULL;
   if (PyErr_Occurred()) return NULL;
   g_i32 = Py_NewRef(a[3]);
   g_f32 = Py_NewRef(a[4]);
@@ -335,6 +347,7 @@ static PyObject* py_init(PyObject* self, PyObject* const* a, Py_ssize_t n_args) 
 static PyMethodDef methods[] = {{"init", (PyCFunction)(void (*)(void))py_init, METH_FASTCALL, NULL},
                                 {"append", (PyCFunction)(void (*)(void))py_append, METH_FASTCALL, NULL},
                                 {"attend", (PyCFunction)(void (*)(void))py_attend, METH_FASTCALL, NULL},
+                                {"capture", py_capture, METH_O, NULL},
                                 {"read", (PyCFunction)(void (*)(void))py_read, METH_FASTCALL, NULL},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_paged", NULL, -1, methods, NULL, NULL, NULL, NULL};

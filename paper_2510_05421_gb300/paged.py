@@ -57,10 +57,20 @@ def _module():
             from . import _paged
         except ImportError as e:
             raise RuntimeError("_paged.so is missing: build it with `python -m paper_2510_05421_gb300.build`") from e
-        at = [ctypes.cast(f, ctypes.c_void_p).value for f in (L.dvi_paged_append, L.dvi_paged_attend, L.dvi_paged_read)]
-        _paged.init(*at, torch.int32, torch.float32, torch.bfloat16)
+        append, attend, read, capture = (ctypes.cast(f, ctypes.c_void_p).value for f in (
+            L.dvi_paged_append, L.dvi_paged_attend, L.dvi_paged_read, L.dvi_paged_capture))
+        _paged.init(append, attend, read, torch.int32, torch.float32, torch.bfloat16, capture)
         _calls = _paged
     return _calls
+
+
+class _Workspaces:
+    """A cache's workspaces for attend: one for each stream (calls on different streams may overlap), and one for the
+    calls of the last capture on it.  A graph keeps its own, as it may be replayed beside other calls of the stream it
+    was captured on.  Entries are (the tensor, its address, its size, the capture's id)."""
+
+    def __init__(self):
+        self.eager, self.captured = {}, {}
 
 
 def rotary_table(n_pos: int, rot_dim: int, theta: float = 10000.0, device="cuda") -> torch.Tensor:
@@ -118,7 +128,7 @@ class PagedCache:
                               v_scale.data_ptr())
         self._lib, self._calls = lib(), _module()
         self._at = (ctypes.addressof(self._c), self._index, self.status_word.data_ptr())
-        self._workspaces = {}
+        self._spaces = _Workspaces()
 
     @classmethod
     def create(cls, n_pages: int, n_kv_heads: int, head_dim: int, page_tokens: int = 64, fmt: str = "int8",
@@ -203,7 +213,10 @@ class PagedCache:
         if out is None:
             out = self._new(q.shape, q.dtype)
         s = _raw_stream(self._index)
-        ws = self._workspaces.get(s) or self._workspace(s)
+        capture = self._calls.capture(s)
+        ws = (self._spaces.captured if capture else self._spaces.eager).get(s)
+        if ws is None or ws[3] != capture:
+            ws = self._workspace(s, capture)
         rc = self._calls.attend(*self._at, table, lens, q, out, self._scale if scale is None else scale, softcap, window,
                                 slopes, row_start, max_rows, ws[1], ws[2], s)
         if rc:
@@ -238,15 +251,11 @@ class PagedCache:
             torch.cuda.synchronize(self._index)
         return [name for bit, name in DEV_BITS.items() if word & bit]
 
-    def _workspace(self, stream: int):
-        """attend's workspace, one for each stream (calls on different streams may overlap): the tensor, its
-        address and its size."""
-        with torch.cuda.device(self._index):
-            n = self._lib.dvi_paged_workspace_bytes(self.head_dim)
-            ws = torch.zeros(n, dtype=torch.uint8, device=self.device)
-            got = (ws, ws.data_ptr(), n)
-            # memory made inside a capture is the graph's: it serves this call only
-            if not torch.cuda.is_current_stream_capturing():
-                torch.cuda.current_stream(self._index).synchronize()   # zeroed for whichever stream asks
-                self._workspaces[stream] = got
+    def _workspace(self, stream: int, capture: int):
+        """A workspace for the current stream's calls, or those of the capture that it is in: the memory is that
+        stream's (the graph's), and it is cleared there, before the calls."""
+        n = self._lib.dvi_paged_workspace_bytes(self.head_dim)
+        ws = torch.zeros(n, dtype=torch.uint8, device=self.device)
+        got = (ws, ws.data_ptr(), n, capture)
+        (self._spaces.captured if capture else self._spaces.eager)[stream] = got
         return got

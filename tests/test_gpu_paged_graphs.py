@@ -1,0 +1,84 @@
+"""attend's workspace under capture: a graph has one of its own, so replays run beside other calls of the stream they
+were captured on."""
+import gc
+
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_paged import ints, make_cache
+
+pytestmark = pytest.mark.gpu
+
+
+def split_case(seed, D=64, ctx=12000):
+    """A call whose groups are cut over many teams and joined through the workspace."""
+    P = 64
+    pages = -(-(ctx + 4) // P)
+    cache = make_cache("int8", pages, 2, P, D, seed)
+    q = torch.randn(4, 8, D, device="cuda").bfloat16()
+    return cache, ints(np.arange(pages)[None]), ints([ctx]), q
+
+
+def busy(graphs, streams, eager, want, times=40):
+    """Replays on their streams and eager calls on the current one, all in flight together; every result looked at."""
+    for _ in range(times):
+        for (g, out), s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                out.zero_()
+                g.replay()
+        got = [eager() for _ in range(4)] if eager else []
+        torch.cuda.synchronize()
+        assert all(torch.equal(out, want) for _, out in graphs) and all(torch.equal(x, want) for x in got)
+
+
+def capture(case, stream):
+    cache, table, lens, q = case
+    graph, out = torch.cuda.CUDAGraph(), torch.zeros_like(q)
+    with torch.cuda.graph(graph, stream=stream):
+        cache.attend(table, lens, q, out=out)
+    return graph, out
+
+
+def test_replays_beside_calls_on_the_stream_they_were_captured_on():
+    case = split_case(1)
+    cache, table, lens, q = case
+    home, away = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(home):
+        want = cache.attend(table, lens, q)
+    torch.cuda.synchronize()
+    graph = capture(case, home)
+    with torch.cuda.stream(home):
+        busy([graph], [away], lambda: cache.attend(table, lens, q), want)
+
+
+def test_two_graphs_of_one_stream_replayed_on_two():
+    case = split_case(2)
+    cache, table, lens, q = case
+    home, away = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(home):
+        want = cache.attend(table, lens, q)
+    torch.cuda.synchronize()
+    graphs = [capture(case, home) for _ in range(2)]
+    busy(graphs, [home, away], lambda: cache.attend(table, lens, q), want)
+
+
+def test_a_graph_outlives_the_next_capture_and_its_cache_object():
+    """What a later capture on the stream, and the end of the PagedCache, give back is not the graph's."""
+    case = split_case(4)
+    cache, table, lens, q = case
+    home = torch.cuda.Stream()
+    want = cache.attend(table, lens, q)
+    torch.cuda.synchronize()
+    graph, out = capture(case, home)
+    later = [capture(split_case(5 + i), home) for i in range(2)]
+    keep = (cache.k, cache.v, cache.k_scale, cache.v_scale, cache.status_word)     # (the codes stay the caller's to keep)
+    del cache, case
+    gc.collect()
+    dirt = [torch.full((1 << 22,), 0xff, dtype=torch.uint8, device="cuda") for _ in range(16)]
+    for _ in range(5):
+        out.zero_()
+        graph.replay()
+        assert torch.equal(out, want)
+        dirt[0].fill_(0x7f)
+    assert len(later) == 2 and len(keep) == 5
