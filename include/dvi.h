@@ -405,8 +405,10 @@ typedef struct {
 /* Attention of the call's rows, already appended: q, o [n_rows][n_heads]
  * [head_dim] with ld_q, ld_o elements from row to row, in dtype.  Scores,
  * softmax and sums are f32.  A row that sees nothing gets zeros.  workspace:
- * dvi_paged_workspace_bytes, 256-byte aligned, zeroed once before its first
- * use; calls that may overlap need one each, the replays of a graph among them. */
+ * dvi_paged_workspace_bytes, 256-byte aligned, its first
+ * dvi_paged_counter_bytes zeroed once before its first use (a call leaves them
+ * zeroed; the rest may hold anything).  Calls that may overlap need one each,
+ * the replays of a graph among them. */
 dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_paged_batch* batch,
                             const dvi_paged_options* options, int dtype, const void* d_q, int64_t ld_q, void* d_o,
                             int64_t ld_o, void* workspace, size_t workspace_bytes, dvi_stream stream);
@@ -414,6 +416,7 @@ dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_paged_batch*
 /* Bytes of workspace that dvi_paged_attend needs on the current device for
  * any batch of this head_dim; 0 for one that it does not take. */
 size_t dvi_paged_workspace_bytes(int head_dim);
+size_t dvi_paged_counter_bytes(void);
 
 /* An id of the capture that `stream` is in, 0 if it is in none: the calls of one
  * capture on one stream follow each other and may share a workspace, which is then

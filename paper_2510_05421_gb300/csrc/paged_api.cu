@@ -192,6 +192,11 @@ extern "C" size_t dvi_paged_workspace_bytes(int head_dim) {
          (paged_part_floats(head_dim, sms) + paged_pf_part_floats(head_dim, sms)) * sizeof(float);
 }
 
+extern "C" size_t dvi_paged_counter_bytes(void) {
+  const int sms = current_sms();
+  return sms > 0 ? paged_counter_bytes(sms) : 0;
+}
+
 extern "C" uint64_t dvi_paged_capture(dvi_stream stream) {
   cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
   unsigned long long id = 0;

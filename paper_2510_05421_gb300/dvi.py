@@ -27,7 +27,7 @@ EXPORTS = ["dvi_workspace_bytes", "dvi_create", "dvi_prefill", "dvi_draft_verify
            "dvi_update_drafter", "dvi_ar_step", "dvi_get_stats", "dvi_last_error", "dvi_destroy",
            "dvi_debug_buffer", "dvi_linear", "dvi_timing", "dvi_get_timing", "dvi_linear_noalloc",
            "dvi_paged_append", "dvi_paged_attend", "dvi_paged_read", "dvi_paged_workspace_bytes",
-           "dvi_paged_capture"]
+           "dvi_paged_counter_bytes", "dvi_paged_capture"]
 
 
 class ModelConfig(ctypes.Structure):
@@ -126,6 +126,8 @@ def lib() -> ctypes.CDLL:
         L.dvi_paged_read.argtypes = [vp, vp, i, vp, vp, vp]
         L.dvi_paged_workspace_bytes.restype = sz
         L.dvi_paged_workspace_bytes.argtypes = [i]
+        L.dvi_paged_counter_bytes.restype = sz
+        L.dvi_paged_counter_bytes.argtypes = []
         L.dvi_paged_capture.restype = ctypes.c_uint64
         L.dvi_paged_capture.argtypes = [vp]
         _lib = L

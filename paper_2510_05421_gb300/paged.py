@@ -253,9 +253,10 @@ class PagedCache:
 
     def _workspace(self, stream: int, capture: int):
         """A workspace for the current stream's calls, or those of the capture that it is in: the memory is that
-        stream's (the graph's), and it is cleared there, before the calls."""
+        stream's (the graph's), and its counters are cleared there, before the calls."""
         n = self._lib.dvi_paged_workspace_bytes(self.head_dim)
-        ws = torch.zeros(n, dtype=torch.uint8, device=self.device)
+        ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+        ws[:self._lib.dvi_paged_counter_bytes()].zero_()
         got = (ws, ws.data_ptr(), n, capture)
         (self._spaces.captured if capture else self._spaces.eager)[stream] = got
         return got

@@ -1,11 +1,12 @@
-"""attend's workspace under capture: a graph has one of its own, so replays run beside other calls of the stream they
-were captured on."""
+"""attend's workspace: captured calls have one of their own, cleared only where it must be, and replays run beside other
+calls of the stream they were captured on."""
 import gc
 
 import numpy as np
 import pytest
 import torch
 
+from paper_2510_05421_gb300 import lib
 from test_gpu_paged import ints, make_cache
 
 pytestmark = pytest.mark.gpu
@@ -82,3 +83,19 @@ def test_a_graph_outlives_the_next_capture_and_its_cache_object():
         assert torch.equal(out, want)
         dirt[0].fill_(0x7f)
     assert len(later) == 2 and len(keep) == 5
+
+
+def test_only_the_counters_have_to_be_zero():
+    """A workspace made of memory that holds anything else."""
+    cache, table, lens, q = split_case(3)
+    want = cache.attend(table, lens, q)
+    n, c = lib().dvi_paged_workspace_bytes(64), lib().dvi_paged_counter_bytes()
+    assert 0 < c <= 4096 and c < n
+    for fill in (0xff, 0x7f, 0x01):
+        other, side = split_case(3)[0], torch.cuda.Stream()
+        other.k.copy_(cache.k), other.v.copy_(cache.v), other.k_scale.copy_(cache.k_scale), other.v_scale.copy_(cache.v_scale)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            dirt = torch.full((n,), fill, dtype=torch.uint8, device="cuda")
+            del dirt
+            assert torch.equal(other.attend(table, lens, q), want)
