@@ -8,6 +8,7 @@ on the GPU than ctypes and Python checks would take to enqueue them."""
 from __future__ import annotations
 
 import ctypes
+import weakref
 from typing import Optional, Tuple
 
 import torch
@@ -65,12 +66,16 @@ def _module():
 
 
 class _Workspaces:
-    """A cache's workspaces for attend: one for each stream (calls on different streams may overlap), and one for the
-    calls of the last capture on it.  A graph keeps its own, as it may be replayed beside other calls of the stream it
-    was captured on.  Entries are (the tensor, its address, its size, the capture's id)."""
+    """attend's workspaces on one device and for one head_dim, shared by its caches (a stream's calls run one after
+    another, whatever their cache): one for each stream, and one for the calls of the last capture on it.  A graph
+    keeps its own, as it may be replayed beside other calls of the stream it was captured on.  Entries are (the
+    tensor, its address, its size, the capture's id)."""
 
     def __init__(self):
         self.eager, self.captured = {}, {}
+
+
+_workspaces = weakref.WeakValueDictionary()     # (device, head_dim): they go with their last cache
 
 
 def rotary_table(n_pos: int, rot_dim: int, theta: float = 10000.0, device="cuda") -> torch.Tensor:
@@ -128,7 +133,7 @@ class PagedCache:
                               v_scale.data_ptr())
         self._lib, self._calls = lib(), _module()
         self._at = (ctypes.addressof(self._c), self._index, self.status_word.data_ptr())
-        self._spaces = _Workspaces()
+        self._spaces = _workspaces.setdefault((self._index, D), _Workspaces())
 
     @classmethod
     def create(cls, n_pages: int, n_kv_heads: int, head_dim: int, page_tokens: int = 64, fmt: str = "int8",

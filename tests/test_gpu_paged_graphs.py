@@ -1,5 +1,6 @@
-"""attend's workspace: captured calls have one of their own, cleared only where it must be, and replays run beside other
-calls of the stream they were captured on."""
+"""attend's workspace: captured calls have one of their own, cleared once a graph and only where it must be, replays run
+beside other calls of the stream they were captured on, and caches share what a stream's calls use one after another."""
+import ctypes
 import gc
 
 import numpy as np
@@ -99,3 +100,50 @@ def test_only_the_counters_have_to_be_zero():
             dirt = torch.full((n,), fill, dtype=torch.uint8, device="cuda")
             del dirt
             assert torch.equal(other.attend(table, lens, q), want)
+
+
+def captured_nodes(stream):
+    """How many nodes the graph has that `stream` is being captured into."""
+    rt = ctypes.CDLL("libcudart.so.13")
+    r, state, cid, graph, n = ctypes.byref, ctypes.c_int(), ctypes.c_uint64(), ctypes.c_void_p(), ctypes.c_size_t()
+    assert rt.cudaStreamGetCaptureInfo(ctypes.c_void_p(stream.cuda_stream), r(state), r(cid), r(graph), None, None,
+                                       None) == 0
+    assert state.value == 1 and rt.cudaGraphGetNodes(graph, None, r(n)) == 0
+    return n.value
+
+
+@pytest.mark.parametrize("warm", [False, True])
+def test_a_graph_clears_its_counters_once(warm):
+    layers = [split_case(i) for i in range(6)]
+    side = torch.cuda.Stream()
+    if warm:
+        with torch.cuda.stream(side):
+            layers[0][0].attend(*layers[0][1:])
+    want = [c.attend(t, n, q) for c, t, n, q in layers]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        outs = [c.attend(t, n, q) for c, t, n, q in layers]
+        n = captured_nodes(side)
+    assert n == len(layers) + 1          # a launch each, and the clearing
+    for _ in range(3):
+        for o in outs:
+            o.zero_()
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_caches_share_a_workspace():
+    """A stream's calls run one after another: they use one workspace, whatever the cache, and it goes with the last."""
+    gc.collect()
+    start = torch.cuda.memory_allocated()
+    layers = [split_case(i) for i in range(6)]
+    before, size = torch.cuda.memory_allocated(), lib().dvi_paged_workspace_bytes(64)
+    want = [c.attend(t, n, q) for c, t, n, q in layers]
+    grown = torch.cuda.memory_allocated() - before - sum(w.numel() * 2 for w in want)
+    assert grown < 2 * size, (grown, size)          # (the allocator rounds it up)
+    for _ in range(3):
+        assert all(torch.equal(c.attend(t, n, q), w) for (c, t, n, q), w in zip(layers, want))
+    del layers, want
+    gc.collect()
+    assert torch.cuda.memory_allocated() - start < size
