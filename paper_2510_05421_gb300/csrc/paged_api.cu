@@ -30,6 +30,14 @@ int current_sms() {
 // device, so the rule cannot ask for them).
 constexpr int kFewVectors = 32;
 
+// Held while an attend is enqueued: the second launch of a mixed batch runs beside the one before
+// it on its stream, which has to be its own first one and not another host thread's attend, as
+// that one shares its counters.  One lock for each of 64 kinds of stream handles.
+std::mutex& enqueue_lock(dvi_stream stream) {
+  static std::mutex locks[64];
+  return locks[(reinterpret_cast<uintptr_t>(stream) * 0x9e3779b97f4a7c15ull) >> 58];
+}
+
 bool on16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool ld_ok(int64_t ld, int64_t least, int esz) { return ld >= least && (ld * esz) % 16 == 0; }
 
@@ -159,6 +167,7 @@ extern "C" dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_p
   a.pf_counters = a.counters + static_cast<size_t>(sms) * kPagedTeams;
   a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + paged_counter_bytes(sms));
   a.pf_part = a.part + paged_part_floats(a.c.D, sms);
+  std::lock_guard<std::mutex> enqueue(enqueue_lock(stream));
   cudaGetLastError();
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const bool e4m3 = cache->format == DVI_KV_E4M3;
