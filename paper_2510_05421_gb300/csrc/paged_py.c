@@ -7,7 +7,8 @@
  * Tensors are looked at through their Python attributes, so the module knows
  * nothing of torch's C++ layout.  It does not link the library: init() gets
  * the addresses of the entry points.  Every refusal is a ValueError, raised
- * before the library is called. */
+ * before the library is called.  Other threads run while the library has a call: a
+ * launch waits where the GPU's queue is full, perhaps for a host function in Python. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -249,9 +250,13 @@ static PyObject* py_append(PyObject* self, PyObject* const* a, Py_ssize_t n_args
   }
   dvi_stream stream = (dvi_stream)PyLong_AsVoidPtr(a[12]);
   if (PyErr_Occurred()) return NULL;
-  return PyLong_FromLong(g_append(c.c, &b, dtype == g_f32 ? DVI_F32 : DVI_BF16, (const void*)k, ld_k, (const void*)v,
-                                  ld_v, (const float*)rot, (int)rot_dim, (int)n_pos, (const void*)q, ld_q, (void*)o,
-                                  ld_o, (int)heads, stream));
+  const int type = dtype == g_f32 ? DVI_F32 : DVI_BF16;
+  dvi_status rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = g_append(c.c, &b, type, (const void*)k, ld_k, (const void*)v, ld_v, (const float*)rot, (int)rot_dim, (int)n_pos,
+                (const void*)q, ld_q, (void*)o, ld_o, (int)heads, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
 }
 
 /* attend(cache, device, status, table, lens, q, out, scale, softcap, window, slopes, row_start, max_rows, workspace,
@@ -299,8 +304,12 @@ static PyObject* py_attend(PyObject* self, PyObject* const* a, Py_ssize_t n_args
   const size_t bytes = PyLong_AsSize_t(a[14]);
   dvi_stream stream = (dvi_stream)PyLong_AsVoidPtr(a[15]);
   if (PyErr_Occurred()) return NULL;
-  return PyLong_FromLong(g_attend(c.c, &b, &op, dtype == g_f32 ? DVI_F32 : DVI_BF16, (const void*)q, ld_q, (void*)o,
-                                  ld_o, ws, bytes, stream));
+  const int type = dtype == g_f32 ? DVI_F32 : DVI_BF16;
+  dvi_status rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = g_attend(c.c, &b, &op, type, (const void*)q, ld_q, (void*)o, ld_o, ws, bytes, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
 }
 
 /* read(cache, device, status, table, lens, k_out, v_out, row_start, max_rows, stream) -> status */
@@ -318,7 +327,12 @@ static PyObject* py_read(PyObject* self, PyObject* const* a, Py_ssize_t n_args) 
     return NULL;
   dvi_stream stream = (dvi_stream)PyLong_AsVoidPtr(a[9]);
   if (PyErr_Occurred()) return NULL;
-  return PyLong_FromLong(g_read(c.c, &b, dtype == g_f32 ? DVI_F32 : DVI_BF16, (void*)k, (void*)v, stream));
+  const int type = dtype == g_f32 ? DVI_F32 : DVI_BF16;
+  dvi_status rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = g_read(c.c, &b, type, (void*)k, (void*)v, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
 }
 
 /* capture(stream) -> the id of the capture it is in, 0 if it is in none */
