@@ -16,7 +16,7 @@ from __future__ import annotations
 
 import argparse
 import json
-from typing import List, Sequence
+from typing import List, Optional, Sequence
 
 import numpy as np
 import torch
@@ -133,35 +133,66 @@ class PagedDecoder:
         self.advance(rows)
         return self.verifier_logits(h[row_start[1:].long() - 1]).argmax(-1).to(torch.int32)
 
-    def step(self, pending: torch.Tensor):
-        """K greedy draft passes, one verify pass over the K rows, the longest agreeing prefix and the correction.
-        Returns (committed tokens [B, K], how many of them, how many drafts agreed, the new pending tokens)."""
-        B, K = len(self.host_lens), self.K
-        self.reserve([K] * B)
-        hs, drafts, tok = [], [], pending
+    def _taking_part(self, live: Optional[Sequence[int]]):
+        """The sequences of a pass (by default those that hold rows), where they lie in tensors of all sequences and
+        the row starts of one row each; both None where every sequence takes part."""
+        B = len(self.host_lens)
+        live = [b for b in range(B) if self.host_lens[b]] if live is None else sorted(set(live))
+        if len(live) == B:
+            return live, None, None
+        takes = [int(b in live) for b in range(B)]
+        start = torch.tensor([0] + np.cumsum(takes).tolist(), dtype=torch.int32).to(self.device)
+        return live, torch.tensor(live, dtype=torch.long).to(self.device), start
+
+    def _spread(self, at, x: torch.Tensor, rest: Optional[torch.Tensor] = None):
+        """x [sequences that took part, ...] among all of them; the others have rest, or 0."""
+        if at is None:
+            return x
+        full = x.new_zeros((len(self.host_lens), *x.shape[1:])) if rest is None else rest.clone()
+        return full.index_copy_(0, at, x)
+
+    def step(self, pending: torch.Tensor, live: Optional[Sequence[int]] = None):
+        """K greedy draft passes, one verify pass over the K rows, the longest agreeing prefix and the correction, of
+        the sequences in `live` (by default those that hold rows: a released one takes none).
+        Returns (committed tokens [B, K], how many of them, how many drafts agreed, the new pending tokens); the
+        sequences that took no part have 0 of them and their pending token as it was."""
+        live, at, start = self._taking_part(live)
+        n_live, K = len(live), self.K
+        if n_live == 0:
+            none = torch.zeros(len(self.host_lens), dtype=torch.long, device=self.device)
+            return torch.zeros(len(none), K, dtype=torch.int32, device=self.device), none, none.clone(), pending
+        self.reserve([K if b in live else 0 for b in range(len(self.host_lens))])
+        hs, drafts = [], []
+        tok = pending if at is None else pending[at]
         for j in range(K):
-            h = self.layers(0, self.split, self.embed(tok), self.lens + j)
+            h = self.layers(0, self.split, self.embed(tok), self.lens + j, start, 1)
             hs.append(h)
             tok = self.drafter_logits(h).argmax(-1).to(torch.int32)
             drafts.append(tok)
-        rows = torch.stack(hs, 1).reshape(B * K, -1)                     # sequence after sequence
-        h = self.layers(self.split, self.s.n_layers, rows, self.lens)
-        y = self.verifier_logits(h).argmax(-1).to(torch.int32).view(B, K)
+        rows = torch.stack(hs, 1).reshape(n_live * K, -1)                # sequence after sequence
+        h = self.layers(self.split, self.s.n_layers, rows, self.lens, None if start is None else start * K, K)
+        y = self.verifier_logits(h).argmax(-1).to(torch.int32).view(n_live, K)
         t = torch.stack(drafts, 1)
         m = (t == y).int().cumprod(1).sum(1)
         n = (m + 1).clamp_max(K)
         out = torch.where(torch.arange(K, device=self.device) < m[:, None], t, y)
         new_pending = out.gather(1, (n - 1).long()[:, None]).squeeze(1)
+        n = self._spread(at, n)
         self.advance(n.tolist())
-        return out, n, m, new_pending
+        return self._spread(at, out), n, self._spread(at, m), self._spread(at, new_pending, pending)
 
-    def ar_step(self, pending: torch.Tensor) -> torch.Tensor:
-        """One greedy token of the whole model for every sequence."""
-        B = len(self.host_lens)
-        self.reserve([1] * B)
-        h = self.layers(0, self.s.n_layers, self.embed(pending), self.lens)
-        self.advance([1] * B)
-        return self.verifier_logits(h).argmax(-1).to(torch.int32)
+    def ar_step(self, pending: torch.Tensor, live: Optional[Sequence[int]] = None) -> torch.Tensor:
+        """One greedy token of the whole model for the sequences in `live` (by default those that hold rows); the
+        others' pending tokens stay."""
+        live, at, start = self._taking_part(live)
+        if not live:
+            return pending
+        takes = [int(b in live) for b in range(len(self.host_lens))]
+        self.reserve(takes)
+        tok = pending if at is None else pending[at]
+        h = self.layers(0, self.s.n_layers, self.embed(tok), self.lens, start, 1)
+        self.advance(takes)
+        return self._spread(at, self.verifier_logits(h).argmax(-1).to(torch.int32), pending)
 
     def generate(self, prompts: Sequence[np.ndarray], n_gen: int, speculative: bool = True):
         """n_gen tokens of each prompt, and the mean accepted length (None without speculation)."""

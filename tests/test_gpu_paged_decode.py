@@ -76,3 +76,29 @@ def test_command(monkeypatch, capsys):
     main()
     out = capsys.readouterr().out
     assert '"device_flags": []' in out and '"fmt": "int8"' in out
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_others_go_on_after_a_release(dtype):
+    """Steps and single tokens of two sequences around a released one, ragged, are (near) greedy as ever."""
+    w, W, dec = make("int8", dtype)
+    prompts = make_prompts(w)
+    tok = dec.prefill(prompts)
+    out = [[int(t)] for t in tok]
+    dec.release(1)
+    free = len(dec.free)
+    for i in range(4):
+        ids, n, _, tok = dec.step(tok)
+        assert int(n[1]) == 0
+        for o, row, c in zip(out, ids.tolist(), n.tolist()):
+            o.extend(row[:c])
+        tok = dec.ar_step(tok)
+        for b in (0, 2):
+            out[b].append(int(tok[b]))
+    assert len(out[1]) == 1 and int(tok[1]) == out[1][0] and dec.held[1] == [] and len(dec.free) <= free
+    assert all(c.status() == [] for c in dec.caches)
+    model = OracleModel(rounded_weights(W) if dtype == "bf16" else W, w.shape, w.lora_gamma)
+    for b in (0, 2):
+        z = teacher_forced_logits(model, np.concatenate([prompts[b], out[b][:-1]]))[len(prompts[b]) - 1:]
+        gap = z.max(-1) - z[np.arange(len(out[b])), out[b]]
+        assert (gap <= 0.15 * z.std(-1)).all(), (gap / z.std(-1)).max()

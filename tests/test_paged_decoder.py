@@ -1,0 +1,83 @@
+"""PagedDecoder's bookkeeping without a GPU, over a stand-in for the layers: which sequences a pass takes, what they may
+need of pages and positions, and what they commit.  In the stand-in's language an even token t is followed by t + 2, and
+the drafter says so; an odd one by t + 4, where the drafter says t + 2 and is always rejected."""
+import numpy as np
+import torch
+
+from paper_2510_05421_gb300.paged_decode import PagedDecoder
+
+V, P, K, SPLIT, LAYERS = 400, 16, 4, 1, 2
+
+
+class Shape:
+    n_layers = LAYERS
+
+
+class Decoder(PagedDecoder):
+    """The layers see nothing and pass on which token each row had; what a pass takes is noted."""
+
+    def __init__(self, slots, max_seq_len, n_pages):
+        self.s, self.split, self.K, self.P = Shape, SPLIT, K, P
+        self.device = torch.device("cpu")
+        self.caches = []
+        self.free = list(range(n_pages))
+        self.held = [[] for _ in range(slots)]
+        self.host_lens = [0] * slots
+        self.max_seq_len = max_seq_len
+        self.table = torch.full((slots, -(-max_seq_len // P)), -1, dtype=torch.int32)
+        self.lens = torch.zeros(slots, dtype=torch.int32)
+        self.rows = []
+
+    def embed(self, tokens):
+        return torch.nn.functional.one_hot(tokens.long(), V).float()
+
+    def layers(self, lo, hi, x, lens, row_start=None, max_rows=None):
+        B = len(self.host_lens)
+        counts = [x.shape[0] // B] * B if row_start is None else row_start.diff().tolist()
+        assert sum(counts) == x.shape[0] and (max_rows is None or max(counts) <= max_rows)
+        for b, n in enumerate(counts):
+            # every row has a position, and its page is held
+            assert int(lens[b]) + n <= self.max_seq_len
+            for p in range(int(lens[b]), int(lens[b]) + n):
+                assert int(self.table[b, p // P]) >= 0
+        self.rows.append(counts)
+        return x
+
+    def drafter_logits(self, h):
+        return torch.roll(h, 2, -1)
+
+    def verifier_logits(self, h):
+        odd = h.argmax(-1) % 2 == 1
+        return torch.where(odd[:, None], torch.roll(h, 4, -1), torch.roll(h, 2, -1))
+
+
+def prompts(*last):
+    return [np.array([9, 9, t], np.int32)[-(1 + t % 3):] for t in last]
+
+
+def chain(t, n):
+    step = 4 if t % 2 else 2
+    return [t + step * (i + 1) for i in range(n)]
+
+
+def test_released_sequences_take_no_rows():
+    p = prompts(2, 3, 4)
+    dec = Decoder(3, 64, 12)
+    tok = dec.prefill(p)
+    assert tok.tolist() == [4, 7, 6]
+    dec.release(1)
+    free = len(dec.free)
+    for _ in range(3):
+        out, n, m, new = dec.step(tok)
+        assert n.tolist() == [K, 0, K] and m.tolist() == [K, 0, K] and new[1] == tok[1]
+        assert out[0].tolist() == chain(int(tok[0]), K) and out[2].tolist() == chain(int(tok[2]), K)
+        tok = new
+    tok = dec.ar_step(tok)
+    assert tok[0] == 4 + 2 * 3 * K + 2 and tok[1] == 7
+    assert dec.held[1] == [] and dec.host_lens[1] == 0 and dec.lens.tolist()[1] == 0
+    assert len(dec.free) <= free and all(c[1] == 0 for c in dec.rows[1:])
+    for b in (0, 2):
+        dec.release(b)
+    assert sorted(dec.free) == list(range(12))
+    out, n, m, new = dec.step(tok)
+    assert n.tolist() == [0, 0, 0] and torch.equal(new, tok) and torch.equal(dec.ar_step(tok), tok)
