@@ -1,6 +1,6 @@
 """Self-speculative decoding over the 8-bit paged KV cache: the draft, verify
 and commit step of Sec. 3.3 for a batch of sequences of any lengths, with
-pages taken as sequences grow and given back when they end.
+pages taken as sequences grow and given back by release().
 
     python -m paper_2510_05421_gb300.paged_decode --workload tiny --fmt int8
 
@@ -195,22 +195,24 @@ class PagedDecoder:
         return self._spread(at, self.verifier_logits(h).argmax(-1).to(torch.int32), pending)
 
     def generate(self, prompts: Sequence[np.ndarray], n_gen: int, speculative: bool = True):
-        """n_gen tokens of each prompt, and the mean accepted length (None without speculation)."""
+        """n_gen tokens of each prompt, and the mean accepted length (None without speculation).  A sequence that has its
+        tokens takes no more rows; its pages stay its own until release()."""
         tok = self.prefill(prompts)
         out = [[int(t)] for t in tok]
         agreed = steps = 0
-        while min(len(o) for o in out) < n_gen:
+        while live := [b for b, o in enumerate(out) if len(o) < n_gen]:
             if speculative:
-                ids, n, m, tok = self.step(tok)
+                ids, n, m, tok = self.step(tok, live)
                 for o, row, c in zip(out, ids.tolist(), n.tolist()):
                     o.extend(row[:c])
                 agreed += int(m.sum())
             else:
-                tok = self.ar_step(tok)
-                for o, t in zip(out, tok.tolist()):
-                    o.append(t)
-            steps += 1
-        return [o[:n_gen] for o in out], agreed / max(1, steps * len(out)) if speculative else None
+                tok = self.ar_step(tok, live)
+                new = tok.tolist()
+                for b in live:
+                    out[b].append(new[b])
+            steps += len(live)
+        return [o[:n_gen] for o in out], agreed / max(1, steps) if speculative else None
 
 
 def run(workload_name: str, fmt: str, n_gen: int, page_tokens: int, batch: int):

@@ -2,6 +2,7 @@
 need of pages and positions, and what they commit.  In the stand-in's language an even token t is followed by t + 2, and
 the drafter says so; an odd one by t + 4, where the drafter says t + 2 and is always rejected."""
 import numpy as np
+import pytest
 import torch
 
 from paper_2510_05421_gb300.paged_decode import PagedDecoder
@@ -58,6 +59,26 @@ def prompts(*last):
 def chain(t, n):
     step = 4 if t % 2 else 2
     return [t + step * (i + 1) for i in range(n)]
+
+
+@pytest.mark.parametrize("first", [(2, 3), (3, 2), (2, 3, 4, 5)])
+@pytest.mark.parametrize("speculative", [True, False])
+def test_sequences_of_unequal_acceptance(first, speculative):
+    """A sequence that has its tokens takes no more rows, while one whose drafts all fail goes on: what both need is
+    bounded by their own lengths."""
+    n_gen, p = 40, prompts(*first)
+    room = max(len(x) for x in p) + n_gen + 2 * K + 1
+    dec = Decoder(len(first), room, len(first) * -(-room // P))
+    tokens, mean = dec.generate(p, n_gen, speculative)
+    assert tokens == [chain(t, n_gen) for t in first]
+    for x, n in zip(p, dec.host_lens):
+        assert len(x) + n_gen - 1 <= n < len(x) + n_gen - 1 + K
+    if speculative:
+        fast = -(-(n_gen - 1) // K)
+        assert sum(c[first.index(2)] > 0 for c in dec.rows[1:]) == fast * (K + 1)
+        # per step of a sequence: all K drafts agree, or none
+        evens = sum(t % 2 == 0 for t in first)
+        assert mean == pytest.approx(evens * fast * K / (evens * fast + (len(first) - evens) * (n_gen - 1)))
 
 
 def test_released_sequences_take_no_rows():
