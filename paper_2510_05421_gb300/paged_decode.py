@@ -123,7 +123,10 @@ class PagedDecoder:
 
     # -- calls ------------------------------------------------------------
     def prefill(self, prompts: Sequence[np.ndarray]) -> torch.Tensor:
-        """Every sequence's prompt in one ragged pass; the greedy token after each (pending, in no cache yet)."""
+        """The prompts, one for each slot, in one ragged pass behind what the sequences hold; the greedy token after each
+        (pending, in no cache yet)."""
+        if len(prompts) != len(self.host_lens):
+            raise ValueError(f"prefill: {len(prompts)} prompts for {len(self.host_lens)} slots")
         rows = [len(p) for p in prompts]
         self.reserve(rows)
         start = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)

@@ -102,3 +102,15 @@ def test_released_sequences_take_no_rows():
     assert sorted(dec.free) == list(range(12))
     out, n, m, new = dec.step(tok)
     assert n.tolist() == [0, 0, 0] and torch.equal(new, tok) and torch.equal(dec.ar_step(tok), tok)
+
+
+def test_prompts_that_do_not_fit_the_slots_are_refused():
+    """Before any page is taken."""
+    dec = Decoder(2, 64, 8)
+    one = np.array([2], np.int32)
+    for bad in ([one], [one] * 3, []):
+        with pytest.raises(ValueError):
+            dec.prefill(bad)
+        with pytest.raises(ValueError):
+            dec.generate(bad, 4)
+    assert len(dec.free) == 8 and dec.host_lens == [0, 0] and dec.rows == []
