@@ -124,17 +124,21 @@ class PagedDecoder:
     # -- calls ------------------------------------------------------------
     def prefill(self, prompts: Sequence[np.ndarray]) -> torch.Tensor:
         """The prompts, one for each slot, in one ragged pass behind what the sequences hold; the greedy token after each
-        (pending, in no cache yet)."""
+        (pending, in no cache yet).  A slot whose prompt is empty takes no rows, and its token is -1."""
         if len(prompts) != len(self.host_lens):
             raise ValueError(f"prefill: {len(prompts)} prompts for {len(self.host_lens)} slots")
         rows = [len(p) for p in prompts]
+        if not any(rows):
+            return torch.full((len(rows),), -1, dtype=torch.int32, device=self.device)
         self.reserve(rows)
         start = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
         row_start = torch.from_numpy(start).to(self.device)
         tokens = torch.from_numpy(np.concatenate(prompts).astype(np.int32)).to(self.device)
         h = self.layers(0, self.s.n_layers, self.embed(tokens), self.lens, row_start, max(rows))
         self.advance(rows)
-        return self.verifier_logits(h[row_start[1:].long() - 1]).argmax(-1).to(torch.int32)
+        some = row_start.diff() > 0
+        last = torch.where(some, row_start[1:] - 1, 0).long()
+        return torch.where(some, self.verifier_logits(h[last]).argmax(-1).to(torch.int32), -1)
 
     def _taking_part(self, live: Optional[Sequence[int]]):
         """The sequences of a pass (by default those that hold rows), where they lie in tensors of all sequences and
@@ -200,6 +204,8 @@ class PagedDecoder:
     def generate(self, prompts: Sequence[np.ndarray], n_gen: int, speculative: bool = True):
         """n_gen tokens of each prompt, and the mean accepted length (None without speculation).  A sequence that has its
         tokens takes no more rows; its pages stay its own until release()."""
+        if not all(len(p) for p in prompts):
+            raise ValueError("generate: an empty prompt has no next token")
         tok = self.prefill(prompts)
         out = [[int(t)] for t in tok]
         agreed = steps = 0

@@ -114,3 +114,19 @@ def test_prompts_that_do_not_fit_the_slots_are_refused():
         with pytest.raises(ValueError):
             dec.generate(bad, 4)
     assert len(dec.free) == 8 and dec.host_lens == [0, 0] and dec.rows == []
+
+
+def test_empty_prompts():
+    """A slot without a prompt gets no rows and no token; the others' tokens are theirs, and a slot filled later joins."""
+    empty = np.zeros(0, np.int32)
+    dec = Decoder(3, 64, 12)
+    assert dec.prefill([empty, np.array([5, 8], np.int32), empty]).tolist() == [-1, 10, -1]
+    assert dec.lens.tolist() == [0, 2, 0] and dec.held[0] == [] and dec.held[2] == []
+    first = dec.prefill([np.array([3], np.int32), empty, empty])
+    assert first.tolist() == [7, -1, -1] and dec.lens.tolist() == [1, 2, 0]
+    assert dec.prefill([empty] * 3).tolist() == [-1, -1, -1]
+    out, n, _, _ = dec.step(torch.tensor([7, 10, -1], dtype=torch.int32))
+    assert n.tolist() == [1, K, 0] and out[0, 0] == 11 and out[1].tolist() == chain(10, K)
+    with pytest.raises(ValueError):
+        dec.generate([empty, np.array([3], np.int32), empty], 4)
+    assert dec.host_lens == [2, 6, 0]
