@@ -391,9 +391,10 @@ dvi_status dvi_paged_append(const dvi_paged_cache* cache, const dvi_paged_batch*
                             dvi_stream stream);
 
 /* Options of dvi_paged_attend: score = scale (q . k), then softcap * tanh(score
- * / softcap) where softcap > 0, then + slopes[head] * (p_key - p_row) where
- * slopes (device f32 [n_heads]) is given.  A row at position p sees the held
- * positions up to p, and with window > 0 only those past p - window. */
+ * / softcap) where softcap > 0 (more than 1e-30 of scale), then + slopes[head]
+ * (p_key - p_row) where slopes (device f32 [n_heads]) is given.  A row at
+ * position p sees the held positions up to p, and with window > 0 only those
+ * past p - window. */
 typedef struct {
   int n_heads;          /* a multiple of H_kv: heads h G .. h G + G - 1 read KV head h */
   float scale;

@@ -137,6 +137,7 @@ extern "C" dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_p
       !(options->scale > 0.f) || !(options->scale < 1e30f) || !(options->softcap >= 0.f) ||
       !(options->softcap < 1e30f) || options->window < 0)
     return DVI_ERR_INVALID_ARG;
+  if (options->softcap > 0.f && !(options->scale / options->softcap < 1e30f)) return DVI_ERR_INVALID_ARG;
   if (a.c.n_rows == 0) return DVI_OK;
   const int64_t least = static_cast<int64_t>(options->n_heads) * a.c.D;
   if (!d_q || !d_o || !on16(d_q) || !on16(d_o) || !ld_ok(ld_q, least, esz) || !ld_ok(ld_o, least, esz))

@@ -282,8 +282,12 @@ static PyObject* py_attend(PyObject* self, PyObject* const* a, Py_ssize_t n_args
   const double scale = PyFloat_AsDouble(a[7]), softcap = PyFloat_AsDouble(a[8]);
   const int64_t window = PyLong_AsLongLong(a[9]);
   if (PyErr_Occurred()) return NULL;
-  if (!(scale > 0.0 && scale < 1e30) || !(softcap >= 0.0 && softcap < 1e30) || window < 0 || window > 0x7fffffff) {
+  if (!((float)scale > 0.f && scale < 1e30) || !(softcap >= 0.0 && softcap < 1e30) || window < 0 || window > 0x7fffffff) {
     refuse("attend", "needs scale > 0, softcap >= 0 and window >= 0");
+    return NULL;
+  }
+  if (softcap > 0.0 && !(scale / softcap < 1e30)) {
+    refuse("attend", "softcap must be 0 or more than 1e-30 of scale");
     return NULL;
   }
   op.n_heads = (int)heads;
