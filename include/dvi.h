@@ -361,7 +361,8 @@ typedef struct {
   int n_seqs;                 /* 1..1024 */
   int max_pages;              /* columns of the page table */
   int n_rows;                 /* rows of the call, all sequences together */
-  int max_rows;               /* no sequence has more (more are dropped: DVI_DEV_KV_FULL) */
+  int max_rows;               /* no sequence has more (more are dropped: DVI_DEV_KV_FULL); the kernels are chosen by
+                                 it where row_start is given: a close bound is a faster one */
   const int32_t* table;       /* [n_seqs][max_pages] pages of each sequence, in order; a negative entry is a
                                  page that is not held: its positions are not attended to (an entry past
                                  n_pages counts as one, DVI_DEV_KV_FULL) */
@@ -375,8 +376,9 @@ typedef struct {
  * rotary: [n_pos][rot_dim / 2] pairs (cos, sin) by which dims d and
  * d + rot_dim / 2 of the keys (d < rot_dim / 2; rot_dim a multiple of 16) are
  * rotated at their position, or null.  q (or null): the call's queries
- * [n_rows][n_heads][head_dim], rotated alike into q_out (which may be q).
- * dtype (dvi_dtype) is that of k, v, q and q_out; the arithmetic is f32.
+ * [n_rows][n_heads][head_dim], rotated alike into q_out (which may be q;
+ * rows of no sequence stay as they are).  dtype (dvi_dtype) is that of k, v, q
+ * and q_out; the arithmetic is f32.
  *
  * A page's scale is the largest magnitude it has held since its first row was
  * written, over 127 (int8) or 448 (e4m3), at least 2^-80; when it grows, the
@@ -404,12 +406,18 @@ typedef struct {
 } dvi_paged_options;
 
 /* Attention of the call's rows, already appended: q, o [n_rows][n_heads]
- * [head_dim] with ld_q, ld_o elements from row to row, in dtype.  Scores,
- * softmax and sums are f32.  A row that sees nothing gets zeros.  workspace:
+ * [head_dim] with ld_q, ld_o elements from row to row, in dtype.  Scores, their
+ * maxima and all sums are f32; a softmax weight, its page's value scale in it,
+ * enters the product with the codes rounded to f16 (by 2^-11 of it; f32 rows: as
+ * two f16 numbers, 2^-21), one below 2^-19 of the row's largest by up to 2^-30 of
+ * that.  A row
+ * that sees nothing gets zeros, a row of no sequence (before the first row start,
+ * from the last on, or dropped past max_rows) stays as it is.  workspace:
  * dvi_paged_workspace_bytes, 256-byte aligned, its first
  * dvi_paged_counter_bytes zeroed once before its first use (a call leaves them
  * zeroed; the rest may hold anything).  Calls that may overlap need one each,
- * the replays of a graph among them. */
+ * the replays of a graph among them; those of one stream follow each other, also
+ * from several host threads, and share one. */
 dvi_status dvi_paged_attend(const dvi_paged_cache* cache, const dvi_paged_batch* batch,
                             const dvi_paged_options* options, int dtype, const void* d_q, int64_t ld_q, void* d_o,
                             int64_t ld_o, void* workspace, size_t workspace_bytes, dvi_stream stream);
@@ -426,7 +434,7 @@ uint64_t dvi_paged_capture(dvi_stream stream);
 
 /* Cached rows as values, in dtype: positions lens[b] .. of each sequence (the
  * batch's rows) to k_out, v_out [n_rows][H_kv][head_dim].  Rows of a page that
- * is not held are zeros. */
+ * is not held are zeros, those of no sequence stay as they are. */
 dvi_status dvi_paged_read(const dvi_paged_cache* cache, const dvi_paged_batch* batch, int dtype, void* d_k_out,
                           void* d_v_out, dvi_stream stream);
 

@@ -21,13 +21,13 @@ int current_sms() {
   return n;
 }
 
-// Query vectors (rows x query heads of a KV head) up to which a bf16 sequence's
-// rows are few.  us by the few-row kernel / the prompt kernel, int8 and 8 KV heads
-// of 128: 24 vectors over 200 positions 12.1 / 11.4 (8 sequences) and over 4000
-// 71.5 / 160 (32), 28 over 16000 26.1 / 32.2 (1), 32 over 500 16.3 / 28.2 (32, hd
-// 64); above the border, one sequence, 40 over 20 10.8 / 7.9, 64 over 500 17.3 /
-// 15.6, 40 over 4000 19.0 / 20.2, 64 over 16000 31.0 / 36.1 (the lengths are on the
-// device, so the rule cannot ask for them).
+// Query vectors (rows x query heads of a KV head) up to which a bf16 sequence's rows are
+// few.  Which kernel is faster depends on the lengths too, and those are on the device:
+// the border is where a wrong choice costs least.  us by the few-row kernel / the prompt
+// kernel, int8 and 8 KV heads of 128: below it 24 vectors over 200 positions 12.1 / 11.4
+// (8 sequences), 28 over 16000 26.1 / 32.2 (1), 24 over 4000 71.5 / 160 (32), 32 over 500
+// 16.3 / 28.2 (32, hd 64); above it, one sequence, 40 over 20 10.8 / 7.9, 64 over 500
+// 17.3 / 15.6, 40 over 4000 19.0 / 20.2, 64 over 16000 31.0 / 36.1.
 constexpr int kFewVectors = 32;
 
 // Held while an attend is enqueued: the second launch of a mixed batch runs beside the one before

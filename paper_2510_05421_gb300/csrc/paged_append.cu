@@ -17,8 +17,9 @@
 // registers, so four blocks of 256 an SM hide each other's chain of loads
 // (lengths, rows and entry, scale); only pages of 128 rows of hd 128 take four.
 // Bound: bytes (the rows in, half or a quarter of them out).  8192 rows of 32 K,
-// V and query heads each, e4m3 pages of 16: 72.6 us, 4.6 TB/s (83.4 with four
-// items and two blocks); 64 sequences' single tokens 5.6 us, one 2.8 us: latency.
+// V and query heads each, e4m3 pages of 16: 73 to 75 us, 4.5 TB/s (83.4 with four
+// items and two blocks; the 64 registers spill 12 to 32 bytes); 64 sequences' single tokens
+// 5.6 us, one 2.8 us: latency.
 #include <algorithm>
 
 #include "paged.cuh"

@@ -31,9 +31,13 @@
 // turn, each with its own running maximum and a private ring of cp.async
 // stages, and are joined in shared memory at the end of the group.
 //
-// f32 queries (PAIR) enter as an f16 pair hi + lo, as do their probabilities.
-// A query vector is scaled by a power of two so that f16's range does not
-// matter.
+// Fewer bits than 32, and why: w goes to f16 for the tensor operation (2^-11 of it,
+// and its error averages over the keys: below the 2^-8 of a bf16 result, measured
+// against 64 bits the same as f32 arithmetic throughout); the denominator sums it
+// unrounded.  f32 queries (PAIR) enter as an f16 pair hi + lo, as do their
+// weights: 2^-21.  A query vector is scaled by a power of two so that f16's
+// range does not matter.  log2 vs shares the exponent's f32 with the score: near
+// the smallest vs (2^-80) its rounding is 2^-18 of the weight.
 #pragma once
 
 #include <algorithm>
@@ -66,7 +70,8 @@ struct PaPlan {
 
 template <int HD, int NT, bool PAIR>
 struct PaShape {
-  // sixteen warps where their registers allow it (128 a thread)
+  // sixteen warps where their registers allow it (128 a thread; two tiles of hd 128 spill
+  // 128 bytes at that, an f32 tile of hd 128 48)
   static constexpr int kWarps = NT * (PAIR ? 2 : 1) <= 2 ? 16 : 8;
   static constexpr int kThreads = kWarps * 32;
   static constexpr int kTeams = kWarps / kPaTeam;            // most teams of a CTA

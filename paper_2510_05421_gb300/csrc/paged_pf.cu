@@ -12,8 +12,9 @@
 //                  back into the TMEM columns of S, sum of w / vs;
 //   O += W C_v     A = W from TMEM, B = the widened codes as they lie (rows are
 //                  the K index: MN-major).
-// The accumulator is rescaled only when a vector's maximum outgrows its
-// reference by 2^13.  A tile's scores are double-buffered in TMEM, two chunks
+// The weights' f16 (2^-11 of each, as in paged_attn.cuh) is what the tensor operation
+// takes beside f16 codes; the denominator sums them unrounded.  The accumulator is
+// rescaled only when a vector's maximum outgrows its reference by 2^13.  A tile's scores are double-buffered in TMEM, two chunks
 // ahead of the product of its weights, so its threads never wait for them.
 //
 // Roles (512 threads): warps 0-3 and 4-7 hold the vectors of tile 0 and 1,

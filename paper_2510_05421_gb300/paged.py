@@ -97,7 +97,11 @@ class PagedCache:
 
     Rows of a call lie sequence after sequence: with row_start None every
     sequence has the same number, else sequence b has rows row_start[b] ..
-    row_start[b + 1] - 1 (int32 [B + 1]) and max_rows bounds the longest.
+    row_start[b + 1] - 1 (int32 [B + 1]) and max_rows bounds the longest (the
+    kernels are chosen by it: without it, by the rows of all sequences
+    together, and single tokens pay for prompts that might be there).  Rows
+    of no sequence (a buffer's unused end) are not written: in a tensor that
+    the call made they hold anything.
 
     A call runs on the current stream.  With `stream` it runs there, behind
     what the current one has in flight; wait for that stream before its
