@@ -438,6 +438,115 @@ uint64_t dvi_paged_capture(dvi_stream stream);
 dvi_status dvi_paged_read(const dvi_paged_cache* cache, const dvi_paged_batch* batch, int dtype, void* d_k_out,
                           void* d_v_out, dvi_stream stream);
 
+/* ---------------------------------------------------------------- page plans
+ * The pages of a paged cache handed out on the device, from the lengths alone:
+ * no copy to the host between the passes of a decoder, and a graph may capture
+ * the call.  The pool is the caller's: a stack of the pages that nobody holds,
+ * and for each of n_seqs slots its page table and how many pages it holds. */
+typedef struct {
+  int n_pages;          /* of the cache */
+  int page_tokens;      /* P: 16, 32, 64 or 128 */
+  int n_seqs;           /* 1..1024 */
+  int max_pages;        /* columns of the page table */
+  int32_t* stack;       /* [n_pages]: its first *n_free entries are the free pages, the last of them is taken first */
+  int32_t* n_free;      /* [1] */
+  int32_t* table;       /* [n_seqs][max_pages]: a slot's pages in order, -1 behind them */
+  int32_t* held;        /* [n_seqs] pages of each slot */
+  int32_t* status;      /* DVI_DEV_* bits, or null */
+} dvi_page_pool;
+
+/* Bring every slot b to the ceil((lens[b] + rows[b]) / P) pages that rows[b]
+ * (d_rows, or rows_each of every slot where it is null) more positions behind
+ * lens[b] need.  First the pages past that go back: slot after slot, in order of
+ * the table, onto the stack; their table entries become -1.  Then pages that are
+ * missing come off the stack's top, in the same order.  A slot whose missing
+ * pages are not all there, or not all in its table, gets none of them
+ * (DVI_DEV_KV_FULL) and the slots after it are served still.  With rows of 0 the
+ * call gives back what a rejected block or (lens[b] = 0) a sequence that ended
+ * held.  Negative lens and rows count as 0.
+ *
+ * d_row_start [n_seqs + 1] (or null): the first row of each slot when their rows
+ * lie one after another, as dvi_paged_append and dvi_paged_attend take it.
+ * d_slots, d_positions [n_rows] (or null): for each of those rows the place of
+ * its position in the cache, page * P + position % P (-1 where its page is not
+ * held), and the position; both -1 behind the last row.  Rows past n_rows have no
+ * entry (DVI_DEV_KV_FULL).
+ *
+ * A pool out of order (a count or page out of its range) is not written past its
+ * arrays; pages out of range are not handed out (DVI_DEV_KV_FULL). */
+dvi_status dvi_paged_plan(const dvi_page_pool* pool, const int32_t* d_lens, const int32_t* d_rows, int rows_each,
+                          int n_rows, int32_t* d_row_start, int64_t* d_slots, int32_t* d_positions,
+                          dvi_stream stream);
+
+/* ---------------------------------------------------------------- sampling
+ * Speculative decoding with sampled tokens (the greedy step's counterpart for
+ * programs that sample): probabilities of logits, and the verification of
+ * drafted tokens against them.  No context; every call only enqueues work on
+ * `stream`, allocates nothing and takes its random numbers as inputs.  Rows may
+ * lie apart (ld elements from row to row) and need only their elements'
+ * alignment.  vocab is at most 262144 (2^18).  d_status: as above, or null. */
+typedef struct {
+  const float* temperature;   /* device [n_rows], or null: temperature_all of every row */
+  const int32_t* top_k;       /* device [n_rows], or null: top_k_all */
+  const float* top_p;         /* device [n_rows], or null: top_p_all */
+  float temperature_all;      /* >= 0 */
+  int top_k_all;              /* >= 0 */
+  float top_p_all;            /* >= 0 */
+} dvi_sampling;
+
+/* Probabilities of n_rows rows of logits x (in dtype, dvi_dtype): with tokens
+ * ordered by logit, equal ones by index, and w_i = exp((x_i - max x) / T), the
+ * first top_k tokens stay (0: all), of those the fewest first ones whose w sum to
+ * top_p of theirs (at least one; 1 or more: all), and their w over the sum of what
+ * stays are the probabilities; 0 elsewhere.  T = 0: 1 at the first of the largest
+ * logits.  T counts as 2^-100 below that and as 2^100 above.  A row of -inf alone
+ * gets zeros.
+ *
+ * Which tokens stay is decided on w in fixed point (2^-44 of the row's largest, off
+ * by about 2^-38), so it does not depend on the order of any sum.  NaN logits count
+ * as -inf and +inf as the largest finite number (DVI_DEV_NONFINITE).  Of settings in
+ * device arrays, T that is negative or NaN counts as 0, top_k below 0 as 0, top_p
+ * NaN as 1 (NaN: DVI_DEV_NONFINITE).  d_probs does not overlap d_logits. */
+dvi_status dvi_token_probs(int dtype, const void* d_logits, int64_t ld_logits, int n_rows, int vocab,
+                           const dvi_sampling* sampling, float* d_probs, int64_t ld_probs, int32_t* d_status,
+                           dvi_stream stream);
+
+typedef struct {
+  int n_seqs;                 /* at most 65536 */
+  int vocab;
+  int n_drafts;               /* drafted tokens of all sequences together */
+  int max_drafts;             /* no sequence has more (more are not looked at) */
+  int bonus;                  /* 1: every sequence has a target row behind those of its drafts */
+  const int32_t* draft_start; /* device [n_seqs + 1] first draft of each sequence, or null: n_drafts / n_seqs each */
+  const int32_t* draft_ids;   /* device [n_drafts] */
+  const float* u_accept;      /* device [n_drafts], uniform in [0, 1) */
+  const float* u_token;       /* device [n_seqs], uniform in [0, 1) */
+  int32_t* status;
+} dvi_draft_batch;
+
+/* Verify drafted tokens x_1 .. x_K of each sequence (Sec. 3.3 with sampling in
+ * the argmax's place): with the target's probabilities p_j and the drafter's q_j
+ * of the place of x_j, x_j is accepted while u_accept_j q_j(x_j) < p_j(x_j); m is
+ * how many are before the first that is not.  Then one token more comes from
+ * max(p_{m+1} - q_{m+1}, 0) (from p_{m+1} where that is zero everywhere), or at m =
+ * K from the bonus row: the first token up to which the numbers sum to more than
+ * u_token of their total.  Committed tokens are so distributed as the target's own.
+ *
+ * d_target: f32 rows, sequence b's first is row draft_start[b] + b * bonus, its
+ * drafts' in order and then its bonus row.  d_draft: f32 rows, one a draft, or null
+ * for tokens that were drafted greedily (q_j is 1 at x_j).  Numbers need not sum to
+ * 1; a negative one counts as 0, NaN and infinities too (DVI_DEV_NONFINITE).  Without
+ * drafts and with bonus = 1 the call samples a token of each row.
+ *
+ * d_out_ids [n_seqs][max_drafts + bonus]: x_1 .. x_m and the token, -1 behind them;
+ * d_n_committed [n_seqs]: m + 1, or K at m = K without a bonus row; d_n_accepted
+ * [n_seqs]: m.  A drafted id outside [0, vocab) is rejected (DVI_DEV_BAD_TOKEN) and
+ * its row's q taken as it is (greedy: as 0).  A row that is zero everywhere gives no
+ * token (DVI_DEV_NONFINITE): n_committed is m. */
+dvi_status dvi_verify_drafts(const dvi_draft_batch* batch, const float* d_target, int64_t ld_target,
+                             const float* d_draft, int64_t ld_draft, int32_t* d_out_ids, int32_t* d_n_committed,
+                             int32_t* d_n_accepted, dvi_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

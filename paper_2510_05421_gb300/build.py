@@ -1,5 +1,5 @@
-"""Build libdvi.so in-tree from csrc/*.cu for sm_103a (nvcc, no torch extension), and the CPython module _paged.so
-(the paged cache's argument checks) from csrc/paged_py.c.
+"""Build libdvi.so in-tree from csrc/*.cu for sm_103a (nvcc, no torch extension), and the CPython modules _paged.so
+and _sampling.so (argument checks of the paged cache, of page plans and sampling) from csrc/*_py.c.
 
     python -m paper_2510_05421_gb300.build
 """
@@ -16,6 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libdvi.so")
 PY_OUT = os.path.join(HERE, "_paged.so")
+PY_SAMPLING_OUT = os.path.join(HERE, "_sampling.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
          "-Xcompiler", "-Wno-deprecated-declarations"]
@@ -33,14 +34,15 @@ def sources():
 
 
 def build_py() -> str:
-    """The CPython side of the paged cache's binding."""
-    tmp = PY_OUT + ".tmp"
-    cmd = [os.environ.get("CC") or "gcc", "-O2", "-fPIC", "-shared", "-std=c11", "-Wall", "-Wextra",
-           "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "paged_py.c"), "-o", tmp]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"{cmd[0]} failed on paged_py.c:\n{r.stderr}")
-    os.replace(tmp, PY_OUT)
+    """The CPython side of the bindings."""
+    for source, out in (("paged_py.c", PY_OUT), ("sampling_py.c", PY_SAMPLING_OUT)):
+        tmp = out + ".tmp"
+        cmd = [os.environ.get("CC") or "gcc", "-O2", "-fPIC", "-shared", "-std=c11", "-Wall", "-Wextra",
+               "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, source), "-o", tmp]
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"{cmd[0]} failed on {source}:\n{r.stderr}")
+        os.replace(tmp, out)
     return PY_OUT
 
 

@@ -4,15 +4,11 @@
  * bound them (one greedy token's attend: 9 us on the GPU, 11.5 us to enqueue
  * through ctypes).
  *
- * Tensors are looked at through their Python attributes, so the module knows
- * nothing of torch's C++ layout.  It does not link the library: init() gets
- * the addresses of the entry points.  Every refusal is a ValueError, raised
- * before the library is called.  Other threads run while the library has a call: a
- * launch waits where the GPU's queue is full, perhaps for a host function in Python. */
-#define PY_SSIZE_T_CLEAN
-#include <Python.h>
-
-#include "../../include/dvi.h"
+ * It does not link the library: init() gets the addresses of the entry points.
+ * Every refusal is a ValueError, raised before the library is called.  Other
+ * threads run while the library has a call: a launch waits where the GPU's queue
+ * is full, perhaps for a host function in Python. */
+#include "tensor_py.h"
 
 typedef dvi_status (*append_fn)(const dvi_paged_cache*, const dvi_paged_batch*, int, const void*, int64_t,
                                 const void*, int64_t, const float*, int, int, const void*, int64_t, void*, int64_t,
@@ -27,16 +23,6 @@ static append_fn g_append;
 static attend_fn g_attend;
 static read_fn g_read;
 static capture_fn g_capture;
-static PyObject *g_i32, *g_f32, *g_bf16;                                  /* torch dtypes */
-static PyObject *s_dtype, *s_shape, *s_stride, *s_get_device, *s_data_ptr; /* interned names */
-
-typedef struct {
-  PyObject* dtype;      /* borrowed: a torch dtype lives as long as torch */
-  int dims;
-  int64_t size[4], step[4];
-  int64_t device;
-  uintptr_t ptr;
-} Tensor;
 
 /* The cache a call is on. */
 typedef struct {
@@ -44,65 +30,6 @@ typedef struct {
   int64_t device;
   int32_t* status;
 } Cache;
-
-static int ints_of(PyObject* tuple, int64_t* out, int want) {
-  if (!PyTuple_Check(tuple) || (want >= 0 && PyTuple_GET_SIZE(tuple) != want) || PyTuple_GET_SIZE(tuple) > 4) return -1;
-  const int n = (int)PyTuple_GET_SIZE(tuple);
-  for (int i = 0; i < n; ++i) {
-    out[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(tuple, i));
-    if (out[i] == -1 && PyErr_Occurred()) return -1;
-  }
-  return n;
-}
-
-static int call_int(PyObject* o, PyObject* name, int64_t* out) {
-  PyObject* r = PyObject_CallMethodNoArgs(o, name);
-  if (!r) return 0;
-  *out = (int64_t)PyLong_AsUnsignedLongLongMask(r);
-  Py_DECREF(r);
-  return !PyErr_Occurred();
-}
-
-/* What a tensor is; an AttributeError or the like passes through as it is. */
-static int look(PyObject* o, const char* what, Tensor* t) {
-  PyObject* r = PyObject_GetAttr(o, s_dtype);
-  if (!r) return 0;
-  t->dtype = r;
-  Py_DECREF(r);
-  r = PyObject_GetAttr(o, s_shape);
-  if (!r) return 0;
-  t->dims = ints_of(r, t->size, -1);
-  Py_DECREF(r);
-  if (t->dims >= 0) {
-    r = PyObject_CallMethodNoArgs(o, s_stride);
-    if (!r) return 0;
-    if (ints_of(r, t->step, t->dims) < 0) t->dims = -1;
-    Py_DECREF(r);
-  }
-  if (t->dims < 0) {
-    if (!PyErr_Occurred()) PyErr_Format(PyExc_ValueError, "%s: too many dimensions", what);
-    return 0;
-  }
-  int64_t p;
-  if (!call_int(o, s_get_device, &t->device) || !call_int(o, s_data_ptr, &p)) return 0;
-  t->ptr = (uintptr_t)p;
-  return 1;
-}
-
-static int contiguous(const Tensor* t) {
-  int64_t step = 1;
-  for (int i = t->dims - 1; i >= 0; --i) {
-    if (t->size[i] == 0) return 1;
-    if (t->size[i] != 1 && t->step[i] != step) return 0;
-    step *= t->size[i];
-  }
-  return 1;
-}
-
-static int refuse(const char* what, const char* why) {
-  PyErr_Format(PyExc_ValueError, "%s: %s", what, why);
-  return 0;
-}
 
 static int cache_of(PyObject* address, PyObject* device, PyObject* status, Cache* c) {
   c->c = (const dvi_paged_cache*)PyLong_AsVoidPtr(address);
@@ -196,12 +123,6 @@ static int lead_of(const char* what, PyObject* o, PyObject** dtype, int64_t* n, 
   *n = size[0];
   *heads = size[1];
   return 1;
-}
-
-static int count(Py_ssize_t got, Py_ssize_t want) {
-  if (got == want) return 1;
-  PyErr_Format(PyExc_TypeError, "%zd arguments expected, got %zd", want, got);
-  return 0;
 }
 
 /* append(cache, device, status, table, lens, k, v, q, rotary, row_start, max_rows, q_out, stream) -> status */
@@ -371,11 +292,6 @@ static PyMethodDef methods[] = {{"init", (PyCFunction)(void (*)(void))py_init, M
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_paged", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__paged(void) {
-  s_dtype = PyUnicode_InternFromString("dtype");
-  s_shape = PyUnicode_InternFromString("shape");
-  s_stride = PyUnicode_InternFromString("stride");
-  s_get_device = PyUnicode_InternFromString("get_device");
-  s_data_ptr = PyUnicode_InternFromString("data_ptr");
-  if (!s_dtype || !s_shape || !s_stride || !s_get_device || !s_data_ptr) return NULL;
+  if (!intern_names()) return NULL;
   return PyModule_Create(&module);
 }

@@ -1,0 +1,294 @@
+/* CPython side of the page plans and of sampling (include/dvi.h): checks a
+ * call's tensors and makes the library call, like the paged cache's (paged_py.c),
+ * and for the same reason: these calls take a few microseconds on the GPU. */
+#include "tensor_py.h"
+
+typedef dvi_status (*probs_fn)(int, const void*, int64_t, int, int, const dvi_sampling*, float*, int64_t, int32_t*,
+                               dvi_stream);
+typedef dvi_status (*verify_fn)(const dvi_draft_batch*, const float*, int64_t, const float*, int64_t, int32_t*,
+                                int32_t*, int32_t*, dvi_stream);
+typedef dvi_status (*plan_fn)(const dvi_page_pool*, const int32_t*, const int32_t*, int, int, int32_t*, int64_t*,
+                              int32_t*, dvi_stream);
+
+static probs_fn g_probs;
+static verify_fn g_verify;
+static plan_fn g_plan;
+static PyObject* g_i64;
+
+#define MAX_VOCAB (1 << 18)
+
+/* Rows [n, vocab] of `dtype` that may lie apart: elements from row to row. */
+static int rows_of(const char* what, PyObject* o, PyObject* dtype, int64_t n, int64_t vocab, int64_t device,
+                   uintptr_t* ptr, int64_t* ld) {
+  Tensor t;
+  if (!look(o, what, &t)) return 0;
+  if (t.dtype != dtype || t.dims != 2 || t.size[0] != n || t.size[1] != vocab) {
+    PyErr_Format(PyExc_ValueError, "%s must be %s [%lld, %lld]", what, dtype == g_f32 ? "float32" : "bfloat16",
+                 (long long)n, (long long)vocab);
+    return 0;
+  }
+  if (t.device != device) return refuse(what, "not on the call's device");
+  *ld = n <= 1 ? vocab : t.step[0];
+  if (n && ((vocab > 1 && t.step[1] != 1) || *ld < vocab)) return refuse(what, "each row must be contiguous");
+  *ptr = t.ptr;
+  return 1;
+}
+
+/* A contiguous array [n] of `dtype`. */
+static int array_of(const char* what, PyObject* o, PyObject* dtype, int64_t n, int64_t device, uintptr_t* ptr) {
+  Tensor t;
+  if (!look(o, what, &t)) return 0;
+  if (t.dtype != dtype || t.dims != 1 || t.size[0] != n || !contiguous(&t)) {
+    PyErr_Format(PyExc_ValueError, "%s must be contiguous %s [%lld]", what,
+                 dtype == g_f32 ? "float32" : dtype == g_i64 ? "int64" : "int32", (long long)n);
+    return 0;
+  }
+  if (t.device != device) return refuse(what, "not on the call's device");
+  *ptr = t.ptr;
+  return 1;
+}
+
+static int is_number(PyObject* o) { return PyFloat_Check(o) || PyLong_Check(o); }
+
+/* A device status word, or None. */
+static int status_of(const char* what, PyObject* o, int64_t device, int32_t** out) {
+  uintptr_t p = 0;
+  if (o != Py_None && !array_of(what, o, g_i32, 1, device, &p)) return 0;
+  *out = (int32_t*)p;
+  return 1;
+}
+
+/* probs(logits, temperature, top_k, top_p, out, status, stream) -> status */
+static PyObject* py_probs(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
+  (void)self;
+  if (!count(n_args, 7)) return NULL;
+  Tensor t;
+  if (!look(a[0], "token_probs: logits", &t)) return NULL;
+  if ((t.dtype != g_f32 && t.dtype != g_bf16) || t.dims != 2 || t.size[1] < 1 || t.size[1] > MAX_VOCAB ||
+      t.size[0] > (1 << 30)) {
+    refuse("token_probs: logits", "must be float32 or bfloat16 [n, vocab], vocab 1 to 262144");
+    return NULL;
+  }
+  if (t.device < 0) {
+    refuse("token_probs: logits", "not on a CUDA device");
+    return NULL;
+  }
+  const int64_t n = t.size[0], vocab = t.size[1], ld = n <= 1 ? vocab : t.step[0];
+  if (n && ((vocab > 1 && t.step[1] != 1) || ld < vocab)) {
+    refuse("token_probs: logits", "each row must be contiguous");
+    return NULL;
+  }
+  uintptr_t out, p = 0;
+  int64_t ld_out;
+  dvi_sampling s = {NULL, NULL, NULL, 0.f, 0, 0.f};
+  if (is_number(a[1])) {
+    const double v = PyFloat_AsDouble(a[1]);
+    if (PyErr_Occurred()) return NULL;
+    if (!(v >= 0.0)) {
+      refuse("token_probs", "temperature must be at least 0");
+      return NULL;
+    }
+    /* (a temperature above 0 stays above it in f32) */
+    s.temperature_all = v > 0.0 && v < 1e-37 ? 1e-37f : (float)v;
+  } else if (!array_of("token_probs: temperature", a[1], g_f32, n, t.device, &p)) {
+    return NULL;
+  }
+  s.temperature = (const float*)p;
+  p = 0;
+  if (PyLong_Check(a[2])) {
+    const int64_t v = PyLong_AsLongLong(a[2]);
+    if (PyErr_Occurred()) return NULL;
+    if (v < 0) {
+      refuse("token_probs", "top_k must not be negative");
+      return NULL;
+    }
+    s.top_k_all = v > MAX_VOCAB ? MAX_VOCAB : (int)v;
+  } else if (!array_of("token_probs: top_k", a[2], g_i32, n, t.device, &p)) {
+    return NULL;
+  }
+  s.top_k = (const int32_t*)p;
+  p = 0;
+  if (is_number(a[3])) {
+    const double v = PyFloat_AsDouble(a[3]);
+    if (PyErr_Occurred()) return NULL;
+    if (!(v >= 0.0)) {
+      refuse("token_probs", "top_p must be at least 0");
+      return NULL;
+    }
+    s.top_p_all = (float)v;
+  } else if (!array_of("token_probs: top_p", a[3], g_f32, n, t.device, &p)) {
+    return NULL;
+  }
+  s.top_p = (const float*)p;
+  int32_t* status;
+  if (!rows_of("token_probs: out", a[4], g_f32, n, vocab, t.device, &out, &ld_out) ||
+      !status_of("token_probs: status", a[5], t.device, &status))
+    return NULL;
+  dvi_stream stream = (dvi_stream)PyLong_AsVoidPtr(a[6]);
+  if (PyErr_Occurred()) return NULL;
+  const int type = t.dtype == g_f32 ? DVI_F32 : DVI_BF16;
+  dvi_status rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = g_probs(type, (const void*)t.ptr, ld, (int)n, (int)vocab, &s, (float*)out, ld_out, status, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+/* verify(target, draft_ids, u_accept, u_token, draft, draft_start, max_drafts, bonus, ids, n_committed, n_accepted,
+ *        status, stream) -> status */
+static PyObject* py_verify(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
+  (void)self;
+  if (!count(n_args, 13)) return NULL;
+  Tensor t, u, d;
+  if (!look(a[0], "verify_drafts: target", &t) || !look(a[3], "verify_drafts: u_token", &u) ||
+      !look(a[1], "verify_drafts: draft_ids", &d))
+    return NULL;
+  if (t.dtype != g_f32 || t.dims != 2 || t.size[1] < 1 || t.size[1] > MAX_VOCAB) {
+    refuse("verify_drafts: target", "must be float32 [rows, vocab], vocab 1 to 262144");
+    return NULL;
+  }
+  if (t.device < 0) {
+    refuse("verify_drafts: target", "not on a CUDA device");
+    return NULL;
+  }
+  if (u.dtype != g_f32 || u.dims != 1 || u.size[0] > (1 << 16)) {
+    refuse("verify_drafts: u_token", "must be float32 [n_seqs], at most 65536 of them");
+    return NULL;
+  }
+  if (d.dtype != g_i32 || d.dims != 1 || d.size[0] > (1 << 30)) {
+    refuse("verify_drafts: draft_ids", "must be int32 [n_drafts]");
+    return NULL;
+  }
+  const int64_t B = u.size[0], n = d.size[0], vocab = t.size[1];
+  const int bonus = PyObject_IsTrue(a[7]);
+  if (bonus < 0) return NULL;
+  if (B == 0 && n) {
+    refuse("verify_drafts", "drafts without a sequence");
+    return NULL;
+  }
+  int64_t most = n;
+  uintptr_t start = 0, ids = 0, ua, ut, p, q = 0, out = 0, nc, na;
+  int64_t ld_p, ld_q = 0;
+  if (a[5] == Py_None) {
+    if (B && n % B) {
+      PyErr_Format(PyExc_ValueError, "verify_drafts: %lld drafts do not divide into %lld sequences (give draft_start)",
+                   (long long)n, (long long)B);
+      return NULL;
+    }
+    most = B ? n / B : 0;
+  } else if (!array_of("verify_drafts: draft_start", a[5], g_i32, B + 1, t.device, &start)) {
+    return NULL;
+  }
+  if (a[6] != Py_None) {
+    const int64_t m = PyLong_AsLongLong(a[6]);
+    if (PyErr_Occurred()) return NULL;
+    if (m < 0 || (a[5] == Py_None && m < most)) {
+      refuse("verify_drafts", "max_drafts must not be negative, nor below the drafts of each sequence");
+      return NULL;
+    }
+    most = m;
+  }
+  if (most > (1 << 20)) {
+    refuse("verify_drafts", "at most 2^20 drafts of a sequence (give max_drafts)");
+    return NULL;
+  }
+  if (!rows_of("verify_drafts: target", a[0], g_f32, n + (bonus ? B : 0), vocab, t.device, &p, &ld_p) ||
+      !array_of("verify_drafts: draft_ids", a[1], g_i32, n, t.device, &ids) ||
+      !array_of("verify_drafts: u_accept", a[2], g_f32, n, t.device, &ua) ||
+      !array_of("verify_drafts: u_token", a[3], g_f32, B, t.device, &ut) ||
+      (a[4] != Py_None && !rows_of("verify_drafts: draft", a[4], g_f32, n, vocab, t.device, &q, &ld_q)) ||
+      !array_of("verify_drafts: n_committed", a[9], g_i32, B, t.device, &nc) ||
+      !array_of("verify_drafts: n_accepted", a[10], g_i32, B, t.device, &na))
+    return NULL;
+  Tensor o;
+  if (!look(a[8], "verify_drafts: ids", &o)) return NULL;
+  if (o.dtype != g_i32 || o.dims != 2 || o.size[0] != B || o.size[1] != most + (bonus ? 1 : 0) || !contiguous(&o) ||
+      o.device != t.device) {
+    refuse("verify_drafts: ids", "must be contiguous int32 [n_seqs, max_drafts + bonus] on the call's device");
+    return NULL;
+  }
+  out = o.ptr;
+  int32_t* status;
+  if (!status_of("verify_drafts: status", a[11], t.device, &status)) return NULL;
+  dvi_stream stream = (dvi_stream)PyLong_AsVoidPtr(a[12]);
+  if (PyErr_Occurred()) return NULL;
+  const dvi_draft_batch b = {(int)B, (int)vocab, (int)n, (int)most, bonus ? 1 : 0, (const int32_t*)start,
+                             (const int32_t*)ids, (const float*)ua, (const float*)ut, status};
+  dvi_status rc;
+  Py_BEGIN_ALLOW_THREADS
+  /* (an empty tensor's rows need no memory, a drafter without rows is still one) */
+  rc = g_verify(&b, (const float*)p, ld_p, n ? (const float*)q : NULL, ld_q, (int32_t*)out, (int32_t*)nc,
+                (int32_t*)na, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+/* plan(pool, device, lens, rows, n_rows, row_start, slots, positions, stream) -> status */
+static PyObject* py_plan(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
+  (void)self;
+  if (!count(n_args, 9)) return NULL;
+  const dvi_page_pool* pool = (const dvi_page_pool*)PyLong_AsVoidPtr(a[0]);
+  const int64_t device = PyLong_AsLongLong(a[1]);
+  if (PyErr_Occurred()) return NULL;
+  const int64_t B = pool->n_seqs;
+  int64_t each = 0, n_rows = 0;
+  uintptr_t lens, rows = 0, start = 0, slots = 0, positions = 0;
+  if (!array_of("plan: lens", a[2], g_i32, B, device, &lens)) return NULL;
+  if (PyLong_Check(a[3])) {
+    each = PyLong_AsLongLong(a[3]);
+    if (PyErr_Occurred()) return NULL;
+    if (each < 0 || each > (1 << 30)) {
+      refuse("plan", "rows must be 0 to 2^30");
+      return NULL;
+    }
+  } else if (!array_of("plan: rows", a[3], g_i32, B, device, &rows)) {
+    return NULL;
+  }
+  if (a[4] != Py_None) {
+    n_rows = PyLong_AsLongLong(a[4]);
+    if (PyErr_Occurred()) return NULL;
+    if (n_rows < 0 || n_rows > (1 << 30)) {
+      refuse("plan", "n_rows must be 0 to 2^30");
+      return NULL;
+    }
+  }
+  if ((a[5] != Py_None && !array_of("plan: row_start", a[5], g_i32, B + 1, device, &start)) ||
+      (a[6] != Py_None && !array_of("plan: slots", a[6], g_i64, n_rows, device, &slots)) ||
+      (a[7] != Py_None && !array_of("plan: positions", a[7], g_i32, n_rows, device, &positions)))
+    return NULL;
+  dvi_stream stream = (dvi_stream)PyLong_AsVoidPtr(a[8]);
+  if (PyErr_Occurred()) return NULL;
+  dvi_status rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = g_plan(pool, (const int32_t*)lens, (const int32_t*)rows, (int)each, (int)n_rows, (int32_t*)start,
+              (int64_t*)slots, (int32_t*)positions, stream);
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong(rc);
+}
+
+/* init(probs, verify, plan addresses, int32, int64, float32, bfloat16) */
+static PyObject* py_init(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
+  (void)self;
+  if (!count(n_args, 7)) return NULL;
+  g_probs = (probs_fn)PyLong_AsVoidPtr(a[0]);
+  g_verify = (verify_fn)PyLong_AsVoidPtr(a[1]);
+  g_plan = (plan_fn)PyLong_AsVoidPtr(a[2]);
+  if (PyErr_Occurred()) return NULL;
+  g_i32 = Py_NewRef(a[3]);
+  g_i64 = Py_NewRef(a[4]);
+  g_f32 = Py_NewRef(a[5]);
+  g_bf16 = Py_NewRef(a[6]);
+  Py_RETURN_NONE;
+}
+
+static PyMethodDef methods[] = {{"init", (PyCFunction)(void (*)(void))py_init, METH_FASTCALL, NULL},
+                                {"plan", (PyCFunction)(void (*)(void))py_plan, METH_FASTCALL, NULL},
+                                {"probs", (PyCFunction)(void (*)(void))py_probs, METH_FASTCALL, NULL},
+                                {"verify", (PyCFunction)(void (*)(void))py_verify, METH_FASTCALL, NULL},
+                                {NULL, NULL, 0, NULL}};
+static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_sampling", NULL, -1, methods, NULL, NULL, NULL, NULL};
+
+PyMODINIT_FUNC PyInit__sampling(void) {
+  if (!intern_names()) return NULL;
+  return PyModule_Create(&module);
+}

@@ -27,7 +27,7 @@ EXPORTS = ["dvi_workspace_bytes", "dvi_create", "dvi_prefill", "dvi_draft_verify
            "dvi_update_drafter", "dvi_ar_step", "dvi_get_stats", "dvi_last_error", "dvi_destroy",
            "dvi_debug_buffer", "dvi_linear", "dvi_timing", "dvi_get_timing", "dvi_linear_noalloc",
            "dvi_paged_append", "dvi_paged_attend", "dvi_paged_read", "dvi_paged_workspace_bytes",
-           "dvi_paged_counter_bytes", "dvi_paged_capture"]
+           "dvi_paged_counter_bytes", "dvi_paged_capture", "dvi_paged_plan", "dvi_token_probs", "dvi_verify_drafts"]
 
 
 class ModelConfig(ctypes.Structure):
@@ -130,6 +130,12 @@ def lib() -> ctypes.CDLL:
         L.dvi_paged_counter_bytes.argtypes = []
         L.dvi_paged_capture.restype = ctypes.c_uint64
         L.dvi_paged_capture.argtypes = [vp]
+        L.dvi_paged_plan.restype = i
+        L.dvi_paged_plan.argtypes = [vp, vp, vp, i, i, vp, vp, vp, vp]
+        L.dvi_token_probs.restype = i
+        L.dvi_token_probs.argtypes = [i, vp, ll, i, i, vp, vp, ll, vp, vp]
+        L.dvi_verify_drafts.restype = i
+        L.dvi_verify_drafts.argtypes = [vp, vp, ll, vp, ll, vp, vp, vp, vp]
         _lib = L
     return _lib
 

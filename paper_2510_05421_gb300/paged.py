@@ -78,6 +78,33 @@ class _Workspaces:
 _workspaces = weakref.WeakValueDictionary()     # (device, head_dim): they go with their last cache
 
 
+def elsewhere(index: int, stream, keep, call, args, whose: str):
+    """`call(*args)` with device `index` current and on a stream of the caller's choice (None: the current one): there
+    it waits for what the current stream has in flight (the inputs may be among it), and no tensor's memory, of `args`,
+    of what is returned or of `keep`, is used again before both streams are done with it."""
+    with torch.cuda.device(index):
+        if stream is None:
+            return call(*args)
+        if stream.device != torch.device("cuda", index):
+            raise ValueError(f"stream: not on {whose}")
+        here = torch.cuda.current_stream(index)
+        if here.cuda_stream == stream.cuda_stream:
+            return call(*args)
+        alone = not torch.cuda.is_current_stream_capturing()
+        with torch.cuda.stream(stream):
+            # (a capture cannot wait for work outside it)
+            if not (alone and torch.cuda.is_current_stream_capturing()):
+                stream.wait_stream(here)
+            got = call(*args)
+        for t in (*keep, *args):
+            if isinstance(t, torch.Tensor):
+                t.record_stream(stream)
+        for t in got if isinstance(got, tuple) else (got,):
+            if t is not None:
+                t.record_stream(here)
+        return got
+
+
 def rotary_table(n_pos: int, rot_dim: int, theta: float = 10000.0, device="cuda") -> torch.Tensor:
     """[n_pos, rot_dim / 2, 2] f32 (cos, sin) of p * theta^(-2 i / rot_dim), from 64-bit angles."""
     inv = theta ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64) / rot_dim)
@@ -162,27 +189,8 @@ class PagedCache:
         """`call` where the cache's device is not current, or on a stream of the caller's choice: there it waits for
         what the current stream has in flight (the inputs may be among it), and no tensor's memory is used again
         before both streams are done with it."""
-        with torch.cuda.device(self._index):
-            if stream is None:
-                return call(*args)
-            if stream.device != self.device:
-                raise ValueError("stream: not on the cache's device")
-            here = torch.cuda.current_stream(self._index)
-            if here.cuda_stream == stream.cuda_stream:
-                return call(*args)
-            alone = not torch.cuda.is_current_stream_capturing()
-            with torch.cuda.stream(stream):
-                # (a capture cannot wait for work outside it)
-                if not (alone and torch.cuda.is_current_stream_capturing()):
-                    stream.wait_stream(here)
-                got = call(*args)
-            for t in (self.k, self.v, self.k_scale, self.v_scale, self.status_word, *args):
-                if isinstance(t, torch.Tensor):
-                    t.record_stream(stream)
-            for t in got if isinstance(got, tuple) else (got,):
-                if t is not None:
-                    t.record_stream(here)
-            return got
+        return elsewhere(self._index, stream, (self.k, self.v, self.k_scale, self.v_scale, self.status_word), call, args,
+                         "the cache's device")
 
     def _new(self, shape, dtype):
         """An output (the cache's device is current)."""

@@ -1,0 +1,220 @@
+"""token_probs against its definition in 64 bits: sizes, cuts, ties, masked rows, strides, settings, streams, graphs."""
+import numpy as np
+import pytest
+import torch
+
+from sampling_ref import probs as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def logits(n, V, seed, dtype=torch.float32, std=2.5):
+    g = np.random.default_rng(seed)
+    x = g.normal(0, std, (n, V))
+    at = g.integers(0, V, (n, 8))
+    np.put_along_axis(x, at, np.take_along_axis(x, at, 1) + g.uniform(2, 9, (n, 8)), 1)
+    return torch.tensor(x, dtype=torch.float32).to(dtype)
+
+
+def each(v, n):
+    return v.tolist() if isinstance(v, torch.Tensor) else [v] * n
+
+
+def check(x, T=1.0, k=0, p=1.0, out=None, flags=0, **kw):
+    """One call on rows x (device), every entry against the definition."""
+    from paper_2510_05421_gb300 import token_probs
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    got = token_probs(x, T, k, p, out=out, status=status, **kw)
+    torch.cuda.synchronize()
+    assert got.dtype == torch.float32 and got.shape == x.shape and (out is None or got is out)
+    assert int(status) == flags
+    host = got.cpu().double().numpy()
+    for r, (t, kk, pp) in enumerate(zip(each(T, len(x)), each(k, len(x)), each(p, len(x)))):
+        want, tol, border = ref(x[r].double().cpu().numpy(), np.float32(t), kk, float(np.float32(pp)))
+        # a decision this near its border is not this test's: the inputs are chosen so that there is none
+        assert border > 1e-10
+        # tokens that stay are above 0, the others 0 (one below 2^-140 of the sum may be lost: f32 ends at 2^-149)
+        assert (host[r] > 0)[want > 2.0 ** -140].all() and (host[r] == 0)[want == 0].all(), f"row {r}: tokens that stay"
+        assert (np.abs(host[r] - want) <= tol).all(), (r, np.abs(host[r] - want).max())
+    return got
+
+
+SIZES = [(1, 1), (3, 2), (2, 31), (1, 33), (4, 1000), (2, 1024), (3, 4099), (2, 16384), (2, 16385), (3, 32000), (2, 50001),
+         (1, 131072), (2, 200003), (1, 262144)]
+
+
+@pytest.mark.parametrize("n,V", SIZES)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_temperature(n, V, dtype):
+    check(logits(n, V, V, dtype).cuda(), 0.8)
+
+
+@pytest.mark.parametrize("n,V", SIZES)
+@pytest.mark.parametrize("k,p", [(0, 0.9), (40, 1.0), (300, 0.7), (1, 0.5), (0, 0.0)])
+def test_cuts(n, V, k, p):
+    check(logits(n, V, 7 * V + n).cuda(), 0.9, k, p)
+
+
+@pytest.mark.parametrize("std,T", [(0.01, 1.0), (30.0, 1.0), (2.0, 0.05), (2.0, 5.0), (1e-6, 1.0), (2.0, 1e-30), (2.0, 1e30)])
+@pytest.mark.parametrize("k,p", [(0, 1.0), (0, 0.8), (500, 0.95)])
+def test_flat_and_peaked_rows(std, T, k, p):
+    check(logits(2, 5003, 11, std=std).cuda(), T, k, p)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [7, 2048, 20011, 140000])
+@pytest.mark.parametrize("k,p", [(5, 1.0), (0, 0.3), (999, 0.301), (0, 1.0)])
+def test_equal_logits_stay_in_order_of_their_index(V, k, p, dtype):
+    x = torch.full((2, V), 1.5, dtype=dtype)
+    x[1, ::3] = 2.0
+    check(x.cuda(), 1.0, k, p)
+
+
+@pytest.mark.parametrize("k,p", [(50, 1.0), (0, 0.9), (20, 0.6)])
+def test_bf16_ties_at_the_cut(k, p):
+    x = logits(8, 32000, 5, torch.bfloat16)
+    top = x.float().sort(-1, descending=True).values
+    assert p < 1 or bool((top[:, k - 1] == top[:, k]).any())
+    check(x.cuda(), 0.7, k, p)
+
+
+def test_zeros_of_either_sign_are_equal():
+    x = torch.zeros(1, 300)
+    x[0, ::2] = -0.0
+    check(x.cuda(), 1.0, 7, 1.0)
+
+
+@pytest.mark.parametrize("low", [-float("inf"), -3.0e38, float(torch.finfo(torch.bfloat16).min)])
+@pytest.mark.parametrize("k,p", [(0, 1.0), (0, 0.9), (10, 1.0), (100, 0.99)])
+def test_masked_tokens(low, k, p):
+    """Grammar masks: most tokens at the lowest value; rows where one, three or none are left."""
+    g = torch.Generator().manual_seed(2)
+    x = logits(4, 3001, 3)
+    x = torch.where(torch.rand(x.shape, generator=g) < 0.9, low, x)
+    x[1] = low
+    x[1, 1234] = -2.0
+    x[2] = low
+    x[2, [0, 17, 3000]] = 0.25
+    x[3] = -float("inf")
+    got = check(x.cuda(), 1.3, k, p)
+    assert int(torch.count_nonzero(got[3])) == 0
+
+
+def test_logits_that_are_no_numbers():
+    x = logits(5, 2500, 4)
+    x[0, 7] = float("nan")
+    x[1] = float("nan")
+    x[2, [3, 99]] = float("inf")
+    for r in range(3):
+        check(x[r:r + 1].cuda(), 0.9, 40, 0.9, flags=1)
+    check(x.cuda(), 1.0, flags=1)
+    check(x[3:].cuda(), 1.0)
+
+
+def test_settings_of_each_row():
+    n, V = 12, 9001
+    x = logits(n, V, 6).cuda()
+    T = torch.tensor([0, 1, .5, 0, 2, 1, 1, .7, 1e-3, 1, 1, 3], dtype=torch.float32).cuda()
+    k = torch.tensor([0, 0, 5, 3, 0, 1, 9001, 99999, 0, 700, 2, 0], dtype=torch.int32).cuda()
+    p = torch.tensor([.5, .9, 1, 1, .95, .5, 1, .8, .5, 2, 0, .999], dtype=torch.float32).cuda()
+    check(x, T, k, p)
+    check(x, T)
+    check(x, 0.8, k)
+    check(x, 0.8, 0, p)
+    check(x.bfloat16(), T, 0, 0.9)
+
+
+def test_greedy_is_the_first_of_the_largest():
+    x = logits(6, 32000, 8)
+    x[2, [5, 77]] = 50.0
+    check(x.cuda(), 0.0)
+    check(x.bfloat16().cuda(), 0.0, 3, 0.5)
+
+
+def test_odd_settings_in_tensors():
+    """Negative temperatures are greedy, a negative top_k cuts nothing; NaN is flagged."""
+    x = logits(3, 1000, 9).cuda()
+    f = lambda *v: torch.tensor(v, dtype=torch.float32).cuda()
+    check(x, f(-1, 1, 1), torch.tensor([0, -5, 3], dtype=torch.int32).cuda(), f(1, 1, -2))
+    from paper_2510_05421_gb300 import token_probs
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    nan = float("nan")
+    got = token_probs(x, f(nan, 1, 1), 0, f(1, nan, 1), status=st)
+    assert int(st) == 1 and torch.equal(got, token_probs(x, f(0, 1, 1)))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("pad,shift", [(1, 0), (64, 0), (7, 3), (0, 1), (5, 2)])
+def test_strides(pad, shift, dtype):
+    """Rows that lie apart and start anywhere; what lies between them is not written."""
+    n, V = 5, 4001
+    buf = torch.full((n * (V + pad) + 8,), 1e30, dtype=dtype, device="cuda")
+    x = buf[shift:shift + n * (V + pad)].view(n, V + pad)[:, :V]
+    x.copy_(logits(n, V, 10).to(dtype))
+    out = torch.full((n, V + 2 * pad + 1), -7.0, device="cuda")
+    check(x, 0.9, 100, 0.9, out=out[:, pad:pad + V])
+    assert bool((out[:, :pad] == -7).all()) and bool((out[:, pad + V:] == -7).all())
+
+
+def test_rows_past_32_bits_of_offset():
+    V, ld = 1000, 1 << 30
+    buf = torch.empty(2 * ld + V, dtype=torch.bfloat16, device="cuda")
+    x = buf.as_strided((3, V), (ld, 1))
+    x.copy_(logits(3, V, 12).to(torch.bfloat16))
+    check(x, 1.0, 20)
+    del buf, x
+    buf = torch.empty(2 * ld + V, device="cuda")
+    check(logits(3, V, 13).cuda(), 1.0, out=buf.as_strided((3, V), (ld, 1)))
+
+
+def test_many_rows_and_none():
+    from paper_2510_05421_gb300 import token_probs
+    x = logits(1, 1031, 14).cuda()
+    one = token_probs(x, 0.8, 30, 0.9)
+    many = token_probs(x.expand(700, -1).contiguous(), 0.8, 30, 0.9)
+    assert torch.equal(many, one.expand(700, -1))                 # a row does not depend on how many there are
+    assert token_probs(x[:0], 0.8).shape == (0, 1031)
+    assert torch.equal(token_probs(x.expand(3, -1).contiguous()[:1], 0.8, 30, 0.9), one)
+
+
+def test_same_bits_every_time():
+    from paper_2510_05421_gb300 import token_probs
+    x = logits(64, 32000, 15, torch.bfloat16).cuda()
+    first = token_probs(x, 0.9, 0, 0.95)
+    for _ in range(5):
+        assert torch.equal(token_probs(x, 0.9, 0, 0.95), first)
+
+
+def test_stream_and_graph():
+    from paper_2510_05421_gb300 import token_probs
+    x = logits(9, 7001, 16).cuda()
+    want = token_probs(x, 0.9, 50, 0.9)
+    side = torch.cuda.Stream()
+    y = x.clone()                                   # in flight on the current stream
+    got = token_probs(y, 0.9, 50, 0.9, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
+    graph = torch.cuda.CUDAGraph()
+    T = torch.full((9,), 0.9, device="cuda")
+    with torch.cuda.graph(graph):
+        got = token_probs(y, T, 50, 0.9)
+    y.copy_(logits(9, 7001, 17).cuda())
+    T[4] = 0.0
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(got, token_probs(y, T, 50, 0.9))
+    assert torch.count_nonzero(got[4]) == 1
+
+
+def test_refusals():
+    from paper_2510_05421_gb300 import token_probs
+    x = logits(3, 100, 18).cuda()
+    f = torch.ones(3, device="cuda")
+    for bad in (dict(temperature=-1.0), dict(temperature=float("nan")), dict(top_k=-1), dict(top_p=-0.1),
+                dict(temperature=f[:2]), dict(temperature=f.double()), dict(top_k=f), dict(top_p=f.cpu()),
+                dict(out=x.bfloat16()), dict(out=x[:2]), dict(status=f), dict(top_p=torch.ones(6, device="cuda")[::2])):
+        with pytest.raises(ValueError):
+            token_probs(x, **bad)
+    for y in (x.half(), x[0], x.cpu(), x.t(), torch.empty(1, 262145, device="cuda"), torch.empty(2, 0, device="cuda")):
+        with pytest.raises(ValueError):
+            token_probs(y)
