@@ -8,7 +8,10 @@ using namespace dvi;
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 // Null, or an array of 4-byte elements.
 bool words_ok(const void* p) { return aligned(p, 4); }
-dvi_status launched(cudaError_t e) { return e == cudaSuccess ? DVI_OK : DVI_ERR_CUDA; }
+// The launchers refuse grids past 31 bits.
+dvi_status launched(cudaError_t e) {
+  return e == cudaSuccess ? DVI_OK : e == cudaErrorInvalidConfiguration ? DVI_ERR_CAPACITY : DVI_ERR_CUDA;
+}
 
 }  // namespace
 
