@@ -1,18 +1,18 @@
 // Probabilities of sampling from logits: temperature, top-k, top-p.
 //
-// A row's slices lie in the shared memory of one cluster's CTAs, so the row is
-// read once; the CTAs exchange (max, sum of exp2) once, which is all that a row
-// without cuts needs.
+// The CTAs of a cluster hold a row between them (in registers where nothing is cut
+// off, else in shared memory), so it is read once.  Without cuts they exchange (max,
+// sum of exp2) of every warp once.
 //
 // With tokens in the order of their logits (equal ones by index) and w =
 // exp((x - max) / T), the kept tokens are a prefix of the order; it ends at the
 // last token whose rank is below top_k and before which the sum of w is below
 // top_p of the whole.  That token is found in two steps: a histogram of counts or
-// of w over (max - x) / T gives its bin, and the bin's tokens are compared with
-// each other.  Sums of w are whole numbers, so they do not depend on the order of
-// the atomics, and every CTA of the cluster comes to the same end.  Where the bin
-// has too many tokens (logits that are nearly equal), the token's place in the
-// order, as a number, is found 11 bits at a time.
+// of w over (max - x) / T gives its bin, and the bin's tokens are sorted out among
+// themselves, by every CTA for itself.  Sums of w are whole numbers, so they do not
+// depend on the order of the atomics, and every CTA comes to the same end.  Where
+// the bin has too many tokens (logits that are nearly equal), the token's place in
+// the order, as a number, is found 10 bits at a time over the cluster.
 #include <cooperative_groups.h>
 
 #include "sample.cuh"
@@ -25,11 +25,13 @@ namespace cg = cooperative_groups;
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCtas = 8;                      // of a row
-constexpr int kBins = 2048;
-constexpr int kBinBits = 11;
+constexpr int kBins = 1024;
+constexpr int kBinBits = 10;
 constexpr int kPer = kBins / kThreads;
-constexpr float kBinsPerOctave = 64.f;           // of w: the last bin has what is below 2^-32
-constexpr int kList = 1024;                      // tokens of a bin that are compared with each other
+constexpr float kBinsPerOctave = 40.f;           // of w: the last bin has what is below 2^-25.6
+constexpr int kList = 1024;                      // tokens of a bin that are sorted out by each CTA
+constexpr int kListPer = kList / kThreads;
+constexpr int kFew = 64;                         // tokens that are compared with each other
 constexpr int kIndexBits = 18;                   // kMaxVocab
 
 // 2^(k / 32), k = -16 .. 16, as f32 pairs hi + lo.
@@ -120,14 +122,11 @@ struct Cuts {
 struct Small {
   float2 exp2_of[33];
   Slope slope;
-  float red[kWarps], sum[kWarps];
-  int first[kWarps];
-  unsigned long long part[kWarps];
-  // written by the CTAs of the cluster, by rank
-  float2 peer[kMaxCtas];                    // (max, sum)
-  int peer_first[kMaxCtas];
+  unsigned long long part[kWarps], least[kWarps], most[kWarps];
+  // written by the warps of the cluster: (max, sum), or (max, first token of it)
+  float2 peer[kMaxCtas * kWarps];
   unsigned long long peer_sum[2][kMaxCtas];
-  int n_list[2];
+  int n_list[2], n_kept;
   int found;
   unsigned long long excl, cut, kept;
 };
@@ -141,6 +140,9 @@ struct RowState {
   Slope c;
   __device__ __forceinline__ unsigned long long place(float v, int i) const {
     return (static_cast<unsigned long long>(top - ord(v)) << kIndexBits) | static_cast<unsigned>(first + i);
+  }
+  __device__ __forceinline__ float logit(unsigned long long place) const {
+    return from_ord(top - static_cast<uint32_t>(place >> kIndexBits));
   }
   __device__ __forceinline__ int bin(float v) const {
     const float t = __fmul_rn(__fmul_rn(__fsub_rn(m, v), c.hi), kBinsPerOctave);
@@ -157,19 +159,20 @@ __device__ __forceinline__ void cluster_barrier(int n_ctas) {
   }
 }
 
-// Sum over the cluster; `slot` is of its own for each call.
-__device__ unsigned long long cluster_sum(unsigned long long v, int slot, int n_ctas, Small& s) {
-  cg::cluster_group cluster = cg::this_cluster();
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+// Gives the sum over this CTA to all of the cluster: peer_sum[slot] is complete behind
+// the next cluster_barrier.  `slot` is of its own for each call.
+__device__ __forceinline__ void give_sum(unsigned long long v, int slot, int rank, int n_ctas, Small& s) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   v = warp_sum_u64(v);
   if (lane == 0) s.part[warp] = v;
   __syncthreads();
   if (warp == 0) {
     v = warp_sum_u64(lane < kWarps ? s.part[lane] : 0);
-    if (lane < n_ctas) *cluster.map_shared_rank(&s.peer_sum[slot][cluster.block_rank()], lane) = v;
+    if (lane < n_ctas) *cg::this_cluster().map_shared_rank(&s.peer_sum[slot][rank], lane) = v;
   }
-  cluster_barrier(n_ctas);
-  v = 0;
+}
+__device__ __forceinline__ unsigned long long given_sum(int slot, int n_ctas, const Small& s) {
+  unsigned long long v = 0;
   for (int r = 0; r < n_ctas; ++r) v += s.peer_sum[slot][r];
   return v;
 }
@@ -181,20 +184,24 @@ __device__ __forceinline__ void add_to_bin(Cuts& h, int bin, unsigned long long 
   if (up) atomicAdd(&h.hi[bin], up);
 }
 
-// The first bin up to which the cluster's sums (and `before`) reach target: its number
-// (-1 if none does) and the sum before it.  Every CTA's bins are complete when it is called.
-__device__ int find_bin(unsigned long long before, unsigned long long target, int n_ctas, Cuts& h, Small& s,
+__device__ __forceinline__ void clear_bins(Cuts& h) {
+  for (int i = threadIdx.x; i < kBins; i += kThreads) h.lo[i] = 0, h.hi[i] = 0;
+  __syncthreads();
+}
+
+// The first bin up to which the sums of CTAs r0 .. r1 - 1 (and `before`) reach target: its
+// number (-1 if none does) and the sum before it.  Their bins are complete when it is called.
+__device__ int find_bin(unsigned long long before, unsigned long long target, int r0, int r1, Cuts& h, Small& s,
                         unsigned long long* excl) {
   cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   unsigned long long v[kPer] = {}, sum = 0;
-  for (int r = 0; r < n_ctas; ++r) {
-    const uint4 lo = reinterpret_cast<const uint4*>(cluster.map_shared_rank(h.lo, r))[tid];
-    const uint4 hi = reinterpret_cast<const uint4*>(cluster.map_shared_rank(h.hi, r))[tid];
+  static_assert(kPer == 2, "a pair of bins a thread");
+  for (int r = r0; r < r1; ++r) {
+    const uint2 lo = reinterpret_cast<const uint2*>(cluster.map_shared_rank(h.lo, r))[tid];
+    const uint2 hi = reinterpret_cast<const uint2*>(cluster.map_shared_rank(h.hi, r))[tid];
     v[0] += (static_cast<unsigned long long>(hi.x) << 32) + lo.x;
     v[1] += (static_cast<unsigned long long>(hi.y) << 32) + lo.y;
-    v[2] += (static_cast<unsigned long long>(hi.z) << 32) + lo.z;
-    v[3] += (static_cast<unsigned long long>(hi.w) << 32) + lo.w;
   }
 #pragma unroll
   for (int j = 0; j < kPer; ++j) sum += v[j];
@@ -219,96 +226,58 @@ __device__ int find_bin(unsigned long long before, unsigned long long target, in
   return s.found;
 }
 
-// The place of the last kept token: before it the counts (MASS: the masses), over tokens
-// up to the place `upto`, sum to less than target.  *kept: the sum up to it.  ~0 if the
-// whole sum is less than target.  MASS: tokens below `least` are known to be cut.
+// Of the n tokens in h.key (with h.mass): the last kept one, where `before` is the sum before
+// them all.  By every CTA for itself.
 template <bool MASS>
-__device__ unsigned long long last_kept(const RowState& row, unsigned long long target, unsigned long long upto,
-                                        float least, int n_ctas, Cuts& h, Small& s, unsigned long long* kept) {
-  cg::cluster_group cluster = cg::this_cluster();
-  const int tid = threadIdx.x;
-  auto zero = [&] {
-    for (int i = tid; i < kBins; i += kThreads) h.lo[i] = 0, h.hi[i] = 0;
+__device__ unsigned long long last_of_list(int n, unsigned long long before, unsigned long long target, int rank,
+                                           Cuts& h, Small& s, unsigned long long* kept) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  while (n > kFew) {
+    // bins of equal width from the first of their places to the last
+    unsigned long long key[kListPer], m[kListPer], least = ~0ull, most = 0;
+#pragma unroll
+    for (int j = 0; j < kListPer; ++j) {
+      const int i = tid + j * kThreads;
+      key[j] = i < n ? h.key[i] : ~0ull;
+      m[j] = i < n && MASS ? h.mass[i] : 1;
+      if (i < n) least = min(least, key[j]), most = max(most, key[j]);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      least = min(least, __shfl_xor_sync(0xffffffffu, least, o));
+      most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+    }
+    if (lane == 0) s.least[warp] = least, s.most[warp] = most;
+    if (tid == 0) s.n_kept = 0;
+    clear_bins(h);
+    for (int w = 0; w < kWarps; ++w) least = min(least, s.least[w]), most = max(most, s.most[w]);
+    const int bits = 64 - __clzll(most - least), shift = bits > kBinBits ? bits - kBinBits : 0;
+#pragma unroll
+    for (int j = 0; j < kListPer; ++j)
+      if (key[j] != ~0ull) add_to_bin(h, static_cast<int>((key[j] - least) >> shift), m[j]);
     __syncthreads();
-  };
-  auto counts = [&](float x, int i) {
-    if (x == -INFINITY || (MASS && weight(x, row.m, row.c) < least)) return false;
-    return upto == ~0ull || row.place(x, i) <= upto;
-  };
-  zero();
-  for (int i = tid; i < row.n; i += kThreads) {
-    const float x = row.x[i];
-    if (!counts(x, i)) continue;
-    if (MASS)
-      add_to_bin(h, row.bin(x), mass(x, row.m, row.c, s.exp2_of));
-    else
-      atomicAdd(&h.lo[row.bin(x)], 1u);
-  }
-  cluster_barrier(n_ctas);
-  unsigned long long before;
-  const int bin = find_bin(0, target, n_ctas, h, s, &before);
-  if (bin < 0) return ~0ull;
-  int& mine = s.n_list[MASS];
-  for (int i = tid; i < row.n; i += kThreads) {
-    const float x = row.x[i];
-    if (!counts(x, i) || row.bin(x) != bin) continue;
-    const int at = atomicAdd(&mine, 1);
-    if (at < kList) h.list[at] = row.place(x, i);
-  }
-  cluster_barrier(n_ctas);
-  int n = 0;
-  for (int r = 0; r < n_ctas; ++r) n += *cluster.map_shared_rank(&mine, r);
-  if (n <= kList) {
-    for (int r = 0, at = 0; r < n_ctas; ++r) {
-      const int there = *cluster.map_shared_rank(&mine, r);
-      const unsigned long long* list = cluster.map_shared_rank(h.list, r);
-      for (int i = tid; i < there; i += kThreads) {
-        const unsigned long long p = list[i];
-        h.key[at + i] = p;
-        if (MASS) h.mass[at + i] = mass(from_ord(row.top - static_cast<uint32_t>(p >> kIndexBits)), row.m, row.c, s.exp2_of);
-      }
-      at += there;
+    const int bin = find_bin(before, target, rank, rank + 1, h, s, &before);
+#pragma unroll
+    for (int j = 0; j < kListPer; ++j) {
+      if (key[j] == ~0ull || static_cast<int>((key[j] - least) >> shift) != bin) continue;
+      const int at = atomicAdd(&s.n_kept, 1);
+      h.key[at] = key[j];
+      if (MASS) h.mass[at] = m[j];
     }
     __syncthreads();
-    for (int i = tid; i < n; i += kThreads) {
-      const unsigned long long p = h.key[i], v = MASS ? h.mass[i] : 1;
-      unsigned long long sum = before;
-      for (int j = 0; j < n; ++j)
-        if (h.key[j] < p) sum += MASS ? h.mass[j] : 1;
-      if (sum < target && sum + v >= target) s.cut = p, s.kept = sum + v;
-    }
+    n = s.n_kept;
     __syncthreads();
-    *kept = s.kept;
-    return s.cut;
   }
-  unsigned long long lo = 0;
-  before = 0;
-  for (int shift = 32 + kIndexBits - kBinBits;; shift = shift > kBinBits ? shift - kBinBits : 0) {
-    zero();
-    for (int i = tid; i < row.n; i += kThreads) {
-      const float x = row.x[i];
-      if (!counts(x, i)) continue;
-      const unsigned long long p = row.place(x, i);
-      if (p < lo || ((p - lo) >> shift) >= kBins) continue;
-      add_to_bin(h, static_cast<int>((p - lo) >> shift), MASS ? mass(x, row.m, row.c, s.exp2_of) : 1ull);
-    }
-    cluster_barrier(n_ctas);
-    unsigned long long excl;
-    const int b = find_bin(before, target, n_ctas, h, s, &excl);   // (found: the sums are those of the first bins)
-    lo += static_cast<unsigned long long>(b) << shift;
-    before = excl;
-    if (shift == 0) {
-      // one token a bin
-      unsigned long long v = 0;
-      for (int r = 0; r < n_ctas; ++r)
-        v += (static_cast<unsigned long long>(cluster.map_shared_rank(h.hi, r)[b]) << 32) +
-             cluster.map_shared_rank(h.lo, r)[b];
-      *kept = before + v;
-      cluster_barrier(n_ctas);
-      return lo;
-    }
-    cluster_barrier(n_ctas);   // before the bins are cleared
+  if (tid < n) {
+    const unsigned long long p = h.key[tid], v = MASS ? h.mass[tid] : 1;
+    unsigned long long sum = before;
+    for (int j = 0; j < n; ++j)
+      if (h.key[j] < p) sum += MASS ? h.mass[j] : 1;
+    if (sum < target && sum + v >= target) s.cut = p, s.kept = sum + v;
   }
+  __syncthreads();
+  *kept = s.kept;
+  return s.cut;
 }
 
 // ceil(p S) for p in [0, 1), at least 1.
@@ -326,40 +295,235 @@ __device__ __forceinline__ unsigned long long share_of(float p, unsigned long lo
   return t ? t : 1;
 }
 
-template <typename T, bool CUTS>
-__global__ void __launch_bounds__(kThreads, 2) token_probs_kernel(TokenProbsArgs a, int n_ctas, int slice) {
-  extern __shared__ __align__(16) unsigned char dynamic[];
-  __shared__ Small s;
-  float* x = reinterpret_cast<float*>(dynamic);
-  Cuts& h = *reinterpret_cast<Cuts*>(dynamic + (static_cast<size_t>(slice) * sizeof(float) + 15) / 16 * 16);
+// The place of the last kept token among those up to the place `upto`: before it the counts
+// sum to less than top_k, or (MASS) the masses to less than top_p of all.  *kept: the sum up
+// to it (that of all where it is ~0: all are kept).  Tokens below `least` are known to be cut.
+// mine: the largest of the thread's own logits.
+template <bool MASS>
+__device__ unsigned long long last_kept(const RowState& row, int top_k, float top_p, unsigned long long upto,
+                                        float least, float mine, int rank, int n_ctas, Cuts& h, Small& s,
+                                        unsigned long long* kept) {
   cg::cluster_group cluster = cg::this_cluster();
+  const int tid = threadIdx.x;
+  unsigned long long before;
+  clear_bins(h);
+  int most = kBins - 1;
+  if (!MASS && top_k <= kThreads) {
+    // top_k threads' largest logits are in the first bins: no token behind these is kept
+    if (mine > -INFINITY) atomicAdd(&h.lo[row.bin(mine)], 1u);
+    __syncthreads();
+    const int b = find_bin(0, top_k, rank, rank + 1, h, s, &before);
+    if (b >= 0) most = b;
+    clear_bins(h);
+  }
+  auto counts = [&](float x, int i) { return x > -INFINITY && x >= least && (upto == ~0ull || row.place(x, i) <= upto); };
+  if (MASS) {
+    unsigned long long all = 0;
+    for (int i = tid; i < row.n; i += kThreads) {
+      const float x = row.x[i];
+      if (upto != ~0ull && row.place(x, i) > upto) continue;
+      const unsigned long long m = mass(x, row.m, row.c, s.exp2_of);
+      all += m;
+      if (x >= least && m) add_to_bin(h, row.bin(x), m);
+    }
+    give_sum(all, 1, rank, n_ctas, s);
+  } else {
+    for (int i = tid; i < row.n; i += kThreads) {
+      const float x = row.x[i];
+      if (!(x > -INFINITY)) continue;
+      const int bin = row.bin(x);
+      if (bin <= most) atomicAdd(&h.lo[bin], 1u);
+    }
+  }
+  cluster_barrier(n_ctas);
+  unsigned long long target = top_k;
+  if (MASS) {
+    *kept = given_sum(1, n_ctas, s);
+    target = share_of(top_p, *kept);
+  }
+  const int bin = find_bin(0, target, 0, n_ctas, h, s, &before);
+  if (bin < 0) return ~0ull;
+  int& found = s.n_list[MASS];
+  for (int i = tid; i < row.n; i += kThreads) {
+    const float x = row.x[i];
+    if (row.bin(x) != bin || !counts(x, i)) continue;
+    const int at = atomicAdd(&found, 1);
+    if (at < kList) h.list[at] = row.place(x, i);
+  }
+  cluster_barrier(n_ctas);
+  int n = 0;
+  for (int r = 0; r < n_ctas; ++r) n += *cluster.map_shared_rank(&found, r);
+  if (n <= kList) {
+    for (int r = 0, at = 0; r < n_ctas; ++r) {
+      const int there = *cluster.map_shared_rank(&found, r);
+      const unsigned long long* list = cluster.map_shared_rank(h.list, r);
+      for (int i = tid; i < there; i += kThreads) {
+        const unsigned long long p = list[i];
+        h.key[at + i] = p;
+        if (MASS) h.mass[at + i] = mass(row.logit(p), row.m, row.c, s.exp2_of);
+      }
+      at += there;
+    }
+    __syncthreads();
+    return last_of_list<MASS>(n, before, target, rank, h, s, kept);
+  }
+  unsigned long long lo = 0;
+  before = 0;
+  for (int shift = 32 + kIndexBits - kBinBits;; shift = shift > kBinBits ? shift - kBinBits : 0) {
+    clear_bins(h);
+    for (int i = tid; i < row.n; i += kThreads) {
+      const float x = row.x[i];
+      if (!counts(x, i)) continue;
+      const unsigned long long p = row.place(x, i);
+      if (p < lo || ((p - lo) >> shift) >= kBins) continue;
+      add_to_bin(h, static_cast<int>((p - lo) >> shift), MASS ? mass(x, row.m, row.c, s.exp2_of) : 1ull);
+    }
+    cluster_barrier(n_ctas);
+    const int b = find_bin(before, target, 0, n_ctas, h, s, &before);   // (found: the sums are those of the first bins)
+    lo += static_cast<unsigned long long>(b) << shift;
+    if (shift == 0) {
+      // one token a bin
+      unsigned long long v = 0;
+      for (int r = 0; r < n_ctas; ++r)
+        v += (static_cast<unsigned long long>(cluster.map_shared_rank(h.hi, r)[b]) << 32) +
+             cluster.map_shared_rank(h.lo, r)[b];
+      *kept = before + v;
+      cluster_barrier(n_ctas);
+      return lo;
+    }
+    cluster_barrier(n_ctas);   // before the bins are cleared
+  }
+}
+
+// The settings of row r, as they count.
+struct Settings {
+  float temperature, top_p;   // 0: greedy; 1: no cut
+  int top_k;                  // 0: no cut
+  bool bad;
+  __device__ __forceinline__ Settings(const TokenProbsArgs& a, int r) {
+    temperature = a.temperature ? a.temperature[r] : a.temperature_all;
+    top_p = a.top_p ? a.top_p[r] : a.top_p_all;
+    top_k = a.top_k ? a.top_k[r] : a.top_k_all;
+    bad = temperature != temperature || top_p != top_p;
+    if (!(temperature > 0.f)) temperature = 0.f;
+    top_p = top_p < 1.f ? fmaxf(top_p, 0.f) : 1.f;
+    if (top_k < 0 || top_k >= a.vocab) top_k = 0;
+  }
+};
+
+// What all warps of the cluster have given: the row's maximum and its sum of w (T > 0) or its
+// first largest token (T = 0).
+__device__ __forceinline__ void join(const Small& s, int n_ctas, bool greedy, Slope c, float* m, float* sum, int* hot) {
+  const int lane = threadIdx.x & 31;
+  float top = -INFINITY;
+  for (int i = lane; i < n_ctas * kWarps; i += 32) top = fmaxf(top, s.peer[i].x);
+  top = warp_max(top);
+  float all = 0.f;
+  int first = 0x7fffffff;
+  for (int i = lane; i < n_ctas * kWarps; i += 32) {
+    const float2 p = s.peer[i];
+    if (greedy) {
+      if (p.x == top) first = min(first, __float_as_int(p.y));
+    } else if (p.x > -INFINITY) {
+      all += p.y * weight(p.x, top, c);
+    }
+  }
+  *m = top;
+  *sum = warp_sum(all);
+  *hot = __reduce_min_sync(0xffffffffu, first);
+}
+
+// Rows without cuts: NV logits a thread, in registers.
+template <typename T, int NV>
+__global__ void __launch_bounds__(kThreads, NV <= 16 ? 3 : NV <= 32 ? 2 : 1)
+    token_probs_kernel(TokenProbsArgs a, int n_ctas, int slice) {
+  __shared__ Small s;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int rank = n_ctas > 1 ? static_cast<int>(cluster.block_rank()) : 0;
+  const int rank = n_ctas > 1 ? static_cast<int>(cg::this_cluster().block_rank()) : 0;
   const int r = blockIdx.x / n_ctas;
   const int first = min(rank * slice, a.vocab), n = min(slice, a.vocab - first);
   if (n_ctas > 1) cluster_arrive_release();              // (waited for below: no CTA writes to one that is not there)
   griddep_wait();
   const T* in = static_cast<const T*>(a.x) + r * a.ld + first;
   float* out = a.out + r * a.ld_out + first;
-  float temp = a.temperature ? a.temperature[r] : a.temperature_all;
-  float top_p = 1.f;
-  int top_k = 0;
-  if (CUTS) {
-    top_p = a.top_p ? a.top_p[r] : a.top_p_all;
-    const int k = a.top_k ? a.top_k[r] : a.top_k_all;
-    top_k = k > 0 && k < a.vocab ? k : 0;
+  float v[NV];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int i = j * kThreads + tid;
+    v[j] = i < n ? DT<T>::ld(in + i) : -INFINITY;
   }
-  bool bad = temp != temp || top_p != top_p;
-  if (!(temp > 0.f)) temp = 0.f;
-  top_p = top_p != top_p ? 1.f : fmaxf(top_p, 0.f);
+  const Settings set(a, r);
+  const bool greedy = set.temperature == 0.f;
+  if (tid == 0) s.slope = slope_of(set.temperature);
+  bool bad = set.bad;
+  float m = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    bad |= !(v[j] < INFINITY);
+    v[j] = clean(v[j]);
+    m = fmaxf(m, v[j]);
+  }
+  m = warp_max(m);
+  if (__syncthreads_or(bad) && tid == 0) flag_status(a.status, DVI_DEV_NONFINITE);
+  const Slope c = s.slope;
+  float2 mine = make_float2(m, 0.f);
+  if (greedy) {
+    int at = 0x7fffffff;
+#pragma unroll
+    for (int j = NV - 1; j >= 0; --j)
+      if (v[j] == m) at = first + j * kThreads + tid;
+    mine.y = __int_as_float(__reduce_min_sync(0xffffffffu, at));
+  } else if (m > -INFINITY) {
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < NV; ++j) sum[j & 3] += v[j] = weight(v[j], m, c);
+    mine.y = warp_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
+  }
+  if (n_ctas > 1) {
+    cluster_wait_acquire();
+    if (lane < n_ctas) *cg::this_cluster().map_shared_rank(&s.peer[rank * kWarps + warp], lane) = mine;
+  } else if (lane == 0) {
+    s.peer[warp] = mine;
+  }
+  cluster_barrier(n_ctas);
+  float top, sum;
+  int hot;
+  join(s, n_ctas, greedy, c, &top, &sum, &hot);
+  const float scale = !greedy && m > -INFINITY ? weight(m, top, c) / sum : 0.f;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int i = j * kThreads + tid;
+    if (i < n) out[i] = scale > 0.f ? v[j] * scale : greedy && top > -INFINITY && first + i == hot ? 1.f : 0.f;
+  }
+}
+
+// Rows with cuts: a slice in shared memory.
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbsArgs a, int n_ctas, int slice) {
+  extern __shared__ __align__(16) unsigned char dynamic[];
+  __shared__ Small s;
+  Cuts& h = *reinterpret_cast<Cuts*>(dynamic);
+  float* x = reinterpret_cast<float*>(dynamic + sizeof(Cuts));
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = n_ctas > 1 ? static_cast<int>(cg::this_cluster().block_rank()) : 0;
+  const int r = blockIdx.x / n_ctas;
+  const int first = min(rank * slice, a.vocab), n = min(slice, a.vocab - first);
+  if (n_ctas > 1) cluster_arrive_release();
+  griddep_wait();
+  const T* in = static_cast<const T*>(a.x) + r * a.ld + first;
+  float* out = a.out + r * a.ld_out + first;
+  const Settings set(a, r);
+  const bool greedy = set.temperature == 0.f;
+  bool bad = set.bad;
   if (tid == 0) {
-    s.slope = slope_of(temp);
+    s.slope = slope_of(set.temperature);
     s.n_list[0] = s.n_list[1] = 0;
   }
-  if (CUTS && tid >= 64 && tid < 64 + 33) s.exp2_of[tid - 64] = kExp2[tid - 64];
+  if (tid >= 64 && tid < 64 + 33) s.exp2_of[tid - 64] = kExp2[tid - 64];
 
   constexpr int kFly = 16;
-  float m = -INFINITY;
+  float own = -INFINITY;
+  int at = 0x7fffffff;
   for (int i0 = 0; i0 < n; i0 += kFly * kThreads) {
     float v[kFly];
 #pragma unroll
@@ -372,118 +536,73 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_kernel(TokenProbsArgs
       const int i = i0 + j * kThreads + tid;
       bad |= !(v[j] < INFINITY);
       v[j] = clean(v[j]);
-      m = fmaxf(m, v[j]);
+      if (v[j] > own) own = v[j], at = first + i;
       if (i < n) x[i] = v[j];
     }
   }
-  m = warp_max(m);
-  if (lane == 0) s.red[warp] = m;
+  const float m = warp_max(own);
   if (__syncthreads_or(bad) && tid == 0) flag_status(a.status, DVI_DEV_NONFINITE);
-  m = warp_max(lane < kWarps ? s.red[lane] : -INFINITY);
   const Slope c = s.slope;
-
-  // this CTA's sum of w (to its own maximum) or, for a greedy row, its first largest token
-  float sum = 0.f;
-  int at = 0x7fffffff;
-  if (temp > 0.f) {
-    if (m > -INFINITY) {
-      for (int i = tid; i < n; i += kThreads) {
-        const float w = weight(x[i], m, c);
-        sum += w;
-        if (!CUTS) x[i] = w;
-      }
-    }
-    sum = warp_sum(sum);
-    if (lane == 0) s.sum[warp] = sum;
-  } else {
-    for (int i = n - 1 - tid; i >= 0; i -= kThreads)
-      if (x[i] == m) at = i;
-    at = __reduce_min_sync(0xffffffffu, at);
-    if (lane == 0) s.first[warp] = at;
-  }
-  __syncthreads();
-  if (warp == 0) {
-    if (n_ctas > 1) cluster_wait_acquire();
-    sum = warp_sum(lane < kWarps && temp > 0.f ? s.sum[lane] : 0.f);
-    at = __reduce_min_sync(0xffffffffu, lane < kWarps && !(temp > 0.f) ? s.first[lane] : 0x7fffffff);
-    if (lane < n_ctas) {
-      float2* p = n_ctas > 1 ? cluster.map_shared_rank(&s.peer[rank], lane) : &s.peer[0];
-      int* f = n_ctas > 1 ? cluster.map_shared_rank(&s.peer_first[rank], lane) : &s.peer_first[0];
-      *p = make_float2(m, sum);
-      *f = at;
-    }
-  } else if (n_ctas > 1) {
+  // (of the sum of w the largest logits of the threads: a lower bound is enough)
+  float2 mine = make_float2(m, 0.f);
+  if (greedy)
+    mine.y = __int_as_float(__reduce_min_sync(0xffffffffu, own == m ? at : 0x7fffffff));
+  else if (m > -INFINITY)
+    mine.y = warp_sum(weight(own, m, c));
+  if (n_ctas > 1) {
     cluster_wait_acquire();
+    if (lane < n_ctas) *cg::this_cluster().map_shared_rank(&s.peer[rank * kWarps + warp], lane) = mine;
+  } else if (lane == 0) {
+    s.peer[warp] = mine;
   }
   cluster_barrier(n_ctas);
-  const float own = m;
-  for (int q = 0; q < n_ctas; ++q) m = fmaxf(m, s.peer[q].x);
-
-  if (!(temp > 0.f) || m == -INFINITY) {
-    int q = 0;
-    while (s.peer[q].x != m) ++q;
-    const int hot = m > -INFINITY && q == rank ? s.peer_first[q] : -1;
-    for (int i = tid; i < n; i += kThreads) out[i] = i == hot ? 1.f : 0.f;
+  float top, sum;
+  int hot;
+  join(s, n_ctas, greedy, c, &top, &sum, &hot);
+  if (greedy || top == -INFINITY) {
+    for (int i = tid; i < n; i += kThreads) out[i] = top > -INFINITY && first + i == hot ? 1.f : 0.f;
     return;
   }
-  sum = 0.f;
-  for (int q = 0; q < n_ctas; ++q)
-    if (s.peer[q].x > -INFINITY) sum += s.peer[q].y * weight(s.peer[q].x, m, c);
-  if (!CUTS) {
-    const float scale = own > -INFINITY ? weight(own, m, c) / sum : 0.f;
-    for (int i = tid; i < n; i += kThreads) out[i] = own > -INFINITY ? x[i] * scale : 0.f;
-    return;
-  }
-  unsigned long long upto = ~0ull;
-  float inv = 1.f / sum;
-  const RowState row = {x, first, n, m, ord(m), c};
-  if (top_k || top_p < 1.f) {
-    unsigned long long kept = 0, all = 0;
-    if (top_k) upto = last_kept<false>(row, top_k, ~0ull, 0.f, n_ctas, h, s, &kept);
+  const RowState row = {x, first, n, top, ord(top), c};
+  unsigned long long upto = ~0ull, kept = 0;
+  if (set.top_k)
+    upto = last_kept<false>(row, set.top_k, 1.f, ~0ull, -INFINITY, own, rank, n_ctas, h, s, &kept);
+  if (set.top_p < 1.f) {
+    // tokens below (1 - p) S / V sum to less than what may be cut, so the last kept one is
+    // above that (half of it, for the sum's rounding)
+    float least = -INFINITY;
+    if (upto == ~0ull)
+      least = top + log2f(0.5f * (1.f - set.top_p) * sum / static_cast<float>(a.vocab)) / c.hi * 1.0001f;
+    const unsigned long long e = last_kept<true>(row, 0, set.top_p, upto, least, own, rank, n_ctas, h, s, &kept);
+    if (e != ~0ull) upto = e;
+  } else {
+    unsigned long long all = 0;
     for (int i = tid; i < n; i += kThreads)
-      if (upto == ~0ull || row.place(x[i], i) <= upto) all += mass(x[i], m, c, s.exp2_of);
-    kept = all = cluster_sum(all, 0, n_ctas, s);
-    if (top_p < 1.f) {
-      // tokens below (1 - p) S / V sum to less than the rest may, so the last kept one is
-      // above that (S by the f32 sum is not less than what top_k leaves; half of it, for
-      // its rounding)
-      const float least = upto == ~0ull ? 0.5f * (1.f - top_p) * sum / static_cast<float>(a.vocab) : 0.f;
-      const unsigned long long e = last_kept<true>(row, share_of(top_p, all), upto, least, n_ctas, h, s, &kept);
-      if (e != ~0ull) upto = e;
-      else kept = all;
-    }
-    inv = 1.f / (__ull2float_rn(kept) * 0x1p-44f);
+      if (upto == ~0ull || row.place(x[i], i) <= upto) all += mass(x[i], top, c, s.exp2_of);
+    give_sum(all, 0, rank, n_ctas, s);
+    cluster_barrier(n_ctas);
+    kept = given_sum(0, n_ctas, s);
   }
-  const float x_cut = upto == ~0ull ? -INFINITY : from_ord(row.top - static_cast<uint32_t>(upto >> kIndexBits));
+  if (n_ctas > 1) cluster_arrive_release();   // nothing of the others is read from here on
+  const float inv = 1.f / (__ull2float_rn(kept) * 0x1p-44f);
+  const float x_cut = upto == ~0ull ? -INFINITY : row.logit(upto);
   const int i_cut = static_cast<int>(upto & ((1u << kIndexBits) - 1)) - first;
   for (int i = tid; i < n; i += kThreads) {
     const float v = x[i];
     const bool in_it = v > x_cut || (v == x_cut && i <= i_cut && v > -INFINITY);
-    out[i] = in_it ? weight(v, m, c) * inv : 0.f;
+    out[i] = in_it ? weight(v, top, c) * inv : 0.f;
   }
-  // no CTA leaves while another may read what it found
-  if (top_k || top_p < 1.f) cluster_barrier(n_ctas);
+  if (n_ctas > 1) cluster_wait_acquire();     // (and no CTA leaves while another may read what it found)
 }
 
-constexpr int kSlice = 16384;   // logits of a CTA where its row may have up to kMaxCtas: two CTAs an SM
-
-template <typename T, bool CUTS>
-cudaError_t launch(const TokenProbsArgs& a, cudaStream_t s) {
-  auto kern = token_probs_kernel<T, CUTS>;
-  static PerDevice per_device;
-  per_device.once([&] {
-    cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                         kMaxVocab / kMaxCtas * static_cast<int>(sizeof(float)) + static_cast<int>(sizeof(Cuts)));
-  });
-  int ctas = 1;
-  while (ctas < kMaxCtas && (ctas * kSlice < a.vocab || (static_cast<int64_t>(a.n_rows) * ctas < 152 && a.vocab / ctas > 4096)))
-    ctas *= 2;
+template <typename K>
+cudaError_t launch(K kern, const TokenProbsArgs& a, int ctas, size_t smem, cudaStream_t s) {
   if (static_cast<int64_t>(a.n_rows) * ctas > 0x7fffffffll) return cudaErrorInvalidConfiguration;
   const int slice = (a.vocab + ctas - 1) / ctas;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(a.n_rows) * ctas);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = (slice * sizeof(float) + 15) / 16 * 16 + (CUTS ? sizeof(Cuts) : 0);
+  cfg.dynamicSmemBytes = smem ? smem + slice * sizeof(float) : 0;
   cfg.stream = s;
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -497,12 +616,37 @@ cudaError_t launch(const TokenProbsArgs& a, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, kern, a, ctas, slice);
 }
 
+template <typename T>
+cudaError_t launch_plain(const TokenProbsArgs& a, cudaStream_t s) {
+  int nv = 16;
+  while (nv * kThreads * kMaxCtas < a.vocab) nv *= 2;
+  int ctas = 1;
+  while (ctas * nv * kThreads < a.vocab) ctas *= 2;
+  if (nv == 16) return launch(token_probs_kernel<T, 16>, a, ctas, 0, s);
+  return nv == 32 ? launch(token_probs_kernel<T, 32>, a, ctas, 0, s) : launch(token_probs_kernel<T, 64>, a, ctas, 0, s);
+}
+
+constexpr int kSlice = 16384;   // logits of a CTA where its row may have up to kMaxCtas: two CTAs an SM
+
+template <typename T>
+cudaError_t launch_cut(const TokenProbsArgs& a, cudaStream_t s) {
+  static PerDevice per_device;
+  per_device.once([&] {
+    cudaFuncSetAttribute(token_probs_cut_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                         kMaxVocab / kMaxCtas * static_cast<int>(sizeof(float)) + static_cast<int>(sizeof(Cuts)));
+  });
+  int ctas = 1;
+  while (ctas < kMaxCtas && (ctas * kSlice < a.vocab || (static_cast<int64_t>(a.n_rows) * ctas < 152 && a.vocab / ctas > 4096)))
+    ctas *= 2;
+  return launch(token_probs_cut_kernel<T>, a, ctas, sizeof(Cuts), s);
+}
+
 }  // namespace
 
 cudaError_t launch_token_probs(const TokenProbsArgs& a, int dtype, cudaStream_t s) {
   const bool cuts = a.top_k || a.top_p || a.top_p_all < 1.f || (a.top_k_all > 0 && a.top_k_all < a.vocab);
-  if (dtype == DVI_BF16) return cuts ? launch<__nv_bfloat16, true>(a, s) : launch<__nv_bfloat16, false>(a, s);
-  return cuts ? launch<float, true>(a, s) : launch<float, false>(a, s);
+  if (dtype == DVI_BF16) return cuts ? launch_cut<__nv_bfloat16>(a, s) : launch_plain<__nv_bfloat16>(a, s);
+  return cuts ? launch_cut<float>(a, s) : launch_plain<float>(a, s);
 }
 
 }  // namespace dvi

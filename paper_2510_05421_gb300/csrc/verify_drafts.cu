@@ -1,12 +1,13 @@
 // Verification of drafted tokens from given uniform numbers.
 //
-// A cluster of CTAs takes a sequence: its first warps look at the drafts (a few
-// words each), then all sum r = max(p - q, 0) over their parts of the row at
-// which the drafts end, and the first CTA finds the token by descending to the
-// part, the warp's share of it and the token at which the running sum passes u
-// times the whole.  Which token that is does not depend on rounding but where u
-// lies within 2^-40 of a border: p - q is exact as a pair of f32 numbers, its
-// sums are pairs too (2^-48), and what is compared is in f64.
+// A cluster of CTAs takes a sequence: each looks at the drafts (a few words each),
+// then all sum r = max(p - q, 0) over their shares of the row at which the drafts
+// end, and the first CTA finds the token by descending to the share, the warp's
+// part of it and the token at which the running sum passes u times the whole.
+// Which token that is does not depend on the order of sums but where u lies within
+// about 2^-44 of a border: p - q is exact as a pair of f32 numbers, its sums are
+// pairs too, and from a warp's sum on they are whole numbers of 2^-61 of the whole
+// (64-bit floating point is as slow here as a hundred of the other operations).
 #include <cooperative_groups.h>
 
 #include "sample.cuh"
@@ -39,17 +40,43 @@ struct Residual {
   __device__ __forceinline__ float q_at(int i) const { return q ? q[i] : i == hot ? 1.f : 0.f; }
 };
 
-// hi + lo += a + b with |b| <= 2^-24 |a|.
-__device__ __forceinline__ void add_pair(float& hi, float& lo, float a, float b) {
-  const float s = __fadd_rn(hi, a), t = __fsub_rn(s, hi);
-  lo = __fadd_rn(lo, __fadd_rn(__fadd_rn(__fsub_rn(hi, __fsub_rn(s, t)), __fsub_rn(a, t)), b));
+// Two f32 numbers in one register pair: their sums take one instruction.
+struct Two {
+  unsigned long long v;
+};
+__device__ __forceinline__ Two two(float a, float b) {
+  Two r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 split(Two a) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+  return r;
+}
+__device__ __forceinline__ Two operator+(Two a, Two b) {
+  Two r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two operator-(Two a, Two b) {   // (the product with -1 is exact)
+  Two r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(b.v), "l"(two(-1.f, -1.f).v), "l"(a.v));
+  return r;
+}
+
+// (hi, lo) += a + b with |b| <= 2^-24 |a|.
+template <typename F>
+__device__ __forceinline__ void add_pair(F& hi, F& lo, F a, F b) {
+  const F s = hi + a, t = s - hi;
+  lo = lo + (((hi - (s - t)) + (a - t)) + b);
   hi = s;
 }
 
-// A warp's sum of r over [lo, hi), on every lane.
-__device__ double sum_range(const Residual& r, int lo, int hi, bool& bad) {
+// A warp's sum of r over [lo, hi) as a pair, on every lane.
+__device__ float2 sum_range(const Residual& r, int lo, int hi, bool& bad) {
   const int lane = threadIdx.x & 31;
-  float s = 0.f, e = 0.f;
+  Two s = two(0.f, 0.f), e = s, odd = s;
   for (int i0 = lo; i0 < hi; i0 += kChunk) {
     float p[kFly], q[kFly];
 #pragma unroll
@@ -59,45 +86,75 @@ __device__ double sum_range(const Residual& r, int lo, int hi, bool& bad) {
       q[j] = i < hi ? r.q_at(i) : 0.f;
     }
 #pragma unroll
-    for (int j = 0; j < kFly; ++j) {
-      const float a = prob(p[j], bad), b = prob(q[j], bad);
-      const float d = __fsub_rn(a, b), t = __fsub_rn(d, a);
-      const float rest = __fsub_rn(__fsub_rn(a, __fsub_rn(d, t)), __fadd_rn(b, t));
-      if (d > 0.f) add_pair(s, e, d, rest);
+    for (int j = 0; j < kFly; j += 2) {
+      // 0 of finite numbers, NaN of others
+      asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(odd.v) : "l"(two(p[j], p[j + 1]).v), "l"(two(0.f, 0.f).v));
+      asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(odd.v) : "l"(two(q[j], q[j + 1]).v), "l"(two(0.f, 0.f).v));
+      const float b0 = fmaxf(q[j], 0.f), b1 = fmaxf(q[j + 1], 0.f);
+      const Two a = two(fmaxf(p[j], b0), fmaxf(p[j + 1], b1)), b = two(b0, b1);   // a >= b >= 0
+      const Two d = a - b;
+      add_pair(s, e, d, (a - d) - b);
     }
   }
+  const float2 z = split(odd);
+  if (__any_sync(0xffffffffu, !(z.x == 0.f && z.y == 0.f))) {
+    // (again, and one by one: an infinity has come into the sums)
+    bad = true;
+    s = e = two(0.f, 0.f);
+    for (int i = lo + lane; i < hi; i += 32) {
+      const float b = prob(r.q_at(i), bad), a = fmaxf(prob(r.p[i], bad), b);
+      const Two d = two(a, 0.f) - two(b, 0.f);
+      add_pair(s, e, d, (two(a, 0.f) - d) - two(b, 0.f));
+    }
+  }
+  float2 hi2 = split(s), lo2 = split(e);
+  float h = hi2.x, l = lo2.x;
+  add_pair(h, l, hi2.y, lo2.y);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    const float s2 = __shfl_xor_sync(0xffffffffu, s, o), e2 = __shfl_xor_sync(0xffffffffu, e, o);
+    const float h2 = __shfl_xor_sync(0xffffffffu, h, o), l2 = __shfl_xor_sync(0xffffffffu, l, o);
     // (the same on both lanes: the larger first)
-    const bool swap = s2 > s || (s2 == s && e2 > e);
-    float hi = swap ? s2 : s, lo = swap ? e2 : e;
-    add_pair(hi, lo, swap ? s : s2, swap ? e : e2);
-    s = hi, e = lo;
+    const bool swap = h2 > h || (h2 == h && l2 > l);
+    float a = swap ? h2 : h, b = swap ? l2 : l;
+    add_pair(a, b, swap ? h : h2, swap ? l : l2);
+    h = a, l = b;
   }
-  return static_cast<double>(s) + static_cast<double>(e);
+  return make_float2(h, l);
 }
 
-// Among n <= 32 * PER numbers >= 0 in order (a lane's lie together): the first up to which
+// Pairs as whole numbers: times 2^k, k so that the largest is below 2^54 (and 128 of them below 2^61).
+struct Scale {
+  float a, b;   // 2^k = a b
+  __device__ __forceinline__ unsigned long long of(float2 v) const {
+    const long long w = __float2ll_rn(v.x * a * b) + __float2ll_rn(v.y * a * b);
+    return w > 0 ? w : 0;
+  }
+};
+__device__ __forceinline__ Scale scale_below(float most) {
+  const int e = static_cast<int>(__float_as_uint(most) >> 23) - 126;   // most < 2^e
+  const int k = 54 - e, half = k / 2;
+  return {__int_as_float((half + 127) << 23), __int_as_float((k - half + 127) << 23)};
+}
+
+// Among n <= 32 * PER numbers in order (a lane's lie together): the first up to which
 // `base` and they sum to more than t, else the last that is above 0.  base: what is before it.
 template <int PER>
-__device__ int pick(const double (&v)[PER], double t, double& base) {
+__device__ int pick(const unsigned long long (&v)[PER], unsigned long long t, unsigned long long& base) {
   const int lane = threadIdx.x & 31;
-  double sum = 0.0;
+  unsigned long long sum = 0;
 #pragma unroll
   for (int j = 0; j < PER; ++j) sum += v[j];
-  double incl = sum;
+  unsigned long long incl = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const double w = __shfl_up_sync(0xffffffffu, incl, o);
+    const unsigned long long w = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += w;
   }
-  double at = base + (incl - sum);
+  unsigned long long at = base + (incl - sum), hit_at = 0, last_at = 0;
   int hit = -1, last = -1;
-  double hit_at = 0.0, last_at = 0.0;
 #pragma unroll
   for (int j = 0; j < PER; ++j) {
-    if (v[j] > 0.0) {
+    if (v[j]) {
       last = j, last_at = at;
       if (hit < 0 && at + v[j] > t) hit = j, hit_at = at;
     }
@@ -110,29 +167,50 @@ __device__ int pick(const double (&v)[PER], double t, double& base) {
   return from * PER + __shfl_sync(0xffffffffu, hits ? hit : last, from);
 }
 
+// floor(u S) for u >= 0; S where u is 1 or more.
+__device__ __forceinline__ unsigned long long share_of(float u, unsigned long long S) {
+  if (!(u < 1.f)) return S;
+  const uint32_t b = __float_as_uint(u);
+  const int e = static_cast<int>(b >> 23);
+  const unsigned long long f = e ? (b & 0x7fffffu) | 0x800000u : b & 0x7fffffu;
+  const int shift = 150 - (e ? e : 1);                   // u = f 2^-shift, shift >= 24
+  const unsigned long long lo = S * f, hi = __umul64hi(S, f);
+  return shift < 64 ? (hi << (64 - shift)) + (lo >> shift) : shift < 128 ? hi >> (shift - 64) : 0;
+}
+
 struct Small {
-  double part[kMaxCtas * kWarps], sub[kWarps];
+  float2 part[kMaxCtas * kWarps], sub[kWarps];
   int m, lo, hi, token;
-  double base;
 };
 
 // The token within [0, V), where s.part holds the sums of the shares [i L, i L + L); called
 // by all threads of a CTA.  -1 if there is none.
-__device__ int find_token(const Residual& r, int V, int L, int shares, double u, Small& s, bool& bad) {
+__device__ int find_token(const Residual& r, int V, int L, int shares, float u, Small& s, bool& bad) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   constexpr int kPer = kMaxCtas * kWarps / 32;
-  double t = 0.0, base = 0.0;
+  unsigned long long t = 0, base = 0;
+  Scale scale = {0.f, 0.f};
   if (warp == 0) {
-    double v[kPer], total = 0.0;
+    float2 part[kPer];
+    float most = 0.f;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-      v[j] = lane * kPer + j < shares ? s.part[lane * kPer + j] : 0.0;
-      total += v[j];
+      part[j] = lane * kPer + j < shares ? s.part[lane * kPer + j] : make_float2(0.f, 0.f);
+      most = fmaxf(most, part[j].x);
     }
+    most = warp_max(most);
+    if (!(most <= 3.402823466e38f)) bad = true;   // the sum is past f32's range
+    int share = -1;
+    if (most > 0.f) {
+      scale = scale_below(most);
+      unsigned long long v[kPer], total = 0;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-    t = u * total;
-    const int share = pick(v, t, base);
+      for (int j = 0; j < kPer; ++j) total += v[j] = scale.of(part[j]);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+      t = share_of(u, total);
+      share = pick(v, t, base);
+    }
     if (lane == 0) {
       s.lo = share < 0 ? -1 : share * L;
       s.hi = min(V, (share + 1) * L);
@@ -142,12 +220,16 @@ __device__ int find_token(const Residual& r, int V, int L, int shares, double u,
   if (s.lo < 0) return -1;
   while (s.hi - s.lo > kChunk) {
     const int lo = s.lo, hi = s.hi, sub = (hi - lo + kThreads - 1) / kThreads * 32;
-    const double v = sum_range(r, min(hi, lo + warp * sub), min(hi, lo + warp * sub + sub), bad);
+    const float2 v = sum_range(r, min(hi, lo + warp * sub), min(hi, lo + warp * sub + sub), bad);
     if (lane == 0) s.sub[warp] = v;
     __syncthreads();
     if (warp == 0) {
-      const double one[1] = {lane < kWarps ? s.sub[lane] : 0.0};
-      const int at = max(pick(one, t, base), 0);
+      const float2 sub_sum = lane < kWarps ? s.sub[lane] : make_float2(0.f, 0.f);
+      const unsigned long long one[1] = {scale.of(sub_sum)};
+      int at = pick(one, t, base);
+      // (parts below 2^-54 of the largest share alone: the first of them)
+      const unsigned any = __ballot_sync(0xffffffffu, sub_sum.x > 0.f);
+      if (at < 0) at = max(__ffs(any) - 1, 0);
       if (lane == 0) {
         s.lo = lo + at * sub;
         s.hi = min(hi, lo + at * sub + sub);
@@ -164,15 +246,30 @@ __device__ int find_token(const Residual& r, int V, int L, int shares, double u,
       p[j] = i < hi ? r.p[i] : 0.f;
       q[j] = i < hi ? r.q_at(i) : 0.f;
     }
-    double v[kFly];
+    unsigned long long v[kFly];
+    bool above = false;
+    int first = -1;
 #pragma unroll
-    for (int j = 0; j < kFly; ++j)
-      v[j] = fmax(static_cast<double>(prob(p[j], bad)) - static_cast<double>(prob(q[j], bad)), 0.0);
-    const int at = pick(v, t, base);
+    for (int j = 0; j < kFly; ++j) {
+      const float b = prob(q[j], bad), a = fmaxf(prob(p[j], bad), b), d = __fsub_rn(a, b);
+      v[j] = scale.of(make_float2(d, __fsub_rn(__fsub_rn(a, d), b)));
+      if (d > 0.f && first < 0) first = j, above = true;
+    }
+    int at = pick(v, t, base);
+    // (numbers below 2^-54 of the largest share alone: the first of them)
+    const unsigned any = __ballot_sync(0xffffffffu, above);
+    if (at < 0 && any) at = (__ffs(any) - 1) * kFly + __shfl_sync(0xffffffffu, first, __ffs(any) - 1);
     if (lane == 0) s.token = at < 0 ? -1 : lo + at;
   }
   __syncthreads();
   return s.token;
+}
+
+// Whether u q < p, exactly.
+__device__ __forceinline__ bool accepts(float u, float q, float p) {
+  const float prod = __fmul_rn(u, q);
+  if (fabsf(prod) < 0x1p-80f) return static_cast<double>(u) * static_cast<double>(q) < static_cast<double>(p);
+  return prod < p || (prod == p && fmaf(u, q, -prod) < 0.f);
 }
 
 __global__ void __launch_bounds__(kThreads) verify_drafts_kernel(VerifyArgs a, int n_ctas, int L) {
@@ -189,6 +286,7 @@ __global__ void __launch_bounds__(kThreads) verify_drafts_kernel(VerifyArgs a, i
   const int K = min(s1 - s0, a.max_drafts);
   const int64_t row0 = static_cast<int64_t>(s0) + static_cast<int64_t>(b) * a.bonus;   // the target's
   bool bad = false;
+  const float u_in = a.u_token[b], u = u_in >= 0.f ? u_in : 0.f;
   if (warp == 0) {
     int m = 0;
     for (; m < K; m += 32) {
@@ -200,7 +298,7 @@ __global__ void __launch_bounds__(kThreads) verify_drafts_kernel(VerifyArgs a, i
         if (id >= 0 && id < V) {
           const float p = prob(a.p[(row0 + j) * a.ld_p + id], bad);
           const float q = a.q ? prob(a.q[(s0 + j) * a.ld_q + id], bad) : 1.f;
-          rejected = !(static_cast<double>(a.u_accept[s0 + j]) * static_cast<double>(q) < static_cast<double>(p));
+          rejected = !accepts(a.u_accept[s0 + j], q, p);
         }
       }
       const unsigned no = __ballot_sync(0xffffffffu, rejected);
@@ -224,7 +322,7 @@ __global__ void __launch_bounds__(kThreads) verify_drafts_kernel(VerifyArgs a, i
       r.hot = -1;
     }
   }
-  double v = 0.0;
+  float2 v = make_float2(0.f, 0.f);
   const int share = rank * kWarps + warp;
   if (some) v = sum_range(r, min(V, share * L), min(V, share * L + L), bad);
   if (n_ctas > 1) {
@@ -243,8 +341,6 @@ __global__ void __launch_bounds__(kThreads) verify_drafts_kernel(VerifyArgs a, i
   }
   int token = -1;
   if (some) {
-    const float u_in = a.u_token[b];
-    const double u = u_in >= 0.f ? static_cast<double>(u_in) : 0.0;
     token = find_token(r, V, L, n_ctas * kWarps, u, s, bad);
     if (token < 0 && m < K) {
       // p is nowhere above q (by rounding: both sum to 1): a token of p, by this CTA alone

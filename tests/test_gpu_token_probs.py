@@ -140,7 +140,7 @@ def test_odd_settings_in_tensors():
     st = torch.zeros(1, dtype=torch.int32, device="cuda")
     nan = float("nan")
     got = token_probs(x, f(nan, 1, 1), 0, f(1, nan, 1), status=st)
-    assert int(st) == 1 and torch.equal(got, token_probs(x, f(0, 1, 1)))
+    assert int(st) == 1 and torch.equal(got, token_probs(x, f(0, 1, 1), 0, f(1, 1, 1)))
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
