@@ -1,6 +1,8 @@
 /* CPython side of the page plans and of sampling (include/dvi.h): checks a
- * call's tensors and makes the library call, like the paged cache's (paged_py.c),
- * and for the same reason: these calls take a few microseconds on the GPU. */
+ * call's tensors, makes its outputs and the library call.  Like the paged cache's
+ * (paged_py.c), and for the same reason: these calls take a few microseconds on the
+ * GPU.  (Of verify_drafts' enqueueing, 9.7 us with Python around these checks: three
+ * outputs 2.4, a launch 1.8, a look at a tensor 0.3.) */
 #include "tensor_py.h"
 
 typedef dvi_status (*probs_fn)(int, const void*, int64_t, int, int, const dvi_sampling*, float*, int64_t, int32_t*,
@@ -13,39 +15,73 @@ typedef dvi_status (*plan_fn)(const dvi_page_pool*, const int32_t*, const int32_
 static probs_fn g_probs;
 static verify_fn g_verify;
 static plan_fn g_plan;
-static PyObject* g_i64;
+static PyObject *g_i64, *g_empty, *g_error;
 
 #define MAX_VOCAB (1 << 18)
 
-/* Rows [n, vocab] of `dtype` that may lie apart: elements from row to row. */
-static int rows_of(const char* what, PyObject* o, PyObject* dtype, int64_t n, int64_t vocab, int64_t device,
-                   uintptr_t* ptr, int64_t* ld) {
-  Tensor t;
-  if (!look(o, what, &t)) return 0;
-  if (t.dtype != dtype || t.dims != 2 || t.size[0] != n || t.size[1] != vocab) {
-    PyErr_Format(PyExc_ValueError, "%s must be %s [%lld, %lld]", what, dtype == g_f32 ? "float32" : "bfloat16",
-                 (long long)n, (long long)vocab);
+/* f32 rows [n, vocab] that may lie apart: elements from row to row. */
+static int are_rows(const char* what, const Tensor* t, int64_t n, int64_t vocab, int64_t device, int64_t* ld) {
+  if (t->dtype != g_f32 || t->dims != 2 || t->size[0] != n || t->size[1] != vocab) {
+    PyErr_Format(PyExc_ValueError, "%s must be float32 [%lld, %lld]", what, (long long)n, (long long)vocab);
     return 0;
   }
-  if (t.device != device) return refuse(what, "not on the call's device");
-  *ld = n <= 1 ? vocab : t.step[0];
-  if (n && ((vocab > 1 && t.step[1] != 1) || *ld < vocab)) return refuse(what, "each row must be contiguous");
+  if (t->device != device) return refuse(what, "not on the call's device");
+  *ld = n <= 1 ? vocab : t->step[0];
+  if (n && ((vocab > 1 && t->step[1] != 1) || *ld < vocab)) return refuse(what, "each row must be contiguous");
+  return 1;
+}
+static int rows_of(const char* what, PyObject* o, int64_t n, int64_t vocab, int64_t device, uintptr_t* ptr,
+                   int64_t* ld) {
+  Tensor t;
+  if (!look(o, what, &t) || !are_rows(what, &t, n, vocab, device, ld)) return 0;
   *ptr = t.ptr;
   return 1;
 }
 
 /* A contiguous array [n] of `dtype`. */
-static int array_of(const char* what, PyObject* o, PyObject* dtype, int64_t n, int64_t device, uintptr_t* ptr) {
-  Tensor t;
-  if (!look(o, what, &t)) return 0;
-  if (t.dtype != dtype || t.dims != 1 || t.size[0] != n || !contiguous(&t)) {
-    PyErr_Format(PyExc_ValueError, "%s must be contiguous %s [%lld]", what,
-                 dtype == g_f32 ? "float32" : dtype == g_i64 ? "int64" : "int32", (long long)n);
+static int is_array(const char* what, const Tensor* t, PyObject* dtype, int64_t n, int64_t device) {
+  if (t->dtype != dtype || t->dims != 1 || t->size[0] != n || !contiguous(t)) {
+    PyErr_Format(PyExc_ValueError, "%s must be contiguous %s [%lld]", what, dtype == g_f32 ? "float32" : "int32",
+                 (long long)n);
     return 0;
   }
-  if (t.device != device) return refuse(what, "not on the call's device");
+  return t->device == device || refuse(what, "not on the call's device");
+}
+static int array_of(const char* what, PyObject* o, PyObject* dtype, int64_t n, int64_t device, uintptr_t* ptr) {
+  Tensor t;
+  if (!look(o, what, &t) || !is_array(what, &t, dtype, n, device)) return 0;
   *ptr = t.ptr;
   return 1;
+}
+
+/* A new contiguous tensor on the current device, [n] or (width >= 0) [n, width], and its address. */
+static PyObject* new_tensor(int64_t n, int64_t width, PyObject* dtype, uintptr_t* ptr) {
+  PyObject *size = width < 0 ? Py_BuildValue("(L)", (long long)n) : Py_BuildValue("(LL)", (long long)n, (long long)width);
+  PyObject *step = width < 0 ? Py_BuildValue("(i)", 1) : Py_BuildValue("(Li)", (long long)width, 1);
+  PyObject* t = NULL;
+  int64_t p;
+  if (size && step) {
+    PyObject* args[3] = {size, step, dtype};
+    t = PyObject_Vectorcall(g_empty, args, 3, NULL);
+  }
+  Py_XDECREF(size);
+  Py_XDECREF(step);
+  if (t && !call_int(t, s_data_ptr, &p)) Py_CLEAR(t);
+  if (t) *ptr = (uintptr_t)p;
+  return t;
+}
+
+/* `out` where the library took the call, else its error. */
+static PyObject* result(const char* what, dvi_status rc, PyObject* out) {
+  static const char* const names[] = {"DVI_OK", "DVI_ERR_INVALID_ARG", "DVI_ERR_CAPACITY", "DVI_ERR_NONFINITE",
+                                      "DVI_ERR_CUDA", "DVI_ERR_UNIMPLEMENTED", "DVI_ERR_TIMEOUT"};
+  if (rc == DVI_OK) return out;
+  Py_XDECREF(out);
+  if (rc < 0 && rc >= -6)
+    PyErr_Format(g_error, "%s: %s", what, names[-rc]);
+  else
+    PyErr_Format(g_error, "%s: %d", what, (int)rc);
+  return NULL;
 }
 
 static int is_number(PyObject* o) { return PyFloat_Check(o) || PyLong_Check(o); }
@@ -58,7 +94,7 @@ static int status_of(const char* what, PyObject* o, int64_t device, int32_t** ou
   return 1;
 }
 
-/* probs(logits, temperature, top_k, top_p, out, status, stream) -> status */
+/* probs(logits, temperature, top_k, top_p, out or None, status, stream) -> out */
 static PyObject* py_probs(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
   (void)self;
   if (!count(n_args, 7)) return NULL;
@@ -121,24 +157,31 @@ static PyObject* py_probs(PyObject* self, PyObject* const* a, Py_ssize_t n_args)
   }
   s.top_p = (const float*)p;
   int32_t* status;
-  if (!rows_of("token_probs: out", a[4], g_f32, n, vocab, t.device, &out, &ld_out) ||
-      !status_of("token_probs: status", a[5], t.device, &status))
-    return NULL;
+  if (!status_of("token_probs: status", a[5], t.device, &status)) return NULL;
   dvi_stream stream = (dvi_stream)PyLong_AsVoidPtr(a[6]);
   if (PyErr_Occurred()) return NULL;
+  PyObject* to;
+  if (a[4] == Py_None) {
+    to = new_tensor(n, vocab, g_f32, &out);
+    if (!to) return NULL;
+    ld_out = vocab;
+  } else {
+    if (!rows_of("token_probs: out", a[4], n, vocab, t.device, &out, &ld_out)) return NULL;
+    to = Py_NewRef(a[4]);
+  }
   const int type = t.dtype == g_f32 ? DVI_F32 : DVI_BF16;
   dvi_status rc;
   Py_BEGIN_ALLOW_THREADS
   rc = g_probs(type, (const void*)t.ptr, ld, (int)n, (int)vocab, &s, (float*)out, ld_out, status, stream);
   Py_END_ALLOW_THREADS
-  return PyLong_FromLong(rc);
+  return result("token_probs", rc, to);
 }
 
-/* verify(target, draft_ids, u_accept, u_token, draft, draft_start, max_drafts, bonus, ids, n_committed, n_accepted,
- *        status, stream) -> status */
+/* verify(target, draft_ids, u_accept, u_token, draft, draft_start, max_drafts, bonus, status, stream)
+ *   -> (ids, n_committed, n_accepted) */
 static PyObject* py_verify(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
   (void)self;
-  if (!count(n_args, 13)) return NULL;
+  if (!count(n_args, 10)) return NULL;
   Tensor t, u, d;
   if (!look(a[0], "verify_drafts: target", &t) || !look(a[3], "verify_drafts: u_token", &u) ||
       !look(a[1], "verify_drafts: draft_ids", &d))
@@ -167,7 +210,7 @@ static PyObject* py_verify(PyObject* self, PyObject* const* a, Py_ssize_t n_args
     return NULL;
   }
   int64_t most = n;
-  uintptr_t start = 0, ids = 0, ua, ut, p, q = 0, out = 0, nc, na;
+  uintptr_t start = 0, ua, q = 0;
   int64_t ld_p, ld_q = 0;
   if (a[5] == Py_None) {
     if (B && n % B) {
@@ -192,47 +235,49 @@ static PyObject* py_verify(PyObject* self, PyObject* const* a, Py_ssize_t n_args
     refuse("verify_drafts", "at most 2^20 drafts of a sequence (give max_drafts)");
     return NULL;
   }
-  if (!rows_of("verify_drafts: target", a[0], g_f32, n + (bonus ? B : 0), vocab, t.device, &p, &ld_p) ||
-      !array_of("verify_drafts: draft_ids", a[1], g_i32, n, t.device, &ids) ||
+  if (!are_rows("verify_drafts: target", &t, n + (bonus ? B : 0), vocab, t.device, &ld_p) ||
+      !is_array("verify_drafts: draft_ids", &d, g_i32, n, t.device) ||
       !array_of("verify_drafts: u_accept", a[2], g_f32, n, t.device, &ua) ||
-      !array_of("verify_drafts: u_token", a[3], g_f32, B, t.device, &ut) ||
-      (a[4] != Py_None && !rows_of("verify_drafts: draft", a[4], g_f32, n, vocab, t.device, &q, &ld_q)) ||
-      !array_of("verify_drafts: n_committed", a[9], g_i32, B, t.device, &nc) ||
-      !array_of("verify_drafts: n_accepted", a[10], g_i32, B, t.device, &na))
+      !is_array("verify_drafts: u_token", &u, g_f32, B, t.device) ||
+      (a[4] != Py_None && !rows_of("verify_drafts: draft", a[4], n, vocab, t.device, &q, &ld_q)))
     return NULL;
-  Tensor o;
-  if (!look(a[8], "verify_drafts: ids", &o)) return NULL;
-  if (o.dtype != g_i32 || o.dims != 2 || o.size[0] != B || o.size[1] != most + (bonus ? 1 : 0) || !contiguous(&o) ||
-      o.device != t.device) {
-    refuse("verify_drafts: ids", "must be contiguous int32 [n_seqs, max_drafts + bonus] on the call's device");
-    return NULL;
-  }
-  out = o.ptr;
   int32_t* status;
-  if (!status_of("verify_drafts: status", a[11], t.device, &status)) return NULL;
-  dvi_stream stream = (dvi_stream)PyLong_AsVoidPtr(a[12]);
+  if (!status_of("verify_drafts: status", a[8], t.device, &status)) return NULL;
+  dvi_stream stream = (dvi_stream)PyLong_AsVoidPtr(a[9]);
   if (PyErr_Occurred()) return NULL;
+  PyObject* got = PyTuple_New(3);
+  if (!got) return NULL;
+  uintptr_t at[3];
+  for (int i = 0; i < 3; ++i) {
+    PyObject* o = new_tensor(B, i ? -1 : most + (bonus ? 1 : 0), g_i32, &at[i]);
+    if (!o) {
+      Py_DECREF(got);
+      return NULL;
+    }
+    PyTuple_SET_ITEM(got, i, o);
+  }
   const dvi_draft_batch b = {(int)B, (int)vocab, (int)n, (int)most, bonus ? 1 : 0, (const int32_t*)start,
-                             (const int32_t*)ids, (const float*)ua, (const float*)ut, status};
+                             (const int32_t*)d.ptr, (const float*)ua, (const float*)u.ptr, status};
   dvi_status rc;
   Py_BEGIN_ALLOW_THREADS
   /* (an empty tensor's rows need no memory, a drafter without rows is still one) */
-  rc = g_verify(&b, (const float*)p, ld_p, n ? (const float*)q : NULL, ld_q, (int32_t*)out, (int32_t*)nc,
-                (int32_t*)na, stream);
+  rc = g_verify(&b, (const float*)t.ptr, ld_p, n ? (const float*)q : NULL, ld_q, (int32_t*)at[0], (int32_t*)at[1],
+                (int32_t*)at[2], stream);
   Py_END_ALLOW_THREADS
-  return PyLong_FromLong(rc);
+  return result("verify_drafts", rc, got);
 }
 
-/* plan(pool, device, lens, rows, n_rows, row_start, slots, positions, stream) -> status */
+/* plan(pool, device, lens, rows, n_rows or None, whether row starts are wanted, stream)
+ *   -> (row_start, slots, positions), None for what is not wanted */
 static PyObject* py_plan(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
   (void)self;
-  if (!count(n_args, 9)) return NULL;
+  if (!count(n_args, 7)) return NULL;
   const dvi_page_pool* pool = (const dvi_page_pool*)PyLong_AsVoidPtr(a[0]);
   const int64_t device = PyLong_AsLongLong(a[1]);
   if (PyErr_Occurred()) return NULL;
   const int64_t B = pool->n_seqs;
   int64_t each = 0, n_rows = 0;
-  uintptr_t lens, rows = 0, start = 0, slots = 0, positions = 0;
+  uintptr_t lens, rows = 0, at[3] = {0, 0, 0};
   if (!array_of("plan: lens", a[2], g_i32, B, device, &lens)) return NULL;
   if (PyLong_Check(a[3])) {
     each = PyLong_AsLongLong(a[3]);
@@ -252,24 +297,37 @@ static PyObject* py_plan(PyObject* self, PyObject* const* a, Py_ssize_t n_args) 
       return NULL;
     }
   }
-  if ((a[5] != Py_None && !array_of("plan: row_start", a[5], g_i32, B + 1, device, &start)) ||
-      (a[6] != Py_None && !array_of("plan: slots", a[6], g_i64, n_rows, device, &slots)) ||
-      (a[7] != Py_None && !array_of("plan: positions", a[7], g_i32, n_rows, device, &positions)))
-    return NULL;
-  dvi_stream stream = (dvi_stream)PyLong_AsVoidPtr(a[8]);
-  if (PyErr_Occurred()) return NULL;
+  const int starts = PyObject_IsTrue(a[5]);
+  dvi_stream stream = (dvi_stream)PyLong_AsVoidPtr(a[6]);
+  if (starts < 0 || PyErr_Occurred()) return NULL;
+  PyObject* got = PyTuple_New(3);
+  if (!got) return NULL;
+  for (int i = 0; i < 3; ++i) {
+    PyObject* o = Py_None;
+    if (i == 0 ? starts : a[4] != Py_None) {
+      o = new_tensor(i ? n_rows : B + 1, -1, i == 1 ? g_i64 : g_i32, &at[i]);
+      if (!o) {
+        Py_DECREF(got);
+        return NULL;
+      }
+    } else {
+      Py_INCREF(o);
+    }
+    PyTuple_SET_ITEM(got, i, o);
+  }
   dvi_status rc;
   Py_BEGIN_ALLOW_THREADS
-  rc = g_plan(pool, (const int32_t*)lens, (const int32_t*)rows, (int)each, (int)n_rows, (int32_t*)start,
-              (int64_t*)slots, (int32_t*)positions, stream);
+  rc = g_plan(pool, (const int32_t*)lens, (const int32_t*)rows, (int)each, (int)n_rows, (int32_t*)at[0],
+              (int64_t*)at[1], (int32_t*)at[2], stream);
   Py_END_ALLOW_THREADS
-  return PyLong_FromLong(rc);
+  return result("plan", rc, got);
 }
 
-/* init(probs, verify, plan addresses, int32, int64, float32, bfloat16) */
+/* init(probs, verify, plan addresses, int32, int64, float32, bfloat16, a function (size, stride, dtype) that makes a
+ *      tensor on the current device, the class of the library's errors) */
 static PyObject* py_init(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
   (void)self;
-  if (!count(n_args, 7)) return NULL;
+  if (!count(n_args, 9)) return NULL;
   g_probs = (probs_fn)PyLong_AsVoidPtr(a[0]);
   g_verify = (verify_fn)PyLong_AsVoidPtr(a[1]);
   g_plan = (plan_fn)PyLong_AsVoidPtr(a[2]);
@@ -278,6 +336,8 @@ static PyObject* py_init(PyObject* self, PyObject* const* a, Py_ssize_t n_args) 
   g_i64 = Py_NewRef(a[4]);
   g_f32 = Py_NewRef(a[5]);
   g_bf16 = Py_NewRef(a[6]);
+  g_empty = Py_NewRef(a[7]);
+  g_error = Py_NewRef(a[8]);
   Py_RETURN_NONE;
 }
 

@@ -497,15 +497,16 @@ struct Settings {
 
 // What all warps of the cluster have given: the row's maximum and its sum of w (T > 0) or its
 // first largest token (T = 0).
-__device__ __forceinline__ void join(const Small& s, int n_ctas, bool greedy, Slope c, float* m, float* sum, int* hot) {
+template <int WARPS>
+__device__ __forceinline__ void join(const float2* peer, int n_ctas, bool greedy, Slope c, float* m, float* sum, int* hot) {
   const int lane = threadIdx.x & 31;
   float top = -INFINITY;
-  for (int i = lane; i < n_ctas * kWarps; i += 32) top = fmaxf(top, s.peer[i].x);
+  for (int i = lane; i < n_ctas * WARPS; i += 32) top = fmaxf(top, peer[i].x);
   top = warp_max(top);
   float all = 0.f;
   int first = 0x7fffffff;
-  for (int i = lane; i < n_ctas * kWarps; i += 32) {
-    const float2 p = s.peer[i];
+  for (int i = lane; i < n_ctas * WARPS; i += 32) {
+    const float2 p = peer[i];
     if (greedy) {
       if (p.x == top) first = min(first, __float_as_int(p.y));
     } else if (p.x > -INFINITY) {
@@ -530,11 +531,11 @@ __device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
 }
 
 // Rows without cuts: NV logits a thread, in registers; four at a time that lie together (V4)
-// or one.  A warp takes w to its own maximum; what is not finite shows in its sum.
-template <typename T, int NV, bool V4>
-__global__ void __launch_bounds__(kThreads, NV <= 16 ? 3 : NV <= 32 ? 2 : 1)
+// or one.  A warp takes w to its own maximum.
+template <typename T, int NV, int THREADS, bool V4>
+__global__ void __launch_bounds__(THREADS, 32768 / (NV * THREADS))
     token_probs_kernel(TokenProbsArgs a, int n_ctas, int slice) {
-  __shared__ Small s;
+  __shared__ float2 peer[kMaxCtas * THREADS / 32];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = n_ctas > 1 ? static_cast<int>(cg::this_cluster().block_rank()) : 0;
   const int r = blockIdx.x / n_ctas;
@@ -543,7 +544,7 @@ __global__ void __launch_bounds__(kThreads, NV <= 16 ? 3 : NV <= 32 ? 2 : 1)
   griddep_wait();
   const T* in = static_cast<const T*>(a.x) + r * a.ld + first;
   float* out = a.out + r * a.ld_out + first;
-  auto index = [&](int j) { return V4 ? ((j >> 2) * kThreads + tid) * 4 + (j & 3) : j * kThreads + tid; };
+  auto index = [&](int j) { return V4 ? ((j >> 2) * THREADS + tid) * 4 + (j & 3) : j * THREADS + tid; };
   float v[NV];
   if (V4) {
 #pragma unroll
@@ -567,18 +568,36 @@ __global__ void __launch_bounds__(kThreads, NV <= 16 ? 3 : NV <= 32 ? 2 : 1)
   const bool greedy = set.temperature == 0.f;
   const Slope c = {__fdiv_rn(1.44269504f, fminf(fmaxf(set.temperature, 0x1p-100f), 0x1p100f)), 0.f};
   bool bad = set.bad;
-  float m = -INFINITY;
+  float m = -INFINITY, odd = 0.f;   // odd: 0 of finite logits
 #pragma unroll
-  for (int j = 0; j < NV; ++j) m = fmaxf(m, v[j]);
+  for (int j = 0; j < NV; ++j) {
+    m = fmaxf(m, v[j]);
+    odd = fmaf(v[j], 0.f, odd);
+  }
+  if (__any_sync(0xffffffffu, odd != 0.f)) {
+    // (masked tokens, too, and what is behind the row's end)
+    m = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      bad |= !(v[j] < INFINITY);
+      v[j] = clean(v[j]);
+      m = fmaxf(m, v[j]);
+    }
+  }
   m = warp_max(m);
   float2 mine = make_float2(m, 0.f);
   float back = 1.f;
-  if (!greedy && m > -INFINITY) {
+  if (greedy) {
+    int at = 0x7fffffff;
+#pragma unroll
+    for (int j = NV - 1; j >= 0; --j)
+      if (v[j] == m) at = first + index(j);
+    mine.y = __int_as_float(__reduce_min_sync(0xffffffffu, at));
+  } else if (m > -INFINITY) {
     // x c - m c in one step where m c is small enough for its rounding to be taken back
     const float mc = m * c.hi;
-    const bool near = fabsf(mc) <= 0x1p20f;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    if (near) {
+    if (fabsf(mc) <= 0x1p20f) {
       back = exp2f(-fmaf(m, c.hi, -mc));
 #pragma unroll
       for (int j = 0; j < NV; ++j) sum[j & 3] += v[j] = exp2f(fmaf(v[j], c.hi, -mc));
@@ -588,43 +607,17 @@ __global__ void __launch_bounds__(kThreads, NV <= 16 ? 3 : NV <= 32 ? 2 : 1)
     }
     mine.y = warp_sum((sum[0] + sum[1]) + (sum[2] + sum[3])) * back;
   }
-  if (greedy || m == -INFINITY || !(mine.y <= 3.402823466e38f)) {
-    // NaN and infinities one by one, and the first token of the maximum
-    m = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      v[j] = index(j) < n ? DT<T>::ld(in + index(j)) : -INFINITY;
-      bad |= !(v[j] < INFINITY);
-      v[j] = clean(v[j]);
-      m = fmaxf(m, v[j]);
-    }
-    m = warp_max(m);
-    back = 1.f;
-    mine.x = m;
-    if (greedy) {
-      int at = 0x7fffffff;
-#pragma unroll
-      for (int j = NV - 1; j >= 0; --j)
-        if (v[j] == m) at = first + index(j);
-      mine.y = __int_as_float(__reduce_min_sync(0xffffffffu, at));
-    } else if (m > -INFINITY) {
-      float sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < NV; ++j) sum += v[j] = weight(v[j], m, c);
-      mine.y = warp_sum(sum);
-    }
-  }
   if (bad) flag_status(a.status, DVI_DEV_NONFINITE);
   if (n_ctas > 1) {
     cluster_wait_acquire();
-    if (lane < n_ctas) *cg::this_cluster().map_shared_rank(&s.peer[rank * kWarps + warp], lane) = mine;
+    if (lane < n_ctas) *cg::this_cluster().map_shared_rank(&peer[rank * THREADS / 32 + warp], lane) = mine;
   } else if (lane == 0) {
-    s.peer[warp] = mine;
+    peer[warp] = mine;
   }
   cluster_barrier(n_ctas);
   float top, sum;
   int hot;
-  join(s, n_ctas, greedy, c, &top, &sum, &hot);
+  join<THREADS / 32>(peer, n_ctas, greedy, c, &top, &sum, &hot);
   float scale = 0.f;
   if (greedy) {
 #pragma unroll
@@ -767,7 +760,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
   cluster_barrier(n_ctas);
   float top, sum;
   int hot;
-  join(s, n_ctas, greedy, c, &top, &sum, &hot);
+  join<kWarps>(s.peer, n_ctas, greedy, c, &top, &sum, &hot);
   if (greedy || top == -INFINITY) {
     for (int i = tid; i < n; i += kThreads) out[i] = top > -INFINITY && first + i == hot ? 1.f : 0.f;
     return;
@@ -814,12 +807,12 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
 }
 
 template <typename K>
-cudaError_t launch(K kern, const TokenProbsArgs& a, int ctas, size_t smem, cudaStream_t s) {
+cudaError_t launch(K kern, const TokenProbsArgs& a, int ctas, int threads, size_t smem, cudaStream_t s) {
   if (static_cast<int64_t>(a.n_rows) * ctas > 0x7fffffffll) return cudaErrorInvalidConfiguration;
   const int slice = ((a.vocab + ctas - 1) / ctas + 3) / 4 * 4;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(a.n_rows) * ctas);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem ? smem + slice * sizeof(float) : 0;
   cfg.stream = s;
   cudaLaunchAttribute at[2];
@@ -843,13 +836,12 @@ bool fours(const TokenProbsArgs& a) {
 
 template <typename T, bool V4>
 cudaError_t launch_plain(const TokenProbsArgs& a, cudaStream_t s) {
-  int nv = 16;
-  while (nv * kThreads * kMaxCtas < a.vocab) nv *= 2;
+  const int most = a.vocab <= 32 * 256 * kMaxCtas ? 32 * 256 : a.vocab <= 32 * 512 * kMaxCtas ? 32 * 512 : 64 * 512;
   int ctas = 1;
-  while (ctas * nv * kThreads < a.vocab) ctas *= 2;
-  if (nv == 16) return launch(token_probs_kernel<T, 16, V4>, a, ctas, 0, s);
-  return nv == 32 ? launch(token_probs_kernel<T, 32, V4>, a, ctas, 0, s)
-                  : launch(token_probs_kernel<T, 64, V4>, a, ctas, 0, s);
+  while (ctas * most < a.vocab) ctas *= 2;
+  if (most == 32 * 256) return launch(token_probs_kernel<T, 32, 256, V4>, a, ctas, 256, 0, s);
+  return most == 32 * 512 ? launch(token_probs_kernel<T, 32, 512, V4>, a, ctas, 512, 0, s)
+                          : launch(token_probs_kernel<T, 64, 512, V4>, a, ctas, 512, 0, s);
 }
 template <typename T>
 cudaError_t launch_plain(const TokenProbsArgs& a, cudaStream_t s) {
@@ -868,7 +860,7 @@ cudaError_t launch_cut(const TokenProbsArgs& a, cudaStream_t s) {
   int ctas = 1;
   while (ctas < kMaxCtas && (ctas * kSlice < a.vocab || (static_cast<int64_t>(a.n_rows) * ctas < 152 && a.vocab / ctas > 4096)))
     ctas *= 2;
-  return launch(token_probs_cut_kernel<T, V4>, a, ctas, sizeof(Cuts), s);
+  return launch(token_probs_cut_kernel<T, V4>, a, ctas, kThreads, sizeof(Cuts), s);
 }
 template <typename T>
 cudaError_t launch_cut(const TokenProbsArgs& a, cudaStream_t s) {

@@ -368,7 +368,7 @@ __global__ void __launch_bounds__(kThreads) verify_drafts_kernel(VerifyArgs a, i
 
 cudaError_t launch_verify_drafts(const VerifyArgs& a, cudaStream_t s) {
   int ctas = 1;
-  while (ctas < kMaxCtas && static_cast<int64_t>(a.n_seqs) * ctas * 2 <= 608 && a.vocab / ctas > 2 * kThreads) ctas *= 2;
+  while (ctas < kMaxCtas && static_cast<int64_t>(a.n_seqs) * ctas * 2 <= 304 && a.vocab / ctas > 2 * kThreads) ctas *= 2;
   const int shares = ctas * kWarps, L = ((a.vocab + shares - 1) / shares + 31) / 32 * 32;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(a.n_seqs) * ctas);

@@ -8,7 +8,7 @@ import torch
 
 from .dvi import DEV_BITS
 from .paged import _raw_stream, elsewhere
-from .sampling import _check, _module, _new, _on_device
+from .sampling import _current, _module
 
 
 class PagePoolC(ctypes.Structure):
@@ -23,6 +23,9 @@ class RowPlan(NamedTuple):
     row_start: torch.Tensor
     slots: Optional[torch.Tensor]
     positions: Optional[torch.Tensor]
+
+
+_new_plan = tuple.__new__     # (a named tuple's own constructor takes 0.3 us)
 
 
 class PagePool:
@@ -73,30 +76,21 @@ class PagePool:
         [B]) need: pages past that go back to the stack, missing ones come off it, in order of the slots.  A slot whose
         missing pages are not all there, or not all in its table, gets none of them (KV_FULL) and is passed over.
         Returns the row starts, and with n_rows (how many rows the pass's buffers have) also slots and positions."""
-        if stream is not None or not _on_device(self._index):
-            return RowPlan(*elsewhere(self._index, stream, self._tensors, self._plan, (lens, rows, n_rows),
-                                      "the pool's device"))
-        return RowPlan(*self._plan(lens, rows, n_rows))
+        if stream is not None or _current() != self._index:
+            got = elsewhere(self._index, stream, self._tensors, self._plan, (lens, rows, n_rows), "the pool's device")
+        else:
+            got = self._plan(lens, rows, n_rows)
+        return _new_plan(RowPlan, got)
 
     def _plan(self, lens, rows, n_rows):
-        if n_rows is not None and not 0 <= n_rows <= 1 << 30:
-            raise ValueError("plan: n_rows must be 0 to 2^30")
-        row_start = _new((self.n_seqs + 1,), torch.int32, self._index)
-        slots = positions = None
-        if n_rows is not None:
-            slots = _new((n_rows,), torch.int64, self._index)
-            positions = _new((n_rows,), torch.int32, self._index)
-        _check("plan", self._calls.plan(self._at, self._index, lens, rows, n_rows, row_start, slots, positions,
-                                        _raw_stream(self._index)))
-        return row_start, slots, positions
+        return self._calls.plan(self._at, self._index, lens, rows, n_rows, True, _raw_stream(self._index))
 
     def trim(self, lens: torch.Tensor, stream=None) -> None:
         """Give back the pages past lens: of rejected rows, and (lens 0) of sequences that ended."""
-        if stream is not None or not _on_device(self._index):
+        if stream is not None or _current() != self._index:
             elsewhere(self._index, stream, self._tensors, self.trim, (lens,), "the pool's device")
             return
-        _check("trim", self._calls.plan(self._at, self._index, lens, 0, None, None, None, None,
-                                        _raw_stream(self._index)))
+        self._calls.plan(self._at, self._index, lens, 0, None, False, _raw_stream(self._index))
 
     def status(self) -> list:
         """Names of the DVI_DEV_* flags set since the last look (waits for the device), then cleared."""

@@ -10,10 +10,17 @@ from typing import Optional, Tuple, Union
 
 import torch
 
-from .dvi import DVIError, STATUS, lib
+from .dvi import DVIError, lib
 from .paged import _empty_strided, _raw_stream, elsewhere
 
 _calls = None
+# (the call behind torch.cuda.current_device, without a look at whether CUDA is there)
+_current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _empty(size, stride, dtype):
+    """A tensor on the current device, where torch has no shorter way."""
+    return torch.empty_strided(size, stride, dtype=dtype, device="cuda")
 
 
 def _module():
@@ -26,35 +33,16 @@ def _module():
         except ImportError as e:
             raise RuntimeError("_sampling.so is missing: build it with `python -m paper_2510_05421_gb300.build`") from e
         at = (ctypes.cast(f, ctypes.c_void_p).value for f in (L.dvi_token_probs, L.dvi_verify_drafts, L.dvi_paged_plan))
-        _sampling.init(*at, torch.int32, torch.int64, torch.float32, torch.bfloat16)
+        _sampling.init(*at, torch.int32, torch.int64, torch.float32, torch.bfloat16, _empty_strided or _empty, DVIError)
         _calls = _sampling
     return _calls
 
 
-def _on_device(index: int) -> bool:
-    """Whether device `index` is current (the library launches on the current one)."""
-    return torch.cuda.current_device() == index
-
-
-def _new(shape, dtype, index: int) -> torch.Tensor:
-    """A contiguous tensor on the current device `index`."""
-    if _empty_strided is None:
-        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", index))
-    if len(shape) == 1:
-        return _empty_strided((shape[0],), (1,), dtype)
-    n, width = shape
-    return _empty_strided((n, width), (width, 1), dtype)
-
-
 def _device_of(what: str, t: torch.Tensor) -> int:
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    index = t.get_device() if isinstance(t, torch.Tensor) else -1
+    if index < 0:
         raise ValueError(f"{what}: not a tensor on a CUDA device")
-    return t.get_device()
-
-
-def _check(what: str, rc: int):
-    if rc:
-        raise DVIError(f"{what}: {STATUS.get(rc, rc)}")
+    return index
 
 
 def token_probs(logits: torch.Tensor, temperature: Union[float, torch.Tensor] = 1.0,
@@ -68,14 +56,10 @@ def token_probs(logits: torch.Tensor, temperature: Union[float, torch.Tensor] = 
     Settings are numbers or tensors with one for each row (f32, int32, f32 [n]).  NaN logits count as -inf, +inf as
     the largest number; status (int32 [1], or None) gets DVI_DEV_NONFINITE then.  `out` must not overlap logits."""
     index = _device_of("token_probs: logits", logits)
-    if stream is not None or not _on_device(index):
+    if stream is not None or _current() != index:
         return elsewhere(index, stream, (), token_probs, (logits, temperature, top_k, top_p, out, status),
                          "the logits' device")
-    if out is None:
-        out = _new(logits.shape, torch.float32, index) if logits.dim() == 2 else logits
-    _check("token_probs", (_calls or _module()).probs(logits, temperature, top_k, top_p, out, status,
-                                                      _raw_stream(index)))
-    return out
+    return (_calls or _module()).probs(logits, temperature, top_k, top_p, out, status, _raw_stream(index))
 
 
 def verify_drafts(target: torch.Tensor, draft_ids: torch.Tensor, u_accept: torch.Tensor, u_token: torch.Tensor,
@@ -97,18 +81,8 @@ def verify_drafts(target: torch.Tensor, draft_ids: torch.Tensor, u_accept: torch
     the vocabulary (rejected), DVI_DEV_NONFINITE for probabilities that are not finite (taken as 0) and rows that are
     zero everywhere (no token)."""
     index = _device_of("verify_drafts: target", target)
-    if stream is not None or not _on_device(index):
+    if stream is not None or _current() != index:
         return elsewhere(index, stream, (), verify_drafts, (target, draft_ids, u_accept, u_token, draft, draft_start,
                                                             max_drafts, bonus, status), "the target's device")
-    n_seqs, n_drafts = u_token.numel(), draft_ids.numel()
-    if max_drafts is None:
-        max_drafts = n_drafts if draft_start is not None else n_drafts // max(n_seqs, 1)
-    elif max_drafts < 0:
-        raise ValueError("verify_drafts: max_drafts must not be negative")
-    ids = _new((n_seqs, max_drafts + bool(bonus)), torch.int32, index)
-    n_committed = _new((n_seqs,), torch.int32, index)
-    n_accepted = _new((n_seqs,), torch.int32, index)
-    _check("verify_drafts", (_calls or _module()).verify(target, draft_ids, u_accept, u_token, draft, draft_start,
-                                                         max_drafts, bonus, ids, n_committed, n_accepted, status,
-                                                         _raw_stream(index)))
-    return ids, n_committed, n_accepted
+    return (_calls or _module()).verify(target, draft_ids, u_accept, u_token, draft, draft_start, max_drafts, bonus,
+                                        status, _raw_stream(index))
