@@ -1,0 +1,105 @@
+// Token probabilities: what the kernels for rows without and with cuts share.
+#pragma once
+
+#include <cooperative_groups.h>
+
+#include "sample.cuh"
+
+namespace dvi {
+
+namespace cg = cooperative_groups;
+
+constexpr int kProbsCtas = 8;   // most CTAs of a row
+
+cudaError_t launch_probs_plain(const TokenProbsArgs& a, int dtype, cudaStream_t s);
+cudaError_t launch_probs_cut(const TokenProbsArgs& a, int dtype, cudaStream_t s);
+
+// log2(e) / T as an f32 pair, T within 2^-100 .. 2^100: the quotient's rest is exact by a fused
+// multiply-add.
+struct Slope {
+  float hi, lo;
+  __device__ __forceinline__ explicit Slope(float T) {
+    const float t = fminf(fmaxf(T, 0x1p-100f), 0x1p100f), log2e = 0x1.715476p+0f, rest = 0x1.4ae0c0p-26f;
+    hi = __fdiv_rn(log2e, t);
+    lo = __fdiv_rn(fmaf(-hi, t, log2e) + rest, t);
+  }
+};
+
+// w in f32.
+__device__ __forceinline__ float weight(float x, float m, Slope c) { return exp2f((x - m) * c.hi); }
+
+// A logit as it counts: NaN as -inf, +inf as the largest number, -0 as 0.
+__device__ __forceinline__ float clean(float v) { return v != v ? -INFINITY : fminf(v, 3.402823466e38f) + 0.f; }
+
+// f32 as a number that grows with it, and back.
+__device__ __forceinline__ uint32_t ord(float x) {
+  const uint32_t b = __float_as_uint(x);
+  return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+}
+__device__ __forceinline__ float from_ord(uint32_t o) {
+  return __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o);
+}
+
+// Four logits that lie together.
+__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+  const uint2 w = *reinterpret_cast<const uint2*>(p);
+  return make_float4(bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y));
+}
+
+// Whether rows start on the boundaries of four elements of both sides.
+template <typename T>
+bool fours(const TokenProbsArgs& a) {
+  return reinterpret_cast<uintptr_t>(a.x) % (4 * sizeof(T)) == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0 &&
+         (a.n_rows == 1 || (a.ld % 4 == 0 && a.ld_out % 4 == 0));
+}
+
+// The settings of row r, as they count.
+struct Settings {
+  float temperature, top_p;   // 0: greedy; 1: no cut
+  int top_k;                  // 0: no cut
+  bool bad;
+  __device__ __forceinline__ Settings(const TokenProbsArgs& a, int r) {
+    temperature = a.temperature ? a.temperature[r] : a.temperature_all;
+    top_p = a.top_p ? a.top_p[r] : a.top_p_all;
+    top_k = a.top_k ? a.top_k[r] : a.top_k_all;
+    bad = temperature != temperature || top_p != top_p;
+    if (!(temperature > 0.f)) temperature = 0.f;
+    top_p = top_p < 1.f ? fmaxf(top_p, 0.f) : 1.f;
+    if (top_k < 0 || top_k >= a.vocab) top_k = 0;
+  }
+};
+
+__device__ __forceinline__ void cluster_barrier(int n_ctas) {
+  if (n_ctas > 1) {
+    cluster_arrive_release();
+    cluster_wait_acquire();
+  } else {
+    __syncthreads();
+  }
+}
+
+// A cluster of `ctas` CTAs for each row, which hold slices of it.
+template <typename K>
+cudaError_t launch_rows(K kern, const TokenProbsArgs& a, int ctas, int threads, size_t smem, size_t smem_a_logit,
+                        cudaStream_t s) {
+  if (static_cast<int64_t>(a.n_rows) * ctas > 0x7fffffffll) return cudaErrorInvalidConfiguration;
+  const int slice = ((a.vocab + ctas - 1) / ctas + 3) / 4 * 4;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(a.n_rows) * ctas);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem + slice * smem_a_logit;
+  cfg.stream = s;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = ctas;
+  at[1].val.clusterDim.y = 1;
+  at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kern, a, ctas, slice);
+}
+
+}  // namespace dvi

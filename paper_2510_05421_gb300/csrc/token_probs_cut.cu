@@ -1,0 +1,720 @@
+// Probabilities of sampling from logits with tokens cut off: top-k, top-p.
+//
+// With tokens in the order of their logits (equal ones by index) and w =
+// exp((x - max) / T), the kept tokens are a prefix of the order; it ends at the
+// last token whose rank is below top_k and before which the sum of w is below
+// top_p of the whole.  A row's slices lie in the shared memory of a cluster's CTAs.
+// The last kept token is found by a histogram of counts or of w over the logits: each
+// CTA gives the others its sums of 32 groups of 32 bins, then of the bins of the
+// group that the cut lies in, then its tokens of the bin, and each sorts these out for
+// itself.  Sums of w are whole numbers, so they do not depend on the order of the
+// atomics, and every CTA comes to the same end.  What the CTAs give each other are
+// stores that the receiver's barrier counts: no CTA waits for its own memory
+// operations, as at a cluster's barrier (three of which took a third of the time).
+// Where the bin has too many tokens (logits that are nearly equal), the token's place
+// in the order, as a number, is found 10 bits at a time.
+#include "token_probs.cuh"
+
+namespace dvi {
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kWarps = kThreads / 32;
+constexpr int kMaxCtas = kProbsCtas;
+constexpr int kBins = 1024;                      // 32 groups of 32
+constexpr int kBinBits = 10;
+constexpr int kPer = kBins / kThreads;
+constexpr float kBinsPerOctave = 40.f;           // of w: the last bin has what is below 2^-25.6
+constexpr int kList = 1024;                      // tokens of a bin that are sorted out by each CTA
+constexpr int kListPer = kList / kThreads;
+constexpr int kFew = 64;                         // tokens that are compared with each other
+constexpr int kIndexBits = 18;                   // kMaxVocab
+
+// 2^(k / 32), k = 0 .. 31, as f32 pairs hi + lo.
+__constant__ float2 kExp2[32] = {
+    {0x1p+0f, 0.f}, {0x1.059b0ep+0f, -0x1.9d4f52p-25f}, {0x1.0b5586p+0f, 0x1.9f3122p-25f}, {0x1.11301ep+0f, -0x1.fdb496p-25f},
+    {0x1.172b84p+0f, -0x1.c15742p-27f}, {0x1.1d4874p+0f, -0x1.d2e8cap-25f}, {0x1.2387a6p+0f, 0x1.ceac48p-25f}, {0x1.29e9ep+0f, -0x1.5c0424p-25f},
+    {0x1.306fep+0f, 0x1.4636e2p-25f}, {0x1.371a74p+0f, -0x1.18aac6p-25f}, {0x1.3dea64p+0f, 0x1.824684p-25f}, {0x1.44e086p+0f, 0x1.8624b4p-30f},
+    {0x1.4bfdaep+0f, -0x1.593abcp-25f}, {0x1.5342b6p+0f, -0x1.2c561p-25f}, {0x1.5ab07ep+0f, -0x1.5bd5ecp-27f}, {0x1.6247ecp+0f, -0x1.f8b55p-25f},
+    {0x1.6a09e6p+0f, 0x1.9fcef4p-26f}, {0x1.71f75ep+0f, 0x1.1d8beep-25f}, {0x1.7a1148p+0f, -0x1.829fdp-25f}, {0x1.82589ap+0f, -0x1.accc7cp-26f},
+    {0x1.8ace54p+0f, 0x1.15506ep-27f}, {0x1.93737cp+0f, -0x1.e64744p-25f}, {0x1.9c4918p+0f, 0x1.51f848p-27f}, {0x1.a5503cp+0f, -0x1.b83b54p-25f},
+    {0x1.ae89fap+0f, -0x1.a94b14p-26f}, {0x1.b7f77p+0f, -0x1.a09438p-25f}, {0x1.c199bep+0f, -0x1.3d56b2p-27f}, {0x1.cb720ep+0f, -0x1.8837ccp-27f},
+    {0x1.d5818ep+0f, -0x1.822dbcp-27f}, {0x1.dfc974p+0f, -0x1.908c94p-25f}, {0x1.ea4afap+0f, 0x1.52486cp-27f}, {0x1.f50766p+0f, -0x1.246ebp-26f}};
+
+// Two f32 numbers in one register pair: an operation on both is one instruction.
+struct Two {
+  unsigned long long v;
+};
+__device__ __forceinline__ Two two(float a, float b) {
+  Two r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ Two two(float a) { return two(a, a); }
+__device__ __forceinline__ float2 split(Two a) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+  return r;
+}
+__device__ __forceinline__ Two operator+(Two a, Two b) {
+  Two r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+  Two r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+  Two r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ Two operator-(Two a, Two b) { return fma2(b, two(-1.f), a); }   // (the product is exact)
+
+// w of two logits in units of 2^-44, off by about 2^-38; 0 below 2^-46.  x - m and its
+// product t with the slope are f32 pairs; t = q / 32 + r, 2^(q / 32) comes from the table and an
+// exponent, and 2^r = e^z = 1 + z + z^2 (1/2 + z/6 + z^2/24 + z^3/120) with |z| <= ln 2 / 64, of
+// which only 1 + z needs the second number.  Adding 1.5 * 2^23 rounds to whole numbers and leaves
+// them in the low bits.
+struct Masses {
+  unsigned long long a, b;
+};
+__device__ __forceinline__ Masses mass2(float xa, float xb, float m, Slope c, const float2* exp2_of) {
+  const float kRound = 12582912.f, kLn2 = 0x1.62e430p-1f, kLn2Lo = -0x1.05c610p-29f;
+  const Two x = two(xa, xb), top = two(m), ch = two(c.hi);
+  const Two dh = x - top, back = dh - x;
+  const Two dl = (x - (dh - back)) - (top + back);
+  const Two th = dh * ch;
+  const Two tl = fma2(dh, two(c.lo), fma2(dl, ch, fma2(dh, ch, two(0.f) - th)));
+  const Two q = fma2(th, two(32.f), two(kRound)), r = fma2(q - two(kRound), two(-0.03125f), th);
+  const Two z = r * two(kLn2);
+  const Two zl = fma2(tl, two(kLn2), fma2(r, two(kLn2Lo), fma2(r, two(kLn2), two(0.f) - z)));
+  const Two poly = fma2(z, fma2(z, fma2(z, two(1.f / 120.f), two(1.f / 24.f)), two(1.f / 6.f)), two(0.5f));
+  const Two zz = z * z * poly;
+  const Two p = z + zz, pl = ((z - p) + zz) + fma2(z, zl, zl);
+  const float2 qs = split(q), ts = split(th);
+  const int qa = __float_as_int(qs.x), qb = __float_as_int(qs.y);
+  const float2 ta = exp2_of[qa & 31], tb = exp2_of[qb & 31];
+  const Two t = two(ta.x, tb.x), prod = t * p;
+  const Two e = fma2(t, p, two(0.f) - prod) + fma2(t, pl, two(ta.y, tb.y));
+  const Two hi = t + prod, lo = ((t - hi) + prod) + e;
+  // times 2^(n + 22), n = q >> 5 (the shift drops what 1.5 * 2^23 leaves above it): 22 bits, then
+  // 22 more of what they leave
+  const Two scale = two(__int_as_float(((qa >> 5) << 23) + ((22 + 127) << 23)),
+                        __int_as_float(((qb >> 5) << 23) + ((22 + 127) << 23)));
+  const Two h = hi * scale, u = h + two(kRound);
+  const Two rest = fma2(lo, scale, h - (u - two(kRound)));
+  const Two f = fma2(rest, two(4194304.f), two(kRound));
+  const float2 us = split(u), fs = split(f);
+  const int kBits = 0x4b400000;   // of 1.5 * 2^23
+  const long long wa = static_cast<long long>(__float_as_int(us.x) - kBits) * 4194304 + (__float_as_int(fs.x) - kBits);
+  const long long wb = static_cast<long long>(__float_as_int(us.y) - kBits) * 4194304 + (__float_as_int(fs.y) - kBits);
+  return {ts.x > -46.f ? static_cast<unsigned long long>(wa) : 0ull,
+          ts.y > -46.f ? static_cast<unsigned long long>(wb) : 0ull};
+}
+__device__ __noinline__ unsigned long long mass(float x, float m, Slope c, const float2* exp2_of) {
+  return mass2(x, x, m, c, exp2_of).a;
+}
+
+__device__ __forceinline__ unsigned long long warp_sum_u64(unsigned long long v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ unsigned long long warp_scan_u64(unsigned long long v) {   // inclusive
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned long long w = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += w;
+  }
+  return v;
+}
+
+// What a row needs beside its slice of logits.
+struct Cuts {
+  unsigned digit[3][kBins];                     // sums of the bins, by digits of 15 bits: no sum passes 32 bits,
+                                                // and the atomics return nothing
+  unsigned long long key[kList], mass[kList];   // the tokens of a bin
+  unsigned long long box[kList];                // as the CTAs send them, kList / n_ctas of each
+};
+
+// What the CTAs of a cluster send each other, by rank, and what counts it.
+struct Boxes {
+  unsigned long long bar[6];                    // of: peers, groups, bins, counts, the list, kept
+  float2 top[kMaxCtas];                         // maximum, least of the threads' maxima
+  int2 first[kMaxCtas];                         // first token of the maximum, how many threads have a maximum
+  unsigned long long group[kMaxCtas][33];       // sums of the groups of bins, and of all tokens
+  unsigned long long bin[kMaxCtas][32];
+  unsigned long long count[kMaxCtas];
+  unsigned long long kept[kMaxCtas];
+};
+
+struct Small {
+  Boxes box;
+  float2 exp2_of[32];
+  unsigned long long part[kWarps], least[kWarps], most[kWarps], group[32];
+  float red[kWarps], low[kWarps];
+  int first[kWarps], some[kWarps];
+  int n_list, n_kept, found;
+  unsigned long long excl, cut, kept;
+};
+
+// One row (its slice in this CTA) and what is known of it.
+struct RowState {
+  const float* x;       // the slice, tokens first .. first + n - 1
+  int first, n;         // (n: up to a multiple of 4, with -inf behind the last token)
+  int rank, n_ctas;
+  float m;              // the row's maximum
+  uint32_t top;         // ord(m)
+  Slope c;
+  int* status;
+  __device__ __forceinline__ unsigned long long place(float v, int i) const {
+    return (static_cast<unsigned long long>(top - ord(v + 0.f)) << kIndexBits) | static_cast<unsigned>(first + i);
+  }
+  __device__ __forceinline__ float logit(unsigned long long place) const {
+    return from_ord(top - static_cast<uint32_t>(place >> kIndexBits));
+  }
+  // (rounded by adding 1.5 * 2^23)
+  __device__ __forceinline__ int bin(float v, float scale) const {
+    const float t = __fmul_rn(__fsub_rn(m, v), scale);
+    return __float_as_int(__fadd_rn(fminf(t, static_cast<float>(kBins - 1)), 12582912.f)) & 0xffff;
+  }
+};
+
+// Eight bytes to the box of CTA r, counted by its barrier.
+__device__ __forceinline__ void send(void* to, unsigned long long v, unsigned long long* bar, int r, int n_ctas) {
+  if (n_ctas == 1) {
+    *static_cast<unsigned long long*>(to) = v;
+    return;
+  }
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(
+                   mapa_shared(smem_u32(to), r)),
+               "l"(v), "r"(mapa_shared(smem_u32(bar), r))
+               : "memory");
+}
+__device__ __forceinline__ unsigned long long bits_of(float a, float b) {
+  return (static_cast<unsigned long long>(__float_as_uint(b)) << 32) | __float_as_uint(a);
+}
+// One thread says how much will come ...
+__device__ __forceinline__ void expect(unsigned long long* bar, int bytes, int n_ctas) {
+  if (n_ctas > 1) mbar_arrive_expect_tx(reinterpret_cast<uint64_t*>(bar), bytes);
+}
+// ... and all wait for it.
+__device__ __forceinline__ bool arrived(unsigned long long* bar, int turn, int n_ctas, int* status) {
+  if (n_ctas > 1) return mbar_wait(reinterpret_cast<uint64_t*>(bar), turn & 1, status);
+  __syncthreads();
+  return true;
+}
+
+__device__ __forceinline__ void add_to_bin(Cuts& h, int bin, unsigned long long v) {
+  const unsigned a = static_cast<unsigned>(v) & 0x7fffu, b = static_cast<unsigned>(v >> 15) & 0x7fffu,
+                 c = static_cast<unsigned>(v >> 30);
+  atomicAdd(&h.digit[0][bin], a);
+  if (b) atomicAdd(&h.digit[1][bin], b);
+  if (c) atomicAdd(&h.digit[2][bin], c);
+}
+__device__ __forceinline__ unsigned long long sum_of(unsigned a, unsigned b, unsigned c) {
+  return a + (static_cast<unsigned long long>(b) << 15) + (static_cast<unsigned long long>(c) << 30);
+}
+__device__ __forceinline__ unsigned long long bin_sum(const Cuts& h, int bin) {
+  return sum_of(h.digit[0][bin], h.digit[1][bin], h.digit[2][bin]);
+}
+__device__ __forceinline__ void clear_bins(Cuts& h) {
+  for (int i = threadIdx.x; i < 3 * kBins; i += kThreads) (&h.digit[0][0])[i] = 0;
+  __syncthreads();
+}
+
+// The first bin up to which the sums of CTAs r0 .. r1 - 1 (and `before`) reach target: its
+// number (-1 if none does) and the sum before it.  Their bins are complete when it is called.
+__device__ __noinline__ int find_bin(unsigned long long before, unsigned long long target, int r0, int r1, Cuts& h,
+                                     Small& s, unsigned long long* excl) {
+  cg::cluster_group cluster = cg::this_cluster();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  static_assert(kPer == 2, "a pair of bins a thread");
+  unsigned long long v[kPer] = {};
+  for (int r = r0; r < r1; ++r) {
+    uint2 d[3];
+    for (int k = 0; k < 3; ++k) d[k] = reinterpret_cast<const uint2*>(cluster.map_shared_rank(h.digit[k], r))[tid];
+    v[0] += sum_of(d[0].x, d[1].x, d[2].x);
+    v[1] += sum_of(d[0].y, d[1].y, d[2].y);
+  }
+  const unsigned long long sum = v[0] + v[1], incl = warp_scan_u64(sum);
+  if (lane == 31) s.part[warp] = incl;
+  if (tid == 0) s.found = -1;
+  __syncthreads();
+  unsigned long long at = before + incl - sum;
+  for (int w = 0; w < warp; ++w) at += s.part[w];
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    if (at < target && at + v[j] >= target) s.found = tid * kPer + j, s.excl = at;
+    at += v[j];
+  }
+  __syncthreads();
+  *excl = s.excl;
+  return s.found;
+}
+
+// Of the n tokens in h.key (with h.mass): the last kept one, where `before` is the sum before
+// them all.  By every CTA for itself.
+template <bool MASS>
+__device__ unsigned long long last_of_list(int n, unsigned long long before, unsigned long long target, int rank,
+                                           Cuts& h, Small& s, unsigned long long* kept) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  while (n > kFew) {
+    // bins of equal width from the first of their places to the last
+    unsigned long long key[kListPer], m[kListPer], least = ~0ull, most = 0;
+#pragma unroll
+    for (int j = 0; j < kListPer; ++j) {
+      const int i = tid + j * kThreads;
+      key[j] = i < n ? h.key[i] : ~0ull;
+      m[j] = i < n && MASS ? h.mass[i] : 1;
+      if (i < n) least = min(least, key[j]), most = max(most, key[j]);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      least = min(least, __shfl_xor_sync(0xffffffffu, least, o));
+      most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+    }
+    if (lane == 0) s.least[warp] = least, s.most[warp] = most;
+    if (tid == 0) s.n_kept = 0;
+    clear_bins(h);
+    for (int w = 0; w < kWarps; ++w) least = min(least, s.least[w]), most = max(most, s.most[w]);
+    const int bits = 64 - __clzll(most - least), shift = bits > kBinBits ? bits - kBinBits : 0;
+#pragma unroll
+    for (int j = 0; j < kListPer; ++j)
+      if (key[j] != ~0ull) add_to_bin(h, static_cast<int>((key[j] - least) >> shift), m[j]);
+    __syncthreads();
+    const int bin = find_bin(before, target, rank, rank + 1, h, s, &before);
+#pragma unroll
+    for (int j = 0; j < kListPer; ++j) {
+      if (key[j] == ~0ull || static_cast<int>((key[j] - least) >> shift) != bin) continue;
+      const int at = atomicAdd(&s.n_kept, 1);
+      h.key[at] = key[j];
+      if (MASS) h.mass[at] = m[j];
+    }
+    __syncthreads();
+    n = s.n_kept;
+    __syncthreads();
+  }
+  if (tid < n) {
+    const unsigned long long p = h.key[tid], v = MASS ? h.mass[tid] : 1;
+    unsigned long long sum = before;
+    for (int j = 0; j < n; ++j)
+      if (h.key[j] < p) sum += MASS ? h.mass[j] : 1;
+    if (sum < target && sum + v >= target) s.cut = p, s.kept = sum + v;
+  }
+  __syncthreads();
+  *kept = s.kept;
+  return s.cut;
+}
+
+// ceil(p S) for p in [0, 1), at least 1.
+__device__ __forceinline__ unsigned long long share_of(float p, unsigned long long S) {
+  const uint32_t b = __float_as_uint(p);
+  const int e = static_cast<int>(b >> 23);
+  const unsigned long long f = e ? (b & 0x7fffffu) | 0x800000u : b & 0x7fffffu;
+  const int shift = 150 - (e ? e : 1);                   // p = f 2^-shift, shift >= 24
+  const unsigned long long lo = S * f, hi = __umul64hi(S, f);
+  unsigned long long t;
+  if (shift < 64)
+    t = (hi << (64 - shift)) + (lo >> shift) + ((lo & ((1ull << shift) - 1)) ? 1 : 0);
+  else
+    t = shift < 128 ? (hi >> (shift - 64)) + 1 : 1;      // (one too many where nothing is left over: below 2^-40 of S)
+  return t ? t : 1;
+}
+
+// Tokens of the order up to one of them (all: those above -inf).
+struct Upto {
+  float x;
+  int i;
+  __device__ __forceinline__ bool has(float v, int at) const { return v > x || (v == x && at <= i); }
+};
+
+// The last kept token among those up to `upto`: before it the counts sum to less than top_k, or
+// (MASS) the masses to less than top_p of all.  Returns the tokens up to it.  *kept: their sum.
+// Bins go down from the maximum, `scale` of them a unit; tokens below `low` are known to be cut.
+// turn, turn2: how often the first barrier of the boxes has been used, and the others.
+template <bool MASS>
+__device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto, float scale, float low, int& turn,
+                          int& turn2, Cuts& h, Small& s, unsigned long long* kept) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n_ctas = row.n_ctas, rank = row.rank;
+  const float4* x4 = reinterpret_cast<const float4*>(row.x);
+  const int n4 = row.n / 4;
+  Boxes& box = s.box;
+  if (tid == 0) {
+    expect(&box.bar[1], n_ctas * 33 * 8, n_ctas);
+    s.n_list = 0;
+  }
+  clear_bins(h);
+  unsigned long long all = 0;
+  for (int g0 = warp * 32; g0 < n4; g0 += kThreads) {
+    const int g = g0 + lane;
+    float4 q = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    if (g < n4) q = x4[g];
+    const float v[4] = {q.x, q.y, q.z, q.w};
+    if (MASS) {
+      // (a mass is 0 below 2^-46, which is `low` here)
+      bool in[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) in[e] = v[e] >= low && upto.has(v[e], 4 * g + e);
+      if (!__any_sync(0xffffffffu, in[0] || in[1] || in[2] || in[3])) continue;
+      const Masses a = mass2(v[0], v[1], row.m, row.c, s.exp2_of), b = mass2(v[2], v[3], row.m, row.c, s.exp2_of);
+      const unsigned long long w[4] = {in[0] ? a.a : 0, in[1] ? a.b : 0, in[2] ? b.a : 0, in[3] ? b.b : 0};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        all += w[e];
+        const int bin = row.bin(v[e], scale);
+        if (w[e] && bin < kBins - 1) add_to_bin(h, bin, w[e]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const bool some = v[e] > -INFINITY;
+        all += some;
+        const int bin = row.bin(v[e], scale);
+        if (some && v[e] >= low && bin < kBins - 1) atomicAdd(&h.digit[0][bin], 1u);
+      }
+    }
+  }
+  all = warp_sum_u64(all);
+  if (lane == 0) s.part[warp] = all;
+  __syncthreads();
+  // the groups' sums to all
+#pragma unroll
+  for (int j = 0; j < 32 / kWarps; ++j) {
+    const int g = warp * (32 / kWarps) + j;
+    const unsigned long long v = warp_sum_u64(bin_sum(h, 32 * g + lane));
+    if (lane == 0) s.group[g] = v;
+  }
+  __syncthreads();
+  if (tid < 33) {
+    unsigned long long v = 0;
+    if (tid < 32) v = s.group[tid];
+    else
+      for (int w = 0; w < kWarps; ++w) v += s.part[w];
+    for (int r = 0; r < n_ctas; ++r) send(&box.group[rank][tid], v, &box.bar[1], r, n_ctas);
+  }
+  if (!arrived(&box.bar[1], turn++, n_ctas, row.status)) return upto;
+  unsigned long long v = 0, total = 0;
+  for (int r = 0; r < n_ctas; ++r) {
+    v += box.group[r][lane];
+    total += box.group[r][32];
+  }
+  *kept = total;
+  const unsigned long long target = MASS ? share_of(top_p, total) : top_k;
+  if (total < target) return upto;   // (fewer tokens than top_k)
+  unsigned long long incl = warp_scan_u64(v);
+  unsigned at = __ballot_sync(0xffffffffu, incl >= target);
+  int n = kList + 1;
+  unsigned long long before = 0;
+    int bin = -1;
+  if (at) {
+    // the bins of the group in which the cut is, to all
+    const int g = __ffs(at) - 1;
+    before = __shfl_sync(0xffffffffu, incl - v, g);
+    if (tid == 0) {
+      expect(&box.bar[2], n_ctas * 32 * 8, n_ctas);
+      expect(&box.bar[3], n_ctas * 8, n_ctas);
+    }
+    if (warp == 0) {
+      const unsigned long long mine = bin_sum(h, 32 * g + lane);
+      for (int r = 0; r < n_ctas; ++r) send(&box.bin[rank][lane], mine, &box.bar[2], r, n_ctas);
+    }
+    if (!arrived(&box.bar[2], turn2, n_ctas, row.status)) return upto;
+    v = 0;
+    for (int r = 0; r < n_ctas; ++r) v += box.bin[r][lane];
+    incl = before + warp_scan_u64(v);
+    at = __ballot_sync(0xffffffffu, incl >= target);
+    bin = 32 * g + __ffs(at) - 1;
+    before = __shfl_sync(0xffffffffu, incl - v, __ffs(at) - 1);
+    // and the tokens of the bin
+    const int cap = kList / n_ctas;
+    for (int g = tid; g < n4; g += kThreads) {
+      const float4 q = x4[g];
+      const float v[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (row.bin(v[e], scale) != bin || !(v[e] >= low) || !upto.has(v[e], 4 * g + e)) continue;
+        const int to = atomicAdd(&s.n_list, 1);
+        if (to >= cap) continue;
+        const unsigned long long p = row.place(v[e], 4 * g + e);
+        for (int r = 0; r < n_ctas; ++r) send(&h.box[rank * cap + to], p, &box.bar[4], r, n_ctas);
+      }
+    }
+    __syncthreads();
+    if (tid < n_ctas) send(&box.count[rank], s.n_list, &box.bar[3], tid, n_ctas);
+    if (!arrived(&box.bar[3], turn2, n_ctas, row.status)) return upto;
+    // how many each CTA has found, a lane a CTA; the warps share the CTAs' lists
+    const int there = lane < n_ctas ? static_cast<int>(box.count[lane]) : 0;
+    const int most = __reduce_max_sync(0xffffffffu, there);
+    n = most > cap ? kList + 1 : __reduce_add_sync(0xffffffffu, there);
+    const int sent = __reduce_add_sync(0xffffffffu, min(there, cap));
+    if (tid == 0) expect(&box.bar[4], sent * 8, n_ctas);
+    if (!arrived(&box.bar[4], turn2, n_ctas, row.status)) return upto;
+    ++turn2;
+    if (n <= kList) {
+      const int per = kWarps / n_ctas, from = warp / per;
+      int before_it = lane < from ? there : 0;
+      before_it = __reduce_add_sync(0xffffffffu, before_it);
+      const int m = __shfl_sync(0xffffffffu, there, from);
+      for (int i = warp % per * 32 + lane; i < m; i += per * 32) {
+        const unsigned long long p = h.box[from * cap + i];
+        h.key[before_it + i] = p;
+        if (MASS) h.mass[before_it + i] = mass(row.logit(p), row.m, row.c, s.exp2_of);
+      }
+      __syncthreads();
+    }
+  }
+  unsigned long long cut;
+  if (n <= kList) {
+    cut = last_of_list<MASS>(n, before, target, rank, h, s, kept);
+  } else {
+    before = cut = 0;
+    cg::cluster_group cluster = cg::this_cluster();
+    for (int shift = 32 + kIndexBits - kBinBits;; shift = shift > kBinBits ? shift - kBinBits : 0) {
+      __syncthreads();
+      clear_bins(h);
+      for (int i = tid; i < row.n; i += kThreads) {
+        const float x = row.x[i];
+        if (!(x > -INFINITY) || !upto.has(x, i)) continue;
+        const unsigned long long p = row.place(x, i);
+        if (p < cut || ((p - cut) >> shift) >= kBins) continue;
+        add_to_bin(h, static_cast<int>((p - cut) >> shift), MASS ? mass(x, row.m, row.c, s.exp2_of) : 1ull);
+      }
+      cluster_barrier(n_ctas);
+      const int b = find_bin(before, target, 0, n_ctas, h, s, &before);   // (found: the whole reaches target)
+      cut += static_cast<unsigned long long>(b) << shift;
+      if (shift == 0) {
+        // one token a bin
+        *kept = before;
+        for (int r = 0; r < n_ctas; ++r) *kept += bin_sum(*cluster.map_shared_rank(&h, r), b);
+      }
+      cluster_barrier(n_ctas);   // before the bins are cleared
+      if (shift == 0) break;
+    }
+  }
+  return {row.logit(cut), static_cast<int>(cut & ((1u << kIndexBits) - 1)) - row.first};
+}
+
+template <typename T, bool V4>
+__global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbsArgs a, int n_ctas, int slice) {
+  extern __shared__ __align__(16) unsigned char dynamic[];
+  __shared__ Small s;
+  Cuts& h = *reinterpret_cast<Cuts*>(dynamic);
+  float* x = reinterpret_cast<float*>(dynamic + sizeof(Cuts));
+  float4* x4 = reinterpret_cast<float4*>(x);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rank = n_ctas > 1 ? static_cast<int>(cg::this_cluster().block_rank()) : 0;
+  const int r = blockIdx.x / n_ctas;
+  const int first = min(rank * slice, a.vocab), n = min(slice, a.vocab - first), n4 = (n + 3) / 4;
+  Boxes& box = s.box;
+  if (tid == 0) {
+    for (int k = 0; k < 6; ++k) mbar_init(reinterpret_cast<uint64_t*>(&box.bar[k]), 1);
+    mbar_fence_init();
+    expect(&box.bar[0], n_ctas * 16, n_ctas);
+    expect(&box.bar[5], n_ctas * 8, n_ctas);
+  }
+  if (n_ctas > 1) cluster_arrive_release();              // (waited for before anything is sent)
+  griddep_wait();
+  const T* in = static_cast<const T*>(a.x) + r * a.ld + first;
+  float* out = a.out + r * a.ld_out + first;
+
+  float own = -INFINITY, odd = 0.f;   // odd: 0 of finite logits
+  constexpr int kFly = 16;
+  if (V4) {
+    for (int g0 = 0; g0 < n4; g0 += kFly / 4 * kThreads) {
+      float4 q[kFly / 4];
+#pragma unroll
+      for (int j = 0; j < kFly / 4; ++j) {
+        const int g = g0 + j * kThreads + tid, i = 4 * g;
+        q[j] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        if (i + 4 <= n) {
+          q[j] = load4(in + i);
+        } else if (i < n) {
+          q[j].x = DT<T>::ld(in + i);
+          if (i + 1 < n) q[j].y = DT<T>::ld(in + i + 1);
+          if (i + 2 < n) q[j].z = DT<T>::ld(in + i + 2);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kFly / 4; ++j) {
+        const int g = g0 + j * kThreads + tid;
+        if (g >= n4) continue;
+        own = fmaxf(own, fmaxf(fmaxf(q[j].x, q[j].y), fmaxf(q[j].z, q[j].w)));
+        odd = fmaf(q[j].x, 0.f, fmaf(q[j].y, 0.f, fmaf(q[j].z, 0.f, fmaf(q[j].w, 0.f, odd))));
+        x4[g] = q[j];
+      }
+    }
+  } else {
+    for (int i0 = 0; i0 < n; i0 += kFly * kThreads) {
+      float v[kFly];
+#pragma unroll
+      for (int j = 0; j < kFly; ++j) {
+        const int i = i0 + j * kThreads + tid;
+        v[j] = i < n ? DT<T>::ld(in + i) : -INFINITY;
+      }
+#pragma unroll
+      for (int j = 0; j < kFly; ++j) {
+        const int i = i0 + j * kThreads + tid;
+        own = fmaxf(own, v[j]);
+        if (i < n) odd = fmaf(v[j], 0.f, odd);
+        if (i < 4 * n4) x[i] = v[j];
+      }
+    }
+  }
+  const Settings set(a, r);
+  const bool greedy = set.temperature == 0.f;
+  const Slope c(set.temperature);
+  if (tid < 32) s.exp2_of[tid] = kExp2[tid];
+  // the tokens that the thread has loaded
+  auto each = [&](auto f) {
+    if (V4) {
+      for (int g = tid; g < n4; g += kThreads)
+        for (int i = 4 * g; i < 4 * g + 4; ++i) f(i);
+    } else {
+      for (int i = tid; i < n; i += kThreads) f(i);
+    }
+  };
+  bool bad = set.bad;
+  if (__syncthreads_or(odd != 0.f)) {
+    // (masked tokens, too, and the -inf behind a row that ends within four)
+    own = -INFINITY;
+    each([&](int i) {
+      bad |= !(x[i] < INFINITY);
+      x[i] = clean(x[i]);
+      own = fmaxf(own, x[i]);
+    });
+  }
+  if (bad) flag_status(a.status, DVI_DEV_NONFINITE);
+  {
+    // the CTA's maximum and its first token, and the least of the threads' maxima, to all
+    const float m = from_ord(__reduce_max_sync(0xffffffffu, ord(own)));
+    const float low = from_ord(__reduce_min_sync(0xffffffffu, own > -INFINITY ? ord(own) : 0xff7fffffu));
+    const unsigned some = __ballot_sync(0xffffffffu, own > -INFINITY);
+    int at = 0x7fffffff;
+    if (greedy) {
+      if (m > -INFINITY && own == m)
+        each([&](int i) {
+          if (x[i] == m) at = min(at, first + i);
+        });
+      at = __reduce_min_sync(0xffffffffu, at);
+    }
+    if (lane == 0) s.red[warp] = m, s.low[warp] = low, s.first[warp] = at, s.some[warp] = __popc(some);
+  }
+  __syncthreads();
+  if (n_ctas > 1) cluster_wait_acquire();
+  if (warp == 0) {
+    const bool is = lane < kWarps;
+    const float w = is ? s.red[lane] : -INFINITY;
+    const float m = from_ord(__reduce_max_sync(0xffffffffu, ord(w)));
+    const float low = from_ord(__reduce_min_sync(0xffffffffu, is ? ord(s.low[lane]) : 0xff7fffffu));
+    const int at = __reduce_min_sync(0xffffffffu, is && w == m ? s.first[lane] : 0x7fffffff);
+    const int some = __reduce_add_sync(0xffffffffu, is ? s.some[lane] : 0);
+    if (lane < n_ctas) {
+      send(&box.top[rank], bits_of(m, low), &box.bar[0], lane, n_ctas);
+      send(&box.first[rank], (static_cast<unsigned long long>(some) << 32) | static_cast<unsigned>(at), &box.bar[0],
+           lane, n_ctas);
+    }
+  }
+  if (!arrived(&box.bar[0], 0, n_ctas, a.status)) return;
+  const bool is = lane < n_ctas;
+  const float2 of_cta = is ? box.top[lane] : make_float2(-INFINITY, 3.402823466e38f);
+  const int2 first_of = is ? box.first[lane] : make_int2(0x7fffffff, 0);
+  const float top = from_ord(__reduce_max_sync(0xffffffffu, ord(of_cta.x)));
+  if (greedy || top == -INFINITY) {
+    const int hot = __reduce_min_sync(0xffffffffu, of_cta.x == top ? first_of.x : 0x7fffffff);
+    for (int i = tid; i < n; i += kThreads) out[i] = top > -INFINITY && first + i == hot ? 1.f : 0.f;
+    return;
+  }
+  const RowState row = {x, first, 4 * n4, rank, n_ctas, top, ord(top + 0.f), c, a.status};
+  Upto upto = {-INFINITY, 0x7fffffff};
+  unsigned long long kept = 0;
+  int turn = 0, turn2 = 0;
+  if (set.top_k) {
+    // Bins from the maximum down to the least of the threads' maxima, where there are top_k
+    // of these (so many tokens are not below it); else as for the masses.
+    const float low = from_ord(__reduce_min_sync(0xffffffffu, ord(of_cta.y)));
+    const bool enough = set.top_k <= __reduce_add_sync(0xffffffffu, first_of.y);
+    upto = last_kept<false>(row, set.top_k, 1.f, upto,
+                            enough ? fminf((kBins - 2) / (top - low), 1e30f) : c.hi * kBinsPerOctave,
+                            enough ? low : -INFINITY, turn, turn2, h, s, &kept);
+  }
+  float inv;
+  if (set.top_p < 1.f) {
+    upto = last_kept<true>(row, 0, set.top_p, upto, c.hi * kBinsPerOctave, top - 46.f / c.hi * 1.0001f, turn, turn2, h,
+                           s, &kept);
+    inv = 1.f / (__ull2float_rn(kept) * 0x1p-44f);
+  } else {
+    float sum = 0.f;
+    for (int g0 = warp * 32; g0 < n4; g0 += kThreads) {
+      const int g = g0 + lane;
+      float4 q = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+      if (g < n4) q = x4[g];
+      const float v[4] = {q.x, q.y, q.z, q.w};
+      bool in[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) in[e] = upto.has(v[e], 4 * g + e);
+      if (!__any_sync(0xffffffffu, in[0] || in[1] || in[2] || in[3])) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += in[e] ? weight(v[e], top, c) : 0.f;
+    }
+    sum = warp_sum(sum);
+    if (lane == 0) s.red[warp] = sum;
+    __syncthreads();
+    if (warp == 0) {
+      sum = warp_sum(lane < kWarps ? s.red[lane] : 0.f);
+      if (lane < n_ctas) send(&box.kept[rank], bits_of(sum, 0.f), &box.bar[5], lane, n_ctas);
+    }
+    if (!arrived(&box.bar[5], 0, n_ctas, a.status)) return;
+    sum = 0.f;
+    for (int q = 0; q < n_ctas; ++q) sum += __uint_as_float(static_cast<unsigned>(box.kept[q]));
+    inv = 1.f / sum;
+  }
+  auto prob = [&](float v, int i) { return upto.has(v, i) ? weight(v, top, c) * inv : 0.f; };
+  if (V4) {
+    for (int g = tid; g < n4; g += kThreads) {
+      const float4 q = x4[g];
+      const int i = 4 * g;
+      const float4 p = make_float4(prob(q.x, i), prob(q.y, i + 1), prob(q.z, i + 2), prob(q.w, i + 3));
+      if (i + 4 <= n) {
+        *reinterpret_cast<float4*>(out + i) = p;
+      } else {
+        out[i] = p.x;
+        if (i + 1 < n) out[i + 1] = p.y;
+        if (i + 2 < n) out[i + 2] = p.z;
+      }
+    }
+  } else {
+    for (int i = tid; i < n; i += kThreads) out[i] = prob(x[i], i);
+  }
+}
+
+constexpr int kSlice = 16384;   // logits of a CTA where its row may have up to kMaxCtas: two CTAs an SM
+
+template <typename T, bool V4>
+cudaError_t launch_cut(const TokenProbsArgs& a, cudaStream_t s) {
+  static PerDevice per_device;
+  per_device.once([&] {
+    cudaFuncSetAttribute(token_probs_cut_kernel<T, V4>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                         kMaxVocab / kMaxCtas * static_cast<int>(sizeof(float)) + static_cast<int>(sizeof(Cuts)));
+  });
+  int ctas = 1;
+  while (ctas < kMaxCtas && (ctas * kSlice < a.vocab || (static_cast<int64_t>(a.n_rows) * ctas < 152 && a.vocab / ctas > 4096)))
+    ctas *= 2;
+  return launch_rows(token_probs_cut_kernel<T, V4>, a, ctas, kThreads, sizeof(Cuts), sizeof(float), s);
+}
+template <typename T>
+cudaError_t launch_cut(const TokenProbsArgs& a, cudaStream_t s) {
+  return fours<T>(a) ? launch_cut<T, true>(a, s) : launch_cut<T, false>(a, s);
+}
+
+}  // namespace
+
+cudaError_t launch_probs_cut(const TokenProbsArgs& a, int dtype, cudaStream_t s) {
+  return dtype == DVI_BF16 ? launch_cut<__nv_bfloat16>(a, s) : launch_cut<float>(a, s);
+}
+
+}  // namespace dvi
