@@ -4,15 +4,20 @@
 // exp((x - max) / T), the kept tokens are a prefix of the order; it ends at the
 // last token whose rank is below top_k and before which the sum of w is below
 // top_p of the whole.  A row's slices lie in the shared memory of a cluster's CTAs.
-// The last kept token is found by a histogram of counts or of w over the logits: each
-// CTA gives the others its sums of 32 groups of 32 bins, then of the bins of the
-// group that the cut lies in, then its tokens of the bin, and each sorts these out for
-// itself.  Sums of w are whole numbers, so they do not depend on the order of the
-// atomics, and every CTA comes to the same end.  What the CTAs give each other are
-// stores that the receiver's barrier counts: no CTA waits for its own memory
-// operations, as at a cluster's barrier (three of which took a third of the time).
-// Where the bin has too many tokens (logits that are nearly equal), the token's place
-// in the order, as a number, is found 10 bits at a time.
+//
+// The last kept token is looked for in a histogram of the logits: how many tokens a
+// bin has and where in it they lie, which gives its sum of w to about 2^-14.  The CTAs
+// give each other their sums of 32 groups of 32 bins, then of the bins of the group in
+// which the cut should be.  Then each sums w exactly, as whole numbers: of all tokens,
+// of those before the bin, of those in it; these sums and the bin's tokens go to all.
+// They show whether the bin is the right one (else it is its neighbour's turn) and,
+// among its tokens, which is the last.  Every CTA comes to the same end, whatever the
+// order of its atomics.  Where the bin has too many tokens (logits that are nearly
+// equal), the token's place in the order, as a number, is found 10 bits at a time.
+//
+// What the CTAs give each other are stores that the receiver's barrier counts: no CTA
+// waits for its own memory operations, as at a cluster's barrier (three of which took
+// a third of the time).
 #include "token_probs.cuh"
 
 namespace dvi {
@@ -24,14 +29,16 @@ constexpr int kMaxCtas = kProbsCtas;
 constexpr int kBins = 1024;                      // 32 groups of 32
 constexpr int kBinBits = 10;
 constexpr int kPer = kBins / kThreads;
+constexpr int kSteps = 8;                        // places within a bin
 constexpr float kBinsPerOctave = 40.f;           // of w: the last bin has what is below 2^-25.6
 constexpr int kList = 1024;                      // tokens of a bin that are sorted out by each CTA
 constexpr int kListPer = kList / kThreads;
-constexpr int kFew = 64;                         // tokens that are compared with each other
+constexpr int kFew = 128;                        // tokens that are compared with each other, by four threads each
+constexpr int kTries = 3;                        // bins that are summed before the slow way is taken
 constexpr int kIndexBits = 18;                   // kMaxVocab
 
-// 2^(k / 32), k = 0 .. 31, as f32 pairs hi + lo.
-__constant__ float2 kExp2[32] = {
+// 2^(k / 32), k = 0 .. 31, as f32 pairs hi + lo.  (Not in constant memory, which gives one lane a time.)
+__device__ const float2 kExp2[32] = {
     {0x1p+0f, 0.f}, {0x1.059b0ep+0f, -0x1.9d4f52p-25f}, {0x1.0b5586p+0f, 0x1.9f3122p-25f}, {0x1.11301ep+0f, -0x1.fdb496p-25f},
     {0x1.172b84p+0f, -0x1.c15742p-27f}, {0x1.1d4874p+0f, -0x1.d2e8cap-25f}, {0x1.2387a6p+0f, 0x1.ceac48p-25f}, {0x1.29e9ep+0f, -0x1.5c0424p-25f},
     {0x1.306fep+0f, 0x1.4636e2p-25f}, {0x1.371a74p+0f, -0x1.18aac6p-25f}, {0x1.3dea64p+0f, 0x1.824684p-25f}, {0x1.44e086p+0f, 0x1.8624b4p-30f},
@@ -143,19 +150,20 @@ struct Cuts {
 
 // What the CTAs of a cluster send each other, by rank, and what counts it.
 struct Boxes {
-  unsigned long long bar[6];                    // of: peers, groups, bins, counts, the list, kept
+  unsigned long long bar[6];                    // of: peers, groups, bins, sums, the list, kept
   float2 top[kMaxCtas];                         // maximum, least of the threads' maxima
   int2 first[kMaxCtas];                         // first token of the maximum, how many threads have a maximum
-  unsigned long long group[kMaxCtas][33];       // sums of the groups of bins, and of all tokens
-  unsigned long long bin[kMaxCtas][32];
-  unsigned long long count[kMaxCtas];
-  unsigned long long kept[kMaxCtas];
+  float2 group[kMaxCtas][32];                   // sums of the groups of bins; .y of the first: how many tokens there are
+  float2 bin[kMaxCtas][32];
+  unsigned long long sum[2][4][kMaxCtas];       // (in turns) before the bin, in it, all; and how many are in it
+  float2 kept[kMaxCtas];
 };
 
 struct Small {
   Boxes box;
   float2 exp2_of[32];
-  unsigned long long part[kWarps], least[kWarps], most[kWarps], group[32];
+  unsigned long long part[3][kWarps], least[kWarps], most[kWarps];
+  float group[32];
   float red[kWarps], low[kWarps];
   int first[kWarps], some[kWarps];
   int n_list, n_kept, found;
@@ -177,11 +185,13 @@ struct RowState {
   __device__ __forceinline__ float logit(unsigned long long place) const {
     return from_ord(top - static_cast<uint32_t>(place >> kIndexBits));
   }
-  // (rounded by adding 1.5 * 2^23)
-  __device__ __forceinline__ int bin(float v, float scale) const {
+  // The place in the histogram, down from the maximum: kSteps of them a bin, `scale` a unit
+  // (rounded by adding 1.5 * 2^23).
+  __device__ __forceinline__ int step(float v, float scale) const {
     const float t = __fmul_rn(__fsub_rn(m, v), scale);
-    return __float_as_int(__fadd_rn(fminf(t, static_cast<float>(kBins - 1)), 12582912.f)) & 0xffff;
+    return __float_as_int(__fadd_rn(fminf(t, static_cast<float>(kBins * kSteps - 1)), 12582912.f)) & 0xffff;
   }
+  __device__ __forceinline__ int bin(float v, float scale) const { return step(v, scale) / kSteps; }
 };
 
 // Eight bytes to the box of CTA r, counted by its barrier.
@@ -242,11 +252,11 @@ __device__ __noinline__ int find_bin(unsigned long long before, unsigned long lo
     v[1] += sum_of(d[0].y, d[1].y, d[2].y);
   }
   const unsigned long long sum = v[0] + v[1], incl = warp_scan_u64(sum);
-  if (lane == 31) s.part[warp] = incl;
+  if (lane == 31) s.part[0][warp] = incl;
   if (tid == 0) s.found = -1;
   __syncthreads();
   unsigned long long at = before + incl - sum;
-  for (int w = 0; w < warp; ++w) at += s.part[w];
+  for (int w = 0; w < warp; ++w) at += s.part[0][w];
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
     if (at < target && at + v[j] >= target) s.found = tid * kPer + j, s.excl = at;
@@ -299,12 +309,15 @@ __device__ unsigned long long last_of_list(int n, unsigned long long before, uns
     n = s.n_kept;
     __syncthreads();
   }
-  if (tid < n) {
-    const unsigned long long p = h.key[tid], v = MASS ? h.mass[tid] : 1;
-    unsigned long long sum = before;
-    for (int j = 0; j < n; ++j)
+  {
+    const int i = tid >> 2;
+    const unsigned long long p = i < n ? h.key[i] : 0, v = i < n && MASS ? h.mass[i] : 1;
+    unsigned long long sum = 0;
+    for (int j = tid & 3; j < n; j += 4)
       if (h.key[j] < p) sum += MASS ? h.mass[j] : 1;
-    if (sum < target && sum + v >= target) s.cut = p, s.kept = sum + v;
+    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 2) + before;
+    if ((tid & 3) == 0 && i < n && sum < target && sum + v >= target) s.cut = p, s.kept = sum + v;
   }
   __syncthreads();
   *kept = s.kept;
@@ -333,147 +346,233 @@ struct Upto {
   __device__ __forceinline__ bool has(float v, int at) const { return v > x || (v == x && at <= i); }
 };
 
+// First of the lanes up to which the numbers reach target (the last that is above 0, where rounding leaves
+// it past all), and the sum before it.
+__device__ __forceinline__ int first_reaching(float v, float target, float* before) {
+  const int lane = threadIdx.x & 31;
+  float incl = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const float w = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += w;
+  }
+  incl += *before;
+  const unsigned at = __ballot_sync(0xffffffffu, v > 0.f && incl >= target), some = __ballot_sync(0xffffffffu, v > 0.f);
+  if (!some) return -1;
+  const int l = at ? __ffs(at) - 1 : 31 - __clz(some);
+  *before = __shfl_sync(0xffffffffu, incl - v, l);
+  return l;
+}
+
 // The last kept token among those up to `upto`: before it the counts sum to less than top_k, or
 // (MASS) the masses to less than top_p of all.  Returns the tokens up to it.  *kept: their sum.
-// Bins go down from the maximum, `scale` of them a unit; tokens below `low` are known to be cut.
-// turn, turn2: how often the first barrier of the boxes has been used, and the others.
+// Tokens below `low` are known to be cut (or, MASS, to be 0).  turn[]: how often the barriers of
+// the groups, of the bins, of the sums and the list have been used.
 template <bool MASS>
-__device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto, float scale, float low, int& turn,
-                          int& turn2, Cuts& h, Small& s, unsigned long long* kept) {
+__device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto, float scale, float low, int (&turn)[3],
+                          Cuts& h, Small& s, unsigned long long* kept) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n_ctas = row.n_ctas, rank = row.rank;
   const float4* x4 = reinterpret_cast<const float4*>(row.x);
   const int n4 = row.n / 4;
+  const bool all_of_them = upto.x == -INFINITY;
   Boxes& box = s.box;
-  if (tid == 0) {
-    expect(&box.bar[1], n_ctas * 33 * 8, n_ctas);
-    s.n_list = 0;
-  }
-  clear_bins(h);
-  unsigned long long all = 0;
+  if (tid == 0) expect(&box.bar[1], n_ctas * 32 * 8, n_ctas);
+  for (int i = tid; i < kBins; i += kThreads) h.digit[0][i] = 0;
+  __syncthreads();
+  int some = 0;
   for (int g0 = warp * 32; g0 < n4; g0 += kThreads) {
     const int g = g0 + lane;
     float4 q = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
     if (g < n4) q = x4[g];
     const float v[4] = {q.x, q.y, q.z, q.w};
-    if (MASS) {
-      // (a mass is 0 below 2^-46, which is `low` here)
-      bool in[4];
+    bool in[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) in[e] = v[e] >= low && upto.has(v[e], 4 * g + e);
-      if (!__any_sync(0xffffffffu, in[0] || in[1] || in[2] || in[3])) continue;
-      const Masses a = mass2(v[0], v[1], row.m, row.c, s.exp2_of), b = mass2(v[2], v[3], row.m, row.c, s.exp2_of);
-      const unsigned long long w[4] = {in[0] ? a.a : 0, in[1] ? a.b : 0, in[2] ? b.a : 0, in[3] ? b.b : 0};
+    for (int e = 0; e < 4; ++e) in[e] = v[e] >= low && (all_of_them ? v[e] > -INFINITY : upto.has(v[e], 4 * g + e));
+    if (!__any_sync(0xffffffffu, in[0] || in[1] || in[2] || in[3])) continue;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        all += w[e];
-        const int bin = row.bin(v[e], scale);
-        if (w[e] && bin < kBins - 1) add_to_bin(h, bin, w[e]);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const bool some = v[e] > -INFINITY;
-        all += some;
-        const int bin = row.bin(v[e], scale);
-        if (some && v[e] >= low && bin < kBins - 1) atomicAdd(&h.digit[0][bin], 1u);
-      }
+    for (int e = 0; e < 4; ++e) {
+      some += in[e];
+      const int step = row.step(v[e], scale);
+      if (in[e] && step < (kBins - 1) * kSteps)
+        atomicAdd(&h.digit[0][step / kSteps], MASS ? (1u << 17) + step % kSteps : 1u);
     }
   }
-  all = warp_sum_u64(all);
-  if (lane == 0) s.part[warp] = all;
+  some = __reduce_add_sync(0xffffffffu, some);
+  if (lane == 0) s.some[warp] = some;
   __syncthreads();
-  // the groups' sums to all
+  // The groups' sums to all.  A token in place q of the histogram has w = 2^(-q / (kSteps kBinsPerOctave)),
+  // which is nearly linear over a bin.  (2^15 tokens of one CTA in a bin are counted as none: then
+  // another bin is tried, in vain.)
+  auto bin_value = [&](int b) {
+    const unsigned d = h.digit[0][b];
+    if (!MASS) return static_cast<float>(d);
+    const float count = static_cast<float>(d >> 17), steps = static_cast<float>(d & 0x1ffffu), step = 1.f / (kSteps * kBinsPerOctave);
+    return exp2f(-b * (1.f / kBinsPerOctave)) * fmaf(steps, -0.69314718f * step, count);
+  };
 #pragma unroll
   for (int j = 0; j < 32 / kWarps; ++j) {
     const int g = warp * (32 / kWarps) + j;
-    const unsigned long long v = warp_sum_u64(bin_sum(h, 32 * g + lane));
+    const float v = warp_sum(bin_value(32 * g + lane));
     if (lane == 0) s.group[g] = v;
   }
   __syncthreads();
-  if (tid < 33) {
-    unsigned long long v = 0;
-    if (tid < 32) v = s.group[tid];
-    else
-      for (int w = 0; w < kWarps; ++w) v += s.part[w];
-    for (int r = 0; r < n_ctas; ++r) send(&box.group[rank][tid], v, &box.bar[1], r, n_ctas);
+  if (warp == 0) {
+    const int here = __reduce_add_sync(0xffffffffu, lane < kWarps ? s.some[lane] : 0);
+    const unsigned long long v = bits_of(s.group[lane], static_cast<float>(here));
+    for (int r = 0; r < n_ctas; ++r) send(&box.group[rank][lane], v, &box.bar[1], r, n_ctas);
   }
-  if (!arrived(&box.bar[1], turn++, n_ctas, row.status)) return upto;
-  unsigned long long v = 0, total = 0;
-  for (int r = 0; r < n_ctas; ++r) {
-    v += box.group[r][lane];
-    total += box.group[r][32];
+  if (!arrived(&box.bar[1], turn[0]++, n_ctas, row.status)) return upto;
+  float v = 0.f, tokens = 0.f;
+#pragma unroll
+  for (int r = 0; r < kMaxCtas; ++r) {
+    const float2 p = r < n_ctas ? box.group[r][lane] : make_float2(0.f, 0.f);
+    v += p.x;
+    tokens += p.y;
   }
-  *kept = total;
-  const unsigned long long target = MASS ? share_of(top_p, total) : top_k;
-  if (total < target) return upto;   // (fewer tokens than top_k)
-  unsigned long long incl = warp_scan_u64(v);
-  unsigned at = __ballot_sync(0xffffffffu, incl >= target);
-  int n = kList + 1;
-  unsigned long long before = 0;
-    int bin = -1;
-  if (at) {
-    // the bins of the group in which the cut is, to all
-    const int g = __ffs(at) - 1;
-    before = __shfl_sync(0xffffffffu, incl - v, g);
-    if (tid == 0) {
-      expect(&box.bar[2], n_ctas * 32 * 8, n_ctas);
-      expect(&box.bar[3], n_ctas * 8, n_ctas);
-    }
+  if (!MASS && tokens < top_k) return upto;   // (fewer tokens than top_k)
+  const float all_bins = warp_sum(v), about = MASS ? top_p * all_bins : static_cast<float>(top_k);
+  float before_it = 0.f;
+  const int group = all_bins >= about ? first_reaching(v, about, &before_it) : -1;
+  int bin = -1, n = kList + 1;
+  unsigned long long before = 0, target = top_k;
+  const int cap = kList / n_ctas;
+  if (group >= 0) {
+    // the bins of the group in which the cut should be, to all
+    if (tid == 0) expect(&box.bar[2], n_ctas * 32 * 8, n_ctas);
     if (warp == 0) {
-      const unsigned long long mine = bin_sum(h, 32 * g + lane);
+      const unsigned long long mine = bits_of(bin_value(32 * group + lane), 0.f);
       for (int r = 0; r < n_ctas; ++r) send(&box.bin[rank][lane], mine, &box.bar[2], r, n_ctas);
     }
-    if (!arrived(&box.bar[2], turn2, n_ctas, row.status)) return upto;
-    v = 0;
-    for (int r = 0; r < n_ctas; ++r) v += box.bin[r][lane];
-    incl = before + warp_scan_u64(v);
-    at = __ballot_sync(0xffffffffu, incl >= target);
-    bin = 32 * g + __ffs(at) - 1;
-    before = __shfl_sync(0xffffffffu, incl - v, __ffs(at) - 1);
-    // and the tokens of the bin
-    const int cap = kList / n_ctas;
-    for (int g = tid; g < n4; g += kThreads) {
-      const float4 q = x4[g];
+    if (!arrived(&box.bar[2], turn[1]++, n_ctas, row.status)) return upto;
+    v = 0.f;
+#pragma unroll
+    for (int r = 0; r < kMaxCtas; ++r) v += r < n_ctas ? box.bin[r][lane].x : 0.f;
+    bin = first_reaching(v, about, &before_it);
+    if (bin >= 0) bin += 32 * group;
+    before = static_cast<unsigned long long>(before_it);   // (of counts, which are exact)
+  }
+  for (int tries = 0; bin >= 0 && tries < kTries; ++tries) {
+    // Sums of the tokens before the bin, in it and of all, and its tokens, to all.  Logits past `above`
+    // are before it, below `under` behind it, by more than what rounding may do.
+    const float width = kSteps / scale;
+    const float above_it = row.m - (bin - 0.25f) * width, under_it = row.m - (bin + 1.25f) * width;
+    const float above = above_it + 0x1p-21f * fmaxf(fabsf(row.m), fabsf(above_it)),
+                under = under_it - 0x1p-21f * fmaxf(fabsf(row.m), fabsf(under_it));
+    if (tid == 0) {
+      expect(&box.bar[3], n_ctas * 4 * 8, n_ctas);
+      s.n_list = 0;
+    }
+    __syncthreads();
+    unsigned long long sum[3] = {0, 0, 0};
+    for (int g0 = warp * 32; g0 < n4; g0 += kThreads) {
+      const int g = g0 + lane;
+      float4 q = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+      if (g < n4) q = x4[g];
       const float v[4] = {q.x, q.y, q.z, q.w};
+      bool in[4], near[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (row.bin(v[e], scale) != bin || !(v[e] >= low) || !upto.has(v[e], 4 * g + e)) continue;
+        in[e] = v[e] >= low && (all_of_them ? v[e] > -INFINITY : upto.has(v[e], 4 * g + e));
+        near[e] = in[e] && v[e] >= under && !(v[e] > above);
+      }
+      if (!__any_sync(0xffffffffu, MASS ? in[0] || in[1] || in[2] || in[3] : near[0] || near[1] || near[2] || near[3]))
+        continue;
+      unsigned long long w[4] = {1, 1, 1, 1};
+      if (MASS) {
+        const Masses a = mass2(v[0], v[1], row.m, row.c, s.exp2_of), b = mass2(v[2], v[3], row.m, row.c, s.exp2_of);
+        w[0] = a.a, w[1] = a.b, w[2] = b.a, w[3] = b.b;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (!in[e]) w[e] = 0;
+          sum[2] += w[e];
+          if (v[e] > above) sum[0] += w[e];
+        }
+      }
+      if (!__any_sync(0xffffffffu, near[0] || near[1] || near[2] || near[3])) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (!near[e]) continue;
+        const int b = row.bin(v[e], scale);
+        if (MASS && b < bin) sum[0] += w[e];
+        if (b != bin) continue;
+        sum[1] += w[e];
         const int to = atomicAdd(&s.n_list, 1);
         if (to >= cap) continue;
         const unsigned long long p = row.place(v[e], 4 * g + e);
         for (int r = 0; r < n_ctas; ++r) send(&h.box[rank * cap + to], p, &box.bar[4], r, n_ctas);
       }
     }
-    __syncthreads();
-    if (tid < n_ctas) send(&box.count[rank], s.n_list, &box.bar[3], tid, n_ctas);
-    if (!arrived(&box.bar[3], turn2, n_ctas, row.status)) return upto;
-    // how many each CTA has found, a lane a CTA; the warps share the CTAs' lists
-    const int there = lane < n_ctas ? static_cast<int>(box.count[lane]) : 0;
-    const int most = __reduce_max_sync(0xffffffffu, there);
-    n = most > cap ? kList + 1 : __reduce_add_sync(0xffffffffu, there);
-    const int sent = __reduce_add_sync(0xffffffffu, min(there, cap));
-    if (tid == 0) expect(&box.bar[4], sent * 8, n_ctas);
-    if (!arrived(&box.bar[4], turn2, n_ctas, row.status)) return upto;
-    ++turn2;
-    if (n <= kList) {
-      const int per = kWarps / n_ctas, from = warp / per;
-      int before_it = lane < from ? there : 0;
-      before_it = __reduce_add_sync(0xffffffffu, before_it);
-      const int m = __shfl_sync(0xffffffffu, there, from);
-      for (int i = warp % per * 32 + lane; i < m; i += per * 32) {
-        const unsigned long long p = h.box[from * cap + i];
-        h.key[before_it + i] = p;
-        if (MASS) h.mass[before_it + i] = mass(row.logit(p), row.m, row.c, s.exp2_of);
+    if (MASS) {
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        sum[k] = warp_sum_u64(sum[k]);
+        if (lane == 0) s.part[k][warp] = sum[k];
       }
-      __syncthreads();
     }
+    __syncthreads();
+    if (warp < 4) {
+      unsigned long long v = s.n_list;
+      if (warp < 3) v = MASS ? warp_sum_u64(lane < kWarps ? s.part[warp][lane] : 0) : 0;
+      if (lane < n_ctas) send(&box.sum[turn[2] & 1][warp][rank], v, &box.bar[3], lane, n_ctas);
+    }
+    if (!arrived(&box.bar[3], turn[2], n_ctas, row.status)) return upto;
+    // (a lane a CTA)
+    const int there = lane < n_ctas ? static_cast<int>(box.sum[turn[2] & 1][3][lane]) : 0;
+    const int sent = __reduce_add_sync(0xffffffffu, min(there, cap));
+    n = __reduce_max_sync(0xffffffffu, there) > cap ? kList + 1 : sent;
+    if (tid == 0) expect(&box.bar[4], sent * 8, n_ctas);
+    bool here = true;
+    if (MASS) {
+      unsigned long long in_it = 0, all = 0;
+      before = 0;
+#pragma unroll
+      for (int r = 0; r < kMaxCtas; ++r) {
+        if (r >= n_ctas) continue;
+        const auto& sums = box.sum[turn[2] & 1];
+        before += sums[0][r];
+        in_it += sums[1][r];
+        all += sums[2][r];
+      }
+      target = share_of(top_p, all);
+      here = before < target && before + in_it >= target;
+      if (!here) bin = before >= target ? bin - 1 : bin < kBins - 2 ? bin + 1 : -1;
+    }
+    if (!arrived(&box.bar[4], turn[2]++, n_ctas, row.status)) return upto;
+    if (here) break;
+    n = kList + 1;
+    __syncthreads();   // (before the list is begun again)
   }
   unsigned long long cut;
   if (n <= kList) {
+    // the warps share the CTAs' lists
+    const int there = lane < n_ctas ? static_cast<int>(box.sum[(turn[2] - 1) & 1][3][lane]) : 0;
+    const int per = kWarps / n_ctas, from = warp / per;
+    const int before_them = __reduce_add_sync(0xffffffffu, lane < from ? there : 0);
+    const int m = __shfl_sync(0xffffffffu, there, from);
+    for (int i = warp % per * 32 + lane; i < m; i += per * 32) {
+      const unsigned long long p = h.box[from * cap + i];
+      h.key[before_them + i] = p;
+      if (MASS) h.mass[before_them + i] = mass(row.logit(p), row.m, row.c, s.exp2_of);
+    }
+    __syncthreads();
     cut = last_of_list<MASS>(n, before, target, rank, h, s, kept);
   } else {
-    before = cut = 0;
     cg::cluster_group cluster = cg::this_cluster();
+    if (MASS) {
+      // (the sum of all, where no bin was looked at)
+      unsigned long long all = 0;
+      for (int i = tid; i < row.n; i += kThreads)
+        if (row.x[i] >= low && upto.has(row.x[i], i)) all += mass(row.x[i], row.m, row.c, s.exp2_of);
+      all = warp_sum_u64(all);
+      __syncthreads();
+      if (lane == 0) s.part[1][warp] = all;
+      cluster_barrier(n_ctas);
+      all = 0;
+      for (int r = 0; r < n_ctas; ++r)
+        for (int w = 0; w < kWarps; ++w) all += cluster.map_shared_rank(&s, r)->part[1][w];
+      target = share_of(top_p, all);
+    }
+    before = cut = 0;
     for (int shift = 32 + kIndexBits - kBinBits;; shift = shift > kBinBits ? shift - kBinBits : 0) {
       __syncthreads();
       clear_bins(h);
@@ -522,6 +621,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
   const T* in = static_cast<const T*>(a.x) + r * a.ld + first;
   float* out = a.out + r * a.ld_out + first;
 
+  if (tid < 32) s.exp2_of[tid] = kExp2[tid];
   float own = -INFINITY, odd = 0.f;   // odd: 0 of finite logits
   constexpr int kFly = 16;
   if (V4) {
@@ -568,7 +668,6 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
   const Settings set(a, r);
   const bool greedy = set.temperature == 0.f;
   const Slope c(set.temperature);
-  if (tid < 32) s.exp2_of[tid] = kExp2[tid];
   // the tokens that the thread has loaded
   auto each = [&](auto f) {
     if (V4) {
@@ -632,20 +731,21 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
   const RowState row = {x, first, 4 * n4, rank, n_ctas, top, ord(top + 0.f), c, a.status};
   Upto upto = {-INFINITY, 0x7fffffff};
   unsigned long long kept = 0;
-  int turn = 0, turn2 = 0;
+  int turn[3] = {0, 0, 0};
   if (set.top_k) {
     // Bins from the maximum down to the least of the threads' maxima, where there are top_k
     // of these (so many tokens are not below it); else as for the masses.
     const float low = from_ord(__reduce_min_sync(0xffffffffu, ord(of_cta.y)));
     const bool enough = set.top_k <= __reduce_add_sync(0xffffffffu, first_of.y);
     upto = last_kept<false>(row, set.top_k, 1.f, upto,
-                            enough ? fminf((kBins - 2) / (top - low), 1e30f) : c.hi * kBinsPerOctave,
-                            enough ? low : -INFINITY, turn, turn2, h, s, &kept);
+                            enough ? fminf((kBins - 2) * kSteps / (top - low), 1e30f) : c.hi * (kSteps * kBinsPerOctave),
+                            enough ? low : -INFINITY, turn, h, s, &kept);
   }
   float inv;
   if (set.top_p < 1.f) {
-    upto = last_kept<true>(row, 0, set.top_p, upto, c.hi * kBinsPerOctave, top - 46.f / c.hi * 1.0001f, turn, turn2, h,
-                           s, &kept);
+    // (a mass is 0 below 2^-46)
+    upto = last_kept<true>(row, 0, set.top_p, upto, c.hi * (kSteps * kBinsPerOctave), top - 46.f / c.hi * 1.0001f, turn,
+                           h, s, &kept);
     inv = 1.f / (__ull2float_rn(kept) * 0x1p-44f);
   } else {
     float sum = 0.f;
@@ -670,7 +770,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
     }
     if (!arrived(&box.bar[5], 0, n_ctas, a.status)) return;
     sum = 0.f;
-    for (int q = 0; q < n_ctas; ++q) sum += __uint_as_float(static_cast<unsigned>(box.kept[q]));
+    for (int q = 0; q < n_ctas; ++q) sum += box.kept[q].x;
     inv = 1.f / sum;
   }
   auto prob = [&](float v, int i) { return upto.has(v, i) ? weight(v, top, c) * inv : 0.f; };
