@@ -6,14 +6,15 @@
 // top_p of the whole.  A row's slices lie in the shared memory of a cluster's CTAs.
 //
 // The last kept token is looked for in a histogram of the logits: how many tokens a
-// bin has and where in it they lie, which gives its sum of w to about 2^-14.  The CTAs
+// bin has and where in it they lie, which gives its sum of w to about 2^-15.  The CTAs
 // give each other their sums of 32 groups of 32 bins, then of the bins of the group in
 // which the cut should be.  Then each sums w exactly, as whole numbers: of all tokens,
 // of those before the bin, of those in it; these sums and the bin's tokens go to all.
 // They show whether the bin is the right one (else it is its neighbour's turn) and,
 // among its tokens, which is the last.  Every CTA comes to the same end, whatever the
-// order of its atomics.  Where the bin has too many tokens (logits that are nearly
-// equal), the token's place in the order, as a number, is found 10 bits at a time.
+// order of its atomics.  Where top_k leaves few tokens, all of these go to all instead,
+// which is all that top_p needs, too.  Where the bin has too many tokens (logits that are
+// nearly equal), the token's place in the order, as a number, is found 10 bits at a time.
 //
 // What the CTAs give each other are stores that the receiver's barrier counts: no CTA
 // waits for its own memory operations, as at a cluster's barrier (three of which took
@@ -29,7 +30,7 @@ constexpr int kMaxCtas = kProbsCtas;
 constexpr int kBins = 1024;                      // 32 groups of 32
 constexpr int kBinBits = 10;
 constexpr int kPer = kBins / kThreads;
-constexpr int kSteps = 8;                        // places within a bin
+constexpr int kSteps = 1024;                     // places within a bin
 constexpr float kBinsPerOctave = 40.f;           // of w: the last bin has what is below 2^-25.6
 constexpr int kList = 1024;                      // tokens of a bin that are sorted out by each CTA
 constexpr int kListPer = kList / kThreads;
@@ -37,93 +38,88 @@ constexpr int kFew = 128;                        // tokens that are compared wit
 constexpr int kTries = 3;                        // bins that are summed before the slow way is taken
 constexpr int kIndexBits = 18;                   // kMaxVocab
 
-// 2^(k / 32), k = 0 .. 31, as f32 pairs hi + lo.  (Not in constant memory, which gives one lane a time.)
-__device__ const float2 kExp2[32] = {
-    {0x1p+0f, 0.f}, {0x1.059b0ep+0f, -0x1.9d4f52p-25f}, {0x1.0b5586p+0f, 0x1.9f3122p-25f}, {0x1.11301ep+0f, -0x1.fdb496p-25f},
-    {0x1.172b84p+0f, -0x1.c15742p-27f}, {0x1.1d4874p+0f, -0x1.d2e8cap-25f}, {0x1.2387a6p+0f, 0x1.ceac48p-25f}, {0x1.29e9ep+0f, -0x1.5c0424p-25f},
-    {0x1.306fep+0f, 0x1.4636e2p-25f}, {0x1.371a74p+0f, -0x1.18aac6p-25f}, {0x1.3dea64p+0f, 0x1.824684p-25f}, {0x1.44e086p+0f, 0x1.8624b4p-30f},
-    {0x1.4bfdaep+0f, -0x1.593abcp-25f}, {0x1.5342b6p+0f, -0x1.2c561p-25f}, {0x1.5ab07ep+0f, -0x1.5bd5ecp-27f}, {0x1.6247ecp+0f, -0x1.f8b55p-25f},
-    {0x1.6a09e6p+0f, 0x1.9fcef4p-26f}, {0x1.71f75ep+0f, 0x1.1d8beep-25f}, {0x1.7a1148p+0f, -0x1.829fdp-25f}, {0x1.82589ap+0f, -0x1.accc7cp-26f},
-    {0x1.8ace54p+0f, 0x1.15506ep-27f}, {0x1.93737cp+0f, -0x1.e64744p-25f}, {0x1.9c4918p+0f, 0x1.51f848p-27f}, {0x1.a5503cp+0f, -0x1.b83b54p-25f},
-    {0x1.ae89fap+0f, -0x1.a94b14p-26f}, {0x1.b7f77p+0f, -0x1.a09438p-25f}, {0x1.c199bep+0f, -0x1.3d56b2p-27f}, {0x1.cb720ep+0f, -0x1.8837ccp-27f},
-    {0x1.d5818ep+0f, -0x1.822dbcp-27f}, {0x1.dfc974p+0f, -0x1.908c94p-25f}, {0x1.ea4afap+0f, 0x1.52486cp-27f}, {0x1.f50766p+0f, -0x1.246ebp-26f}};
-
-// Two f32 numbers in one register pair: an operation on both is one instruction.
-struct Two {
-  unsigned long long v;
+// Numbers T_k near 2^(k / kPowers) that are f32 numbers themselves, and how far log2 T_k is from
+// k / kPowers: so 2^t = T_k 2^(t - k / kPowers - d_k) without a second number for T_k.
+constexpr int kPowers = 512;
+struct Powers {
+  float2 of[kPowers];
 };
-__device__ __forceinline__ Two two(float a, float b) {
-  Two r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
-  return r;
+// e^x and the logarithm of numbers near 1 by their series, in 64 bits.
+constexpr double series_exp(double x) {
+  double sum = 1.0, term = 1.0;
+  for (int i = 1; i < 30; ++i) sum += term *= x / i;
+  return sum;
 }
-__device__ __forceinline__ Two two(float a) { return two(a, a); }
-__device__ __forceinline__ float2 split(Two a) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
-  return r;
+constexpr double series_log1p(double x) {
+  double sum = 0.0, term = 1.0;
+  for (int i = 1; i < 6; ++i) sum += (term *= x) / (i % 2 ? i : -i);
+  return sum;
 }
-__device__ __forceinline__ Two operator+(Two a, Two b) {
-  Two r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
+constexpr Powers make_powers() {
+  constexpr double ln2 = 0.69314718055994530942;
+  Powers p{};
+  for (int k = 0; k < kPowers; ++k) {
+    const double t = series_exp(k * (ln2 / kPowers));
+    p.of[k].x = static_cast<float>(t);
+    p.of[k].y = static_cast<float>(series_log1p((static_cast<double>(p.of[k].x) - t) / t) / ln2);
+  }
+  return p;
 }
-__device__ __forceinline__ Two operator*(Two a, Two b) {
-  Two r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
-  Two r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
-}
-__device__ __forceinline__ Two operator-(Two a, Two b) { return fma2(b, two(-1.f), a); }   // (the product is exact)
+__device__ const Powers kPowersOf2 = make_powers();
 
-// w of two logits in units of 2^-44, off by about 2^-38; 0 below 2^-46.  x - m and its
-// product t with the slope are f32 pairs; t = q / 32 + r, 2^(q / 32) comes from the table and an
-// exponent, and 2^r = e^z = 1 + z + z^2 (1/2 + z/6 + z^2/24 + z^3/120) with |z| <= ln 2 / 64, of
-// which only 1 + z needs the second number.  Adding 1.5 * 2^23 rounds to whole numbers and leaves
-// them in the low bits.
-struct Masses {
-  unsigned long long a, b;
+// w in units of 2^-44, off by about 2^-34 of itself; 0 below 2^-46 (low: where that is, or above).
+// x - m and its product t with the slope are f32 pairs; t = q / kPowers + u, 2^(q / kPowers) comes from
+// the table and an exponent, and 2^u - 1 = u ln 2 + ... is small enough for one number.  Adding
+// 1.5 * 2^23 rounds to whole numbers and leaves them in the low bits: 22 bits of w, then 22 more.
+struct Weigher {
+  float m;
+  Slope c;
+  const float2* powers;
+  // The two halves, each beside kBits.
+  static constexpr unsigned kBits = 0x4b400000u;   // of 1.5 * 2^23
+  __device__ __forceinline__ void halves(float x, unsigned& high, unsigned& rest) const {
+    const float kRound = 12582912.f;
+    const float dh = __fsub_rn(x, m), back = __fsub_rn(dh, x);
+    const float dl = __fsub_rn(__fsub_rn(x, __fsub_rn(dh, back)), __fadd_rn(m, back));
+    const float th = __fmul_rn(dh, c.hi);
+    const float tl = fmaf(dl, c.hi, fmaf(dh, c.lo, fmaf(dh, c.hi, -th)));
+    const float q = fmaf(th, static_cast<float>(kPowers), kRound);
+    const float r = fmaf(__fsub_rn(q, kRound), -1.f / kPowers, th);
+    const unsigned bits = __float_as_uint(q);
+    const float2 power = powers[bits % kPowers];
+    const float u = __fadd_rn(r, __fsub_rn(tl, power.y));
+    const float p = u * fmaf(u, fmaf(u, 0.055504109f, 0.24022651f), 0.69314718f);
+    // (kPowers = 2^9: q / kPowers to the exponent's place, where what 1.5 * 2^23 leaves has gone)
+    const float h = __uint_as_float(__float_as_uint(power.x) + (22u << 23) + ((bits & ~(kPowers - 1u)) << 14));
+    const float hp = fmaf(h, p, h);
+    const float a = __fadd_rn(hp, kRound);
+    const float left = __fadd_rn(__fsub_rn(hp, __fsub_rn(a, kRound)), fmaf(h, p, __fsub_rn(h, hp)));
+    high = __float_as_uint(a);
+    rest = __float_as_uint(fmaf(left, 4194304.f, kRound));
+  }
+  __device__ __forceinline__ static unsigned long long join(unsigned high, unsigned rest) {
+    return static_cast<unsigned long long>(high - kBits) * 4194304ull + static_cast<long long>(static_cast<int>(rest - kBits));
+  }
+  __device__ __forceinline__ float low() const { return m - 46.f / c.hi * 1.0001f; }
 };
-__device__ __forceinline__ Masses mass2(float xa, float xb, float m, Slope c, const float2* exp2_of) {
-  const float kRound = 12582912.f, kLn2 = 0x1.62e430p-1f, kLn2Lo = -0x1.05c610p-29f;
-  const Two x = two(xa, xb), top = two(m), ch = two(c.hi);
-  const Two dh = x - top, back = dh - x;
-  const Two dl = (x - (dh - back)) - (top + back);
-  const Two th = dh * ch;
-  const Two tl = fma2(dh, two(c.lo), fma2(dl, ch, fma2(dh, ch, two(0.f) - th)));
-  const Two q = fma2(th, two(32.f), two(kRound)), r = fma2(q - two(kRound), two(-0.03125f), th);
-  const Two z = r * two(kLn2);
-  const Two zl = fma2(tl, two(kLn2), fma2(r, two(kLn2Lo), fma2(r, two(kLn2), two(0.f) - z)));
-  const Two poly = fma2(z, fma2(z, fma2(z, two(1.f / 120.f), two(1.f / 24.f)), two(1.f / 6.f)), two(0.5f));
-  const Two zz = z * z * poly;
-  const Two p = z + zz, pl = ((z - p) + zz) + fma2(z, zl, zl);
-  const float2 qs = split(q), ts = split(th);
-  const int qa = __float_as_int(qs.x), qb = __float_as_int(qs.y);
-  const float2 ta = exp2_of[qa & 31], tb = exp2_of[qb & 31];
-  const Two t = two(ta.x, tb.x), prod = t * p;
-  const Two e = fma2(t, p, two(0.f) - prod) + fma2(t, pl, two(ta.y, tb.y));
-  const Two hi = t + prod, lo = ((t - hi) + prod) + e;
-  // times 2^(n + 22), n = q >> 5 (the shift drops what 1.5 * 2^23 leaves above it): 22 bits, then
-  // 22 more of what they leave
-  const Two scale = two(__int_as_float(((qa >> 5) << 23) + ((22 + 127) << 23)),
-                        __int_as_float(((qb >> 5) << 23) + ((22 + 127) << 23)));
-  const Two h = hi * scale, u = h + two(kRound);
-  const Two rest = fma2(lo, scale, h - (u - two(kRound)));
-  const Two f = fma2(rest, two(4194304.f), two(kRound));
-  const float2 us = split(u), fs = split(f);
-  const int kBits = 0x4b400000;   // of 1.5 * 2^23
-  const long long wa = static_cast<long long>(__float_as_int(us.x) - kBits) * 4194304 + (__float_as_int(fs.x) - kBits);
-  const long long wb = static_cast<long long>(__float_as_int(us.y) - kBits) * 4194304 + (__float_as_int(fs.y) - kBits);
-  return {ts.x > -46.f ? static_cast<unsigned long long>(wa) : 0ull,
-          ts.y > -46.f ? static_cast<unsigned long long>(wb) : 0ull};
+__device__ __noinline__ unsigned long long mass_of(float x, float m, float c_hi, float c_lo, const float2* powers) {
+  Weigher w = {m, Slope(1.f), powers};
+  w.c.hi = c_hi, w.c.lo = c_lo;
+  unsigned high, rest;
+  w.halves(x, high, rest);
+  return x >= w.low() ? Weigher::join(high, rest) : 0;
 }
-__device__ __noinline__ unsigned long long mass(float x, float m, Slope c, const float2* exp2_of) {
-  return mass2(x, x, m, c, exp2_of).a;
-}
+// A sum of masses (kBits of every half are taken out at the end; sums may pass 64 bits until then).
+struct MassSum {
+  unsigned long long sum = 0;
+  unsigned n = 0;
+  __device__ __forceinline__ void add(unsigned high, unsigned rest) {
+    sum += high * 4194304ull;
+    sum += rest;
+    ++n;
+  }
+  __device__ __forceinline__ unsigned long long value() const { return sum - n * (Weigher::kBits * 4194305ull); }
+};
 
 __device__ __forceinline__ unsigned long long warp_sum_u64(unsigned long long v) {
 #pragma unroll
@@ -146,6 +142,7 @@ struct Cuts {
                                                 // and the atomics return nothing
   unsigned long long key[kList], mass[kList];   // the tokens of a bin
   unsigned long long box[kList];                // as the CTAs send them, kList / n_ctas of each
+  float2 powers[kPowers];
 };
 
 // What the CTAs of a cluster send each other, by rank, and what counts it.
@@ -161,7 +158,6 @@ struct Boxes {
 
 struct Small {
   Boxes box;
-  float2 exp2_of[32];
   unsigned long long part[3][kWarps], least[kWarps], most[kWarps];
   float group[32];
   float red[kWarps], low[kWarps];
@@ -179,17 +175,21 @@ struct RowState {
   uint32_t top;         // ord(m)
   Slope c;
   int* status;
+  Weigher mass;
   __device__ __forceinline__ unsigned long long place(float v, int i) const {
     return (static_cast<unsigned long long>(top - ord(v + 0.f)) << kIndexBits) | static_cast<unsigned>(first + i);
   }
   __device__ __forceinline__ float logit(unsigned long long place) const {
     return from_ord(top - static_cast<uint32_t>(place >> kIndexBits));
   }
+  __device__ __forceinline__ unsigned long long mass_at(float v) const {
+    return mass_of(v, m, c.hi, c.lo, mass.powers);
+  }
   // The place in the histogram, down from the maximum: kSteps of them a bin, `scale` a unit
   // (rounded by adding 1.5 * 2^23).
   __device__ __forceinline__ int step(float v, float scale) const {
     const float t = __fmul_rn(__fsub_rn(m, v), scale);
-    return __float_as_int(__fadd_rn(fminf(t, static_cast<float>(kBins * kSteps - 1)), 12582912.f)) & 0xffff;
+    return __float_as_int(__fadd_rn(fminf(t, static_cast<float>(kBins * kSteps - 1)), 12582912.f)) & 0x1fffff;
   }
   __device__ __forceinline__ int bin(float v, float scale) const { return step(v, scale) / kSteps; }
 };
@@ -364,20 +364,21 @@ __device__ __forceinline__ int first_reaching(float v, float target, float* befo
   return l;
 }
 
-// The last kept token among those up to `upto`: before it the counts sum to less than top_k, or
-// (MASS) the masses to less than top_p of all.  Returns the tokens up to it.  *kept: their sum.
-// Tokens below `low` are known to be cut (or, MASS, to be 0).  turn[]: how often the barriers of
-// the groups, of the bins, of the sums and the list have been used.
+// The last kept token among those up to `upto`: before it the counts sum to less than top_k (and then
+// the masses to less than top_p of what top_k leaves: *done; else that is still to do), or (MASS) the
+// masses to less than top_p of all.  Returns the tokens up to it.  *kept: the sum of their masses, where
+// it is known (*done, or MASS).  Tokens below `low` are known to be cut (or, MASS, to be 0).  turn[]: how
+// often the barriers of the groups, of the bins, of the sums and the list have been used.
 template <bool MASS>
 __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto, float scale, float low, int (&turn)[3],
-                          Cuts& h, Small& s, unsigned long long* kept) {
+                          Cuts& h, Small& s, unsigned long long* kept, bool* done) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n_ctas = row.n_ctas, rank = row.rank;
   const float4* x4 = reinterpret_cast<const float4*>(row.x);
   const int n4 = row.n / 4;
   const bool all_of_them = upto.x == -INFINITY;
   Boxes& box = s.box;
   if (tid == 0) expect(&box.bar[1], n_ctas * 32 * 8, n_ctas);
-  for (int i = tid; i < kBins; i += kThreads) h.digit[0][i] = 0;
+  for (int i = tid; i < 2 * kBins; i += kThreads) (&h.digit[0][0])[i] = 0;
   __syncthreads();
   int some = 0;
   for (int g0 = warp * 32; g0 < n4; g0 += kThreads) {
@@ -387,27 +388,35 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     const float v[4] = {q.x, q.y, q.z, q.w};
     bool in[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) in[e] = v[e] >= low && (all_of_them ? v[e] > -INFINITY : upto.has(v[e], 4 * g + e));
+    for (int e = 0; e < 4; ++e) in[e] = v[e] >= low && v[e] > -INFINITY;
+    if (MASS && !all_of_them) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) in[e] = in[e] && upto.has(v[e], 4 * g + e);
+    }
     if (!__any_sync(0xffffffffu, in[0] || in[1] || in[2] || in[3])) continue;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      some += in[e];
+      if (!MASS) some += in[e];
       const int step = row.step(v[e], scale);
-      if (in[e] && step < (kBins - 1) * kSteps)
-        atomicAdd(&h.digit[0][step / kSteps], MASS ? (1u << 17) + step % kSteps : 1u);
+      if (in[e] && step < (kBins - 1) * kSteps) {
+        atomicAdd(&h.digit[0][step / kSteps], 1u);
+        if (MASS) atomicAdd(&h.digit[1][step / kSteps], static_cast<unsigned>(step % kSteps));
+      }
     }
   }
-  some = __reduce_add_sync(0xffffffffu, some);
-  if (lane == 0) s.some[warp] = some;
+  if (!MASS) {
+    some = __reduce_add_sync(0xffffffffu, some);
+    if (lane == 0) s.some[warp] = some;
+  }
   __syncthreads();
   // The groups' sums to all.  A token in place q of the histogram has w = 2^(-q / (kSteps kBinsPerOctave)),
-  // which is nearly linear over a bin.  (2^15 tokens of one CTA in a bin are counted as none: then
-  // another bin is tried, in vain.)
+  // which is nearly linear over a bin; what is not is taken as if its tokens lay evenly in it.
   auto bin_value = [&](int b) {
-    const unsigned d = h.digit[0][b];
-    if (!MASS) return static_cast<float>(d);
-    const float count = static_cast<float>(d >> 17), steps = static_cast<float>(d & 0x1ffffu), step = 1.f / (kSteps * kBinsPerOctave);
-    return exp2f(-b * (1.f / kBinsPerOctave)) * fmaf(steps, -0.69314718f * step, count);
+    const float count = static_cast<float>(h.digit[0][b]);
+    if (!MASS) return count;
+    const float width = 0.69314718f / kBinsPerOctave;
+    const float steps = fmaf(static_cast<float>(h.digit[1][b]), 1.f / kSteps, -0.5f * count);
+    return exp2f((b + 0.5f) * (-1.f / kBinsPerOctave)) * fmaf(steps, -width, count * (1.f + width * width / 24.f));
   };
 #pragma unroll
   for (int j = 0; j < 32 / kWarps; ++j) {
@@ -417,7 +426,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
   }
   __syncthreads();
   if (warp == 0) {
-    const int here = __reduce_add_sync(0xffffffffu, lane < kWarps ? s.some[lane] : 0);
+    const int here = MASS ? 0 : __reduce_add_sync(0xffffffffu, lane < kWarps ? s.some[lane] : 0);
     const unsigned long long v = bits_of(s.group[lane], static_cast<float>(here));
     for (int r = 0; r < n_ctas; ++r) send(&box.group[rank][lane], v, &box.bar[1], r, n_ctas);
   }
@@ -434,6 +443,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
   float before_it = 0.f;
   const int group = all_bins >= about ? first_reaching(v, about, &before_it) : -1;
   int bin = -1, n = kList + 1;
+  bool wide = false;   // (counts) all tokens up to the bin's are listed
   unsigned long long before = 0, target = top_k;
   const int cap = kList / n_ctas;
   if (group >= 0) {
@@ -450,6 +460,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     bin = first_reaching(v, about, &before_it);
     if (bin >= 0) bin += 32 * group;
     before = static_cast<unsigned long long>(before_it);   // (of counts, which are exact)
+    wide = !MASS && bin >= 0 && before_it + __shfl_sync(0xffffffffu, v, bin & 31) <= kList;
   }
   for (int tries = 0; bin >= 0 && tries < kTries; ++tries) {
     // Sums of the tokens before the bin, in it and of all, and its tokens, to all.  Logits past `above`
@@ -463,45 +474,51 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
       s.n_list = 0;
     }
     __syncthreads();
-    unsigned long long sum[3] = {0, 0, 0};
-    for (int g0 = warp * 32; g0 < n4; g0 += kThreads) {
+    // (two tokens a turn: more are no faster, and the code is read for the first time)
+    const float2* x2 = reinterpret_cast<const float2*>(row.x);
+    MassSum ahead, within, all;
+#pragma unroll 1
+    for (int g0 = warp * 32; g0 < 2 * n4; g0 += kThreads) {
       const int g = g0 + lane;
-      float4 q = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-      if (g < n4) q = x4[g];
-      const float v[4] = {q.x, q.y, q.z, q.w};
-      bool in[4], near[4];
+      const float2 q = g < 2 * n4 ? x2[g] : make_float2(-INFINITY, -INFINITY);
+      float v[2] = {q.x, q.y};
+      if (MASS && !all_of_them) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        in[e] = v[e] >= low && (all_of_them ? v[e] > -INFINITY : upto.has(v[e], 4 * g + e));
-        near[e] = in[e] && v[e] >= under && !(v[e] > above);
+        for (int e = 0; e < 2; ++e)
+          if (!upto.has(v[e], 2 * g + e)) v[e] = -INFINITY;
       }
-      if (!__any_sync(0xffffffffu, MASS ? in[0] || in[1] || in[2] || in[3] : near[0] || near[1] || near[2] || near[3]))
-        continue;
-      unsigned long long w[4] = {1, 1, 1, 1};
-      if (MASS) {
-        const Masses a = mass2(v[0], v[1], row.m, row.c, s.exp2_of), b = mass2(v[2], v[3], row.m, row.c, s.exp2_of);
-        w[0] = a.a, w[1] = a.b, w[2] = b.a, w[3] = b.b;
+      // (a token of the bin is not below `low`, but all are where low is -inf)
+      bool past[2], near[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (!in[e]) w[e] = 0;
-          sum[2] += w[e];
-          if (v[e] > above) sum[0] += w[e];
+      for (int e = 0; e < 2; ++e) {
+        past[e] = v[e] > above && !wide;
+        near[e] = v[e] >= under && v[e] > -INFINITY && !past[e];
+      }
+      if (!__any_sync(0xffffffffu, MASS ? v[0] >= low || v[1] >= low : near[0] || near[1])) continue;
+      unsigned high[2], rest[2];
+      if (MASS) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          row.mass.halves(v[e], high[e], rest[e]);
+          if (v[e] >= low) all.add(high[e], rest[e]);
+          if (past[e]) ahead.add(high[e], rest[e]);
         }
       }
-      if (!__any_sync(0xffffffffu, near[0] || near[1] || near[2] || near[3])) continue;
+      if (!__any_sync(0xffffffffu, near[0] || near[1])) continue;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
+      for (int e = 0; e < 2; ++e) {
         if (!near[e]) continue;
         const int b = row.bin(v[e], scale);
-        if (MASS && b < bin) sum[0] += w[e];
-        if (b != bin) continue;
-        sum[1] += w[e];
+        if (MASS && b < bin) ahead.add(high[e], rest[e]);
+        if (wide ? b > bin : b != bin) continue;
+        if (MASS) within.add(high[e], rest[e]);
         const int to = atomicAdd(&s.n_list, 1);
         if (to >= cap) continue;
-        const unsigned long long p = row.place(v[e], 4 * g + e);
+        const unsigned long long p = row.place(v[e], 2 * g + e);
         for (int r = 0; r < n_ctas; ++r) send(&h.box[rank * cap + to], p, &box.bar[4], r, n_ctas);
       }
     }
+    unsigned long long sum[3] = {ahead.value(), within.value(), all.value()};
     if (MASS) {
 #pragma unroll
       for (int k = 0; k < 3; ++k) {
@@ -521,7 +538,8 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     const int sent = __reduce_add_sync(0xffffffffu, min(there, cap));
     n = __reduce_max_sync(0xffffffffu, there) > cap ? kList + 1 : sent;
     if (tid == 0) expect(&box.bar[4], sent * 8, n_ctas);
-    bool here = true;
+    bool here = MASS || !wide || n <= kList;   // (else the bin's tokens alone)
+    wide = wide && here;
     if (MASS) {
       unsigned long long in_it = 0, all = 0;
       before = 0;
@@ -552,17 +570,43 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     for (int i = warp % per * 32 + lane; i < m; i += per * 32) {
       const unsigned long long p = h.box[from * cap + i];
       h.key[before_them + i] = p;
-      if (MASS) h.mass[before_them + i] = mass(row.logit(p), row.m, row.c, s.exp2_of);
+      if (MASS) h.mass[before_them + i] = row.mass_at(row.logit(p));
     }
+    if (tid == 0) s.n_kept = 0;
     __syncthreads();
-    cut = last_of_list<MASS>(n, before, target, rank, h, s, kept);
+    cut = last_of_list<MASS>(n, wide ? 0 : before, target, rank, h, s, kept);
+    if (wide) {
+      // the tokens that are left, and of these the last one of top_p
+      __syncthreads();
+      if (tid == 0) s.n_kept = 0;
+      __syncthreads();
+      unsigned long long all = 0;
+      for (int i = warp % per * 32 + lane; i < m; i += per * 32) {
+        const unsigned long long p = h.box[from * cap + i];
+        if (p > cut) continue;
+        const int to = atomicAdd(&s.n_kept, 1);
+        h.key[to] = p;
+        all += h.mass[to] = row.mass_at(row.logit(p));
+      }
+      all = warp_sum_u64(all);
+      if (lane == 0) s.part[0][warp] = all;
+      __syncthreads();
+      all = warp_sum_u64(lane < kWarps ? s.part[0][lane] : 0);
+      *kept = all;
+      *done = true;
+      if (top_p < 1.f) {
+        const int left = s.n_kept;
+        __syncthreads();
+        cut = last_of_list<true>(left, 0, share_of(top_p, all), rank, h, s, kept);
+      }
+    }
   } else {
     cg::cluster_group cluster = cg::this_cluster();
     if (MASS) {
       // (the sum of all, where no bin was looked at)
       unsigned long long all = 0;
       for (int i = tid; i < row.n; i += kThreads)
-        if (row.x[i] >= low && upto.has(row.x[i], i)) all += mass(row.x[i], row.m, row.c, s.exp2_of);
+        if (row.x[i] >= low && upto.has(row.x[i], i)) all += row.mass_at(row.x[i]);
       all = warp_sum_u64(all);
       __syncthreads();
       if (lane == 0) s.part[1][warp] = all;
@@ -581,7 +625,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
         if (!(x > -INFINITY) || !upto.has(x, i)) continue;
         const unsigned long long p = row.place(x, i);
         if (p < cut || ((p - cut) >> shift) >= kBins) continue;
-        add_to_bin(h, static_cast<int>((p - cut) >> shift), MASS ? mass(x, row.m, row.c, s.exp2_of) : 1ull);
+        add_to_bin(h, static_cast<int>((p - cut) >> shift), MASS ? row.mass_at(x) : 1ull);
       }
       cluster_barrier(n_ctas);
       const int b = find_bin(before, target, 0, n_ctas, h, s, &before);   // (found: the whole reaches target)
@@ -621,7 +665,8 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
   const T* in = static_cast<const T*>(a.x) + r * a.ld + first;
   float* out = a.out + r * a.ld_out + first;
 
-  if (tid < 32) s.exp2_of[tid] = kExp2[tid];
+  static_assert(kPowers == kThreads, "one each");
+  h.powers[tid] = kPowersOf2.of[tid];
   float own = -INFINITY, odd = 0.f;   // odd: 0 of finite logits
   constexpr int kFly = 16;
   if (V4) {
@@ -728,24 +773,27 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
     for (int i = tid; i < n; i += kThreads) out[i] = top > -INFINITY && first + i == hot ? 1.f : 0.f;
     return;
   }
-  const RowState row = {x, first, 4 * n4, rank, n_ctas, top, ord(top + 0.f), c, a.status};
+  const RowState row = {x, first, 4 * n4, rank, n_ctas, top, ord(top + 0.f), c, a.status, {top, c, h.powers}};
   Upto upto = {-INFINITY, 0x7fffffff};
   unsigned long long kept = 0;
   int turn[3] = {0, 0, 0};
+  bool done = false;
   if (set.top_k) {
     // Bins from the maximum down to the least of the threads' maxima, where there are top_k
     // of these (so many tokens are not below it); else as for the masses.
     const float low = from_ord(__reduce_min_sync(0xffffffffu, ord(of_cta.y)));
     const bool enough = set.top_k <= __reduce_add_sync(0xffffffffu, first_of.y);
-    upto = last_kept<false>(row, set.top_k, 1.f, upto,
+    upto = last_kept<false>(row, set.top_k, set.top_p, upto,
                             enough ? fminf((kBins - 2) * kSteps / (top - low), 1e30f) : c.hi * (kSteps * kBinsPerOctave),
-                            enough ? low : -INFINITY, turn, h, s, &kept);
+                            enough ? low : -INFINITY, turn, h, s, &kept, &done);
   }
   float inv;
-  if (set.top_p < 1.f) {
+  if (done) {
+    inv = 1.f / (__ull2float_rn(kept) * 0x1p-44f);
+  } else if (set.top_p < 1.f) {
     // (a mass is 0 below 2^-46)
-    upto = last_kept<true>(row, 0, set.top_p, upto, c.hi * (kSteps * kBinsPerOctave), top - 46.f / c.hi * 1.0001f, turn,
-                           h, s, &kept);
+    upto = last_kept<true>(row, 0, set.top_p, upto, c.hi * (kSteps * kBinsPerOctave), row.mass.low(), turn, h, s, &kept,
+                           &done);
     inv = 1.f / (__ull2float_rn(kept) * 0x1p-44f);
   } else {
     float sum = 0.f;
@@ -788,6 +836,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
       }
     }
   } else {
+#pragma unroll 4
     for (int i = tid; i < n; i += kThreads) out[i] = prob(x[i], i);
   }
 }
