@@ -3,11 +3,15 @@ and commit step of Sec. 3.3 for a batch of sequences of any lengths, with
 pages taken as sequences grow and given back by release().
 
     python -m paper_2510_05421_gb300.paged_decode --workload tiny --fmt int8
+    python -m paper_2510_05421_gb300.paged_decode --temperature 0.8 --top-p 0.9 --device-pages
 
 One PagedCache per layer, one page table and one `lens` for all of them: every
 pass appends its rows behind lens and attends from there, so a rejected draft
-costs nothing but lens staying where it is.  Projections run through
-linear_noalloc and attention through PagedCache; the glue between them
+costs nothing but lens staying where it is.  With `sampling`, drafts are drawn
+from the drafter's probabilities (token_probs) and verified so that what is
+committed is distributed as the model's own tokens (verify_drafts); with
+`device_pages` a PagePool hands out the pages on the GPU.  Projections run
+through linear_noalloc and attention through PagedCache; the glue between them
 (norms, SwiGLU, argmax) is plain torch, so this shows how the calls go
 together, not how fast a decoder on them can be.  The contiguous-cache
 engine (DVIEngine) is the fast path of a fixed batch.
@@ -16,6 +20,7 @@ from __future__ import annotations
 
 import argparse
 import json
+from dataclasses import dataclass
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -23,6 +28,8 @@ import torch
 
 from .dvi import DeviceWeights, linear_noalloc
 from .paged import PagedCache, rotary_table
+from .pages import PagePool
+from .sampling import token_probs, verify_drafts
 
 _ROWS = 256     # rows of one linear_noalloc call
 
@@ -37,12 +44,35 @@ def _linear(w: torch.Tensor, x: torch.Tensor) -> torch.Tensor:
     return y
 
 
+@dataclass
+class Sampling:
+    """How tokens are drawn (as in token_probs), and from which numbers."""
+    temperature: float = 1.0
+    top_k: int = 0
+    top_p: float = 1.0
+    generator: Optional[torch.Generator] = None
+
+    def uniform(self, n: int, device) -> torch.Tensor:
+        return torch.rand(n, device=device, generator=self.generator)
+
+    def probs(self, logits: torch.Tensor) -> torch.Tensor:
+        return token_probs(logits, self.temperature, self.top_k, self.top_p)
+
+    def draw(self, probs: torch.Tensor) -> torch.Tensor:
+        """A token of each row."""
+        n = probs.shape[0]
+        none = probs.new_empty(0)
+        return verify_drafts(probs, none.to(torch.int32), none, self.uniform(n, probs.device))[0][:, 0]
+
+
 class PagedDecoder:
     """A layer-split decoder whose sequences live in a pool of 8-bit pages."""
 
+    pool: Optional[PagePool] = None
+
     def __init__(self, shape, weights: DeviceWeights, *, split_k: int, k_spec: int, max_seqs: int, n_pages: int,
                  max_seq_len: int, lora_gamma: float = 1.0, page_tokens: int = 16, fmt: str = "int8",
-                 device="cuda"):
+                 device="cuda", device_pages: bool = False):
         self.s, self.w = shape, weights
         self.split, self.K, self.gamma, self.P = split_k, k_spec, lora_gamma, page_tokens
         self.device = torch.device(device)
@@ -57,12 +87,20 @@ class PagedDecoder:
         self.held: List[List[int]] = [[] for _ in range(max_seqs)]
         self.host_lens = [0] * max_seqs
         self.max_seq_len = max_seq_len
-        self.table = torch.full((max_seqs, -(-max_seq_len // page_tokens)), -1, dtype=torch.int32, device=device)
+        width = -(-max_seq_len // page_tokens)
+        if device_pages:
+            self.pool = PagePool.create(n_pages, max_seqs, width, page_tokens, device)
+            self.table = self.pool.table
+        else:
+            self.table = torch.full((max_seqs, width), -1, dtype=torch.int32, device=device)
         self.lens = torch.zeros(max_seqs, dtype=torch.int32, device=device)
 
     # -- pages ------------------------------------------------------------
     def reserve(self, rows: Sequence[int]):
         """Pages for rows[b] more positions of each sequence."""
+        if self.pool is not None:
+            self._plan(rows)
+            return
         for b, n in enumerate(rows):
             if self.host_lens[b] + n > self.max_seq_len:
                 raise RuntimeError("a sequence would outgrow max_seq_len")
@@ -76,13 +114,28 @@ class PagedDecoder:
             self.table[b, at:at + need] = torch.tensor(new, dtype=torch.int32).to(self.device)
             self.held[b] += new
 
+    def _plan(self, rows: Sequence[int]):
+        """The same on the GPU: what the plan will find follows from the lengths, without a look at the device."""
+        after = [len_ + n for len_, n in zip(self.host_lens, rows)]
+        if max(after) > self.max_seq_len:
+            raise RuntimeError("a sequence would outgrow max_seq_len")
+        if sum(-(-n // self.P) for n in after) > self.pool.n_pages:
+            raise RuntimeError("out of pages")
+        self.pool.plan(self.lens, torch.tensor(list(rows), dtype=torch.int32).to(self.device))
+
     def release(self, b: int):
         """Sequence b is over: its pages go back."""
+        self.host_lens[b] = 0
+        self.lens[b] = 0
+        if self.pool is not None:
+            self.pool.trim(self.lens)
+            return
         self.free += self.held[b]
         self.held[b] = []
-        self.host_lens[b] = 0
         self.table[b].fill_(-1)
-        self.lens[b] = 0
+
+    def pages_in_use(self) -> int:
+        return sum(len(h) for h in self.held) if self.pool is None else int(self.pool.held.sum())
 
     def advance(self, rows: Sequence[int]):
         """Keep rows[b] of the rows appended behind lens."""
@@ -122,9 +175,9 @@ class PagedDecoder:
         return self.w.embed[tokens.long()].float()
 
     # -- calls ------------------------------------------------------------
-    def prefill(self, prompts: Sequence[np.ndarray]) -> torch.Tensor:
-        """The prompts, one for each slot, in one ragged pass behind what the sequences hold; the greedy token after each
-        (pending, in no cache yet).  A slot whose prompt is empty takes no rows, and its token is -1."""
+    def prefill(self, prompts: Sequence[np.ndarray], sampling: Optional[Sampling] = None) -> torch.Tensor:
+        """The prompts, one for each slot, in one ragged pass behind what the sequences hold; the greedy (or sampled) token
+        after each (pending, in no cache yet).  A slot whose prompt is empty takes no rows, and its token is -1."""
         if len(prompts) != len(self.host_lens):
             raise ValueError(f"prefill: {len(prompts)} prompts for {len(self.host_lens)} slots")
         rows = [len(p) for p in prompts]
@@ -138,7 +191,13 @@ class PagedDecoder:
         self.advance(rows)
         some = row_start.diff() > 0
         last = torch.where(some, row_start[1:] - 1, 0).long()
-        return torch.where(some, self.verifier_logits(h[last]).argmax(-1).to(torch.int32), -1)
+        return torch.where(some, self._choose(self.verifier_logits(h[last]), sampling), -1)
+
+    def _choose(self, logits: torch.Tensor, sampling: Optional[Sampling]) -> torch.Tensor:
+        """The greedy token of each row, or a sampled one."""
+        if sampling is None:
+            return logits.argmax(-1).to(torch.int32)
+        return sampling.draw(sampling.probs(logits))
 
     def _taking_part(self, live: Optional[Sequence[int]]):
         """The sequences of a pass (by default those that hold rows), where they lie in tensors of all sequences and
@@ -158,9 +217,10 @@ class PagedDecoder:
         full = x.new_zeros((len(self.host_lens), *x.shape[1:])) if rest is None else rest.clone()
         return full.index_copy_(0, at, x)
 
-    def step(self, pending: torch.Tensor, live: Optional[Sequence[int]] = None):
+    def step(self, pending: torch.Tensor, live: Optional[Sequence[int]] = None, sampling: Optional[Sampling] = None):
         """K greedy draft passes, one verify pass over the K rows, the longest agreeing prefix and the correction, of
-        the sequences in `live` (by default those that hold rows: a released one takes none).
+        the sequences in `live` (by default those that hold rows: a released one takes none).  With `sampling` the drafts
+        are drawn from the drafter's probabilities and verified against the model's.
         Returns (committed tokens [B, K], how many of them, how many drafts agreed, the new pending tokens); the
         sequences that took no part have 0 of them and their pending token as it was."""
         live, at, start = self._taking_part(live)
@@ -169,28 +229,41 @@ class PagedDecoder:
             none = torch.zeros(len(self.host_lens), dtype=torch.long, device=self.device)
             return torch.zeros(len(none), K, dtype=torch.int32, device=self.device), none, none.clone(), pending
         self.reserve([K if b in live else 0 for b in range(len(self.host_lens))])
-        hs, drafts = [], []
+        hs, drafts, drawn_from = [], [], []
         tok = pending if at is None else pending[at]
         for j in range(K):
             h = self.layers(0, self.split, self.embed(tok), self.lens + j, start, 1)
             hs.append(h)
-            tok = self.drafter_logits(h).argmax(-1).to(torch.int32)
+            z = self.drafter_logits(h)
+            if sampling is None:
+                tok = z.argmax(-1).to(torch.int32)
+            else:
+                drawn_from.append(sampling.probs(z))
+                tok = sampling.draw(drawn_from[-1])
             drafts.append(tok)
         rows = torch.stack(hs, 1).reshape(n_live * K, -1)                # sequence after sequence
         h = self.layers(self.split, self.s.n_layers, rows, self.lens, None if start is None else start * K, K)
-        y = self.verifier_logits(h).argmax(-1).to(torch.int32).view(n_live, K)
         t = torch.stack(drafts, 1)
-        m = (t == y).int().cumprod(1).sum(1)
-        n = (m + 1).clamp_max(K)
-        out = torch.where(torch.arange(K, device=self.device) < m[:, None], t, y)
+        if sampling is None:
+            y = self.verifier_logits(h).argmax(-1).to(torch.int32).view(n_live, K)
+            m = (t == y).int().cumprod(1).sum(1)
+            n = (m + 1).clamp_max(K)
+            out = torch.where(torch.arange(K, device=self.device) < m[:, None], t, y)
+        else:
+            q = torch.stack(drawn_from, 1).view(n_live * K, -1)
+            out, n, m = verify_drafts(sampling.probs(self.verifier_logits(h)), t.view(-1),
+                                      sampling.uniform(n_live * K, self.device), sampling.uniform(n_live, self.device),
+                                      draft=q, max_drafts=K, bonus=False)
+            n, m = n.long(), m.long()
         new_pending = out.gather(1, (n - 1).long()[:, None]).squeeze(1)
         n = self._spread(at, n)
         self.advance(n.tolist())
         return self._spread(at, out), n, self._spread(at, m), self._spread(at, new_pending, pending)
 
-    def ar_step(self, pending: torch.Tensor, live: Optional[Sequence[int]] = None) -> torch.Tensor:
-        """One greedy token of the whole model for the sequences in `live` (by default those that hold rows); the
-        others' pending tokens stay."""
+    def ar_step(self, pending: torch.Tensor, live: Optional[Sequence[int]] = None,
+                sampling: Optional[Sampling] = None) -> torch.Tensor:
+        """One greedy (or sampled) token of the whole model for the sequences in `live` (by default those that hold rows);
+        the others' pending tokens stay."""
         live, at, start = self._taking_part(live)
         if not live:
             return pending
@@ -199,24 +272,25 @@ class PagedDecoder:
         tok = pending if at is None else pending[at]
         h = self.layers(0, self.s.n_layers, self.embed(tok), self.lens, start, 1)
         self.advance(takes)
-        return self._spread(at, self.verifier_logits(h).argmax(-1).to(torch.int32), pending)
+        return self._spread(at, self._choose(self.verifier_logits(h), sampling), pending)
 
-    def generate(self, prompts: Sequence[np.ndarray], n_gen: int, speculative: bool = True):
+    def generate(self, prompts: Sequence[np.ndarray], n_gen: int, speculative: bool = True,
+                 sampling: Optional[Sampling] = None):
         """n_gen tokens of each prompt, and the mean accepted length (None without speculation).  A sequence that has its
         tokens takes no more rows; its pages stay its own until release()."""
         if not all(len(p) for p in prompts):
             raise ValueError("generate: an empty prompt has no next token")
-        tok = self.prefill(prompts)
+        tok = self.prefill(prompts, sampling)
         out = [[int(t)] for t in tok]
         agreed = steps = 0
         while live := [b for b, o in enumerate(out) if len(o) < n_gen]:
             if speculative:
-                ids, n, m, tok = self.step(tok, live)
+                ids, n, m, tok = self.step(tok, live, sampling)
                 for o, row, c in zip(out, ids.tolist(), n.tolist()):
                     o.extend(row[:c])
                 agreed += int(m.sum())
             else:
-                tok = self.ar_step(tok, live)
+                tok = self.ar_step(tok, live, sampling)
                 new = tok.tolist()
                 for b in live:
                     out[b].append(new[b])
@@ -224,7 +298,8 @@ class PagedDecoder:
         return [o[:n_gen] for o in out], agreed / max(1, steps) if speculative else None
 
 
-def run(workload_name: str, fmt: str, n_gen: int, page_tokens: int, batch: int):
+def run(workload_name: str, fmt: str, n_gen: int, page_tokens: int, batch: int, temperature: Optional[float] = None,
+        top_k: int = 0, top_p: float = 1.0, seed: int = 0, device_pages: bool = False):
     from workloads import make_prompts, make_weights, workload
 
     w = workload(workload_name)
@@ -234,11 +309,14 @@ def run(workload_name: str, fmt: str, n_gen: int, page_tokens: int, batch: int):
     longest = max(len(p) for p in prompts) + n_gen + 2 * w.k_spec + 1
     dec = PagedDecoder(w.shape, DeviceWeights.from_host(make_weights(w), w.dtype), split_k=w.split_k, k_spec=w.k_spec,
                        max_seqs=w.batch, n_pages=w.batch * (-(-longest // page_tokens)), max_seq_len=longest,
-                       lora_gamma=w.lora_gamma, page_tokens=page_tokens, fmt=fmt)
-    tokens, mat = dec.generate(prompts, n_gen)
-    flags = sorted({f for c in dec.caches for f in c.status()})
+                       lora_gamma=w.lora_gamma, page_tokens=page_tokens, fmt=fmt, device_pages=device_pages)
+    sampling = None
+    if temperature is not None:
+        sampling = Sampling(temperature, top_k, top_p, torch.Generator(device="cuda").manual_seed(seed))
+    tokens, mat = dec.generate(prompts, n_gen, sampling=sampling)
+    flags = sorted({f for c in [*dec.caches, *([dec.pool] if dec.pool else [])] for f in c.status()})
     return dict(workload=w.name, fmt=fmt, page_tokens=page_tokens, mean_accepted=mat, device_flags=flags,
-                pages_in_use=sum(len(h) for h in dec.held), tokens=[t[:8] for t in tokens])
+                pages_in_use=dec.pages_in_use(), tokens=[t[:8] for t in tokens])
 
 
 def main():
@@ -248,8 +326,14 @@ def main():
     ap.add_argument("--tokens", type=int, default=32)
     ap.add_argument("--page-tokens", type=int, default=16)
     ap.add_argument("--batch", type=int, default=0, help="sequences of unequal prompts (0: the workload's batch)")
+    ap.add_argument("--temperature", type=float, help="sample at this temperature (default: greedy)")
+    ap.add_argument("--top-k", type=int, default=0)
+    ap.add_argument("--top-p", type=float, default=1.0)
+    ap.add_argument("--seed", type=int, default=0)
+    ap.add_argument("--device-pages", action="store_true", help="plan the pages on the GPU")
     a = ap.parse_args()
-    print(json.dumps(run(a.workload, a.fmt, a.tokens, a.page_tokens, a.batch)))
+    print(json.dumps(run(a.workload, a.fmt, a.tokens, a.page_tokens, a.batch, a.temperature, a.top_k, a.top_p, a.seed,
+                         a.device_pages)))
 
 
 if __name__ == "__main__":
