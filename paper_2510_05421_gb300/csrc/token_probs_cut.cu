@@ -31,7 +31,9 @@ constexpr int kBins = 1024;                      // 32 groups of 32
 constexpr int kBinBits = 10;
 constexpr int kPer = kBins / kThreads;
 constexpr int kSteps = 1024;                     // places within a bin
-constexpr float kBinsPerOctave = 40.f;           // of w: the last bin has what is below 2^-25.6
+constexpr float kBinsPerOctave = 40.f;           // of w
+constexpr int kWide = 768;                       // from this bin on they are four times as wide: the last one has what
+                                                 // is below 2^-44.6
 constexpr int kList = 1024;                      // tokens of a bin that are sorted out by each CTA
 constexpr int kListPer = kList / kThreads;
 constexpr int kFew = 128;                        // tokens that are compared with each other, by four threads each
@@ -189,8 +191,11 @@ struct RowState {
   // (rounded by adding 1.5 * 2^23).
   __device__ __forceinline__ int step(float v, float scale) const {
     const float t = __fmul_rn(__fsub_rn(m, v), scale);
-    return __float_as_int(__fadd_rn(fminf(t, static_cast<float>(kBins * kSteps - 1)), 12582912.f)) & 0x1fffff;
+    const float wide = fmaf(t, 0.25f, 0.75f * kWide * kSteps);
+    return __float_as_int(__fadd_rn(fminf(fminf(t, wide), static_cast<float>(kBins * kSteps - 1)), 12582912.f)) & 0x1fffff;
   }
+  // (what lies before it, in bins of the first kind)
+  static __device__ __forceinline__ float from(float bin) { return bin < kWide ? bin : kWide + 4.f * (bin - kWide); }
   __device__ __forceinline__ int bin(float v, float scale) const { return step(v, scale) / kSteps; }
 };
 
@@ -409,14 +414,15 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     if (lane == 0) s.some[warp] = some;
   }
   __syncthreads();
-  // The groups' sums to all.  A token in place q of the histogram has w = 2^(-q / (kSteps kBinsPerOctave)),
-  // which is nearly linear over a bin; what is not is taken as if its tokens lay evenly in it.
+  // The groups' sums to all.  w falls by 2^(1 / kBinsPerOctave) over a bin, nearly linearly; what is not
+  // linear is taken as if the bin's tokens lay evenly in it.
   auto bin_value = [&](int b) {
     const float count = static_cast<float>(h.digit[0][b]);
     if (!MASS) return count;
-    const float width = 0.69314718f / kBinsPerOctave;
+    const float width = 0.69314718f / kBinsPerOctave * (b < kWide ? 1.f : 4.f);
     const float steps = fmaf(static_cast<float>(h.digit[1][b]), 1.f / kSteps, -0.5f * count);
-    return exp2f((b + 0.5f) * (-1.f / kBinsPerOctave)) * fmaf(steps, -width, count * (1.f + width * width / 24.f));
+    return exp2f(0.5f * (row.from(b) + row.from(b + 1)) * (-1.f / kBinsPerOctave)) *
+           fmaf(steps, -width, count * fmaf(width, width * (1.f / 24.f), 1.f));
   };
 #pragma unroll
   for (int j = 0; j < 32 / kWarps; ++j) {
@@ -466,7 +472,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     // Sums of the tokens before the bin, in it and of all, and its tokens, to all.  Logits past `above`
     // are before it, below `under` behind it, by more than what rounding may do.
     const float width = kSteps / scale;
-    const float above_it = row.m - (bin - 0.25f) * width, under_it = row.m - (bin + 1.25f) * width;
+    const float above_it = row.m - row.from(bin - 0.25f) * width, under_it = row.m - row.from(bin + 1.25f) * width;
     const float above = above_it + 0x1p-21f * fmaxf(fabsf(row.m), fabsf(above_it)),
                 under = under_it - 0x1p-21f * fmaxf(fabsf(row.m), fabsf(under_it));
     if (tid == 0) {
@@ -784,7 +790,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
     const float low = from_ord(__reduce_min_sync(0xffffffffu, ord(of_cta.y)));
     const bool enough = set.top_k <= __reduce_add_sync(0xffffffffu, first_of.y);
     upto = last_kept<false>(row, set.top_k, set.top_p, upto,
-                            enough ? fminf((kBins - 2) * kSteps / (top - low), 1e30f) : c.hi * (kSteps * kBinsPerOctave),
+                            enough ? fminf(row.from(kBins - 2) * kSteps / (top - low), 1e30f) : c.hi * (kSteps * kBinsPerOctave),
                             enough ? low : -INFINITY, turn, h, s, &kept, &done);
   }
   float inv;

@@ -218,3 +218,28 @@ def test_refusals():
     for y in (x.half(), x[0], x.cpu(), x.t(), torch.empty(1, 262145, device="cuda"), torch.empty(2, 0, device="cuda")):
         with pytest.raises(ValueError):
             token_probs(y)
+
+
+@pytest.mark.parametrize("p", [0.99, 0.9999, 0.9999999, 1 - 2.0 ** -24])
+@pytest.mark.parametrize("T", [0.25, 1.0])
+@pytest.mark.parametrize("V", [3000, 100003])
+def test_cuts_deep_in_the_tail(V, T, p):
+    """top_p just below 1: the last kept token's w is down to 2^-40 of the largest, or below what a mass resolves."""
+    from paper_2510_05421_gb300 import token_probs
+    x = logits(2, V, 19)
+    got = token_probs(x.cuda(), T, 0, p).cpu().double().numpy()
+    p = float(np.float32(p))
+    for r in range(2):
+        v = x[r].double().numpy()
+        w = np.exp((v - v.max()) / np.float32(T))
+        order = np.argsort(-v, kind="stable")
+        kept = int((got[r] > 0).sum())
+        assert (got[r][order[:kept]] > 0).all()                     # a prefix of the order
+        # its end is where the sum reaches p of the whole, within what the masses' rounding may move: each is off by
+        # 2^-45 and 2^-34 of itself
+        before, all_of_it = w[order].cumsum() - w[order], w.sum()
+        slack = V * 2.0 ** -44 + all_of_it * 2.0 ** -33
+        assert before[kept - 1] < p * all_of_it + slack and (kept == V or before[kept] >= p * all_of_it - slack)
+        want = np.where(np.isin(np.arange(V), order[:kept]), w, 0) / w[order[:kept]].sum()
+        t = np.abs((v - v.max()) / np.float32(T))
+        assert (np.abs(got[r] - want) <= want * (t * 3 * 2.0 ** -24 + 2.0 ** -21) + 2.0 ** -140).all()
