@@ -111,17 +111,18 @@ __device__ __noinline__ unsigned long long mass_of(float x, float m, float c_hi,
   w.halves(x, high, rest);
   return x >= w.low() ? Weigher::join(high, rest) : 0;
 }
-// A sum of masses (kBits of every half are taken out at the end; sums may pass 64 bits until then).
+// A thread's sum of masses: at most 64 halves of at most 2^22 each.
 struct MassSum {
-  unsigned long long sum = 0;
-  unsigned n = 0;
-  __device__ __forceinline__ void add(unsigned high, unsigned rest) {
-    sum += high * 4194304ull;
-    sum += rest;
-    ++n;
+  unsigned high = 0, rest = 0;
+  __device__ __forceinline__ void add(unsigned h, unsigned r) {
+    high += h - Weigher::kBits;
+    rest += r - Weigher::kBits;
   }
-  __device__ __forceinline__ unsigned long long value() const { return sum - n * (Weigher::kBits * 4194305ull); }
+  __device__ __forceinline__ unsigned long long value() const {
+    return high * 4194304ull + static_cast<long long>(static_cast<int>(rest));
+  }
 };
+static_assert(kMaxVocab / kMaxCtas <= 64 * kThreads, "64 logits a thread");
 
 __device__ __forceinline__ unsigned long long warp_sum_u64(unsigned long long v) {
 #pragma unroll
@@ -393,7 +394,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     const float v[4] = {q.x, q.y, q.z, q.w};
     bool in[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) in[e] = v[e] >= low && v[e] > -INFINITY;
+    for (int e = 0; e < 4; ++e) in[e] = v[e] >= low && (MASS || v[e] > -INFINITY);   // (MASS: low is a number)
     if (MASS && !all_of_them) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) in[e] = in[e] && upto.has(v[e], 4 * g + e);
@@ -700,7 +701,19 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
       }
     }
   } else {
-    for (int i0 = 0; i0 < n; i0 += kFly * kThreads) {
+    int i0 = 0;
+    for (; i0 + kFly * kThreads <= n; i0 += kFly * kThreads) {
+      float v[kFly];
+#pragma unroll
+      for (int j = 0; j < kFly; ++j) v[j] = DT<T>::ld(in + i0 + j * kThreads + tid);
+#pragma unroll
+      for (int j = 0; j < kFly; ++j) {
+        own = fmaxf(own, v[j]);
+        odd = fmaf(v[j], 0.f, odd);
+        x[i0 + j * kThreads + tid] = v[j];
+      }
+    }
+    if (i0 < n) {
       float v[kFly];
 #pragma unroll
       for (int j = 0; j < kFly; ++j) {
