@@ -502,11 +502,12 @@ typedef struct {
  * logits.  T counts as 2^-100 below that and as 2^100 above.  A row of -inf alone
  * gets zeros.
  *
- * Which tokens stay is decided on w in fixed point (2^-44 of the row's largest, off
- * by about 2^-38), so it does not depend on the order of any sum.  NaN logits count
- * as -inf and +inf as the largest finite number (DVI_DEV_NONFINITE).  Of settings in
- * device arrays, T that is negative or NaN counts as 0, top_k below 0 as 0, top_p
- * NaN as 1 (NaN: DVI_DEV_NONFINITE).  d_probs does not overlap d_logits. */
+ * Which tokens stay is decided on w as whole multiples of 2^-44 of the row's largest
+ * (off by 2^-45, and by about 2^-34 of themselves), so it does not depend on the
+ * order of any sum.  NaN logits count as -inf and +inf as the largest finite number
+ * (DVI_DEV_NONFINITE).  Of settings in device arrays, T that is negative or NaN counts
+ * as 0, top_k below 0 as 0, top_p NaN as 1 (NaN: DVI_DEV_NONFINITE).  d_probs may be
+ * d_logits itself (f32, the same ld); else they do not overlap. */
 dvi_status dvi_token_probs(int dtype, const void* d_logits, int64_t ld_logits, int n_rows, int vocab,
                            const dvi_sampling* sampling, float* d_probs, int64_t ld_probs, int32_t* d_status,
                            dvi_stream stream);

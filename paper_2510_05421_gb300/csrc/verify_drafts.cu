@@ -22,6 +22,7 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCtas = 8;        // of a sequence
 constexpr int kFly = 8;            // numbers of each row that a thread has in flight
 constexpr int kChunk = 32 * kFly;
+constexpr int kLast = 2;           // numbers of a lane where a single warp finds the token
 
 // A probability as it counts: NaN, infinities and negative numbers are 0.
 __device__ __forceinline__ float prob(float p, bool& bad) {
@@ -218,7 +219,7 @@ __device__ int find_token(const Residual& r, int V, int L, int shares, float u, 
   }
   __syncthreads();
   if (s.lo < 0) return -1;
-  while (s.hi - s.lo > kChunk) {
+  while (s.hi - s.lo > 32 * kLast) {
     const int lo = s.lo, hi = s.hi, sub = (hi - lo + kThreads - 1) / kThreads * 32;
     const float2 v = sum_range(r, min(hi, lo + warp * sub), min(hi, lo + warp * sub + sub), bad);
     if (lane == 0) s.sub[warp] = v;
@@ -239,18 +240,18 @@ __device__ int find_token(const Residual& r, int V, int L, int shares, float u, 
   }
   if (warp == 0) {
     const int lo = s.lo, hi = s.hi;
-    float p[kFly], q[kFly];
+    float p[kLast], q[kLast];
 #pragma unroll
-    for (int j = 0; j < kFly; ++j) {
-      const int i = lo + lane * kFly + j;
+    for (int j = 0; j < kLast; ++j) {
+      const int i = lo + lane * kLast + j;
       p[j] = i < hi ? r.p[i] : 0.f;
       q[j] = i < hi ? r.q_at(i) : 0.f;
     }
-    unsigned long long v[kFly];
+    unsigned long long v[kLast];
     bool above = false;
     int first = -1;
 #pragma unroll
-    for (int j = 0; j < kFly; ++j) {
+    for (int j = 0; j < kLast; ++j) {
       const float b = prob(q[j], bad), a = fmaxf(prob(p[j], bad), b), d = __fsub_rn(a, b);
       v[j] = scale.of(make_float2(d, __fsub_rn(__fsub_rn(a, d), b)));
       if (d > 0.f && first < 0) first = j, above = true;
@@ -258,7 +259,7 @@ __device__ int find_token(const Residual& r, int V, int L, int shares, float u, 
     int at = pick(v, t, base);
     // (numbers below 2^-54 of the largest share alone: the first of them)
     const unsigned any = __ballot_sync(0xffffffffu, above);
-    if (at < 0 && any) at = (__ffs(any) - 1) * kFly + __shfl_sync(0xffffffffu, first, __ffs(any) - 1);
+    if (at < 0 && any) at = (__ffs(any) - 1) * kLast + __shfl_sync(0xffffffffu, first, __ffs(any) - 1);
     if (lane == 0) s.token = at < 0 ? -1 : lo + at;
   }
   __syncthreads();

@@ -206,6 +206,16 @@ def test_stream_and_graph():
     assert torch.count_nonzero(got[4]) == 1
 
 
+@pytest.mark.parametrize("V", [500, 4099, 32000, 200003])
+@pytest.mark.parametrize("kw", [dict(), dict(top_p=0.9), dict(top_k=30), dict(temperature=0.0)])
+def test_in_place(V, kw):
+    from paper_2510_05421_gb300 import token_probs
+    x = logits(9, V, 20).cuda()
+    want = token_probs(x, **kw)
+    assert token_probs(x, out=x, **kw) is x
+    assert torch.equal(x, want)
+
+
 def test_refusals():
     from paper_2510_05421_gb300 import token_probs
     x = logits(3, 100, 18).cuda()
