@@ -79,6 +79,18 @@ __device__ __forceinline__ void cluster_barrier(int n_ctas) {
   }
 }
 
+// Eight bytes to the same place of CTA `rank`, counted by its barrier: no fence goes with them, so
+// nothing waits for the sender's own memory operations.
+__device__ __forceinline__ void send_to(void* to, unsigned long long v, void* bar, int rank) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(
+                   mapa_shared(smem_u32(to), rank)),
+               "l"(v), "r"(mapa_shared(smem_u32(bar), rank))
+               : "memory");
+}
+__device__ __forceinline__ unsigned long long bits_of(float a, float b) {
+  return (static_cast<unsigned long long>(__float_as_uint(b)) << 32) | __float_as_uint(a);
+}
+
 // A cluster of `ctas` CTAs for each row, which hold slices of it.
 template <typename K>
 cudaError_t launch_rows(K kern, const TokenProbsArgs& a, int ctas, int threads, size_t smem, size_t smem_a_logit,

@@ -206,13 +206,7 @@ __device__ __forceinline__ void send(void* to, unsigned long long v, unsigned lo
     *static_cast<unsigned long long*>(to) = v;
     return;
   }
-  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(
-                   mapa_shared(smem_u32(to), r)),
-               "l"(v), "r"(mapa_shared(smem_u32(bar), r))
-               : "memory");
-}
-__device__ __forceinline__ unsigned long long bits_of(float a, float b) {
-  return (static_cast<unsigned long long>(__float_as_uint(b)) << 32) | __float_as_uint(a);
+  send_to(to, v, bar, r);
 }
 // One thread says how much will come ...
 __device__ __forceinline__ void expect(unsigned long long* bar, int bytes, int n_ctas) {
@@ -375,9 +369,15 @@ __device__ __forceinline__ int first_reaching(float v, float target, float* befo
 // masses to less than top_p of all.  Returns the tokens up to it.  *kept: the sum of their masses, where
 // it is known (*done, or MASS).  Tokens below `low` are known to be cut (or, MASS, to be 0).  turn[]: how
 // often the barriers of the groups, of the bins, of the sums and the list have been used.
+//
+// by_maxima (counts): the histogram has the largest logit of each thread alone (`mine`), which are at
+// least top_k: the tokens that are not behind the bin in which the top_k-th of these lies are few more than
+// top_k, and all are listed.  Where they do not fit, returns with *fits = false: then all tokens have to be
+// counted.
 template <bool MASS>
 __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto, float scale, float low, int (&turn)[3],
-                          Cuts& h, Small& s, unsigned long long* kept, bool* done) {
+                          Cuts& h, Small& s, unsigned long long* kept, bool* done,
+                          bool by_maxima = false, float mine = 0.f, bool* fits = nullptr) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n_ctas = row.n_ctas, rank = row.rank;
   const float4* x4 = reinterpret_cast<const float4*>(row.x);
   const int n4 = row.n / 4;
@@ -387,7 +387,11 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
   for (int i = tid; i < 2 * kBins; i += kThreads) (&h.digit[0][0])[i] = 0;
   __syncthreads();
   int some = 0;
-  for (int g0 = warp * 32; g0 < n4; g0 += kThreads) {
+  if (!MASS && by_maxima) {
+    some = mine >= low && mine > -INFINITY;
+    if (some) atomicAdd(&h.digit[0][row.bin(mine, scale)], 1u);
+  }
+  for (int g0 = !MASS && by_maxima ? n4 : warp * 32; g0 < n4; g0 += kThreads) {
     const int g = g0 + lane;
     float4 q = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
     if (g < n4) q = x4[g];
@@ -467,7 +471,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     bin = first_reaching(v, about, &before_it);
     if (bin >= 0) bin += 32 * group;
     before = static_cast<unsigned long long>(before_it);   // (of counts, which are exact)
-    wide = !MASS && bin >= 0 && before_it + __shfl_sync(0xffffffffu, v, bin & 31) <= kList;
+    wide = !MASS && (by_maxima || before_it + __shfl_sync(0xffffffffu, v, bin & 31) <= kList);
   }
   for (int tries = 0; bin >= 0 && tries < kTries; ++tries) {
     // Sums of the tokens before the bin, in it and of all, and its tokens, to all.  Logits past `above`
@@ -546,6 +550,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     n = __reduce_max_sync(0xffffffffu, there) > cap ? kList + 1 : sent;
     if (tid == 0) expect(&box.bar[4], sent * 8, n_ctas);
     bool here = MASS || !wide || n <= kList;   // (else the bin's tokens alone)
+    if (!MASS && by_maxima) *fits = here;
     wide = wide && here;
     if (MASS) {
       unsigned long long in_it = 0, all = 0;
@@ -564,6 +569,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     }
     if (!arrived(&box.bar[4], turn[2]++, n_ctas, row.status)) return upto;
     if (here) break;
+    if (!MASS && by_maxima) return upto;
     n = kList + 1;
     __syncthreads();   // (before the list is begun again)
   }
@@ -661,11 +667,11 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
   const int r = blockIdx.x / n_ctas;
   const int first = min(rank * slice, a.vocab), n = min(slice, a.vocab - first), n4 = (n + 3) / 4;
   Boxes& box = s.box;
-  if (tid == 0) {
-    for (int k = 0; k < 6; ++k) mbar_init(reinterpret_cast<uint64_t*>(&box.bar[k]), 1);
+  if (tid < 6) {
+    mbar_init(reinterpret_cast<uint64_t*>(&box.bar[tid]), 1);
     mbar_fence_init();
-    expect(&box.bar[0], n_ctas * 16, n_ctas);
-    expect(&box.bar[5], n_ctas * 8, n_ctas);
+    if (tid == 0) expect(&box.bar[0], n_ctas * 16, n_ctas);
+    if (tid == 5) expect(&box.bar[5], n_ctas * 8, n_ctas);
   }
   if (n_ctas > 1) cluster_arrive_release();              // (waited for before anything is sent)
   griddep_wait();
@@ -802,9 +808,15 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
     // of these (so many tokens are not below it); else as for the masses.
     const float low = from_ord(__reduce_min_sync(0xffffffffu, ord(of_cta.y)));
     const bool enough = set.top_k <= __reduce_add_sync(0xffffffffu, first_of.y);
-    upto = last_kept<false>(row, set.top_k, set.top_p, upto,
-                            enough ? fminf(row.from(kBins - 2) * kSteps / (top - low), 1e30f) : c.hi * (kSteps * kBinsPerOctave),
-                            enough ? low : -INFINITY, turn, h, s, &kept, &done);
+    Upto cut;
+    for (bool by_maxima = enough && set.top_k <= kList / 2, fits = false; !fits; by_maxima = false) {
+      fits = true;
+      cut = last_kept<false>(row, set.top_k, set.top_p, upto,
+                             enough ? fminf(row.from(kBins - 2) * kSteps / (top - low), 1e30f)
+                                    : c.hi * (kSteps * kBinsPerOctave),
+                             enough ? low : -INFINITY, turn, h, s, &kept, &done, by_maxima, own, &fits);
+    }
+    upto = cut;
   }
   float inv;
   if (done) {

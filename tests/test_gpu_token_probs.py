@@ -253,3 +253,20 @@ def test_cuts_deep_in_the_tail(V, T, p):
         want = np.where(np.isin(np.arange(V), order[:kept]), w, 0) / w[order[:kept]].sum()
         t = np.abs((v - v.max()) / np.float32(T))
         assert (np.abs(got[r] - want) <= want * (t * 3 * 2.0 ** -24 + 2.0 ** -21) + 2.0 ** -140).all()
+
+
+@pytest.mark.parametrize("V", [3001, 32000, 128001])
+@pytest.mark.parametrize("k", [1, 50, 400, 512, 513, 1024, 1025, 2999])
+def test_top_k_where_the_likeliest_lie_together(V, k):
+    """The largest logits one after another (one CTA, a few threads have them all), or spread by a stride of the threads."""
+    n = min(V, 1500)
+    x = logits(4, V, 21)
+    g = torch.Generator().manual_seed(1)
+    top = 12 + 3 * torch.rand(n, generator=g)
+    x[0, :n] = top
+    x[1, V - n:] = top
+    at = torch.arange(0, V, 512)[:n]
+    x[2, at] = top[:len(at)]
+    x[3, :n] = top.bfloat16().float()                           # with ties
+    check(x.cuda(), 1.0, k)
+    check(x.cuda(), 1.0, k, 0.9)
