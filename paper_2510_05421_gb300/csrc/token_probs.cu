@@ -35,18 +35,13 @@ __device__ __forceinline__ void join(const float2* peer, int n_ctas, bool greedy
 template <typename T, int NV, int THREADS, bool V4>
 __global__ void __launch_bounds__(THREADS, 32768 / (NV * THREADS))
     token_probs_kernel(TokenProbsArgs a, int n_ctas, int slice) {
-  __shared__ __align__(8) float2 peer[kProbsCtas * THREADS / 32];
-  __shared__ uint64_t bar;                               // they are there
+  __shared__ float2 peer[kProbsCtas * THREADS / 32];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = n_ctas > 1 ? static_cast<int>(cg::this_cluster().block_rank()) : 0;
   const int r = blockIdx.x / n_ctas;
   const int first = min(rank * slice, a.vocab), n = min(slice, a.vocab - first);
-  if (tid == 0) {
-    mbar_init(&bar, 1);
-    mbar_fence_init();
-    if (n_ctas > 1) mbar_arrive_expect_tx(&bar, n_ctas * (THREADS / 32) * sizeof(float2));
-  }
-  if (n_ctas > 1) cluster_arrive_release();              // (waited for before anything is sent)
+  // (that it is there: waited for before anything is written to it)
+  if (n_ctas > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   griddep_wait();
   const T* in = static_cast<const T*>(a.x) + r * a.ld + first;
   float* out = a.out + r * a.ld_out + first;
@@ -116,13 +111,11 @@ __global__ void __launch_bounds__(THREADS, 32768 / (NV * THREADS))
   if (bad) flag_status(a.status, DVI_DEV_NONFINITE);
   if (n_ctas > 1) {
     cluster_wait_acquire();
-    if (lane < n_ctas)
-      send_to(&peer[rank * (THREADS / 32) + warp], bits_of(mine.x, mine.y), &bar, lane);
-    if (!mbar_wait(&bar, 0, a.status)) return;
-  } else {
-    if (lane == 0) peer[warp] = mine;
-    __syncthreads();
+    if (lane < n_ctas) *cg::this_cluster().map_shared_rank(&peer[rank * (THREADS / 32) + warp], lane) = mine;
+  } else if (lane == 0) {
+    peer[warp] = mine;
   }
+  cluster_barrier(n_ctas);
   float top, sum;
   int hot;
   join<THREADS / 32>(peer, n_ctas, greedy, c, &top, &sum, &hot);

@@ -73,31 +73,66 @@ __device__ const Powers kPowersOf2 = make_powers();
 // x - m and its product t with the slope are f32 pairs; t = q / kPowers + u, 2^(q / kPowers) comes from
 // the table and an exponent, and 2^u - 1 = u ln 2 + ... is small enough for one number.  Adding
 // 1.5 * 2^23 rounds to whole numbers and leaves them in the low bits: 22 bits of w, then 22 more.
+// Two numbers are weighed together: an operation on a register pair is one instruction.
+struct Two {
+  unsigned long long v;
+};
+__device__ __forceinline__ Two two(float a, float b) {
+  Two r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ Two two(float a) { return two(a, a); }
+__device__ __forceinline__ float2 split(Two a) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+  return r;
+}
+__device__ __forceinline__ Two operator+(Two a, Two b) {
+  Two r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+  Two r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Two fma(Two a, Two b, Two c) {
+  Two r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ Two operator-(Two a, Two b) { return fma(b, two(-1.f), a); }   // (the product is exact)
+
 struct Weigher {
   float m;
   Slope c;
   const float2* powers;
-  // The two halves, each beside kBits.
+  // The two halves of each, beside kBits.
   static constexpr unsigned kBits = 0x4b400000u;   // of 1.5 * 2^23
-  __device__ __forceinline__ void halves(float x, unsigned& high, unsigned& rest) const {
-    const float kRound = 12582912.f;
-    const float dh = __fsub_rn(x, m), back = __fsub_rn(dh, x);
-    const float dl = __fsub_rn(__fsub_rn(x, __fsub_rn(dh, back)), __fadd_rn(m, back));
-    const float th = __fmul_rn(dh, c.hi);
-    const float tl = fmaf(dl, c.hi, fmaf(dh, c.lo, fmaf(dh, c.hi, -th)));
-    const float q = fmaf(th, static_cast<float>(kPowers), kRound);
-    const float r = fmaf(__fsub_rn(q, kRound), -1.f / kPowers, th);
-    const unsigned bits = __float_as_uint(q);
-    const float2 power = powers[bits % kPowers];
-    const float u = __fadd_rn(r, __fsub_rn(tl, power.y));
-    const float p = u * fmaf(u, fmaf(u, 0.055504109f, 0.24022651f), 0.69314718f);
+  __device__ __forceinline__ void halves(float x0, float x1, unsigned (&high)[2], unsigned (&rest)[2]) const {
+    const Two kRound = two(12582912.f), ch = two(c.hi), x = two(x0, x1), top = two(m);
+    const Two dh = x - top, back = dh - x;
+    const Two dl = (x - (dh - back)) - (top + back);
+    const Two th = dh * ch;
+    const Two tl = fma(dl, ch, fma(dh, two(c.lo), fma(dh, ch, dh * two(-c.hi))));
+    const Two q = fma(th, two(static_cast<float>(kPowers)), kRound);
+    const Two r = fma(q - kRound, two(-1.f / kPowers), th);
+    const float2 qs = split(q);
+    const unsigned b0 = __float_as_uint(qs.x), b1 = __float_as_uint(qs.y);
+    const float2 p0 = powers[b0 % kPowers], p1 = powers[b1 % kPowers];
+    const Two u = r + (tl - two(p0.y, p1.y));
+    const Two p = u * fma(u, fma(u, two(0.055504109f), two(0.24022651f)), two(0.69314718f));
     // (kPowers = 2^9: q / kPowers to the exponent's place, where what 1.5 * 2^23 leaves has gone)
-    const float h = __uint_as_float(__float_as_uint(power.x) + (22u << 23) + ((bits & ~(kPowers - 1u)) << 14));
-    const float hp = fmaf(h, p, h);
-    const float a = __fadd_rn(hp, kRound);
-    const float left = __fadd_rn(__fsub_rn(hp, __fsub_rn(a, kRound)), fmaf(h, p, __fsub_rn(h, hp)));
-    high = __float_as_uint(a);
-    rest = __float_as_uint(fmaf(left, 4194304.f, kRound));
+    const Two h = two(__uint_as_float(__float_as_uint(p0.x) + (22u << 23) + ((b0 & ~(kPowers - 1u)) << 14)),
+                      __uint_as_float(__float_as_uint(p1.x) + (22u << 23) + ((b1 & ~(kPowers - 1u)) << 14)));
+    const Two hp = fma(h, p, h);
+    const Two a = hp + kRound;
+    const Two left = (hp - (a - kRound)) + fma(h, p, h - hp);
+    const float2 as = split(a), rs = split(fma(left, two(4194304.f), kRound));
+    high[0] = __float_as_uint(as.x), high[1] = __float_as_uint(as.y);
+    rest[0] = __float_as_uint(rs.x), rest[1] = __float_as_uint(rs.y);
   }
   __device__ __forceinline__ static unsigned long long join(unsigned high, unsigned rest) {
     return static_cast<unsigned long long>(high - kBits) * 4194304ull + static_cast<long long>(static_cast<int>(rest - kBits));
@@ -107,9 +142,9 @@ struct Weigher {
 __device__ __noinline__ unsigned long long mass_of(float x, float m, float c_hi, float c_lo, const float2* powers) {
   Weigher w = {m, Slope(1.f), powers};
   w.c.hi = c_hi, w.c.lo = c_lo;
-  unsigned high, rest;
-  w.halves(x, high, rest);
-  return x >= w.low() ? Weigher::join(high, rest) : 0;
+  unsigned high[2], rest[2];
+  w.halves(x, x, high, rest);
+  return x >= w.low() ? Weigher::join(high[0], rest[0]) : 0;
 }
 // A thread's sum of masses: at most 64 halves of at most 2^22 each.
 struct MassSum {
@@ -508,9 +543,9 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
       if (!__any_sync(0xffffffffu, MASS ? v[0] >= low || v[1] >= low : near[0] || near[1])) continue;
       unsigned high[2], rest[2];
       if (MASS) {
+        row.mass.halves(v[0], v[1], high, rest);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          row.mass.halves(v[e], high[e], rest[e]);
           if (v[e] >= low) all.add(high[e], rest[e]);
           if (past[e]) ahead.add(high[e], rest[e]);
         }
