@@ -30,9 +30,9 @@ __device__ __forceinline__ void join(const float2* peer, int n_ctas, bool greedy
   *hot = __reduce_min_sync(0xffffffffu, first);
 }
 
-// Rows without cuts: NV logits a thread, in registers; four at a time that lie together (V4)
-// or one.  A warp takes w to its own maximum.
-template <typename T, int NV, int THREADS, bool V4>
+// Rows without cuts: NV logits a thread, in registers; 16 bytes at a time (WIDE) or one by one.  A warp
+// takes w to its own maximum.
+template <typename T, int NV, int THREADS, bool WIDE>
 __global__ void __launch_bounds__(THREADS, 32768 / (NV * THREADS))
     token_probs_kernel(TokenProbsArgs a, int n_ctas, int slice) {
   __shared__ float2 peer[kProbsCtas * THREADS / 32];
@@ -45,21 +45,19 @@ __global__ void __launch_bounds__(THREADS, 32768 / (NV * THREADS))
   griddep_wait();
   const T* in = static_cast<const T*>(a.x) + r * a.ld + first;
   float* out = a.out + r * a.ld_out + first;
-  auto index = [&](int j) { return V4 ? ((j >> 2) * THREADS + tid) * 4 + (j & 3) : j * THREADS + tid; };
+  constexpr int kTogether = WIDE ? 16 / sizeof(T) : 1;
+  auto index = [&](int j) { return (j / kTogether * THREADS + tid) * kTogether + j % kTogether; };
   float v[NV];
-  if (V4) {
+  if constexpr (WIDE) {
 #pragma unroll
-    for (int j = 0; j < NV; j += 4) {
+    for (int j = 0; j < NV; j += kTogether) {
       const int i = index(j);
-      float4 q = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-      if (i + 4 <= n) {
-        q = load4(in + i);
-      } else if (i < n) {
-        q.x = DT<T>::ld(in + i);
-        if (i + 1 < n) q.y = DT<T>::ld(in + i + 1);
-        if (i + 2 < n) q.z = DT<T>::ld(in + i + 2);
+      if (i + kTogether <= n) {
+        load16(in + i, &v[j]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kTogether; ++e) v[j + e] = i + e < n ? DT<T>::ld(in + i + e) : -INFINITY;
       }
-      v[j] = q.x, v[j + 1] = q.y, v[j + 2] = q.z, v[j + 3] = q.w;
     }
   } else {
 #pragma unroll
@@ -130,17 +128,19 @@ __global__ void __launch_bounds__(THREADS, 32768 / (NV * THREADS))
 #pragma unroll
     for (int j = 0; j < NV; ++j) v[j] = 0.f;
   }
-  if (V4) {
+  if constexpr (WIDE) {
 #pragma unroll
-    for (int j = 0; j < NV; j += 4) {
+    for (int j = 0; j < NV; j += kTogether) {
       const int i = index(j);
-      if (i + 4 <= n) {
-        *reinterpret_cast<float4*>(out + i) =
-            make_float4(v[j] * scale, v[j + 1] * scale, v[j + 2] * scale, v[j + 3] * scale);
-      } else if (i < n) {
-        out[i] = v[j] * scale;
-        if (i + 1 < n) out[i + 1] = v[j + 1] * scale;
-        if (i + 2 < n) out[i + 2] = v[j + 2] * scale;
+      if (i + kTogether <= n) {
+#pragma unroll
+        for (int e = 0; e < kTogether; e += 4)
+          *reinterpret_cast<float4*>(out + i + e) = make_float4(v[j + e] * scale, v[j + e + 1] * scale,
+                                                                v[j + e + 2] * scale, v[j + e + 3] * scale);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kTogether; ++e)
+          if (i + e < n) out[i + e] = v[j + e] * scale;
       }
     }
   } else {
@@ -150,18 +150,18 @@ __global__ void __launch_bounds__(THREADS, 32768 / (NV * THREADS))
   }
 }
 
-template <typename T, bool V4>
+template <typename T, bool WIDE>
 cudaError_t launch_plain(const TokenProbsArgs& a, cudaStream_t s) {
   const int most = a.vocab <= 32 * 256 * kProbsCtas ? 32 * 256 : a.vocab <= 32 * 512 * kProbsCtas ? 32 * 512 : 64 * 512;
   int ctas = 1;
   while (ctas * most < a.vocab) ctas *= 2;
-  if (most == 32 * 256) return launch_rows(token_probs_kernel<T, 32, 256, V4>, a, ctas, 256, 0, 0, s);
-  return most == 32 * 512 ? launch_rows(token_probs_kernel<T, 32, 512, V4>, a, ctas, 512, 0, 0, s)
-                          : launch_rows(token_probs_kernel<T, 64, 512, V4>, a, ctas, 512, 0, 0, s);
+  if (most == 32 * 256) return launch_rows(token_probs_kernel<T, 32, 256, WIDE>, a, ctas, 256, 0, 0, s);
+  return most == 32 * 512 ? launch_rows(token_probs_kernel<T, 32, 512, WIDE>, a, ctas, 512, 0, 0, s)
+                          : launch_rows(token_probs_kernel<T, 64, 512, WIDE>, a, ctas, 512, 0, 0, s);
 }
 template <typename T>
 cudaError_t launch_plain(const TokenProbsArgs& a, cudaStream_t s) {
-  return fours<T>(a) ? launch_plain<T, true>(a, s) : launch_plain<T, false>(a, s);
+  return rows_aligned<T>(a) ? launch_plain<T, true>(a, s) : launch_plain<T, false>(a, s);
 }
 
 }  // namespace

@@ -40,18 +40,23 @@ __device__ __forceinline__ float from_ord(uint32_t o) {
   return __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o);
 }
 
-// Four logits that lie together.
-__device__ __forceinline__ float4 load4(const float* p) { return *reinterpret_cast<const float4*>(p); }
-__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
-  const uint2 w = *reinterpret_cast<const uint2*>(p);
-  return make_float4(bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y));
+// 16 bytes of logits.
+__device__ __forceinline__ void load16(const float* p, float* v) {
+  const float4 q = *reinterpret_cast<const float4*>(p);
+  v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
+}
+__device__ __forceinline__ void load16(const __nv_bfloat16* p, float* v) {
+  const uint4 q = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[2 * i] = bf16_lo(w[i]), v[2 * i + 1] = bf16_hi(w[i]);
 }
 
-// Whether rows start on the boundaries of four elements of both sides.
+// Whether rows start on 16-byte boundaries on both sides.
 template <typename T>
-bool fours(const TokenProbsArgs& a) {
-  return reinterpret_cast<uintptr_t>(a.x) % (4 * sizeof(T)) == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0 &&
-         (a.n_rows == 1 || (a.ld % 4 == 0 && a.ld_out % 4 == 0));
+bool rows_aligned(const TokenProbsArgs& a) {
+  return reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0 &&
+         (a.n_rows == 1 || (a.ld * sizeof(T) % 16 == 0 && a.ld_out % 4 == 0));
 }
 
 // The settings of row r, as they count.
@@ -96,7 +101,7 @@ template <typename K>
 cudaError_t launch_rows(K kern, const TokenProbsArgs& a, int ctas, int threads, size_t smem, size_t smem_a_logit,
                         cudaStream_t s) {
   if (static_cast<int64_t>(a.n_rows) * ctas > 0x7fffffffll) return cudaErrorInvalidConfiguration;
-  const int slice = ((a.vocab + ctas - 1) / ctas + 3) / 4 * 4;
+  const int slice = ((a.vocab + ctas - 1) / ctas + 7) / 8 * 8;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(a.n_rows) * ctas);
   cfg.blockDim = dim3(threads);

@@ -690,7 +690,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
   return {row.logit(cut), static_cast<int>(cut & ((1u << kIndexBits) - 1)) - row.first};
 }
 
-template <typename T, bool V4>
+template <typename T, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbsArgs a, int n_ctas, int slice) {
   extern __shared__ __align__(16) unsigned char dynamic[];
   __shared__ Small s;
@@ -717,28 +717,32 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
   h.powers[tid] = kPowersOf2.of[tid];
   float own = -INFINITY, odd = 0.f;   // odd: 0 of finite logits
   constexpr int kFly = 16;
-  if (V4) {
-    for (int g0 = 0; g0 < n4; g0 += kFly / 4 * kThreads) {
-      float4 q[kFly / 4];
+  constexpr int kTogether = WIDE ? 16 / sizeof(T) : 1;
+  if constexpr (WIDE) {
+    for (int g0 = 0; g0 * kTogether < n; g0 += kFly / kTogether * kThreads) {
+      float v[kFly];
 #pragma unroll
-      for (int j = 0; j < kFly / 4; ++j) {
-        const int g = g0 + j * kThreads + tid, i = 4 * g;
-        q[j] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-        if (i + 4 <= n) {
-          q[j] = load4(in + i);
-        } else if (i < n) {
-          q[j].x = DT<T>::ld(in + i);
-          if (i + 1 < n) q[j].y = DT<T>::ld(in + i + 1);
-          if (i + 2 < n) q[j].z = DT<T>::ld(in + i + 2);
+      for (int j = 0; j < kFly; j += kTogether) {
+        const int i = (g0 + j / kTogether * kThreads + tid) * kTogether;
+        if (i + kTogether <= n) {
+          load16(in + i, &v[j]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < kTogether; ++e) v[j + e] = i + e < n ? DT<T>::ld(in + i + e) : -INFINITY;
         }
       }
 #pragma unroll
-      for (int j = 0; j < kFly / 4; ++j) {
-        const int g = g0 + j * kThreads + tid;
-        if (g >= n4) continue;
-        own = fmaxf(own, fmaxf(fmaxf(q[j].x, q[j].y), fmaxf(q[j].z, q[j].w)));
-        odd = fmaf(q[j].x, 0.f, fmaf(q[j].y, 0.f, fmaf(q[j].z, 0.f, fmaf(q[j].w, 0.f, odd))));
-        x4[g] = q[j];
+      for (int j = 0; j < kFly; j += kTogether) {
+        const int i = (g0 + j / kTogether * kThreads + tid) * kTogether;
+        if (i >= n) continue;
+#pragma unroll
+        for (int e = 0; e < kTogether; ++e) {
+          own = fmaxf(own, v[j + e]);
+          odd = fmaf(v[j + e], 0.f, odd);
+        }
+#pragma unroll
+        for (int e = 0; e < kTogether; e += 4)
+          if (i + e < 4 * n4) x4[i / 4 + e / 4] = make_float4(v[j + e], v[j + e + 1], v[j + e + 2], v[j + e + 3]);
       }
     }
   } else {
@@ -775,16 +779,16 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
   const Slope c(set.temperature);
   // the tokens that the thread has loaded
   auto each = [&](auto f) {
-    if (V4) {
-      for (int g = tid; g < n4; g += kThreads)
-        for (int i = 4 * g; i < 4 * g + 4; ++i) f(i);
+    if (WIDE) {
+      for (int g = tid; g * kTogether < 4 * n4; g += kThreads)
+        for (int i = g * kTogether; i < min((g + 1) * kTogether, 4 * n4); ++i) f(i);
     } else {
       for (int i = tid; i < n; i += kThreads) f(i);
     }
   };
   bool bad = set.bad;
   if (__syncthreads_or(odd != 0.f)) {
-    // (masked tokens, too, and the -inf behind a row that ends within four)
+    // (masked tokens, too, and the -inf behind a row's end)
     own = -INFINITY;
     each([&](int i) {
       bad |= !(x[i] < INFINITY);
@@ -888,7 +892,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
     inv = 1.f / sum;
   }
   auto prob = [&](float v, int i) { return upto.has(v, i) ? weight(v, top, c) * inv : 0.f; };
-  if (V4) {
+  if (WIDE) {
     for (int g = tid; g < n4; g += kThreads) {
       const float4 q = x4[g];
       const int i = 4 * g;
@@ -909,21 +913,21 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
 
 constexpr int kSlice = 16384;   // logits of a CTA where its row may have up to kMaxCtas: two CTAs an SM
 
-template <typename T, bool V4>
+template <typename T, bool WIDE>
 cudaError_t launch_cut(const TokenProbsArgs& a, cudaStream_t s) {
   static PerDevice per_device;
   per_device.once([&] {
-    cudaFuncSetAttribute(token_probs_cut_kernel<T, V4>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    cudaFuncSetAttribute(token_probs_cut_kernel<T, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                          kMaxVocab / kMaxCtas * static_cast<int>(sizeof(float)) + static_cast<int>(sizeof(Cuts)));
   });
   int ctas = 1;
   while (ctas < kMaxCtas && (ctas * kSlice < a.vocab || (static_cast<int64_t>(a.n_rows) * ctas < 152 && a.vocab / ctas > 4096)))
     ctas *= 2;
-  return launch_rows(token_probs_cut_kernel<T, V4>, a, ctas, kThreads, sizeof(Cuts), sizeof(float), s);
+  return launch_rows(token_probs_cut_kernel<T, WIDE>, a, ctas, kThreads, sizeof(Cuts), sizeof(float), s);
 }
 template <typename T>
 cudaError_t launch_cut(const TokenProbsArgs& a, cudaStream_t s) {
-  return fours<T>(a) ? launch_cut<T, true>(a, s) : launch_cut<T, false>(a, s);
+  return rows_aligned<T>(a) ? launch_cut<T, true>(a, s) : launch_cut<T, false>(a, s);
 }
 
 }  // namespace
