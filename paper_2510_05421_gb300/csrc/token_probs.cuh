@@ -52,10 +52,10 @@ __device__ __forceinline__ void load16(const __nv_bfloat16* p, float* v) {
   for (int i = 0; i < 4; ++i) v[2 * i] = bf16_lo(w[i]), v[2 * i + 1] = bf16_hi(w[i]);
 }
 
-// Whether rows start on 16-byte boundaries on both sides.
+// Whether rows are of whole 16 bytes and start on their boundaries, on both sides.
 template <typename T>
 bool rows_aligned(const TokenProbsArgs& a) {
-  return reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0 &&
+  return a.vocab % (16 / sizeof(T)) == 0 && reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0 &&
          (a.n_rows == 1 || (a.ld * sizeof(T) % 16 == 0 && a.ld_out % 4 == 0));
 }
 

@@ -8,6 +8,12 @@
 // about 2^-44 of a border: p - q is exact as a pair of f32 numbers, its sums are
 // pairs too, and from a warp's sum on they are whole numbers of 2^-61 of the whole
 // (64-bit floating point is as slow here as a hundred of the other operations).
+//
+// Bound by memory where there is much of it: 128 sequences of 128001 tokens (two rows
+// each, 131 MB) take 30 us, a dot product of them 27; of these 5 are the looks at the
+// drafts and the search.  One sequence takes 6.7 us, a chain of five dependent loads.
+// Copies by the bulk engine, 1 KB a warp and three ahead, took 48 us; the next numbers'
+// loads under way in registers changed nothing.
 #include <cooperative_groups.h>
 
 #include "sample.cuh"
@@ -367,6 +373,8 @@ __global__ void __launch_bounds__(kThreads) verify_drafts_kernel(VerifyArgs a, i
 
 }  // namespace
 
+// As many CTAs a sequence as are resident at once (two an SM) and have something to do: 128 sequences of
+// 128001 over 2 CTAs 30 us, over 4 37; 64 of 32000 over 4 10.7, over 8 14.2.
 cudaError_t launch_verify_drafts(const VerifyArgs& a, cudaStream_t s) {
   int ctas = 1;
   while (ctas < kMaxCtas && static_cast<int64_t>(a.n_seqs) * ctas * 2 <= 304 && a.vocab / ctas > 2 * kThreads) ctas *= 2;
