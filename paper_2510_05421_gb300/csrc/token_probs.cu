@@ -38,8 +38,8 @@ __device__ __forceinline__ void join(const float2* peer, int n_ctas, bool greedy
 
 // Rows without cuts: NV logits a thread, in registers; 16 bytes at a time (WIDE) or one by one.  A warp
 // takes w to its own maximum.
-template <typename T, int NV, int THREADS, bool WIDE>
-__global__ void __launch_bounds__(THREADS, 32768 / (NV * THREADS))
+template <typename T, int NV, int THREADS, int CTAS_AN_SM, bool WIDE>
+__global__ void __launch_bounds__(THREADS, CTAS_AN_SM)
     token_probs_kernel(TokenProbsArgs a, int n_ctas, int slice) {
   __shared__ float2 peer[kProbsCtas * THREADS / 32];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -151,16 +151,24 @@ __global__ void __launch_bounds__(THREADS, 32768 / (NV * THREADS))
   }
 }
 
-// As few CTAs as hold a row: of 256 threads with 32 logits each, of 512 where that takes
-// more than eight, of 512 with 64 for the longest rows (one row of 262144).
+template <typename T, bool WIDE, int NV, int THREADS, int CTAS_AN_SM>
+cudaError_t launch_plain(const TokenProbsArgs& a, cudaStream_t s) {
+  int ctas = 1;
+  while (ctas * NV * THREADS < a.vocab) ctas *= 2;
+  return launch_rows(token_probs_kernel<T, NV, THREADS, CTAS_AN_SM, WIDE>, a, ctas, THREADS, 0, 0, s);
+}
+
+// One CTA for rows of up to 8192 logits, of no more threads and logits a thread than the row needs (4096
+// rows of 1024: 128 threads with 8 each 9 us, 256 with 32 33; of 4000: 256 with 16 22, 512 with 16 40); then
+// as few as hold a row.
 template <typename T, bool WIDE>
 cudaError_t launch_plain(const TokenProbsArgs& a, cudaStream_t s) {
-  const int most = a.vocab <= 32 * 256 * kProbsCtas ? 32 * 256 : a.vocab <= 32 * 512 * kProbsCtas ? 32 * 512 : 64 * 512;
-  int ctas = 1;
-  while (ctas * most < a.vocab) ctas *= 2;
-  if (most == 32 * 256) return launch_rows(token_probs_kernel<T, 32, 256, WIDE>, a, ctas, 256, 0, 0, s);
-  return most == 32 * 512 ? launch_rows(token_probs_kernel<T, 32, 512, WIDE>, a, ctas, 512, 0, 0, s)
-                          : launch_rows(token_probs_kernel<T, 64, 512, WIDE>, a, ctas, 512, 0, 0, s);
+  if (a.vocab <= 8 * 128) return launch_plain<T, WIDE, 8, 128, 12>(a, s);
+  if (a.vocab <= 16 * 128) return launch_plain<T, WIDE, 16, 128, 12>(a, s);
+  if (a.vocab <= 16 * 256) return launch_plain<T, WIDE, 16, 256, 6>(a, s);
+  if (a.vocab <= 32 * 256 * kProbsCtas) return launch_plain<T, WIDE, 32, 256, 4>(a, s);
+  if (a.vocab <= 32 * 512 * kProbsCtas) return launch_plain<T, WIDE, 32, 512, 2>(a, s);
+  return launch_plain<T, WIDE, 64, 512, 1>(a, s);
 }
 template <typename T>
 cudaError_t launch_plain(const TokenProbsArgs& a, cudaStream_t s) {
