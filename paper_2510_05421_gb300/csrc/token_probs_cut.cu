@@ -490,7 +490,10 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     v += p.x;
     tokens += p.y;
   }
-  if (!MASS && tokens < top_k) return upto;   // (fewer tokens than top_k)
+  if (!MASS && tokens < top_k) {              // (fewer tokens than top_k)
+    cluster_barrier(n_ctas);                  // (all have read the sums before the next are sent)
+    return upto;
+  }
   const float all_bins = warp_sum(v), about = MASS ? top_p * all_bins : static_cast<float>(top_k);
   float before_it = 0.f;
   const int group = all_bins >= about ? first_reaching(v, about, &before_it) : -1;
@@ -612,7 +615,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     if (here) break;
     if (!MASS && by_maxima) return upto;
     n = kList + 1;
-    __syncthreads();   // (before the list is begun again)
+    cluster_barrier(n_ctas);   // (all have what was sent before more is)
   }
   unsigned long long cut;
   if (n <= kList) {
