@@ -13,8 +13,10 @@
 // They show whether the bin is the right one (else it is its neighbour's turn) and,
 // among its tokens, which is the last.  Every CTA comes to the same end, whatever the
 // order of its atomics.  Where top_k leaves few tokens, all of these go to all instead,
-// which is all that top_p needs, too.  Where the bin has too many tokens (logits that are
-// nearly equal), the token's place in the order, as a number, is found 10 bits at a time.
+// which is all that top_p needs, too.  Where the bin has too many tokens, a part of it is
+// tried, where the cut would be if they lay evenly (a row of 128001 with top_p 26 us, such a
+// row 38, and 102 by what follows); where that has too many, too (logits that are equal),
+// the token's place in the order, as a number, is found 10 bits at a time.
 //
 // What the CTAs give each other are stores that the receiver's barrier counts: no CTA
 // waits for its own memory operations, as at a cluster's barrier (a block of 6 rows of
@@ -43,7 +45,7 @@ constexpr int kWide = 768;                       // from this bin on they are fo
 constexpr int kList = 1024;                      // tokens of a bin that are sorted out by each CTA
 constexpr int kListPer = kList / kThreads;
 constexpr int kFew = 128;                        // tokens that are compared with each other, by four threads each
-constexpr int kTries = 3;                        // bins that are summed before the slow way is taken
+constexpr int kTries = 4;                        // parts of the histogram that are summed before the slow way is taken
 constexpr int kIndexBits = 18;                   // kMaxVocab
 
 // Numbers T_k near 2^(k / kPowers) that are f32 numbers themselves, and how far log2 T_k is from
@@ -517,11 +519,13 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     before = static_cast<unsigned long long>(before_it);   // (of counts, which are exact)
     wide = !MASS && (by_maxima || before_it + __shfl_sync(0xffffffffu, v, bin & 31) <= kList);
   }
-  for (int tries = 0; bin >= 0 && tries < kTries; ++tries) {
-    // Sums of the tokens before the bin, in it and of all, and its tokens, to all.  Logits past `above`
+  int lo = bin * kSteps, hi = lo + kSteps;   // the part of the histogram that is looked at
+  for (int tries = 0; lo >= 0 && hi <= (kBins - 1) * kSteps && tries < kTries; ++tries) {
+    // Sums of the tokens before the part, in it and of all, and its tokens, to all.  Logits past `above`
     // are before it, below `under` behind it, by more than what rounding may do.
     const float width = kSteps / scale;
-    const float above_it = row.m - row.from(bin - 0.25f) * width, under_it = row.m - row.from(bin + 1.25f) * width;
+    const float above_it = row.m - row.from(lo * (1.f / kSteps) - 0.25f) * width,
+                under_it = row.m - row.from(hi * (1.f / kSteps) + 0.25f) * width;
     const float above = above_it + 0x1p-21f * fmaxf(fabsf(row.m), fabsf(above_it)),
                 under = under_it - 0x1p-21f * fmaxf(fabsf(row.m), fabsf(under_it));
     if (tid == 0) {
@@ -542,7 +546,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
         for (int e = 0; e < 2; ++e)
           if (!upto.has(v[e], 2 * g + e)) v[e] = -INFINITY;
       }
-      // (a token of the bin is not below `low`, but all are where low is -inf)
+      // (a token of the part is not below `low`, but all are where low is -inf)
       bool past[2], near[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -563,9 +567,9 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         if (!near[e]) continue;
-        const int b = row.bin(v[e], scale);
-        if (MASS && b < bin) ahead.add(high[e], rest[e]);
-        if (wide ? b > bin : b != bin) continue;
+        const int step = row.step(v[e], scale);
+        if (MASS && step < lo) ahead.add(high[e], rest[e]);
+        if (step >= hi || (step < lo && !wide)) continue;
         if (MASS) within.add(high[e], rest[e]);
         const int to = atomicAdd(&s.n_list, 1);
         if (to >= cap) continue;
@@ -591,7 +595,8 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     // (a lane a CTA)
     const int there = lane < n_ctas ? static_cast<int>(box.sum[turn[2] & 1][3][lane]) : 0;
     const int sent = __reduce_add_sync(0xffffffffu, min(there, cap));
-    n = __reduce_max_sync(0xffffffffu, there) > cap ? kList + 1 : sent;
+    const int most = __reduce_max_sync(0xffffffffu, there);
+    n = most > cap ? kList + 1 : sent;
     if (tid == 0) expect(&box.bar[4], sent * 8, n_ctas);
     bool here = MASS || !wide || n <= kList;   // (else the bin's tokens alone)
     if (!MASS && by_maxima) *fits = here;
@@ -609,7 +614,18 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
       }
       target = share_of(top_p, all);
       here = before < target && before + in_it >= target;
-      if (!here) bin = before >= target ? bin - 1 : bin < kBins - 2 ? bin + 1 : -1;
+      const int span = hi - lo;
+      if (!here) {
+        lo += before >= target ? -span : span;
+        hi = lo + span;
+      } else if (n > kList && span > 1) {
+        // as much of it as should have half of a list, where the cut would be if its tokens lay evenly
+        const int part = max(1, span * (kList / 2) / (most * n_ctas));
+        lo += min(max(static_cast<int>(__ull2float_rn(target - before) / __ull2float_rn(in_it) * span) - part / 2, 0),
+                  span - part);
+        hi = lo + part;
+        here = false;
+      }
     }
     if (!arrived(&box.bar[4], turn[2]++, n_ctas, row.status)) return upto;
     if (here) break;

@@ -270,3 +270,25 @@ def test_top_k_where_the_likeliest_lie_together(V, k):
     x[3, :n] = top.bfloat16().float()                           # with ties
     check(x.cuda(), 1.0, k)
     check(x.cuda(), 1.0, k, 0.9)
+
+
+@pytest.mark.parametrize("V", [32000, 128001])
+@pytest.mark.parametrize("p", [0.1137, 0.5377, 0.9861])
+@pytest.mark.parametrize("how", ["wide", "dense", "sorted", "lumps", "two"])
+def test_many_tokens_where_the_cut_is(V, p, how):
+    """More tokens lie together at top_p's cut than are sorted out at once: spread evenly, in order, in lumps."""
+    g = torch.Generator().manual_seed(int(p * 1e4) + V)
+    if how == "wide":                                           # logits as they are, the cut far below the largest
+        x, T = logits(6, V, 23, std=2.0) + torch.tensor([[0.0], [1.0], [2.0], [3.0], [4.0], [5.0]]) * 0.01, 0.78
+        x[:, 7] = 17.0
+    elif how == "dense":
+        x, T = 5 + 1e-3 * torch.rand(3, V, generator=g), 1.0
+    elif how == "sorted":
+        x, T = (5 + 1e-2 * torch.rand(3, V, generator=g)).sort(-1)[0], 1.0
+    elif how == "lumps":                                        # most of them equal, the others on one side or both
+        x, T = 5 + 1e-2 * torch.rand(3, V, generator=g), 1.0
+        lump = torch.rand(3, V, generator=g) < torch.tensor([[0.5], [0.9], [0.99]])
+        x[lump] = torch.tensor([[5.001], [5.009], [5.005]]).expand(3, V)[lump]
+    else:                                                       # two values, next to each other
+        x, T = torch.where(torch.rand(3, V, generator=g) < 0.5, 5.0, 5.0 + 2.0 ** -21), 1.0
+    check(x.cuda(), T, 0, p)
