@@ -507,7 +507,7 @@ typedef struct {
  * order of any sum.  NaN logits count as -inf and +inf as the largest finite number
  * (DVI_DEV_NONFINITE).  Of settings in device arrays, T that is negative or NaN counts
  * as 0, top_k below 0 as 0, top_p NaN as 1 (NaN: DVI_DEV_NONFINITE).  d_probs may be
- * d_logits itself (f32, the same ld); else they do not overlap. */
+ * d_logits itself (f32, the same ld); rows that overlap in another way are refused. */
 dvi_status dvi_token_probs(int dtype, const void* d_logits, int64_t ld_logits, int n_rows, int vocab,
                            const dvi_sampling* sampling, float* d_probs, int64_t ld_probs, int32_t* d_status,
                            dvi_stream stream);

@@ -8,6 +8,15 @@ using namespace dvi;
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 // Null, or an array of 4-byte elements.
 bool words_ok(const void* p) { return aligned(p, 4); }
+// Whether rows of the probabilities share memory with rows of the logits (n of each, ld bytes from row to
+// row).  They may be the same numbers; rows that lie between the others' are found apart only for equal ld.
+bool overlap(uintptr_t x, int64_t ld_x, int64_t row_x, uintptr_t out, int64_t ld_out, int64_t row_out, int64_t n) {
+  if (x == out && row_x == row_out && (n == 1 || ld_x == ld_out)) return false;
+  if (x + (n - 1) * ld_x + row_x <= out || out + (n - 1) * ld_out + row_out <= x) return false;
+  if (n == 1 || ld_x != ld_out) return true;
+  const int64_t d = static_cast<int64_t>(out - x) % ld_x, at = d < 0 ? d + ld_x : d;
+  return at < row_x || at + row_out > ld_x;
+}
 // The launchers refuse grids past 31 bits.
 dvi_status launched(cudaError_t e) {
   return e == cudaSuccess ? DVI_OK : e == cudaErrorInvalidConfiguration ? DVI_ERR_CAPACITY : DVI_ERR_CUDA;
@@ -30,6 +39,10 @@ extern "C" dvi_status dvi_token_probs(int dtype, const void* d_logits, int64_t l
   if (n_rows == 0) return DVI_OK;
   if (!d_logits || !d_probs || !aligned(d_logits, dtype == DVI_F32 ? 4 : 2) || !aligned(d_probs, 4) ||
       ld_logits < vocab || ld_probs < vocab)
+    return DVI_ERR_INVALID_ARG;
+  const int64_t e = dtype == DVI_F32 ? 4 : 2;
+  if (overlap(reinterpret_cast<uintptr_t>(d_logits), ld_logits * e, vocab * e, reinterpret_cast<uintptr_t>(d_probs),
+              ld_probs * 4, vocab * int64_t{4}, n_rows))
     return DVI_ERR_INVALID_ARG;
   TokenProbsArgs a{};
   a.x = d_logits;

@@ -292,3 +292,18 @@ def test_many_tokens_where_the_cut_is(V, p, how):
     else:                                                       # two values, next to each other
         x, T = torch.where(torch.rand(3, V, generator=g) < 0.5, 5.0, 5.0 + 2.0 ** -21), 1.0
     check(x.cuda(), T, 0, p)
+
+
+def test_rows_beside_each_other_and_over_each_other():
+    from paper_2510_05421_gb300 import DVIError, token_probs
+    V = 1000
+    buf = torch.zeros(5, 2 * V + 8, device="cuda")
+    x = logits(5, V, 24).cuda()
+    for cuts in (dict(), dict(top_k=20, top_p=0.9)):
+        want = token_probs(x, **cuts)
+        buf[:, 4:V + 4] = x
+        assert torch.equal(token_probs(buf[:, 4:V + 4], out=buf[:, V + 4:2 * V + 4], **cuts), want)
+        assert torch.equal(buf[:, 4:V + 4], x)
+        for out in (buf[:, 5:V + 5], buf[:, :V], buf[:, V + 3:2 * V + 3]):
+            with pytest.raises(DVIError):
+                token_probs(buf[:, 4:V + 4], out=out, **cuts)

@@ -105,3 +105,12 @@ def test_paged_plan_sizes(L, kw):
 
 def test_paged_plan_of_nothing(L):
     assert L.dvi_paged_plan(None, A, A, 0, 8, A, A, A, None) == -1
+
+
+@pytest.mark.parametrize("kw", [dict(out=A + 4), dict(out=A - 4), dict(out=A + 400), dict(out=A + 1600 - 4), dict(ld=128),
+                                dict(ld_out=128, out=A + 256), dict(dtype=1), dict(dtype=1, ld=200, out=A + 4),
+                                dict(ld=210, ld_out=210, out=A + 396), dict(ld=210, ld_out=210, out=A + 210 * 4 - 4),
+                                dict(n=1, out=A + 4), dict(n=1, dtype=1)])
+def test_probabilities_over_their_own_logits(L, kw):
+    """Rows that share memory and are not the same: 100 numbers of 4 (logits in bf16: 2) bytes a row."""
+    assert probs(L, **kw) == -1
