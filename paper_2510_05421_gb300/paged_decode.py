@@ -59,7 +59,7 @@ class Sampling:
         return token_probs(logits, self.temperature, self.top_k, self.top_p)
 
     def draw(self, probs: torch.Tensor) -> torch.Tensor:
-        """A token of each row."""
+        """A token of each row (-1 of a row without probabilities)."""
         n = probs.shape[0]
         none = probs.new_empty(0)
         return verify_drafts(probs, none.to(torch.int32), none, self.uniform(n, probs.device))[0][:, 0]
@@ -255,9 +255,12 @@ class PagedDecoder:
                                       sampling.uniform(n_live * K, self.device), sampling.uniform(n_live, self.device),
                                       draft=q, max_drafts=K, bonus=False)
             n, m = n.long(), m.long()
-        new_pending = out.gather(1, (n - 1).long()[:, None]).squeeze(1)
+        new_pending = out.gather(1, (n - 1).clamp_min(0).long()[:, None]).squeeze(1)
         n = self._spread(at, n)
-        self.advance(n.tolist())
+        kept = n.tolist()
+        if not all(kept[b] for b in live):
+            raise RuntimeError("step: no token has a probability above 0 (logits that are no numbers)")
+        self.advance(kept)
         return self._spread(at, out), n, self._spread(at, m), self._spread(at, new_pending, pending)
 
     def ar_step(self, pending: torch.Tensor, live: Optional[Sequence[int]] = None,

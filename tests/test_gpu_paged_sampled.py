@@ -143,3 +143,15 @@ def test_command(monkeypatch, capsys):
                                      "0.8", "--top-p", "0.9", "--top-k", "50", "--device-pages"])
     main()
     assert '"device_flags": []' in capsys.readouterr().out
+
+
+def test_logits_that_are_no_numbers():
+    """A step whose target gives no token says so (its sequence would never end)."""
+    w, _, dec = make(True)
+    tok = dec.prefill(make_prompts(w))
+    lens = dec.lens.tolist()
+    good = dec.verifier_logits
+    dec.verifier_logits = lambda h: torch.where(torch.arange(len(good(h)), device="cuda")[:, None] < w.k_spec, torch.nan, good(h))
+    with pytest.raises(RuntimeError, match="no token"):
+        dec.step(tok, sampling=sampling(1))
+    assert dec.lens.tolist() == lens
