@@ -542,8 +542,10 @@ typedef struct {
  * d_out_ids [n_seqs][max_drafts + bonus]: x_1 .. x_m and the token, -1 behind them;
  * d_n_committed [n_seqs]: m + 1, or K at m = K without a bonus row; d_n_accepted
  * [n_seqs]: m.  A drafted id outside [0, vocab) is rejected (DVI_DEV_BAD_TOKEN) and
- * its row's q taken as it is (greedy: as 0).  A row that is zero everywhere gives no
- * token (DVI_DEV_NONFINITE): n_committed is m. */
+ * its row's q taken as it is (greedy: as 0).  Of draft_start, an entry outside [0,
+ * n_drafts] counts as the nearest in it, one below its sequence's first as that
+ * (DVI_DEV_BAD_TOKEN).  A row that is zero everywhere gives no token
+ * (DVI_DEV_NONFINITE): n_committed is m. */
 dvi_status dvi_verify_drafts(const dvi_draft_batch* batch, const float* d_target, int64_t ld_target,
                              const float* d_draft, int64_t ld_draft, int32_t* d_out_ids, int32_t* d_n_committed,
                              int32_t* d_n_accepted, dvi_stream stream);

@@ -319,13 +319,13 @@ __global__ void __launch_bounds__(kThreads) verify_drafts_kernel(VerifyArgs a, i
   __syncthreads();
   const int m = s.m;
   const bool some = m < K || a.bonus;
-  int flags = 0;
+  int flags = a.start && (a.start[b] != s0 || a.start[b + 1] != s1) ? DVI_DEV_BAD_TOKEN : 0;
   Residual r = {a.p + (row0 + m) * a.ld_p, nullptr, -1};
   if (m < K) {
     if (a.q) r.q = a.q + (s0 + m) * a.ld_q;
     r.hot = a.ids[s0 + m];
     if (r.hot < 0 || r.hot >= V) {
-      flags = DVI_DEV_BAD_TOKEN;
+      flags |= DVI_DEV_BAD_TOKEN;
       r.hot = -1;
     }
   }

@@ -79,7 +79,7 @@ def verify_drafts(target: torch.Tensor, draft_ids: torch.Tensor, u_accept: torch
 
     Returns (ids int32 [n_seqs, max_drafts + bonus], how many of them are committed, how many drafts were accepted);
     entries behind the committed ones are -1.  status (int32 [1], or None): DVI_DEV_BAD_TOKEN for a drafted id outside
-    the vocabulary (rejected), DVI_DEV_NONFINITE for probabilities that are not finite (taken as 0) and rows that are
+    the vocabulary (rejected) and for starts that fall or lie outside the drafts (cut to them), DVI_DEV_NONFINITE for probabilities that are not finite (taken as 0) and rows that are
     zero everywhere (no token)."""
     index = _device_of("verify_drafts: target", target)
     if stream is not None or _current() != index:

@@ -155,6 +155,17 @@ def test_starts_out_of_order_stay_inside():
     assert torch.equal(got[0][0], want[0][0]) and int(got[2][1]) == 0
 
 
+@pytest.mark.parametrize("start,flag", [([0, 2, 4, 6], 0), ([0, 2, 6, 6], 0), ([1, 2, 3, 5], 0), ([0, 4, 2, 6], 8),
+                                        ([0, 2, 4, 7], 8), ([-1, 2, 4, 6], 8), ([0, 2, 4, -1], 8)])
+def test_starts_out_of_order_are_flagged(start, flag):
+    from paper_2510_05421_gb300 import verify_drafts
+    p, ids, ua, ut, q = (torch.from_numpy(t).cuda() for t in case([2, 2, 2], 300, 9, 1))
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    verify_drafts(p, ids, ua, ut, draft=q, draft_start=torch.tensor(start, dtype=torch.int32).cuda(), max_drafts=6,
+                  status=status)
+    assert int(status) == flag
+
+
 def test_committed_tokens_are_distributed_as_the_targets():
     """One draft, a grid of both uniform numbers: the committed first token has the target's probabilities.  A cell of
     the grid is 2^-8 wide; acceptance and each of the V ranges of the token can be off by one cell."""
