@@ -177,7 +177,8 @@ class PagedDecoder:
     # -- calls ------------------------------------------------------------
     def prefill(self, prompts: Sequence[np.ndarray], sampling: Optional[Sampling] = None) -> torch.Tensor:
         """The prompts, one for each slot, in one ragged pass behind what the sequences hold; the greedy (or sampled) token
-        after each (pending, in no cache yet).  A slot whose prompt is empty takes no rows, and its token is -1."""
+        after each (pending, in no cache yet).  A slot whose prompt is empty takes no rows, and its token is -1, as is a
+        sampled one where no token has a probability above 0 (logits that are no numbers)."""
         if len(prompts) != len(self.host_lens):
             raise ValueError(f"prefill: {len(prompts)} prompts for {len(self.host_lens)} slots")
         rows = [len(p) for p in prompts]
@@ -198,6 +199,12 @@ class PagedDecoder:
         if sampling is None:
             return logits.argmax(-1).to(torch.int32)
         return sampling.draw(sampling.probs(logits))
+
+    @staticmethod
+    def _some_token(what: str, got: Sequence[int]):
+        """Refuses the -1 of a row that gave no token."""
+        if min(got, default=0) < 0:
+            raise RuntimeError(f"{what}: no token has a probability above 0 (logits that are no numbers)")
 
     def _taking_part(self, live: Optional[Sequence[int]]):
         """The sequences of a pass (by default those that hold rows), where they lie in tensors of all sequences and
@@ -258,8 +265,7 @@ class PagedDecoder:
         new_pending = out.gather(1, (n - 1).clamp_min(0).long()[:, None]).squeeze(1)
         n = self._spread(at, n)
         kept = n.tolist()
-        if not all(kept[b] for b in live):
-            raise RuntimeError("step: no token has a probability above 0 (logits that are no numbers)")
+        self._some_token("step", [kept[b] - 1 for b in live])
         self.advance(kept)
         return self._spread(at, out), n, self._spread(at, m), self._spread(at, new_pending, pending)
 
@@ -284,7 +290,8 @@ class PagedDecoder:
         if not all(len(p) for p in prompts):
             raise ValueError("generate: an empty prompt has no next token")
         tok = self.prefill(prompts, sampling)
-        out = [[int(t)] for t in tok]
+        out = [[t] for t in tok.tolist()]
+        self._some_token("generate", [t for t, in out])
         agreed = steps = 0
         while live := [b for b, o in enumerate(out) if len(o) < n_gen]:
             if speculative:
@@ -295,6 +302,7 @@ class PagedDecoder:
             else:
                 tok = self.ar_step(tok, live, sampling)
                 new = tok.tolist()
+                self._some_token("generate", [new[b] for b in live])
                 for b in live:
                     out[b].append(new[b])
             steps += len(live)

@@ -155,3 +155,20 @@ def test_logits_that_are_no_numbers():
     with pytest.raises(RuntimeError, match="no token"):
         dec.step(tok, sampling=sampling(1))
     assert dec.lens.tolist() == lens
+
+
+@pytest.mark.parametrize("at", [0, 2])
+def test_generated_tokens_that_are_none(at):
+    """Without drafts too: the prompt's next token, or a later one, that no probability gives is an error, not a token."""
+    w, _, dec = make(True)
+    good, calls = dec.verifier_logits, []
+
+    def logits(h):
+        calls.append(len(h))
+        z = good(h)
+        return torch.where(torch.arange(len(z), device="cuda")[:, None] < 1, torch.nan, z) if len(calls) == at + 1 else z
+
+    dec.verifier_logits = logits
+    with pytest.raises(RuntimeError, match="no token"):
+        dec.generate(make_prompts(w), 12, False, sampling(1))
+    assert len(calls) == at + 1
