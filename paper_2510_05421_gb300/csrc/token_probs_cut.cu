@@ -38,10 +38,17 @@ constexpr int kMaxCtas = kProbsCtas;
 constexpr int kBins = 1024;                      // 32 groups of 32
 constexpr int kBinBits = 10;
 constexpr int kPer = kBins / kThreads;
+constexpr int kRow = 128;                        // logits that a warp looks at together, four a thread
 constexpr int kSteps = 1024;                     // places within a bin
 constexpr float kBinsPerOctave = 40.f;           // of w
 constexpr int kWide = 768;                       // from this bin on they are four times as wide: the last one has what
                                                  // is below 2^-44.6
+constexpr float kFall = 0.69314718f / kBinsPerOctave;   // of w over a bin, by its tangent (a wide one: four times that)
+// w at a bin's begin, less 1 for every step, where w falls by 1 over a step at the bin's middle; and what w is
+// above its tangent, for tokens that lie evenly.
+constexpr unsigned kTop = static_cast<unsigned>(kSteps * (1.f / kFall + 0.5f + kFall / 24.f) + 0.5f),
+                   kTopWide = static_cast<unsigned>(kSteps * (0.25f / kFall + 0.5f + kFall / 6.f) + 0.5f);
+static_assert(kMaxVocab / kMaxCtas * static_cast<unsigned long long>(kTop) < 1ull << 32, "a bin's sum");
 constexpr int kList = 1024;                      // tokens of a bin that are sorted out by each CTA
 constexpr int kListPer = kList / kThreads;
 constexpr int kFew = 128;                        // tokens that are compared with each other, by four threads each
@@ -50,7 +57,7 @@ constexpr int kIndexBits = 18;                   // kMaxVocab
 
 // Numbers T_k near 2^(k / kPowers) that are f32 numbers themselves, and how far log2 T_k is from
 // k / kPowers: so 2^t = T_k 2^(t - k / kPowers - d_k) without a second number for T_k.
-constexpr int kPowers = 512;
+constexpr int kPowers = 1024;
 struct Powers {
   float2 of[kPowers];
 };
@@ -78,9 +85,11 @@ constexpr Powers make_powers() {
 __device__ const Powers kPowersOf2 = make_powers();
 
 // w in units of 2^-44, off by about 2^-34 of itself; 0 below 2^-46 (low: where that is, or above).
-// x - m and its product t with the slope are f32 pairs; t = q / kPowers + u, 2^(q / kPowers) comes from
-// the table and an exponent, and 2^u - 1 = u ln 2 + ... is small enough for one number.  Adding
-// 1.5 * 2^23 rounds to whole numbers and leaves them in the low bits: 22 bits of w, then 22 more.
+// t = (x - m) c is x c less m c.  Adding 1.5 * 2^23 / kPowers rounds x c to multiples q of 1 / kPowers and
+// leaves them in the low bits; the rest x c - q is one number, as a fused multiply-add rounds only what is
+// left.  (|x c| stays below 4096: where |m c| does not, what counts is so near to m that x - m is exact and
+// takes x's place.)  The rest of m c is in the table, turned by m's own q: 2^q from the table and an
+// exponent, 2^u - 1 = u ln 2 + ... is small enough for one number.  w in 22 bits, then 22 more.
 // Two numbers are weighed together: an operation on a register pair is one instruction.
 struct Two {
   unsigned long long v;
@@ -116,31 +125,39 @@ __device__ __forceinline__ Two operator-(Two a, Two b) { return fma(b, two(-1.f)
 struct Weigher {
   float m;
   Slope c;
-  const float2* powers;
+  const float2* powers;   // turned: by the low bits of the sum with kGrid, as bits that want (q's other bits) << 13 only
+  float base;             // 0, or m
+  float least;            // of x - base: w there is 2^-46, which rounds to 0, as it is below
+  static constexpr float kGrid = 12582912.f / kPowers;
   // The two halves of each, beside kBits.
   static constexpr unsigned kBits = 0x4b400000u;   // of 1.5 * 2^23
+  __device__ __forceinline__ Weigher(float m, Slope c, const float2* powers)
+      : m(m), c(c), powers(powers), base(fabsf(m * c.hi) < 4000.f ? 0.f : m), least((m - base) - 46.f / c.hi * 1.0001f) {}
   __device__ __forceinline__ void halves(float x0, float x1, unsigned (&high)[2], unsigned (&rest)[2]) const {
-    const Two kRound = two(12582912.f), ch = two(c.hi), x = two(x0, x1), top = two(m);
-    const Two dh = x - top, back = dh - x;
-    const Two dl = (x - (dh - back)) - (top + back);
-    const Two th = dh * ch;
-    const Two tl = fma(dl, ch, fma(dh, two(c.lo), fma(dh, ch, dh * two(-c.hi))));
-    const Two q = fma(th, two(static_cast<float>(kPowers)), kRound);
-    const Two r = fma(q - kRound, two(-1.f / kPowers), th);
+    const float2 xs = split(two(x0, x1) + two(-base));
+    const Two kRound = two(12582912.f), ch = two(c.hi), x = two(fmaxf(xs.x, least), fmaxf(xs.y, least));
+    const Two q = fma(x, ch, two(kGrid));
+    const Two r = fma(x, two(c.lo), fma(x, ch, two(kGrid) - q));
     const float2 qs = split(q);
     const unsigned b0 = __float_as_uint(qs.x), b1 = __float_as_uint(qs.y);
     const float2 p0 = powers[b0 % kPowers], p1 = powers[b1 % kPowers];
-    const Two u = r + (tl - two(p0.y, p1.y));
+    const Two u = r + two(p0.y, p1.y);
     const Two p = u * fma(u, fma(u, two(0.055504109f), two(0.24022651f)), two(0.69314718f));
-    // (kPowers = 2^9: q / kPowers to the exponent's place, where what 1.5 * 2^23 leaves has gone)
-    const Two h = two(__uint_as_float(__float_as_uint(p0.x) + (22u << 23) + ((b0 & ~(kPowers - 1u)) << 14)),
-                      __uint_as_float(__float_as_uint(p1.x) + (22u << 23) + ((b1 & ~(kPowers - 1u)) << 14)));
-    const Two hp = fma(h, p, h);
-    const Two a = hp + kRound;
-    const Two left = (hp - (a - kRound)) + fma(h, p, h - hp);
+    const Two h = two(__uint_as_float(__float_as_uint(p0.x) + ((b0 & ~(kPowers - 1u)) << 13)),
+                      __uint_as_float(__float_as_uint(p1.x) + ((b1 & ~(kPowers - 1u)) << 13)));
+    // (a: a whole number within 1 of h + h p; what h has over it is exact)
+    const Two a = fma(h, p, h + kRound);
+    const Two left = fma(h, p, h - (a - kRound));
     const float2 as = split(a), rs = split(fma(left, two(4194304.f), kRound));
     high[0] = __float_as_uint(as.x), high[1] = __float_as_uint(as.y);
     rest[0] = __float_as_uint(rs.x), rest[1] = __float_as_uint(rs.y);
+  }
+  // The entry of low bits i, from the table of make_powers.
+  __device__ __forceinline__ float2 entry(int i, const float2* of) const {
+    static_assert(kPowers == 1 << 10, "a shift by 23 - 10 takes the other bits to the exponent's place");
+    const float x = m - base, q = fmaf(x, c.hi, kGrid), r = fmaf(x, c.lo, fmaf(x, c.hi, kGrid - q));
+    const unsigned from = static_cast<unsigned>(i) - __float_as_uint(q), k = from % kPowers;
+    return make_float2(__uint_as_float(__float_as_uint(of[k].x) + (22u << 23) + ((from - k) << 13)), -(r + of[k].y));
   }
   __device__ __forceinline__ static unsigned long long join(unsigned high, unsigned rest) {
     return static_cast<unsigned long long>(high - kBits) * 4194304ull + static_cast<long long>(static_cast<int>(rest - kBits));
@@ -148,11 +165,12 @@ struct Weigher {
   __device__ __forceinline__ float low() const { return m - 46.f / c.hi * 1.0001f; }
 };
 __device__ __noinline__ unsigned long long mass_of(float x, float m, float c_hi, float c_lo, const float2* powers) {
-  Weigher w = {m, Slope(1.f), powers};
-  w.c.hi = c_hi, w.c.lo = c_lo;
+  Slope c(1.f);
+  c.hi = c_hi, c.lo = c_lo;
+  const Weigher w(m, c, powers);
   unsigned high[2], rest[2];
   w.halves(x, x, high, rest);
-  return x >= w.low() ? Weigher::join(high[0], rest[0]) : 0;
+  return Weigher::join(high[0], rest[0]);
 }
 // A thread's sum of masses: at most 64 halves of at most 2^22 each.
 struct MassSum {
@@ -160,6 +178,15 @@ struct MassSum {
   __device__ __forceinline__ void add(unsigned h, unsigned r) {
     high += h - Weigher::kBits;
     rest += r - Weigher::kBits;
+  }
+  // All of a pair; `of` says how many pairs there were.
+  __device__ __forceinline__ void add(const unsigned (&h)[2], const unsigned (&r)[2]) {
+    high += h[0] + h[1];
+    rest += r[0] + r[1];
+  }
+  __device__ __forceinline__ void of(int pairs) {
+    high -= 2 * pairs * Weigher::kBits;
+    rest -= 2 * pairs * Weigher::kBits;
   }
   __device__ __forceinline__ unsigned long long value() const {
     return high * 4194304ull + static_cast<long long>(static_cast<int>(rest));
@@ -186,10 +213,12 @@ __device__ __forceinline__ unsigned long long warp_scan_u64(unsigned long long v
 struct Cuts {
   unsigned digit[3][kBins];                     // sums of the bins, by digits of 15 bits: no sum passes 32 bits,
                                                 // and the atomics return nothing
-  unsigned long long key[kList], mass[kList];   // the tokens of a bin
+  unsigned long long key[kList];                // the tokens of a bin, and their masses in the higher digits' place
   unsigned long long box[kList];                // as the CTAs send them, kList / n_ctas of each
   float2 powers[kPowers];
+  __device__ __forceinline__ unsigned long long* mass() { return reinterpret_cast<unsigned long long*>(digit[1]); }
 };
+static_assert(2 * kBins * sizeof(unsigned) >= kList * sizeof(unsigned long long), "masses over the digits");
 
 // What the CTAs of a cluster send each other, by rank, and what counts it.
 struct Boxes {
@@ -215,7 +244,7 @@ struct Small {
 // One row (its slice in this CTA) and what is known of it.
 struct RowState {
   const float* x;       // the slice, tokens first .. first + n - 1
-  int first, n;         // (n: up to a multiple of 4, with -inf behind the last token)
+  int first, n;         // (n: up to a multiple of kRow, with -inf behind the last token)
   int rank, n_ctas;
   float m;              // the row's maximum
   uint32_t top;         // ord(m)
@@ -237,6 +266,14 @@ struct RowState {
     const float t = __fmul_rn(__fsub_rn(m, v), scale);
     const float wide = fmaf(t, 0.25f, 0.75f * kWide * kSteps);
     return __float_as_int(__fadd_rn(fminf(fminf(t, wide), static_cast<float>(kBins * kSteps - 1)), 12582912.f)) & 0x1fffff;
+  }
+  // The same of two that are not below the last bins' end (of others: any number).
+  __device__ __forceinline__ void steps(float v0, float v1, float scale, int (&to)[2]) const {
+    const float2 t = split((two(m) - two(v0, v1)) * two(scale));
+    const float2 wide = split(fma(two(t.x, t.y), two(0.25f), two(0.75f * kWide * kSteps)));
+    const float2 at = split(two(fminf(t.x, wide.x), fminf(t.y, wide.y)) + two(12582912.f));
+    to[0] = __float_as_int(at.x) - 0x4b400000;
+    to[1] = __float_as_int(at.y) - 0x4b400000;
   }
   // (what lies before it, in bins of the first kind)
   static __device__ __forceinline__ float from(float bin) { return bin < kWide ? bin : kWide + 4.f * (bin - kWide); }
@@ -310,7 +347,7 @@ __device__ __noinline__ int find_bin(unsigned long long before, unsigned long lo
   return s.found;
 }
 
-// Of the n tokens in h.key (with h.mass): the last kept one, where `before` is the sum before
+// Of the n tokens in h.key (with h.mass()): the last kept one, where `before` is the sum before
 // them all.  By every CTA for itself.
 template <bool MASS>
 __device__ unsigned long long last_of_list(int n, unsigned long long before, unsigned long long target, int rank,
@@ -323,7 +360,7 @@ __device__ unsigned long long last_of_list(int n, unsigned long long before, uns
     for (int j = 0; j < kListPer; ++j) {
       const int i = tid + j * kThreads;
       key[j] = i < n ? h.key[i] : ~0ull;
-      m[j] = i < n && MASS ? h.mass[i] : 1;
+      m[j] = i < n && MASS ? h.mass()[i] : 1;
       if (i < n) least = min(least, key[j]), most = max(most, key[j]);
     }
 #pragma unroll
@@ -333,6 +370,7 @@ __device__ unsigned long long last_of_list(int n, unsigned long long before, uns
     }
     if (lane == 0) s.least[warp] = least, s.most[warp] = most;
     if (tid == 0) s.n_kept = 0;
+    __syncthreads();   // (the masses lie in the bins' place)
     clear_bins(h);
     for (int w = 0; w < kWarps; ++w) least = min(least, s.least[w]), most = max(most, s.most[w]);
     const int bits = 64 - __clzll(most - least), shift = bits > kBinBits ? bits - kBinBits : 0;
@@ -346,7 +384,7 @@ __device__ unsigned long long last_of_list(int n, unsigned long long before, uns
       if (key[j] == ~0ull || static_cast<int>((key[j] - least) >> shift) != bin) continue;
       const int at = atomicAdd(&s.n_kept, 1);
       h.key[at] = key[j];
-      if (MASS) h.mass[at] = m[j];
+      if (MASS) h.mass()[at] = m[j];
     }
     __syncthreads();
     n = s.n_kept;
@@ -354,10 +392,10 @@ __device__ unsigned long long last_of_list(int n, unsigned long long before, uns
   }
   {
     const int i = tid >> 2;
-    const unsigned long long p = i < n ? h.key[i] : 0, v = i < n && MASS ? h.mass[i] : 1;
+    const unsigned long long p = i < n ? h.key[i] : 0, v = i < n && MASS ? h.mass()[i] : 1;
     unsigned long long sum = 0;
     for (int j = tid & 3; j < n; j += 4)
-      if (h.key[j] < p) sum += MASS ? h.mass[j] : 1;
+      if (h.key[j] < p) sum += MASS ? h.mass()[j] : 1;
     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
     sum += __shfl_xor_sync(0xffffffffu, sum, 2) + before;
     if ((tid & 3) == 0 && i < n && sum < target && sum + v >= target) s.cut = p, s.kept = sum + v;
@@ -427,33 +465,37 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
   const bool all_of_them = upto.x == -INFINITY;
   Boxes& box = s.box;
   if (tid == 0) expect(&box.bar[1], n_ctas * 32 * 8, n_ctas);
-  for (int i = tid; i < 2 * kBins; i += kThreads) (&h.digit[0][0])[i] = 0;
+  for (int i = tid; i < kBins; i += kThreads) h.digit[0][i] = 0;
   __syncthreads();
   int some = 0;
   if (!MASS && by_maxima) {
     some = mine >= low && mine > -INFINITY;
     if (some) atomicAdd(&h.digit[0][row.bin(mine, scale)], 1u);
   }
-  for (int g0 = !MASS && by_maxima ? n4 : warp * 32; g0 < n4; g0 += kThreads) {
-    const int g = g0 + lane;
-    float4 q = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-    if (g < n4) q = x4[g];
-    const float v[4] = {q.x, q.y, q.z, q.w};
-    bool in[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) in[e] = v[e] >= low && (MASS || v[e] > -INFINITY);   // (MASS: low is a number)
+  for (int g = !MASS && by_maxima ? n4 : tid; g < n4; g += kThreads) {
+    const float4 q = x4[g];
+    float v[4] = {q.x, q.y, q.z, q.w};
     if (MASS && !all_of_them) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) in[e] = in[e] && upto.has(v[e], 4 * g + e);
+      for (int e = 0; e < 4; ++e)
+        if (!upto.has(v[e], 4 * g + e)) v[e] = -INFINITY;
     }
-    if (!__any_sync(0xffffffffu, in[0] || in[1] || in[2] || in[3])) continue;
+    const float top = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+    if (!__any_sync(0xffffffffu, top >= low && top > -INFINITY)) continue;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (!MASS) some += in[e];
-      const int step = row.step(v[e], scale);
-      if (in[e] && step < (kBins - 1) * kSteps) {
-        atomicAdd(&h.digit[0][step / kSteps], 1u);
-        if (MASS) atomicAdd(&h.digit[1][step / kSteps], static_cast<unsigned>(step % kSteps));
+    for (int e = 0; e < 4; e += 2) {
+      int step[2];
+      if (MASS)
+        row.steps(v[e], v[e + 1], scale, step);   // (low is near the bins' end)
+      else
+        step[0] = row.step(v[e], scale), step[1] = row.step(v[e + 1], scale);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const bool in = v[e + k] >= low && (MASS || v[e + k] > -INFINITY);   // (MASS: low is a number)
+        if (!MASS) some += in;
+        const int bin = step[k] / kSteps;
+        if (in && step[k] < (kBins - 1) * kSteps)
+          atomicAdd(&h.digit[0][bin], MASS ? (bin < kWide ? kTop : kTopWide) - static_cast<unsigned>(step[k] % kSteps) : 1u);
       }
     }
   }
@@ -462,15 +504,13 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     if (lane == 0) s.some[warp] = some;
   }
   __syncthreads();
-  // The groups' sums to all.  w falls by 2^(1 / kBinsPerOctave) over a bin, nearly linearly; what is not
-  // linear is taken as if the bin's tokens lay evenly in it.
+  // The groups' sums to all.  Of masses: a bin's tokens have been added up as what w is at their places, in units
+  // of its fall over a step, by the tangent at the bin's middle.
   auto bin_value = [&](int b) {
-    const float count = static_cast<float>(h.digit[0][b]);
-    if (!MASS) return count;
-    const float width = 0.69314718f / kBinsPerOctave * (b < kWide ? 1.f : 4.f);
-    const float steps = fmaf(static_cast<float>(h.digit[1][b]), 1.f / kSteps, -0.5f * count);
-    return exp2f(0.5f * (row.from(b) + row.from(b + 1)) * (-1.f / kBinsPerOctave)) *
-           fmaf(steps, -width, count * fmaf(width, width * (1.f / 24.f), 1.f));
+    const float sum = static_cast<float>(h.digit[0][b]);
+    if (!MASS) return sum;
+    return exp2f(0.5f * (row.from(b) + row.from(b + 1)) * (-1.f / kBinsPerOctave)) * sum *
+           (b < kWide ? kFall / kSteps : 4.f * kFall / kSteps);
   };
 #pragma unroll
   for (int j = 0; j < 32 / kWarps; ++j) {
@@ -533,50 +573,48 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
       s.n_list = 0;
     }
     __syncthreads();
-    // (two tokens a turn: more are no faster, and the code is read for the first time)
-    const float2* x2 = reinterpret_cast<const float2*>(row.x);
     MassSum ahead, within, all;
+    int pairs = 0;
 #pragma unroll 1
-    for (int g0 = warp * 32; g0 < 2 * n4; g0 += kThreads) {
-      const int g = g0 + lane;
-      const float2 q = g < 2 * n4 ? x2[g] : make_float2(-INFINITY, -INFINITY);
-      float v[2] = {q.x, q.y};
+    for (int g = tid; g < n4; g += kThreads) {
+      const float4 q = x4[g];
+      float v[4] = {q.x, q.y, q.z, q.w};
       if (MASS && !all_of_them) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-          if (!upto.has(v[e], 2 * g + e)) v[e] = -INFINITY;
+        for (int e = 0; e < 4; ++e)
+          if (!upto.has(v[e], 4 * g + e)) v[e] = -INFINITY;
       }
-      // (a token of the part is not below `low`, but all are where low is -inf)
-      bool past[2], near[2];
+      const float top = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+      const bool some = __any_sync(0xffffffffu, top >= under);
+      if (MASS ? !__any_sync(0xffffffffu, top >= low) : !some) continue;
+      pairs += 2;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        past[e] = v[e] > above && !wide;
-        near[e] = v[e] >= under && v[e] > -INFINITY && !past[e];
-      }
-      if (!__any_sync(0xffffffffu, MASS ? v[0] >= low || v[1] >= low : near[0] || near[1])) continue;
-      unsigned high[2], rest[2];
-      if (MASS) {
-        row.mass.halves(v[0], v[1], high, rest);
+      for (int k = 0; k < 4; k += 2) {
+        unsigned high[2], rest[2];
+        if (MASS) {
+          row.mass.halves(v[k], v[k + 1], high, rest);
+          all.add(high, rest);
+          if (!some) continue;
+        }
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          if (v[e] >= low) all.add(high[e], rest[e]);
-          if (past[e]) ahead.add(high[e], rest[e]);
+          // (a token of the part is not below `low`, but all are where low is -inf)
+          const float x = v[k + e];
+          const bool past = x > above && !wide;
+          if (MASS && past) ahead.add(high[e], rest[e]);
+          if (past || !(x >= under && x > -INFINITY)) continue;
+          const int step = row.step(x, scale);
+          if (MASS && step < lo) ahead.add(high[e], rest[e]);
+          if (step >= hi || (step < lo && !wide)) continue;
+          if (MASS) within.add(high[e], rest[e]);
+          const int to = atomicAdd(&s.n_list, 1);
+          if (to >= cap) continue;
+          const unsigned long long p = row.place(x, 4 * g + k + e);
+          for (int r = 0; r < n_ctas; ++r) send(&h.box[rank * cap + to], p, &box.bar[4], r, n_ctas);
         }
       }
-      if (!__any_sync(0xffffffffu, near[0] || near[1])) continue;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        if (!near[e]) continue;
-        const int step = row.step(v[e], scale);
-        if (MASS && step < lo) ahead.add(high[e], rest[e]);
-        if (step >= hi || (step < lo && !wide)) continue;
-        if (MASS) within.add(high[e], rest[e]);
-        const int to = atomicAdd(&s.n_list, 1);
-        if (to >= cap) continue;
-        const unsigned long long p = row.place(v[e], 2 * g + e);
-        for (int r = 0; r < n_ctas; ++r) send(&h.box[rank * cap + to], p, &box.bar[4], r, n_ctas);
-      }
     }
+    all.of(pairs);
     unsigned long long sum[3] = {ahead.value(), within.value(), all.value()};
     if (MASS) {
 #pragma unroll
@@ -643,7 +681,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     for (int i = warp % per * 32 + lane; i < m; i += per * 32) {
       const unsigned long long p = h.box[from * cap + i];
       h.key[before_them + i] = p;
-      if (MASS) h.mass[before_them + i] = row.mass_at(row.logit(p));
+      if (MASS) h.mass()[before_them + i] = row.mass_at(row.logit(p));
     }
     if (tid == 0) s.n_kept = 0;
     __syncthreads();
@@ -659,7 +697,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
         if (p > cut) continue;
         const int to = atomicAdd(&s.n_kept, 1);
         h.key[to] = p;
-        all += h.mass[to] = row.mass_at(row.logit(p));
+        all += h.mass()[to] = row.mass_at(row.logit(p));
       }
       all = warp_sum_u64(all);
       if (lane == 0) s.part[0][warp] = all;
@@ -725,7 +763,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = n_ctas > 1 ? static_cast<int>(cg::this_cluster().block_rank()) : 0;
   const int r = blockIdx.x / n_ctas;
-  const int first = min(rank * slice, a.vocab), n = min(slice, a.vocab - first), n4 = (n + 3) / 4;
+  const int first = min(rank * slice, a.vocab), n = min(slice, a.vocab - first), n4 = (n + kRow - 1) / kRow * (kRow / 4);
   Boxes& box = s.box;
   if (tid < 6) {
     mbar_init(reinterpret_cast<uint64_t*>(&box.bar[tid]), 1);
@@ -738,10 +776,11 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
   const T* in = static_cast<const T*>(a.x) + r * a.ld + first;
   float* out = a.out + r * a.ld_out + first;
 
-  static_assert(kPowers == kThreads, "one each");
+  static_assert(kPowers == 2 * kThreads, "two each");
   h.powers[tid] = kPowersOf2.of[tid];
+  h.powers[tid + kThreads] = kPowersOf2.of[tid + kThreads];
   float own = -INFINITY, odd = 0.f;   // odd: 0 of finite logits
-  constexpr int kFly = 16;
+  constexpr int kFly = WIDE ? 16 : 32;   // logits of a thread on their way
   constexpr int kTogether = WIDE ? 16 / sizeof(T) : 1;
   if constexpr (WIDE) {
     for (int g0 = 0; g0 * kTogether < n; g0 += kFly / kTogether * kThreads) {
@@ -795,10 +834,11 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
         const int i = i0 + j * kThreads + tid;
         own = fmaxf(own, v[j]);
         if (i < n) odd = fmaf(v[j], 0.f, odd);
-        if (i < 4 * n4) x[i] = v[j];
+        if (i < n) x[i] = v[j];
       }
     }
   }
+  if (n + tid < 4 * n4) x[n + tid] = -INFINITY;
   const Settings set(a, r);
   const bool greedy = set.temperature == 0.f;
   const Slope c(set.temperature);
@@ -862,7 +902,13 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
     for (int i = tid; i < n; i += kThreads) out[i] = top > -INFINITY && first + i == hot ? 1.f : 0.f;
     return;
   }
-  const RowState row = {x, first, 4 * n4, rank, n_ctas, top, ord(top + 0.f), c, a.status, {top, c, h.powers}};
+  const RowState row = {x, first, 4 * n4, rank, n_ctas, top, ord(top + 0.f), c, a.status, Weigher(top, c, h.powers)};
+  {
+    const float2 e0 = row.mass.entry(tid, h.powers), e1 = row.mass.entry(tid + kThreads, h.powers);
+    __syncthreads();
+    h.powers[tid] = e0;
+    h.powers[tid + kThreads] = e1;   // (read behind the next barrier)
+  }
   Upto upto = {-INFINITY, 0x7fffffff};
   unsigned long long kept = 0;
   int turn[3] = {0, 0, 0};
@@ -892,17 +938,12 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
     inv = 1.f / (__ull2float_rn(kept) * 0x1p-44f);
   } else {
     float sum = 0.f;
-    for (int g0 = warp * 32; g0 < n4; g0 += kThreads) {
-      const int g = g0 + lane;
-      float4 q = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-      if (g < n4) q = x4[g];
+    for (int g = tid; g < n4; g += kThreads) {
+      const float4 q = x4[g];
       const float v[4] = {q.x, q.y, q.z, q.w};
-      bool in[4];
+      if (!__any_sync(0xffffffffu, fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= upto.x)) continue;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) in[e] = upto.has(v[e], 4 * g + e);
-      if (!__any_sync(0xffffffffu, in[0] || in[1] || in[2] || in[3])) continue;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum += in[e] ? weight(v[e], top, c) : 0.f;
+      for (int e = 0; e < 4; ++e) sum += upto.has(v[e], 4 * g + e) ? weight(v[e], top, c) : 0.f;
     }
     sum = warp_sum(sum);
     if (lane == 0) s.red[warp] = sum;
@@ -917,16 +958,31 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
     inv = 1.f / sum;
   }
   auto prob = [&](float v, int i) { return upto.has(v, i) ? weight(v, top, c) * inv : 0.f; };
+  // (most tokens are cut off, mostly whole warps of them)
   if (WIDE) {
     for (int g = tid; g < n4; g += kThreads) {
       const float4 q = x4[g];
       const int i = 4 * g;
-      *reinterpret_cast<float4*>(out + i) =
-          make_float4(prob(q.x, i), prob(q.y, i + 1), prob(q.z, i + 2), prob(q.w, i + 3));
+      float4 p = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (__any_sync(0xffffffffu, fmaxf(fmaxf(q.x, q.y), fmaxf(q.z, q.w)) >= upto.x))
+        p = make_float4(prob(q.x, i), prob(q.y, i + 1), prob(q.z, i + 2), prob(q.w, i + 3));
+      if (i < n) *reinterpret_cast<float4*>(out + i) = p;
     }
   } else {
-#pragma unroll 4
-    for (int i = tid; i < n; i += kThreads) out[i] = prob(x[i], i);
+    for (int i0 = tid; i0 < 4 * n4; i0 += 4 * kThreads) {
+      float v[4], m = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[j] = i0 + j * kThreads < 4 * n4 ? x[i0 + j * kThreads] : -INFINITY;
+        m = fmaxf(m, v[j]);
+      }
+      const bool some = __any_sync(0xffffffffu, m >= upto.x);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = i0 + j * kThreads;
+        if (i < n) out[i] = some ? prob(v[j], i) : 0.f;
+      }
+    }
   }
 }
 
@@ -940,12 +996,12 @@ cudaError_t launch_cut(const TokenProbsArgs& a, cudaStream_t s) {
   static PerDevice per_device;
   per_device.once([&] {
     cudaFuncSetAttribute(token_probs_cut_kernel<T, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                         kMaxVocab / kMaxCtas * static_cast<int>(sizeof(float)) + static_cast<int>(sizeof(Cuts)));
+                         (kMaxVocab / kMaxCtas + kRow) * static_cast<int>(sizeof(float)) + static_cast<int>(sizeof(Cuts)));
   });
   int ctas = 1;
   while (ctas < kMaxCtas && (ctas * kSlice < a.vocab || (static_cast<int64_t>(a.n_rows) * ctas < 152 && a.vocab / ctas > 4096)))
     ctas *= 2;
-  return launch_rows(token_probs_cut_kernel<T, WIDE>, a, ctas, kThreads, sizeof(Cuts), sizeof(float), s);
+  return launch_rows(token_probs_cut_kernel<T, WIDE>, a, ctas, kThreads, sizeof(Cuts) + kRow * sizeof(float), sizeof(float), s);
 }
 template <typename T>
 cudaError_t launch_cut(const TokenProbsArgs& a, cudaStream_t s) {
