@@ -519,10 +519,9 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     if (lane == 0) s.group[g] = v;
   }
   __syncthreads();
-  if (warp == 0) {
+  if (warp < n_ctas) {   // (a warp for each)
     const int here = MASS ? 0 : __reduce_add_sync(0xffffffffu, lane < kWarps ? s.some[lane] : 0);
-    const unsigned long long v = bits_of(s.group[lane], static_cast<float>(here));
-    for (int r = 0; r < n_ctas; ++r) send(&box.group[rank][lane], v, &box.bar[1], r, n_ctas);
+    send(&box.group[rank][lane], bits_of(s.group[lane], static_cast<float>(here)), &box.bar[1], warp, n_ctas);
   }
   if (!arrived(&box.bar[1], turn[0]++, n_ctas, row.status)) return upto;
   float v = 0.f, tokens = 0.f;
@@ -546,10 +545,8 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
   if (group >= 0) {
     // the bins of the group in which the cut should be, to all
     if (tid == 0) expect(&box.bar[2], n_ctas * 32 * 8, n_ctas);
-    if (warp == 0) {
-      const unsigned long long mine = bits_of(bin_value(32 * group + lane), 0.f);
-      for (int r = 0; r < n_ctas; ++r) send(&box.bin[rank][lane], mine, &box.bar[2], r, n_ctas);
-    }
+    if (warp < n_ctas)
+      send(&box.bin[rank][lane], bits_of(bin_value(32 * group + lane), 0.f), &box.bar[2], warp, n_ctas);
     if (!arrived(&box.bar[2], turn[1]++, n_ctas, row.status)) return upto;
     v = 0.f;
 #pragma unroll
@@ -610,6 +607,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
           const int to = atomicAdd(&s.n_list, 1);
           if (to >= cap) continue;
           const unsigned long long p = row.place(x, 4 * g + k + e);
+#pragma unroll 1
           for (int r = 0; r < n_ctas; ++r) send(&h.box[rank * cap + to], p, &box.bar[4], r, n_ctas);
         }
       }
@@ -845,9 +843,12 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
   // the tokens that the thread has loaded
   auto each = [&](auto f) {
     if (WIDE) {
+#pragma unroll 1
       for (int g = tid; g * kTogether < n; g += kThreads)
+#pragma unroll 1
         for (int i = g * kTogether; i < (g + 1) * kTogether; ++i) f(i);
     } else {
+#pragma unroll 1
       for (int i = tid; i < n; i += kThreads) f(i);
     }
   };
