@@ -73,14 +73,14 @@ __global__ void __launch_bounds__(THREADS, CTAS_AN_SM)
   const bool greedy = set.temperature == 0.f;
   const Slope c(set.temperature);
   bool bad = set.bad;
-  float m = -INFINITY, odd = 0.f;   // odd: 0 of finite logits
+  float m = -INFINITY;
+  bool odd = false;   // NaN or +inf among them
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     m = fmaxf(m, v[j]);
-    odd = fmaf(v[j], 0.f, odd);
+    odd |= !(v[j] < INFINITY);
   }
-  if (__any_sync(0xffffffffu, odd != 0.f)) {
-    // (masked tokens, too, and what is behind the row's end)
+  if (__any_sync(0xffffffffu, odd)) {
     m = -INFINITY;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {

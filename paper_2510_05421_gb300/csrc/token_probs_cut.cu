@@ -751,7 +751,42 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
   return {row.logit(cut), static_cast<int>(cut & ((1u << kIndexBits) - 1)) - row.first};
 }
 
-template <typename T, bool WIDE>
+// How a row's logits and probabilities are taken: one by one, 16 bytes at a time, or so but for the ends of rows that
+// begin anywhere (64 rows of 128001, the 50 likeliest, 33.5 us, one by one 38.5; 576 of 32000 with top_p as if they
+// began anywhere 106.7, else 104.2).
+enum How { kSingle, kWhole, kRagged };
+
+// Ragged: a slice begins at the 16 bytes that its first logit lies in, `skip` logits earlier, where the probabilities'
+// 16 bytes begin, too.
+template <typename T>
+bool rows_alike(const TokenProbsArgs& a) {
+  return (reinterpret_cast<uintptr_t>(a.x) / sizeof(T) - reinterpret_cast<uintptr_t>(a.out) / 4) % 4 == 0 &&
+         (a.n_rows == 1 || (a.ld - a.ld_out) % 4 == 0);
+}
+// The logits from i on that are within [from, to), -inf for others.
+template <How HOW, typename T>
+__device__ __forceinline__ void load_within(const T* p, int i, int from, int to, float* v) {
+  constexpr int K = 16 / sizeof(T);
+  if (HOW == kWhole ? i < to : i >= from && i + K <= to) {
+    load16(p + i, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < K; ++e) v[e] = HOW == kRagged && i + e >= from && i + e < to ? DT<T>::ld(p + i + e) : -INFINITY;
+  }
+}
+template <How HOW>
+__device__ __forceinline__ void store_within(float* p, int i, int from, int to, float4 v) {
+  if (HOW == kWhole ? i < to : i >= from && i + 4 <= to) {
+    *reinterpret_cast<float4*>(p + i) = v;
+  } else if (HOW == kRagged) {
+    if (i >= from && i < to) p[i] = v.x;
+    if (i + 1 >= from && i + 1 < to) p[i + 1] = v.y;
+    if (i + 2 >= from && i + 2 < to) p[i + 2] = v.z;
+    if (i + 3 >= from && i + 3 < to) p[i + 3] = v.w;
+  }
+}
+
+template <typename T, How HOW>
 __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbsArgs a, int n_ctas, int slice) {
   extern __shared__ __align__(16) unsigned char dynamic[];
   __shared__ Small s;
@@ -761,7 +796,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = n_ctas > 1 ? static_cast<int>(cg::this_cluster().block_rank()) : 0;
   const int r = blockIdx.x / n_ctas;
-  const int first = min(rank * slice, a.vocab), n = min(slice, a.vocab - first), n4 = (n + kRow - 1) / kRow * (kRow / 4);
+  int first = min(rank * slice, a.vocab), n = min(slice, a.vocab - first);
   Boxes& box = s.box;
   if (tid < 6) {
     mbar_init(reinterpret_cast<uint64_t*>(&box.bar[tid]), 1);
@@ -773,11 +808,16 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
   griddep_wait();
   const T* in = static_cast<const T*>(a.x) + r * a.ld + first;
   float* out = a.out + r * a.ld_out + first;
+  constexpr bool WIDE = HOW != kSingle;
+  const int skip = HOW == kRagged && n ? reinterpret_cast<uintptr_t>(in) / sizeof(T) % (16 / sizeof(T)) : 0;
+  in -= skip, out -= skip, first -= skip, n += skip;
+  const int n4 = (n + kRow - 1) / kRow * (kRow / 4);
 
   static_assert(kPowers == 2 * kThreads, "two each");
   h.powers[tid] = kPowersOf2.of[tid];
   h.powers[tid + kThreads] = kPowersOf2.of[tid + kThreads];
-  float own = -INFINITY, odd = 0.f;   // odd: 0 of finite logits
+  float own = -INFINITY;
+  bool odd = false;   // NaN or +inf among them
   constexpr int kFly = WIDE ? 16 : 32;   // logits of a thread on their way
   constexpr int kTogether = WIDE ? 16 / sizeof(T) : 1;
   if constexpr (WIDE) {
@@ -785,13 +825,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
       float v[kFly];
 #pragma unroll
       for (int j = 0; j < kFly; j += kTogether) {
-        const int i = (g0 + j / kTogether * kThreads + tid) * kTogether;
-        if (i < n) {
-          load16(in + i, &v[j]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < kTogether; ++e) v[j + e] = -INFINITY;
-        }
+        load_within<HOW>(in, (g0 + j / kTogether * kThreads + tid) * kTogether, skip, n, &v[j]);
       }
 #pragma unroll
       for (int j = 0; j < kFly; j += kTogether) {
@@ -800,7 +834,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
 #pragma unroll
         for (int e = 0; e < kTogether; ++e) {
           own = fmaxf(own, v[j + e]);
-          odd = fmaf(v[j + e], 0.f, odd);
+          odd |= !(v[j + e] < INFINITY);
         }
 #pragma unroll
         for (int e = 0; e < kTogether; e += 4)
@@ -816,7 +850,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
 #pragma unroll
       for (int j = 0; j < kFly; ++j) {
         own = fmaxf(own, v[j]);
-        odd = fmaf(v[j], 0.f, odd);
+        odd |= !(v[j] < INFINITY);
         x[i0 + j * kThreads + tid] = v[j];
       }
     }
@@ -831,12 +865,12 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
       for (int j = 0; j < kFly; ++j) {
         const int i = i0 + j * kThreads + tid;
         own = fmaxf(own, v[j]);
-        if (i < n) odd = fmaf(v[j], 0.f, odd);
+        odd |= !(v[j] < INFINITY);
         if (i < n) x[i] = v[j];
       }
     }
   }
-  if (n + tid < 4 * n4) x[n + tid] = -INFINITY;
+  if (const int i = (n + kTogether - 1) / kTogether * kTogether + tid; i < 4 * n4) x[i] = -INFINITY;
   const Settings set(a, r);
   const bool greedy = set.temperature == 0.f;
   const Slope c(set.temperature);
@@ -853,8 +887,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
     }
   };
   bool bad = set.bad;
-  if (__syncthreads_or(odd != 0.f)) {
-    // (masked tokens, too, and the -inf behind a row's end)
+  if (__syncthreads_or(odd)) {
     own = -INFINITY;
     each([&](int i) {
       bad |= !(x[i] < INFINITY);
@@ -900,7 +933,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
   const float top = from_ord(__reduce_max_sync(0xffffffffu, ord(of_cta.x)));
   if (greedy || top == -INFINITY) {
     const int hot = __reduce_min_sync(0xffffffffu, of_cta.x == top ? first_of.x : 0x7fffffff);
-    for (int i = tid; i < n; i += kThreads) out[i] = top > -INFINITY && first + i == hot ? 1.f : 0.f;
+    for (int i = skip + tid; i < n; i += kThreads) out[i] = top > -INFINITY && first + i == hot ? 1.f : 0.f;
     return;
   }
   const RowState row = {x, first, 4 * n4, rank, n_ctas, top, ord(top + 0.f), c, a.status, Weigher(top, c, h.powers)};
@@ -967,7 +1000,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
       float4 p = make_float4(0.f, 0.f, 0.f, 0.f);
       if (__any_sync(0xffffffffu, fmaxf(fmaxf(q.x, q.y), fmaxf(q.z, q.w)) >= upto.x))
         p = make_float4(prob(q.x, i), prob(q.y, i + 1), prob(q.z, i + 2), prob(q.w, i + 3));
-      if (i < n) *reinterpret_cast<float4*>(out + i) = p;
+      store_within<HOW>(out, i, skip, n, p);
     }
   } else {
     for (int i0 = tid; i0 < 4 * n4; i0 += 4 * kThreads) {
@@ -992,21 +1025,22 @@ constexpr int kSlice = 16384;   // logits of a CTA where its row may have up to 
 // As few CTAs as hold a row in slices, and more while there are fewer than SMs (152) and the slices are
 // worth it: 6 rows of 32000 over 8 CTAs 11.5 us, over 4 13.9, over 2 19.7; 48 rows over 4 14.2, over 2 14.6,
 // over 8 (more than are resident) 22.9.
-template <typename T, bool WIDE>
+template <typename T, How HOW>
 cudaError_t launch_cut(const TokenProbsArgs& a, cudaStream_t s) {
   static PerDevice per_device;
   per_device.once([&] {
-    cudaFuncSetAttribute(token_probs_cut_kernel<T, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                         (kMaxVocab / kMaxCtas + kRow) * static_cast<int>(sizeof(float)) + static_cast<int>(sizeof(Cuts)));
+    cudaFuncSetAttribute(token_probs_cut_kernel<T, HOW>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                         (kMaxVocab / kMaxCtas + 2 * kRow) * static_cast<int>(sizeof(float)) + static_cast<int>(sizeof(Cuts)));
   });
   int ctas = 1;
   while (ctas < kMaxCtas && (ctas * kSlice < a.vocab || (static_cast<int64_t>(a.n_rows) * ctas < 152 && a.vocab / ctas > 4096)))
     ctas *= 2;
-  return launch_rows(token_probs_cut_kernel<T, WIDE>, a, ctas, kThreads, sizeof(Cuts) + kRow * sizeof(float), sizeof(float), s);
+  return launch_rows(token_probs_cut_kernel<T, HOW>, a, ctas, kThreads, sizeof(Cuts) + 2 * kRow * sizeof(float), sizeof(float), s);
 }
 template <typename T>
 cudaError_t launch_cut(const TokenProbsArgs& a, cudaStream_t s) {
-  return rows_aligned<T>(a) ? launch_cut<T, true>(a, s) : launch_cut<T, false>(a, s);
+  if (rows_aligned<T>(a)) return launch_cut<T, kWhole>(a, s);
+  return rows_alike<T>(a) ? launch_cut<T, kRagged>(a, s) : launch_cut<T, kSingle>(a, s);
 }
 
 }  // namespace

@@ -307,3 +307,38 @@ def test_rows_beside_each_other_and_over_each_other():
         for out in (buf[:, 5:V + 5], buf[:, :V], buf[:, V + 3:2 * V + 3]):
             with pytest.raises(DVIError):
                 token_probs(buf[:, 4:V + 4], out=out, **cuts)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [1, 6, 1019, 4097, 16381, 65531, 131069, 262137, 262144])
+@pytest.mark.parametrize("shift,out_shift", [(0, 0), (1, 1), (3, 7), (6, 2), (5, 0), (7, 3)])
+def test_rows_that_begin_anywhere(V, shift, out_shift, dtype):
+    """Between numbers that would show if they were read, and that show if they are written; rows of odd lengths one after
+    another, so that each begins elsewhere in its 16 bytes."""
+    n = 3
+    buf = torch.full((n * V + 16,), float("nan"), dtype=dtype, device="cuda")
+    x = buf[shift:shift + n * V].view(n, V)
+    x.copy_(logits(n, V, 25).to(dtype))
+    for kw in (dict(), dict(T=0.0), dict(k=60), dict(p=0.9)):
+        room = torch.full((n * V + 16,), -7.0, device="cuda")
+        check(x, out=room[out_shift:out_shift + n * V].view(n, V), **kw)
+        assert bool((room[:out_shift] == -7).all()) and bool((room[out_shift + n * V:] == -7).all())
+
+
+@pytest.mark.parametrize("V", [1021, 50257, 100003])
+@pytest.mark.parametrize("kw", [dict(), dict(top_p=0.9), dict(top_k=30), dict(temperature=0.0)])
+def test_odd_rows_in_place(V, kw):
+    from paper_2510_05421_gb300 import token_probs
+    x = logits(5, V, 26).cuda()
+    want = token_probs(x, **kw)
+    assert token_probs(x, out=x, **kw) is x
+    assert torch.equal(x, want)
+
+
+@pytest.mark.parametrize("kw", [dict(T=0.7), dict(T=0.7, p=0.9), dict(T=0.7, k=40, p=0.8), dict(T=1e-4, p=0.5),
+                                dict(T=30.0, p=0.999), dict(T=1e-5, k=3, p=0.9)])
+@pytest.mark.parametrize("shift", [0.0, 40.0, -500.0, 3e4, -3e4])
+def test_logits_far_from_zero(shift, kw):
+    """Rows that lie far up or down: their distance from the largest counts, not where it is."""
+    x = logits(3, 20000, 27) + shift
+    check(x.cuda(), **kw)
