@@ -183,7 +183,8 @@ cudaError_t launch_probs_plain(const TokenProbsArgs& a, int dtype, cudaStream_t 
 
 cudaError_t launch_token_probs(const TokenProbsArgs& a, int dtype, cudaStream_t s) {
   const bool cuts = a.top_k || a.top_p || a.top_p_all < 1.f || (a.top_k_all > 0 && a.top_k_all < a.vocab);
-  return cuts ? launch_probs_cut(a, dtype, s) : launch_probs_plain(a, dtype, s);
+  if (!cuts) return launch_probs_plain(a, dtype, s);
+  return a.vocab <= kShortRow ? launch_probs_short(a, dtype, s) : launch_probs_cut(a, dtype, s);
 }
 
 }  // namespace dvi

@@ -13,6 +13,8 @@ constexpr int kProbsCtas = 8;   // most CTAs of a row
 
 cudaError_t launch_probs_plain(const TokenProbsArgs& a, int dtype, cudaStream_t s);
 cudaError_t launch_probs_cut(const TokenProbsArgs& a, int dtype, cudaStream_t s);
+constexpr int kShortRow = 2048;   // most logits of a row for:
+cudaError_t launch_probs_short(const TokenProbsArgs& a, int dtype, cudaStream_t s);
 
 // log2(e) / T as an f32 pair, T within 2^-100 .. 2^100: the quotient's rest is exact by a fused
 // multiply-add.

@@ -342,3 +342,27 @@ def test_logits_far_from_zero(shift, kw):
     """Rows that lie far up or down: their distance from the largest counts, not where it is."""
     x = logits(3, 20000, 27) + shift
     check(x.cuda(), **kw)
+
+
+@pytest.mark.parametrize("V", [1, 2, 32, 33, 127, 600, 1024, 1025, 2047, 2048, 2049])
+@pytest.mark.parametrize("how", ["normal", "ties", "masked", "infinite", "equal", "lump", "apart", "near"])
+def test_short_rows(V, how):
+    g = torch.Generator().manual_seed(V)
+    x = logits(6, V, 28)
+    if how == "ties":
+        x = x.bfloat16().float()
+    elif how in ("masked", "infinite"):                         # a few are left, one, none
+        low = -3.0e38 if how == "masked" else -float("inf")
+        x[torch.rand(6, V, generator=g) < 0.95] = low
+        x[4], x[5] = low, low
+        x[4, V // 2] = 1.0
+    elif how == "equal":
+        x[:] = torch.tensor([-7.0, 0.0, 1e-40, 3e38, -3e38, 0.125])[:, None]
+    elif how == "lump":                                         # many equal ones at the top, in the middle, at the end
+        x[:, ::3] = torch.tensor([20.0, 2.0, 0.0, -3.0, -20.0, -1e30])[:, None]
+    elif how == "apart":                                        # by orders of magnitude, on both sides of 0
+        x = torch.exp(60 * (torch.rand(6, V, generator=g) - 0.7)) * torch.where(torch.rand(6, V, generator=g) < 0.5, -1, 1)
+    elif how == "near":                                         # neighbours, as far as f32 tells them apart
+        x = 1.0 + torch.randint(0, V, (6, V), generator=g) * 2.0 ** -23
+    for k, p in ((1, 1.0), (31, 1.0), (40, 0.9), (500, 1.0), (0, 0.3717), (0, 0.9137), (1000, 0.5113), (V - 1, 0.0)):
+        check(x.cuda(), 0.9, k, p)
