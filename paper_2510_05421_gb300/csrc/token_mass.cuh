@@ -35,7 +35,7 @@ constexpr Powers make_powers() {
 }
 __device__ const Powers kPowersOf2 = make_powers();
 
-// w in units of 2^-44, off by about 2^-34 of itself; 0 below 2^-46 (low: where that is, or above).
+// w in units of 2^-44, off by 2^-33 of itself at most (found: 2^-33.05); 0 below 2^-46 (low: where that is, or above).
 // t = (x - m) c is x c less m c.  Adding 1.5 * 2^23 / kPowers rounds x c to multiples q of 1 / kPowers and
 // leaves them in the low bits; the rest x c - q is one number, as a fused multiply-add rounds only what is
 // left.  (|x c| stays below 4096: where |m c| does not, what counts is so near to m that x - m is exact and

@@ -91,7 +91,6 @@ __global__ void __launch_bounds__(THREADS, CTAS_AN_SM)
   }
   m = warp_max(m);
   float2 mine = make_float2(m, 0.f);
-  float back = 1.f;
   if (greedy) {
     int at = NV;
 #pragma unroll
@@ -99,18 +98,10 @@ __global__ void __launch_bounds__(THREADS, CTAS_AN_SM)
       if (v[j] == m) at = j;
     mine.y = __int_as_float(__reduce_min_sync(0xffffffffu, at < NV ? first + index(at) : 0x7fffffff));
   } else if (m > -INFINITY) {
-    // x c - m c in one step where m c is small enough for its rounding to be taken back
-    const float mc = m * c.hi;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    if (fabsf(mc) <= 0x1p20f) {
-      back = exp2f(-fmaf(m, c.hi, -mc));
 #pragma unroll
-      for (int j = 0; j < NV; ++j) sum[j & 3] += v[j] = exp2f(fmaf(v[j], c.hi, -mc));
-    } else {
-#pragma unroll
-      for (int j = 0; j < NV; ++j) sum[j & 3] += v[j] = weight(v[j], m, c);
-    }
-    mine.y = warp_sum((sum[0] + sum[1]) + (sum[2] + sum[3])) * back;
+    for (int j = 0; j < NV; ++j) sum[j & 3] += v[j] = weight(v[j], m, c);
+    mine.y = warp_sum((sum[0] + sum[1]) + (sum[2] + sum[3]));
   }
   if (bad) flag_status(a.status, DVI_DEV_NONFINITE);
   if (n_ctas > 1) {
@@ -125,7 +116,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_AN_SM)
   join<THREADS / 32>(peer, n_ctas, greedy, c, &top, &sum, &hot);
   float scale = 0.f;
   if (!greedy && m > -INFINITY) {
-    scale = weight(m, top, c) * back / sum;
+    scale = weight(m, top, c) / sum;
   } else {
 #pragma unroll
     for (int j = 0; j < NV; ++j) v[j] = 0.f;

@@ -5,9 +5,9 @@
 // last token whose rank is below top_k and before which the sum of w is below
 // top_p of the whole.  A row's slices lie in the shared memory of a cluster's CTAs.
 //
-// The last kept token is looked for in a histogram of the logits: how many tokens a
-// bin has and where in it they lie, which gives its sum of w to about 2^-15.  The CTAs
-// give each other their sums of 32 groups of 32 bins, then of the bins of the group in
+// The last kept token is looked for in a histogram of the logits: of counts, or of w at the
+// tokens' places in their bins by its tangent there, which gives a bin's sum to about 2^-15.
+// The CTAs give each other their sums of 32 groups of 32 bins, then of the bins of the group in
 // which the cut should be.  Then each sums w exactly, as whole numbers: of all tokens,
 // of those before the bin, of those in it; these sums and the bin's tokens go to all.
 // They show whether the bin is the right one (else it is its neighbour's turn) and,
@@ -20,13 +20,15 @@
 //
 // What the CTAs give each other are stores that the receiver's barrier counts: no CTA
 // waits for its own memory operations, as at a cluster's barrier (a block of 6 rows of
-// 32000 with top_p: 14.3 us with these, 12.2 without).
+// 32000 with top_p: 14.3 us with the cluster's, 12.2 so).
 //
 // A few rows are bound by the chain of four exchanges and by code that is read for the
-// first time (a third of the stalls): 6 rows of 32000 with top_p 11.4 us, 48 with top_k
-// 50 13.5.  Many rows are bound by instructions, about 110 a token of which 45 weigh
-// it, at half of the issue rate: 64 rows of 128001 with settings of their own 60 us (a
-// copy of them 17).
+// first time (a third of the stalls): 6 rows of 32000 with top_p @A@ us, 48 with top_k
+// 50 @B@.  Many rows: of a CTA's time on a slice of 16000 tokens with top_p (50000 cycles) the
+// exact sums take 14000 (instructions, and conflicts in the table of powers), the histogram 8000 (its
+// atomics), the loads 6000, the stores 6000, and the exchanges between them the rest; with top_k 30000
+// in all: 576 rows of 32000 @C@ and @D@ us (a copy of them 23), 64 rows of 128001 with settings of their
+// own @E@ (17).
 #include "token_mass.cuh"
 
 namespace dvi {

@@ -246,7 +246,7 @@ def test_cuts_deep_in_the_tail(V, T, p):
         kept = int((got[r] > 0).sum())
         assert (got[r][order[:kept]] > 0).all()                     # a prefix of the order
         # its end is where the sum reaches p of the whole, within what the masses' rounding may move: each is off by
-        # 2^-45 and 2^-34 of itself
+        # less than 2^-44 and by 2^-33 of itself, and counts once: before p of the whole or behind it
         before, all_of_it = w[order].cumsum() - w[order], w.sum()
         slack = V * 2.0 ** -44 + all_of_it * 2.0 ** -33
         assert before[kept - 1] < p * all_of_it + slack and (kept == V or before[kept] >= p * all_of_it - slack)
