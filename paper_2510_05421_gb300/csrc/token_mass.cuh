@@ -85,7 +85,7 @@ struct Weigher {
   __device__ __forceinline__ Weigher(float m, Slope c, const float2* powers)
       : m(m), c(c), powers(powers), base(fabsf(m * c.hi) < 4000.f ? 0.f : m), least((m - base) - 46.f / c.hi * 1.0001f) {}
   __device__ __forceinline__ void halves(float x0, float x1, unsigned (&high)[2], unsigned (&rest)[2]) const {
-    halves_by([&](unsigned i) { return powers[i]; }, x0, x1, high, rest);
+    halves_by([of = powers](unsigned i) { return of[i]; }, x0, x1, high, rest);
   }
   template <typename F>
   __device__ __forceinline__ void halves_by(F power, float x0, float x1, unsigned (&high)[2], unsigned (&rest)[2]) const {

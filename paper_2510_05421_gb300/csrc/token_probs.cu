@@ -3,8 +3,8 @@
 // The CTAs of a cluster hold a row between them in registers, so it is read once, and
 // every warp gives (its maximum, its sum of exp2) to all of them once.
 //
-// Bound by memory and that exchange: 576 rows of 32000 f32 logits (147 MB) take 32 us
-// (4.6 TB/s; 4096 rows 5.3), of which the exchange is 5.5, a copy of them 23 us.  32
+// Bound by memory and that exchange: 576 rows of 32000 f32 logits (147 MB) take 29 us
+// (5.0 TB/s), of which the exchange is 5.5, a copy of them 23 us.  32
 // logits a thread and four CTAs of 256 threads an SM: 16 a thread 34 us, 64 a thread 37,
 // clusters that take row after row with the next one's loads under way 32, a row a CTA
 // with the next one's bulk copy under way 35.

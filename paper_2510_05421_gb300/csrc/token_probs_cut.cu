@@ -14,21 +14,21 @@
 // among its tokens, which is the last.  Every CTA comes to the same end, whatever the
 // order of its atomics.  Where top_k leaves few tokens, all of these go to all instead,
 // which is all that top_p needs, too.  Where the bin has too many tokens, a part of it is
-// tried, where the cut would be if they lay evenly (a row of 128001 with top_p 26 us, such a
-// row 38, and 102 by what follows); where that has too many, too (logits that are equal),
-// the token's place in the order, as a number, is found 10 bits at a time.
+// tried, where the cut would be if they lay evenly; where that has too many, too, the token's
+// place in the order, as a number, is found 10 bits at a time (a row of 128001 with top_p 21 us;
+// of equal logits, or of logits within 0.001, 160).
 //
 // What the CTAs give each other are stores that the receiver's barrier counts: no CTA
 // waits for its own memory operations, as at a cluster's barrier (a block of 6 rows of
 // 32000 with top_p: 14.3 us with the cluster's, 12.2 so).
 //
 // A few rows are bound by the chain of four exchanges and by code that is read for the
-// first time (a third of the stalls): 6 rows of 32000 with top_p @A@ us, 48 with top_k
-// 50 @B@.  Many rows: of a CTA's time on a slice of 16000 tokens with top_p (50000 cycles) the
+// first time (a third of the stalls): 6 rows of 32000 with top_p 10.9 us, 48 with top_k
+// 50 12.2.  Many rows: of a CTA's time on a slice of 16000 tokens with top_p (50000 cycles) the
 // exact sums take 14000 (instructions, and conflicts in the table of powers), the histogram 8000 (its
 // atomics), the loads 6000, the stores 6000, and the exchanges between them the rest; with top_k 30000
-// in all: 576 rows of 32000 @C@ and @D@ us (a copy of them 23), 64 rows of 128001 with settings of their
-// own @E@ (17).
+// in all: 576 rows of 32000 105 and 63 us (a copy of them 23), 64 rows of 128001 with settings of their
+// own 57 to 66 (17).
 #include "token_mass.cuh"
 
 namespace dvi {
@@ -889,8 +889,8 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
 constexpr int kSlice = 16384;   // logits of a CTA where its row may have up to kMaxCtas: two CTAs an SM
 
 // As few CTAs as hold a row in slices, and more while there are fewer than SMs (152) and the slices are
-// worth it: 6 rows of 32000 over 8 CTAs 11.5 us, over 4 13.9, over 2 19.7; 48 rows over 4 14.2, over 2 14.6,
-// over 8 (more than are resident) 22.9.
+// worth it: 6 rows of 32000 with top_p over 8 CTAs 10.9 us, over 4 12.7, over 2 17.1; 48 rows over 4 18.1, over
+// 2 18.8, over 8 (more than are resident) 26.5.
 template <typename T, How HOW>
 cudaError_t launch_cut(const TokenProbsArgs& a, cudaStream_t s) {
   static PerDevice per_device;
