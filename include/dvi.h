@@ -507,7 +507,10 @@ typedef struct {
  * order of any sum.  NaN logits count as -inf and +inf as the largest finite number
  * (DVI_DEV_NONFINITE).  Of settings in device arrays, T that is negative or NaN counts
  * as 0, top_k below 0 as 0, top_p NaN as 1 (NaN: DVI_DEV_NONFINITE).  d_probs may be
- * d_logits itself (f32, the same ld); rows that overlap in another way are refused. */
+ * d_logits itself (f32, the same ld); rows that overlap in another way are refused.
+ *
+ * Long rows with cuts are shared by CTAs that wait for each other's sums.  Where such a wait runs out (a second)
+ * the whole row gets zeros (DVI_DEV_TIMEOUT). */
 dvi_status dvi_token_probs(int dtype, const void* d_logits, int64_t ld_logits, int n_rows, int vocab,
                            const dvi_sampling* sampling, float* d_probs, int64_t ld_probs, int32_t* d_status,
                            dvi_stream stream);

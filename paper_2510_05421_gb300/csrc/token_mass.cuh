@@ -139,6 +139,9 @@ __device__ __forceinline__ unsigned long long share_of(float p, unsigned long lo
 struct Upto {
   float x;
   int i;
+  // (of a row that is lost; an index within a slice is above -kMaxVocab)
+  static __device__ __forceinline__ Upto lost_row() { return {0.f, -0x7fffffff}; }
+  __device__ __forceinline__ bool lost() const { return i == -0x7fffffff; }
   __device__ __forceinline__ bool has(float v, int at) const { return v > x || (v == x && at <= i); }
 };
 

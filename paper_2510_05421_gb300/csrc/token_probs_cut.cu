@@ -126,6 +126,9 @@ struct Small {
   float red[kWarps], low[kWarps];
   int first[kWarps], some[kWarps];
   int n_list, n_kept, found;
+  int vain;                                     // a warp has waited in vain
+  int meetings;                                 // of the cluster, so far
+  int lost;                                     // the one to which a CTA comes that has given up (none: -1)
   unsigned long long excl, cut, kept;
 };
 
@@ -168,23 +171,71 @@ struct RowState {
   __device__ __forceinline__ int bin(float v, float scale) const { return step(v, scale) / kSteps; }
 };
 
-// Eight bytes to the box of CTA r, counted by its barrier.
-__device__ __forceinline__ void send(void* to, unsigned long long v, unsigned long long* bar, int r, int n_ctas) {
+// Eight bytes to the box of CTA r, counted by its k-th barrier.  (DVI_SENDS: whether they are, for a build that holds
+// some back.)
+#ifndef DVI_SENDS
+#define DVI_SENDS(k, r) true
+#endif
+__device__ __forceinline__ void send(void* to, unsigned long long v, Boxes& box, int k, int r, int n_ctas) {
   if (n_ctas == 1) {
     *static_cast<unsigned long long*>(to) = v;
     return;
   }
-  send_to(to, v, bar, r);
+  if (DVI_SENDS(k, r)) send_to(to, v, &box.bar[k], r);
 }
 // One thread says how much will come ...
 __device__ __forceinline__ void expect(unsigned long long* bar, int bytes, int n_ctas) {
   if (n_ctas > 1) mbar_arrive_expect_tx(reinterpret_cast<uint64_t*>(bar), bytes);
 }
-// ... and all wait for it.
+// ... and all wait for it, a warp together.
 __device__ __forceinline__ bool arrived(unsigned long long* bar, int turn, int n_ctas, int* status) {
-  if (n_ctas > 1) return mbar_wait(reinterpret_cast<uint64_t*>(bar), turn & 1, status);
+  if (n_ctas > 1) return __all_sync(0xffffffffu, mbar_wait(reinterpret_cast<uint64_t*>(bar), turn & 1, status));
   __syncthreads();
   return true;
+}
+
+// A wait that runs out (a second: a CTA of the cluster has not sent what it should) costs the row, which gets zeros,
+// in every CTA alike:
+// - The CTA's first barrier behind a wait says whether a warp has waited in vain; one that has sends nothing more and
+//   goes straight to that barrier.  (Between what it says and the next wait lies another barrier, so all see the same.)
+// - If so, the CTA gives up: it leaves the number of the cluster's next meeting (its barrier) with all, and comes to
+//   that meeting, which is its last.
+// - The others find the number when they come there, if not before they have waited in vain themselves: it is
+//   everybody's last.  So nobody leaves, or clears what others read, while a CTA might still send to it or read it,
+//   and what a CTA goes on with has come whole from CTAs that had not given up.
+// - A row that is right ends with a meeting, too, on whose way it is stored.
+// (6 rows of 32000 with top_p 0.25 us of 12.6, half of it the last meeting; 576 with the 50 likeliest 1.3 of 64.7.)
+__device__ __forceinline__ int now(const int& v) { return *static_cast<const volatile int*>(&v); }
+__device__ __forceinline__ bool all_came(const Small& s) {
+  __syncthreads();
+  return now(s.vain) == 0;
+}
+__device__ __forceinline__ void in_vain(Small& s) {
+  s.vain = 1;
+  __syncthreads();
+}
+__device__ __forceinline__ bool meet(Small& s, int n_ctas) {   // (a barrier of the CTA lies between two of them)
+  if (threadIdx.x == 0) ++s.meetings;
+  cluster_barrier(n_ctas);
+  return now(s.lost) != now(s.meetings);
+}
+// The last one, when nothing comes to this CTA or goes from it any more, and its end, when the row is stored.
+__device__ __forceinline__ void arrive_at_last(int n_ctas) {
+  if (n_ctas > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+// Zeros for a row that is lost; what was sent to this CTA before the last meeting (over: it is) has come when it ends.
+__device__ __noinline__ void leave_zeros(float* probs, int64_t ld, int vocab, int n_ctas, int slice, Small& s, bool over) {
+  if (!over && now(s.lost) != now(s.meetings)) {
+    if (threadIdx.x < n_ctas) *cg::this_cluster().map_shared_rank(&s.lost, threadIdx.x) = now(s.meetings) + 1;
+    __syncwarp();
+    cluster_barrier(n_ctas);
+  }
+  __syncthreads();   // (behind what other threads have stored)
+  const int first = static_cast<int>(cg::this_cluster().block_rank()) * slice;
+  float* out = probs + blockIdx.x / n_ctas * ld;
+  for (int i = first + threadIdx.x; i < min(first + slice, vocab); i += kThreads) out[i] = 0.f;
+  for (const uint64_t t0 = global_ns(); global_ns() - t0 < 1000000;) {
+  }
 }
 
 __device__ __forceinline__ void add_to_bin(Cuts& h, int bin, unsigned long long v) {
@@ -314,8 +365,8 @@ __device__ __forceinline__ int first_reaching(float v, float target, float* befo
 // The last kept token among those up to `upto`: before it the counts sum to less than top_k (and then
 // the masses to less than top_p of what top_k leaves: *done; else that is still to do), or (MASS) the
 // masses to less than top_p of all.  Returns the tokens up to it.  *kept: the sum of their masses, where
-// it is known (*done, or MASS).  Tokens below `low` are known to be cut (or, MASS, to be 0).  turn[]: how
-// often the barriers of the groups, of the bins, of the sums and the list have been used.
+// it is known (*done, or MASS).  Tokens below `low` are known to be cut (or, MASS, to be 0).  Where a wait
+// has run out, here or elsewhere: a lost row.
 //
 // by_maxima (counts): the histogram has the largest logit of each thread alone (`mine`), which are at
 // least top_k: the tokens that are not behind the bin in which the top_k-th of these lies are few more than
@@ -332,7 +383,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
   Boxes& box = s.box;
   if (tid == 0) expect(&box.bar[1], n_ctas * 32 * 8, n_ctas);
   for (int i = tid; i < kBins; i += kThreads) h.digit[0][i] = 0;
-  __syncthreads();
+  if (!all_came(s)) return Upto::lost_row();
   int some = 0;
   if (!MASS && by_maxima) {
     some = mine >= low && mine > -INFINITY;
@@ -387,9 +438,13 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
   __syncthreads();
   if (warp < n_ctas) {   // (a warp for each)
     const int here = MASS ? 0 : __reduce_add_sync(0xffffffffu, lane < kWarps ? s.some[lane] : 0);
-    send(&box.group[rank][lane], bits_of(s.group[lane], static_cast<float>(here)), &box.bar[1], warp, n_ctas);
+    send(&box.group[rank][lane], bits_of(s.group[lane], static_cast<float>(here)), box, 1, warp, n_ctas);
   }
-  if (!arrived(&box.bar[1], turn[0]++, n_ctas, row.status)) return upto;
+  if (!arrived(&box.bar[1], turn[0] & 1, n_ctas, row.status)) {
+    in_vain(s);
+    return Upto::lost_row();
+  }
+  ++turn[0];
   float v = 0.f, tokens = 0.f;
 #pragma unroll
   for (int r = 0; r < kMaxCtas; ++r) {
@@ -398,7 +453,8 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     tokens += p.y;
   }
   if (!MASS && tokens < top_k) {              // (fewer tokens than top_k)
-    cluster_barrier(n_ctas);                  // (all have read the sums before the next are sent)
+    // (all have read the sums before the next are sent)
+    if (!all_came(s) || !meet(s, n_ctas)) return Upto::lost_row();
     return upto;
   }
   const float all_bins = warp_sum(v), about = MASS ? top_p * all_bins : static_cast<float>(top_k);
@@ -412,8 +468,12 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     // the bins of the group in which the cut should be, to all
     if (tid == 0) expect(&box.bar[2], n_ctas * 32 * 8, n_ctas);
     if (warp < n_ctas)
-      send(&box.bin[rank][lane], bits_of(bin_value(32 * group + lane), 0.f), &box.bar[2], warp, n_ctas);
-    if (!arrived(&box.bar[2], turn[1]++, n_ctas, row.status)) return upto;
+      send(&box.bin[rank][lane], bits_of(bin_value(32 * group + lane), 0.f), box, 2, warp, n_ctas);
+    if (!arrived(&box.bar[2], turn[1] & 1, n_ctas, row.status)) {
+      in_vain(s);
+      return Upto::lost_row();
+    }
+    ++turn[1];
     v = 0.f;
 #pragma unroll
     for (int r = 0; r < kMaxCtas; ++r) v += r < n_ctas ? box.bin[r][lane].x : 0.f;
@@ -435,7 +495,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
       expect(&box.bar[3], n_ctas * 4 * 8, n_ctas);
       s.n_list = 0;
     }
-    __syncthreads();
+    if (!all_came(s)) return Upto::lost_row();
     MassSum ahead, within, all;
     int pairs = 0;
 #pragma unroll 1
@@ -474,7 +534,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
           if (to >= cap) continue;
           const unsigned long long p = row.place(x, 4 * g + k + e);
 #pragma unroll 1
-          for (int r = 0; r < n_ctas; ++r) send(&h.box[rank * cap + to], p, &box.bar[4], r, n_ctas);
+          for (int r = 0; r < n_ctas; ++r) send(&h.box[rank * cap + to], p, box, 4, r, n_ctas);
         }
       }
     }
@@ -491,9 +551,12 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     if (warp < 4) {
       unsigned long long v = s.n_list;
       if (warp < 3) v = MASS ? warp_sum_u64(lane < kWarps ? s.part[warp][lane] : 0) : 0;
-      if (lane < n_ctas) send(&box.sum[turn[2] & 1][warp][rank], v, &box.bar[3], lane, n_ctas);
+      if (lane < n_ctas) send(&box.sum[turn[2] & 1][warp][rank], v, box, 3, lane, n_ctas);
     }
-    if (!arrived(&box.bar[3], turn[2], n_ctas, row.status)) return upto;
+    if (!arrived(&box.bar[3], turn[2] & 1, n_ctas, row.status)) {
+      in_vain(s);
+      return Upto::lost_row();
+    }
     // (a lane a CTA)
     const int there = lane < n_ctas ? static_cast<int>(box.sum[turn[2] & 1][3][lane]) : 0;
     const int sent = __reduce_add_sync(0xffffffffu, min(there, cap));
@@ -529,16 +592,22 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
         here = false;
       }
     }
-    if (!arrived(&box.bar[4], turn[2]++, n_ctas, row.status)) return upto;
+    if (!arrived(&box.bar[4], turn[2] & 1, n_ctas, row.status)) {
+      in_vain(s);
+      return Upto::lost_row();
+    }
+    ++turn[2];
     if (here) break;
     if (!MASS && by_maxima) return upto;
     n = kList + 1;
-    cluster_barrier(n_ctas);   // (all have what was sent before more is)
+    // (all have what was sent before more is)
+    if (!all_came(s)) return Upto::lost_row();
+    if (!meet(s, n_ctas)) return Upto::lost_row();
   }
   unsigned long long cut;
   if (n <= kList) {
     // the warps share the CTAs' lists
-    const int there = lane < n_ctas ? static_cast<int>(box.sum[(turn[2] - 1) & 1][3][lane]) : 0;
+    const int there = lane < n_ctas ? static_cast<int>(box.sum[(turn[2] & 1) ^ 1][3][lane]) : 0;
     const int per = kWarps / n_ctas, from = warp / per;
     const int before_them = __reduce_add_sync(0xffffffffu, lane < from ? there : 0);
     const int m = __shfl_sync(0xffffffffu, there, from);
@@ -548,7 +617,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
       if (MASS) h.mass()[before_them + i] = row.mass_at(row.logit(p));
     }
     if (tid == 0) s.n_kept = 0;
-    __syncthreads();
+    if (!all_came(s)) return Upto::lost_row();
     cut = last_of_list<MASS>(n, wide ? 0 : before, target, rank, h, s, kept);
     if (wide) {
       // the tokens that are left, and of these the last one of top_p
@@ -577,6 +646,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
     }
   } else {
     cg::cluster_group cluster = cg::this_cluster();
+    if (!all_came(s)) return Upto::lost_row();
     if (MASS) {
       // (the sum of all, where no bin was looked at)
       unsigned long long all = 0;
@@ -585,7 +655,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
       all = warp_sum_u64(all);
       __syncthreads();
       if (lane == 0) s.part[1][warp] = all;
-      cluster_barrier(n_ctas);
+      if (!meet(s, n_ctas)) return Upto::lost_row();
       all = 0;
       for (int r = 0; r < n_ctas; ++r)
         for (int w = 0; w < kWarps; ++w) all += cluster.map_shared_rank(&s, r)->part[1][w];
@@ -602,7 +672,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
         if (p < cut || ((p - cut) >> shift) >= kBins) continue;
         add_to_bin(h, static_cast<int>((p - cut) >> shift), MASS ? row.mass_at(x) : 1ull);
       }
-      cluster_barrier(n_ctas);
+      if (!meet(s, n_ctas)) return Upto::lost_row();
       const int b = find_bin(before, target, 0, n_ctas, h, s, &before);   // (found: the whole reaches target)
       cut += static_cast<unsigned long long>(b) << shift;
       if (shift == 0) {
@@ -610,7 +680,7 @@ __device__ Upto last_kept(const RowState& row, int top_k, float top_p, Upto upto
         *kept = before;
         for (int r = 0; r < n_ctas; ++r) *kept += bin_sum(*cluster.map_shared_rank(&h, r), b);
       }
-      cluster_barrier(n_ctas);   // before the bins are cleared
+      if (!meet(s, n_ctas)) return Upto::lost_row();   // before the bins are cleared
       if (shift == 0) break;
     }
   }
@@ -669,6 +739,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
     mbar_fence_init();
     if (tid == 0) expect(&box.bar[0], n_ctas * 16, n_ctas);
     if (tid == 5) expect(&box.bar[5], n_ctas * 8, n_ctas);
+    if (tid == 0) s.meetings = 0, s.lost = -1, s.vain = 0;
   }
   if (n_ctas > 1) cluster_arrive_release();              // (waited for before anything is sent)
   griddep_wait();
@@ -787,31 +858,40 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
     const int at = __reduce_min_sync(0xffffffffu, is && w == m ? s.first[lane] : 0x7fffffff);
     const int some = __reduce_add_sync(0xffffffffu, is ? s.some[lane] : 0);
     if (lane < n_ctas) {
-      send(&box.top[rank], bits_of(m, low), &box.bar[0], lane, n_ctas);
-      send(&box.first[rank], (static_cast<unsigned long long>(some) << 32) | static_cast<unsigned>(at), &box.bar[0],
+      send(&box.top[rank], bits_of(m, low), box, 0, lane, n_ctas);
+      send(&box.first[rank], (static_cast<unsigned long long>(some) << 32) | static_cast<unsigned>(at), box, 0,
            lane, n_ctas);
     }
   }
-  if (!arrived(&box.bar[0], 0, n_ctas, a.status)) return;
+  int turn[3] = {0, 0, 0};
+  const bool came = arrived(&box.bar[0], 0, n_ctas, a.status);
   const bool is = lane < n_ctas;
   const float2 of_cta = is ? box.top[lane] : make_float2(-INFINITY, 3.402823466e38f);
   const int2 first_of = is ? box.first[lane] : make_int2(0x7fffffff, 0);
   const float top = from_ord(__reduce_max_sync(0xffffffffu, ord(of_cta.x)));
-  if (greedy || top == -INFINITY) {
-    const int hot = __reduce_min_sync(0xffffffffu, of_cta.x == top ? first_of.x : 0x7fffffff);
-    for (int i = skip + tid; i < n; i += kThreads) out[i] = top > -INFINITY && first + i == hot ? 1.f : 0.f;
-    return;
-  }
   const RowState row = {x, first, 4 * n4, rank, n_ctas, top, ord(top + 0.f), c, a.status, Weigher(top, c, h.powers)};
   {
     const float2 e0 = row.mass.entry(tid, h.powers), e1 = row.mass.entry(tid + kThreads, h.powers);
-    __syncthreads();
+    if (!came) s.vain = 1;
+    if (!all_came(s)) return leave_zeros(a.out, a.ld_out, a.vocab, n_ctas, slice, s, false);
     h.powers[tid] = e0;
     h.powers[tid + kThreads] = e1;   // (read behind the next barrier)
   }
+  auto nothing = [&](bool over) { leave_zeros(a.out, a.ld_out, a.vocab, n_ctas, slice, s, over); };
+  auto last_wait = [&] {
+    if (n_ctas == 1) return;
+    cluster_wait_acquire();
+    if (now(s.lost) == s.meetings + 1) nothing(true);
+  };
+  if (greedy || top == -INFINITY) {
+    arrive_at_last(n_ctas);
+    const int hot = __reduce_min_sync(0xffffffffu, of_cta.x == top ? first_of.x : 0x7fffffff);
+    for (int i = skip + tid; i < n; i += kThreads) out[i] = top > -INFINITY && first + i == hot ? 1.f : 0.f;
+    last_wait();
+    return;
+  }
   Upto upto = {-INFINITY, 0x7fffffff};
   unsigned long long kept = 0;
-  int turn[3] = {0, 0, 0};
   bool done = false;
   if (set.top_k) {
     // Bins from the maximum down to the least of the threads' maxima, where there are top_k
@@ -825,6 +905,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
                              enough ? fminf(row.from(kBins - 2) * kSteps / (top - low), 1e30f)
                                     : c.hi * (kSteps * kBinsPerOctave),
                              enough ? low : -INFINITY, turn, h, s, &kept, &done, by_maxima, own, &fits);
+      if (cut.lost()) return nothing(false);
     }
     upto = cut;
   }
@@ -835,6 +916,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
     // (a mass is 0 below 2^-46)
     upto = last_kept<true>(row, 0, set.top_p, upto, c.hi * (kSteps * kBinsPerOctave), row.mass.low(), turn, h, s, &kept,
                            &done);
+    if (upto.lost()) return nothing(false);
     inv = 1.f / (__ull2float_rn(kept) * 0x1p-44f);
   } else {
     float sum = 0.f;
@@ -850,13 +932,15 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
     __syncthreads();
     if (warp == 0) {
       sum = warp_sum(lane < kWarps ? s.red[lane] : 0.f);
-      if (lane < n_ctas) send(&box.kept[rank], bits_of(sum, 0.f), &box.bar[5], lane, n_ctas);
+      if (lane < n_ctas) send(&box.kept[rank], bits_of(sum, 0.f), box, 5, lane, n_ctas);
     }
-    if (!arrived(&box.bar[5], 0, n_ctas, a.status)) return;
+    if (!arrived(&box.bar[5], 0, n_ctas, a.status)) s.vain = 1;
+    if (!all_came(s)) return nothing(false);
     sum = 0.f;
     for (int q = 0; q < n_ctas; ++q) sum += box.kept[q].x;
     inv = 1.f / sum;
   }
+  arrive_at_last(n_ctas);
   auto prob = [&](float v, int i) { return upto.has(v, i) ? weight(v, top, c) * inv : 0.f; };
   // (most tokens are cut off, mostly whole warps of them)
   if (WIDE) {
@@ -884,6 +968,7 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
       }
     }
   }
+  last_wait();
 }
 
 constexpr int kSlice = 16384;   // logits of a CTA where its row may have up to kMaxCtas: two CTAs an SM

@@ -54,7 +54,8 @@ def token_probs(logits: torch.Tensor, temperature: Union[float, torch.Tensor] = 
     largest.  A row of -inf alone gets zeros.
 
     Settings are numbers or tensors with one for each row (f32, int32, f32 [n]).  NaN logits count as -inf, +inf as
-    the largest number; status (int32 [1], or None) gets DVI_DEV_NONFINITE then.  `out` may be the logits (f32); one that
+    the largest number; status (int32 [1], or None) gets DVI_DEV_NONFINITE then, and DVI_DEV_TIMEOUT where a bounded wait
+    of the device ran out, whose row gets zeros.  `out` may be the logits (f32); one that
     overlaps them in another way is refused.  No gradient passes through."""
     index = _device_of("token_probs: logits", logits)
     if stream is not None or _current() != index:
