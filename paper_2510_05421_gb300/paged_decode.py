@@ -26,7 +26,7 @@ from typing import List, Optional, Sequence
 import numpy as np
 import torch
 
-from .dvi import DeviceWeights, linear_noalloc
+from .dvi import DEV_BITS, DeviceWeights, linear_noalloc
 from .paged import PagedCache, rotary_table
 from .pages import PagePool
 from .sampling import token_probs, verify_drafts
@@ -55,20 +55,21 @@ class Sampling:
     def uniform(self, n: int, device) -> torch.Tensor:
         return torch.rand(n, device=device, generator=self.generator)
 
-    def probs(self, logits: torch.Tensor) -> torch.Tensor:
-        return token_probs(logits, self.temperature, self.top_k, self.top_p)
+    def probs(self, logits: torch.Tensor, status: Optional[torch.Tensor] = None) -> torch.Tensor:
+        return token_probs(logits, self.temperature, self.top_k, self.top_p, status=status)
 
-    def draw(self, probs: torch.Tensor) -> torch.Tensor:
+    def draw(self, probs: torch.Tensor, status: Optional[torch.Tensor] = None) -> torch.Tensor:
         """A token of each row (-1 of a row without probabilities)."""
         n = probs.shape[0]
         none = probs.new_empty(0)
-        return verify_drafts(probs, none.to(torch.int32), none, self.uniform(n, probs.device))[0][:, 0]
+        return verify_drafts(probs, none.to(torch.int32), none, self.uniform(n, probs.device), status=status)[0][:, 0]
 
 
 class PagedDecoder:
     """A layer-split decoder whose sequences live in a pool of 8-bit pages."""
 
     pool: Optional[PagePool] = None
+    status_word: Optional[torch.Tensor] = None      # of the sampling calls
 
     def __init__(self, shape, weights: DeviceWeights, *, split_k: int, k_spec: int, max_seqs: int, n_pages: int,
                  max_seq_len: int, lora_gamma: float = 1.0, page_tokens: int = 16, fmt: str = "int8",
@@ -94,6 +95,15 @@ class PagedDecoder:
         else:
             self.table = torch.full((max_seqs, width), -1, dtype=torch.int32, device=device)
         self.lens = torch.zeros(max_seqs, dtype=torch.int32, device=device)
+        self.status_word = torch.zeros(1, dtype=torch.int32, device=device)
+
+    def status(self) -> list:
+        """Names of the DVI_DEV_* flags that the caches, the pool and the sampling calls have set since the last look
+        (waits for the device), then cleared."""
+        names = {f for c in [*self.caches, *([self.pool] if self.pool else [])] for f in c.status()}
+        word = int(self.status_word.item())
+        self.status_word.bitwise_and_(~word)
+        return sorted(names | {name for bit, name in DEV_BITS.items() if word & bit})
 
     # -- pages ------------------------------------------------------------
     def reserve(self, rows: Sequence[int]):
@@ -198,7 +208,7 @@ class PagedDecoder:
         """The greedy token of each row, or a sampled one."""
         if sampling is None:
             return logits.argmax(-1).to(torch.int32)
-        return sampling.draw(sampling.probs(logits))
+        return sampling.draw(sampling.probs(logits, self.status_word), self.status_word)
 
     @staticmethod
     def _some_token(what: str, got: Sequence[int]):
@@ -245,8 +255,8 @@ class PagedDecoder:
             if sampling is None:
                 tok = z.argmax(-1).to(torch.int32)
             else:
-                drawn_from.append(sampling.probs(z))
-                tok = sampling.draw(drawn_from[-1])
+                drawn_from.append(sampling.probs(z, self.status_word))
+                tok = sampling.draw(drawn_from[-1], self.status_word)
             drafts.append(tok)
         rows = torch.stack(hs, 1).reshape(n_live * K, -1)                # sequence after sequence
         h = self.layers(self.split, self.s.n_layers, rows, self.lens, None if start is None else start * K, K)
@@ -258,9 +268,9 @@ class PagedDecoder:
             out = torch.where(torch.arange(K, device=self.device) < m[:, None], t, y)
         else:
             q = torch.stack(drawn_from, 1).view(n_live * K, -1)
-            out, n, m = verify_drafts(sampling.probs(self.verifier_logits(h)), t.view(-1),
+            out, n, m = verify_drafts(sampling.probs(self.verifier_logits(h), self.status_word), t.view(-1),
                                       sampling.uniform(n_live * K, self.device), sampling.uniform(n_live, self.device),
-                                      draft=q, max_drafts=K, bonus=False)
+                                      draft=q, max_drafts=K, bonus=False, status=self.status_word)
             n, m = n.long(), m.long()
         new_pending = out.gather(1, (n - 1).clamp_min(0).long()[:, None]).squeeze(1)
         n = self._spread(at, n)
@@ -325,8 +335,7 @@ def run(workload_name: str, fmt: str, n_gen: int, page_tokens: int, batch: int, 
     if temperature is not None:
         sampling = Sampling(temperature, top_k, top_p, torch.Generator(device="cuda").manual_seed(seed))
     tokens, mat = dec.generate(prompts, n_gen, sampling=sampling)
-    flags = sorted({f for c in [*dec.caches, *([dec.pool] if dec.pool else [])] for f in c.status()})
-    return dict(workload=w.name, fmt=fmt, page_tokens=page_tokens, mean_accepted=mat, device_flags=flags,
+    return dict(workload=w.name, fmt=fmt, page_tokens=page_tokens, mean_accepted=mat, device_flags=dec.status(),
                 pages_in_use=dec.pages_in_use(), tokens=[t[:8] for t in tokens])
 
 
