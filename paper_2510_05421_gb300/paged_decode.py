@@ -182,7 +182,8 @@ class PagedDecoder:
         return _linear(self.w.lm_head, self._norm(h, self.w.final_norm))
 
     def embed(self, tokens: torch.Tensor):
-        return self.w.embed[tokens.long()].float()
+        # (a draft that is none, -1, stands for token 0: it is rejected, and no row behind it counts)
+        return self.w.embed[tokens.long().clamp_min(0)].float()
 
     # -- calls ------------------------------------------------------------
     def prefill(self, prompts: Sequence[np.ndarray], sampling: Optional[Sampling] = None) -> torch.Tensor:
@@ -216,6 +217,12 @@ class PagedDecoder:
         if min(got, default=0) < 0:
             raise RuntimeError(f"{what}: no token has a probability above 0 (logits that are no numbers)")
 
+    @staticmethod
+    def _has_token(what: str, pending: torch.Tensor):
+        """Refuses a pending token of -1 (waits for the device)."""
+        if bool((pending < 0).any()):
+            raise ValueError(f"{what}: a sequence that takes part has no pending token")
+
     def _taking_part(self, live: Optional[Sequence[int]]):
         """The sequences of a pass (by default those that hold rows), where they lie in tensors of all sequences and
         the row starts of one row each; both None where every sequence takes part."""
@@ -239,15 +246,17 @@ class PagedDecoder:
         the sequences in `live` (by default those that hold rows: a released one takes none).  With `sampling` the drafts
         are drawn from the drafter's probabilities and verified against the model's.
         Returns (committed tokens [B, K], how many of them, how many drafts agreed, the new pending tokens); the
-        sequences that took no part have 0 of them and their pending token as it was."""
+        sequences that took no part have 0 of them and their pending token as it was.  One that takes part without a
+        pending token (-1) is a ValueError."""
         live, at, start = self._taking_part(live)
         n_live, K = len(live), self.K
         if n_live == 0:
             none = torch.zeros(len(self.host_lens), dtype=torch.long, device=self.device)
             return torch.zeros(len(none), K, dtype=torch.int32, device=self.device), none, none.clone(), pending
+        tok = pending if at is None else pending[at]
+        self._has_token("step", tok)
         self.reserve([K if b in live else 0 for b in range(len(self.host_lens))])
         hs, drafts, drawn_from = [], [], []
-        tok = pending if at is None else pending[at]
         for j in range(K):
             h = self.layers(0, self.split, self.embed(tok), self.lens + j, start, 1)
             hs.append(h)
@@ -282,13 +291,14 @@ class PagedDecoder:
     def ar_step(self, pending: torch.Tensor, live: Optional[Sequence[int]] = None,
                 sampling: Optional[Sampling] = None) -> torch.Tensor:
         """One greedy (or sampled) token of the whole model for the sequences in `live` (by default those that hold rows);
-        the others' pending tokens stay."""
+        the others' pending tokens stay.  One that takes part without a pending token (-1) is a ValueError."""
         live, at, start = self._taking_part(live)
         if not live:
             return pending
+        tok = pending if at is None else pending[at]
+        self._has_token("ar_step", tok)
         takes = [int(b in live) for b in range(len(self.host_lens))]
         self.reserve(takes)
-        tok = pending if at is None else pending[at]
         h = self.layers(0, self.s.n_layers, self.embed(tok), self.lens, start, 1)
         self.advance(takes)
         return self._spread(at, self._choose(self.verifier_logits(h), sampling), pending)
