@@ -88,6 +88,7 @@ class PagedDecoder:
         self.held: List[List[int]] = [[] for _ in range(max_seqs)]
         self.host_lens = [0] * max_seqs
         self.max_seq_len = max_seq_len
+        self.reserved = [0] * max_seqs      # positions that reserve() has pages for (with device_pages)
         width = -(-max_seq_len // page_tokens)
         if device_pages:
             self.pool = PagePool.create(n_pages, max_seqs, width, page_tokens, device)
@@ -107,7 +108,14 @@ class PagedDecoder:
 
     # -- pages ------------------------------------------------------------
     def reserve(self, rows: Sequence[int]):
-        """Pages for rows[b] more positions of each sequence."""
+        """Pages for rows[b] more positions of each sequence.  They stay its own, whatever calls come before its rows do,
+        until release(b)."""
+        self._hold(rows)
+        if self.pool is not None:
+            self.reserved = [max(r, len_ + n) for r, len_, n in zip(self.reserved, self.host_lens, rows)]
+
+    def _hold(self, rows: Sequence[int]):
+        """The same for the pass that follows at once."""
         if self.pool is not None:
             self._plan(rows)
             return
@@ -125,20 +133,23 @@ class PagedDecoder:
             self.held[b] += new
 
     def _plan(self, rows: Sequence[int]):
-        """The same on the GPU: what the plan will find follows from the lengths, without a look at the device."""
-        after = [len_ + n for len_, n in zip(self.host_lens, rows)]
-        if max(after) > self.max_seq_len:
+        """The same on the GPU: what the plan will find follows from the lengths, without a look at the device.  A plan
+        brings every sequence to its rows, so those that are reserved are among them."""
+        if max(len_ + n for len_, n in zip(self.host_lens, rows)) > self.max_seq_len:
             raise RuntimeError("a sequence would outgrow max_seq_len")
+        after = [max(r, len_ + n) for r, len_, n in zip(self.reserved, self.host_lens, rows)]
         if sum(-(-n // self.P) for n in after) > self.pool.n_pages:
             raise RuntimeError("out of pages")
-        self.pool.plan(self.lens, torch.tensor(list(rows), dtype=torch.int32).to(self.device))
+        more = [n - len_ for n, len_ in zip(after, self.host_lens)]
+        self.pool.plan(self.lens, torch.tensor(more, dtype=torch.int32).to(self.device))
 
     def release(self, b: int):
         """Sequence b is over: its pages go back."""
         self.host_lens[b] = 0
         self.lens[b] = 0
         if self.pool is not None:
-            self.pool.trim(self.lens)
+            self.reserved[b] = 0
+            self._plan([0] * len(self.host_lens))
             return
         self.free += self.held[b]
         self.held[b] = []
@@ -195,7 +206,7 @@ class PagedDecoder:
         rows = [len(p) for p in prompts]
         if not any(rows):
             return torch.full((len(rows),), -1, dtype=torch.int32, device=self.device)
-        self.reserve(rows)
+        self._hold(rows)
         start = np.concatenate([[0], np.cumsum(rows)]).astype(np.int32)
         row_start = torch.from_numpy(start).to(self.device)
         tokens = torch.from_numpy(np.concatenate(prompts).astype(np.int32)).to(self.device)
@@ -255,7 +266,7 @@ class PagedDecoder:
             return torch.zeros(len(none), K, dtype=torch.int32, device=self.device), none, none.clone(), pending
         tok = pending if at is None else pending[at]
         self._has_token("step", tok)
-        self.reserve([K if b in live else 0 for b in range(len(self.host_lens))])
+        self._hold([K if b in live else 0 for b in range(len(self.host_lens))])
         hs, drafts, drawn_from = [], [], []
         for j in range(K):
             h = self.layers(0, self.split, self.embed(tok), self.lens + j, start, 1)
@@ -298,7 +309,7 @@ class PagedDecoder:
         tok = pending if at is None else pending[at]
         self._has_token("ar_step", tok)
         takes = [int(b in live) for b in range(len(self.host_lens))]
-        self.reserve(takes)
+        self._hold(takes)
         h = self.layers(0, self.s.n_layers, self.embed(tok), self.lens, start, 1)
         self.advance(takes)
         return self._spread(at, self._choose(self.verifier_logits(h), sampling), pending)
