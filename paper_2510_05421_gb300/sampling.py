@@ -56,12 +56,16 @@ def token_probs(logits: torch.Tensor, temperature: Union[float, torch.Tensor] = 
     Settings are numbers or tensors with one for each row (f32, int32, f32 [n]).  NaN logits count as -inf, +inf as
     the largest number; status (int32 [1], or None) gets DVI_DEV_NONFINITE then, and DVI_DEV_TIMEOUT where a bounded wait
     of the device ran out, whose row gets zeros.  `out` may be the logits (f32); one that
-    overlaps them in another way is refused.  No gradient passes through."""
+    overlaps them in another way is refused.  No gradient passes through; that `out` was written in place is known to
+    autograd, which refuses a backward pass that has saved what it held."""
     index = _device_of("token_probs: logits", logits)
     if stream is not None or _current() != index:
         return elsewhere(index, stream, (), token_probs, (logits, temperature, top_k, top_p, out, status),
                          "the logits' device")
-    return (_calls or _module()).probs(logits, temperature, top_k, top_p, out, status, _raw_stream(index))
+    got = (_calls or _module()).probs(logits, temperature, top_k, top_p, out, status, _raw_stream(index))
+    if out is not None and not out.is_inference():
+        torch.autograd.graph.increment_version(out)
+    return got
 
 
 def verify_drafts(target: torch.Tensor, draft_ids: torch.Tensor, u_accept: torch.Tensor, u_token: torch.Tensor,
