@@ -84,7 +84,44 @@ static PyObject* result(const char* what, dvi_status rc, PyObject* out) {
   return NULL;
 }
 
-static int is_number(PyObject* o) { return PyFloat_Check(o) || PyLong_Check(o); }
+/* A number, and a whole one (past 64 bits: the nearest), of any type that says it is one: numpy's scalars are not
+ * Python's numbers. */
+static int not_a_number(const char* what) {
+  if (PyErr_ExceptionMatches(PyExc_TypeError) || PyErr_ExceptionMatches(PyExc_ValueError) ||
+      PyErr_ExceptionMatches(PyExc_OverflowError)) {
+    PyErr_Clear();
+    refuse(what, "not a number that it may be");
+  }
+  return 0;
+}
+static int number_of(const char* what, PyObject* o, double* v) {
+  *v = PyFloat_AsDouble(o);
+  return !(*v == -1.0 && PyErr_Occurred()) || not_a_number(what);
+}
+static int whole_of(const char* what, PyObject* o, int64_t* v) {
+  PyObject* i = PyNumber_Index(o);
+  if (!i) return not_a_number(what);
+  int past;
+  *v = PyLong_AsLongLongAndOverflow(i, &past);
+  Py_DECREF(i);
+  if (past) *v = past > 0 ? INT64_MAX : INT64_MIN;
+  return 1;
+}
+/* Whether a setting is a number (1) or a contiguous array [n] of `dtype`, one for each row (2); 0: refused.  Python's
+ * own numbers first, then tensors: the others are found by not being one. */
+static int setting_of(const char* what, PyObject* o, PyObject* dtype, int64_t n, int64_t device, uintptr_t* ptr) {
+  if (dtype == g_f32 ? PyFloat_Check(o) || PyLong_Check(o) : PyLong_Check(o)) return 1;
+  Tensor t;
+  if (look(o, what, &t)) {
+    *ptr = t.ptr;
+    return is_array(what, &t, dtype, n, device) ? 2 : 0;
+  }
+  if (!PyErr_ExceptionMatches(PyExc_AttributeError)) return 0;
+  PyErr_Clear();
+  const PyNumberMethods* m = Py_TYPE(o)->tp_as_number;
+  if (m && (m->nb_index || (dtype == g_f32 && m->nb_float))) return 1;
+  return refuse(what, dtype == g_f32 ? "must be a number or a tensor" : "must be a whole number or a tensor");
+}
 
 /* A device status word, or None. */
 static int status_of(const char* what, PyObject* o, int64_t device, int32_t** out) {
@@ -117,43 +154,39 @@ static PyObject* py_probs(PyObject* self, PyObject* const* a, Py_ssize_t n_args)
   uintptr_t out, p = 0;
   int64_t ld_out;
   dvi_sampling s = {NULL, NULL, NULL, 0.f, 0, 0.f};
-  if (is_number(a[1])) {
-    const double v = PyFloat_AsDouble(a[1]);
-    if (PyErr_Occurred()) return NULL;
+  double v;
+  int64_t k;
+  int kind = setting_of("token_probs: temperature", a[1], g_f32, n, t.device, &p);
+  if (!kind || (kind == 1 && !number_of("token_probs: temperature", a[1], &v))) return NULL;
+  if (kind == 1) {
     if (!(v >= 0.0)) {
       refuse("token_probs", "temperature must be at least 0");
       return NULL;
     }
     /* (a temperature above 0 stays above it in f32) */
     s.temperature_all = v > 0.0 && v < 1e-37 ? 1e-37f : (float)v;
-  } else if (!array_of("token_probs: temperature", a[1], g_f32, n, t.device, &p)) {
-    return NULL;
   }
   s.temperature = (const float*)p;
   p = 0;
-  if (PyLong_Check(a[2])) {
-    const int64_t v = PyLong_AsLongLong(a[2]);
-    if (PyErr_Occurred()) return NULL;
-    if (v < 0) {
+  kind = setting_of("token_probs: top_k", a[2], g_i32, n, t.device, &p);
+  if (!kind || (kind == 1 && !whole_of("token_probs: top_k", a[2], &k))) return NULL;
+  if (kind == 1) {
+    if (k < 0) {
       refuse("token_probs", "top_k must not be negative");
       return NULL;
     }
-    s.top_k_all = v > MAX_VOCAB ? MAX_VOCAB : (int)v;
-  } else if (!array_of("token_probs: top_k", a[2], g_i32, n, t.device, &p)) {
-    return NULL;
+    s.top_k_all = k > MAX_VOCAB ? MAX_VOCAB : (int)k;
   }
   s.top_k = (const int32_t*)p;
   p = 0;
-  if (is_number(a[3])) {
-    const double v = PyFloat_AsDouble(a[3]);
-    if (PyErr_Occurred()) return NULL;
+  kind = setting_of("token_probs: top_p", a[3], g_f32, n, t.device, &p);
+  if (!kind || (kind == 1 && !number_of("token_probs: top_p", a[3], &v))) return NULL;
+  if (kind == 1) {
     if (!(v >= 0.0)) {
       refuse("token_probs", "top_p must be at least 0");
       return NULL;
     }
     s.top_p_all = (float)v;
-  } else if (!array_of("token_probs: top_p", a[3], g_f32, n, t.device, &p)) {
-    return NULL;
   }
   s.top_p = (const float*)p;
   int32_t* status;
@@ -223,8 +256,8 @@ static PyObject* py_verify(PyObject* self, PyObject* const* a, Py_ssize_t n_args
     return NULL;
   }
   if (a[6] != Py_None) {
-    const int64_t m = PyLong_AsLongLong(a[6]);
-    if (PyErr_Occurred()) return NULL;
+    int64_t m;
+    if (!whole_of("verify_drafts: max_drafts", a[6], &m)) return NULL;
     if (m < 0 || (a[5] == Py_None && m < most)) {
       refuse("verify_drafts", "max_drafts must not be negative, nor below the drafts of each sequence");
       return NULL;
@@ -279,19 +312,16 @@ static PyObject* py_plan(PyObject* self, PyObject* const* a, Py_ssize_t n_args) 
   int64_t each = 0, n_rows = 0;
   uintptr_t lens, rows = 0, at[3] = {0, 0, 0};
   if (!array_of("plan: lens", a[2], g_i32, B, device, &lens)) return NULL;
-  if (PyLong_Check(a[3])) {
-    each = PyLong_AsLongLong(a[3]);
-    if (PyErr_Occurred()) return NULL;
+  const int kind = setting_of("plan: rows", a[3], g_i32, B, device, &rows);
+  if (!kind || (kind == 1 && !whole_of("plan: rows", a[3], &each))) return NULL;
+  if (kind == 1) {
     if (each < 0 || each > (1 << 30)) {
       refuse("plan", "rows must be 0 to 2^30");
       return NULL;
     }
-  } else if (!array_of("plan: rows", a[3], g_i32, B, device, &rows)) {
-    return NULL;
   }
   if (a[4] != Py_None) {
-    n_rows = PyLong_AsLongLong(a[4]);
-    if (PyErr_Occurred()) return NULL;
+    if (!whole_of("plan: n_rows", a[4], &n_rows)) return NULL;
     if (n_rows < 0 || n_rows > (1 << 30)) {
       refuse("plan", "n_rows must be 0 to 2^30");
       return NULL;

@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes
+import operator
 from typing import NamedTuple, Optional, Union
 
 import torch
@@ -41,6 +42,7 @@ class PagePool:
 
     def __init__(self, stack: torch.Tensor, n_free: torch.Tensor, table: torch.Tensor, held: torch.Tensor,
                  page_tokens: int = 64):
+        page_tokens = operator.index(page_tokens)
         if page_tokens not in (16, 32, 64, 128):
             raise ValueError("PagePool: pages of 16, 32, 64 or 128 tokens")
         for t, dims in ((stack, 1), (n_free, 1), (table, 2), (held, 1)):
