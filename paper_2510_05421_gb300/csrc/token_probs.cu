@@ -3,8 +3,10 @@
 // The CTAs of a cluster hold a row between them in registers, so it is read once, and
 // every warp gives (its maximum, its sum of exp2) to all of them once.
 //
-// Bound by memory and that exchange: 576 rows of 32000 f32 logits (147 MB) take 29 us
-// (5.0 TB/s), of which the exchange is 5.5, a copy of them 23 us.  32
+// Bound by memory and that exchange: 576 rows of 32000 f32 logits (147 MB) take 30 us
+// (4.9 TB/s), of which the exchange is 5.5, a copy of them 23 us; of bf16 logits (110 MB), whose
+// 16 bytes a lane are 32 bytes of probabilities in two stores, 31.  (Of the 64 registers a thread that
+// leave room for four CTAs some 80 bytes more are spilled.)  32
 // logits a thread and four CTAs of 256 threads an SM: 16 a thread 34 us, 64 a thread 37,
 // clusters that take row after row with the next one's loads under way 32, a row a CTA
 // with the next one's bulk copy under way 35.
@@ -71,7 +73,7 @@ __global__ void __launch_bounds__(THREADS, CTAS_AN_SM)
   }
   const Settings set(a, r);
   const bool greedy = set.temperature == 0.f;
-  const Slope c(set.temperature);
+  const Slope c = Slope(set.temperature).below();
   bool bad = set.bad;
   float m = -INFINITY;
   bool odd = false;   // NaN or +inf among them

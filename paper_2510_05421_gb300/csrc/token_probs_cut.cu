@@ -919,13 +919,14 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
     if (upto.lost()) return nothing(false);
     inv = 1.f / (__ull2float_rn(kept) * 0x1p-44f);
   } else {
+    const Slope below = c.below();
     float sum = 0.f;
     for (int g = tid; g < n4; g += kThreads) {
       const float4 q = x4[g];
       const float v[4] = {q.x, q.y, q.z, q.w};
       if (!__any_sync(0xffffffffu, fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) >= upto.x)) continue;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum += upto.has(v[e], 4 * g + e) ? weight(v[e], top, c) : 0.f;
+      for (int e = 0; e < 4; ++e) sum += upto.has(v[e], 4 * g + e) ? weight(v[e], top, below) : 0.f;
     }
     sum = warp_sum(sum);
     if (lane == 0) s.red[warp] = sum;
@@ -941,7 +942,8 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
     inv = 1.f / sum;
   }
   arrive_at_last(n_ctas);
-  auto prob = [&](float v, int i) { return upto.has(v, i) ? weight(v, top, c) * inv : 0.f; };
+  const Slope below = c.below();
+  auto prob = [&](float v, int i) { return upto.has(v, i) ? weight(v, top, below) * inv : 0.f; };
   // (most tokens are cut off, mostly whole warps of them)
   if (WIDE) {
     for (int g = tid; g < n4; g += kThreads) {

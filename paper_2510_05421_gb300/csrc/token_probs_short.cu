@@ -243,10 +243,11 @@ __global__ void __launch_bounds__(THREADS, CTAS_AN_SM) token_probs_short_kernel(
   unsigned long long kept = all.sum;
   if (set.top_p < 1.f)
     kept = cut_after<true, THREADS>(o, mass, share_of(set.top_p, kept), all, least, ord(top), turns);
+  const Slope below = c.below();
   const float inv = 1.f / (__ull2float_rn(kept) * 0x1p-44f);
 #pragma unroll
   for (int j = 0; j < NV; ++j)
-    if (j * THREADS + tid < n) out[j * THREADS + tid] = o[j] ? weight(x[j], top, c) * inv : 0.f;
+    if (j * THREADS + tid < n) out[j * THREADS + tid] = o[j] ? weight(x[j], top, below) * inv : 0.f;
 }
 
 template <typename T, int NV, int THREADS, int CTAS_AN_SM>
