@@ -503,7 +503,7 @@ typedef struct {
  * gets zeros.
  *
  * Which tokens stay is decided on w as whole multiples of 2^-44 of the row's largest
- * (off by less than one of them, and by 2^-33 of themselves), so it does not depend on the
+ * (off by less than one of them, and by less than 2^-31 of themselves), so it does not depend on the
  * order of any sum.  NaN logits count as -inf and +inf as the largest finite number
  * (DVI_DEV_NONFINITE).  Of settings in device arrays, T that is negative or NaN counts
  * as 0, top_k below 0 as 0, top_p NaN as 1 (NaN: DVI_DEV_NONFINITE).  d_probs may be

@@ -35,12 +35,16 @@ constexpr Powers make_powers() {
 }
 __device__ const Powers kPowersOf2 = make_powers();
 
-// w in units of 2^-44, off by 2^-33 of itself at most (found: 2^-33.05); 0 below 2^-46 (low: where that is, or above).
+// w in units of 2^-44, off by less than 2^-31 of itself; 0 below 2^-46 (low: where that is, or above).
 // t = (x - m) c is x c less m c.  Adding 1.5 * 2^23 / kPowers rounds x c to multiples q of 1 / kPowers and
 // leaves them in the low bits; the rest x c - q is one number, as a fused multiply-add rounds only what is
 // left.  (|x c| stays below 4096: where |m c| does not, what counts is so near to m that x - m is exact and
 // takes x's place.)  The rest of m c is in the table, turned by m's own q: 2^q from the table and an
 // exponent, 2^u - 1 = u ln 2 + ... is small enough for one number.  w in 22 bits, then 22 more.
+// What it is off by: u, below 3 2^-11, is rounded in six places, by 6 2^-35 together, 4.2 2^-35 of w; the cubic's
+// coefficient and two roundings are 2.3 2^-24 of 2^u - 1 < 2^-9.9, 4.6 2^-35: 2^-31.8 if all went one way (found among
+// 70 million: 2^-32.97, in the mean of a row 2^-35.6).  That is chosen: u and 2^u - 1 as two numbers each would take
+// more instructions in the sums that many rows are bound by.
 // Two numbers are weighed together: an operation on a register pair is one instruction.
 struct Two {
   unsigned long long v;

@@ -6,7 +6,7 @@
 // Bound by memory and that exchange: 576 rows of 32000 f32 logits (147 MB) take 30 us
 // (4.9 TB/s), of which the exchange is 5.5, a copy of them 23 us; of bf16 logits (110 MB), whose
 // 16 bytes a lane are 32 bytes of probabilities in two stores, 31.  (Of the 64 registers a thread that
-// leave room for four CTAs some 80 bytes more are spilled.)  32
+// leave room for four CTAs some 70 bytes are spilled.)  32
 // logits a thread and four CTAs of 256 threads an SM: 16 a thread 34 us, 64 a thread 37,
 // clusters that take row after row with the next one's loads under way 32, a row a CTA
 // with the next one's bulk copy under way 35.

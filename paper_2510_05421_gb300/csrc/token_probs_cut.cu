@@ -23,12 +23,15 @@
 // 32000 with top_p: 14.3 us with the cluster's, 12.2 so).
 //
 // A few rows are bound by the chain of four exchanges and by code that is read for the
-// first time (a third of the stalls): 6 rows of 32000 with top_p 10.9 us, 48 with top_k
-// 50 12.2.  Many rows: of a CTA's time on a slice of 16000 tokens with top_p (50000 cycles) the
+// first time (a third of the stalls): 6 rows of 32000 with top_p 11.2 us, 48 with top_k
+// 50 12.7.  Many rows: of a CTA's time on a slice of 16000 tokens with top_p (50000 cycles) the
 // exact sums take 14000 (instructions, and conflicts in the table of powers), the histogram 8000 (its
 // atomics), the loads 6000, the stores 6000, and the exchanges between them the rest; with top_k 30000
-// in all: 576 rows of 32000 105 and 63 us (a copy of them 23), 64 rows of 128001 with settings of their
-// own 57 to 66 (17).
+// in all: 576 rows of 32000 108 and 65 us (a copy of them 23), 64 rows of 128001 with settings of their
+// own 58 to 67 (17).  Further from a copy: flat rows, where a bin has too many tokens and the next try weighs
+// all tokens again (64 rows of 128001 with T = 3 and top_p 0.9 104 us, with T = 1 71); top_k above 512, where
+// all tokens down to the least of the threads' maxima are counted (576 rows of 32000, 900 likeliest, 123); short
+// rows, which have as many barriers and as large a table as long ones (2000 of 4000 with top_p 77, without cuts 12.5).
 #include "token_mass.cuh"
 
 namespace dvi {
@@ -976,8 +979,8 @@ __global__ void __launch_bounds__(kThreads, 2) token_probs_cut_kernel(TokenProbs
 constexpr int kSlice = 16384;   // logits of a CTA where its row may have up to kMaxCtas: two CTAs an SM
 
 // As few CTAs as hold a row in slices, and more while there are fewer than SMs (152) and the slices are
-// worth it: 6 rows of 32000 with top_p over 8 CTAs 10.9 us, over 4 12.7, over 2 17.1; 48 rows over 4 18.1, over
-// 2 18.8, over 8 (more than are resident) 26.5.
+// worth it: 6 rows of 32000 with top_p over 8 CTAs 11.2 us, over 4 13.0, over 2 17.4; 48 rows over 4 18.0, over
+// 2 20.4, over 8 (more than are resident) 25.8.
 template <typename T, How HOW>
 cudaError_t launch_cut(const TokenProbsArgs& a, cudaStream_t s) {
   static PerDevice per_device;

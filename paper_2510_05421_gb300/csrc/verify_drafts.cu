@@ -10,7 +10,7 @@
 // (64-bit floating point is as slow here as a hundred of the other operations).
 //
 // Bound by memory where there is much of it: 128 sequences of 128001 tokens (two rows
-// each, 131 MB) take 30 us, a dot product of them 27; of these 5 are the looks at the
+// each, 131 MB) take 31 to 33 us, a dot product of them 27; 5 are the looks at the
 // drafts and the search.  One sequence takes 6.7 us, a chain of five dependent loads.
 // Copies by the bulk engine, 1 KB a warp and three ahead, took 48 us; the next numbers'
 // loads under way in registers changed nothing.
